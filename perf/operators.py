@@ -110,6 +110,11 @@ def _vector(gen, n, mean, scale):
     return torch.randn(n, generator=gen, device="cuda", dtype=torch.float32).mul_(scale).add_(mean)
 
 
+def _power(e):
+    """2^e as float32, exactly, for whole -126 <= e <= 127."""
+    return ((e + 127) << 23).view(torch.float32)
+
+
 def _to_codes(x):
     """The 8-bit form of x (rows x cols) as two byte tensors: the codes and the exponents."""
     rows, cols = x.shape
@@ -122,8 +127,8 @@ def _to_codes(x):
     top = torch.where(finite, top, torch.zeros_like(top))
     e = torch.frexp(top)[1] - 7                                   # 64 <= top / 2^e < 128
     e = torch.where(top == 0, torch.full_like(e, -126), e).clamp_(min=-126)
-    e = e + (torch.round(torch.ldexp(top, -e)) > 127)
-    mag = torch.round(torch.ldexp(v.abs(), -e)).to(torch.uint8)
+    e = e + (torch.round(top * _power(-e)) > 127)
+    mag = torch.round(v.abs() * _power(-e)).to(torch.uint8)
     codes = torch.where(v < 0, mag + 128, mag).view(rows, -1)[:, :cols].contiguous()
     exps = torch.where(finite, e + 126, torch.full_like(e, 255)).to(torch.uint8).view(rows, groups)
     return codes, exps
@@ -135,7 +140,7 @@ def _from_codes(codes, exps):
     e = exps.to(torch.int32).unsqueeze(2)
     v = torch.nn.functional.pad(codes, (0, -cols % GROUP)).view(rows, -1, GROUP)
     mag = (v & 127).float()
-    v = torch.ldexp(torch.where(v >= 128, -mag, mag), e - 126)
+    v = torch.where(v >= 128, -mag, mag) * _power(e.clamp(max=248) - 126)
     v = torch.where(e == 255, torch.full_like(v, math.nan), v)
     return v.view(rows, -1)[:, :cols].contiguous()
 
@@ -332,16 +337,15 @@ def _kept64(x):
     rows, cols = x.shape
     v = torch.nn.functional.pad(x.double(), (0, -cols % GROUP)).reshape(rows, -1, GROUP)
     top = v.abs().max(dim=2, keepdim=True).values
-    step = torch.exp2(torch.floor(torch.log2(top.clamp(min=1e-300))) - 6)
-    step = torch.where(top / step >= 128, step * 2, torch.where(top / step < 64, step / 2, step))   # log2 may be one off
-    step = torch.where(top / step > 127.5, step * 2, step)
-    step = torch.where(top / step == 127.5, step * 2, step).clamp(min=2.0 ** -126)
+    half = torch.frexp(top.clamp(min=1e-300))[1].long() - 1                                # 2^half <= top < 2^(half + 1)
+    step = ((half - 6 + 1023) << 52).view(torch.float64)
+    step = torch.where(top / step >= 127.5, step * 2, step).clamp(min=2.0 ** -126)
     return (torch.round(v / step) * step).reshape(rows, -1)[:, :cols]
 
 
 def _decode64(codes, exps):
-    e = exps.double().repeat_interleave(GROUP, dim=1)[:, :codes.shape[1]] - 126
-    return (codes.bitwise_and(127).double() * torch.exp2(e)) * (1 - 2 * (codes >> 7).double())
+    e = exps.long().repeat_interleave(GROUP, dim=1)[:, :codes.shape[1]] - 126
+    return codes.bitwise_and(127).double() * ((e + 1023) << 52).view(torch.float64) * (1 - 2 * (codes >> 7).double())
 
 
 def exact(case, seed):
