@@ -403,6 +403,125 @@ int lqsgd_launches_per_step(const lqsgd_ctx* ctx, int32_t* host_out);
 int lqsgd_orthonormalize_noalloc(const float* dev_p_in, float* dev_p_out, int32_t rows, int32_t rank,
                                  uint32_t* dev_status_out, void* cuda_stream);
 
+/* ---- Training operators: what makes the gradients that a round compresses. ----
+ * A data-parallel step runs a forward pass, keeps activations until the backward pass, and hands lqsgd_step one
+ * fp32 weight gradient per layer and worker.  These calls are the layers of such a step: linear layers whose bias,
+ * activation and residual are applied in the matrix product's epilogue, group norms with an activation on
+ * channels-last tensors, and both with their activations kept in 8 bits in between.
+ *
+ * They hold no state: every call takes its tensors, enqueues its kernels on cuda_stream of the current device and
+ * returns.  Matrices are row-major with unit stride along a row; every "ld" is the distance between two rows in
+ * elements, >= the row length (any value: rows that are not 16-byte aligned cost an aligned copy in the workspace or
+ * narrower accesses).  Base pointers are aligned to their element.  Outputs must not overlap inputs, except where a
+ * call says so.  A call on zero rows writes what an empty sum gives (zeros in weight and bias gradients) and nothing else.
+ * Workspaces: device memory, 16-byte aligned, of the size the matching *_workspace_bytes reports (0: may be NULL); it
+ * may be reused by the next call on the same stream.  All sums are taken in fp32 in an order fixed by the sizes alone:
+ * the same call gives the same bits.  The calls may be captured in CUDA graphs. */
+typedef enum lqsgd_dtype { LQSGD_BF16 = 0, LQSGD_F16 = 1, LQSGD_F32 = 2 } lqsgd_dtype;
+typedef enum lqsgd_act {
+  LQSGD_ACT_NONE = 0,
+  LQSGD_ACT_RELU = 1, /* max(z, 0); slope 0 at z = 0; NaN stays NaN */
+  LQSGD_ACT_GELU = 2, /* z Phi(z), Phi the normal distribution function (erf) */
+  LQSGD_ACT_SILU = 3  /* z / (1 + e^-z) */
+} lqsgd_act;
+
+/* A rows x cols matrix kept in 8 bits.  Each row is cut into groups of 32 columns (the last may be shorter).  A group
+ * has one step 2^e, e the smallest integer >= -126 with rint(max |x| / 2^e) <= 127, stored as the byte e + 126; a value
+ * is one byte in the form of the round's codes: the sign bit of x on top, below it the magnitude rint(|x| / 2^e)
+ * (halves to even).  |x - decoded| <= 2^e / 2, i.e. at most 1/127 of the group's largest |x| (half of that on average
+ * over its range).  Steps are powers of two so that every decoded value is exact in bf16 (8 significant bits): the
+ * weight gradient multiplies exactly what was kept.  A group with a value that is not finite has the byte 255 and
+ * decodes to NaN throughout, so that an overflow is not lost.  Decoding into a type whose range is exceeded
+ * gives its largest finite value.  1 + 1/32 bytes per value. */
+#define LQSGD_PACK8_GROUP 32
+typedef struct lqsgd_packed8 {
+  uint8_t* dev_codes; /* rows x cols */
+  int64_t ld_codes;   /* bytes between rows, >= cols; a multiple of 16 (and a 16-byte aligned base) is read fastest */
+  uint8_t* dev_exps;  /* rows x ceil(cols / 32) */
+  int64_t ld_exps;    /* bytes between rows, >= ceil(cols / 32) */
+} lqsgd_packed8;
+
+int lqsgd_pack8(const void* dev_x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols,
+                const lqsgd_packed8* host_out, void* cuda_stream);
+int lqsgd_unpack8(const lqsgd_packed8* host_in, int64_t rows, int32_t cols, void* dev_y, int64_t ld_y, int32_t dtype,
+                  void* cuda_stream);
+
+/* dz = dy * act'(z) and db = the column sums of dz (before its rounding to dtype), z decoded from its 8-bit form.
+ * With LQSGD_ACT_NONE host_z8 and dev_dz may be NULL (dz is dy).  dev_db (fp32, cols) may be NULL, but not both
+ * outputs.  dev_dz may be dev_dy with the same ld. */
+int lqsgd_act_grad_workspace_bytes(int64_t rows, int32_t cols, size_t* host_bytes_out);
+int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_packed8* host_z8, int32_t act, int32_t dtype,
+                   int64_t rows, int32_t cols, void* dev_dz, int64_t ld_dz, float* dev_db, void* dev_workspace,
+                   size_t workspace_bytes, void* cuda_stream);
+
+/* The three products of a linear layer, w of shape out x in (Section IV's n x m), on the tensor cores with fp32
+ * accumulators.  x, w, dz, residual, y, dx have one type, LQSGD_BF16 or LQSGD_F16; bias and dw are fp32.
+ *   lqsgd_linear_forward      y  = act(x w^T + bias) + residual     rows x out     bias, residual optional
+ *                             z8 = pack8(x w^T + bias), y8 = pack8(y as stored)    each optional (NULL codes)
+ *   lqsgd_linear_grad_input   dx = dz w + residual                  rows x in      residual: the skip connection's gradient
+ *   lqsgd_linear_grad_weight  dw = dz^T x  (or dw += dz^T x)        out x in       x from x8 when its codes are set
+ * Where few tiles would leave SMs idle the sum is cut in pieces whose partial results meet in the workspace.
+ * dev_status: NULL, or one device uint32 into which LQSGD_STATUS_TIMEOUT is ORed should a bounded device-side wait run
+ * out (the outputs are then undefined). */
+typedef struct lqsgd_linear {
+  uint32_t struct_size; /* sizeof(lqsgd_linear) */
+  int32_t dtype;        /* LQSGD_BF16 or LQSGD_F16 */
+  int32_t act;          /* forward only */
+  int32_t accumulate;   /* grad_weight only: 1 adds to dw, 0 overwrites it */
+  int64_t rows;         /* 0 .. 2^31 - 512 */
+  int32_t in, out;      /* 1 .. 2^24 */
+  const void* dev_x;    int64_t ld_x;      /* rows x in   (forward, grad_weight without x8) */
+  const void* dev_w;    int64_t ld_w;      /* out x in    (forward, grad_input) */
+  const void* dev_dz;   int64_t ld_dz;     /* rows x out  (grad_input, grad_weight) */
+  const float* dev_bias;                   /* out, fp32   (forward), or NULL */
+  const void* dev_residual; int64_t ld_residual; /* shaped like the output (forward, grad_input), or NULL; may be the output */
+  void* dev_out;        int64_t ld_out;    /* y, dx (dtype) or dw (fp32) */
+  lqsgd_packed8 x8;                        /* grad_weight input */
+  lqsgd_packed8 z8, y8;                    /* forward outputs */
+  uint32_t* dev_status;
+  void* dev_workspace;  size_t workspace_bytes;
+} lqsgd_linear;
+#define LQSGD_LINEAR_FORWARD 0
+#define LQSGD_LINEAR_GRAD_INPUT 1
+#define LQSGD_LINEAR_GRAD_WEIGHT 2
+/* Workspace of one of the three products for these arguments (sizes, strides and the presence and alignment of the
+ * pointers count; nothing is read through them). */
+int lqsgd_linear_workspace_bytes(int32_t product, const lqsgd_linear* host_args, size_t* host_bytes_out);
+int lqsgd_linear_forward(const lqsgd_linear* host_args, void* cuda_stream);
+int lqsgd_linear_grad_input(const lqsgd_linear* host_args, void* cuda_stream);
+int lqsgd_linear_grad_weight(const lqsgd_linear* host_args, void* cuda_stream);
+
+/* Group norm with an activation on channels-last tensors: n samples of hw pixels of c channels, the channels in
+ * `groups` equal groups.  With m and v the mean and the (biased) variance of a sample's group over its pixels and channels,
+ *   forward   rstd = 1 / sqrt(v + eps),  h = gamma (x - m) rstd + beta,  y = act(h)
+ *             x8 = pack8(x), y8 = pack8(y as stored), rows = pixels, each optional (NULL codes)
+ *   backward  dh = dy act'(h),  u = gamma dh,  xh = (x - m) rstd,  < > the mean over the group's values:
+ *             dx = rstd (u - <u> - xh <u xh>),  dgamma = sum of dh xh,  dbeta = sum of dh  over samples and pixels
+ * with x from x8 when its codes are set (its rows are the n * hw pixels), m and rstd as the forward call gave them. */
+typedef struct lqsgd_group_norm {
+  uint32_t struct_size; /* sizeof(lqsgd_group_norm) */
+  int32_t dtype;        /* of x, y, dy, dx: any lqsgd_dtype */
+  int32_t act;
+  int32_t groups;       /* divides c */
+  int32_t n, hw, c;     /* n >= 0, hw >= 1, c 1 .. 2^16 */
+  float eps;            /* forward only, > 0 */
+  const void* dev_x;    int64_t ld_x, sample_x;   /* elements between pixels and between samples */
+  const void* dev_dy;   int64_t ld_dy, sample_dy; /* backward */
+  void* dev_out;        int64_t ld_out, sample_out; /* y or dx */
+  const float* dev_gamma; /* c */
+  const float* dev_beta;  /* c */
+  float* dev_mean;      /* n x groups: written by the forward call, read by the backward call */
+  float* dev_rstd;      /* n x groups */
+  float* dev_dgamma;    /* c (backward) */
+  float* dev_dbeta;     /* c (backward) */
+  lqsgd_packed8 x8;     /* forward: output; backward: input instead of x */
+  lqsgd_packed8 y8;     /* forward: output */
+  void* dev_workspace;  size_t workspace_bytes;
+} lqsgd_group_norm;
+int lqsgd_group_norm_workspace_bytes(int32_t backward, const lqsgd_group_norm* host_args, size_t* host_bytes_out);
+int lqsgd_group_norm_forward(const lqsgd_group_norm* host_args, void* cuda_stream);
+int lqsgd_group_norm_backward(const lqsgd_group_norm* host_args, void* cuda_stream);
+
 /* Frees the host-side context.  The workspace stays the caller's. */
 void lqsgd_destroy(lqsgd_ctx* ctx);
 

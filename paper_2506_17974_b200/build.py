@@ -6,14 +6,16 @@ import shutil
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("lqsgd_kernels.cu", "lqsgd_api.cu", "lqsgd_noalloc.cu", "lqsgd_stream.cu", "lqsgd_tc.cu", "lqsgd_resident.cu", "lqsgd_stats.cu")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("lqsgd_kernels.cu", "lqsgd_api.cu", "lqsgd_noalloc.cu", "lqsgd_stream.cu", "lqsgd_tc.cu", "lqsgd_resident.cu", "lqsgd_stats.cu",
+                                                      "lqsgd_act8.cu", "lqsgd_norm.cu", "lqsgd_linear.cu")]
 HEADERS = [os.path.join(_HERE, "csrc", "lqsgd_dev.h"), os.path.join(_HERE, "csrc", "lqsgd_stream_common.cuh"),
            os.path.join(_HERE, "csrc", "lqsgd_factor.cuh"), os.path.join(_HERE, "csrc", "lqsgd_stats.h"),
+           os.path.join(_HERE, "csrc", "lqsgd_train.h"), os.path.join(_HERE, "csrc", "lqsgd_train_dev.cuh"), os.path.join(_HERE, "csrc", "lqsgd_linear_dev.cuh"),
            os.path.join(os.path.dirname(_HERE), "include", "lqsgd.h")]
 TARGET = os.path.join(_HERE, "liblqsgd.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-ldl"]
+              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-ldl", "--threads", "0"]
 
 
 def _nvcc() -> str:

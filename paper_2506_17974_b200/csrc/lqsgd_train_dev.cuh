@@ -1,0 +1,157 @@
+// Device helpers of the training operators: the 8-bit form of activations, the activations and their slopes,
+// and loads / stores of short runs of elements at any alignment.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "lqsgd_train.h"
+
+namespace lqsgd {
+namespace {
+
+constexpr int kGroup = LQSGD_PACK8_GROUP;
+constexpr int kExpBias = 126;            // stored exponent byte = e + 126
+constexpr int kExpNonFinite = 255;       // group with an infinity or a NaN
+
+__device__ __forceinline__ void train_pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void train_pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ---- element types
+template <int DT> struct Elem;
+template <> struct Elem<LQSGD_BF16> {
+  using T = __nv_bfloat16;
+  static __device__ __forceinline__ float up(T v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ T down(float v) { return __float2bfloat16_rn(v); }
+};
+template <> struct Elem<LQSGD_F16> {
+  using T = __half;
+  static __device__ __forceinline__ float up(T v) { return __half2float(v); }
+  static __device__ __forceinline__ T down(float v) { return __float2half_rn(v); }
+};
+template <> struct Elem<LQSGD_F32> {
+  using T = float;
+  static __device__ __forceinline__ float up(T v) { return v; }
+  static __device__ __forceinline__ T down(float v) { return v; }
+};
+
+// N consecutive elements as floats, and back.  VEC: the address is aligned to min(16, N * size) bytes and all N exist;
+// otherwise element by element, those from `have` on read as 0 / are not written.
+template <int DT, int N>
+__device__ __forceinline__ void load_run(const typename Elem<DT>::T* p, bool vec, int have, float (&v)[N]) {
+  using E = Elem<DT>;
+  constexpr int kBytes = N * (int)sizeof(typename E::T);
+  if (vec) {
+    if constexpr (kBytes % 16 == 0) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 w = *(reinterpret_cast<const uint4*>(p) + i);
+        constexpr int kPer = 16 / (int)sizeof(typename E::T);
+        const typename E::T* t = reinterpret_cast<const typename E::T*>(&w);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[i * kPer + j] = E::up(t[j]);
+      }
+    } else {
+      static_assert(kBytes == 8, "a run is 8 bytes or a multiple of 16");
+      const uint2 w = *reinterpret_cast<const uint2*>(p);
+      const typename E::T* t = reinterpret_cast<const typename E::T*>(&w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = E::up(t[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = j < have ? E::up(p[j]) : 0.f;
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void store_run(typename Elem<DT>::T* p, bool vec, int have, const float (&v)[N]) {
+  using E = Elem<DT>;
+  constexpr int kBytes = N * (int)sizeof(typename E::T);
+  if (vec) {
+    if constexpr (kBytes % 16 == 0) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        uint4 w;
+        constexpr int kPer = 16 / (int)sizeof(typename E::T);
+        typename E::T* t = reinterpret_cast<typename E::T*>(&w);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) t[j] = E::down(v[i * kPer + j]);
+        *(reinterpret_cast<uint4*>(p) + i) = w;
+      }
+    } else {
+      uint2 w;
+      typename E::T* t = reinterpret_cast<typename E::T*>(&w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) t[j] = E::down(v[j]);
+      *reinterpret_cast<uint2*>(p) = w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < have) p[j] = E::down(v[j]);
+  }
+}
+// Rounds to the element type and back: the value a later reader of the stored output sees.
+template <int DT> __device__ __forceinline__ float as_stored(float v) { return Elem<DT>::up(Elem<DT>::down(v)); }
+
+// ---- the 8-bit form
+// Exponent byte of a group whose largest magnitude is `top` (not negative; an infinity or NaN gives 255).
+// top = f 2^k with 1 <= f < 2: e = k - 6 puts top / 2^e into [64, 128), one more where that rounds to 128; never below -126
+// (then top / 2^e < 64, whatever top is, subnormal numbers included).
+__device__ __forceinline__ int exp_byte(float top) {
+  const uint32_t b = __float_as_uint(top);
+  if (b >= 0x7f800000u) return kExpNonFinite;
+  const int k = (int)(b >> 23) - 127;                                  // -127 for subnormal numbers and 0
+  const int e = max(k - 6, -126);
+  // top / 2^e >= 127.5 exactly when the significand is >= 127.5 / 64 = 1.9921875 (and e was not raised to -126)
+  const bool up = (b & 0x007fffffu) >= 0x007f0000u && k - 6 >= -126;
+  return e + (up ? 1 : 0) + kExpBias;
+}
+// 2^-e of an exponent byte as a float (e <= 122, so it is a normal number); 255 gives 0: the codes of such a group are 0.
+__device__ __forceinline__ float inv_step(int eb) {
+  return eb == kExpNonFinite ? 0.f : __uint_as_float((uint32_t)(127 + kExpBias - eb) << 23);
+}
+// 2^e as a float; NaN for 255.
+__device__ __forceinline__ float step_of(int eb) {
+  return eb == kExpNonFinite ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(eb + 127 - kExpBias) << 23);
+}
+// Low byte = rint(|x| * inv), halves to even (adding 1.5 * 2^23 leaves an integer in the significand; |x| * inv is
+// exact).  NaN and infinities only meet inv = 0; what they leave in the low byte is masked by the decoder's NaN step.
+__device__ __forceinline__ uint32_t mag_bits(float x, float inv) { return __float_as_uint(fmaf(fabsf(x), inv, 12582912.f)); }
+// Four codes in one word: magnitudes below, sign bits of the four values on top.
+__device__ __forceinline__ uint32_t code_word(float a, float b, float c, float d, float inv) {
+  const uint32_t m = __byte_perm(__byte_perm(mag_bits(a, inv), mag_bits(b, inv), 0x0040), __byte_perm(mag_bits(c, inv), mag_bits(d, inv), 0x0040), 0x5410);
+  const uint32_t s = __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0073), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0073), 0x5410);
+  return (m & 0x7f7f7f7fu) | (s & 0x80808080u);
+}
+__device__ __forceinline__ float decode8(uint32_t code, float step) {
+  const float m = (float)(code & 127u) * step;
+  const float sat = m > 3.402823466e38f ? 3.402823466e38f : m;          // a NaN stays
+  return __uint_as_float(__float_as_uint(sat) | ((code & 128u) << 24));
+}
+
+// ---- activations, all in fp32
+__device__ __forceinline__ float act_value(int act, float z) {
+  switch (act) {
+    case LQSGD_ACT_RELU: return z < 0.f ? 0.f : z;                       // keeps NaN
+    case LQSGD_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case LQSGD_ACT_SILU: return z / (1.f + expf(-z));
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+  switch (act) {
+    case LQSGD_ACT_RELU: return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);    // keeps NaN
+    case LQSGD_ACT_GELU:
+      return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    case LQSGD_ACT_SILU: {
+      const float s = 1.f / (1.f + expf(-z));
+      return s * (1.f + z * (1.f - s));
+    }
+    default: return 1.f;
+  }
+}
+
+}  // namespace
+}  // namespace lqsgd
