@@ -159,8 +159,12 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
       if (act != LQSGD_ACT_NONE) {
         const uint2 w = load_codes(z8.dev_codes + r * z8.ld_codes + s.col, vec_c && s.have == kRun, s.have);
         const float step = step_of(z8.dev_exps[r * z8.ld_exps + s.col / kGroup]);
+        float z[kRun];
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) g[j] *= act_slope(act, decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step));
+        for (int j = 0; j < kRun; ++j) z[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step);
+        slope_run(act, z);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) g[j] *= z[j];
       }
       if (dz) store_run<DT, kRun>(static_cast<T*>(dz) + r * ld_dz + s.col, vec_dz && s.have == kRun, s.have, g);
 #pragma unroll

@@ -9,41 +9,74 @@
 namespace lqsgd {
 namespace {
 
-// Adds the partial sums of a split product in the order of the pieces and applies the epilogue: a warp per row and 32
-// columns, lane by lane.
+// Adds the pieces of tiles that several clusters summed, in the order of the clusters, and applies the epilogue.  A unit is 32
+// neighbouring columns of a row of a tile, a column per lane.  `ways` warps (1 or 8) take turns at a unit's pieces and meet
+// in shared memory: with a hundred pieces one warp alone would wait for them one after the other.
+struct LinPieces {
+  const float* partial;
+  int32_t tiles_m, tiles_n, kb_total, share, cg, bn, swap, ways;
+};
 __global__ void __launch_bounds__(256)
-linear_join_kernel(const float* __restrict__ partial, int64_t ld_partial, int splits, LinEpilogue e) {
+linear_join_kernel(LinPieces q, LinEpilogue e) {
   train_pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const int groups = (e.cols + 31) / 32;
-  const int64_t units = (int64_t)e.rows * groups, plane = (int64_t)e.rows * ld_partial;
-  for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
-    const int64_t row = u / groups;
-    const int col = (int)(u - row * groups) * 32 + lane;
-    const bool on = col < e.cols;
+  __shared__ float sums[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int high = q.cg * kLinBM;                                   // rows of a tile; its columns are q.bn, or the other way round
+  const int unit_rows = q.swap ? q.bn : high, unit_groups = (q.swap ? high : q.bn) / 32;
+  const int64_t per_tile = (int64_t)unit_rows * unit_groups, units = (int64_t)q.tiles_m * q.tiles_n * per_tile;
+  const int at_once = 8 / q.ways, sub = warp % q.ways;
+  for (int64_t u0 = (int64_t)blockIdx.x * at_once; u0 < units; u0 += (int64_t)gridDim.x * at_once) {
+    const bool real = u0 + warp / q.ways < units;
+    const int64_t u = real ? u0 + warp / q.ways : 0;
+    const int t = (int)(u / per_tile), in = (int)(u - t * per_tile);
+    const int tr = in / unit_groups, tc = (in - tr * unit_groups) * 32;
+    int m_tile, n_tile;
+    LinWalk::place(q.tiles_m, q.tiles_n, t, m_tile, n_tile);
+    const int64_t row = (int64_t)(q.swap ? n_tile : m_tile) * unit_rows + tr;
+    const int col = (q.swap ? m_tile * high : n_tile * q.bn) + tc + lane;
+    const int64_t first = (int64_t)t * q.kb_total, last = first + q.kb_total - 1;
+    const int g0 = (int)(first / q.share), g1 = (int)(last / q.share);
+    const bool mine = real && g1 > g0 && row < e.rows && col - lane < e.cols;
     float v = 0.f;
-    if (on) {
-      const float* src = partial + row * ld_partial + col;
+    if (mine) {
+      // [row of the tile][bn], with few rows [row][128]: either way rows of the result, a column per lane
+      const float* src = q.partial + (int64_t)tr * (q.swap ? high : q.bn) + tc + lane;
+      const int64_t tile = (int64_t)high * q.bn;
 #pragma unroll 4
-      for (int s = 0; s < splits; ++s) v += src[s * plane];
+      for (int g = g0 + sub; g <= g1; g += q.ways)
+        v += src[(2 * g + ((int64_t)g * q.share < first ? 1 : 0)) * tile];
     }
-    finish_lane(e, row, col, on, v, on && e.bias ? __ldg(e.bias + col) : 0.f);
+    if (q.ways > 1) {
+      sums[warp][lane] = v;
+      __syncthreads();
+      if (sub == 0) {
+        v = 0.f;
+        for (int k = 0; k < q.ways; ++k) v += sums[warp + k][lane];
+      }
+      __syncthreads();
+    }
+    if (mine && sub == 0) finish_lane(e, row, col, col < e.cols, v, col < e.cols && e.bias ? __ldg(e.bias + col) : 0.f);
   }
 }
 
-// Copies a matrix of 16-bit values whose rows TMA cannot address (base or row distance not a multiple of 16 bytes) to
-// rows of ld_dst elements, a multiple of 8; what lies past cols is never read.
+// Copies a matrix whose rows TMA cannot address (base or row distance not a multiple of 16 bytes) to rows of ld_dst elements, a
+// multiple of 16 bytes; what lies past cols is never read.
+template <typename T>
 __global__ void __launch_bounds__(256)
-realign_kernel(const uint16_t* __restrict__ src, int64_t ld_src, int64_t rows, int cols, uint16_t* __restrict__ dst, int64_t ld_dst) {
+realign_kernel(const T* __restrict__ src, int64_t ld_src, int64_t rows, int cols, T* __restrict__ dst, int64_t ld_dst) {
   train_pdl_wait();
-  const int pairs = (cols + 1) / 2;
-  const int64_t units = rows * pairs;
+  constexpr int kPer = 4 / sizeof(T);
+  const int words = (cols + kPer - 1) / kPer;
+  const int64_t units = rows * words;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t row = u / pairs;
-    const int col = (int)(u - row * pairs) * 2;
-    const uint16_t* s = src + row * ld_src + col;
-    const uint32_t lo = s[0], hi = col + 1 < cols ? s[1] : 0;
-    *reinterpret_cast<uint32_t*>(dst + row * ld_dst + col) = lo | (hi << 16);
+    const int64_t row = u / words;
+    const int col = (int)(u - row * words) * kPer;
+    const T* s = src + row * ld_src + col;
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (col + j < cols) w |= (uint32_t)s[j] << (8 * sizeof(T) * j);
+    *reinterpret_cast<uint32_t*>(dst + row * ld_dst + col) = w;
   }
 }
 
@@ -61,83 +94,89 @@ EncodeFn tensor_map_encoder() {
   cached.store(fn, std::memory_order_release);
   return fn;
 }
-// Map over a matrix of 16-bit values: boxes of 64 columns x box_rows rows, 128-byte swizzle, zeros outside.
-int encode_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+// One operand as it lies in memory; elem = 2 bytes, or 1 (codes and exponents of a packed one).
+struct Stored {
+  const void* base = nullptr;
+  int64_t rows = 0, cols = 0, ld = 0;
+  int elem = 2;
+  int64_t aligned_ld() const { return ceil_div64(cols * elem, 16) * 16 / elem; }
+  // One row needs no row distance.
+  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld * elem % 16 == 0); }
+  size_t copy_bytes() const { return tma_ready() ? 0 : (size_t)rows * aligned_ld() * elem; }
+};
+// Map over an operand: boxes of box_cols x box_rows elements, zeros outside.
+int encode_map(CUtensorMap* map, const Stored& s, int box_cols, int box_rows, bool swizzle) {
   EncodeFn fn = tensor_map_encoder();
   if (!fn) return record_cuda_failure(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
-  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t stride[1] = {(cuuint64_t)(rows == 1 ? ceil_div64(cols, 8) * 8 : ld) * 2};   // one row has no distance to the next
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, es[2] = {1, 1};
-  if (fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dim, stride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  const cuuint64_t dim[2] = {(cuuint64_t)s.cols, (cuuint64_t)s.rows};
+  const cuuint64_t stride[1] = {(cuuint64_t)(s.rows == 1 ? s.aligned_ld() : s.ld) * s.elem};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, es[2] = {1, 1};
+  if (fn(map, s.elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(s.base), dim, stride, box, es,
+         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return record_cuda_failure(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   return LQSGD_OK;
 }
 
-// One operand as it lies in memory.
-struct Stored {
-  const void* base = nullptr;
-  int64_t rows = 0, cols = 0, ld = 0;
-  bool packed = false;
-  // One row needs no row distance.
-  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld % 8 == 0); }
-};
-
 struct Plan {
   int product;
   bool swap;                     // few rows: A and B exchanged
+  bool packed;                   // B is x8, decoded inside the product's kernel ...
+  bool unpacked;                 // ... or before it, into the workspace
   int cg, bn;
   int64_t M, N, K;
-  Stored a, b;
-  int tiles_m, tiles_n, splits, kb_total, kb_per_split;
-  int64_t ld_partial;
-  size_t off_a, off_b, off_partial, bytes;
+  Stored a, b, e;                // e: exponents of a packed b
+  int tiles_m, tiles_n, kb_total, share, clusters;
+  size_t off_a, off_b, off_e, off_x, off_partial, bytes;
 };
 
 constexpr int64_t kFewRows = 64;       // at most this many rows: the weights are the operand that is streamed
+constexpr int kSms = 148;              // sums are cut for this many SMs whatever the card has: results do not depend on it
 
-// Microseconds one work item of `kb` k-blocks costs: the fixed part (filling the pipeline, draining the accumulator) and the blocks.
-double item_us(int cg, int bn, int64_t kb) {
-  const double per_kb = cg == 2 ? 0.32 : (bn >= 128 ? 0.24 : 0.13);
-  return 2.0 + kb * per_kb;
-}
+// Microseconds: one k block of a tile, and what a tile costs besides (filling the pipeline, draining the accumulator).
+double block_us(int cg, int bn) { return cg == 2 ? 0.32 : (bn >= 128 ? 0.24 : 0.13); }
+constexpr double kTileUs = 2.0, kJoinUs = 3.0;
+constexpr int kDecodeFirstTiles = 4;
 
 int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   Plan p = {};
   p.product = product;
   const int64_t rows = a.rows;
-  const Stored x = {a.dev_x, rows, a.in, a.ld_x, false}, w = {a.dev_w, a.out, a.in, a.ld_w, false},
-               dz = {a.dev_dz, rows, a.out, a.ld_dz, false};
+  const Stored x = {a.dev_x, rows, a.in, a.ld_x}, w = {a.dev_w, a.out, a.in, a.ld_w}, dz = {a.dev_dz, rows, a.out, a.ld_dz};
   p.swap = product != LQSGD_LINEAR_GRAD_WEIGHT && rows <= kFewRows;
-  int64_t out_rows = rows, out_cols;
   if (product == LQSGD_LINEAR_FORWARD) {
-    p.a = x; p.b = w; p.M = rows; p.N = a.out; p.K = a.in; out_cols = a.out;
+    p.a = x; p.b = w; p.M = rows; p.N = a.out; p.K = a.in;
   } else if (product == LQSGD_LINEAR_GRAD_INPUT) {
-    p.a = dz; p.b = w; p.M = rows; p.N = a.in; p.K = a.out; out_cols = a.in;
+    p.a = dz; p.b = w; p.M = rows; p.N = a.in; p.K = a.out;
   } else {
-    p.a = dz; p.b = x; p.M = a.out; p.N = a.in; p.K = rows; out_rows = a.out; out_cols = a.in;
-    if (a.x8.dev_codes) p.b = {a.x8.dev_codes, rows, a.in, a.x8.ld_codes, true};
+    p.a = dz; p.b = x; p.M = a.out; p.N = a.in; p.K = rows;
+    p.packed = a.x8.dev_codes != nullptr;
+    if (p.packed) {
+      p.b = {a.x8.dev_codes, rows, a.in, a.x8.ld_codes, 1};
+      p.e = {a.x8.dev_exps, rows, ceil_div64(a.in, kGroup), a.x8.ld_exps, 1};
+    }
   }
   if (p.swap) { std::swap(p.a, p.b); std::swap(p.M, p.N); }
   p.kb_total = (int)ceil_div64(p.K, kLinBK);
-  const int slots = 148;               // a constant, so that sums are cut the same way on every card
   double best = 1e30;
   auto consider = [&](int cg, int bn) {
-    const int64_t tm = ceil_div64(p.M, (int64_t)kLinBM * cg), tn = ceil_div64(p.N, bn);
-    if (tm * tn > (1 << 28)) return;
-    const int units = slots / cg;
-    for (int s = 1; s <= 148 && s <= p.kb_total; ++s) {
-      if (tm * tn * s > 4 * units && s > 1) break;
-      const int64_t kb = ceil_div64(p.kb_total, s);
-      if (ceil_div64(p.kb_total, kb) != s) continue;         // the same pieces as a smaller s
-      const int64_t waves = ceil_div64(tm * tn * s, units);
-      double t = waves * item_us(cg, bn, kb);
-      if (s > 1) t += 2.5 + 8.0 * s * out_rows * out_cols / 4.0e6;
-      if (t < best) {
-        best = t;
-        p.cg = cg; p.bn = bn; p.tiles_m = (int)tm; p.tiles_n = (int)tn; p.splits = s; p.kb_per_split = (int)kb;
-      }
-    }
+    const int64_t tm = ceil_div64(p.M, (int64_t)kLinBM * cg), tn = ceil_div64(p.N, bn), tiles = tm * tn;
+    if (tiles > (1 << 28)) return;
+    const int units = kSms / cg;
+    const double per = block_us(cg, bn);
+    auto take = [&](double t, int64_t share, int64_t clusters) {
+      if (t >= best) return;
+      best = t;
+      p.cg = cg; p.bn = bn; p.tiles_m = (int)tm; p.tiles_n = (int)tn; p.share = (int)share; p.clusters = (int)clusters;
+    };
+    take(ceil_div64(tiles, units) * (kTileUs + p.kb_total * per), 0, std::min<int64_t>(tiles, units));
+    // equal shares of at least 4 k blocks each, where tiles are few
+    const int64_t pairs = tiles * p.kb_total;
+    if (tiles >= 2 * units || p.kb_total < 8) return;
+    const int64_t share = std::max<int64_t>(4, ceil_div64(pairs, units)), clusters = ceil_div64(pairs, share);
+    if (clusters <= tiles && share % p.kb_total == 0) return;
+    const double bytes = 4.0 * kLinBM * cg * bn * (double)clusters;
+    take(kTileUs * (share >= p.kb_total ? 2 : 1) + share * per + kJoinUs + bytes / 2.0e6, share, clusters);
   };
   if (p.swap) {
     consider(1, p.N <= 16 ? 16 : (p.N <= 32 ? 32 : 64));
@@ -146,13 +185,19 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
     consider(2, 256);
   }
   if (best > 1e29) return LQSGD_ERR_BAD_SHAPE;
-  p.ld_partial = ceil_div64(out_cols, 8) * 8;
   size_t off = 0;
-  auto take = [&](size_t n) { const size_t at = off; off += (n + 255) / 256 * 256; return at; };
-  auto copied = [&](const Stored& s) { return !s.packed && !s.tma_ready(); };
-  if (copied(p.a)) p.off_a = take((size_t)p.a.rows * (ceil_div64(p.a.cols, 8) * 8) * 2);
-  if (copied(p.b)) p.off_b = take((size_t)p.b.rows * (ceil_div64(p.b.cols, 8) * 8) * 2);
-  if (p.splits > 1) p.off_partial = take((size_t)p.splits * out_rows * p.ld_partial * 4);
+  auto room = [&](size_t n) { const size_t at = off; off += (n + 255) / 256 * 256; return at; };
+  // Every row tile decodes x8 again; from the fourth on it is cheaper to decode it once, into the workspace.
+  if (p.packed && p.tiles_m * p.cg >= kDecodeFirstTiles) {
+    p.packed = false;
+    p.unpacked = true;
+    p.b = {nullptr, rows, a.in, ceil_div64(a.in, 8) * 8, 2};
+    p.off_x = room((size_t)rows * p.b.ld * 2);
+  }
+  p.off_a = room(p.a.copy_bytes());
+  if (!p.unpacked) p.off_b = room(p.b.copy_bytes());
+  if (p.packed) p.off_e = room(p.e.copy_bytes());
+  if (p.share) p.off_partial = room((size_t)2 * p.clusters * kLinBM * p.cg * p.bn * 4);
   p.bytes = off;
   *out = p;
   return LQSGD_OK;
@@ -173,21 +218,25 @@ int check_matrix(const void* p, int64_t ld, int32_t cols, int elem) {
 
 // TMA reads an operand in place, or a copy of it with aligned rows in the workspace.
 int place(Stored* s, char* ws, size_t off, cudaStream_t st) {
-  if (s->packed || s->tma_ready()) return LQSGD_OK;
-  const int64_t ld = ceil_div64(s->cols, 8) * 8;
-  uint16_t* dst = reinterpret_cast<uint16_t*>(ws + off);
-  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ((s->cols + 1) / 2), 256), 148 * 16);
-  TRAIN_CK(train_launch(realign_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows,
-                        (int)s->cols, dst, ld), "realign_kernel launch");
-  s->base = dst;
+  if (s->tma_ready()) return LQSGD_OK;
+  const int64_t ld = s->aligned_ld();
+  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ceil_div64(s->cols * s->elem, 4), 256), 148 * 16);
+  const dim3 grid((unsigned)blocks), block(256);
+  if (s->elem == 2)
+    TRAIN_CK(train_launch(realign_kernel<uint16_t>, grid, block, 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows, (int)s->cols,
+                          reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
+  else
+    TRAIN_CK(train_launch(realign_kernel<uint8_t>, grid, block, 0, st, 1, static_cast<const uint8_t*>(s->base), s->ld, s->rows, (int)s->cols,
+                          reinterpret_cast<uint8_t*>(ws + off), ld), "realign_kernel launch");
+  s->base = ws + off;
   s->ld = ld;
   return LQSGD_OK;
 }
 
-template <int CG, int BN, int OA, int OB, bool SWAP>
+template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
 int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
-  using S = LinCfg<CG, BN, OA, OB>;
-  auto kernel = linear_kernel<CG, BN, OA, OB, SWAP>;
+  using S = LinCfg<CG, BN, OA, OB, SWAP, WF32>;
+  auto kernel = linear_kernel<CG, BN, OA, OB, SWAP, WF32>;
   static std::atomic<uint64_t> ready{0};                     // devices on which the kernel may use its shared memory
   int dev = 0;
   TRAIN_CK(cudaGetDevice(&dev), "cudaGetDevice");
@@ -195,13 +244,17 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
     TRAIN_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem), "cudaFuncSetAttribute(linear_kernel)");
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
-  int rc = encode_map(&q.ta, p.a.base, p.a.rows, p.a.cols, p.a.ld, OA == kOpK ? kLinBM : kLinBK);
+  int rc = encode_map(&q.ta, p.a, 64, OA == kOpK ? kLinBM : kLinBK, true);
   if (rc != LQSGD_OK) return rc;
-  if (OB != kOpPacked && (rc = encode_map(&q.tb, p.b.base, p.b.rows, p.b.cols, p.b.ld, OB == kOpK ? S::kBNc : kLinBK)) != LQSGD_OK) return rc;
+  if (OB == kOpPacked) {
+    if ((rc = encode_map(&q.tb, p.b, 128, kLinBK, true)) != LQSGD_OK || (rc = encode_map(&q.te, p.e, 16, kLinBK, false)) != LQSGD_OK) return rc;
+  } else if ((rc = encode_map(&q.tb, p.b, 64, OB == kOpK ? S::kBNc : kLinBK, true)) != LQSGD_OK) {
+    return rc;
+  }
   const int sms = train_sm_count();
   if (sms < CG) return record_cuda_failure(cudaErrorInvalidDevice, "cudaDevAttrMultiProcessorCount");
-  const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-  const int clusters = (int)std::min<int64_t>(items, sms / CG);
+  // Whole tiles may be dealt to any number of clusters, equal shares were cut for p.clusters (which then run in turn).
+  const int clusters = p.share ? p.clusters : (int)std::min<int64_t>((int64_t)p.tiles_m * p.tiles_n, sms / CG);
   TRAIN_CK(train_launch(kernel, dim3((unsigned)(clusters * CG)), dim3(S::kThreads), S::kSmem, st, CG, q), "linear_kernel launch");
   return LQSGD_OK;
 }
@@ -215,7 +268,12 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
     if (!train_aligned(a.dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;
   }
   char* ws = static_cast<char*>(a.dev_workspace);
+  if (p.unpacked) {
+    p.b.base = ws + p.off_x;
+    if ((rc = lqsgd_unpack8(&a.x8, a.rows, a.in, ws + p.off_x, p.b.ld, a.dtype, st)) != LQSGD_OK) return rc;
+  }
   if ((rc = place(&p.a, ws, p.off_a, st)) != LQSGD_OK || (rc = place(&p.b, ws, p.off_b, st)) != LQSGD_OK) return rc;
+  if (p.packed && (rc = place(&p.e, ws, p.off_e, st)) != LQSGD_OK) return rc;
   const int es = ep.dtype == LQSGD_F32 ? 4 : 2;
   auto rows_aligned = [](const void* ptr, int64_t bytes, size_t to) { return train_aligned(ptr, to) && bytes % (int64_t)to == 0; };
   ep.vec_out = rows_aligned(ep.out, ep.ld_out * es, 32);
@@ -225,30 +283,29 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   LinProblem q;
   std::memset(&q, 0, sizeof(q));
   q.ep = ep;
-  q.partial = p.splits > 1 ? reinterpret_cast<float*>(ws + p.off_partial) : nullptr;
-  q.ld_partial = p.ld_partial;
-  q.x8 = a.x8;
-  q.x8_vec = rows_aligned(a.x8.dev_codes, a.x8.ld_codes, 16);
+  q.partial = p.share ? reinterpret_cast<float*>(ws + p.off_partial) : nullptr;
   q.M = (int32_t)p.M; q.N = (int32_t)p.N; q.K = (int32_t)p.K;
-  q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.splits = p.splits; q.kb_total = p.kb_total; q.kb_per_split = p.kb_per_split;
+  q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total; q.share = p.share;
   q.dtype = a.dtype;
   q.status = a.dev_status;
   if (product == LQSGD_LINEAR_FORWARD) {
-    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpK, kOpK, true>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpK, kOpK, true>(p, q, st) : launch<1, 64, kOpK, kOpK, true>(p, q, st);
-    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false>(p, q, st);
+    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpK, kOpK, true, false>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpK, kOpK, true, false>(p, q, st) : launch<1, 64, kOpK, kOpK, true, false>(p, q, st);
+    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false, false>(p, q, st);
   } else if (product == LQSGD_LINEAR_GRAD_INPUT) {
-    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpMN, kOpK, true>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpMN, kOpK, true>(p, q, st) : launch<1, 64, kOpMN, kOpK, true>(p, q, st);
-    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false>(p, q, st);
-  } else if (p.b.packed) {
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpPacked, false>(p, q, st) : launch<1, 128, kOpMN, kOpPacked, false>(p, q, st);
+    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpMN, kOpK, true, false>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpMN, kOpK, true, false>(p, q, st) : launch<1, 64, kOpMN, kOpK, true, false>(p, q, st);
+    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false, false>(p, q, st);
+  } else if (p.packed) {
+    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpPacked, false, true>(p, q, st) : launch<1, 128, kOpMN, kOpPacked, false, true>(p, q, st);
   } else {
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, false>(p, q, st) : launch<1, 128, kOpMN, kOpMN, false>(p, q, st);
+    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, false, true>(p, q, st) : launch<1, 128, kOpMN, kOpMN, false, true>(p, q, st);
   }
   if (rc != LQSGD_OK) return rc;
-  if (p.splits > 1) {
-    const int64_t units = (int64_t)ep.rows * ((ep.cols + 31) / 32);
-    TRAIN_CK(train_launch(linear_join_kernel, dim3((unsigned)std::min<int64_t>(ceil_div64(units, 8), 148 * 8)), dim3(256), 0, st, 1,
-                          static_cast<const float*>(q.partial), p.ld_partial, p.splits, ep), "linear_join_kernel launch");
+  if (p.share) {
+    const int most = (int)((p.kb_total - 1) / p.share + 2);           // pieces of one tile
+    LinPieces j = {q.partial, p.tiles_m, p.tiles_n, p.kb_total, p.share, p.cg, p.bn, p.swap ? 1 : 0, most >= 16 ? 8 : 1};
+    const int64_t units = (int64_t)p.tiles_m * p.tiles_n * kLinBM * p.cg * p.bn / 32;
+    const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div64(units, 8 / j.ways), kSms * 8);
+    TRAIN_CK(train_launch(linear_join_kernel, dim3(blocks), dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
   }
   return LQSGD_OK;
 }

@@ -14,8 +14,9 @@
 //
 // A cluster of CG CTAs (1 or 2) works on a tile of 128 CG x BN: with CG = 2 each SM holds 128 rows of A and half of B's, and
 // one tcgen05.mma.cta_group::2 drives both tensor cores, so that an SM fetches (128 + BN / 2) rows per k instead of
-// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-7 drain the
-// accumulator (two of them, so that the next tile's sum runs under the epilogue), warps 8.. decode x8.  Clusters walk
+// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 (4-7 with few rows) drain the
+// accumulator (two of them, so that the next tile's sum runs under the epilogue); with x8 warp 3 loads its codes and the last
+// eight warps decode them.  Clusters walk
 // the work items (tile, piece of the sum) with a fixed stride.
 //
 // Every wait is bounded (lqsgd_stream_common.cuh): on expiry the CTA's abort flag goes up, all roles leave their loops,
@@ -48,14 +49,13 @@ struct LinEpilogue {
 };
 
 struct alignas(64) LinProblem {
-  CUtensorMap ta, tb;
+  CUtensorMap ta, tb;                  // operands; tb of a packed B: its codes
+  CUtensorMap te;                      // exponents of a packed B
   LinEpilogue ep;
-  float* partial;                      // [splits][rows][ld_partial] when splits > 1
-  int64_t ld_partial;
-  lqsgd_packed8 x8;                    // operand B when it is packed
-  int32_t x8_vec;                      // its rows are 16-byte aligned
+  float* partial;                      // pieces of sums: two per cluster, each a tile (see LinWalk)
   int32_t M, N, K;
-  int32_t tiles_m, tiles_n, splits, kb_total, kb_per_split;
+  int32_t tiles_m, tiles_n, kb_total;
+  int32_t share;                       // 0: clusters take whole tiles; otherwise every cluster takes this many k-blocks in a row
   int32_t dtype;                       // of the operands
   uint32_t* status;
 };
@@ -72,28 +72,24 @@ __device__ __forceinline__ uint32_t map_to(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
   return a;
 }
+// Arrival on a barrier of either CTA of the cluster.  What it announces was written through, or read by, the tensor core's side
+// (after fence.proxy.async or tcgen05.fence): nothing passes through ordinary memory accesses, so it needs no release at
+// cluster scope, which would wait for every load the thread has in flight (it made the weight gradient 4 times slower).
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// Bounded wait that also acquires what other CTAs of the cluster released.
+// Bounded wait: a plain try first, which costs a few cycles when the phase is complete, then the timed ones (testing in a
+// loop first took 12 % off a large product's rate: the waiting warps' instructions displace the others').
 __device__ __forceinline__ bool lin_wait(uint64_t* b, uint32_t parity, volatile int* abort_flag) {
-  const uint32_t limit = wait_limit_of(abort_flag);
-  for (uint32_t i = 0; i < limit; ++i) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity), "r"(1000u) : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  return ok ? true : mbar_wait(b, parity, abort_flag);
 }
 __device__ __forceinline__ bool lin_wait_warp(uint64_t* b, uint32_t parity, volatile int* abort_flag, int lane) {
   int ok = 1;
   if (lane == 0) ok = lin_wait(b, parity, abort_flag) ? 1 : 0;
-  ok = __shfl_sync(0xffffffffu, ok, 0);
-  return ok != 0;
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
 template <int CG>
@@ -217,31 +213,53 @@ __device__ __forceinline__ void put_packed(const lqsgd_packed8& p, bool vec, int
   p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
 }
 
-// Epilogue of 32 consecutive columns of one row held by one thread.
-__device__ __forceinline__ void finish_row32(const LinEpilogue& e, int64_t row, int col, float (&v)[32]) {
+// Epilogues of a 32 x 32 piece held by a warp, a row per thread (on: the row exists; row0: lane 0's row): a weight gradient, ...
+// Rows that are not 32-byte aligned go through the warp's scratch in shared memory, so that a warp's access is one row's
+// 32 columns instead of one column of 32 rows (which costs a sector per element).
+constexpr int kScratchPitch = 33;                      // words; odd, so neither rows nor columns meet on one bank
+constexpr uint32_t kScratchBytes = 32 * kScratchPitch * 4, kScratchBytes16 = 32 * 34 * 2;
+__device__ __forceinline__ void finish_rows_f32(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], float* scratch) {
+  const int lane = threadIdx.x & 31;
   const int have = min(32, e.cols - col);
-  if (e.dtype == LQSGD_F32) {
-    float* o = static_cast<float*>(e.out) + row * e.ld_out + col;
-    if (e.vec_out && have == 32) {
+  if (e.vec_out && have == 32) {
+    if (!on) return;
+    float* o = static_cast<float*>(e.out) + (row0 + lane) * e.ld_out + col;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t w[8];
-        if (e.accumulate) {
-          ld_global_32(o + 8 * i, w);
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w[8];
+      if (e.accumulate) {
+        ld_global_32(o + 8 * i, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[8 * i + j] += __uint_as_float(w[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
-        st_global_32(o + 8 * i, w);
+        for (int j = 0; j < 8; ++j) v[8 * i + j] += __uint_as_float(w[j]);
       }
-    } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i < have) o[i] = e.accumulate ? o[i] + v[i] : v[i];
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
+      st_global_32(o + 8 * i, w);
     }
     return;
   }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) scratch[lane * kScratchPitch + i] = v[i];
+  __syncwarp();
+  const int rows = (int)min((int64_t)32, e.rows - row0);
+  float* o = static_cast<float*>(e.out) + row0 * e.ld_out + col + lane;
+  if (lane < have) {
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+      const float t = scratch[r * kScratchPitch + lane];
+      o[r * e.ld_out] = e.accumulate ? o[r * e.ld_out] + t : t;
+    }
+  }
+  __syncwarp();
+}
+// ... or a layer's output.
+__device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], float* scratch) {
+  const int lane = threadIdx.x & 31;
+  const int have = min(32, e.cols - col);
+  const int64_t row = row0 + lane;
+  const int rows = (int)min((int64_t)32, e.rows - row0);
+  uint16_t* half = reinterpret_cast<uint16_t*>(scratch);                // 16-bit values: rows of 2 x 17 halves
+  constexpr int kHalfPitch = 34;
   if (e.bias) {
     if (have == 32) {
 #pragma unroll
@@ -257,55 +275,64 @@ __device__ __forceinline__ void finish_row32(const LinEpilogue& e, int64_t row, 
     for (int i = 0; i < 32; ++i)
       if (i >= have) v[i] = 0.f;
   }
-  if (e.z8.dev_codes) put_packed(e.z8, e.vec_z8, row, col, have, v);
-  if (e.act == LQSGD_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = act_value(LQSGD_ACT_RELU, v[i]);
-  } else if (e.act == LQSGD_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = act_value(LQSGD_ACT_GELU, v[i]);
-  } else if (e.act == LQSGD_ACT_SILU) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = act_value(LQSGD_ACT_SILU, v[i]);
-  }
+  if (e.z8.dev_codes && on) put_packed(e.z8, e.vec_z8, row, col, have, v);
+  act_run(e.act, v);
   if (e.residual) {
-    const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row * e.ld_res + col;
+    const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row0 * e.ld_res + col;
     if (e.vec_res && have == 32) {
+      if (on) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t w[8];
-        ld_global_32(r + 16 * i, w);
+        for (int i = 0; i < 2; ++i) {
+          uint32_t w[8];
+          ld_global_32(r + lane * e.ld_res + 16 * i, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float2 f = unpack2(e.dtype, w[j]);
-          v[16 * i + 2 * j] += f.x;
-          v[16 * i + 2 * j + 1] += f.y;
+          for (int j = 0; j < 8; ++j) {
+            const float2 f = unpack2(e.dtype, w[j]);
+            v[16 * i + 2 * j] += f.x;
+            v[16 * i + 2 * j + 1] += f.y;
+          }
         }
       }
     } else {
+      if (lane < have) {
+#pragma unroll 8
+        for (int k = 0; k < rows; ++k) half[k * kHalfPitch + lane] = r[k * e.ld_res + lane];
+      }
+      __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i < have) v[i] += unpack1(e.dtype, r[i]);
+      for (int j = 0; j < 16; ++j) {
+        const float2 f = unpack2(e.dtype, *reinterpret_cast<const uint32_t*>(half + lane * kHalfPitch + 2 * j));
+        if (2 * j < have) v[2 * j] += f.x;
+        if (2 * j + 1 < have) v[2 * j + 1] += f.y;
+      }
+      __syncwarp();
     }
   }
   uint32_t w[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) w[i] = pack2(e.dtype, v[2 * i], v[2 * i + 1]);
-  uint16_t* o = static_cast<uint16_t*>(e.out) + row * e.ld_out + col;
+  uint16_t* o = static_cast<uint16_t*>(e.out) + row0 * e.ld_out + col;
   if (e.vec_out && have == 32) {
+    if (on) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t h[8];
+      for (int i = 0; i < 2; ++i) {
+        uint32_t h[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = w[8 * i + j];
-      st_global_32(o + 16 * i, h);
+        for (int j = 0; j < 8; ++j) h[j] = w[8 * i + j];
+        st_global_32(o + lane * e.ld_out + 16 * i, h);
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < have) o[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(half + lane * kHalfPitch + 2 * j) = w[j];
+    __syncwarp();
+    if (lane < have) {
+#pragma unroll 8
+      for (int k = 0; k < rows; ++k) o[k * e.ld_out + lane] = half[k * kHalfPitch + lane];
+    }
+    __syncwarp();
   }
-  if (e.y8.dev_codes) {
+  if (e.y8.dev_codes && on) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float2 f = unpack2(e.dtype, w[i]);
@@ -334,102 +361,159 @@ __device__ __forceinline__ void finish_lane(const LinEpilogue& e, int64_t row, i
   }
   v = on ? v + bias : 0.f;
   if (e.z8.dev_codes) put_packed_lane(e.z8, row, col, on, v);
-  v = act_value(e.act, v);
+  float one[1] = {v};
+  act_run(e.act, one);
+  v = one[0];
   if (e.residual && on) v += unpack1(e.dtype, static_cast<const uint16_t*>(e.residual)[row * e.ld_res + col]);
   const uint16_t w = pack1(e.dtype, v);
   if (on) static_cast<uint16_t*>(e.out)[row * e.ld_out + col] = w;
   if (e.y8.dev_codes) put_packed_lane(e.y8, row, col, on, on ? unpack1(e.dtype, w) : 0.f);
 }
 
-// ---- decoding 8-bit codes into operand words: two codes (bytes `sel`, sel + 1 of w) -> two 16-bit numbers
-// bf16: 0x4300 | m is 128 + m, so subtracting 128 gives m exactly, and m 2^e has 8 significant bits.
-// fp16: 0x6400 | m is 1024 + m, likewise.
-__device__ __forceinline__ uint32_t decode2_bf16(uint32_t w, int hi, uint32_t step2) {
-  const uint32_t p = __byte_perm(w, 0u, hi ? 0x4342 : 0x4140);             // [c0, 0, c1, 0]
-  const uint32_t s = __byte_perm(w, 0u, hi ? 0x3424 : 0x1404) & 0x80008000u;  // [0, c0, 0, c1]
-  uint32_t t = (p & 0x007f007fu) | 0x43004300u;
-  __nv_bfloat162 m = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&t), __nv_bfloat162(__ushort_as_bfloat16(0x4300), __ushort_as_bfloat16(0x4300)));
-  m = __hmul2(m, *reinterpret_cast<const __nv_bfloat162*>(&step2));
-  return *reinterpret_cast<uint32_t*>(&m) | s;
+// ---- decoding 8-bit codes into operand words: four codes (one word) -> two words of two 16-bit numbers
+// bf16: 0x4300 | m is 128 + m, so (128 + m) 2^e - 128 2^e is m 2^e, exactly, in one fused operation; then the sign is put on top.
+// fp16: 0x6400 | m is 1024 + m; 1024 2^e may be out of range, so the 1024 goes first.
+// Codes 0 and 2 make the first word, 1 and 3 the second, which takes no byte shuffles: within every four columns the operand
+// holds columns 0, 2, 1, 3, and the epilogue puts them back.
+__device__ __forceinline__ void decode4_bf16(uint32_t w, uint32_t step2, uint32_t off2, uint32_t& even, uint32_t& odd) {
+  const uint32_t te = (w & 0x007f007fu) | 0x43004300u, to = ((w >> 8) & 0x007f007fu) | 0x43004300u;
+  const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&step2), o = *reinterpret_cast<const __nv_bfloat162*>(&off2);
+  const __nv_bfloat162 e = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&te), s, o), d = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&to), s, o);
+  even = *reinterpret_cast<const uint32_t*>(&e) | ((w << 8) & 0x80008000u);
+  odd = *reinterpret_cast<const uint32_t*>(&d) | (w & 0x80008000u);
 }
-__device__ __forceinline__ uint32_t decode2_fp16(uint32_t w, int hi, uint32_t step2) {
-  const uint32_t p = __byte_perm(w, 0u, hi ? 0x4342 : 0x4140);
-  const uint32_t s = __byte_perm(w, 0u, hi ? 0x3424 : 0x1404) & 0x80008000u;
-  uint32_t t = (p & 0x007f007fu) | 0x64006400u;
-  __half2 m = __hsub2(*reinterpret_cast<__half2*>(&t), __half2(__ushort_as_half(0x6400), __ushort_as_half(0x6400)));
-  m = __hmul2(m, *reinterpret_cast<const __half2*>(&step2));
-  return *reinterpret_cast<uint32_t*>(&m) | s;
+__device__ __forceinline__ void decode4_fp16(uint32_t w, uint32_t step2, uint32_t& even, uint32_t& odd) {
+  const uint32_t te = (w & 0x007f007fu) | 0x64006400u, to = ((w >> 8) & 0x007f007fu) | 0x64006400u;
+  const __half2 s = *reinterpret_cast<const __half2*>(&step2), k = __half2(__ushort_as_half(0x6400), __ushort_as_half(0x6400));
+  const __half2 e = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&te), k), s), d = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&to), k), s);
+  even = *reinterpret_cast<const uint32_t*>(&e) | ((w << 8) & 0x80008000u);
+  odd = *reinterpret_cast<const uint32_t*>(&d) | (w & 0x80008000u);
 }
 // Any step: through fp32, saturated to the type's largest finite number (NaN stays).
-__device__ __forceinline__ uint32_t decode2_any(int dtype, uint32_t w, int hi, int eb) {
+__device__ __forceinline__ float decode1_any(float top, uint32_t code, int eb) {
+  const float a = decode8(code & 255u, step_of(eb));
+  return fabsf(a) > top ? copysignf(top, a) : a;
+}
+__device__ __forceinline__ void decode4_any(int dtype, uint32_t w, int eb, uint32_t& even, uint32_t& odd) {
   const float top = dtype == LQSGD_BF16 ? 3.3895314e38f : 65504.f;
-  float a = decode8(w >> (hi ? 16 : 0) & 255u, step_of(eb)), b = decode8(w >> (hi ? 24 : 8) & 255u, step_of(eb));
-  if (fabsf(a) > top) a = copysignf(top, a);
-  if (fabsf(b) > top) b = copysignf(top, b);
-  return pack2(dtype, a, b);
+  even = pack2(dtype, decode1_any(top, w, eb), decode1_any(top, w >> 16, eb));
+  odd = pack2(dtype, decode1_any(top, w >> 8, eb), decode1_any(top, w >> 24, eb));
 }
 
-// ---- the walk over (work item, k block) pairs that every role of a CTA makes
+// ---- the walk over (tile, k block) pairs that every role of a CTA makes
+// Two ways to deal them out.  Whole tiles: cluster g takes tiles g, g + G, ...  Equal shares (few tiles, long sums): all
+// (tile, k block) pairs stand in one row, tile after tile, and cluster g takes pairs [g share, (g + 1) share).  A tile
+// that a share begins or ends inside of is summed by several clusters: each writes what it has to a piece of the
+// workspace (at most two per cluster: piece 2 g where its share begins, 2 g + 1 for a tile that its share ends
+// inside of), and linear_join_kernel adds a tile's pieces in the order of the clusters.
 struct LinWalk {
-  int item, stride, items;
-  int kb, kb_end;
-  int m_tile, n_tile, split;
-  // Tiles are taken in bands of 8 rows of tiles, column by column: 74 clusters at work then share 8 row tiles and
+  int64_t pos, end;                    // equal shares: pairs; whole tiles: tiles
+  int64_t begin;
+  int stride, cluster;
+  int kb, kb_end;                      // the k blocks of the current tile that are this cluster's
+  int m_tile, n_tile;
+  // Tiles are taken in bands of 8 rows of tiles, column by column: the clusters at work then share 8 row tiles and
   // about as many column tiles, which keeps their operands in L2.
-  __device__ __forceinline__ void locate(const LinProblem& p) {
-    const int tiles = p.tiles_m * p.tiles_n;
-    split = item / tiles;
-    const int t = item - split * tiles;
+  static __device__ __forceinline__ void place(int tiles_m, int tiles_n, int t, int& m_tile, int& n_tile) {
     constexpr int kBand = 8;
-    const int band = t / (kBand * p.tiles_n), first = band * kBand, high = min(kBand, p.tiles_m - first);
-    const int in = t - band * kBand * p.tiles_n;
+    const int band = t / (kBand * tiles_n), first = band * kBand, high = min(kBand, tiles_m - first);
+    const int in = t - band * kBand * tiles_n;
     m_tile = first + in % high;
     n_tile = in / high;
-    kb = split * p.kb_per_split;
-    kb_end = min(p.kb_total, kb + p.kb_per_split);
   }
-  __device__ __forceinline__ LinWalk(const LinProblem& p, int first, int step) : item(first), stride(step) {
-    items = p.tiles_m * p.tiles_n * p.splits;
-    if (item < items) locate(p);
+  __device__ __forceinline__ void locate(const LinProblem& p) {
+    int t;
+    if (p.share) {
+      t = (int)(pos / p.kb_total);
+      kb = (int)(pos - (int64_t)t * p.kb_total);
+      kb_end = (int)min((int64_t)p.kb_total, kb + (end - pos));
+    } else {
+      t = (int)pos;
+      kb = 0;
+      kb_end = p.kb_total;
+    }
+    place(p.tiles_m, p.tiles_n, t, m_tile, n_tile);
   }
-  __device__ __forceinline__ bool done() const { return item >= items; }
-  __device__ __forceinline__ void next_item(const LinProblem& p) {
-    item += stride;
-    if (item < items) locate(p);
+  __device__ __forceinline__ LinWalk(const LinProblem& p, int g, int clusters) : cluster(g) {
+    if (p.share) {
+      pos = (int64_t)g * p.share;
+      end = min((int64_t)p.tiles_m * p.tiles_n * p.kb_total, pos + p.share);
+      stride = 0;
+    } else {
+      pos = g;
+      end = (int64_t)p.tiles_m * p.tiles_n;
+      stride = clusters;
+    }
+    begin = pos;
+    if (pos < end) locate(p);
   }
+  __device__ __forceinline__ bool done() const { return pos >= end; }
+  // The piece the current tile's sum goes to, or -1: the cluster has the whole tile.
+  __device__ __forceinline__ int piece(const LinProblem& p) const {
+    return kb_end - kb == p.kb_total ? -1 : (pos == begin ? 2 * cluster : 2 * cluster + 1);
+  }
+  __device__ __forceinline__ int blocks() const { return kb_end - kb; }
+  // To the next tile; only from the state locate() left (next() below moves kb).
+  __device__ __forceinline__ void next_tile(const LinProblem& p) {
+    pos += p.share ? kb_end - kb : stride;
+    if (pos < end) locate(p);
+  }
+  // To the next k block, of this tile or the next.
   __device__ __forceinline__ void next(const LinProblem& p) {
-    if (++kb == kb_end) next_item(p);
+    if (p.share) ++pos;
+    if (++kb == kb_end) {
+      if (!p.share) pos += stride;
+      if (pos < end) locate(p);
+    }
   }
 };
 
-template <int CG, int BN, int OA, int OB>
+// WF32: the result is fp32 (a weight gradient); SWAP: few rows.
+template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
 struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
   static constexpr uint32_t kStage = kABytes + ((kBBytes + 1023) / 1024 * 1024);
-  static constexpr int kStages = (int)((216u * 1024) / kStage) > 12 ? 12 : (int)((216u * 1024) / kStage);
+  // a packed B passes through a second, small ring: 64 rows of kBNc codes and of the 16 exponents that hold the tile's
+  static constexpr int kRaw = OB == kOpPacked ? 4 : 0;
+  static constexpr uint32_t kRawCodes = kLinBK * kBNc, kRawBytes = kRawCodes + kLinBK * 16;
+  static constexpr uint32_t kScratch = SWAP ? 0 : (WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16);   // one per epilogue warp
+  static constexpr uint32_t kRoom = 225u * 1024 - kRaw * kRawBytes - kScratch;
+  static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
   static constexpr uint32_t kTxBytes = CG * (kABytes + (OB == kOpPacked ? 0 : kBBytes));
-  static constexpr int kConvWarps = OB == kOpPacked ? kBNc / 16 : 0;      // a thread decodes 32 codes of one row of x
-  static constexpr int kThreads = 256 + kConvWarps * 32;
+  // Two warps per quarter of tensor memory where the epilogue computes per value (GELU and the 8-bit form take as
+  // long as the product of a 4096-wide layer with one).
+  static constexpr int kEpiWarps = SWAP || WF32 ? 4 : 8;
+  // A thread decodes 32 codes of one row of x; two teams of warps take the stages in turn, because one team's
+  // chain of waits, loads, decoding and hand-over (about 700 cycles) is longer than a stage's MMAs (512).
+  static constexpr int kTeams = 2;
+  static constexpr int kConvWarps = OB == kOpPacked ? kBNc / 16 : 0;      // of one team
+  static constexpr int kConvWarp0 = 4 + kEpiWarps;
+  static constexpr int kThreads = (kConvWarp0 + kTeams * kConvWarps) * 32;
   static constexpr int kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
-  static constexpr int kBars = 3 * kStages + 2 + 2 + 1;
-  static constexpr uint32_t kBarOff = kStages * kStage;
+  static constexpr int kBars = 3 * kStages + 2 * kRaw + 2 + 2 + 1;
+  static constexpr uint32_t kRawBase = kStages * kStage;
+  static constexpr uint32_t kScratchOff = kRawBase + kRaw * kRawBytes;
+  static constexpr uint32_t kBarOff = (kScratchOff + kScratch + 7) / 8 * 8;
   static constexpr uint32_t kSmem = kBarOff + kBars * 8 + 32 + 1024;
   static_assert(kSmem <= 227 * 1024 && kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "one CTA per SM");
   static_assert(OB == kOpK || kBNc % 64 == 0, "MN-major operands come in blocks of 64");
+  static_assert(OB != kOpPacked || kBNc == 128, "a row of codes is one 128-byte swizzle span");
 };
 
 // SWAP: A's rows are the result's columns (few rows); otherwise A's rows are its rows.
-template <int CG, int BN, int OA, int OB, bool SWAP>
-__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB>::kThreads, 1)
+template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
+__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB, SWAP, WF32>::kThreads, 1)
 linear_kernel(const __grid_constant__ LinProblem p) {
-  using S = LinCfg<CG, BN, OA, OB>;
+  using S = LinCfg<CG, BN, OA, OB, SWAP, WF32>;
   extern __shared__ uint8_t lin_smem[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(lin_smem) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(base + S::kBarOff);   // [stages] TMA bytes landed, in both CTAs (first CTA's barrier)
   uint64_t* conv = full + S::kStages;                                // [stages] decoded rows of B written, in both CTAs (first CTA's)
   uint64_t* empty = conv + S::kStages;                               // [stages] the MMAs that read the stage are done
-  uint64_t* d_full = empty + S::kStages;                             // [2] accumulator complete
+  uint64_t* raw_full = empty + S::kStages;                           // [raw] codes and exponents of B landed in this CTA
+  uint64_t* raw_empty = raw_full + S::kRaw;                          // [raw] every converter warp has them in registers
+  uint64_t* d_full = raw_empty + S::kRaw;                            // [2] accumulator complete
   uint64_t* d_empty = d_full + 2;                                    // [2] accumulator drained by both CTAs (first CTA's)
   uint64_t* fin = d_empty + 2;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(fin + 1);
@@ -437,7 +521,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
-  const int first_item = (int)blockIdx.x / CG, item_step = (int)gridDim.x / CG;
+  const int cluster = (int)blockIdx.x / CG, clusters = (int)gridDim.x / CG;
 
   if (tid == 0) {
     for (int s = 0; s < S::kStages; ++s) {
@@ -445,7 +529,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       mbar_init(conv + s, CG * (S::kConvWarps ? S::kConvWarps : 1));
       mbar_init(empty + s, 1);
     }
-    for (int s = 0; s < 2; ++s) { mbar_init(d_full + s, 1); mbar_init(d_empty + s, 4 * CG); }
+    for (int s = 0; s < S::kRaw; ++s) { mbar_init(raw_full + s, 1); mbar_init(raw_empty + s, S::kConvWarps); }
+    for (int s = 0; s < 2; ++s) { mbar_init(d_full + s, 1); mbar_init(d_empty + s, S::kEpiWarps * CG); }
     mbar_init(fin, 1);
     wait_ctl_init(abort_flag, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -453,7 +538,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   }
   if (warp == 0 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&p.ta) : "memory");
-    if constexpr (OB != kOpPacked) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tb) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tb) : "memory");
+    if constexpr (OB == kOpPacked) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.te) : "memory");
   }
   if (warp == 2) {
     if constexpr (CG == 2) {
@@ -477,7 +563,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      for (LinWalk w(p, first_item, item_step); !w.done(); w.next(p), ++it) {
+      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p), ++it) {
         const int s = it % S::kStages;
         if (!lin_wait(empty + s, ((it / S::kStages) & 1) ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* a = base + s * S::kStage;
@@ -515,7 +601,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
                              ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((kLinBM * CG) >> 4) << 24);
       uint32_t it = 0, seq = 0;
       bool ok = true;
-      for (LinWalk w(p, first_item, item_step); !w.done() && ok; w.next_item(p), ++seq) {
+      for (LinWalk w(p, cluster, clusters); !w.done() && ok; w.next_tile(p), ++seq) {
         const uint32_t db = seq & 1;
         if (!lin_wait(d_empty + db, ((seq >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
         lin_fence_after();
@@ -542,44 +628,71 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       for (uint32_t i = 0; i < limit && !mbar_try(fin, 0); ++i) {}
     }
     __syncwarp();
-  } else if (warp >= 4 && warp < 8) {
-    // ---- epilogue
+  } else if (OB == kOpPacked && warp == 3) {
+    // ---- loader of the codes: one thread; each CTA brings its own part, for its own converters
+    if constexpr (OB == kOpPacked) if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p), ++it) {
+        const int r = it % S::kRaw;
+        if (!lin_wait(raw_empty + r, ((it / S::kRaw) & 1) ^ 1, abort_flag)) { ok = false; break; }
+        uint8_t* raw = base + S::kRawBase + r * S::kRawBytes;
+        const int k0 = w.kb * kLinBK, n0 = w.n_tile * BN + (int)rank * S::kBNc;
+        mbar_arrive_expect_tx(raw_full + r, S::kRawBytes);
+        lin_tma<1>(raw, &p.tb, n0, k0, smem_u32(raw_full + r));
+        lin_tma<1>(raw + S::kRawCodes, &p.te, n0 / kGroup / 16 * 16, k0, smem_u32(raw_full + r));
+      }
+      if (!ok) {
+        const uint32_t limit = wait_limit_of(abort_flag);
+        for (uint32_t j = it > (uint32_t)S::kRaw ? it - S::kRaw : 0; j < it; ++j)
+          for (uint32_t i = 0; i < limit && !mbar_try(raw_full + j % S::kRaw, (j / S::kRaw) & 1); ++i) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4 && warp < 4 + S::kEpiWarps) {
+    // ---- epilogue: a warp reads its quarter of the accumulator's rows (warp % 4), and with eight warps half of its columns
     uint32_t seq = 0;
     const int q = warp & 3;
-    for (LinWalk w(p, first_item, item_step); !w.done(); w.next_item(p), ++seq) {
+    for (LinWalk w(p, cluster, clusters); !w.done(); w.next_tile(p), ++seq) {
       const uint32_t db = seq & 1;
       if (!lin_wait_warp(d_full + db, (seq >> 1) & 1, abort_flag, lane)) break;
       lin_fence_after();
       const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + db * BN;
       const int m = (w.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane;
       const int n0 = w.n_tile * BN;
-      float* part = p.splits > 1 ? p.partial + (int64_t)w.split * p.ep.rows * p.ld_partial : nullptr;
+      const int piece = w.piece(p);
+      float* part = piece >= 0 ? p.partial + (int64_t)piece * (CG * kLinBM * BN) : nullptr;
       if constexpr (!SWAP) {
-        constexpr int kStep = 32;
+        constexpr int kStep = 32, kMine = BN / (S::kEpiWarps / 4);
+        const int c0 = ((warp - 4) >> 2) * kMine;
+        float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * (WF32 ? kScratchBytes : kScratchBytes16));
 #pragma unroll 1
-        for (int c = 0; c < BN; c += kStep) {
+        for (int c = c0; c < c0 + kMine; c += kStep) {
           float v[32];
           tmem_ld32(taddr + c, v);
-          if (c + kStep >= BN) {                    // the accumulator is in registers: hand it back
+          if (c + kStep >= c0 + kMine) {            // the accumulator is in registers: hand it back
             lin_fence_before();
             __syncwarp();
             if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
           }
-          if (m < p.M && n0 + c < p.N) {
-            if (part) {
-              float* o = part + (int64_t)m * p.ld_partial + n0 + c;          // rows of 32-byte aligned runs
-              const int have = min(32, p.N - n0 - c);
+          if (n0 + c >= p.N || m - lane >= p.M) continue;
+          if constexpr (OB == kOpPacked) {          // back from the order of the decoder
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (8 * i < have) {
-                  uint32_t u[8];
+            for (int j = 0; j < 32; j += 4) { const float t = v[j + 1]; v[j + 1] = v[j + 2]; v[j + 2] = t; }
+          }
+          if (part) {                               // [row of the tile][BN]
+            float* o = part + (int64_t)((int)rank * kLinBM + 32 * q + lane) * BN + c;
 #pragma unroll
-                  for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
-                  st_global_32(o + 8 * i, u);       // the row's pad takes what lies past N
-                }
-            } else {
-              finish_row32(p.ep, m, n0 + c, v);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t u[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
+              st_global_32(o + 8 * i, u);
             }
+          } else if constexpr (WF32) {
+            finish_rows_f32(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
+          } else {
+            finish_rows(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
           }
         }
       } else {
@@ -599,84 +712,63 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           for (int j = 0; j < 16; ++j) {
             const int row = n0 + c + j;
             if (row < p.N) {
-              if (part) { if (on) part[(int64_t)row * p.ld_partial + m] = v[j]; }
+              if (part) part[(c + j) * kLinBM + 32 * q + lane] = v[j];       // [row][column of the tile]
               else finish_lane(p.ep, row, m, on, v[j], bias);
             }
           }
         }
       }
     }
-  } else if (OB == kOpPacked && warp >= 8) {
-    // ---- converters: rows of x8 (k) x the CTA's 32-column groups (n) -> the MN-major operand.  A warp takes 32 rows of one
-    // group: its lanes' 16-byte chunks then fall on different banks (the swizzle runs over rows), and a lane's 32 codes are
-    // one sector.  Loads run two stages ahead of the decoding.
-    const int ct = tid - 256;
-    const int krow = ct & 63, group = ct >> 6;
-    struct Frag { uint32_t w[8]; int eb; };
-    auto fetch = [&](const LinWalk& w, Frag& f) {
-      const int k = w.kb * kLinBK + krow;
-      const int col = w.n_tile * BN + (int)rank * S::kBNc + group * kGroup;
-      const int have = k < p.K ? min(kGroup, p.N - col) : 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f.w[i] = 0u;
-      f.eb = kExpBias;
-      if (have <= 0) return;
-      const uint8_t* c = p.x8.dev_codes + (int64_t)k * p.x8.ld_codes + col;
-      f.eb = p.x8.dev_exps[(int64_t)k * p.x8.ld_exps + col / kGroup];
-      if (have == kGroup && p.x8_vec) {
-        const uint4 lo = *reinterpret_cast<const uint4*>(c), hi = *(reinterpret_cast<const uint4*>(c) + 1);
-        f.w[0] = lo.x; f.w[1] = lo.y; f.w[2] = lo.z; f.w[3] = lo.w;
-        f.w[4] = hi.x; f.w[5] = hi.y; f.w[6] = hi.z; f.w[7] = hi.w;
-      } else if (have == kGroup) {
-        // any alignment: the 4-byte words that hold the 32 codes, shifted into place (each word read holds one of them)
-        const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(c) & 3);
-        const uint32_t* q = reinterpret_cast<const uint32_t*>(c - off);
-        uint32_t t[9];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = q[i];
-        t[8] = off ? q[8] : 0u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f.w[i] = __funnelshift_r(t[i], t[i + 1], 8 * off);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i)
-          if (i < have) f.w[i >> 2] |= (uint32_t)c[i] << (8 * (i & 3));
-      }
-    };
-    LinWalk ahead(p, first_item, item_step);
-    Frag f0, f1, f2;
-    bool v0 = !ahead.done(), v1 = false, v2 = false;
-    if (v0) { fetch(ahead, f0); ahead.next(p); }
-    v1 = !ahead.done();
-    if (v1) { fetch(ahead, f1); ahead.next(p); }
-    for (uint32_t it = 0; v0; ++it) {
-      v2 = !ahead.done();
-      if (v2) { fetch(ahead, f2); ahead.next(p); }
-      const int s = it % S::kStages;
-      if (!lin_wait_warp(empty + s, ((it / S::kStages) & 1) ^ 1, abort_flag, lane)) break;
-      uint8_t* b = base + s * S::kStage + S::kABytes + (group >> 1) * (kLinBK * 128) + krow * 128;
+  } else if (OB == kOpPacked && warp >= S::kConvWarp0) {
+    // ---- converters: codes and exponents of 64 rows of x8 (k) -> the MN-major operand (n).  A warp takes 32 rows of one group
+    // of 32 columns, a lane one row: its 16-byte accesses, to the codes (swizzled by TMA) and to the operand (swizzled for the
+    // tensor core), then fall on different banks.  The codes come through shared memory and not straight into registers
+    // because the fence before the hand-over waits for a thread's own loads, however far ahead they were issued.
+    if constexpr (OB == kOpPacked) {
+      const int ct = tid - S::kConvWarp0 * 32;
+      const int team = ct / (S::kConvWarps * 32), krow = ct & 63, group = (ct >> 6) & 3;
       const bool bf = p.dtype == LQSGD_BF16;
-      const int e = f0.eb - kExpBias;
-      const bool plain = bf ? f0.eb <= 246 : (e >= -14 && e <= 8);          // the step and every product are normal numbers in range
-      const uint32_t one = bf ? (uint32_t)(e + 127) << 7 : (uint32_t)((e + 15) & 31) << 10;
-      const uint32_t step2 = one | (one << 16);
+      int r = 0, s = 0, turn = 0;
+      uint32_t rpar = 0, spar = 1;                                       // phase parities of the raw ring and of `empty`
+      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p)) {
+        if (turn == team) {
+          if (!lin_wait_warp(raw_full + r, rpar, abort_flag, lane)) break;
+          const uint8_t* raw = base + S::kRawBase + r * S::kRawBytes;
+          const uint4 lo = *reinterpret_cast<const uint4*>(raw + krow * 128 + (((2 * group) ^ (krow & 7)) << 4));
+          const uint4 hi = *reinterpret_cast<const uint4*>(raw + krow * 128 + (((2 * group + 1) ^ (krow & 7)) << 4));
+          const int eb = raw[S::kRawCodes + krow * 16 + (((w.n_tile * BN + (int)rank * S::kBNc) / kGroup + group) & 15)];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(raw_empty + r);
+          const uint32_t cw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+          const int e = eb - kExpBias;
+          // the step, 128 steps (bf16) and every product are normal numbers in range; anything else goes through fp32
+          const bool plain = bf ? eb <= 246 : (e >= -14 && e <= 8);
+          uint32_t o[16];
+          if (!plain) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint4 o;
-        uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+            for (int i = 0; i < 8; ++i) decode4_any(p.dtype, cw[i], eb, o[2 * i], o[2 * i + 1]);
+          } else if (bf) {
+            const uint32_t one = (uint32_t)(e + 127) << 7, off = 0x8000u | ((uint32_t)(e + 127 + 7) << 7);    // 2^e, -128 2^e
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const uint32_t cw = f0.w[2 * i + (h >> 1)];
-          if (!plain) ow[h] = decode2_any(p.dtype, cw, h & 1, f0.eb);
-          else ow[h] = bf ? decode2_bf16(cw, h & 1, step2) : decode2_fp16(cw, h & 1, step2);
+            for (int i = 0; i < 8; ++i) decode4_bf16(cw[i], one | (one << 16), off | (off << 16), o[2 * i], o[2 * i + 1]);
+          } else {
+            const uint32_t one = (uint32_t)(e + 15) << 10;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) decode4_fp16(cw[i], one | (one << 16), o[2 * i], o[2 * i + 1]);
+          }
+          if (!lin_wait_warp(empty + s, spar, abort_flag, lane)) break;
+          uint8_t* b = base + s * S::kStage + S::kABytes + (group >> 1) * (kLinBK * 128) + krow * 128;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(b + ((((group & 1) * 4 + i) ^ (krow & 7)) << 4)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(conv + s, 0)); else mbar_arrive(conv + s); }
         }
-        *reinterpret_cast<uint4*>(b + ((((group & 1) * 4 + i) ^ (krow & 7)) << 4)) = o;
+        if (++turn == S::kTeams) turn = 0;
+        if (++r == S::kRaw) { r = 0; rpar ^= 1; }
+        if (++s == S::kStages) { s = 0; spar ^= 1; }
       }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(conv + s, 0)); else mbar_arrive(conv + s); }
-      f0 = f1; f1 = f2;
-      v0 = v1; v1 = v2;
     }
   }
   lin_fence_before();

@@ -222,7 +222,8 @@ norm_apply_kernel(NormDev d) {
     if (x8.dev_codes) pack_run(x8, d.vec_x8, row, s.col, s.have, on, v);
     if (on) {
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] = act_value(d.act, fmaf(v[j] - mean[j], scale[j], beta[j]));
+      for (int j = 0; j < kRun; ++j) v[j] = fmaf(v[j] - mean[j], scale[j], beta[j]);
+      act_run(d.act, v);
       store_run<DT, kRun>(static_cast<T*>(d.out) + s.sample * d.sample_out + p * d.ld_out + s.col, d.vec_out && s.have == kRun, s.have, v);
     }
     if (d.y8.dev_codes) {
@@ -250,12 +251,15 @@ norm_grad_sums_kernel(NormDev d) {
       float v[kRun], g[kRun];
       load_x<DT>(d, s, p, v);
       load_run<DT, kRun>(static_cast<const T*>(d.dy) + s.sample * d.sample_dy + p * d.ld_dy + s.col, d.vec_dy && s.have == kRun, s.have, g);
+      float h[kRun];
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) { v[j] = (v[j] - mean[j]) * rstd[j]; h[j] = fmaf(v[j], gamma[j], beta[j]); }
+      slope_run(d.act, h);
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {
-        const float xh = (v[j] - mean[j]) * rstd[j];
-        const float dh = g[j] * act_slope(d.act, fmaf(xh, gamma[j], beta[j]));
+        const float dh = g[j] * h[j];
         a[j] += dh;
-        b[j] = fmaf(dh, xh, b[j]);
+        b[j] = fmaf(dh, v[j], b[j]);
       }
     }
   }
@@ -341,12 +345,12 @@ norm_grad_apply_kernel(NormDev d) {
     float v[kRun], g[kRun];
     load_x<DT>(d, s, p, v);
     load_run<DT, kRun>(static_cast<const T*>(d.dy) + s.sample * d.sample_dy + p * d.ld_dy + s.col, d.vec_dy && s.have == kRun, s.have, g);
+    float h[kRun];
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-      const float xh = (v[j] - mean[j]) * rstd[j];
-      const float u = gamma[j] * g[j] * act_slope(d.act, fmaf(xh, gamma[j], beta[j]));
-      v[j] = rstd[j] * (u - c0[j] - xh * c1[j]);
-    }
+    for (int j = 0; j < kRun; ++j) { v[j] = (v[j] - mean[j]) * rstd[j]; h[j] = fmaf(v[j], gamma[j], beta[j]); }
+    slope_run(d.act, h);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) v[j] = rstd[j] * (gamma[j] * g[j] * h[j] - c0[j] - v[j] * c1[j]);
     store_run<DT, kRun>(static_cast<T*>(d.out) + s.sample * d.sample_out + p * d.ld_out + s.col, d.vec_out && s.have == kRun, s.have, v);
   }
 }
