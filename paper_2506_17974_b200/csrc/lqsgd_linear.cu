@@ -9,53 +9,62 @@
 namespace lqsgd {
 namespace {
 
-// Adds the pieces of tiles that several clusters summed, in the order of the clusters, and applies the epilogue.  A unit is 32
-// neighbouring columns of a row of a tile, a column per lane.  `ways` warps (1 or 8) take turns at a unit's pieces and meet
-// in shared memory: with a hundred pieces one warp alone would wait for them one after the other.
+// Adds the pieces of tiles that several clusters summed, in the order of the clusters, and applies the epilogue.  A block takes
+// `rows` rows of a tile, a warp 128 columns of a row at a time (four of them per lane, 32 apart: the loads of a piece are
+// independent).  `ways` warps (1 or 8) take turns at the pieces and meet in shared memory: with a hundred pieces one warp
+// alone would wait for them one after the other.
 struct LinPieces {
   const float* partial;
-  int32_t tiles_m, tiles_n, kb_total, share, cg, bn, swap, ways;
+  uint32_t tiles_m, tiles_n, kb_total, share, cg, bn, rows, ways;
 };
 __global__ void __launch_bounds__(256)
 linear_join_kernel(LinPieces q, LinEpilogue e) {
+  __shared__ float4 sums[8][32];
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t high = q.cg * kLinBM, parts = high / q.rows;
+  const uint32_t t = blockIdx.x / parts, part = blockIdx.x - t * parts;
+  const uint32_t first = t * q.kb_total, g0 = first / q.share, g1 = (first + q.kb_total - 1) / q.share;
+  int m_tile, n_tile;
+  LinWalk::place(q.tiles_m, q.tiles_n, t, m_tile, n_tile);
+  const uint32_t row0 = m_tile * high + part * q.rows;
   train_pdl_wait();
-  __shared__ float sums[8][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int high = q.cg * kLinBM;                                   // rows of a tile; its columns are q.bn, or the other way round
-  const int unit_rows = q.swap ? q.bn : high, unit_groups = (q.swap ? high : q.bn) / 32;
-  const int64_t per_tile = (int64_t)unit_rows * unit_groups, units = (int64_t)q.tiles_m * q.tiles_n * per_tile;
-  const int at_once = 8 / q.ways, sub = warp % q.ways;
-  for (int64_t u0 = (int64_t)blockIdx.x * at_once; u0 < units; u0 += (int64_t)gridDim.x * at_once) {
-    const bool real = u0 + warp / q.ways < units;
-    const int64_t u = real ? u0 + warp / q.ways : 0;
-    const int t = (int)(u / per_tile), in = (int)(u - t * per_tile);
-    const int tr = in / unit_groups, tc = (in - tr * unit_groups) * 32;
-    int m_tile, n_tile;
-    LinWalk::place(q.tiles_m, q.tiles_n, t, m_tile, n_tile);
-    const int64_t row = (int64_t)(q.swap ? n_tile : m_tile) * unit_rows + tr;
-    const int col = (q.swap ? m_tile * high : n_tile * q.bn) + tc + lane;
-    const int64_t first = (int64_t)t * q.kb_total, last = first + q.kb_total - 1;
-    const int g0 = (int)(first / q.share), g1 = (int)(last / q.share);
-    const bool mine = real && g1 > g0 && row < e.rows && col - lane < e.cols;
-    float v = 0.f;
+  if (g0 == g1 || row0 >= (uint32_t)e.rows) return;                 // one cluster had the tile and finished it
+  const size_t tile = (size_t)high * q.bn;
+  const uint32_t sub = warp % q.ways, strips = q.bn / 128, units = q.rows * strips;
+  for (uint32_t u0 = 0; u0 < units; u0 += 8 / q.ways) {
+    const uint32_t u = u0 + warp / q.ways, r = u / strips;
+    const int col = (int)(n_tile * q.bn + (u - r * strips) * 128 + lane);
+    const int64_t row = row0 + r;
+    const bool mine = u < units && row < e.rows;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (mine) {
-      // [row of the tile][bn], with few rows [row][128]: either way rows of the result, a column per lane
-      const float* src = q.partial + (int64_t)tr * (q.swap ? high : q.bn) + tc + lane;
-      const int64_t tile = (int64_t)high * q.bn;
+      const float* src = q.partial + (size_t)(part * q.rows + r) * q.bn + (u - r * strips) * 128 + lane;
 #pragma unroll 4
-      for (int g = g0 + sub; g <= g1; g += q.ways)
-        v += src[(2 * g + ((int64_t)g * q.share < first ? 1 : 0)) * tile];
+      for (uint32_t g = g0 + sub; g <= g1; g += q.ways) {
+        const float* s = src + (2 * g + (g * q.share < first ? 1 : 0)) * tile;
+        v.x += s[0]; v.y += s[32]; v.z += s[64]; v.w += s[96];
+      }
     }
     if (q.ways > 1) {
       sums[warp][lane] = v;
       __syncthreads();
       if (sub == 0) {
-        v = 0.f;
-        for (int k = 0; k < q.ways; ++k) v += sums[warp + k][lane];
+        for (uint32_t k = 1; k < q.ways; ++k) {
+          const float4 w = sums[warp + k][lane];
+          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
       }
       __syncthreads();
     }
-    if (mine && sub == 0) finish_lane(e, row, col, col < e.cols, v, col < e.cols && e.bias ? __ldg(e.bias + col) : 0.f);
+    if (mine && sub == 0) {
+      const float s[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = col + 32 * k;
+        const bool on = c < e.cols;
+        if (c - (int)lane < e.cols) finish_lane(e, row, c, on, s[k], on && e.bias ? __ldg(e.bias + c) : 0.f);
+      }
+    }
   }
 }
 
@@ -120,7 +129,6 @@ int encode_map(CUtensorMap* map, const Stored& s, int box_cols, int box_rows, bo
 
 struct Plan {
   int product;
-  bool swap;                     // few rows: A and B exchanged
   bool packed;                   // B is x8, decoded inside the product's kernel ...
   bool unpacked;                 // ... or before it, into the workspace
   int cg, bn;
@@ -130,11 +138,10 @@ struct Plan {
   size_t off_a, off_b, off_e, off_x, off_partial, bytes;
 };
 
-constexpr int64_t kFewRows = 64;       // at most this many rows: the weights are the operand that is streamed
 constexpr int kSms = 148;              // sums are cut for this many SMs whatever the card has: results do not depend on it
 
 // Microseconds: one k block of a tile, and what a tile costs besides (filling the pipeline, draining the accumulator).
-double block_us(int cg, int bn) { return cg == 2 ? 0.32 : (bn >= 128 ? 0.24 : 0.13); }
+double block_us(int cg) { return cg == 2 ? 0.32 : 0.24; }
 constexpr double kTileUs = 2.0, kJoinUs = 3.0;
 constexpr int kDecodeFirstTiles = 4;
 
@@ -143,7 +150,6 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   p.product = product;
   const int64_t rows = a.rows;
   const Stored x = {a.dev_x, rows, a.in, a.ld_x}, w = {a.dev_w, a.out, a.in, a.ld_w}, dz = {a.dev_dz, rows, a.out, a.ld_dz};
-  p.swap = product != LQSGD_LINEAR_GRAD_WEIGHT && rows <= kFewRows;
   if (product == LQSGD_LINEAR_FORWARD) {
     p.a = x; p.b = w; p.M = rows; p.N = a.out; p.K = a.in;
   } else if (product == LQSGD_LINEAR_GRAD_INPUT) {
@@ -156,14 +162,13 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
       p.e = {a.x8.dev_exps, rows, ceil_div64(a.in, kGroup), a.x8.ld_exps, 1};
     }
   }
-  if (p.swap) { std::swap(p.a, p.b); std::swap(p.M, p.N); }
   p.kb_total = (int)ceil_div64(p.K, kLinBK);
   double best = 1e30;
   auto consider = [&](int cg, int bn) {
     const int64_t tm = ceil_div64(p.M, (int64_t)kLinBM * cg), tn = ceil_div64(p.N, bn), tiles = tm * tn;
     if (tiles > (1 << 28)) return;
     const int units = kSms / cg;
-    const double per = block_us(cg, bn);
+    const double per = block_us(cg);
     auto take = [&](double t, int64_t share, int64_t clusters) {
       if (t >= best) return;
       best = t;
@@ -172,18 +177,14 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
     take(ceil_div64(tiles, units) * (kTileUs + p.kb_total * per), 0, std::min<int64_t>(tiles, units));
     // equal shares of at least 4 k blocks each, where tiles are few
     const int64_t pairs = tiles * p.kb_total;
-    if (tiles >= 2 * units || p.kb_total < 8) return;
+    if (tiles >= 2 * units || p.kb_total < 8 || pairs >= (1ll << 31)) return;
     const int64_t share = std::max<int64_t>(4, ceil_div64(pairs, units)), clusters = ceil_div64(pairs, share);
     if (clusters <= tiles && share % p.kb_total == 0) return;
     const double bytes = 4.0 * kLinBM * cg * bn * (double)clusters;
     take(kTileUs * (share >= p.kb_total ? 2 : 1) + share * per + kJoinUs + bytes / 2.0e6, share, clusters);
   };
-  if (p.swap) {
-    consider(1, p.N <= 16 ? 16 : (p.N <= 32 ? 32 : 64));
-  } else {
-    consider(1, 128);
-    consider(2, 256);
-  }
+  consider(1, 128);
+  consider(2, 256);
   if (best > 1e29) return LQSGD_ERR_BAD_SHAPE;
   size_t off = 0;
   auto room = [&](size_t n) { const size_t at = off; off += (n + 255) / 256 * 256; return at; };
@@ -233,10 +234,10 @@ int place(Stored* s, char* ws, size_t off, cudaStream_t st) {
   return LQSGD_OK;
 }
 
-template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
+template <int CG, int BN, int OA, int OB, bool WF32>
 int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
-  using S = LinCfg<CG, BN, OA, OB, SWAP, WF32>;
-  auto kernel = linear_kernel<CG, BN, OA, OB, SWAP, WF32>;
+  using S = LinCfg<CG, BN, OA, OB, WF32>;
+  auto kernel = linear_kernel<CG, BN, OA, OB, WF32>;
   static std::atomic<uint64_t> ready{0};                     // devices on which the kernel may use its shared memory
   int dev = 0;
   TRAIN_CK(cudaGetDevice(&dev), "cudaGetDevice");
@@ -244,7 +245,8 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
     TRAIN_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem), "cudaFuncSetAttribute(linear_kernel)");
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
-  int rc = encode_map(&q.ta, p.a, 64, OA == kOpK ? kLinBM : kLinBK, true);
+  q.box_a = OA == kOpK ? (uint32_t)std::min<int64_t>(kLinBM, ceil_div64(p.M, 8) * 8) : kLinBM;
+  int rc = encode_map(&q.ta, p.a, 64, OA == kOpK ? (int)q.box_a : kLinBK, true);
   if (rc != LQSGD_OK) return rc;
   if (OB == kOpPacked) {
     if ((rc = encode_map(&q.tb, p.b, 128, kLinBK, true)) != LQSGD_OK || (rc = encode_map(&q.te, p.e, 16, kLinBK, false)) != LQSGD_OK) return rc;
@@ -288,24 +290,22 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total; q.share = p.share;
   q.dtype = a.dtype;
   q.status = a.dev_status;
-  if (product == LQSGD_LINEAR_FORWARD) {
-    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpK, kOpK, true, false>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpK, kOpK, true, false>(p, q, st) : launch<1, 64, kOpK, kOpK, true, false>(p, q, st);
-    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false, false>(p, q, st);
-  } else if (product == LQSGD_LINEAR_GRAD_INPUT) {
-    if (p.swap) rc = p.bn == 16 ? launch<1, 16, kOpMN, kOpK, true, false>(p, q, st) : p.bn == 32 ? launch<1, 32, kOpMN, kOpK, true, false>(p, q, st) : launch<1, 64, kOpMN, kOpK, true, false>(p, q, st);
-    else rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false, false>(p, q, st);
-  } else if (p.packed) {
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpPacked, false, true>(p, q, st) : launch<1, 128, kOpMN, kOpPacked, false, true>(p, q, st);
-  } else {
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, false, true>(p, q, st) : launch<1, 128, kOpMN, kOpMN, false, true>(p, q, st);
-  }
+  if (product == LQSGD_LINEAR_FORWARD)
+    rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false>(p, q, st);
+  else if (product == LQSGD_LINEAR_GRAD_INPUT)
+    rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false>(p, q, st);
+  else if (p.packed)
+    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpPacked, true>(p, q, st) : launch<1, 128, kOpMN, kOpPacked, true>(p, q, st);
+  else
+    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, true>(p, q, st) : launch<1, 128, kOpMN, kOpMN, true>(p, q, st);
   if (rc != LQSGD_OK) return rc;
   if (p.share) {
     const int most = (int)((p.kb_total - 1) / p.share + 2);           // pieces of one tile
-    LinPieces j = {q.partial, p.tiles_m, p.tiles_n, p.kb_total, p.share, p.cg, p.bn, p.swap ? 1 : 0, most >= 16 ? 8 : 1};
-    const int64_t units = (int64_t)p.tiles_m * p.tiles_n * kLinBM * p.cg * p.bn / 32;
-    const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div64(units, 8 / j.ways), kSms * 8);
-    TRAIN_CK(train_launch(linear_join_kernel, dim3(blocks), dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
+    const uint32_t tiles = (uint32_t)p.tiles_m * p.tiles_n, high = kLinBM * p.cg, ways = most >= 16 ? 8 : 1;
+    uint32_t rows = ways == 8 ? 8 : 32;                               // fewer per block until the card is full
+    while (rows > (ways == 8 ? 1u : 8u) && tiles * (high / rows) < kSms * 4) rows /= 2;
+    const LinPieces j = {q.partial, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.kb_total, (uint32_t)p.share, (uint32_t)p.cg, (uint32_t)p.bn, rows, ways};
+    TRAIN_CK(train_launch(linear_join_kernel, dim3(tiles * (high / rows)), dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
   }
   return LQSGD_OK;
 }

@@ -5,7 +5,6 @@
 //   forward        x    [rows]         w   [out]              in                   A: k    B: k
 //   grad_input     dz   [rows]         w^T [in]               out                  A: k    B: n
 //   grad_weight    dz^T [out]          x^T [in]               rows                 A: m    B: n
-//   few rows       w or w^T            x or dz                in / out             the first two with A and B exchanged
 //
 // An operand whose rows hold k ("K-major") is staged as 64 k x R rows; one whose rows hold m or n ("MN-major") as blocks of
 // 64 columns x 64 k: both arrive from TMA with the 128-byte swizzle that the tensor core reads, so nothing is transposed.
@@ -14,7 +13,7 @@
 //
 // A cluster of CG CTAs (1 or 2) works on a tile of 128 CG x BN: with CG = 2 each SM holds 128 rows of A and half of B's, and
 // one tcgen05.mma.cta_group::2 drives both tensor cores, so that an SM fetches (128 + BN / 2) rows per k instead of
-// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 (4-7 with few rows) drain the
+// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 (4-7 for a weight gradient) drain the
 // accumulator (two of them, so that the next tile's sum runs under the epilogue); with x8 warp 3 loads its codes and the last
 // eight warps decode them.  Clusters walk
 // the work items (tile, piece of the sum) with a fixed stride.
@@ -57,6 +56,8 @@ struct alignas(64) LinProblem {
   int32_t tiles_m, tiles_n, kb_total;
   int32_t share;                       // 0: clusters take whole tiles; otherwise every cluster takes this many k-blocks in a row
   int32_t dtype;                       // of the operands
+  uint32_t box_a;                      // rows of A that TMA brings per stage and CTA: 128, fewer (a multiple of 8) where A has fewer and
+                                       // they lie along k; what the stage holds beyond them only meets rows that do not exist
   uint32_t* status;
 };
 
@@ -150,17 +151,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&f)[16]) {
-  uint32_t v[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n tcgen05.wait::ld.sync.aligned;"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-      : "r"(taddr) : "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
-}
-
 // ---- 16-bit words of either operand type
 __device__ __forceinline__ uint32_t pack2(int dtype, float lo, float hi) {
   if (dtype == LQSGD_BF16) {
@@ -407,43 +397,36 @@ __device__ __forceinline__ void decode4_any(int dtype, uint32_t w, int eb, uint3
 // workspace (at most two per cluster: piece 2 g where its share begins, 2 g + 1 for a tile that its share ends
 // inside of), and linear_join_kernel adds a tile's pieces in the order of the clusters.
 struct LinWalk {
-  int64_t pos, end;                    // equal shares: pairs; whole tiles: tiles
-  int64_t begin;
-  int stride, cluster;
+  uint32_t pos, end, begin;            // equal shares: pairs (fewer than 2^31); whole tiles: tiles
+  uint32_t stride;
+  int cluster;
   int kb, kb_end;                      // the k blocks of the current tile that are this cluster's
   int m_tile, n_tile;
   // Tiles are taken in bands of 8 rows of tiles, column by column: the clusters at work then share 8 row tiles and
   // about as many column tiles, which keeps their operands in L2.
-  static __device__ __forceinline__ void place(int tiles_m, int tiles_n, int t, int& m_tile, int& n_tile) {
-    constexpr int kBand = 8;
-    const int band = t / (kBand * tiles_n), first = band * kBand, high = min(kBand, tiles_m - first);
-    const int in = t - band * kBand * tiles_n;
-    m_tile = first + in % high;
-    n_tile = in / high;
+  static __device__ __forceinline__ void place(uint32_t tiles_m, uint32_t tiles_n, uint32_t t, int& m_tile, int& n_tile) {
+    constexpr uint32_t kBand = 8;
+    const uint32_t band = t / (kBand * tiles_n), first = band * kBand, high = min(kBand, tiles_m - first);
+    const uint32_t in = t - band * kBand * tiles_n;
+    n_tile = (int)(in / high);
+    m_tile = (int)(first + in - n_tile * high);
   }
   __device__ __forceinline__ void locate(const LinProblem& p) {
-    int t;
+    uint32_t t = pos;
+    kb = 0;
+    kb_end = p.kb_total;
     if (p.share) {
-      t = (int)(pos / p.kb_total);
-      kb = (int)(pos - (int64_t)t * p.kb_total);
-      kb_end = (int)min((int64_t)p.kb_total, kb + (end - pos));
-    } else {
-      t = (int)pos;
-      kb = 0;
-      kb_end = p.kb_total;
+      t = pos / (uint32_t)p.kb_total;
+      kb = (int)(pos - t * p.kb_total);
+      kb_end = min(p.kb_total, kb + (int)(end - pos));
     }
     place(p.tiles_m, p.tiles_n, t, m_tile, n_tile);
   }
   __device__ __forceinline__ LinWalk(const LinProblem& p, int g, int clusters) : cluster(g) {
-    if (p.share) {
-      pos = (int64_t)g * p.share;
-      end = min((int64_t)p.tiles_m * p.tiles_n * p.kb_total, pos + p.share);
-      stride = 0;
-    } else {
-      pos = g;
-      end = (int64_t)p.tiles_m * p.tiles_n;
-      stride = clusters;
-    }
+    const uint32_t tiles = p.tiles_m * p.tiles_n;
+    pos = p.share ? (uint32_t)g * p.share : (uint32_t)g;
+    end = p.share ? min(tiles * p.kb_total, pos + p.share) : tiles;
+    stride = clusters;
     begin = pos;
     if (pos < end) locate(p);
   }
@@ -452,10 +435,9 @@ struct LinWalk {
   __device__ __forceinline__ int piece(const LinProblem& p) const {
     return kb_end - kb == p.kb_total ? -1 : (pos == begin ? 2 * cluster : 2 * cluster + 1);
   }
-  __device__ __forceinline__ int blocks() const { return kb_end - kb; }
   // To the next tile; only from the state locate() left (next() below moves kb).
   __device__ __forceinline__ void next_tile(const LinProblem& p) {
-    pos += p.share ? kb_end - kb : stride;
+    pos += p.share ? (uint32_t)(kb_end - kb) : stride;
     if (pos < end) locate(p);
   }
   // To the next k block, of this tile or the next.
@@ -468,8 +450,8 @@ struct LinWalk {
   }
 };
 
-// WF32: the result is fp32 (a weight gradient); SWAP: few rows.
-template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
+// WF32: the result is fp32 (a weight gradient).
+template <int CG, int BN, int OA, int OB, bool WF32>
 struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
@@ -477,13 +459,13 @@ struct LinCfg {
   // a packed B passes through a second, small ring: 64 rows of kBNc codes and of the 16 exponents that hold the tile's
   static constexpr int kRaw = OB == kOpPacked ? 4 : 0;
   static constexpr uint32_t kRawCodes = kLinBK * kBNc, kRawBytes = kRawCodes + kLinBK * 16;
-  static constexpr uint32_t kScratch = SWAP ? 0 : (WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16);   // one per epilogue warp
+  static constexpr uint32_t kScratch = WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16;   // one per epilogue warp
   static constexpr uint32_t kRoom = 225u * 1024 - kRaw * kRawBytes - kScratch;
   static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
-  static constexpr uint32_t kTxBytes = CG * (kABytes + (OB == kOpPacked ? 0 : kBBytes));
+  static constexpr uint32_t kTxB = OB == kOpPacked ? 0 : kBBytes;         // what TMA brings of B per stage and CTA
   // Two warps per quarter of tensor memory where the epilogue computes per value (GELU and the 8-bit form take as
   // long as the product of a 4096-wide layer with one).
-  static constexpr int kEpiWarps = SWAP || WF32 ? 4 : 8;
+  static constexpr int kEpiWarps = WF32 ? 4 : 8;
   // A thread decodes 32 codes of one row of x; two teams of warps take the stages in turn, because one team's
   // chain of waits, loads, decoding and hand-over (about 700 cycles) is longer than a stage's MMAs (512).
   static constexpr int kTeams = 2;
@@ -501,11 +483,10 @@ struct LinCfg {
   static_assert(OB != kOpPacked || kBNc == 128, "a row of codes is one 128-byte swizzle span");
 };
 
-// SWAP: A's rows are the result's columns (few rows); otherwise A's rows are its rows.
-template <int CG, int BN, int OA, int OB, bool SWAP, bool WF32>
-__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB, SWAP, WF32>::kThreads, 1)
+template <int CG, int BN, int OA, int OB, bool WF32>
+__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB, WF32>::kThreads, 1)
 linear_kernel(const __grid_constant__ LinProblem p) {
-  using S = LinCfg<CG, BN, OA, OB, SWAP, WF32>;
+  using S = LinCfg<CG, BN, OA, OB, WF32>;
   extern __shared__ uint8_t lin_smem[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(lin_smem) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(base + S::kBarOff);   // [stages] TMA bytes landed, in both CTAs (first CTA's barrier)
@@ -568,7 +549,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
         if (!lin_wait(empty + s, ((it / S::kStages) & 1) ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* a = base + s * S::kStage;
         uint8_t* b = a + S::kABytes;
-        if (rank == 0) mbar_arrive_expect_tx(full + s, S::kTxBytes);
+        if (rank == 0) mbar_arrive_expect_tx(full + s, CG * (p.box_a * 128 + S::kTxB));
         const uint32_t bar = CG == 2 ? map_to(full + s, 0) : smem_u32(full + s);
         const int k0 = w.kb * kLinBK, m0 = (w.m_tile * CG + (int)rank) * kLinBM;
         if constexpr (OA == kOpK) {
@@ -662,60 +643,36 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       const int n0 = w.n_tile * BN;
       const int piece = w.piece(p);
       float* part = piece >= 0 ? p.partial + (int64_t)piece * (CG * kLinBM * BN) : nullptr;
-      if constexpr (!SWAP) {
-        constexpr int kStep = 32, kMine = BN / (S::kEpiWarps / 4);
-        const int c0 = ((warp - 4) >> 2) * kMine;
-        float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * (WF32 ? kScratchBytes : kScratchBytes16));
+      constexpr int kStep = 32, kMine = BN / (S::kEpiWarps / 4);
+      const int c0 = ((warp - 4) >> 2) * kMine;
+      float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * (WF32 ? kScratchBytes : kScratchBytes16));
 #pragma unroll 1
-        for (int c = c0; c < c0 + kMine; c += kStep) {
-          float v[32];
-          tmem_ld32(taddr + c, v);
-          if (c + kStep >= c0 + kMine) {            // the accumulator is in registers: hand it back
-            lin_fence_before();
-            __syncwarp();
-            if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
-          }
-          if (n0 + c >= p.N || m - lane >= p.M) continue;
-          if constexpr (OB == kOpPacked) {          // back from the order of the decoder
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) { const float t = v[j + 1]; v[j + 1] = v[j + 2]; v[j + 2] = t; }
-          }
-          if (part) {                               // [row of the tile][BN]
-            float* o = part + (int64_t)((int)rank * kLinBM + 32 * q + lane) * BN + c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t u[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
-              st_global_32(o + 8 * i, u);
-            }
-          } else if constexpr (WF32) {
-            finish_rows_f32(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
-          } else {
-            finish_rows(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
-          }
+      for (int c = c0; c < c0 + kMine; c += kStep) {
+        float v[32];
+        tmem_ld32(taddr + c, v);
+        if (c + kStep >= c0 + kMine) {            // the accumulator is in registers: hand it back
+          lin_fence_before();
+          __syncwarp();
+          if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
         }
-      } else {
-        const bool on = m < p.M;
-        const float bias = (!part && p.ep.bias && on) ? __ldg(p.ep.bias + m) : 0.f;
-#pragma unroll 1
-        for (int c = 0; c < BN; c += 16) {
-          float v[16];
-          tmem_ld16(taddr + c, v);
-          if (c + 16 >= BN) {
-            lin_fence_before();
-            __syncwarp();
-            if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
-          }
-          if (m - lane >= p.M) continue;            // none of the warp's columns exists
+        if (n0 + c >= p.N || m - lane >= p.M) continue;
+        if constexpr (OB == kOpPacked) {          // back from the order of the decoder
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int row = n0 + c + j;
-            if (row < p.N) {
-              if (part) part[(c + j) * kLinBM + 32 * q + lane] = v[j];       // [row][column of the tile]
-              else finish_lane(p.ep, row, m, on, v[j], bias);
-            }
+          for (int j = 0; j < 32; j += 4) { const float t = v[j + 1]; v[j + 1] = v[j + 2]; v[j + 2] = t; }
+        }
+        if (part) {                               // [row of the tile][BN]
+          float* o = part + (int64_t)((int)rank * kLinBM + 32 * q + lane) * BN + c;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t u[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
+            st_global_32(o + 8 * i, u);
           }
+        } else if constexpr (WF32) {
+          finish_rows_f32(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
+        } else {
+          finish_rows(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
         }
       }
     }
