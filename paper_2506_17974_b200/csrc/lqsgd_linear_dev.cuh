@@ -93,14 +93,30 @@ __device__ __forceinline__ bool lin_wait_warp(uint64_t* b, uint32_t parity, vola
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
+// For the loader and MMA warps, whose instructions take uniform operands: the whole warp waits and walks, one elected lane
+// issues.  Inside `if (lane == 0)` every operand would first be moved from the lane's registers (a k block cost its lone
+// thread about 690 cycles that way, more than the 512 of its MMAs).
+__device__ __forceinline__ bool lin_wait_all(uint32_t bar, uint64_t* b, uint32_t parity, volatile int* abort_flag) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  if (__all_sync(0xffffffffu, ok)) return true;
+  return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag));
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+  return ok != 0;
+}
+
 template <int CG>
-__device__ __forceinline__ void lin_tma(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+__device__ __forceinline__ void lin_tma(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   if constexpr (CG == 2)
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
   else
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void lin_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -113,12 +129,12 @@ __device__ __forceinline__ void lin_mma(uint32_t d, uint64_t a, uint64_t b, uint
 }
 // Arrives, once every MMA issued so far has completed, on the barrier at this offset in every CTA of the cluster.
 template <int CG>
-__device__ __forceinline__ void lin_commit(uint64_t* bar) {
+__device__ __forceinline__ void lin_commit(uint32_t bar) {
   if constexpr (CG == 2)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
   else
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void lin_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void lin_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -536,29 +552,30 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   if constexpr (CG == 2) cluster_sync_all();
   lin_fence_after();
   const uint32_t tmem = *tmem_slot;
-  train_pdl_wait();
   train_pdl_trigger();
+  // Every role first finds its place in the work, then waits for the kernel in front.
+  const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), conv_s = smem_u32(conv), empty_s = smem_u32(empty);
 
   if (warp == 0) {
-    // ---- loader: one thread
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p), ++it) {
-        const int s = it % S::kStages;
-        if (!lin_wait(empty + s, ((it / S::kStages) & 1) ^ 1, abort_flag)) { ok = false; break; }
-        uint8_t* a = base + s * S::kStage;
-        uint8_t* b = a + S::kABytes;
-        if (rank == 0) mbar_arrive_expect_tx(full + s, CG * (p.box_a * 128 + S::kTxB));
-        const uint32_t bar = CG == 2 ? map_to(full + s, 0) : smem_u32(full + s);
-        const int k0 = w.kb * kLinBK, m0 = (w.m_tile * CG + (int)rank) * kLinBM;
+    // ---- loader
+    LinWalk w(p, cluster, clusters);
+    train_pdl_wait();
+    const uint32_t full0 = CG == 2 ? map_to(full, 0) : full_s;          // the first CTA's barriers count both CTAs' bytes
+    const uint32_t tx = CG * (p.box_a * 128 + S::kTxB);
+    uint32_t s = 0, turn = 0, it = 0;
+    bool ok = true;
+    for (; !w.done(); w.next(p), ++it) {
+      if (!lin_wait_all(empty_s + 8 * s, empty + s, turn ^ 1, abort_flag)) { ok = false; break; }
+      const uint32_t a = base_s + s * S::kStage, b = a + S::kABytes, bar = full0 + 8 * s;
+      const int k0 = w.kb * kLinBK, m0 = (w.m_tile * CG + (int)rank) * kLinBM, n0 = w.n_tile * BN + (int)rank * S::kBNc;
+      if (elect_one()) {
+        if (rank == 0) mbar_arrive_expect_tx(full + s, tx);
         if constexpr (OA == kOpK) {
           lin_tma<CG>(a, &p.ta, k0, m0, bar);
         } else {
 #pragma unroll
           for (int i = 0; i < kLinBM / 64; ++i) lin_tma<CG>(a + i * kLinBK * 128, &p.ta, m0 + 64 * i, k0, bar);
         }
-        const int n0 = w.n_tile * BN + (int)rank * S::kBNc;
         if constexpr (OB == kOpK) {
           lin_tma<CG>(b, &p.tb, k0, n0, bar);
         } else if constexpr (OB == kOpMN) {
@@ -566,47 +583,60 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           for (int i = 0; i < S::kBNc / 64; ++i) lin_tma<CG>(b + i * kLinBK * 128, &p.tb, n0 + 64 * i, k0, bar);
         }
       }
-      if (!ok && rank == 0) {                       // copies in flight land before the CTA's memory goes away
-        const uint32_t limit = wait_limit_of(abort_flag);
-        for (uint32_t j = it > (uint32_t)S::kStages ? it - S::kStages : 0; j < it; ++j)
-          for (uint32_t i = 0; i < limit && !mbar_try(full + j % S::kStages, (j / S::kStages) & 1); ++i) {}
-      }
+      __syncwarp();
+      if (++s == S::kStages) { s = 0; turn ^= 1; }
+    }
+    if (!ok && rank == 0 && lane == 0) {            // copies in flight land before the CTA's memory goes away
+      const uint32_t limit = wait_limit_of(abort_flag);
+      for (uint32_t j = it > (uint32_t)S::kStages ? it - S::kStages : 0; j < it; ++j)
+        for (uint32_t i = 0; i < limit && !mbar_try(full + j % S::kStages, (j / S::kStages) & 1); ++i) {}
     }
     __syncwarp();
   } else if (warp == 1) {
-    // ---- MMA issue: one thread of the cluster's first CTA
-    if (rank == 0 && lane == 0) {
+    // ---- MMA issue: the cluster's first CTA
+    if (rank == 0) {
       const uint32_t fmt = p.dtype == LQSGD_BF16 ? 1u : 0u;
       // fp32 accumulator, operand type, which operands are MN-major, N / 8, M / 16
       const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((OA == kOpK ? 0u : 1u) << 15) | ((OB == kOpK ? 0u : 1u) << 16) |
                              ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((kLinBM * CG) >> 4) << 24);
-      uint32_t it = 0, seq = 0;
+      const uint64_t ad0 = lin_desc<OA != kOpK>(base_s), bd0 = lin_desc<OB != kOpK>(base_s + S::kABytes);
+      const uint32_t d_full_s = smem_u32(d_full), d_empty_s = smem_u32(d_empty);
+      uint32_t s = 0, turn = 0, db = 0, dturn = 0;
       bool ok = true;
-      for (LinWalk w(p, cluster, clusters); !w.done() && ok; w.next_tile(p), ++seq) {
-        const uint32_t db = seq & 1;
-        if (!lin_wait(d_empty + db, ((seq >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+      LinWalk w(p, cluster, clusters);
+      for (; !w.done() && ok; w.next_tile(p)) {
+        if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
         lin_fence_after();
         const uint32_t d = tmem + db * BN;
-        for (int kb = w.kb; kb < w.kb_end; ++kb, ++it) {
-          const int s = it % S::kStages;
-          if (!lin_wait(full + s, (it / S::kStages) & 1, abort_flag)) { ok = false; break; }
+        uint32_t more = 0;                          // the tile's first product starts the sum
+        for (int kb = w.kb; kb < w.kb_end; ++kb) {
+          if (!lin_wait_all(full_s + 8 * s, full + s, turn, abort_flag)) { ok = false; break; }
           if constexpr (OB == kOpPacked) {
-            if (!lin_wait(conv + s, (it / S::kStages) & 1, abort_flag)) { ok = false; break; }
+            if (!lin_wait_all(conv_s + 8 * s, conv + s, turn, abort_flag)) { ok = false; break; }
           }
           lin_fence_after();
-          const uint64_t ad = lin_desc<OA != kOpK>(smem_u32(base + s * S::kStage));
-          const uint64_t bd = lin_desc<OB != kOpK>(smem_u32(base + s * S::kStage + S::kABytes));
+          const uint64_t ad = ad0 + (uint64_t)(s * (S::kStage >> 4)), bd = bd0 + (uint64_t)(s * (S::kStage >> 4));
+          if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < kLinBK / 16; ++ks)
-            lin_mma<CG>(d, ad + ((ks * lin_kstep<OA != kOpK>()) >> 4), bd + ((ks * lin_kstep<OB != kOpK>()) >> 4), idesc,
-                        (kb > w.kb || ks > 0) ? 1u : 0u);
-          lin_commit<CG>(empty + s);
+            for (int ks = 0; ks < kLinBK / 16; ++ks)
+              lin_mma<CG>(d, ad + ((ks * lin_kstep<OA != kOpK>()) >> 4), bd + ((ks * lin_kstep<OB != kOpK>()) >> 4), idesc, ks > 0 ? 1u : more);
+            lin_commit<CG>(empty_s + 8 * s);
+          }
+          __syncwarp();
+          more = 1;
+          if (++s == S::kStages) { s = 0; turn ^= 1; }
         }
-        if (ok) lin_commit<CG>(d_full + db);
+        if (ok && elect_one()) lin_commit<CG>(d_full_s + 8 * db);
+        __syncwarp();
+        db ^= 1;
+        if (db == 0) dturn ^= 1;
       }
-      lin_commit<CG>(fin);                          // every MMA has completed before tensor memory is released
-      const uint32_t limit = wait_limit_of(abort_flag);
-      for (uint32_t i = 0; i < limit && !mbar_try(fin, 0); ++i) {}
+      if (elect_one()) lin_commit<CG>(smem_u32(fin));   // every MMA has completed before tensor memory is released
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t limit = wait_limit_of(abort_flag);
+        for (uint32_t i = 0; i < limit && !mbar_try(fin, 0); ++i) {}
+      }
     }
     __syncwarp();
   } else if (OB == kOpPacked && warp == 3) {
@@ -614,14 +644,16 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     if constexpr (OB == kOpPacked) if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p), ++it) {
+      LinWalk w(p, cluster, clusters);
+      train_pdl_wait();
+      for (; !w.done(); w.next(p), ++it) {
         const int r = it % S::kRaw;
         if (!lin_wait(raw_empty + r, ((it / S::kRaw) & 1) ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* raw = base + S::kRawBase + r * S::kRawBytes;
         const int k0 = w.kb * kLinBK, n0 = w.n_tile * BN + (int)rank * S::kBNc;
         mbar_arrive_expect_tx(raw_full + r, S::kRawBytes);
-        lin_tma<1>(raw, &p.tb, n0, k0, smem_u32(raw_full + r));
-        lin_tma<1>(raw + S::kRawCodes, &p.te, n0 / kGroup / 16 * 16, k0, smem_u32(raw_full + r));
+        lin_tma<1>(smem_u32(raw), &p.tb, n0, k0, smem_u32(raw_full + r));
+        lin_tma<1>(smem_u32(raw) + S::kRawCodes, &p.te, n0 / kGroup / 16 * 16, k0, smem_u32(raw_full + r));
       }
       if (!ok) {
         const uint32_t limit = wait_limit_of(abort_flag);
@@ -634,7 +666,9 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     // ---- epilogue: a warp reads its quarter of the accumulator's rows (warp % 4), and with eight warps half of its columns
     uint32_t seq = 0;
     const int q = warp & 3;
-    for (LinWalk w(p, cluster, clusters); !w.done(); w.next_tile(p), ++seq) {
+    LinWalk w(p, cluster, clusters);
+    train_pdl_wait();
+    for (; !w.done(); w.next_tile(p), ++seq) {
       const uint32_t db = seq & 1;
       if (!lin_wait_warp(d_full + db, (seq >> 1) & 1, abort_flag, lane)) break;
       lin_fence_after();
