@@ -10,82 +10,67 @@ namespace lqsgd {
 namespace {
 
 // Adds the pieces of tiles that several clusters summed, in the order of the clusters, and applies the epilogue.  A block takes
-// `rows` rows of a tile, a warp 128 columns of a row at a time (four of them per lane, 32 apart: the loads of a piece are
-// independent).  `ways` warps (1 or 8) take turns at the pieces and meet in shared memory: with a hundred pieces one warp
-// alone would wait for them one after the other.
+// `rows` rows of a tile, a warp 128 columns of a row.  With many pieces the block's 8 warps take turns at them (WAYS = 8) and
+// meet in shared memory: one warp alone would wait for them one after the other.
 struct LinPieces {
   const float* partial;
-  uint32_t tiles_m, tiles_n, kb_total, share, cg, bn, rows, ways;
+  uint32_t tiles_m, tiles_n, kb_total, share, cg, bn, rows;
 };
+template <uint32_t WAYS>
 __global__ void __launch_bounds__(256)
 linear_join_kernel(LinPieces q, LinEpilogue e) {
   __shared__ float4 sums[8][32];
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t high = q.cg * kLinBM, parts = high / q.rows;
-  const uint32_t t = blockIdx.x / parts, part = blockIdx.x - t * parts;
-  const uint32_t first = t * q.kb_total, g0 = first / q.share, g1 = (first + q.kb_total - 1) / q.share;
+  const uint32_t t = quick_div(blockIdx.x, parts), part = blockIdx.x - t * parts;
+  const uint32_t first = t * q.kb_total, g0 = quick_div(first, q.share), g1 = quick_div(first + q.kb_total - 1, q.share);
   int m_tile, n_tile;
   LinWalk::place(q.tiles_m, q.tiles_n, t, m_tile, n_tile);
   const uint32_t row0 = m_tile * high + part * q.rows;
   train_pdl_wait();
   if (g0 == g1 || row0 >= (uint32_t)e.rows) return;                 // one cluster had the tile and finished it
   const size_t tile = (size_t)high * q.bn;
-  const uint32_t sub = warp % q.ways, strips = q.bn / 128, units = q.rows * strips;
-  for (uint32_t u0 = 0; u0 < units; u0 += 8 / q.ways) {
-    const uint32_t u = u0 + warp / q.ways, r = u / strips;
-    const int col = (int)(n_tile * q.bn + (u - r * strips) * 128 + lane);
+  const uint32_t sub = warp % WAYS, strips = q.bn / 128, units = q.rows * strips;
+  for (uint32_t u0 = 0; u0 < units; u0 += 8 / WAYS) {
+    const uint32_t u = u0 + warp / WAYS, r = u / strips, strip = u - r * strips;
     const int64_t row = row0 + r;
-    const bool mine = u < units && row < e.rows;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool mine = u < units && row < e.rows && (int)(n_tile * q.bn + strip * 128) < e.cols;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (mine) {
-      const float* src = q.partial + (size_t)(part * q.rows + r) * q.bn + (u - r * strips) * 128 + lane;
-#pragma unroll 4
-      for (uint32_t g = g0 + sub; g <= g1; g += q.ways) {
-        const float* s = src + (2 * g + (g * q.share < first ? 1 : 0)) * tile;
-        v.x += s[0]; v.y += s[32]; v.z += s[64]; v.w += s[96];
+      const float* src = q.partial + (size_t)(part * q.rows + r) * q.bn + strip * 128 + 4 * lane;
+#pragma unroll 6
+      for (uint32_t g = g0 + sub; g <= g1; g += WAYS) {
+        const float4 s = *reinterpret_cast<const float4*>(src + (2 * g + (g * q.share < first ? 1 : 0)) * tile);
+        v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
       }
     }
-    if (q.ways > 1) {
-      sums[warp][lane] = v;
+    if (WAYS > 1) {
+      sums[warp][lane] = make_float4(v[0], v[1], v[2], v[3]);
       __syncthreads();
-      if (sub == 0) {
-        for (uint32_t k = 1; k < q.ways; ++k) {
-          const float4 w = sums[warp + k][lane];
-          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+      if (sub == 0)
+        for (uint32_t k = 1; k < WAYS; ++k) {
+          const float4 s = sums[warp + k][lane];
+          v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
         }
-      }
       __syncthreads();
     }
-    if (mine && sub == 0) {
-      const float s[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = col + 32 * k;
-        const bool on = c < e.cols;
-        if (c - (int)lane < e.cols) finish_lane(e, row, c, on, s[k], on && e.bias ? __ldg(e.bias + c) : 0.f);
-      }
-    }
+    if (mine && sub == 0) finish_quad(e, row, n_tile * q.bn + strip * 128 + 4 * lane, v);
   }
 }
 
 // Copies a matrix whose rows TMA cannot address (base or row distance not a multiple of 16 bytes) to rows of ld_dst elements, a
 // multiple of 16 bytes; what lies past cols is never read.
-template <typename T>
 __global__ void __launch_bounds__(256)
-realign_kernel(const T* __restrict__ src, int64_t ld_src, int64_t rows, int cols, T* __restrict__ dst, int64_t ld_dst) {
+realign_kernel(const uint16_t* __restrict__ src, int64_t ld_src, int64_t rows, int cols, uint16_t* __restrict__ dst, int64_t ld_dst) {
   train_pdl_wait();
-  constexpr int kPer = 4 / sizeof(T);
-  const int words = (cols + kPer - 1) / kPer;
-  const int64_t units = rows * words;
+  const int pairs = (cols + 1) / 2;
+  const int64_t units = rows * pairs;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t row = u / words;
-    const int col = (int)(u - row * words) * kPer;
-    const T* s = src + row * ld_src + col;
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (col + j < cols) w |= (uint32_t)s[j] << (8 * sizeof(T) * j);
-    *reinterpret_cast<uint32_t*>(dst + row * ld_dst + col) = w;
+    const int64_t row = u / pairs;
+    const int col = (int)(u - row * pairs) * 2;
+    const uint16_t* s = src + row * ld_src + col;
+    const uint32_t lo = s[0], hi = col + 1 < cols ? s[1] : 0;
+    *reinterpret_cast<uint32_t*>(dst + row * ld_dst + col) = lo | (hi << 16);
   }
 }
 
@@ -103,51 +88,41 @@ EncodeFn tensor_map_encoder() {
   cached.store(fn, std::memory_order_release);
   return fn;
 }
-// One operand as it lies in memory; elem = 2 bytes, or 1 (codes and exponents of a packed one).
+// One operand as it lies in memory, 16-bit values.
 struct Stored {
   const void* base = nullptr;
   int64_t rows = 0, cols = 0, ld = 0;
-  int elem = 2;
-  int64_t aligned_ld() const { return ceil_div64(cols * elem, 16) * 16 / elem; }
+  int64_t aligned_ld() const { return ceil_div64(cols, 8) * 8; }
   // One row needs no row distance.
-  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld * elem % 16 == 0); }
-  size_t copy_bytes() const { return tma_ready() ? 0 : (size_t)rows * aligned_ld() * elem; }
+  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld % 8 == 0); }
+  size_t copy_bytes() const { return tma_ready() ? 0 : (size_t)rows * aligned_ld() * 2; }
 };
-// Map over an operand: boxes of box_cols x box_rows elements, zeros outside.
-int encode_map(CUtensorMap* map, const Stored& s, int box_cols, int box_rows, bool swizzle) {
+// Map over an operand: boxes of 64 columns x box_rows, 128-byte swizzle, zeros outside.
+int encode_map(CUtensorMap* map, const Stored& s, int box_rows) {
   EncodeFn fn = tensor_map_encoder();
   if (!fn) return record_cuda_failure(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
   const cuuint64_t dim[2] = {(cuuint64_t)s.cols, (cuuint64_t)s.rows};
-  const cuuint64_t stride[1] = {(cuuint64_t)(s.rows == 1 ? s.aligned_ld() : s.ld) * s.elem};
-  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, es[2] = {1, 1};
-  if (fn(map, s.elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(s.base), dim, stride, box, es,
-         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  const cuuint64_t stride[1] = {(cuuint64_t)(s.rows == 1 ? s.aligned_ld() : s.ld) * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, es[2] = {1, 1};
+  if (fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(s.base), dim, stride, box, es,
+         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return record_cuda_failure(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   return LQSGD_OK;
 }
 
 struct Plan {
-  int product;
-  bool packed;                   // B is x8, decoded inside the product's kernel ...
-  bool unpacked;                 // ... or before it, into the workspace
-  int cg, bn;
   int64_t M, N, K;
-  Stored a, b, e;                // e: exponents of a packed b
-  int tiles_m, tiles_n, kb_total, share, clusters;
-  size_t off_a, off_b, off_e, off_x, off_partial, bytes;
+  Stored a, b;
+  bool unpacked;                 // b is x8, decoded into the workspace first
+  int cg, bn, tiles_m, tiles_n, kb_total, deal, share, meet, clusters;
+  size_t off_a, off_b, off_x, off_partial, bytes;
 };
 
 constexpr int kSms = 148;              // sums are cut for this many SMs whatever the card has: results do not depend on it
 
-// Microseconds: one k block of a tile, and what a tile costs besides (filling the pipeline, draining the accumulator).
-double block_us(int cg) { return cg == 2 ? 0.32 : 0.24; }
-constexpr double kTileUs = 2.0, kJoinUs = 3.0;
-constexpr int kDecodeFirstTiles = 4;
-
 int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   Plan p = {};
-  p.product = product;
   const int64_t rows = a.rows;
   const Stored x = {a.dev_x, rows, a.in, a.ld_x}, w = {a.dev_w, a.out, a.in, a.ld_w}, dz = {a.dev_dz, rows, a.out, a.ld_dz};
   if (product == LQSGD_LINEAR_FORWARD) {
@@ -156,49 +131,47 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
     p.a = dz; p.b = w; p.M = rows; p.N = a.in; p.K = a.out;
   } else {
     p.a = dz; p.b = x; p.M = a.out; p.N = a.in; p.K = rows;
-    p.packed = a.x8.dev_codes != nullptr;
-    if (p.packed) {
-      p.b = {a.x8.dev_codes, rows, a.in, a.x8.ld_codes, 1};
-      p.e = {a.x8.dev_exps, rows, ceil_div64(a.in, kGroup), a.x8.ld_exps, 1};
-    }
+    p.unpacked = a.x8.dev_codes != nullptr;
+    if (p.unpacked) p.b = {nullptr, rows, a.in, ceil_div64(a.in, 8) * 8};
   }
   p.kb_total = (int)ceil_div64(p.K, kLinBK);
+  // The cheapest of the ways to deal the tiles out, by what they were measured to cost (microseconds).
+  constexpr double kTileUs = 2.2, kMeetUs = 4.0, kJoinUs = 4.0;
   double best = 1e30;
   auto consider = [&](int cg, int bn) {
     const int64_t tm = ceil_div64(p.M, (int64_t)kLinBM * cg), tn = ceil_div64(p.N, bn), tiles = tm * tn;
     if (tiles > (1 << 28)) return;
     const int units = kSms / cg;
-    const double per = block_us(cg);
-    auto take = [&](double t, int64_t share, int64_t clusters) {
+    const double per = cg == 2 ? 0.31 : 0.22;
+    auto take = [&](double t, int deal, int64_t share, int meet, int64_t clusters) {
       if (t >= best) return;
       best = t;
-      p.cg = cg; p.bn = bn; p.tiles_m = (int)tm; p.tiles_n = (int)tn; p.share = (int)share; p.clusters = (int)clusters;
+      p.cg = cg; p.bn = bn; p.tiles_m = (int)tm; p.tiles_n = (int)tn;
+      p.deal = deal; p.share = (int)share; p.meet = meet; p.clusters = (int)clusters;
     };
-    take(ceil_div64(tiles, units) * (kTileUs + p.kb_total * per), 0, std::min<int64_t>(tiles, units));
+    take(ceil_div64(tiles, units) * (kTileUs + p.kb_total * per), kWhole, 0, 1, std::min<int64_t>(tiles, units));
+    // how many clusters of 2 .. 8 such CTAs a B200 runs at once (SMs of one cluster lie in one GPC)
+    constexpr int kAtOnce[9] = {0, 0, 74, 45, 33, 26, 22, 15, 15};
+    for (int meet = 2; cg == 1 && meet <= 8; ++meet) {
+      const int64_t share = ceil_div64(p.kb_total, meet);
+      if (tiles <= kAtOnce[meet] && ceil_div64(p.kb_total, share) == meet) take(kTileUs + share * per + kMeetUs, kMeet, share, meet, tiles * meet);
+    }
     // equal shares of at least 4 k blocks each, where tiles are few
     const int64_t pairs = tiles * p.kb_total;
     if (tiles >= 2 * units || p.kb_total < 8 || pairs >= (1ll << 31)) return;
     const int64_t share = std::max<int64_t>(4, ceil_div64(pairs, units)), clusters = ceil_div64(pairs, share);
-    if (clusters <= tiles && share % p.kb_total == 0) return;
     const double bytes = 4.0 * kLinBM * cg * bn * (double)clusters;
-    take(kTileUs * (share >= p.kb_total ? 2 : 1) + share * per + kJoinUs + bytes / 2.0e6, share, clusters);
+    take(kTileUs * (share >= p.kb_total ? 2 : 1) + share * per + kJoinUs + bytes / 2.0e6, kShares, share, 1, clusters);
   };
   consider(1, 128);
   consider(2, 256);
   if (best > 1e29) return LQSGD_ERR_BAD_SHAPE;
   size_t off = 0;
   auto room = [&](size_t n) { const size_t at = off; off += (n + 255) / 256 * 256; return at; };
-  // Every row tile decodes x8 again; from the fourth on it is cheaper to decode it once, into the workspace.
-  if (p.packed && p.tiles_m * p.cg >= kDecodeFirstTiles) {
-    p.packed = false;
-    p.unpacked = true;
-    p.b = {nullptr, rows, a.in, ceil_div64(a.in, 8) * 8, 2};
-    p.off_x = room((size_t)rows * p.b.ld * 2);
-  }
+  if (p.unpacked) p.off_x = room((size_t)rows * p.b.ld * 2);
   p.off_a = room(p.a.copy_bytes());
-  if (!p.unpacked) p.off_b = room(p.b.copy_bytes());
-  if (p.packed) p.off_e = room(p.e.copy_bytes());
-  if (p.share) p.off_partial = room((size_t)2 * p.clusters * kLinBM * p.cg * p.bn * 4);
+  p.off_b = room(p.b.copy_bytes());
+  if (p.deal == kShares) p.off_partial = room((size_t)2 * p.clusters * kLinBM * p.cg * p.bn * 4);
   p.bytes = off;
   *out = p;
   return LQSGD_OK;
@@ -221,14 +194,9 @@ int check_matrix(const void* p, int64_t ld, int32_t cols, int elem) {
 int place(Stored* s, char* ws, size_t off, cudaStream_t st) {
   if (s->tma_ready()) return LQSGD_OK;
   const int64_t ld = s->aligned_ld();
-  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ceil_div64(s->cols * s->elem, 4), 256), 148 * 16);
-  const dim3 grid((unsigned)blocks), block(256);
-  if (s->elem == 2)
-    TRAIN_CK(train_launch(realign_kernel<uint16_t>, grid, block, 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows, (int)s->cols,
-                          reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
-  else
-    TRAIN_CK(train_launch(realign_kernel<uint8_t>, grid, block, 0, st, 1, static_cast<const uint8_t*>(s->base), s->ld, s->rows, (int)s->cols,
-                          reinterpret_cast<uint8_t*>(ws + off), ld), "realign_kernel launch");
+  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ((s->cols + 1) / 2), 256), kSms * 16);
+  TRAIN_CK(train_launch(realign_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows,
+                        (int)s->cols, reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
   s->base = ws + off;
   s->ld = ld;
   return LQSGD_OK;
@@ -246,18 +214,13 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   q.box_a = OA == kOpK ? (uint32_t)std::min<int64_t>(kLinBM, ceil_div64(p.M, 8) * 8) : kLinBM;
-  int rc = encode_map(&q.ta, p.a, 64, OA == kOpK ? (int)q.box_a : kLinBK, true);
-  if (rc != LQSGD_OK) return rc;
-  if (OB == kOpPacked) {
-    if ((rc = encode_map(&q.tb, p.b, 128, kLinBK, true)) != LQSGD_OK || (rc = encode_map(&q.te, p.e, 16, kLinBK, false)) != LQSGD_OK) return rc;
-  } else if ((rc = encode_map(&q.tb, p.b, 64, OB == kOpK ? S::kBNc : kLinBK, true)) != LQSGD_OK) {
-    return rc;
-  }
+  int rc = encode_map(&q.ta, p.a, OA == kOpK ? (int)q.box_a : kLinBK);
+  if (rc != LQSGD_OK || (rc = encode_map(&q.tb, p.b, OB == kOpK ? S::kBNc : kLinBK)) != LQSGD_OK) return rc;
   const int sms = train_sm_count();
   if (sms < CG) return record_cuda_failure(cudaErrorInvalidDevice, "cudaDevAttrMultiProcessorCount");
-  // Whole tiles may be dealt to any number of clusters, equal shares were cut for p.clusters (which then run in turn).
-  const int clusters = p.share ? p.clusters : (int)std::min<int64_t>((int64_t)p.tiles_m * p.tiles_n, sms / CG);
-  TRAIN_CK(train_launch(kernel, dim3((unsigned)(clusters * CG)), dim3(S::kThreads), S::kSmem, st, CG, q), "linear_kernel launch");
+  // Whole tiles may be dealt to any number of clusters; the others were cut for p.clusters (on a smaller card they run in turn).
+  const int clusters = p.deal == kWhole ? (int)std::min<int64_t>((int64_t)p.tiles_m * p.tiles_n, sms / CG) : p.clusters;
+  TRAIN_CK(train_launch(kernel, dim3((unsigned)(clusters * CG)), dim3(S::kThreads), S::kSmem, st, CG * p.meet, q), "linear_kernel launch");
   return LQSGD_OK;
 }
 
@@ -275,7 +238,6 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
     if ((rc = lqsgd_unpack8(&a.x8, a.rows, a.in, ws + p.off_x, p.b.ld, a.dtype, st)) != LQSGD_OK) return rc;
   }
   if ((rc = place(&p.a, ws, p.off_a, st)) != LQSGD_OK || (rc = place(&p.b, ws, p.off_b, st)) != LQSGD_OK) return rc;
-  if (p.packed && (rc = place(&p.e, ws, p.off_e, st)) != LQSGD_OK) return rc;
   const int es = ep.dtype == LQSGD_F32 ? 4 : 2;
   auto rows_aligned = [](const void* ptr, int64_t bytes, size_t to) { return train_aligned(ptr, to) && bytes % (int64_t)to == 0; };
   ep.vec_out = rows_aligned(ep.out, ep.ld_out * es, 32);
@@ -285,27 +247,28 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   LinProblem q;
   std::memset(&q, 0, sizeof(q));
   q.ep = ep;
-  q.partial = p.share ? reinterpret_cast<float*>(ws + p.off_partial) : nullptr;
+  q.partial = p.deal == kShares ? reinterpret_cast<float*>(ws + p.off_partial) : nullptr;
   q.M = (int32_t)p.M; q.N = (int32_t)p.N; q.K = (int32_t)p.K;
-  q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total; q.share = p.share;
+  q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total;
+  q.deal = p.deal; q.share = p.share; q.meet = p.meet;
   q.dtype = a.dtype;
   q.status = a.dev_status;
   if (product == LQSGD_LINEAR_FORWARD)
     rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false>(p, q, st);
   else if (product == LQSGD_LINEAR_GRAD_INPUT)
     rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false>(p, q, st);
-  else if (p.packed)
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpPacked, true>(p, q, st) : launch<1, 128, kOpMN, kOpPacked, true>(p, q, st);
   else
     rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, true>(p, q, st) : launch<1, 128, kOpMN, kOpMN, true>(p, q, st);
   if (rc != LQSGD_OK) return rc;
-  if (p.share) {
+  if (p.deal == kShares) {
     const int most = (int)((p.kb_total - 1) / p.share + 2);           // pieces of one tile
-    const uint32_t tiles = (uint32_t)p.tiles_m * p.tiles_n, high = kLinBM * p.cg, ways = most >= 16 ? 8 : 1;
-    uint32_t rows = ways == 8 ? 8 : 32;                               // fewer per block until the card is full
-    while (rows > (ways == 8 ? 1u : 8u) && tiles * (high / rows) < kSms * 4) rows /= 2;
-    const LinPieces j = {q.partial, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.kb_total, (uint32_t)p.share, (uint32_t)p.cg, (uint32_t)p.bn, rows, ways};
-    TRAIN_CK(train_launch(linear_join_kernel, dim3(tiles * (high / rows)), dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
+    const uint32_t tiles = (uint32_t)p.tiles_m * p.tiles_n, high = kLinBM * p.cg;
+    uint32_t rows = 32;                                               // fewer per block until the card is full
+    while (rows > (most >= 8 ? 1u : 8u) && tiles * (high / rows) < kSms * 4) rows /= 2;
+    const LinPieces j = {q.partial, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.kb_total, (uint32_t)p.share, (uint32_t)p.cg, (uint32_t)p.bn, rows};
+    const dim3 grid(tiles * (high / rows));
+    if (most >= 8) TRAIN_CK(train_launch(linear_join_kernel<8>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
+    else TRAIN_CK(train_launch(linear_join_kernel<1>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
   }
   return LQSGD_OK;
 }

@@ -8,14 +8,15 @@
 //
 // An operand whose rows hold k ("K-major") is staged as 64 k x R rows; one whose rows hold m or n ("MN-major") as blocks of
 // 64 columns x 64 k: both arrive from TMA with the 128-byte swizzle that the tensor core reads, so nothing is transposed.
-// x kept in 8 bits is the one operand TMA cannot bring: converter warps read its codes, decode them to 16 bits (exactly,
-// see lqsgd_pack8) and write the same swizzled layout.
+// x kept in 8 bits is decoded to 16 bits (exactly, see lqsgd_pack8) into the workspace ahead of the product: 5 bytes of
+// traffic per value, once.  Decoding inside the product (warps that turn codes into the operand's layout in shared memory)
+// was built and measured: every row tile decodes x again, and the decoders' shared memory traffic and hand-over take the
+// MMAs' time: 1.37 against 0.86 ms for 8192 rows, 16384 x 4096, and 22.7 against 18.4 us for 65536 rows, 64 x 128.
 //
 // A cluster of CG CTAs (1 or 2) works on a tile of 128 CG x BN: with CG = 2 each SM holds 128 rows of A and half of B's, and
 // one tcgen05.mma.cta_group::2 drives both tensor cores, so that an SM fetches (128 + BN / 2) rows per k instead of
 // 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 (4-7 for a weight gradient) drain the
-// accumulator (two of them, so that the next tile's sum runs under the epilogue); with x8 warp 3 loads its codes and the last
-// eight warps decode them.  Clusters walk
+// accumulator (two of them, so that the next tile's sum runs under the epilogue).  Clusters walk
 // the work items (tile, piece of the sum) with a fixed stride.
 //
 // Every wait is bounded (lqsgd_stream_common.cuh): on expiry the CTA's abort flag goes up, all roles leave their loops,
@@ -30,7 +31,8 @@ namespace lqsgd {
 
 constexpr int kLinBM = 128;            // rows of A per CTA
 constexpr int kLinBK = 64;             // k per stage: 128 bytes of a 16-bit type, one swizzle span
-enum LinOperand { kOpK = 0, kOpMN = 1, kOpPacked = 2 };
+enum LinOperand { kOpK = 0, kOpMN = 1 };
+enum LinDeal { kWhole = 0, kShares = 1, kMeet = 2 };
 
 // What happens to a sum: y = act(sum + bias) + residual, and the 8-bit forms.  rows x cols is the result as the caller sees it.
 struct LinEpilogue {
@@ -48,13 +50,14 @@ struct LinEpilogue {
 };
 
 struct alignas(64) LinProblem {
-  CUtensorMap ta, tb;                  // operands; tb of a packed B: its codes
-  CUtensorMap te;                      // exponents of a packed B
+  CUtensorMap ta, tb;                  // operands
   LinEpilogue ep;
   float* partial;                      // pieces of sums: two per cluster, each a tile (see LinWalk)
   int32_t M, N, K;
   int32_t tiles_m, tiles_n, kb_total;
-  int32_t share;                       // 0: clusters take whole tiles; otherwise every cluster takes this many k-blocks in a row
+  int32_t deal;                        // how the work is dealt out (LinDeal), see LinWalk
+  int32_t share;                       // k blocks per cluster (kShares) or per CTA of a cluster (kMeet)
+  int32_t meet;                        // CTAs that sum one tile (kMeet)
   int32_t dtype;                       // of the operands
   uint32_t box_a;                      // rows of A that TMA brings per stage and CTA: 128, fewer (a multiple of 8) where A has fewer and
                                        // they lie along k; what the stage holds beyond them only meets rows that do not exist
@@ -349,69 +352,99 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
   }
 }
 
-// One value's 8-bit form where a warp holds 32 neighbouring columns of a row, lane by lane (0 in lanes past the end).
-__device__ __forceinline__ void put_packed_lane(const lqsgd_packed8& p, int64_t row, int col, bool on, float v) {
-  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+// ---- epilogue of a row whose columns a warp holds side by side, four neighbouring ones per lane (128 in all)
+// 8-bit form: eight neighbouring lanes hold a group of 32.  The values of columns that do not exist are 0.
+__device__ __forceinline__ void put_packed_quad(const lqsgd_packed8& p, int64_t row, int col, int have, const float (&v)[4]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   const int eb = exp_byte(__uint_as_float(top));
-  if (on) p.dev_codes[row * p.ld_codes + col] = (uint8_t)((mag_bits(v, inv_step(eb)) & 127u) | ((__float_as_uint(v) >> 24) & 128u));
-  if ((threadIdx.x & 31) == 0) p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
+  if (have <= 0) return;
+  const uint32_t w = code_word(v[0], v[1], v[2], v[3], inv_step(eb));
+  uint8_t* c = p.dev_codes + row * p.ld_codes + col;
+  if (have == 4 && (reinterpret_cast<uintptr_t>(c) & 3) == 0) {
+    *reinterpret_cast<uint32_t*>(c) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < have) c[i] = (uint8_t)(w >> (8 * i));
+  }
+  if ((col & (kGroup - 1)) == 0) p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
 }
-// Epilogue of one row's 32 neighbouring columns, one per lane; col = the lane's column, on = it exists.  The whole warp calls it.
-__device__ __forceinline__ void finish_lane(const LinEpilogue& e, int64_t row, int col, bool on, float v, float bias) {
+// The whole warp calls it; col is the lane's first column.
+__device__ __forceinline__ void finish_quad(const LinEpilogue& e, int64_t row, int col, float (&v)[4]) {
+  const int have = min(4, e.cols - col);
   if (e.dtype == LQSGD_F32) {
-    if (on) {
-      float* o = static_cast<float*>(e.out) + row * e.ld_out + col;
-      *o = e.accumulate ? *o + v : v;
+    float* o = static_cast<float*>(e.out) + row * e.ld_out + col;
+    if (have == 4 && e.vec_out) {
+      float4 t = make_float4(v[0], v[1], v[2], v[3]);
+      if (e.accumulate) {
+        const float4 u = *reinterpret_cast<const float4*>(o);
+        t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+      }
+      *reinterpret_cast<float4*>(o) = t;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < have) o[i] = e.accumulate ? o[i] + v[i] : v[i];
     }
     return;
   }
-  v = on ? v + bias : 0.f;
-  if (e.z8.dev_codes) put_packed_lane(e.z8, row, col, on, v);
-  float one[1] = {v};
-  act_run(e.act, one);
-  v = one[0];
-  if (e.residual && on) v += unpack1(e.dtype, static_cast<const uint16_t*>(e.residual)[row * e.ld_res + col]);
-  const uint16_t w = pack1(e.dtype, v);
-  if (on) static_cast<uint16_t*>(e.out)[row * e.ld_out + col] = w;
-  if (e.y8.dev_codes) put_packed_lane(e.y8, row, col, on, on ? unpack1(e.dtype, w) : 0.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= have) v[i] = 0.f;
+    else if (e.bias) v[i] += __ldg(e.bias + col + i);
+  }
+  if (e.z8.dev_codes) put_packed_quad(e.z8, row, col, have, v);
+  act_run(e.act, v);
+  if (e.residual && have > 0) {
+    const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row * e.ld_res + col;
+    if (have == 4 && e.vec_res) {
+      const uint2 w = *reinterpret_cast<const uint2*>(r);
+      const float2 f = unpack2(e.dtype, w.x), g = unpack2(e.dtype, w.y);
+      v[0] += f.x; v[1] += f.y; v[2] += g.x; v[3] += g.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < have) v[i] += unpack1(e.dtype, r[i]);
+    }
+  }
+  const uint2 w = make_uint2(pack2(e.dtype, v[0], v[1]), pack2(e.dtype, v[2], v[3]));
+  uint16_t* o = static_cast<uint16_t*>(e.out) + row * e.ld_out + col;
+  if (have == 4 && e.vec_out) {
+    *reinterpret_cast<uint2*>(o) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < have) o[i] = (uint16_t)((i < 2 ? w.x : w.y) >> (16 * (i & 1)));
+  }
+  if (e.y8.dev_codes) {
+    const float2 f = unpack2(e.dtype, w.x), g = unpack2(e.dtype, w.y);
+    const float u[4] = {f.x, f.y, g.x, g.y};
+    put_packed_quad(e.y8, row, col, have, u);
+  }
 }
 
-// ---- decoding 8-bit codes into operand words: four codes (one word) -> two words of two 16-bit numbers
-// bf16: 0x4300 | m is 128 + m, so (128 + m) 2^e - 128 2^e is m 2^e, exactly, in one fused operation; then the sign is put on top.
-// fp16: 0x6400 | m is 1024 + m; 1024 2^e may be out of range, so the 1024 goes first.
-// Codes 0 and 2 make the first word, 1 and 3 the second, which takes no byte shuffles: within every four columns the operand
-// holds columns 0, 2, 1, 3, and the epilogue puts them back.
-__device__ __forceinline__ void decode4_bf16(uint32_t w, uint32_t step2, uint32_t off2, uint32_t& even, uint32_t& odd) {
-  const uint32_t te = (w & 0x007f007fu) | 0x43004300u, to = ((w >> 8) & 0x007f007fu) | 0x43004300u;
-  const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&step2), o = *reinterpret_cast<const __nv_bfloat162*>(&off2);
-  const __nv_bfloat162 e = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&te), s, o), d = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&to), s, o);
-  even = *reinterpret_cast<const uint32_t*>(&e) | ((w << 8) & 0x80008000u);
-  odd = *reinterpret_cast<const uint32_t*>(&d) | (w & 0x80008000u);
-}
-__device__ __forceinline__ void decode4_fp16(uint32_t w, uint32_t step2, uint32_t& even, uint32_t& odd) {
-  const uint32_t te = (w & 0x007f007fu) | 0x64006400u, to = ((w >> 8) & 0x007f007fu) | 0x64006400u;
-  const __half2 s = *reinterpret_cast<const __half2*>(&step2), k = __half2(__ushort_as_half(0x6400), __ushort_as_half(0x6400));
-  const __half2 e = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&te), k), s), d = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&to), k), s);
-  even = *reinterpret_cast<const uint32_t*>(&e) | ((w << 8) & 0x80008000u);
-  odd = *reinterpret_cast<const uint32_t*>(&d) | (w & 0x80008000u);
-}
-// Any step: through fp32, saturated to the type's largest finite number (NaN stays).
-__device__ __forceinline__ float decode1_any(float top, uint32_t code, int eb) {
-  const float a = decode8(code & 255u, step_of(eb));
-  return fabsf(a) > top ? copysignf(top, a) : a;
-}
-__device__ __forceinline__ void decode4_any(int dtype, uint32_t w, int eb, uint32_t& even, uint32_t& odd) {
-  const float top = dtype == LQSGD_BF16 ? 3.3895314e38f : 65504.f;
-  even = pack2(dtype, decode1_any(top, w, eb), decode1_any(top, w >> 16, eb));
-  odd = pack2(dtype, decode1_any(top, w >> 8, eb), decode1_any(top, w >> 24, eb));
+// a / b for a < 2^31, b >= 1: in floating point and put right, where 32-bit integer division is a long chain.
+__device__ __forceinline__ uint32_t quick_div(uint32_t a, uint32_t b) {
+  if (a >= (1u << 22)) return a / b;
+  uint32_t q = (uint32_t)(__fdividef((float)a, (float)b));
+  if (q * b > a) --q;
+  if ((q + 1) * b <= a) ++q;
+  return q;
 }
 
 // ---- the walk over (tile, k block) pairs that every role of a CTA makes
-// Two ways to deal them out.  Whole tiles: cluster g takes tiles g, g + G, ...  Equal shares (few tiles, long sums): all
-// (tile, k block) pairs stand in one row, tile after tile, and cluster g takes pairs [g share, (g + 1) share).  A tile
-// that a share begins or ends inside of is summed by several clusters: each writes what it has to a piece of the
-// workspace (at most two per cluster: piece 2 g where its share begins, 2 g + 1 for a tile that its share ends
-// inside of), and linear_join_kernel adds a tile's pieces in the order of the clusters.
+// Three ways to deal them out.
+// kWhole: cluster g (of CG CTAs) takes tiles g, g + G, ...
+// kMeet (few tiles): a cluster of up to 8 CTAs sums one tile, CTA r the k blocks [r share, (r + 1) share); the sums meet in the
+//   CTAs' shared memory: each sends every other its slice of the rows, adds up what it got, in their order, and finishes it.
+// kShares (few tiles, long sums): all (tile, k block) pairs stand in one row, tile after tile, and cluster g takes pairs
+//   [g share, (g + 1) share).  A tile that a share begins or ends inside of is summed by several clusters: each writes what
+//   it has to a piece of the workspace (at most two per cluster: piece 2 g where its share begins, 2 g + 1 for a tile that its
+//   share ends inside of), and linear_join_kernel adds a tile's pieces in the order of the clusters.
 struct LinWalk {
   uint32_t pos, end, begin;            // equal shares: pairs (fewer than 2^31); whole tiles: tiles
   uint32_t stride;
@@ -422,45 +455,50 @@ struct LinWalk {
   // about as many column tiles, which keeps their operands in L2.
   static __device__ __forceinline__ void place(uint32_t tiles_m, uint32_t tiles_n, uint32_t t, int& m_tile, int& n_tile) {
     constexpr uint32_t kBand = 8;
-    const uint32_t band = t / (kBand * tiles_n), first = band * kBand, high = min(kBand, tiles_m - first);
+    const uint32_t band = quick_div(t, kBand * tiles_n), first = band * kBand, high = min(kBand, tiles_m - first);
     const uint32_t in = t - band * kBand * tiles_n;
-    n_tile = (int)(in / high);
+    n_tile = (int)quick_div(in, high);
     m_tile = (int)(first + in - n_tile * high);
   }
   __device__ __forceinline__ void locate(const LinProblem& p) {
     uint32_t t = pos;
     kb = 0;
     kb_end = p.kb_total;
-    if (p.share) {
-      t = pos / (uint32_t)p.kb_total;
+    if (p.deal == kShares) {
+      t = quick_div(pos, p.kb_total);
       kb = (int)(pos - t * p.kb_total);
       kb_end = min(p.kb_total, kb + (int)(end - pos));
     }
     place(p.tiles_m, p.tiles_n, t, m_tile, n_tile);
   }
-  __device__ __forceinline__ LinWalk(const LinProblem& p, int g, int clusters) : cluster(g) {
+  // g of `clusters` clusters; with kMeet the CTA `part` of the cluster that has tile g.
+  __device__ __forceinline__ LinWalk(const LinProblem& p, int g, int clusters, int part) : cluster(g) {
     const uint32_t tiles = p.tiles_m * p.tiles_n;
-    pos = p.share ? (uint32_t)g * p.share : (uint32_t)g;
-    end = p.share ? min(tiles * p.kb_total, pos + p.share) : tiles;
-    stride = clusters;
+    pos = p.deal == kShares ? (uint32_t)g * p.share : (uint32_t)g;
+    end = p.deal == kShares ? min(tiles * p.kb_total, pos + p.share) : tiles;
+    stride = p.deal == kMeet ? tiles : (uint32_t)clusters;
     begin = pos;
     if (pos < end) locate(p);
+    if (p.deal == kMeet) {
+      kb = part * p.share;
+      kb_end = min(p.kb_total, kb + p.share);
+    }
   }
   __device__ __forceinline__ bool done() const { return pos >= end; }
   // The piece the current tile's sum goes to, or -1: the cluster has the whole tile.
   __device__ __forceinline__ int piece(const LinProblem& p) const {
-    return kb_end - kb == p.kb_total ? -1 : (pos == begin ? 2 * cluster : 2 * cluster + 1);
+    return p.deal != kShares || kb_end - kb == p.kb_total ? -1 : (pos == begin ? 2 * cluster : 2 * cluster + 1);
   }
   // To the next tile; only from the state locate() left (next() below moves kb).
   __device__ __forceinline__ void next_tile(const LinProblem& p) {
-    pos += p.share ? (uint32_t)(kb_end - kb) : stride;
+    pos += p.deal == kShares ? (uint32_t)(kb_end - kb) : stride;
     if (pos < end) locate(p);
   }
   // To the next k block, of this tile or the next.
   __device__ __forceinline__ void next(const LinProblem& p) {
-    if (p.share) ++pos;
+    if (p.deal == kShares) ++pos;
     if (++kb == kb_end) {
-      if (!p.share) pos += stride;
+      if (p.deal != kShares) pos += stride;
       if (pos < end) locate(p);
     }
   }
@@ -472,31 +510,25 @@ struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
   static constexpr uint32_t kStage = kABytes + ((kBBytes + 1023) / 1024 * 1024);
-  // a packed B passes through a second, small ring: 64 rows of kBNc codes and of the 16 exponents that hold the tile's
-  static constexpr int kRaw = OB == kOpPacked ? 4 : 0;
-  static constexpr uint32_t kRawCodes = kLinBK * kBNc, kRawBytes = kRawCodes + kLinBK * 16;
-  static constexpr uint32_t kScratch = WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16;   // one per epilogue warp
-  static constexpr uint32_t kRoom = 225u * 1024 - kRaw * kRawBytes - kScratch;
-  static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
-  static constexpr uint32_t kTxB = OB == kOpPacked ? 0 : kBBytes;         // what TMA brings of B per stage and CTA
   // Two warps per quarter of tensor memory where the epilogue computes per value (GELU and the 8-bit form take as
   // long as the product of a 4096-wide layer with one).
   static constexpr int kEpiWarps = WF32 ? 4 : 8;
-  // A thread decodes 32 codes of one row of x; two teams of warps take the stages in turn, because one team's
-  // chain of waits, loads, decoding and hand-over (about 700 cycles) is longer than a stage's MMAs (512).
-  static constexpr int kTeams = 2;
-  static constexpr int kConvWarps = OB == kOpPacked ? kBNc / 16 : 0;      // of one team
-  static constexpr int kConvWarp0 = 4 + kEpiWarps;
-  static constexpr int kThreads = (kConvWarp0 + kTeams * kConvWarps) * 32;
-  static constexpr int kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
-  static constexpr int kBars = 3 * kStages + 2 * kRaw + 2 + 2 + 1;
-  static constexpr uint32_t kRawBase = kStages * kStage;
-  static constexpr uint32_t kScratchOff = kRawBase + kRaw * kRawBytes;
+  static constexpr int kThreads = (4 + kEpiWarps) * 32;
+  static constexpr uint32_t kScratch = WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16;   // one per epilogue warp
+  static constexpr uint32_t kRoom = 225u * 1024 - kScratch;
+  static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
+  static constexpr int kTmemCols = 2 * BN;
+  static constexpr int kBars = 2 * kStages + 2 + 2 + 1;
+  static constexpr uint32_t kScratchOff = kStages * kStage;
   static constexpr uint32_t kBarOff = (kScratchOff + kScratch + 7) / 8 * 8;
   static constexpr uint32_t kSmem = kBarOff + kBars * 8 + 32 + 1024;
+  // A tile summed by a cluster meets in shared memory, in the place of the operand stages: rows of BN + 4 words (a lane's
+  // 16-byte accesses, a row each, then cover all banks).
+  static constexpr int kMeetPitch = BN + 4;
   static_assert(kSmem <= 227 * 1024 && kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "one CTA per SM");
   static_assert(OB == kOpK || kBNc % 64 == 0, "MN-major operands come in blocks of 64");
-  static_assert(OB != kOpPacked || kBNc == 128, "a row of codes is one 128-byte swizzle span");
+  static_assert(CG == 2 || BN == 128, "a warp finishes a row of a tile");
+  static_assert(CG == 2 || (kLinBM + 7) * kMeetPitch * 4 <= kStages * kStage, "a tile, in up to 8 slices, fits in the operand stages");
 };
 
 template <int CG, int BN, int OA, int OB, bool WF32>
@@ -506,11 +538,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   extern __shared__ uint8_t lin_smem[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(lin_smem) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(base + S::kBarOff);   // [stages] TMA bytes landed, in both CTAs (first CTA's barrier)
-  uint64_t* conv = full + S::kStages;                                // [stages] decoded rows of B written, in both CTAs (first CTA's)
-  uint64_t* empty = conv + S::kStages;                               // [stages] the MMAs that read the stage are done
-  uint64_t* raw_full = empty + S::kStages;                           // [raw] codes and exponents of B landed in this CTA
-  uint64_t* raw_empty = raw_full + S::kRaw;                          // [raw] every converter warp has them in registers
-  uint64_t* d_full = raw_empty + S::kRaw;                            // [2] accumulator complete
+  uint64_t* empty = full + S::kStages;                               // [stages] the MMAs that read the stage are done
+  uint64_t* d_full = empty + S::kStages;                             // [2] accumulator complete
   uint64_t* d_empty = d_full + 2;                                    // [2] accumulator drained by both CTAs (first CTA's)
   uint64_t* fin = d_empty + 2;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(fin + 1);
@@ -518,15 +547,14 @@ linear_kernel(const __grid_constant__ LinProblem p) {
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
-  const int cluster = (int)blockIdx.x / CG, clusters = (int)gridDim.x / CG;
+  const int meet = CG == 1 && p.deal == kMeet ? p.meet : 1, part_of = meet > 1 ? (int)cluster_rank() : 0;
+  const int cluster = (int)blockIdx.x / (CG * meet), clusters = (int)gridDim.x / (CG * meet);
 
   if (tid == 0) {
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(full + s, 1);
-      mbar_init(conv + s, CG * (S::kConvWarps ? S::kConvWarps : 1));
       mbar_init(empty + s, 1);
     }
-    for (int s = 0; s < S::kRaw; ++s) { mbar_init(raw_full + s, 1); mbar_init(raw_empty + s, S::kConvWarps); }
     for (int s = 0; s < 2; ++s) { mbar_init(d_full + s, 1); mbar_init(d_empty + s, S::kEpiWarps * CG); }
     mbar_init(fin, 1);
     wait_ctl_init(abort_flag, 0);
@@ -536,7 +564,6 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   if (warp == 0 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&p.ta) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tb) : "memory");
-    if constexpr (OB == kOpPacked) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.te) : "memory");
   }
   if (warp == 2) {
     if constexpr (CG == 2) {
@@ -554,14 +581,15 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   const uint32_t tmem = *tmem_slot;
   train_pdl_trigger();
   // Every role first finds its place in the work, then waits for the kernel in front.
-  const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), conv_s = smem_u32(conv), empty_s = smem_u32(empty);
+  bool met = false;                    // kMeet: this warp has passed the cluster's first barrier
+  const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), empty_s = smem_u32(empty);
 
   if (warp == 0) {
     // ---- loader
-    LinWalk w(p, cluster, clusters);
+    LinWalk w(p, cluster, clusters, part_of);
     train_pdl_wait();
     const uint32_t full0 = CG == 2 ? map_to(full, 0) : full_s;          // the first CTA's barriers count both CTAs' bytes
-    const uint32_t tx = CG * (p.box_a * 128 + S::kTxB);
+    const uint32_t tx = CG * (p.box_a * 128 + S::kBBytes);
     uint32_t s = 0, turn = 0, it = 0;
     bool ok = true;
     for (; !w.done(); w.next(p), ++it) {
@@ -578,7 +606,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
         }
         if constexpr (OB == kOpK) {
           lin_tma<CG>(b, &p.tb, k0, n0, bar);
-        } else if constexpr (OB == kOpMN) {
+        } else {
 #pragma unroll
           for (int i = 0; i < S::kBNc / 64; ++i) lin_tma<CG>(b + i * kLinBK * 128, &p.tb, n0 + 64 * i, k0, bar);
         }
@@ -603,7 +631,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       const uint32_t d_full_s = smem_u32(d_full), d_empty_s = smem_u32(d_empty);
       uint32_t s = 0, turn = 0, db = 0, dturn = 0;
       bool ok = true;
-      LinWalk w(p, cluster, clusters);
+      LinWalk w(p, cluster, clusters, part_of);
       for (; !w.done() && ok; w.next_tile(p)) {
         if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
         lin_fence_after();
@@ -611,9 +639,6 @@ linear_kernel(const __grid_constant__ LinProblem p) {
         uint32_t more = 0;                          // the tile's first product starts the sum
         for (int kb = w.kb; kb < w.kb_end; ++kb) {
           if (!lin_wait_all(full_s + 8 * s, full + s, turn, abort_flag)) { ok = false; break; }
-          if constexpr (OB == kOpPacked) {
-            if (!lin_wait_all(conv_s + 8 * s, conv + s, turn, abort_flag)) { ok = false; break; }
-          }
           lin_fence_after();
           const uint64_t ad = ad0 + (uint64_t)(s * (S::kStage >> 4)), bd = bd0 + (uint64_t)(s * (S::kStage >> 4));
           if (elect_one()) {
@@ -639,34 +664,11 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       }
     }
     __syncwarp();
-  } else if (OB == kOpPacked && warp == 3) {
-    // ---- loader of the codes: one thread; each CTA brings its own part, for its own converters
-    if constexpr (OB == kOpPacked) if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      LinWalk w(p, cluster, clusters);
-      train_pdl_wait();
-      for (; !w.done(); w.next(p), ++it) {
-        const int r = it % S::kRaw;
-        if (!lin_wait(raw_empty + r, ((it / S::kRaw) & 1) ^ 1, abort_flag)) { ok = false; break; }
-        uint8_t* raw = base + S::kRawBase + r * S::kRawBytes;
-        const int k0 = w.kb * kLinBK, n0 = w.n_tile * BN + (int)rank * S::kBNc;
-        mbar_arrive_expect_tx(raw_full + r, S::kRawBytes);
-        lin_tma<1>(smem_u32(raw), &p.tb, n0, k0, smem_u32(raw_full + r));
-        lin_tma<1>(smem_u32(raw) + S::kRawCodes, &p.te, n0 / kGroup / 16 * 16, k0, smem_u32(raw_full + r));
-      }
-      if (!ok) {
-        const uint32_t limit = wait_limit_of(abort_flag);
-        for (uint32_t j = it > (uint32_t)S::kRaw ? it - S::kRaw : 0; j < it; ++j)
-          for (uint32_t i = 0; i < limit && !mbar_try(raw_full + j % S::kRaw, (j / S::kRaw) & 1); ++i) {}
-      }
-    }
-    __syncwarp();
-  } else if (warp >= 4 && warp < 4 + S::kEpiWarps) {
+  } else if (warp >= 4) {
     // ---- epilogue: a warp reads its quarter of the accumulator's rows (warp % 4), and with eight warps half of its columns
     uint32_t seq = 0;
     const int q = warp & 3;
-    LinWalk w(p, cluster, clusters);
+    LinWalk w(p, cluster, clusters, part_of);
     train_pdl_wait();
     for (; !w.done(); w.next_tile(p), ++seq) {
       const uint32_t db = seq & 1;
@@ -675,6 +677,10 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + db * BN;
       const int m = (w.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane;
       const int n0 = w.n_tile * BN;
+      if (CG == 1 && meet > 1) {                  // every CTA's MMAs are done with the stages that the sums go to
+        cluster_sync_all();
+        met = true;
+      }
       const int piece = w.piece(p);
       float* part = piece >= 0 ? p.partial + (int64_t)piece * (CG * kLinBM * BN) : nullptr;
       constexpr int kStep = 32, kMine = BN / (S::kEpiWarps / 4);
@@ -689,11 +695,16 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           __syncwarp();
           if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
         }
-        if (n0 + c >= p.N || m - lane >= p.M) continue;
-        if constexpr (OB == kOpPacked) {          // back from the order of the decoder
+        if (CG == 1 && meet > 1) {                // to the CTA whose slice the row is in, for this CTA's place there
+          const int r = 32 * q + lane, slice = (kLinBM + meet - 1) / meet, to = r / slice;
+          const uint32_t o = map_to(reinterpret_cast<float*>(base) + (part_of * slice + r - to * slice) * S::kMeetPitch + c, to);
 #pragma unroll
-          for (int j = 0; j < 32; j += 4) { const float t = v[j + 1]; v[j + 1] = v[j + 2]; v[j + 2] = t; }
+          for (int i = 0; i < 8; ++i)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(o + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
+          continue;
         }
+        if (n0 + c >= p.N || m - lane >= p.M) continue;
         if (part) {                               // [row of the tile][BN]
           float* o = part + (int64_t)((int)rank * kLinBM + 32 * q + lane) * BN + c;
 #pragma unroll
@@ -710,62 +721,30 @@ linear_kernel(const __grid_constant__ LinProblem p) {
         }
       }
     }
-  } else if (OB == kOpPacked && warp >= S::kConvWarp0) {
-    // ---- converters: codes and exponents of 64 rows of x8 (k) -> the MN-major operand (n).  A warp takes 32 rows of one group
-    // of 32 columns, a lane one row: its 16-byte accesses, to the codes (swizzled by TMA) and to the operand (swizzled for the
-    // tensor core), then fall on different banks.  The codes come through shared memory and not straight into registers
-    // because the fence before the hand-over waits for a thread's own loads, however far ahead they were issued.
-    if constexpr (OB == kOpPacked) {
-      const int ct = tid - S::kConvWarp0 * 32;
-      const int team = ct / (S::kConvWarps * 32), krow = ct & 63, group = (ct >> 6) & 3;
-      const bool bf = p.dtype == LQSGD_BF16;
-      int r = 0, s = 0, turn = 0;
-      uint32_t rpar = 0, spar = 1;                                       // phase parities of the raw ring and of `empty`
-      for (LinWalk w(p, cluster, clusters); !w.done(); w.next(p)) {
-        if (turn == team) {
-          if (!lin_wait_warp(raw_full + r, rpar, abort_flag, lane)) break;
-          const uint8_t* raw = base + S::kRawBase + r * S::kRawBytes;
-          const uint4 lo = *reinterpret_cast<const uint4*>(raw + krow * 128 + (((2 * group) ^ (krow & 7)) << 4));
-          const uint4 hi = *reinterpret_cast<const uint4*>(raw + krow * 128 + (((2 * group + 1) ^ (krow & 7)) << 4));
-          const int eb = raw[S::kRawCodes + krow * 16 + (((w.n_tile * BN + (int)rank * S::kBNc) / kGroup + group) & 15)];
-          __syncwarp();
-          if (lane == 0) mbar_arrive(raw_empty + r);
-          const uint32_t cw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-          const int e = eb - kExpBias;
-          // the step, 128 steps (bf16) and every product are normal numbers in range; anything else goes through fp32
-          const bool plain = bf ? eb <= 246 : (e >= -14 && e <= 8);
-          uint32_t o[16];
-          if (!plain) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) decode4_any(p.dtype, cw[i], eb, o[2 * i], o[2 * i + 1]);
-          } else if (bf) {
-            const uint32_t one = (uint32_t)(e + 127) << 7, off = 0x8000u | ((uint32_t)(e + 127 + 7) << 7);    // 2^e, -128 2^e
-#pragma unroll
-            for (int i = 0; i < 8; ++i) decode4_bf16(cw[i], one | (one << 16), off | (off << 16), o[2 * i], o[2 * i + 1]);
-          } else {
-            const uint32_t one = (uint32_t)(e + 15) << 10;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) decode4_fp16(cw[i], one | (one << 16), o[2 * i], o[2 * i + 1]);
-          }
-          if (!lin_wait_warp(empty + s, spar, abort_flag, lane)) break;
-          uint8_t* b = base + s * S::kStage + S::kABytes + (group >> 1) * (kLinBK * 128) + krow * 128;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(b + ((((group & 1) * 4 + i) ^ (krow & 7)) << 4)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(conv + s, 0)); else mbar_arrive(conv + s); }
-        }
-        if (++turn == S::kTeams) turn = 0;
-        if (++r == S::kRaw) { r = 0; rpar ^= 1; }
-        if (++s == S::kStages) { s = 0; spar ^= 1; }
-      }
-    }
   }
+  if (CG == 1 && meet > 1 && !met) cluster_sync_all();
   lin_fence_before();
   __syncthreads();
   if (tid == 0 && *abort_flag && p.status) atomicOr(p.status, kStatusTimeout);
-  if constexpr (CG == 2) cluster_sync_all();        // no CTA leaves while the other may still signal its barriers
+  if (CG == 2 || meet > 1) cluster_sync_all();      // the sums have arrived; no CTA leaves while another may still signal its barriers
+  if (CG == 1 && meet > 1) {
+    // ---- the CTAs' sums of one tile have met: a warp takes a row of this CTA's slice, a lane four of its columns
+    train_pdl_wait();                               // (the warps that had no need to yet)
+    const LinWalk w(p, cluster, clusters, part_of);
+    const int slice = (kLinBM + meet - 1) / meet, rows = min(slice, kLinBM - part_of * slice);
+    for (int r = warp; r < rows; r += S::kThreads / 32) {
+      const int row = w.m_tile * kLinBM + part_of * slice + r;
+      if (row >= p.ep.rows) break;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      const float* mine = reinterpret_cast<const float*>(base) + r * S::kMeetPitch + 4 * lane;
+#pragma unroll 4
+      for (int k = 0; k < meet; ++k) {
+        const float4 t = *reinterpret_cast<const float4*>(mine + k * slice * S::kMeetPitch);
+        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
+      }
+      finish_quad(p.ep, row, w.n_tile * BN + 4 * lane, v);
+    }
+  }
   if (warp == 2) {
     if constexpr (CG == 2)
       asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::kTmemCols) : "memory");
