@@ -415,7 +415,7 @@ int lqsgd_orthonormalize_noalloc(const float* dev_p_in, float* dev_p_out, int32_
  * narrower accesses).  Base pointers are aligned to their element.  Outputs must not overlap inputs, except where a
  * call says so.  A call on zero rows writes what an empty sum gives (zeros in weight and bias gradients) and nothing else.
  * Workspaces: device memory, 16-byte aligned, of the size the matching *_workspace_bytes reports (0: may be NULL); it
- * may be reused by the next call on the same stream.  All sums are taken in fp32 in an order fixed by the sizes alone:
+ * may be reused by the next call on the same stream.  All sums are taken in fp32 in an order fixed by the sizes and alignments:
  * the same call gives the same bits.  The calls may be captured in CUDA graphs. */
 typedef enum lqsgd_dtype { LQSGD_BF16 = 0, LQSGD_F16 = 1, LQSGD_F32 = 2 } lqsgd_dtype;
 typedef enum lqsgd_act {

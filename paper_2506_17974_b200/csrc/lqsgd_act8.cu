@@ -1,9 +1,13 @@
 // Activations kept in 8 bits: packing, unpacking, and the activation's backward step that reads them.
 //
-// All three are streams: each value is read once and written once, and what bounds them is HBM.  A thread owns 8
-// consecutive columns (16 bytes of a 16-bit type, 8 bytes of codes) of a row, so four neighbouring lanes hold one group of
-// 32 and agree on its exponent with two shuffles.  A warp covers `lanes` x 8 columns of 32 / lanes rows, lanes = 4 .. 32
-// by the row length, so that short rows do not leave lanes idle.
+// All three are streams: each value is read once and written once, and what bounds them is HBM.  Two layouts of the work:
+//   runs      rows of 16-byte pieces: a thread owns 8 consecutive columns of a row, so four neighbouring lanes hold one group of
+//             32 and agree on its exponent with two shuffles.  A warp covers `lanes` x 8 columns of 32 / lanes rows, lanes = 4 .. 32
+//             by the row length, so that short rows do not leave lanes idle.
+//   strides   rows at any alignment, more than 128 columns: a thread owns 8 columns 32 apart, so that a warp's access to one of
+//             them is 32 neighbouring elements (a run of 8 read element by element touches 32 places instead), and a group is
+//             one column of every lane.
+// A thread takes several rows at a time, all their loads first: one row in flight per thread does not fill HBM's latency.
 #include "lqsgd_train_dev.cuh"
 
 #include <algorithm>
@@ -36,139 +40,293 @@ struct Deal {
   int64_t rows, rows_per_block;
   int32_t cols, lane_shift;                  // lanes = 1 << lane_shift
 };
+template <bool RUNS>
 struct Spot {
   int64_t row, row_end, row_step;            // rows row, row + row_step, ... < row_end
   int col, have;                             // first column; how many of its 8 exist (<= 0: none)
+  int sub;                                   // which of the warp's rows
+  __device__ __forceinline__ explicit Spot(const Deal& d) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lanes = 1 << d.lane_shift, per_warp = 32 >> d.lane_shift;
+    sub = lane >> d.lane_shift;
+    const int seg = (int)blockIdx.x * lanes * kRun, in = lane & (lanes - 1);
+    col = seg + (RUNS ? in * kRun : in);
+    have = RUNS ? min(kRun, d.cols - col) : (col < d.cols ? min(kRun, (d.cols - col + 31) / 32) : 0);
+    const int64_t first = (int64_t)blockIdx.y * d.rows_per_block;
+    row = first + warp * per_warp + sub;
+    row_end = min(d.rows, first + d.rows_per_block);
+    row_step = kWarps * per_warp;
+  }
+  static __device__ __forceinline__ constexpr int step() { return RUNS ? 1 : 32; }      // between the thread's columns
 };
-__device__ __forceinline__ Spot spot_of(const Deal& d) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int lanes = 1 << d.lane_shift, sub = lane >> d.lane_shift, per_warp = 32 >> d.lane_shift;
-  Spot s;
-  s.col = ((int)blockIdx.x * lanes + (lane & (lanes - 1))) * kRun;
-  s.have = min(kRun, d.cols - s.col);
-  const int64_t first = (int64_t)blockIdx.y * d.rows_per_block;
-  s.row = first + warp * per_warp + sub;
-  s.row_end = min(d.rows, first + d.rows_per_block);
-  s.row_step = kWarps * per_warp;
-  return s;
-}
-Deal make_deal(int64_t rows, int32_t cols, int ctas_wanted, dim3* grid) {
+Deal make_deal(int64_t rows, int32_t cols, bool runs, int ctas_wanted, int64_t least_rows, dim3* grid) {
   Deal d;
   d.rows = rows;
   d.cols = cols;
-  d.lane_shift = 2;
+  d.lane_shift = runs ? 2 : 5;
   while (d.lane_shift < 5 && (8 << d.lane_shift) < cols) ++d.lane_shift;
   const int64_t segs = ceil_div64(cols, 8ll << d.lane_shift);
   const int64_t step = kWarps * (32 >> d.lane_shift);              // rows one pass of a block covers
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({ceil_div64(rows, step), ceil_div64(ctas_wanted, segs), 65535}));
+  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({ceil_div64(rows, step * least_rows), ceil_div64(ctas_wanted, segs), 65535}));
   d.rows_per_block = ceil_div64(ceil_div64(rows, blocks), step) * step;
   *grid = dim3((unsigned)segs, (unsigned)std::max<int64_t>(1, ceil_div64(rows, d.rows_per_block)));
   return d;
 }
+// Layout for these operands: runs where every one has 16-byte pieces (8-byte for codes), or rows too short for strides.
+bool use_runs(bool vec_a, bool vec_b, bool vec_c, int32_t cols) { return (vec_a && vec_b && vec_c) || cols <= 128; }
 
-// Largest magnitude of the group of 32 columns that four neighbouring lanes hold, as its bit pattern: for numbers without
-// sign the order of the patterns is the order of the values, and NaN comes out on top.
-__device__ __forceinline__ float group_top(const float (&v)[kRun]) {
-  uint32_t top = 0;
+// Raw pieces, so that several rows' loads can be outstanding before any is converted.
+template <int DT> struct Piece { uint32_t w[kRun * sizeof(typename Elem<DT>::T) / 4]; };
+template <int DT, bool RUNS>
+__device__ __forceinline__ void load_piece(const typename Elem<DT>::T* p, bool vec, int have, Piece<DT>& out) {
+  using T = typename Elem<DT>::T;
+  if (RUNS && vec) {
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  return __uint_as_float(top);
+    for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) *reinterpret_cast<uint4*>(out.w + 4 * i) = reinterpret_cast<const uint4*>(p)[i];
+  } else {
+    T* t = reinterpret_cast<T*>(out.w);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) t[j] = j < have ? p[j * Spot<RUNS>::step()] : Elem<DT>::down(0.f);
+  }
 }
+template <int DT>
+__device__ __forceinline__ void open_piece(const Piece<DT>& in, float (&v)[kRun]) {
+  const typename Elem<DT>::T* t = reinterpret_cast<const typename Elem<DT>::T*>(in.w);
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) v[j] = Elem<DT>::up(t[j]);
+}
+template <int DT, bool RUNS>
+__device__ __forceinline__ void store_piece(typename Elem<DT>::T* p, bool vec, int have, const float (&v)[kRun]) {
+  if (RUNS) {
+    store_run<DT, kRun>(p, vec, have, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j)
+      if (j < have) p[32 * j] = Elem<DT>::down(v[j]);
+  }
+}
+template <bool RUNS>
 __device__ __forceinline__ void store_codes(uint8_t* p, bool vec, int have, uint2 w) {
-  if (vec) {
+  if (RUNS && vec) {
     *reinterpret_cast<uint2*>(p) = w;
   } else {
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
-      if (j < have) p[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+      if (j < have) p[j * Spot<RUNS>::step()] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
   }
 }
-__device__ __forceinline__ uint2 load_codes(const uint8_t* __restrict__ p, bool vec, int have) {
-  if (vec) return *reinterpret_cast<const uint2*>(p);
+template <bool RUNS>
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, bool vec, int have) {
+  if (RUNS && vec) return *reinterpret_cast<const uint2*>(p);
   uint2 w = make_uint2(0u, 0u);
 #pragma unroll
   for (int j = 0; j < kRun; ++j)
-    if (j < have) (j < 4 ? w.x : w.y) |= (uint32_t)p[j] << (8 * (j & 3));
+    if (j < have) (j < 4 ? w.x : w.y) |= (uint32_t)p[j * Spot<RUNS>::step()] << (8 * (j & 3));
   return w;
 }
+// The exponent bytes of a thread's columns: one for a run, eight (of consecutive groups) for strides.
+template <bool RUNS>
+__device__ __forceinline__ uint2 load_exps(const uint8_t* row, int col, int have) {
+  uint2 e = make_uint2(0u, 0u);
+  if (RUNS) {
+    e.x = row[col / kGroup];
+  } else {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j)
+      if (j < have) (j < 4 ? e.x : e.y) |= (uint32_t)row[col / kGroup + j] << (8 * (j & 3));
+  }
+  return e;
+}
+template <bool RUNS>
+__device__ __forceinline__ void decode_piece(uint2 w, uint2 e, float (&v)[kRun]) {
+  if (RUNS) {
+    decode_run(w, (int)e.x, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j)
+      v[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step_of((int)((j < 4 ? e.x : e.y) >> (8 * (j & 3)) & 255u)));
+  }
+}
 
-template <int DT>
+template <int DT, bool RUNS>
 __global__ void __launch_bounds__(kThreads)
 pack8_kernel(Deal d, const void* __restrict__ x, int64_t ld_x, bool vec_x, lqsgd_packed8 out, bool vec_c) {
+  constexpr int kRows = DT == LQSGD_F32 ? 2 : 4;
   train_pdl_wait();
   using T = typename Elem<DT>::T;
-  const Spot s = spot_of(d);
-  const int sub = (threadIdx.x & 31) >> d.lane_shift;
+  const Spot<RUNS> s(d);
+  const bool vx = vec_x && s.have == kRun, vc = vec_c && s.have == kRun;
   // a warp whose last rows lie past the end stays together for the shuffles: those lanes hold zeros and store nothing
-  for (int64_t r0 = s.row; r0 - sub < s.row_end; r0 += s.row_step) {
-    const bool on = r0 < s.row_end && s.have > 0;
-    float v[kRun];
+  for (int64_t r0 = s.row; r0 - s.sub < s.row_end; r0 += kRows * s.row_step) {
+    Piece<DT> raw[kRows];
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] = 0.f;
-    if (on) load_run<DT, kRun>(static_cast<const T*>(x) + r0 * ld_x + s.col, vec_x && s.have == kRun, s.have, v);
-    const int eb = exp_byte(group_top(v));
-    const float inv = inv_step(eb);
-    if (on) {
-      const uint2 w = make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv));
-      store_codes(out.dev_codes + r0 * out.ld_codes + s.col, vec_c && s.have == kRun, s.have, w);
-      if ((s.col & (kGroup - 1)) == 0) out.dev_exps[r0 * out.ld_exps + s.col / kGroup] = (uint8_t)eb;
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * s.row_step;
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(raw[u].w) / 4); ++i) raw[u].w[i] = 0u;
+      if (r < s.row_end && s.have > 0) load_piece<DT, RUNS>(static_cast<const T*>(x) + r * ld_x + s.col, vx, s.have, raw[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * s.row_step;
+      if (r - s.sub >= s.row_end) break;
+      const bool on = r < s.row_end && s.have > 0;
+      float v[kRun];
+      open_piece<DT>(raw[u], v);
+      uint8_t* codes = out.dev_codes + r * out.ld_codes + s.col;
+      uint8_t* exps = out.dev_exps + r * out.ld_exps + s.col / kGroup;
+      if (RUNS) {
+        // magnitudes as bit patterns: their order is the values', and NaN comes out on top
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int eb = exp_byte(__uint_as_float(top));
+        const float inv = inv_step(eb);
+        if (on) {
+          store_codes<RUNS>(codes, vc, s.have, make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
+          if ((s.col & (kGroup - 1)) == 0) *exps = (uint8_t)eb;
+        }
+      } else {
+        const int lane = threadIdx.x & 31;
+        uint32_t mine = 0;                                // lane j keeps the j-th group's byte
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+          const int eb = exp_byte(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu)));
+          if (lane == j) mine = (uint32_t)eb;
+          const uint32_t c = (mag_bits(v[j], inv_step(eb)) & 127u) | ((__float_as_uint(v[j]) >> 24) & 128u);
+          if (on && j < s.have) codes[32 * j] = (uint8_t)c;
+        }
+        // the segment's groups that exist: those whose first column, lane 0's, does
+        if (r < s.row_end && lane < kRun && s.col - lane + 32 * lane < d.cols) exps[lane] = (uint8_t)mine;
+      }
     }
   }
 }
 
-template <int DT>
+template <int DT, bool RUNS>
 __global__ void __launch_bounds__(kThreads)
 unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64_t ld_y, bool vec_y) {
+  constexpr int kRows = 4;
   train_pdl_wait();
   using T = typename Elem<DT>::T;
-  const Spot s = spot_of(d);
+  const Spot<RUNS> s(d);
   if (s.have <= 0) return;
-  for (int64_t r = s.row; r < s.row_end; r += s.row_step) {
-    const uint2 w = load_codes(in.dev_codes + r * in.ld_codes + s.col, vec_c && s.have == kRun, s.have);
-    const float step = step_of(in.dev_exps[r * in.ld_exps + s.col / kGroup]);
-    float v[kRun];
+  const bool vy = vec_y && s.have == kRun, vc = vec_c && s.have == kRun;
+  for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
+    uint2 w[kRows], e[kRows];
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-      v[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step);
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
+      w[u] = load_codes<RUNS>(in.dev_codes + r * in.ld_codes + s.col, vc, s.have);
+      e[u] = load_exps<RUNS>(in.dev_exps + r * in.ld_exps, s.col, s.have);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * s.row_step;
+      if (r >= s.row_end) break;
+      float v[kRun];
+      decode_piece<RUNS>(w[u], e[u], v);
       // only sources wider than the target can exceed its range: the largest finite value then (a NaN stays)
       constexpr float kTop = DT == LQSGD_F16 ? 65504.f : (DT == LQSGD_BF16 ? 3.3895314e38f : 3.402823466e38f);
-      if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
+      if (DT != LQSGD_F32 && (!RUNS || (int)e[u].x >= (DT == LQSGD_F16 ? kExpBias + 9 : kQuickByte))) {
+#pragma unroll
+        for (int j = 0; j < kRun; ++j)
+          if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
+      }
+      store_piece<DT, RUNS>(static_cast<T*>(y) + r * ld_y + s.col, vy, s.have, v);
     }
-    store_run<DT, kRun>(static_cast<T*>(y) + r * ld_y + s.col, vec_y && s.have == kRun, s.have, v);
   }
 }
 
 // dz = dy act'(z); the block's column sums of dz go to partial[blockIdx.y][cols].
-template <int DT>
+// GELU's and SiLU's slopes cost 20 to 30 instructions, more than HBM leaves time for.  But z takes few values: 128 magnitudes
+// times a step, and both slopes satisfy s(-z) = 1 - s(z).  So a block that has work enough first tabulates the slopes for the
+// steps 2^-16 .. 2^4; below them the slope is 1/2 + s'(0) z to 2^-31, above them 0 or 1 (or 1/2 at 0) to 2^-23: those, and
+// blocks with little work, compute them.
+enum SlopeKind { kSlopeNone = 0, kSlopeRelu = 1, kSlopeCurve = 2 };
+constexpr int kTabLow = kExpBias - 16, kTabSteps = 21;
+template <int DT, bool RUNS, int KIND>
 __global__ void __launch_bounds__(kThreads)
-act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed8 z8, bool vec_c, int act,
+act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed8 z8, bool vec_c, int act, bool table,
                 void* dz, int64_t ld_dz, bool vec_dz, float* __restrict__ partial) {
-  train_pdl_wait();
+  constexpr int kRows = DT == LQSGD_F32 ? 2 : 4;
   using T = typename Elem<DT>::T;
+  __shared__ float tab[KIND == kSlopeCurve ? kTabSteps * 128 : 1];
   __shared__ float sums[kWarps][32][kRun + 1];
-  const Spot s = spot_of(d);
+  const Spot<RUNS> s(d);
+  if (KIND == kSlopeCurve && table) {
+    for (int i = threadIdx.x; i < kTabSteps * 128; i += kThreads) {
+      const float z = (float)(i & 127) * step_of(kTabLow + (i >> 7));
+      tab[i] = act == LQSGD_ACT_GELU ? act_slope<LQSGD_ACT_GELU>(z) : act_slope<LQSGD_ACT_SILU>(z);
+    }
+    __syncthreads();
+  }
+  train_pdl_wait();
+  const bool vg = vec_dy && s.have == kRun, vz = vec_dz && s.have == kRun, vc = vec_c && s.have == kRun;
   float acc[kRun];
 #pragma unroll
   for (int j = 0; j < kRun; ++j) acc[j] = 0.f;
   if (s.have > 0)
-    for (int64_t r = s.row; r < s.row_end; r += s.row_step) {
-      float g[kRun];
-      load_run<DT, kRun>(static_cast<const T*>(dy) + r * ld_dy + s.col, vec_dy && s.have == kRun, s.have, g);
-      if (act != LQSGD_ACT_NONE) {
-        const uint2 w = load_codes(z8.dev_codes + r * z8.ld_codes + s.col, vec_c && s.have == kRun, s.have);
-        const float step = step_of(z8.dev_exps[r * z8.ld_exps + s.col / kGroup]);
-        float z[kRun];
+    for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
+      Piece<DT> raw[kRows];
+      uint2 w[kRows], e[kRows];
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) z[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step);
-        slope_run(act, z);
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) g[j] *= z[j];
+      for (int u = 0; u < kRows; ++u) {
+        const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
+        load_piece<DT, RUNS>(static_cast<const T*>(dy) + r * ld_dy + s.col, vg, s.have, raw[u]);
+        if (KIND != kSlopeNone) {
+          w[u] = load_codes<RUNS>(z8.dev_codes + r * z8.ld_codes + s.col, vc, s.have);
+          e[u] = load_exps<RUNS>(z8.dev_exps + r * z8.ld_exps, s.col, s.have);
+        }
       }
-      if (dz) store_run<DT, kRun>(static_cast<T*>(dz) + r * ld_dz + s.col, vec_dz && s.have == kRun, s.have, g);
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) acc[j] += g[j];
+      for (int u = 0; u < kRows; ++u) {
+        const int64_t r = r0 + u * s.row_step;
+        if (r >= s.row_end) break;
+        float g[kRun], z[kRun];
+        open_piece<DT>(raw[u], g);
+        if (KIND == kSlopeRelu) {
+          // 1 for a positive value, 0 for the others, NaN for a group that is not finite
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) {
+            const uint32_t c = (j < 4 ? w[u].x : w[u].y) >> (8 * (j & 3)) & 255u;
+            const uint32_t eb = RUNS ? e[u].x : (j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u;
+            const float one = c - 1u < 127u ? 1.f : 0.f;                // 1 .. 127
+            g[j] *= eb == kExpNonFinite ? step_of(kExpNonFinite) : one;
+          }
+        } else if (KIND == kSlopeCurve) {
+          bool quick = table;
+          if (RUNS) {
+            quick = quick && e[u].x - kTabLow < (uint32_t)kTabSteps;
+          } else {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) quick = quick && (j >= s.have || ((j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u) - kTabLow < (uint32_t)kTabSteps);
+          }
+          if (quick) {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) {
+              const uint32_t c = (j < 4 ? w[u].x : w[u].y) >> (8 * (j & 3));
+              const uint32_t eb = RUNS ? e[u].x : (j < s.have ? (j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u : (uint32_t)kTabLow);
+              const float t = tab[(eb - kTabLow) * 128 + (c & 127u)];
+              g[j] *= c & 128u ? 1.f - t : t;
+            }
+          } else {
+            decode_piece<RUNS>(w[u], e[u], z);
+            if (act == LQSGD_ACT_GELU) {
+#pragma unroll
+              for (int j = 0; j < kRun; ++j) g[j] *= act_slope<LQSGD_ACT_GELU>(z[j]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < kRun; ++j) g[j] *= act_slope<LQSGD_ACT_SILU>(z[j]);
+            }
+          }
+        }
+        if (dz) store_piece<DT, RUNS>(static_cast<T*>(dz) + r * ld_dz + s.col, vz, s.have, g);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) acc[j] += g[j];
+      }
     }
   if (!partial) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -179,36 +337,40 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
   for (int c = threadIdx.x; c < lanes * kRun; c += kThreads) {
     const int col = (int)blockIdx.x * lanes * kRun + c;
     if (col >= d.cols) continue;
+    const int from = RUNS ? c / kRun : c & 31, j = RUNS ? c % kRun : c >> 5;
     float t = 0.f;
     for (int w = 0; w < kWarps; ++w)
-      for (int sub = 0; sub < (32 >> d.lane_shift); ++sub) t += sums[w][(sub << d.lane_shift) + c / kRun][c % kRun];
+      for (int sub = 0; sub < (32 >> d.lane_shift); ++sub) t += sums[w][(sub << d.lane_shift) + from][j];
     partial[(size_t)blockIdx.y * d.cols + col] = t;
   }
 }
 
-// out[c] = sum over b of partial[b][c], 32 columns x 8 threads per block, fixed order.
-__global__ void __launch_bounds__(kThreads)
+// out[c] = sum over b of partial[b][c]: 32 columns x 32 warps per block, fixed order.
+__global__ void __launch_bounds__(1024)
 join_columns_kernel(const float* __restrict__ partial, int blocks, int cols, float* __restrict__ out) {
   train_pdl_wait();
-  __shared__ float part[kWarps][33];
+  __shared__ float part[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int col = (int)blockIdx.x * 32 + lane;
   float t = 0.f;
-  if (col < cols)
-    for (int b = warp; b < blocks; b += kWarps) t += partial[(size_t)b * cols + col];
+  if (col < cols) {
+#pragma unroll 8
+    for (int b = warp; b < blocks; b += 32) t += partial[(size_t)b * cols + col];
+  }
   part[warp][lane] = t;
   __syncthreads();
   if (warp == 0 && col < cols) {
     float u = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) u += part[w][lane];
+    for (int w = 0; w < 32; ++w) u += part[w][lane];
     out[col] = u;
   }
 }
 
-// CTAs that fill the card: 148 SMs x 8 blocks of 256 threads.  A constant, so that the order of the sums (and the
-// workspace) depends on the sizes alone.
-constexpr int kCtas = 148 * 8;
+// CTAs that fill the card: 148 SMs x 8 blocks of 256 threads (x 4 where they leave column sums behind to be joined).  Constants,
+// so that the order of the sums, and the workspace, depend on the sizes alone.
+constexpr int kCtas = 148 * 8, kCtasSums = 148 * 4;
+Deal deal_sums(int64_t rows, int32_t cols, bool runs, dim3* grid) { return make_deal(rows, cols, runs, kCtasSums, 4, grid); }
 
 int check_matrix(int64_t rows, int32_t cols) {
   return rows < 0 || cols < 1 || rows > (int64_t)1 << 40 ? LQSGD_ERR_BAD_SHAPE : LQSGD_OK;
@@ -219,10 +381,10 @@ int check_matrix(int64_t rows, int32_t cols) {
 
 using namespace lqsgd;
 
-#define BY_DTYPE(dtype, kernel, ...)                                               \
-  ((dtype) == LQSGD_BF16 ? train_launch(kernel<LQSGD_BF16>, __VA_ARGS__)           \
-   : (dtype) == LQSGD_F16 ? train_launch(kernel<LQSGD_F16>, __VA_ARGS__)           \
-                          : train_launch(kernel<LQSGD_F32>, __VA_ARGS__))
+#define BY_DTYPE(dtype, runs, kernel, ...)                                                       \
+  ((dtype) == LQSGD_BF16 ? ((runs) ? train_launch(kernel<LQSGD_BF16, true>, __VA_ARGS__) : train_launch(kernel<LQSGD_BF16, false>, __VA_ARGS__)) \
+   : (dtype) == LQSGD_F16 ? ((runs) ? train_launch(kernel<LQSGD_F16, true>, __VA_ARGS__) : train_launch(kernel<LQSGD_F16, false>, __VA_ARGS__))  \
+                          : ((runs) ? train_launch(kernel<LQSGD_F32, true>, __VA_ARGS__) : train_launch(kernel<LQSGD_F32, false>, __VA_ARGS__)))
 
 static bool vec_rows(const void* p, int64_t ld, int elem, int bytes) {
   return train_aligned(p, bytes) && (ld * elem) % bytes == 0;
@@ -238,10 +400,11 @@ extern "C" int lqsgd_pack8(const void* dev_x, int64_t ld_x, int32_t dtype, int64
   if ((rc = check_packed8(*host_out, cols)) != LQSGD_OK) return rc;
   const int es = train_elem(dtype);
   if (!train_aligned(dev_x, es)) return LQSGD_ERR_MISALIGNED;
-  dim3 grid;
-  const Deal d = make_deal(rows, cols, kCtas, &grid);
   const bool vx = vec_rows(dev_x, ld_x, es, 16), vc = vec_rows(host_out->dev_codes, host_out->ld_codes, 1, 8);
-  TRAIN_CK(BY_DTYPE(dtype, pack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, dev_x, ld_x, vx, *host_out, vc), "pack8_kernel launch");
+  const bool runs = use_runs(vx, vc, true, cols);
+  dim3 grid;
+  const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
+  TRAIN_CK(BY_DTYPE(dtype, runs, pack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, dev_x, ld_x, vx, *host_out, vc), "pack8_kernel launch");
   return LQSGD_OK;
 }
 
@@ -255,12 +418,16 @@ extern "C" int lqsgd_unpack8(const lqsgd_packed8* host_in, int64_t rows, int32_t
   if ((rc = check_packed8(*host_in, cols)) != LQSGD_OK) return rc;
   const int es = train_elem(dtype);
   if (!train_aligned(dev_y, es)) return LQSGD_ERR_MISALIGNED;
-  dim3 grid;
-  const Deal d = make_deal(rows, cols, kCtas, &grid);
   const bool vy = vec_rows(dev_y, ld_y, es, 16), vc = vec_rows(host_in->dev_codes, host_in->ld_codes, 1, 8);
-  TRAIN_CK(BY_DTYPE(dtype, unpack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, *host_in, vc, dev_y, ld_y, vy), "unpack8_kernel launch");
+  const bool runs = use_runs(vy, vc, true, cols);
+  dim3 grid;
+  const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
+  TRAIN_CK(BY_DTYPE(dtype, runs, unpack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, *host_in, vc, dev_y, ld_y, vy), "unpack8_kernel launch");
   return LQSGD_OK;
 }
+
+// Row blocks of act_grad's column sums; the workspace has room for either layout.
+static size_t sums_bytes(const dim3& grid, int32_t cols) { return grid.y > 1 ? (size_t)grid.y * cols * sizeof(float) : 0; }
 
 extern "C" int lqsgd_act_grad_workspace_bytes(int64_t rows, int32_t cols, size_t* host_bytes_out) {
   if (!host_bytes_out) return LQSGD_ERR_INVALID_ARG;
@@ -268,10 +435,23 @@ extern "C" int lqsgd_act_grad_workspace_bytes(int64_t rows, int32_t cols, size_t
   if (rc != LQSGD_OK) return rc;
   *host_bytes_out = 0;
   if (rows == 0) return LQSGD_OK;
-  dim3 grid;
-  make_deal(rows, cols, kCtas, &grid);
-  *host_bytes_out = grid.y > 1 ? (size_t)grid.y * cols * sizeof(float) : 0;
+  dim3 a, b;
+  deal_sums(rows, cols, true, &a);
+  deal_sums(rows, cols, cols <= 128, &b);
+  *host_bytes_out = std::max(sums_bytes(a, cols), sums_bytes(b, cols));
   return LQSGD_OK;
+}
+
+template <int DT, bool RUNS>
+static cudaError_t launch_act_grad(int act, dim3 grid, cudaStream_t st, const Deal& d, const void* dy, int64_t ld_dy, bool vg, const lqsgd_packed8& z8,
+                                   bool vc, void* dz, int64_t ld_dz, bool vz, float* partial) {
+  if (act == LQSGD_ACT_NONE)
+    return train_launch(act_grad_kernel<DT, RUNS, kSlopeNone>, grid, dim3(kThreads), 0, st, 1, d, dy, ld_dy, vg, z8, vc, act, false, dz, ld_dz, vz, partial);
+  if (act == LQSGD_ACT_RELU)
+    return train_launch(act_grad_kernel<DT, RUNS, kSlopeRelu>, grid, dim3(kThreads), 0, st, 1, d, dy, ld_dy, vg, z8, vc, act, false, dz, ld_dz, vz, partial);
+  // a block's table takes about ten slopes per thread: worth it from four times as many values on
+  const bool table = d.rows_per_block * (kRun << d.lane_shift) >= 40 * kThreads;
+  return train_launch(act_grad_kernel<DT, RUNS, kSlopeCurve>, grid, dim3(kThreads), 0, st, 1, d, dy, ld_dy, vg, z8, vc, act, table, dz, ld_dz, vz, partial);
 }
 
 extern "C" int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_packed8* host_z8, int32_t act, int32_t dtype,
@@ -296,18 +476,29 @@ extern "C" int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_pac
   }
   const int es = train_elem(dtype);
   if (!train_aligned(dev_dy, es) || !train_aligned(dev_dz, es)) return LQSGD_ERR_MISALIGNED;
+  const bool vg = vec_rows(dev_dy, ld_dy, es, 16), vz = !dev_dz || vec_rows(dev_dz, ld_dz, es, 16),
+             vc = act == LQSGD_ACT_NONE || vec_rows(z8.dev_codes, z8.ld_codes, 1, 8);
+  const bool runs = use_runs(vg, vz, vc, cols);
   dim3 grid;
-  const Deal d = make_deal(rows, cols, kCtas, &grid);
+  const Deal d = deal_sums(rows, cols, runs, &grid);
   float* partial = dev_db;
   if (dev_db && grid.y > 1) {
-    if (!dev_workspace || workspace_bytes < (size_t)grid.y * cols * sizeof(float)) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
+    if (!dev_workspace || workspace_bytes < sums_bytes(grid, cols)) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
     if (!train_aligned(dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;
     partial = static_cast<float*>(dev_workspace);
   }
-  TRAIN_CK(BY_DTYPE(dtype, act_grad_kernel, grid, dim3(kThreads), 0, st, 1, d, dev_dy, ld_dy, vec_rows(dev_dy, ld_dy, es, 16), z8,
-                    vec_rows(z8.dev_codes, z8.ld_codes, 1, 8), act, dev_dz, ld_dz, vec_rows(dev_dz, ld_dz, es, 16), partial),
-           "act_grad_kernel launch");
+  cudaError_t e;
+  if (dtype == LQSGD_BF16)
+    e = runs ? launch_act_grad<LQSGD_BF16, true>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial)
+             : launch_act_grad<LQSGD_BF16, false>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial);
+  else if (dtype == LQSGD_F16)
+    e = runs ? launch_act_grad<LQSGD_F16, true>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial)
+             : launch_act_grad<LQSGD_F16, false>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial);
+  else
+    e = runs ? launch_act_grad<LQSGD_F32, true>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial)
+             : launch_act_grad<LQSGD_F32, false>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial);
+  TRAIN_CK(e, "act_grad_kernel launch");
   if (partial != dev_db)
-    TRAIN_CK(train_launch(join_columns_kernel, dim3((cols + 31) / 32), dim3(kThreads), 0, st, 1, partial, (int)grid.y, cols, dev_db), "join_columns_kernel launch");
+    TRAIN_CK(train_launch(join_columns_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, 1, partial, (int)grid.y, cols, dev_db), "join_columns_kernel launch");
   return LQSGD_OK;
 }

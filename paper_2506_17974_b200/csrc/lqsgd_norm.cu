@@ -1,15 +1,21 @@
 // Group norm with an activation on channels-last tensors, forward and backward.
 //
-// A thread owns 8 consecutive channels and walks over pixels, so that a warp reads whole 16-byte pieces of neighbouring
-// pixels, and what it sums stays in its registers per channel: groups of any width, and rows of any alignment, need no
-// special case.  Per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups' figures; the
-// last kernel reads the tensor a second time and applies them.
+// A thread owns 8 consecutive channels (16 bytes of a 16-bit type) and walks over pixels; what it sums stays in its registers
+// per channel, so groups of any width need no special case.  What bounds it is HBM: every tensor should be read once.
 //
-// Forward sums are kept as (mean, sum of squared distances from it) about a value of the channel itself and merged
-// pairwise: a mean far from zero cancels nothing.
+// Resident kernels (rows of 16-byte pieces, slices that fit): a cluster of 1 .. 8 CTAs takes one sample's block of whole groups
+// (at least 64 bytes of a pixel), each CTA a range of its pixels, and brings it into shared memory with asynchronous
+// copies of 16 bytes (no registers are held meanwhile, so the whole slice is in flight at once).  Sums meet through
+// distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
+//
+// Streaming kernels (everything else): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
+// figures, and a last kernel reads the tensor a second time (from L2 up to about 100 MB) and applies them.  Their forward sums
+// are (mean, squared distances from it) about a value of the channel itself, merged pairwise; the resident kernel takes the
+// mean first and the distances from it in a second pass.  Either way a mean far from zero cancels nothing.
 #include "lqsgd_train_dev.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace lqsgd {
 namespace {
@@ -69,7 +75,7 @@ __device__ __forceinline__ void load_x(const NormDev& d, const Spot& s, int pix,
   if (d.x8.dev_codes) {                                     // only the backward kernels set it as an input
     const int64_t row = (int64_t)s.sample * d.hw + pix;
     const uint8_t* p = d.x8.dev_codes + row * d.x8.ld_codes + s.col;
-    const float step = step_of(d.x8.dev_exps[row * d.x8.ld_exps + s.col / kGroup]);
+    const int eb = d.x8.dev_exps[row * d.x8.ld_exps + s.col / kGroup];
     uint2 w = make_uint2(0u, 0u);
     if (d.vec_x8 && s.have == kRun) {
       w = *reinterpret_cast<const uint2*>(p);
@@ -78,8 +84,7 @@ __device__ __forceinline__ void load_x(const NormDev& d, const Spot& s, int pix,
       for (int j = 0; j < kRun; ++j)
         if (j < s.have) (j < 4 ? w.x : w.y) |= (uint32_t)p[j] << (8 * (j & 3));
     }
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step);
+    decode_run(w, eb, v);
     return;
   }
   load_run<DT, kRun>(static_cast<const T*>(d.x) + s.sample * d.sample_x + pix * d.ld_x + s.col, d.vec_x && s.have == kRun, s.have, v);
@@ -355,6 +360,399 @@ norm_grad_apply_kernel(NormDev d) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------------- resident kernels
+struct Resident {
+  NormDev d;
+  int32_t cb;                         // channels of a block: whole groups, a multiple of 8 (of 32 where something is packed)
+  int32_t blocks;                     // blocks per sample
+  int32_t lane_shift;                 // a pixel's 8-channel pieces are dealt to 1 << lane_shift threads
+  int32_t parts;                      // CTAs (of one cluster) that share the pixels
+  int32_t part_rows, steps;           // pixels per CTA; pieces per thread
+};
+constexpr int kResThreads = 256, kResWarps = kResThreads / 32;
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(dst)), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_at(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void norm_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float read_peer(const float* p, uint32_t rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_at(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+struct Place {
+  int sample, c0, channels;           // the block's first channel and how many it has (the last block may have fewer)
+  int part, first, rows;              // this CTA's pixels
+  int col, row, row_step;             // the thread's first channel (of the tensor) and its pixels row, row + row_step, ... < rows
+  bool on;
+};
+__device__ __forceinline__ Place place_of(const Resident& r) {
+  Place q;
+  q.part = r.parts > 1 ? (int)(blockIdx.x % (unsigned)r.parts) : 0;
+  const unsigned unit = r.parts > 1 ? blockIdx.x / (unsigned)r.parts : blockIdx.x;
+  q.sample = (int)(unit / (unsigned)r.blocks);
+  q.c0 = (int)(unit - (unsigned)q.sample * r.blocks) * r.cb;
+  q.channels = min(r.cb, r.d.c - q.c0);
+  q.first = q.part * r.part_rows;
+  q.rows = min(r.part_rows, r.d.hw - q.first);
+  const int piece = threadIdx.x & ((1 << r.lane_shift) - 1);
+  q.col = q.c0 + piece * kRun;
+  q.row = threadIdx.x >> r.lane_shift;
+  q.row_step = kResThreads >> r.lane_shift;
+  q.on = piece * kRun < q.channels;
+  return q;
+}
+
+// Sums over the block's threads per channel: v[j] of every thread -> chan[channel of the block].  Lanes of a warp that have the
+// same channels are folded first; then a thread per channel adds the warps, in order.
+__device__ __forceinline__ void channel_sums(const Resident& r, float (&v)[kRun], float* scratch, float* chan, int channels) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int o = 16; o >= (1 << r.lane_shift); o >>= 1) {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) v[j] += __shfl_down_sync(0xffffffffu, v[j], o);
+  }
+  __syncthreads();                                        // scratch and chan are free
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) scratch[(warp * 32 + lane) * (kRun + 1) + j] = v[j];
+  __syncthreads();
+  const int wide = max(1, (1 << r.lane_shift) >> 5);       // warps that a pixel spans
+  for (int ch = threadIdx.x; ch < channels; ch += kResThreads) {
+    const int piece = ch / kRun;
+    float t = 0.f;
+    for (int w = piece >> 5; w < kResWarps; w += wide) t += scratch[(w * 32 + (piece & 31)) * (kRun + 1) + ch % kRun];
+    chan[ch] = t;
+  }
+  __syncthreads();
+}
+// Group totals of chan (times weight, if given) over the block and the cluster: total[g], the same bits in every CTA.
+__device__ __forceinline__ void group_totals(const Resident& r, const Place& q, const float* chan, const float* __restrict__ weight, float* mine, float* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cpg = r.d.cpg, groups = q.channels / cpg;
+  for (int g = warp; g < groups; g += kResWarps) {
+    float t = 0.f;
+    for (int i = lane; i < cpg; i += 32) t += weight ? chan[g * cpg + i] * weight[q.c0 + g * cpg + i] : chan[g * cpg + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_down_sync(0xffffffffu, t, o);
+    if (lane == 0) (r.parts > 1 ? mine : total)[g] = t;
+  }
+  if (r.parts > 1) {
+    norm_cluster_sync();
+    for (int g = threadIdx.x; g < groups; g += kResThreads) {
+      float t = 0.f;
+      for (int k = 0; k < r.parts; ++k) t += read_peer(mine + g, k);
+      total[g] = t;
+    }
+  }
+  __syncthreads();
+}
+
+template <int DT>
+__device__ __forceinline__ void unpack_run(const uint8_t* p, float (&v)[kRun]) {
+  using T = typename Elem<DT>::T;
+#pragma unroll
+  for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) {
+    const uint4 w = reinterpret_cast<const uint4*>(p)[i];
+    const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[i * (16 / (int)sizeof(T)) + j] = Elem<DT>::up(t[j]);
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kResThreads)
+norm_resident_kernel(Resident r) {
+  using T = typename Elem<DT>::T;
+  constexpr int kBytes = kRun * (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t res_smem[];
+  const NormDev& d = r.d;
+  const Place q = place_of(r);
+  uint8_t* data = res_smem;                                             // [steps][threads] pieces
+  float* scratch = reinterpret_cast<float*>(data + (size_t)r.steps * kResThreads * kBytes);
+  float* chan = scratch + kResThreads * (kRun + 1);                     // [cb]
+  float* mine = chan + r.cb;                                            // [2][groups of a block]
+  const int groups_cap = r.cb / d.cpg;
+  float* mean = mine + 2 * groups_cap;                                  // [groups]
+  float* rstd = mean + groups_cap;
+  train_pdl_wait();
+  const T* src = static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)q.first * d.ld_x + q.col;
+  uint8_t* own = data + threadIdx.x * kBytes;
+  if (q.on)
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i)
+        copy_async<16>(own + (size_t)k * kResThreads * kBytes + 16 * i, reinterpret_cast<const uint8_t*>(src + p * d.ld_x) + 16 * i);
+    }
+  copy_async_wait();
+  float s[kRun], v[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) s[j] = 0.f;
+  if (q.on)
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+      unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) s[j] += v[j];
+    }
+  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
+  channel_sums(r, s, scratch, chan, q.channels);
+  group_totals(r, q, chan, nullptr, mine, mean);
+  const int groups = q.channels / d.cpg;
+  for (int g = threadIdx.x; g < groups; g += kResThreads) mean[g] *= inv;
+  __syncthreads();
+  float m[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    s[j] = 0.f;
+    m[j] = q.on ? mean[(q.col - q.c0 + j) / d.cpg] : 0.f;
+  }
+  if (q.on)
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+      unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) { const float t = v[j] - m[j]; s[j] = fmaf(t, t, s[j]); }
+    }
+  channel_sums(r, s, scratch, chan, q.channels);
+  group_totals(r, q, chan, nullptr, mine + groups_cap, rstd);
+  for (int g = threadIdx.x; g < groups; g += kResThreads) {
+    rstd[g] = 1.f / sqrtf(rstd[g] * inv + d.eps);
+    if (q.part == 0) {
+      const size_t at = (size_t)q.sample * d.groups + q.c0 / d.cpg + g;
+      d.mean[at] = mean[g];
+      d.rstd[at] = rstd[g];
+    }
+  }
+  __syncthreads();
+  float scale[kRun], beta[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    scale[j] = q.on ? rstd[(q.col - q.c0 + j) / d.cpg] * __ldg(d.gamma + q.col + j) : 0.f;
+    beta[j] = q.on ? __ldg(d.beta + q.col + j) : 0.f;
+  }
+  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)q.first * d.ld_out + q.col;
+  const bool packs = d.x8.dev_codes || d.y8.dev_codes;                  // then groups of 32 need the warp together
+  const int lead = packs ? (int)((threadIdx.x & 31) >> min(r.lane_shift, 5)) : 0;
+  for (int p = q.row, k = 0; p - lead < q.rows; p += q.row_step, ++k) {
+    const bool on = q.on && p < q.rows;
+    const int64_t row = (int64_t)q.sample * d.hw + q.first + p;
+    if (on) unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
+    if (d.x8.dev_codes) pack_run(d.x8, d.vec_x8, row, q.col, kRun, on, v);
+    if (on) {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) v[j] = fmaf(v[j] - m[j], scale[j], beta[j]);
+      act_run(d.act, v);
+      store_run<DT, kRun>(dst + p * d.ld_out, true, kRun, v);
+    }
+    if (d.y8.dev_codes) {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
+      pack_run(d.y8, d.vec_y8, row, q.col, kRun, on, v);
+    }
+  }
+  if (r.parts > 1) norm_cluster_sync();                                 // nobody leaves while its sums may be read
+}
+
+// KEPT: x comes from its 8-bit form.
+template <int DT, bool KEPT>
+__global__ void __launch_bounds__(kResThreads)
+norm_grad_resident_kernel(Resident r) {
+  using T = typename Elem<DT>::T;
+  constexpr int kDy = kRun * (int)sizeof(T), kX = KEPT ? kRun : kDy, kBytes = kDy + kX;
+  extern __shared__ __align__(16) uint8_t res_smem[];
+  const NormDev& d = r.d;
+  const Place q = place_of(r);
+  uint8_t* dys = res_smem;                                              // [steps][threads] pieces of dy, then of x
+  uint8_t* xs = dys + (size_t)r.steps * kResThreads * kDy;
+  float* scratch = reinterpret_cast<float*>(res_smem + (size_t)r.steps * kResThreads * kBytes);
+  float* chan = scratch + kResThreads * (kRun + 1);
+  float* mine = chan + r.cb;
+  const int groups_cap = r.cb / d.cpg;
+  float* t0 = mine + 2 * groups_cap;
+  float* t1 = t0 + groups_cap;
+  train_pdl_wait();
+  const T* gsrc = static_cast<const T*>(d.dy) + q.sample * d.sample_dy + (int64_t)q.first * d.ld_dy + q.col;
+  const T* xsrc = static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)q.first * d.ld_x + q.col;
+  const int64_t row0 = (int64_t)q.sample * d.hw + q.first;
+  const uint8_t* csrc = d.x8.dev_codes + row0 * d.x8.ld_codes + q.col;
+  const uint8_t* esrc = d.x8.dev_exps + row0 * d.x8.ld_exps + q.col / kGroup;
+  uint8_t* gown = dys + threadIdx.x * kDy;
+  uint8_t* xown = xs + threadIdx.x * kX;
+  if (q.on)
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+#pragma unroll
+      for (int i = 0; i < kDy / 16; ++i)
+        copy_async<16>(gown + (size_t)k * kResThreads * kDy + 16 * i, reinterpret_cast<const uint8_t*>(gsrc + p * d.ld_dy) + 16 * i);
+      if constexpr (KEPT) {
+        copy_async<8>(xown + (size_t)k * kResThreads * kX, csrc + p * d.x8.ld_codes);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kX / 16; ++i)
+          copy_async<16>(xown + (size_t)k * kResThreads * kX + 16 * i, reinterpret_cast<const uint8_t*>(xsrc + p * d.ld_x) + 16 * i);
+      }
+    }
+  float mean[kRun], rstd[kRun], gamma[kRun], beta[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    const int ch = q.on ? q.col + j : q.c0;
+    const size_t at = (size_t)q.sample * d.groups + ch / d.cpg;
+    mean[j] = d.mean[at];
+    rstd[j] = d.rstd[at];
+    gamma[j] = __ldg(d.gamma + ch);
+    beta[j] = __ldg(d.beta + ch);
+  }
+  copy_async_wait();
+  // xh and dh = dy act'(h) of the thread's k-th piece
+  auto piece = [&](int p, int k, float (&xh)[kRun], float (&dh)[kRun]) {
+    if constexpr (KEPT) {
+      const uint2 w = *reinterpret_cast<const uint2*>(xown + (size_t)k * kResThreads * kX);
+      decode_run(w, esrc[p * d.x8.ld_exps], xh);
+    } else {
+      unpack_run<DT>(xown + (size_t)k * kResThreads * kX, xh);
+    }
+    float h[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) { xh[j] = (xh[j] - mean[j]) * rstd[j]; h[j] = fmaf(xh[j], gamma[j], beta[j]); }
+    slope_run(d.act, h);
+    unpack_run<DT>(gown + (size_t)k * kResThreads * kDy, dh);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) dh[j] *= h[j];
+  };
+  float a[kRun], b[kRun], xh[kRun], dh[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) a[j] = b[j] = 0.f;
+  if (q.on)
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+      piece(p, k, xh, dh);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) { a[j] += dh[j]; b[j] = fmaf(dh[j], xh[j], b[j]); }
+    }
+  const size_t out_row = ((size_t)q.sample * r.parts + q.part) * d.c + q.c0;
+  channel_sums(r, a, scratch, chan, q.channels);
+  for (int ch = threadIdx.x; ch < q.channels; ch += kResThreads) d.part0[out_row + ch] = chan[ch];
+  group_totals(r, q, chan, d.gamma, mine, t0);
+  channel_sums(r, b, scratch, chan, q.channels);
+  for (int ch = threadIdx.x; ch < q.channels; ch += kResThreads) d.part1[out_row + ch] = chan[ch];
+  group_totals(r, q, chan, d.gamma, mine + groups_cap, t1);
+  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
+  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)q.first * d.ld_out + q.col;
+  if (q.on) {
+    float c0[kRun], c1[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      const int g = (q.col - q.c0 + j) / d.cpg;
+      c0[j] = t0[g] * inv;
+      c1[j] = t1[g] * inv;
+    }
+    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+      piece(p, k, xh, dh);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) xh[j] = rstd[j] * (gamma[j] * dh[j] - c0[j] - xh[j] * c1[j]);
+      store_run<DT, kRun>(dst + p * d.ld_out, true, kRun, xh);
+    }
+  }
+  if (r.parts > 1) norm_cluster_sync();
+}
+
+// dgamma and dbeta: sums over the rows of part1 and part0, 32 channels per block.
+__global__ void __launch_bounds__(1024)
+norm_dparam_kernel(NormDev d, int rows) {
+  train_pdl_wait();
+  __shared__ float s0[32][33], s1[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int col = (int)blockIdx.x * 32 + lane;
+  float a = 0.f, b = 0.f;
+  if (col < d.c) {
+#pragma unroll 8
+    for (int r = warp; r < rows; r += 32) {
+      a += d.part0[(size_t)r * d.c + col];
+      b += d.part1[(size_t)r * d.c + col];
+    }
+  }
+  s0[warp][lane] = a;
+  s1[warp][lane] = b;
+  __syncthreads();
+  if (warp < 2 && col < d.c) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) t += (warp ? s1 : s0)[k][lane];
+    (warp ? d.dgamma : d.dbeta)[col] = t;
+  }
+}
+
+constexpr size_t kResSmemMax = 200 * 1024;
+
+// Whether the resident kernels take a problem, and how.  piece_bytes: shared memory per 8 channels of a pixel.
+bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
+  auto gcd = [](int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; };
+  if (d.c % kRun) return false;
+  const int unit = packs ? kGroup : kRun;
+  const int64_t base = (int64_t)d.cpg / gcd(d.cpg, unit) * unit;
+  Resident best = {};
+  double best_score = 1e30;
+  for (int64_t cb = base;; cb += base) {
+    const int64_t block = std::min<int64_t>(cb, d.c);
+    if (block > kResThreads * kRun) break;
+    // 64 bytes of a pixel at least, where it has them
+    const bool last = block == d.c;
+    if (block * (piece_bytes < 32 ? 2 : 4) < 64 && !last) continue;
+    Resident r = {};
+    r.d = d;
+    r.cb = (int)block;
+    r.blocks = (int)ceil_div64(d.c, block);
+    if (packs) r.lane_shift = 2;                            // a group of 32 is four neighbouring lanes
+    while ((kRun << r.lane_shift) < block) ++r.lane_shift;
+    const int row_step = kResThreads >> r.lane_shift;
+    for (int parts = 1; parts <= 8; parts *= 2) {
+      r.parts = parts;
+      r.part_rows = (int)ceil_div64(d.hw, parts);
+      if (parts > 1 && (int64_t)(parts - 1) * r.part_rows >= d.hw) break;
+      r.steps = (int)ceil_div64(r.part_rows, row_step);
+      const size_t smem = (size_t)r.steps * kResThreads * piece_bytes + 4 * (kResThreads * (kRun + 1) + r.cb + 4 * (r.cb / d.cpg));
+      if (smem > kResSmemMax) continue;
+      const int64_t ctas = (int64_t)d.n * r.blocks * parts;
+      if (ctas > 0x7fffffff) return false;
+      const int per_sm = (int)std::min<size_t>(8, 226 * 1024 / (smem + 1024));
+      // rounds of CTAs over the card, by the bytes of one CTA; meeting costs; idle lanes cost
+      const double rounds = (double)ceil_div64(ctas, 148 * per_sm), bytes = (double)r.steps * kResThreads * piece_bytes;
+      const double score = rounds * per_sm * bytes / 45.0e3 + rounds * (per_sm == 1 ? 4.0 : 2.0) + (parts > 1 ? 2.0 : 0.0) + (block * (piece_bytes < 32 ? 2 : 4) < 128 && !last ? 0.5 : 0.0);
+      if (score < best_score) { best_score = score; best = r; }
+    }
+    if (last) break;
+  }
+  if (best_score > 1e29) return false;
+  *out = best;
+  return true;
+}
+size_t resident_smem(const Resident& r, int piece_bytes) {
+  return (size_t)r.steps * kResThreads * piece_bytes + 4 * (kResThreads * (kRun + 1) + r.cb + 4 * (r.cb / r.d.cpg));
+}
+template <void (*kernel)(Resident)>
+int launch_resident(const Resident& r, int piece_bytes, cudaStream_t st, const char* what) {
+  static std::atomic<uint64_t> ready{0};                    // devices on which the kernel may use its shared memory
+  int dev = 0;
+  TRAIN_CK(cudaGetDevice(&dev), "cudaGetDevice");
+  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+    TRAIN_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResSmemMax), "cudaFuncSetAttribute(norm)");
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  TRAIN_CK(train_launch(kernel, dim3((unsigned)((int64_t)r.d.n * r.blocks * r.parts)), dim3(kResThreads), resident_smem(r, piece_bytes), st, r.parts, r), what);
+  return LQSGD_OK;
+}
+// The resident kernels' terms: 16-byte pieces everywhere.
+bool forward_resident(const NormDev& d, int dtype, Resident* r) {
+  return d.vec_x && d.vec_out && make_resident(d, d.x8.dev_codes || d.y8.dev_codes, kRun * train_elem(dtype), r);
+}
+bool backward_resident(const NormDev& d, int dtype, Resident* r) {
+  const bool kept = d.x8.dev_codes != nullptr;
+  return d.vec_dy && d.vec_out && (kept ? d.vec_x8 : d.vec_x) && make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun : kRun * train_elem(dtype)), r);
+}
+
 void make_geometry(NormDev* d) {
   d->cpg = d->c / d->groups;
   d->lane_shift = 2;
@@ -368,10 +766,12 @@ void make_geometry(NormDev* d) {
   d->chunk_rows = (int)(ceil_div64(ceil_div64(d->hw, chunks), step) * step);
   d->chunks = (int)ceil_div64(d->hw, d->chunk_rows);
 }
-size_t part_floats(const NormDev& d) { return ((size_t)d.n * d.chunks * d.c + 63) / 64 * 64; }
-size_t workspace_of(const NormDev& d, bool backward) {
-  const size_t groups = ((size_t)d.n * d.groups + 63) / 64 * 64;
-  return 4 * (2 * part_floats(d) + (backward ? 2 * groups : 0));
+size_t rounded(size_t n) { return (n + 63) / 64 * 64; }
+size_t workspace_of(const NormDev& d, int dtype, bool backward) {
+  Resident r;
+  if (backward ? backward_resident(d, dtype, &r) : forward_resident(d, dtype, &r))
+    return backward ? 8 * rounded((size_t)d.n * r.parts * d.c) : 0;
+  return 4 * (2 * rounded((size_t)d.n * d.chunks * d.c) + (backward ? 2 * rounded((size_t)d.n * d.groups) : 0));
 }
 
 int check_common(const lqsgd_group_norm* a) {
@@ -405,14 +805,16 @@ NormDev to_dev(const lqsgd_group_norm& a) {
   make_geometry(&d);
   return d;
 }
-int place_workspace(NormDev* d, const lqsgd_group_norm& a, bool backward) {
-  if (!a.dev_workspace || a.workspace_bytes < workspace_of(*d, backward)) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
-  if (!train_aligned(a.dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;
+int check_workspace(const NormDev& d, const lqsgd_group_norm& a, bool backward) {
+  const size_t need = workspace_of(d, a.dtype, backward);
+  if (need && (!a.dev_workspace || a.workspace_bytes < need)) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
+  return train_aligned(a.dev_workspace, 16) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+}
+void place_workspace(NormDev* d, const lqsgd_group_norm& a, size_t part) {
   d->part0 = static_cast<float*>(a.dev_workspace);
-  d->part1 = d->part0 + part_floats(*d);
-  d->group0 = d->part1 + part_floats(*d);
-  d->group1 = d->group0 + ((size_t)d->n * d->groups + 63) / 64 * 64;
-  return LQSGD_OK;
+  d->part1 = d->part0 + rounded(part);
+  d->group0 = d->part1 + rounded(part);
+  d->group1 = d->group0 + rounded((size_t)d->n * d->groups);
 }
 
 }  // namespace
@@ -429,7 +831,7 @@ extern "C" int lqsgd_group_norm_workspace_bytes(int32_t backward, const lqsgd_gr
   if (!host_bytes_out || (backward != 0 && backward != 1)) return LQSGD_ERR_INVALID_ARG;
   const int rc = check_common(host_args);
   if (rc != LQSGD_OK) return rc;
-  *host_bytes_out = host_args->n ? workspace_of(to_dev(*host_args), backward != 0) : 0;
+  *host_bytes_out = host_args->n ? workspace_of(to_dev(*host_args), host_args->dtype, backward != 0) : 0;
   return LQSGD_OK;
 }
 
@@ -444,8 +846,16 @@ extern "C" int lqsgd_group_norm_forward(const lqsgd_group_norm* a, void* cuda_st
   if (a->x8.dev_codes && (rc = check_packed8(a->x8, a->c)) != LQSGD_OK) return rc;
   if (a->y8.dev_codes && (rc = check_packed8(a->y8, a->c)) != LQSGD_OK) return rc;
   NormDev d = to_dev(*a);
-  if ((rc = place_workspace(&d, *a, false)) != LQSGD_OK) return rc;
+  if ((rc = check_workspace(d, *a, false)) != LQSGD_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  Resident r;
+  if (forward_resident(d, a->dtype, &r)) {
+    const int piece = kRun * train_elem(a->dtype);
+    return a->dtype == LQSGD_BF16 ? launch_resident<norm_resident_kernel<LQSGD_BF16>>(r, piece, st, "norm_resident_kernel launch")
+           : a->dtype == LQSGD_F16 ? launch_resident<norm_resident_kernel<LQSGD_F16>>(r, piece, st, "norm_resident_kernel launch")
+                                   : launch_resident<norm_resident_kernel<LQSGD_F32>>(r, piece, st, "norm_resident_kernel launch");
+  }
+  place_workspace(&d, *a, (size_t)d.n * d.chunks * d.c);
   const dim3 grid((unsigned)((int64_t)d.n * d.chunks * d.segs));
   TRAIN_CK(NORM_BY_DTYPE(a->dtype, norm_stats_kernel, grid, dim3(kThreads), 0, st, 1, d), "norm_stats_kernel launch");
   TRAIN_CK(train_launch(norm_group_kernel, dim3((unsigned)ceil_div64((int64_t)d.n * d.groups, kWarps)), dim3(kThreads), 0, st, 1, d), "norm_group_kernel launch");
@@ -471,7 +881,21 @@ extern "C" int lqsgd_group_norm_backward(const lqsgd_group_norm* a, void* cuda_s
   if (!a->dev_gamma || !a->dev_beta || !a->dev_mean || !a->dev_rstd) return LQSGD_ERR_INVALID_ARG;
   if (!train_aligned(a->dev_gamma, 4) || !train_aligned(a->dev_beta, 4) || !train_aligned(a->dev_mean, 4) || !train_aligned(a->dev_rstd, 4)) return LQSGD_ERR_MISALIGNED;
   NormDev d = to_dev(*a);
-  if ((rc = place_workspace(&d, *a, true)) != LQSGD_OK) return rc;
+  if ((rc = check_workspace(d, *a, true)) != LQSGD_OK) return rc;
+  Resident r;
+  if (backward_resident(d, a->dtype, &r)) {
+    const bool kept = d.x8.dev_codes != nullptr;
+    const int piece = kRun * train_elem(a->dtype) + (kept ? kRun : kRun * train_elem(a->dtype));
+    place_workspace(&r.d, *a, (size_t)d.n * r.parts * d.c);
+    const char* what = "norm_grad_resident_kernel launch";
+    if (a->dtype == LQSGD_BF16) rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_BF16, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_BF16, false>>(r, piece, st, what);
+    else if (a->dtype == LQSGD_F16) rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_F16, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_F16, false>>(r, piece, st, what);
+    else rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_F32, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_F32, false>>(r, piece, st, what);
+    if (rc != LQSGD_OK) return rc;
+    TRAIN_CK(train_launch(norm_dparam_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, st, 1, r.d, (int)(d.n * r.parts)), "norm_dparam_kernel launch");
+    return LQSGD_OK;
+  }
+  place_workspace(&d, *a, (size_t)d.n * d.chunks * d.c);
   const dim3 grid((unsigned)((int64_t)d.n * d.chunks * d.segs));
   const int group_blocks = (int)ceil_div64((int64_t)d.n * d.groups, kWarps);
   TRAIN_CK(NORM_BY_DTYPE(a->dtype, norm_grad_sums_kernel, grid, dim3(kThreads), 0, st, 1, d), "norm_grad_sums_kernel launch");

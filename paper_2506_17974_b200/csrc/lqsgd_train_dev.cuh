@@ -131,6 +131,27 @@ __device__ __forceinline__ float decode8(uint32_t code, float step) {
   return __uint_as_float(__float_as_uint(sat) | ((code & 128u) << 24));
 }
 
+// Four codes of a word at once, without conversions: 0x4b000000 | m is 2^23 + m, and (2^23 + m) 2^e - 2^23 2^e is m 2^e exactly.
+// For exponent bytes up to 230 (2^23 2^e is in range); the others take decode8().
+constexpr int kQuickByte = 230;
+__device__ __forceinline__ void decode4(uint32_t w, float step, float off, float* v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float m = fmaf(__uint_as_float(((w >> (8 * j)) & 127u) | 0x4b000000u), step, off);
+    v[j] = __uint_as_float(__float_as_uint(m) | ((w << (24 - 8 * j)) & 0x80000000u));
+  }
+}
+__device__ __forceinline__ void decode_run(uint2 w, int eb, float (&v)[8]) {
+  const float step = step_of(eb);
+  if (eb <= kQuickByte) {
+    decode4(w.x, step, step * -8388608.f, v);
+    decode4(w.y, step, step * -8388608.f, v + 4);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step);
+  }
+}
+
 // ---- activations, all in fp32, without branches: two special-function instructions each
 __device__ __forceinline__ float exp2_approx(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float rcp_approx(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
