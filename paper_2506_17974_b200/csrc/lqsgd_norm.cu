@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 namespace lqsgd {
 namespace {
@@ -412,43 +413,62 @@ __device__ __forceinline__ Place place_of(const Resident& r) {
   return q;
 }
 
-// Sums over the block's threads per channel: v[j] of every thread -> chan[channel of the block].  Lanes of a warp that have the
-// same channels are folded first; then a thread per channel adds the warps, in order.
-__device__ __forceinline__ void channel_sums(const Resident& r, float (&v)[kRun], float* scratch, float* chan, int channels) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// Sums over the block's threads of NV values each; threads whose piece (8 channels) is the same are added up.  On return
+// scratch holds the sums of every warp that has the piece (see piece_sum).
+template <int NV>
+__device__ __forceinline__ void fold_rows(const Resident& r, float (&v)[NV], float* scratch) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, shift = min(r.lane_shift, 5);
   for (int o = 16; o >= (1 << r.lane_shift); o >>= 1) {
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] += __shfl_down_sync(0xffffffffu, v[j], o);
+    for (int j = 0; j < NV; ++j) v[j] += __shfl_down_sync(0xffffffffu, v[j], o);
   }
-  __syncthreads();                                        // scratch and chan are free
+  __syncthreads();                                        // scratch is free
+  if (lane < (1 << shift)) {
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) scratch[(warp * 32 + lane) * (kRun + 1) + j] = v[j];
-  __syncthreads();
-  const int wide = max(1, (1 << r.lane_shift) >> 5);       // warps that a pixel spans
-  for (int ch = threadIdx.x; ch < channels; ch += kResThreads) {
-    const int piece = ch / kRun;
-    float t = 0.f;
-    for (int w = piece >> 5; w < kResWarps; w += wide) t += scratch[(w * 32 + (piece & 31)) * (kRun + 1) + ch % kRun];
-    chan[ch] = t;
+    for (int j = 0; j < NV; ++j) scratch[(((j * kResWarps) + warp) << shift) + lane] = v[j];
   }
   __syncthreads();
 }
-// Group totals of chan (times weight, if given) over the block and the cluster: total[g], the same bits in every CTA.
-__device__ __forceinline__ void group_totals(const Resident& r, const Place& q, const float* chan, const float* __restrict__ weight, float* mine, float* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cpg = r.d.cpg, groups = q.channels / cpg;
-  for (int g = warp; g < groups; g += kResWarps) {
-    float t = 0.f;
-    for (int i = lane; i < cpg; i += 32) t += weight ? chan[g * cpg + i] * weight[q.c0 + g * cpg + i] : chan[g * cpg + i];
+__device__ __forceinline__ float piece_sum(const Resident& r, const float* scratch, int v, int piece) {
+  const int shift = min(r.lane_shift, 5), wide = max(1, (1 << r.lane_shift) >> 5);    // warps that a pixel spans
+  float t = 0.f;
+#pragma unroll 4
+  for (int w = piece >> 5; w < kResWarps; w += wide) t += scratch[((v * kResWarps + w) << shift) + (piece & 31)];
+  return t;
+}
+// NT totals of each of the block's groups over the block and the cluster: total[t * cap + g], the same bits in every CTA.
+// value(t, g, i) is the i-th part of the t-th sum, `count` of them.
+template <int NT, typename F>
+__device__ __forceinline__ void group_totals(const Resident& r, int groups, int cap, int count, float* mine, float* total, F&& value) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int width = 32;                                         // lanes per group
+  while (width > 1 && width / 2 >= count) width >>= 1;
+  const int per_warp = 32 / width, sub = lane / width, in = lane & (width - 1);
+  for (int g0 = warp * per_warp; g0 < groups; g0 += kResWarps * per_warp) {
+    const int g = g0 + sub;
+    float t[NT];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) t += __shfl_down_sync(0xffffffffu, t, o);
-    if (lane == 0) (r.parts > 1 ? mine : total)[g] = t;
+    for (int k = 0; k < NT; ++k) t[k] = 0.f;
+    if (g < groups)
+      for (int i = in; i < count; i += width) {
+#pragma unroll
+        for (int k = 0; k < NT; ++k) t[k] += value(k, g, i);
+      }
+    for (int o = width >> 1; o > 0; o >>= 1) {
+#pragma unroll
+      for (int k = 0; k < NT; ++k) t[k] += __shfl_down_sync(0xffffffffu, t[k], o);
+    }
+    if (in == 0 && g < groups) {
+#pragma unroll
+      for (int k = 0; k < NT; ++k) (r.parts > 1 ? mine : total)[k * cap + g] = t[k];
+    }
   }
   if (r.parts > 1) {
     norm_cluster_sync();
-    for (int g = threadIdx.x; g < groups; g += kResThreads) {
+    for (int i = threadIdx.x; i < NT * cap; i += kResThreads) {
       float t = 0.f;
-      for (int k = 0; k < r.parts; ++k) t += read_peer(mine + g, k);
-      total[g] = t;
+      for (int k = 0; k < r.parts; ++k) t += read_peer(mine + i, k);
+      total[i] = t;
     }
   }
   __syncthreads();
@@ -456,206 +476,283 @@ __device__ __forceinline__ void group_totals(const Resident& r, const Place& q, 
 
 template <int DT>
 __device__ __forceinline__ void unpack_run(const uint8_t* p, float (&v)[kRun]) {
-  using T = typename Elem<DT>::T;
-#pragma unroll
-  for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) {
-    const uint4 w = reinterpret_cast<const uint4*>(p)[i];
-    const T* t = reinterpret_cast<const T*>(&w);
-#pragma unroll
-    for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[i * (16 / (int)sizeof(T)) + j] = Elem<DT>::up(t[j]);
+  if constexpr (DT == LQSGD_F32) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const float2 a = open_pair<DT>(w.x), b = open_pair<DT>(w.y), c = open_pair<DT>(w.z), e = open_pair<DT>(w.w);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = e.x; v[7] = e.y;
   }
 }
+// Index in 0 .. NG - 1 of channel j of a piece: ONE group per piece (8 divides the group's width), or any.
+template <bool ONE>
+struct Groups {
+  static constexpr int kN = ONE ? 1 : kRun;
+  int first, at[kN];                                                    // groups of the block
+  __device__ __forceinline__ Groups(int channel, int cpg) {
+    first = channel / cpg;
+    at[0] = first;
+    if (!ONE) {
+      int left = cpg - (channel - first * cpg), g = first;
+#pragma unroll
+      for (int j = 1; j < kN; ++j) {
+        if (--left == 0) { ++g; left = cpg; }
+        at[j] = g;
+      }
+    }
+  }
+  static __device__ __forceinline__ constexpr int of(int j) { return ONE ? 0 : j; }
+};
 
-template <int DT>
-__global__ void __launch_bounds__(kResThreads)
+template <int DT, bool ONE>
+__global__ void __launch_bounds__(kResThreads, ONE ? 4 : 3)
 norm_resident_kernel(Resident r) {
   using T = typename Elem<DT>::T;
-  constexpr int kBytes = kRun * (int)sizeof(T);
+  using G = Groups<ONE>;
+  constexpr int kBytes = kRun * (int)sizeof(T), kStep = kResThreads * kBytes;
   extern __shared__ __align__(16) uint8_t res_smem[];
   const NormDev& d = r.d;
   const Place q = place_of(r);
   uint8_t* data = res_smem;                                             // [steps][threads] pieces
-  float* scratch = reinterpret_cast<float*>(data + (size_t)r.steps * kResThreads * kBytes);
-  float* chan = scratch + kResThreads * (kRun + 1);                     // [cb]
-  float* mine = chan + r.cb;                                            // [2][groups of a block]
-  const int groups_cap = r.cb / d.cpg;
+  float* scratch = reinterpret_cast<float*>(data + (size_t)r.steps * kStep);
+  const int groups_cap = r.cb / d.cpg, groups = q.channels / d.cpg;
+  float* mine = scratch + (G::kN * kResWarps << min(r.lane_shift, 5));  // [2][groups of a block]
   float* mean = mine + 2 * groups_cap;                                  // [groups]
   float* rstd = mean + groups_cap;
-  train_pdl_wait();
-  const T* src = static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)q.first * d.ld_x + q.col;
+  const int count = q.on && q.row < q.rows ? (q.rows - q.row + q.row_step - 1) / q.row_step : 0;
   uint8_t* own = data + threadIdx.x * kBytes;
-  if (q.on)
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+  train_pdl_wait();
+  {
+    const uint8_t* src = reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col);
+    const int64_t hop = q.row_step * d.ld_x * (int64_t)sizeof(T);
+    uint32_t to = smem_at(own);
+#pragma unroll 4
+    for (int k = 0; k < count; ++k, src += hop, to += kStep) {
 #pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i)
-        copy_async<16>(own + (size_t)k * kResThreads * kBytes + 16 * i, reinterpret_cast<const uint8_t*>(src + p * d.ld_x) + 16 * i);
-    }
-  copy_async_wait();
-  float s[kRun], v[kRun];
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) s[j] = 0.f;
-  if (q.on)
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
-      unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) s[j] += v[j];
-    }
-  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
-  channel_sums(r, s, scratch, chan, q.channels);
-  group_totals(r, q, chan, nullptr, mine, mean);
-  const int groups = q.channels / d.cpg;
-  for (int g = threadIdx.x; g < groups; g += kResThreads) mean[g] *= inv;
-  __syncthreads();
-  float m[kRun];
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) {
-    s[j] = 0.f;
-    m[j] = q.on ? mean[(q.col - q.c0 + j) / d.cpg] : 0.f;
-  }
-  if (q.on)
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
-      unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) { const float t = v[j] - m[j]; s[j] = fmaf(t, t, s[j]); }
-    }
-  channel_sums(r, s, scratch, chan, q.channels);
-  group_totals(r, q, chan, nullptr, mine + groups_cap, rstd);
-  for (int g = threadIdx.x; g < groups; g += kResThreads) {
-    rstd[g] = 1.f / sqrtf(rstd[g] * inv + d.eps);
-    if (q.part == 0) {
-      const size_t at = (size_t)q.sample * d.groups + q.c0 / d.cpg + g;
-      d.mean[at] = mean[g];
-      d.rstd[at] = rstd[g];
+      for (int i = 0; i < kBytes / 16; ++i) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16 * i), "l"(src + 16 * i) : "memory");
     }
   }
-  __syncthreads();
-  float scale[kRun], beta[kRun];
+  const G at(q.col - q.c0, d.cpg);
+  float gamma[kRun], beta[kRun];
 #pragma unroll
   for (int j = 0; j < kRun; ++j) {
-    scale[j] = q.on ? rstd[(q.col - q.c0 + j) / d.cpg] * __ldg(d.gamma + q.col + j) : 0.f;
+    gamma[j] = q.on ? __ldg(d.gamma + q.col + j) : 0.f;
     beta[j] = q.on ? __ldg(d.beta + q.col + j) : 0.f;
   }
-  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)q.first * d.ld_out + q.col;
-  const bool packs = d.x8.dev_codes || d.y8.dev_codes;                  // then groups of 32 need the warp together
-  const int lead = packs ? (int)((threadIdx.x & 31) >> min(r.lane_shift, 5)) : 0;
-  for (int p = q.row, k = 0; p - lead < q.rows; p += q.row_step, ++k) {
-    const bool on = q.on && p < q.rows;
-    const int64_t row = (int64_t)q.sample * d.hw + q.first + p;
-    if (on) unpack_run<DT>(own + (size_t)k * kResThreads * kBytes, v);
-    if (d.x8.dev_codes) pack_run(d.x8, d.vec_x8, row, q.col, kRun, on, v);
-    if (on) {
+  copy_async_wait();
+  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
+  const int per_group = ONE ? d.cpg / kRun : d.cpg;
+  auto part = [&](int, int g, int i) {
+    const int ch = ONE ? (g * per_group + i) * kRun : g * d.cpg + i;
+    return piece_sum(r, scratch, ONE ? 0 : ch % kRun, ch / kRun);
+  };
+  float s[G::kN], v[kRun];
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] = fmaf(v[j] - m[j], scale[j], beta[j]);
-      act_run(d.act, v);
-      store_run<DT, kRun>(dst + p * d.ld_out, true, kRun, v);
-    }
-    if (d.y8.dev_codes) {
+  for (int j = 0; j < G::kN; ++j) s[j] = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < count; ++k) {
+    unpack_run<DT>(own + k * kStep, v);
+    if (ONE) s[0] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    else {
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
-      pack_run(d.y8, d.vec_y8, row, q.col, kRun, on, v);
+      for (int j = 0; j < kRun; ++j) s[G::of(j)] += v[j];
     }
+  }
+  fold_rows(r, s, scratch);
+  group_totals<1>(r, groups, groups_cap, per_group, mine, mean, part);
+  float m[G::kN];
+#pragma unroll
+  for (int j = 0; j < G::kN; ++j) {
+    s[j] = 0.f;
+    m[j] = q.on ? mean[at.at[j]] * inv : 0.f;
+  }
+#pragma unroll 4
+  for (int k = 0; k < count; ++k) {
+    unpack_run<DT>(own + k * kStep, v);
+    float u[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) u[j] = v[j] - m[G::of(j)];
+    if (ONE) {
+      float t0 = u[0] * u[0], t1 = u[4] * u[4];
+#pragma unroll
+      for (int j = 1; j < 4; ++j) { t0 = fmaf(u[j], u[j], t0); t1 = fmaf(u[4 + j], u[4 + j], t1); }
+      s[0] += t0 + t1;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) s[G::of(j)] = fmaf(u[j], u[j], s[G::of(j)]);
+    }
+  }
+  fold_rows(r, s, scratch);
+  group_totals<1>(r, groups, groups_cap, per_group, mine + groups_cap, rstd, part);
+  if (q.part == 0)
+    for (int g = threadIdx.x; g < groups; g += kResThreads) {
+      const size_t to = (size_t)q.sample * d.groups + q.c0 / d.cpg + g;
+      d.mean[to] = mean[g] * inv;
+      d.rstd[to] = 1.f / sqrtf(rstd[g] * inv + d.eps);
+    }
+  float scale[G::kN];
+#pragma unroll
+  for (int j = 0; j < G::kN; ++j) scale[j] = q.on ? 1.f / sqrtf(rstd[at.at[j]] * inv + d.eps) : 0.f;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) gamma[j] *= scale[G::of(j)];
+  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)(q.first + q.row) * d.ld_out + q.col;
+  const int64_t hop = q.row_step * d.ld_out;
+  if (!d.x8.dev_codes && !d.y8.dev_codes) {
+    with_act(d.act, [&](auto tag) {
+#pragma unroll 2
+      for (int k = 0; k < count; ++k, dst += hop) {
+        unpack_run<DT>(own + k * kStep, v);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) v[j] = act_value<decltype(tag)::value>(fmaf(v[j] - m[G::of(j)], gamma[j], beta[j]));
+        store_run<DT, kRun>(dst, true, kRun, v);
+      }
+    });
+  } else {
+    // groups of 32 channels need a warp's lanes together
+    const int lead = (int)((threadIdx.x & 31) >> min(r.lane_shift, 5));
+    with_act(d.act, [&](auto tag) {
+      for (int p = q.row, k = 0; p - lead < q.rows; p += q.row_step, ++k, dst += hop) {
+        const bool on = k < count;
+        const int64_t row = (int64_t)q.sample * d.hw + q.first + p;
+        if (on) unpack_run<DT>(own + k * kStep, v);
+        if (d.x8.dev_codes) pack_run(d.x8, d.vec_x8, row, q.col, kRun, on, v);
+        if (on) {
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) v[j] = act_value<decltype(tag)::value>(fmaf(v[j] - m[G::of(j)], gamma[j], beta[j]));
+          store_run<DT, kRun>(dst, true, kRun, v);
+        }
+        if (d.y8.dev_codes) {
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
+          pack_run(d.y8, d.vec_y8, row, q.col, kRun, on, v);
+        }
+      }
+    });
   }
   if (r.parts > 1) norm_cluster_sync();                                 // nobody leaves while its sums may be read
 }
 
 // KEPT: x comes from its 8-bit form.
-template <int DT, bool KEPT>
-__global__ void __launch_bounds__(kResThreads)
+template <int DT, bool KEPT, bool ONE>
+__global__ void __launch_bounds__(kResThreads, ONE ? 4 : 2)
 norm_grad_resident_kernel(Resident r) {
   using T = typename Elem<DT>::T;
-  constexpr int kDy = kRun * (int)sizeof(T), kX = KEPT ? kRun : kDy, kBytes = kDy + kX;
+  using G = Groups<ONE>;
+  constexpr int kDy = kRun * (int)sizeof(T), kX = KEPT ? kRun : kDy, kBytes = kDy + kX + (KEPT ? 1 : 0);
   extern __shared__ __align__(16) uint8_t res_smem[];
   const NormDev& d = r.d;
   const Place q = place_of(r);
   uint8_t* dys = res_smem;                                              // [steps][threads] pieces of dy, then of x
   uint8_t* xs = dys + (size_t)r.steps * kResThreads * kDy;
+  uint8_t* es = xs + (size_t)r.steps * kResThreads * kX + threadIdx.x;   // exponent byte of every piece
   float* scratch = reinterpret_cast<float*>(res_smem + (size_t)r.steps * kResThreads * kBytes);
-  float* chan = scratch + kResThreads * (kRun + 1);
-  float* mine = chan + r.cb;
-  const int groups_cap = r.cb / d.cpg;
-  float* t0 = mine + 2 * groups_cap;
-  float* t1 = t0 + groups_cap;
-  train_pdl_wait();
-  const T* gsrc = static_cast<const T*>(d.dy) + q.sample * d.sample_dy + (int64_t)q.first * d.ld_dy + q.col;
-  const T* xsrc = static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)q.first * d.ld_x + q.col;
-  const int64_t row0 = (int64_t)q.sample * d.hw + q.first;
-  const uint8_t* csrc = d.x8.dev_codes + row0 * d.x8.ld_codes + q.col;
-  const uint8_t* esrc = d.x8.dev_exps + row0 * d.x8.ld_exps + q.col / kGroup;
+  const int groups_cap = r.cb / d.cpg, groups = q.channels / d.cpg;
+  float* chan = scratch + (2 * kRun * kResWarps << min(r.lane_shift, 5));   // [2][channels of a block]
+  float* mine = chan + 2 * r.cb;                                        // [2][groups of a block]
+  float* total = mine + 2 * groups_cap;
+  const int count = q.on && q.row < q.rows ? (q.rows - q.row + q.row_step - 1) / q.row_step : 0;
   uint8_t* gown = dys + threadIdx.x * kDy;
   uint8_t* xown = xs + threadIdx.x * kX;
-  if (q.on)
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
+  train_pdl_wait();
+  const int64_t row0 = (int64_t)q.sample * d.hw + q.first + q.row;
+  {
+    const uint8_t* gsrc = reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.dy) + q.sample * d.sample_dy + (int64_t)(q.first + q.row) * d.ld_dy + q.col);
+    const uint8_t* xsrc = KEPT ? d.x8.dev_codes + row0 * d.x8.ld_codes + q.col
+                               : reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col);
+    const int64_t ghop = q.row_step * d.ld_dy * (int64_t)sizeof(T), xhop = KEPT ? q.row_step * d.x8.ld_codes : q.row_step * d.ld_x * (int64_t)sizeof(T);
+#pragma unroll 4
+    for (int k = 0; k < count; ++k, gsrc += ghop, xsrc += xhop) {
 #pragma unroll
-      for (int i = 0; i < kDy / 16; ++i)
-        copy_async<16>(gown + (size_t)k * kResThreads * kDy + 16 * i, reinterpret_cast<const uint8_t*>(gsrc + p * d.ld_dy) + 16 * i);
+      for (int i = 0; i < kDy / 16; ++i) copy_async<16>(gown + k * (kResThreads * kDy) + 16 * i, gsrc + 16 * i);
       if constexpr (KEPT) {
-        copy_async<8>(xown + (size_t)k * kResThreads * kX, csrc + p * d.x8.ld_codes);
+        copy_async<8>(xown + k * (kResThreads * kX), xsrc);
       } else {
 #pragma unroll
-        for (int i = 0; i < kX / 16; ++i)
-          copy_async<16>(xown + (size_t)k * kResThreads * kX + 16 * i, reinterpret_cast<const uint8_t*>(xsrc + p * d.ld_x) + 16 * i);
+        for (int i = 0; i < kX / 16; ++i) copy_async<16>(xown + k * (kResThreads * kX) + 16 * i, xsrc + 16 * i);
       }
     }
-  float mean[kRun], rstd[kRun], gamma[kRun], beta[kRun];
+    if constexpr (KEPT) {
+      const uint8_t* esrc = d.x8.dev_exps + row0 * d.x8.ld_exps + q.col / kGroup;
+      const int64_t ehop = q.row_step * d.x8.ld_exps;
+#pragma unroll 8
+      for (int k = 0; k < count; ++k) es[k * kResThreads] = esrc[k * ehop];
+    }
+  }
+  const G at(q.col - q.c0, d.cpg);
+  float mean[G::kN], rstd[G::kN], gamma[kRun], beta[kRun];
+#pragma unroll
+  for (int j = 0; j < G::kN; ++j) {
+    const size_t from = (size_t)q.sample * d.groups + (q.on ? q.c0 / d.cpg + at.at[j] : 0);
+    mean[j] = d.mean[from];
+    rstd[j] = d.rstd[from];
+  }
 #pragma unroll
   for (int j = 0; j < kRun; ++j) {
-    const int ch = q.on ? q.col + j : q.c0;
-    const size_t at = (size_t)q.sample * d.groups + ch / d.cpg;
-    mean[j] = d.mean[at];
-    rstd[j] = d.rstd[at];
-    gamma[j] = __ldg(d.gamma + ch);
-    beta[j] = __ldg(d.beta + ch);
+    gamma[j] = q.on ? __ldg(d.gamma + q.col + j) : 0.f;
+    beta[j] = q.on ? __ldg(d.beta + q.col + j) : 0.f;
   }
   copy_async_wait();
-  // xh and dh = dy act'(h) of the thread's k-th piece
-  auto piece = [&](int p, int k, float (&xh)[kRun], float (&dh)[kRun]) {
-    if constexpr (KEPT) {
-      const uint2 w = *reinterpret_cast<const uint2*>(xown + (size_t)k * kResThreads * kX);
-      decode_run(w, esrc[p * d.x8.ld_exps], xh);
-    } else {
-      unpack_run<DT>(xown + (size_t)k * kResThreads * kX, xh);
-    }
-    float h[kRun];
+  // With e = x - mean and f = gamma rstd:  h = f e + beta,  dh = dy act'(h),  dgamma = rstd sum of dh e,
+  // dx = f dh - rstd <u> - rstd^2 <u xh> e
+  float f[kRun];
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) { xh[j] = (xh[j] - mean[j]) * rstd[j]; h[j] = fmaf(xh[j], gamma[j], beta[j]); }
-    slope_run(d.act, h);
-    unpack_run<DT>(gown + (size_t)k * kResThreads * kDy, dh);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) dh[j] *= h[j];
-  };
-  float a[kRun], b[kRun], xh[kRun], dh[kRun];
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) a[j] = b[j] = 0.f;
-  if (q.on)
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
-      piece(p, k, xh, dh);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) { a[j] += dh[j]; b[j] = fmaf(dh[j], xh[j], b[j]); }
-    }
-  const size_t out_row = ((size_t)q.sample * r.parts + q.part) * d.c + q.c0;
-  channel_sums(r, a, scratch, chan, q.channels);
-  for (int ch = threadIdx.x; ch < q.channels; ch += kResThreads) d.part0[out_row + ch] = chan[ch];
-  group_totals(r, q, chan, d.gamma, mine, t0);
-  channel_sums(r, b, scratch, chan, q.channels);
-  for (int ch = threadIdx.x; ch < q.channels; ch += kResThreads) d.part1[out_row + ch] = chan[ch];
-  group_totals(r, q, chan, d.gamma, mine + groups_cap, t1);
-  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
-  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)q.first * d.ld_out + q.col;
-  if (q.on) {
-    float c0[kRun], c1[kRun];
+  for (int j = 0; j < kRun; ++j) f[j] = gamma[j] * rstd[G::of(j)];
+  auto piece = [&](auto tag, int k, float (&e)[kRun], float (&dh)[kRun]) {
+    if constexpr (KEPT) decode_run(*reinterpret_cast<const uint2*>(xown + k * (kResThreads * kX)), es[k * kResThreads], e);
+    else unpack_run<DT>(xown + k * (kResThreads * kX), e);
+    unpack_run<DT>(gown + k * (kResThreads * kDy), dh);
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      const int g = (q.col - q.c0 + j) / d.cpg;
-      c0[j] = t0[g] * inv;
-      c1[j] = t1[g] * inv;
+      e[j] -= mean[G::of(j)];
+      dh[j] *= act_slope<decltype(tag)::value>(fmaf(e[j], f[j], beta[j]));
     }
-    for (int p = q.row, k = 0; p < q.rows; p += q.row_step, ++k) {
-      piece(p, k, xh, dh);
+  };
+  float ab[2 * kRun];                                                   // sums of dh, of dh e
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) xh[j] = rstd[j] * (gamma[j] * dh[j] - c0[j] - xh[j] * c1[j]);
-      store_run<DT, kRun>(dst + p * d.ld_out, true, kRun, xh);
+  for (int j = 0; j < 2 * kRun; ++j) ab[j] = 0.f;
+  with_act(d.act, [&](auto tag) {
+#pragma unroll 1
+    for (int k = 0; k < count; ++k) {
+      float e[kRun], dh[kRun];
+      piece(tag, k, e, dh);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) { ab[j] += dh[j]; ab[kRun + j] = fmaf(dh[j], e[j], ab[kRun + j]); }
     }
+  });
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) ab[kRun + j] *= rstd[G::of(j)];
+  fold_rows(r, ab, scratch);
+  const size_t out_row = ((size_t)q.sample * r.parts + q.part) * d.c + q.c0;
+  for (int i = threadIdx.x; i < 2 * q.channels; i += kResThreads) {
+    const bool second = i >= q.channels;
+    const int ch = second ? i - q.channels : i;
+    const float t = piece_sum(r, scratch, (second ? kRun : 0) + ch % kRun, ch / kRun);
+    (second ? d.part1 : d.part0)[out_row + ch] = t;
+    chan[second * r.cb + ch] = t * __ldg(d.gamma + q.c0 + ch);
   }
+  __syncthreads();
+  group_totals<2>(r, groups, groups_cap, d.cpg, mine, total, [&](int t, int g, int i) { return chan[t * r.cb + g * d.cpg + i]; });
+  const float inv = 1.f / ((float)d.hw * (float)d.cpg);
+  float c0[G::kN], c1[G::kN];
+#pragma unroll
+  for (int j = 0; j < G::kN; ++j) {
+    c0[j] = q.on ? -rstd[j] * total[at.at[j]] * inv : 0.f;
+    c1[j] = q.on ? -rstd[j] * rstd[j] * total[groups_cap + at.at[j]] * inv : 0.f;
+  }
+  T* dst = static_cast<T*>(d.out) + q.sample * d.sample_out + (int64_t)(q.first + q.row) * d.ld_out + q.col;
+  const int64_t hop = q.row_step * d.ld_out;
+  with_act(d.act, [&](auto tag) {
+    T* to = dst;
+#pragma unroll 1
+    for (int k = 0; k < count; ++k, to += hop) {
+      float e[kRun], dh[kRun];
+      piece(tag, k, e, dh);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) e[j] = fmaf(dh[j], f[j], fmaf(e[j], c1[G::of(j)], c0[G::of(j)]));
+      store_run<DT, kRun>(to, true, kRun, e);
+    }
+  });
   if (r.parts > 1) norm_cluster_sync();
 }
 
@@ -685,8 +782,12 @@ norm_dparam_kernel(NormDev d, int rows) {
   }
 }
 
-constexpr size_t kResSmemMax = 200 * 1024;
+constexpr size_t kResSmemMax = 220 * 1024;
 
+size_t resident_smem(const Resident& r, int piece_bytes) {
+  // pieces; the scratch of 16 sums per warp and piece; channel sums (two); group sums (four)
+  return (size_t)r.steps * kResThreads * piece_bytes + 4 * ((size_t)(2 * kRun * kResWarps << std::min(r.lane_shift, 5)) + 2 * r.cb + 4 * (r.cb / r.d.cpg));
+}
 // Whether the resident kernels take a problem, and how.  piece_bytes: shared memory per 8 channels of a pixel.
 bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
   auto gcd = [](int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; };
@@ -713,14 +814,16 @@ bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
       r.part_rows = (int)ceil_div64(d.hw, parts);
       if (parts > 1 && (int64_t)(parts - 1) * r.part_rows >= d.hw) break;
       r.steps = (int)ceil_div64(r.part_rows, row_step);
-      const size_t smem = (size_t)r.steps * kResThreads * piece_bytes + 4 * (kResThreads * (kRun + 1) + r.cb + 4 * (r.cb / d.cpg));
+      const size_t smem = resident_smem(r, piece_bytes);
       if (smem > kResSmemMax) continue;
       const int64_t ctas = (int64_t)d.n * r.blocks * parts;
       if (ctas > 0x7fffffff) return false;
-      const int per_sm = (int)std::min<size_t>(8, 226 * 1024 / (smem + 1024));
-      // rounds of CTAs over the card, by the bytes of one CTA; meeting costs; idle lanes cost
-      const double rounds = (double)ceil_div64(ctas, 148 * per_sm), bytes = (double)r.steps * kResThreads * piece_bytes;
-      const double score = rounds * per_sm * bytes / 45.0e3 + rounds * (per_sm == 1 ? 4.0 : 2.0) + (parts > 1 ? 2.0 : 0.0) + (block * (piece_bytes < 32 ? 2 : 4) < 128 && !last ? 0.5 : 0.0);
+      const int per_sm = (int)std::min<size_t>(4, 226 * 1024 / (smem + 1024));
+      // What was measured: 6 ns per CTA whatever it holds (9 where CTAs meet), 0.9 ns per 1000 values while at least three
+      // CTAs overlap on an SM, up to 1.5 times that with one; and the last round of CTAs is paid in full.
+      const double values = (double)d.n * d.hw * d.c, wave = 148.0 * per_sm, full = std::ceil(ctas / wave) * wave / ctas;
+      const double idle = (double)((1 << r.lane_shift) * kRun * r.blocks) / d.c;
+      const double score = ctas * (parts > 1 ? 9e-3 : 6e-3) + values * 0.9e-6 * (per_sm == 1 ? 1.5 : per_sm == 2 ? 1.1 : 1.0) * std::min(full, 2.0) * idle;
       if (score < best_score) { best_score = score; best = r; }
     }
     if (last) break;
@@ -728,9 +831,6 @@ bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
   if (best_score > 1e29) return false;
   *out = best;
   return true;
-}
-size_t resident_smem(const Resident& r, int piece_bytes) {
-  return (size_t)r.steps * kResThreads * piece_bytes + 4 * (kResThreads * (kRun + 1) + r.cb + 4 * (r.cb / r.d.cpg));
 }
 template <void (*kernel)(Resident)>
 int launch_resident(const Resident& r, int piece_bytes, cudaStream_t st, const char* what) {
@@ -744,13 +844,25 @@ int launch_resident(const Resident& r, int piece_bytes, cudaStream_t st, const c
   TRAIN_CK(train_launch(kernel, dim3((unsigned)((int64_t)r.d.n * r.blocks * r.parts)), dim3(kResThreads), resident_smem(r, piece_bytes), st, r.parts, r), what);
   return LQSGD_OK;
 }
+template <int DT>
+int launch_forward(const Resident& r, cudaStream_t st) {
+  const int piece = kRun * (int)sizeof(typename Elem<DT>::T);
+  return r.d.cpg % kRun == 0 ? launch_resident<norm_resident_kernel<DT, true>>(r, piece, st, "norm_resident_kernel launch")
+                             : launch_resident<norm_resident_kernel<DT, false>>(r, piece, st, "norm_resident_kernel launch");
+}
+template <int DT, bool KEPT>
+int launch_backward(const Resident& r, cudaStream_t st) {
+  const int dy = kRun * (int)sizeof(typename Elem<DT>::T), piece = dy + (KEPT ? kRun + 1 : dy);
+  return r.d.cpg % kRun == 0 ? launch_resident<norm_grad_resident_kernel<DT, KEPT, true>>(r, piece, st, "norm_grad_resident_kernel launch")
+                             : launch_resident<norm_grad_resident_kernel<DT, KEPT, false>>(r, piece, st, "norm_grad_resident_kernel launch");
+}
 // The resident kernels' terms: 16-byte pieces everywhere.
 bool forward_resident(const NormDev& d, int dtype, Resident* r) {
   return d.vec_x && d.vec_out && make_resident(d, d.x8.dev_codes || d.y8.dev_codes, kRun * train_elem(dtype), r);
 }
 bool backward_resident(const NormDev& d, int dtype, Resident* r) {
   const bool kept = d.x8.dev_codes != nullptr;
-  return d.vec_dy && d.vec_out && (kept ? d.vec_x8 : d.vec_x) && make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun : kRun * train_elem(dtype)), r);
+  return d.vec_dy && d.vec_out && (kept ? d.vec_x8 : d.vec_x) && make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun + 1 : kRun * train_elem(dtype)), r);
 }
 
 void make_geometry(NormDev* d) {
@@ -850,10 +962,7 @@ extern "C" int lqsgd_group_norm_forward(const lqsgd_group_norm* a, void* cuda_st
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   Resident r;
   if (forward_resident(d, a->dtype, &r)) {
-    const int piece = kRun * train_elem(a->dtype);
-    return a->dtype == LQSGD_BF16 ? launch_resident<norm_resident_kernel<LQSGD_BF16>>(r, piece, st, "norm_resident_kernel launch")
-           : a->dtype == LQSGD_F16 ? launch_resident<norm_resident_kernel<LQSGD_F16>>(r, piece, st, "norm_resident_kernel launch")
-                                   : launch_resident<norm_resident_kernel<LQSGD_F32>>(r, piece, st, "norm_resident_kernel launch");
+    return a->dtype == LQSGD_BF16 ? launch_forward<LQSGD_BF16>(r, st) : a->dtype == LQSGD_F16 ? launch_forward<LQSGD_F16>(r, st) : launch_forward<LQSGD_F32>(r, st);
   }
   place_workspace(&d, *a, (size_t)d.n * d.chunks * d.c);
   const dim3 grid((unsigned)((int64_t)d.n * d.chunks * d.segs));
@@ -885,12 +994,10 @@ extern "C" int lqsgd_group_norm_backward(const lqsgd_group_norm* a, void* cuda_s
   Resident r;
   if (backward_resident(d, a->dtype, &r)) {
     const bool kept = d.x8.dev_codes != nullptr;
-    const int piece = kRun * train_elem(a->dtype) + (kept ? kRun : kRun * train_elem(a->dtype));
     place_workspace(&r.d, *a, (size_t)d.n * r.parts * d.c);
-    const char* what = "norm_grad_resident_kernel launch";
-    if (a->dtype == LQSGD_BF16) rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_BF16, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_BF16, false>>(r, piece, st, what);
-    else if (a->dtype == LQSGD_F16) rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_F16, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_F16, false>>(r, piece, st, what);
-    else rc = kept ? launch_resident<norm_grad_resident_kernel<LQSGD_F32, true>>(r, piece, st, what) : launch_resident<norm_grad_resident_kernel<LQSGD_F32, false>>(r, piece, st, what);
+    if (a->dtype == LQSGD_BF16) rc = kept ? launch_backward<LQSGD_BF16, true>(r, st) : launch_backward<LQSGD_BF16, false>(r, st);
+    else if (a->dtype == LQSGD_F16) rc = kept ? launch_backward<LQSGD_F16, true>(r, st) : launch_backward<LQSGD_F16, false>(r, st);
+    else rc = kept ? launch_backward<LQSGD_F32, true>(r, st) : launch_backward<LQSGD_F32, false>(r, st);
     if (rc != LQSGD_OK) return rc;
     TRAIN_CK(train_launch(norm_dparam_kernel, dim3((unsigned)((d.c + 31) / 32)), dim3(1024), 0, st, 1, r.d, (int)(d.n * r.parts)), "norm_dparam_kernel launch");
     return LQSGD_OK;

@@ -64,8 +64,33 @@ __device__ __forceinline__ void load_run(const typename Elem<DT>::T* p, bool vec
     for (int j = 0; j < N; ++j) v[j] = j < have ? E::up(p[j]) : 0.f;
   }
 }
+// Two neighbouring elements of a 16-bit type in one word.
+template <int DT>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+  if constexpr (DT == LQSGD_BF16) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+  } else {
+    const __half2 t = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+  }
+}
+template <int DT>
+__device__ __forceinline__ float2 open_pair(uint32_t w) {
+  if constexpr (DT == LQSGD_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
 template <int DT, int N>
 __device__ __forceinline__ void store_run(typename Elem<DT>::T* p, bool vec, int have, const float (&v)[N]) {
+  if constexpr (DT != LQSGD_F32 && N % 8 == 0) {
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < N / 8; ++i)
+        reinterpret_cast<uint4*>(p)[i] = make_uint4(pack_pair<DT>(v[8 * i], v[8 * i + 1]), pack_pair<DT>(v[8 * i + 2], v[8 * i + 3]),
+                                                    pack_pair<DT>(v[8 * i + 4], v[8 * i + 5]), pack_pair<DT>(v[8 * i + 6], v[8 * i + 7]));
+      return;
+    }
+  }
   using E = Elem<DT>;
   constexpr int kBytes = N * (int)sizeof(typename E::T);
   if (vec) {
@@ -186,6 +211,15 @@ __device__ __forceinline__ float act_slope(float z) {
   if constexpr (ACT == LQSGD_ACT_GELU) { float g; const float c = normal_cdf(z, g); return fmaf(z * 0.39894228f, g, c); }
   if constexpr (ACT == LQSGD_ACT_SILU) { const float s = logistic(z); return s * fmaf(z, 1.f - s, 1.f); }
   return 1.f;
+}
+// Calls f with the activation as a compile-time constant: one branch outside a loop instead of one per value.
+template <int A> struct ActTag { static constexpr int value = A; };
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == LQSGD_ACT_RELU) f(ActTag<LQSGD_ACT_RELU>());
+  else if (act == LQSGD_ACT_GELU) f(ActTag<LQSGD_ACT_GELU>());
+  else if (act == LQSGD_ACT_SILU) f(ActTag<LQSGD_ACT_SILU>());
+  else f(ActTag<LQSGD_ACT_NONE>());
 }
 // The same for runs of values, the choice made once.
 template <int N>
