@@ -67,23 +67,26 @@ def _dtype(t: torch.Tensor, what: str, products: bool = False) -> int:
     return code
 
 
-def _matrix(t: torch.Tensor, what: str, device: int, dtype: Optional[torch.dtype] = None, shape=None) -> torch.Tensor:
-    """Checks a matrix argument; device is the index all tensors of the call must be on."""
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what} must be a matrix with unit stride along its rows")
-    if t.get_device() != device:
-        raise ValueError(f"{what} must be on the device of the call's other tensors")
+# The calls below are short on the device, so their own cost on the host counts: a matrix is checked and taken apart in one
+# go, arguments are packed in one go, and nothing is formatted unless it is refused.
+
+def _matrix(t: torch.Tensor, what: str, device: int, dtype: Optional[torch.dtype] = None, rows: int = -1, cols: int = -1) -> Tuple[int, int]:
+    """(address, elements between rows) of a checked matrix; device is the index that all tensors of the call are on."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be a matrix")
+    r, c = shape
+    ld, one = t.stride()
+    if one != 1 and c > 1:
+        raise ValueError(f"{what} must have unit stride along its rows")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{what} must be a CUDA tensor on the device of the call's other tensors")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    return t
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if (rows >= 0 and r != rows) or (cols >= 0 and c != cols):
+        raise ValueError(f"{what} must have {rows if rows >= 0 else 'any number of'} rows and {cols if cols >= 0 else 'any number of'} columns, "
+                         f"not {tuple(shape)}")
+    return t.data_ptr(), ld if r > 1 or ld > c else c
 
 
 def _vector(t: torch.Tensor, what: str, device: int, n: int) -> int:
@@ -93,28 +96,21 @@ def _vector(t: torch.Tensor, what: str, device: int, n: int) -> int:
     return t.data_ptr()
 
 
-class _On:
-    """Makes a device current for a call (nothing to do when it already is) and gives its current stream's handle."""
-    __slots__ = ("guard", "index")
-
-    def __init__(self, index: int):
-        self.index = index
-        self.guard = None if torch.cuda.current_device() == index else torch.cuda.device(index)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _elsewhere(device: int) -> bool:
+    """Whether `device` is not the current one: the calls then run again under torch.cuda.device."""
+    if device < 0:
+        raise ValueError("the tensors must be CUDA tensors")
+    return torch._C._cuda_getDevice() != device
 
 
-def _call(fn, args: tuple, layout: struct.Struct, bytes_fn, which: int, device: torch.device, stream) -> None:
+_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _call(fn, args: tuple, layout: struct.Struct, bytes_fn, which: int, device: torch.device) -> None:
     """Runs fn on a packed argument struct whose last two fields are the workspace.  Calls that need none are done at once;
     the others are refused on the host, before anything is launched, and get one from PyTorch's allocator (on the current
     stream, so its memory is not handed out again before the call's kernels are done)."""
+    stream = _stream(device.index)
     rc = fn(layout.pack(*args, 0, 0), stream)
     if rc == B.ERR_WORKSPACE_TOO_SMALL:
         need = C.c_size_t(0)
@@ -153,10 +149,8 @@ class Packed8:
     __slots__ = ("codes", "exps")
 
     def __init__(self, codes: torch.Tensor, exps: torch.Tensor):
-        dev = codes.get_device()
-        _matrix(codes, "codes", dev, torch.uint8)
-        _matrix(exps, "exps", dev, torch.uint8, (codes.shape[0], (codes.shape[1] + GROUP - 1) // GROUP))
         self.codes, self.exps = codes, exps
+        self.fields()
 
     @staticmethod
     def empty(rows: int, cols: int, device) -> "Packed8":
@@ -176,22 +170,36 @@ class Packed8:
     def device(self):
         return self.codes.device
 
-    def fields(self) -> tuple:
-        return self.codes.data_ptr(), _ld(self.codes), self.exps.data_ptr(), _ld(self.exps)
+    def fields(self) -> Tuple[int, int, int, int]:
+        """The members of lqsgd_packed8, checked."""
+        codes, exps = self.codes, self.exps
+        dev = codes.get_device()
+        cp, cl = _matrix(codes, "codes", dev, torch.uint8)
+        ep, el = _matrix(exps, "exps", dev, torch.uint8, codes.shape[0], (codes.shape[1] + GROUP - 1) // GROUP)
+        return cp, cl, ep, el
+
+
+def _kept(p: Optional[Packed8], what: str, device: int, rows: int, cols: int = -1) -> Tuple[int, int, int, int]:
+    """The fields of an 8-bit argument of rows x cols (any number of columns where -1)."""
+    if p is None:
+        raise ValueError(f"{what} must be the 8-bit form of a matrix")
+    r, c = p.codes.shape
+    if r != rows or (cols >= 0 and c != cols) or p.codes.get_device() != device:
+        raise ValueError(f"{what} must be the 8-bit form of {rows} x {cols if cols >= 0 else 'any'} values on the call's device, not of {r} x {c}")
+    return p.fields()
 
 
 def pack8(x: torch.Tensor, out: Optional[Packed8] = None) -> Packed8:
     """The 8-bit form of a matrix (bfloat16, float16 or float32)."""
     dev = x.get_device()
-    _matrix(x, "x", dev)
-    dt = _dtype(x, "x")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return pack8(x, out)
+    xp, xl = _matrix(x, "x", dev)
     rows, cols = x.shape
-    with _On(dev) as stream:
-        if out is None:
-            out = Packed8.empty(rows, cols, x.device)
-        else:
-            _matrix(out.codes, "out", dev, torch.uint8, (rows, cols))
-        rc = _library().lqsgd_pack8(x.data_ptr(), _ld(x), dt, rows, cols, _PACKED8.pack(*out.fields()), stream)
+    if out is None:
+        out = Packed8.empty(rows, cols, x.device)
+    rc = _library().lqsgd_pack8(xp, xl, _dtype(x, "x"), rows, cols, _PACKED8.pack(*_kept(out, "out", dev, rows, cols)), _stream(dev))
     if rc:
         B._check(rc)
     return out
@@ -199,16 +207,18 @@ def pack8(x: torch.Tensor, out: Optional[Packed8] = None) -> Packed8:
 
 def unpack8(p: Packed8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values an 8-bit form stands for: exact in bfloat16 and float32 (float16: within its range)."""
-    rows, cols = p.codes.shape
-    dev = p.codes.get_device()
+    codes = p.codes
+    dev = codes.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return unpack8(p, dtype, out)
+    rows, cols = codes.shape
     if dtype not in DTYPES:
         raise ValueError(f"dtype must be one of {list(DTYPES)}")
-    with _On(dev) as stream:
-        if out is None:
-            out = torch.empty((rows, cols), dtype=dtype, device=p.codes.device)
-        else:
-            _matrix(out, "out", dev, dtype, (rows, cols))
-        rc = _library().lqsgd_unpack8(_PACKED8.pack(*p.fields()), rows, cols, out.data_ptr(), _ld(out), DTYPES[dtype], stream)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    yp, yl = _matrix(out, "out", dev, dtype, rows, cols)
+    rc = _library().lqsgd_unpack8(_PACKED8.pack(*p.fields()), rows, cols, yp, yl, DTYPES[dtype], _stream(dev))
     if rc:
         B._check(rc)
     return out
@@ -219,32 +229,29 @@ def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_gr
     """(dz, db): dz = dy act'(z) with z from its 8-bit form, db its column sums in float32 (None without bias_grad).
     With act "none" dz is dy itself.  `out` may be dy."""
     dev = dy.get_device()
-    _matrix(dy, "dy", dev)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return act_grad(dy, z8, act, bias_grad, out)
+    yp, yl = _matrix(dy, "dy", dev)
     dt, a = _dtype(dy, "dy"), _act(act)
     rows, cols = dy.shape
-    if a == 0:
-        if not bias_grad:
-            return dy, None
-    elif z8 is None:
-        raise ValueError("z8 must be the 8-bit form of the pre-activation")
-    else:
-        _matrix(z8.codes, "z8", dev, torch.uint8, (rows, cols))
-    lib = _library()
-    with _On(dev) as stream:
-        dz, dz_ptr, ld_dz, zf = dy, 0, 0, None
-        if a:
-            dz = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if out is None else _matrix(out, "out", dev, dy.dtype, (rows, cols))
-            dz_ptr, ld_dz, zf = dz.data_ptr(), _ld(dz), _PACKED8.pack(*z8.fields())
-        db, db_ptr = None, 0
-        if bias_grad:
-            db = torch.empty(cols, dtype=torch.float32, device=dy.device)
-            db_ptr = db.data_ptr()
-        rc = lib.lqsgd_act_grad(dy.data_ptr(), _ld(dy), zf, a, dt, rows, cols, dz_ptr, ld_dz, db_ptr, 0, 0, stream)
-        if rc == B.ERR_WORKSPACE_TOO_SMALL:
-            need = C.c_size_t(0)
-            B._check(lib.lqsgd_act_grad_workspace_bytes(rows, cols, C.byref(need)))
+    dz, dp, dl, zf = dy, 0, 0, None
+    if a:
+        zf = _PACKED8.pack(*_kept(z8, "z8", dev, rows, cols))
+        dz = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if out is None else out
+        dp, dl = _matrix(dz, "out", dev, dy.dtype, rows, cols)
+    elif not bias_grad:
+        return dy, None
+    lib, stream = _library(), _stream(dev)
+    db, bp, wp, need = None, 0, 0, C.c_size_t(0)
+    if bias_grad:
+        db = torch.empty(cols, dtype=torch.float32, device=dy.device)
+        bp = db.data_ptr()
+        B._check(lib.lqsgd_act_grad_workspace_bytes(rows, cols, C.byref(need)))
+        if need.value:
             ws = torch.empty(need.value, dtype=torch.uint8, device=dy.device)
-            rc = lib.lqsgd_act_grad(dy.data_ptr(), _ld(dy), zf, a, dt, rows, cols, dz_ptr, ld_dz, db_ptr, ws.data_ptr(), need.value, stream)
+            wp = ws.data_ptr()
+    rc = lib.lqsgd_act_grad(yp, yl, zf, a, dt, rows, cols, dp, dl, bp, wp, need.value, stream)
     if rc:
         B._check(rc)
     return dz, db
@@ -264,27 +271,27 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     """y = act(x w^T + bias) + residual, x rows x in and w out x in, bfloat16 or float16; bias float32.
     save_z8 / save_y8 also return the 8-bit form of the pre-activation x w^T + bias / of y.  `out` may be the residual."""
     dev = x.get_device()
-    _matrix(x, "x", dev)
-    dt, code = _dtype(x, "x", True), _act(act)
-    _matrix(w, "w", dev, x.dtype)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return linear(x, w, bias, act, residual, save_z8, save_y8, out)
+    dtype, device = x.dtype, x.device
+    xp, xl = _matrix(x, "x", dev)
     rows, cin = x.shape
+    wp, wl = _matrix(w, "w", dev, dtype, -1, cin)
     cout = w.shape[0]
-    if w.shape[1] != cin:
-        raise ValueError(f"w must have {cin} columns, not {w.shape[1]}")
-    bias_ptr = 0 if bias is None else _vector(bias, "bias", dev, cout)
-    res_ptr = ld_res = 0
+    rp = rl = 0
     if residual is not None:
-        _matrix(residual, "residual", dev, x.dtype, (rows, cout))
-        res_ptr, ld_res = residual.data_ptr(), _ld(residual)
+        rp, rl = _matrix(residual, "residual", dev, dtype, rows, cout)
+    y = torch.empty((rows, cout), dtype=dtype, device=device) if out is None else out
+    yp, yl = _matrix(y, "out", dev, dtype, rows, cout)
+    z8 = Packed8.empty(rows, cout, device) if save_z8 else None
+    y8 = Packed8.empty(rows, cout, device) if save_y8 else None
     lib = _library()
-    with _On(dev) as stream:
-        y = torch.empty((rows, cout), dtype=x.dtype, device=x.device) if out is None else _matrix(out, "out", dev, x.dtype, (rows, cout))
-        z8 = Packed8.empty(rows, cout, x.device) if save_z8 else None
-        y8 = Packed8.empty(rows, cout, x.device) if save_y8 else None
-        args = (_LINEAR.size, dt, code, 0, rows, cin, cout, x.data_ptr(), _ld(x), w.data_ptr(), _ld(w), 0, 0, bias_ptr, res_ptr, ld_res,
-                y.data_ptr(), _ld(y), *_NONE8, *(z8.fields() if save_z8 else _NONE8), *(y8.fields() if save_y8 else _NONE8),
-                _status_word(x.device))
-        _call(lib.lqsgd_linear_forward, args, _LINEAR, lib.lqsgd_linear_workspace_bytes, FORWARD, x.device, stream)
+    _call(lib.lqsgd_linear_forward,
+          (_LINEAR.size, _dtype(x, "x", True), _act(act), 0, rows, cin, cout, xp, xl, wp, wl, 0, 0,
+           0 if bias is None else _vector(bias, "bias", dev, cout), rp, rl, yp, yl, *_NONE8,
+           *(z8.fields() if save_z8 else _NONE8), *(y8.fields() if save_y8 else _NONE8), _status_word(device)),
+          _LINEAR, lib.lqsgd_linear_workspace_bytes, FORWARD, device)
     return LinearOut(y, z8, y8)
 
 
@@ -292,52 +299,54 @@ def linear_grad_input(dz: torch.Tensor, w: torch.Tensor, residual: Optional[torc
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dx = dz w + residual (the gradient that came down the skip connection).  `out` may be the residual."""
     dev = dz.get_device()
-    _matrix(dz, "dz", dev)
-    dt = _dtype(dz, "dz", True)
-    _matrix(w, "w", dev, dz.dtype)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return linear_grad_input(dz, w, residual, out)
+    dtype, device = dz.dtype, dz.device
+    zp, zl = _matrix(dz, "dz", dev)
     rows, cout = dz.shape
+    wp, wl = _matrix(w, "w", dev, dtype, cout)
     cin = w.shape[1]
-    if w.shape[0] != cout:
-        raise ValueError(f"w must have {cout} rows, not {w.shape[0]}")
-    res_ptr = ld_res = 0
+    rp = rl = 0
     if residual is not None:
-        _matrix(residual, "residual", dev, dz.dtype, (rows, cin))
-        res_ptr, ld_res = residual.data_ptr(), _ld(residual)
+        rp, rl = _matrix(residual, "residual", dev, dtype, rows, cin)
+    dx = torch.empty((rows, cin), dtype=dtype, device=device) if out is None else out
+    op, ol = _matrix(dx, "out", dev, dtype, rows, cin)
     lib = _library()
-    with _On(dev) as stream:
-        dx = torch.empty((rows, cin), dtype=dz.dtype, device=dz.device) if out is None else _matrix(out, "out", dev, dz.dtype, (rows, cin))
-        args = (_LINEAR.size, dt, 0, 0, rows, cin, cout, 0, 0, w.data_ptr(), _ld(w), dz.data_ptr(), _ld(dz), 0, res_ptr, ld_res,
-                dx.data_ptr(), _ld(dx), *_NONE8, *_NONE8, *_NONE8, _status_word(dz.device))
-        _call(lib.lqsgd_linear_grad_input, args, _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_INPUT, dz.device, stream)
+    _call(lib.lqsgd_linear_grad_input,
+          (_LINEAR.size, _dtype(dz, "dz", True), 0, 0, rows, cin, cout, 0, 0, wp, wl, zp, zl, 0, rp, rl, op, ol, *_NONE8, *_NONE8, *_NONE8,
+           _status_word(device)),
+          _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_INPUT, device)
     return dx
 
 
 def linear_grad_weight(dz: torch.Tensor, x: Union[torch.Tensor, Packed8], out: Optional[torch.Tensor] = None,
                        accumulate: bool = False) -> torch.Tensor:
-    """dw = dz^T x in float32, out x in: the gradient a round takes.  x is a matrix of dz's type or its 8-bit form.
-    accumulate adds to `out` (a gradient over several micro-batches)."""
+    """dw = dz^T x in float32, out x in: the gradient a round takes.  x is a matrix of dz's type or its 8-bit form (which is
+    decoded into a workspace of rows x in 16-bit values for the call).  accumulate adds to `out` (a gradient over several
+    micro-batches)."""
     dev = dz.get_device()
-    _matrix(dz, "dz", dev)
-    dt = _dtype(dz, "dz", True)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return linear_grad_weight(dz, x, out, accumulate)
+    device = dz.device
+    zp, zl = _matrix(dz, "dz", dev)
     rows, cout = dz.shape
-    packed = isinstance(x, Packed8)
-    if packed:
-        _matrix(x.codes, "x", dev, torch.uint8)
-        x_ptr, ld_x, xf = 0, 0, x.fields()
+    xp, xl, xf = 0, 0, _NONE8
+    if isinstance(x, Packed8):
+        xf = _kept(x, "x", dev, rows)
     else:
-        _matrix(x, "x", dev, dz.dtype)
-        x_ptr, ld_x, xf = x.data_ptr(), _ld(x), _NONE8
-    if x.shape[0] != rows:
-        raise ValueError(f"x must have {rows} rows, not {x.shape[0]}")
+        xp, xl = _matrix(x, "x", dev, dz.dtype, rows)
+    cin = x.shape[1]
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    cin = x.shape[1]
+    dw = torch.empty((cout, cin), dtype=torch.float32, device=device) if out is None else out
+    op, ol = _matrix(dw, "out", dev, torch.float32, cout, cin)
     lib = _library()
-    with _On(dev) as stream:
-        dw = torch.empty((cout, cin), dtype=torch.float32, device=dz.device) if out is None else _matrix(out, "out", dev, torch.float32, (cout, cin))
-        args = (_LINEAR.size, dt, 0, int(accumulate), rows, cin, cout, x_ptr, ld_x, 0, 0, dz.data_ptr(), _ld(dz), 0, 0, 0,
-                dw.data_ptr(), _ld(dw), *xf, *_NONE8, *_NONE8, _status_word(dz.device))
-        _call(lib.lqsgd_linear_grad_weight, args, _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_WEIGHT, dz.device, stream)
+    _call(lib.lqsgd_linear_grad_weight,
+          (_LINEAR.size, _dtype(dz, "dz", True), 0, int(accumulate), rows, cin, cout, xp, xl, 0, 0, zp, zl, 0, 0, 0, op, ol,
+           *xf, *_NONE8, *_NONE8, _status_word(device)),
+          _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_WEIGHT, device)
     return dw
 
 
@@ -377,46 +386,53 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor, beta: torch.Te
                save_x8: bool = False, save_y8: bool = False) -> GroupNormOut:
     """y = act(gamma (x - mean) rstd + beta) over `groups` groups of channels of each sample; x is samples x ... x channels,
     bfloat16, float16 or float32, gamma and beta float32.  save_x8 / save_y8 also return 8-bit forms (rows = pixels)."""
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return group_norm(x, groups, gamma, beta, eps, act, save_x8, save_y8)
     n, hw, c, ld, sample = _pixels(x, "x")
-    dt, code, dev = _dtype(x, "x"), _act(act), x.get_device()
-    gamma_ptr, beta_ptr = _vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c)
+    device = x.device
+    y = torch.empty(x.shape, dtype=x.dtype, device=device)
+    shape = (n, max(1, groups))
+    mean = torch.empty(shape, dtype=torch.float32, device=device)
+    rstd = torch.empty(shape, dtype=torch.float32, device=device)
+    x8 = Packed8.empty(n * hw, c, device) if save_x8 else None
+    y8 = Packed8.empty(n * hw, c, device) if save_y8 else None
     lib = _library()
-    with _On(dev) as stream:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        stats = torch.empty((2, n, max(1, groups)), dtype=torch.float32, device=x.device)
-        mean, rstd = stats.unbind(0)
-        x8 = Packed8.empty(n * hw, c, x.device) if save_x8 else None
-        y8 = Packed8.empty(n * hw, c, x.device) if save_y8 else None
-        args = (_NORM.size, dt, code, groups, n, hw, c, eps, x.data_ptr(), ld, sample, 0, 0, 0, y.data_ptr(), c, hw * c,
-                gamma_ptr, beta_ptr, mean.data_ptr(), rstd.data_ptr(), 0, 0,
-                *(x8.fields() if save_x8 else _NONE8), *(y8.fields() if save_y8 else _NONE8))
-        _call(lib.lqsgd_group_norm_forward, args, _NORM, lib.lqsgd_group_norm_workspace_bytes, 0, x.device, stream)
+    _call(lib.lqsgd_group_norm_forward,
+          (_NORM.size, _dtype(x, "x"), _act(act), groups, n, hw, c, eps, x.data_ptr(), ld, sample, 0, 0, 0, y.data_ptr(), c, hw * c,
+           _vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c), mean.data_ptr(), rstd.data_ptr(), 0, 0,
+           *(x8.fields() if save_x8 else _NONE8), *(y8.fields() if save_y8 else _NONE8)),
+          _NORM, lib.lqsgd_group_norm_workspace_bytes, 0, device)
     return GroupNormOut(y, mean, rstd, x8, y8)
 
 
 def group_norm_grad(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], groups: int, gamma: torch.Tensor, beta: torch.Tensor,
                     mean: torch.Tensor, rstd: torch.Tensor, act: str = "none") -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dx, dgamma, dbeta) of group_norm; x as the forward call had it, or its 8-bit form; mean and rstd as it returned them."""
+    dev = dy.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return group_norm_grad(dy, x, groups, gamma, beta, mean, rstd, act)
     n, hw, c, ld, sample = _pixels(dy, "dy")
-    dt, code, dev = _dtype(dy, "dy"), _act(act), dy.get_device()
-    vectors = (_vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c), _vector(mean, "mean", dev, n * groups),
-               _vector(rstd, "rstd", dev, n * groups))
+    device = dy.device
+    xp, xl, xs, xf = 0, 0, 0, _NONE8
     if isinstance(x, Packed8):
-        _matrix(x.codes, "x", dev, torch.uint8, (n * hw, c))
-        x_ptr, ld_x, sample_x, xf = 0, 0, 0, x.fields()
+        xf = _kept(x, "x", dev, n * hw, c)
     else:
         if x.dtype != dy.dtype or x.shape != dy.shape or x.get_device() != dev:
             raise ValueError("x must have dy's type, shape and device")
-        _, _, _, ld_x, sample_x = _pixels(x, "x")
-        x_ptr, xf = x.data_ptr(), _NONE8
+        _, _, _, xl, xs = _pixels(x, "x")
+        xp = x.data_ptr()
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=device)
+    dgamma = torch.empty(c, dtype=torch.float32, device=device)
+    dbeta = torch.empty(c, dtype=torch.float32, device=device)
     lib = _library()
-    with _On(dev) as stream:
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-        dparam = torch.empty((2, c), dtype=torch.float32, device=dy.device)
-        dgamma, dbeta = dparam.unbind(0)
-        args = (_NORM.size, dt, code, groups, n, hw, c, 1.0, x_ptr, ld_x, sample_x, dy.data_ptr(), ld, sample, dx.data_ptr(), c, hw * c,
-                *vectors, dgamma.data_ptr(), dbeta.data_ptr(), *xf, *_NONE8)
-        _call(lib.lqsgd_group_norm_backward, args, _NORM, lib.lqsgd_group_norm_workspace_bytes, 1, dy.device, stream)
+    _call(lib.lqsgd_group_norm_backward,
+          (_NORM.size, _dtype(dy, "dy"), _act(act), groups, n, hw, c, 1.0, xp, xl, xs, dy.data_ptr(), ld, sample, dx.data_ptr(), c, hw * c,
+           _vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c), _vector(mean, "mean", dev, n * groups),
+           _vector(rstd, "rstd", dev, n * groups), dgamma.data_ptr(), dbeta.data_ptr(), *xf, *_NONE8),
+          _NORM, lib.lqsgd_group_norm_workspace_bytes, 1, device)
     return dx, dgamma, dbeta
 
 
