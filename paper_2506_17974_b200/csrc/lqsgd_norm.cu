@@ -789,7 +789,7 @@ size_t resident_smem(const Resident& r, int piece_bytes) {
   return (size_t)r.steps * kResThreads * piece_bytes + 4 * ((size_t)(2 * kRun * kResWarps << std::min(r.lane_shift, 5)) + 2 * r.cb + 4 * (r.cb / r.d.cpg));
 }
 // Whether the resident kernels take a problem, and how.  piece_bytes: shared memory per 8 channels of a pixel.
-bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
+bool plan_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
   auto gcd = [](int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; };
   if (d.c % kRun) return false;
   const int unit = packs ? kGroup : kRun;
@@ -831,6 +831,22 @@ bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
   if (best_score > 1e29) return false;
   *out = best;
   return true;
+}
+// The last plans of this host thread, by the sizes they are made from: a training step asks for the same ones over and over.
+bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
+  struct Memo { int32_t n = -1, hw, c, groups, packs, piece_bytes; bool ok; Resident r; };
+  static thread_local Memo memo[16];
+  static thread_local unsigned next = 0;
+  for (const Memo& m : memo)
+    if (m.n == d.n && m.hw == d.hw && m.c == d.c && m.groups == d.groups && m.packs == (int)packs && m.piece_bytes == piece_bytes) {
+      if (m.ok) { *out = m.r; out->d = d; }
+      return m.ok;
+    }
+  Memo& m = memo[next++ % 16];
+  m.ok = plan_resident(d, packs, piece_bytes, &m.r);
+  m.n = d.n; m.hw = d.hw; m.c = d.c; m.groups = d.groups; m.packs = packs; m.piece_bytes = piece_bytes;
+  if (m.ok) *out = m.r;
+  return m.ok;
 }
 template <void (*kernel)(Resident)>
 int launch_resident(const Resident& r, int piece_bytes, cudaStream_t st, const char* what) {

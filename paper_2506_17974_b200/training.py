@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import threading
 from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
@@ -106,19 +107,48 @@ def _elsewhere(device: int) -> bool:
 _stream = torch._C._cuda_getCurrentRawStream
 
 
+# Workspaces up to _KEEP bytes are kept per host thread, device and stream, so that a call in a training step needs no
+# allocation of its own; larger ones, and those of calls that are being captured in a graph (whose memory has to last as
+# long as the graph), come from PyTorch's allocator for the one call.  Calls of one thread on one stream follow one
+# another, so they may share one; the allocator does not hand out a call's own workspace again before its kernels are done.
+_KEEP = 16 << 20
+_scratch = {}
+
+
+def _workspace(need: int, device: torch.device, stream: int) -> torch.Tensor:
+    if need > _KEEP or torch._C._cuda_isCurrentStreamCapturing():
+        return torch.empty_strided((need,), (1,), dtype=torch.uint8, device=device)
+    ws = torch.empty_strided((max(need, 1 << 20),), (1,), dtype=torch.uint8, device=device)
+    _scratch[(threading.get_ident(), device.index, stream)] = (ws, ws.data_ptr(), ws.numel())
+    return ws
+
+
+_NO_SCRATCH = (None, 0, 0)
+
+
+def _kept_scratch(index: int, stream: int) -> tuple:
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return _NO_SCRATCH
+    return _scratch.get((threading.get_ident(), index, stream), _NO_SCRATCH)
+
+
 def _call(fn, args: tuple, layout: struct.Struct, bytes_fn, which: int, device: torch.device) -> None:
-    """Runs fn on a packed argument struct whose last two fields are the workspace.  Calls that need none are done at once;
-    the others are refused on the host, before anything is launched, and get one from PyTorch's allocator (on the current
-    stream, so its memory is not handed out again before the call's kernels are done)."""
+    """Runs fn on a packed argument struct whose last two fields are the workspace: the kept one, or, where the library refuses
+    that as too small (on the host, before anything is launched), one of the size it asks for."""
     stream = _stream(device.index)
-    rc = fn(layout.pack(*args, 0, 0), stream)
+    _, ptr, size = _kept_scratch(device.index, stream)
+    rc = fn(layout.pack(*args, ptr, size), stream)
     if rc == B.ERR_WORKSPACE_TOO_SMALL:
         need = C.c_size_t(0)
         B._check(bytes_fn(which, layout.pack(*args, 0, 0), C.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
-        rc = fn(layout.pack(*args, ws.data_ptr(), need.value), stream)
+        ws = _workspace(need.value, device, stream)
+        rc = fn(layout.pack(*args, ws.data_ptr(), ws.numel()), stream)
     if rc != 0:
         B._check(rc)
+
+
+def _empty(rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
 
 
 _status = {}
@@ -156,11 +186,14 @@ class Packed8:
     def empty(rows: int, cols: int, device) -> "Packed8":
         """Uninitialised; rows of codes start on 16-byte boundaries."""
         p = object.__new__(Packed8)
-        ld = (cols + 15) & -16
-        codes = torch.empty((rows, ld), dtype=torch.uint8, device=device)
-        p.codes = codes if ld == cols else codes[:, :cols]
-        p.exps = torch.empty((rows, (cols + GROUP - 1) // GROUP), dtype=torch.uint8, device=device)
+        p.codes = torch.empty_strided((rows, cols), ((cols + 15) & -16, 1), dtype=torch.uint8, device=device)
+        p.exps = _empty(rows, (cols + GROUP - 1) // GROUP, torch.uint8, device)
         return p
+
+    def _fresh(self) -> Tuple[int, int, int, int]:
+        """fields() of what empty() just made."""
+        rows, cols = self.codes.shape
+        return self.codes.data_ptr(), (cols + 15) & -16, self.exps.data_ptr(), (cols + GROUP - 1) // GROUP
 
     @property
     def shape(self):
@@ -199,7 +232,10 @@ def pack8(x: torch.Tensor, out: Optional[Packed8] = None) -> Packed8:
     rows, cols = x.shape
     if out is None:
         out = Packed8.empty(rows, cols, x.device)
-    rc = _library().lqsgd_pack8(xp, xl, _dtype(x, "x"), rows, cols, _PACKED8.pack(*_kept(out, "out", dev, rows, cols)), _stream(dev))
+        of = out._fresh()
+    else:
+        of = _kept(out, "out", dev, rows, cols)
+    rc = _library().lqsgd_pack8(xp, xl, _dtype(x, "x"), rows, cols, _PACKED8.pack(*of), _stream(dev))
     if rc:
         B._check(rc)
     return out
@@ -216,7 +252,7 @@ def unpack8(p: Packed8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch
     if dtype not in DTYPES:
         raise ValueError(f"dtype must be one of {list(DTYPES)}")
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+        out = _empty(rows, cols, dtype, codes.device)
     yp, yl = _matrix(out, "out", dev, dtype, rows, cols)
     rc = _library().lqsgd_unpack8(_PACKED8.pack(*p.fields()), rows, cols, yp, yl, DTYPES[dtype], _stream(dev))
     if rc:
@@ -238,20 +274,22 @@ def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_gr
     dz, dp, dl, zf = dy, 0, 0, None
     if a:
         zf = _PACKED8.pack(*_kept(z8, "z8", dev, rows, cols))
-        dz = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if out is None else out
+        dz = _empty(rows, cols, dy.dtype, dy.device) if out is None else out
         dp, dl = _matrix(dz, "out", dev, dy.dtype, rows, cols)
     elif not bias_grad:
         return dy, None
     lib, stream = _library(), _stream(dev)
-    db, bp, wp, need = None, 0, 0, C.c_size_t(0)
+    db, bp = None, 0
     if bias_grad:
-        db = torch.empty(cols, dtype=torch.float32, device=dy.device)
+        db = torch.empty_strided((cols,), (1,), dtype=torch.float32, device=dy.device)
         bp = db.data_ptr()
+    _, wp, size = _kept_scratch(dev, stream)
+    rc = lib.lqsgd_act_grad(yp, yl, zf, a, dt, rows, cols, dp, dl, bp, wp, size, stream)
+    if rc == B.ERR_WORKSPACE_TOO_SMALL:
+        need = C.c_size_t(0)
         B._check(lib.lqsgd_act_grad_workspace_bytes(rows, cols, C.byref(need)))
-        if need.value:
-            ws = torch.empty(need.value, dtype=torch.uint8, device=dy.device)
-            wp = ws.data_ptr()
-    rc = lib.lqsgd_act_grad(yp, yl, zf, a, dt, rows, cols, dp, dl, bp, wp, need.value, stream)
+        ws = _workspace(need.value, dy.device, stream)
+        rc = lib.lqsgd_act_grad(yp, yl, zf, a, dt, rows, cols, dp, dl, bp, ws.data_ptr(), ws.numel(), stream)
     if rc:
         B._check(rc)
     return dz, db
@@ -282,7 +320,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     rp = rl = 0
     if residual is not None:
         rp, rl = _matrix(residual, "residual", dev, dtype, rows, cout)
-    y = torch.empty((rows, cout), dtype=dtype, device=device) if out is None else out
+    y = _empty(rows, cout, dtype, device) if out is None else out
     yp, yl = _matrix(y, "out", dev, dtype, rows, cout)
     z8 = Packed8.empty(rows, cout, device) if save_z8 else None
     y8 = Packed8.empty(rows, cout, device) if save_y8 else None
@@ -290,7 +328,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     _call(lib.lqsgd_linear_forward,
           (_LINEAR.size, _dtype(x, "x", True), _act(act), 0, rows, cin, cout, xp, xl, wp, wl, 0, 0,
            0 if bias is None else _vector(bias, "bias", dev, cout), rp, rl, yp, yl, *_NONE8,
-           *(z8.fields() if save_z8 else _NONE8), *(y8.fields() if save_y8 else _NONE8), _status_word(device)),
+           *(z8._fresh() if save_z8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8), _status_word(device)),
           _LINEAR, lib.lqsgd_linear_workspace_bytes, FORWARD, device)
     return LinearOut(y, z8, y8)
 
@@ -310,7 +348,7 @@ def linear_grad_input(dz: torch.Tensor, w: torch.Tensor, residual: Optional[torc
     rp = rl = 0
     if residual is not None:
         rp, rl = _matrix(residual, "residual", dev, dtype, rows, cin)
-    dx = torch.empty((rows, cin), dtype=dtype, device=device) if out is None else out
+    dx = _empty(rows, cin, dtype, device) if out is None else out
     op, ol = _matrix(dx, "out", dev, dtype, rows, cin)
     lib = _library()
     _call(lib.lqsgd_linear_grad_input,
@@ -340,7 +378,7 @@ def linear_grad_weight(dz: torch.Tensor, x: Union[torch.Tensor, Packed8], out: O
     cin = x.shape[1]
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    dw = torch.empty((cout, cin), dtype=torch.float32, device=device) if out is None else out
+    dw = _empty(cout, cin, torch.float32, device) if out is None else out
     op, ol = _matrix(dw, "out", dev, torch.float32, cout, cin)
     lib = _library()
     _call(lib.lqsgd_linear_grad_weight,
@@ -392,17 +430,16 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor, beta: torch.Te
             return group_norm(x, groups, gamma, beta, eps, act, save_x8, save_y8)
     n, hw, c, ld, sample = _pixels(x, "x")
     device = x.device
-    y = torch.empty(x.shape, dtype=x.dtype, device=device)
-    shape = (n, max(1, groups))
-    mean = torch.empty(shape, dtype=torch.float32, device=device)
-    rstd = torch.empty(shape, dtype=torch.float32, device=device)
+    y = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=device)
+    mean = _empty(n, max(1, groups), torch.float32, device)
+    rstd = _empty(n, max(1, groups), torch.float32, device)
     x8 = Packed8.empty(n * hw, c, device) if save_x8 else None
     y8 = Packed8.empty(n * hw, c, device) if save_y8 else None
     lib = _library()
     _call(lib.lqsgd_group_norm_forward,
           (_NORM.size, _dtype(x, "x"), _act(act), groups, n, hw, c, eps, x.data_ptr(), ld, sample, 0, 0, 0, y.data_ptr(), c, hw * c,
            _vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c), mean.data_ptr(), rstd.data_ptr(), 0, 0,
-           *(x8.fields() if save_x8 else _NONE8), *(y8.fields() if save_y8 else _NONE8)),
+           *(x8._fresh() if save_x8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8)),
           _NORM, lib.lqsgd_group_norm_workspace_bytes, 0, device)
     return GroupNormOut(y, mean, rstd, x8, y8)
 
@@ -424,9 +461,9 @@ def group_norm_grad(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], groups: i
             raise ValueError("x must have dy's type, shape and device")
         _, _, _, xl, xs = _pixels(x, "x")
         xp = x.data_ptr()
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=device)
-    dgamma = torch.empty(c, dtype=torch.float32, device=device)
-    dbeta = torch.empty(c, dtype=torch.float32, device=device)
+    dx = torch.empty_like(dy) if dy.is_contiguous() else torch.empty(dy.shape, dtype=dy.dtype, device=device)
+    dgamma = torch.empty_strided((c,), (1,), dtype=torch.float32, device=device)
+    dbeta = torch.empty_strided((c,), (1,), dtype=torch.float32, device=device)
     lib = _library()
     _call(lib.lqsgd_group_norm_backward,
           (_NORM.size, _dtype(dy, "dy"), _act(act), groups, n, hw, c, 1.0, xp, xl, xs, dy.data_ptr(), ld, sample, dx.data_ptr(), c, hw * c,
