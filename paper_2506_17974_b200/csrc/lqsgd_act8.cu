@@ -35,10 +35,12 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kRun = 8;                      // columns per thread
 
-// How a matrix is dealt out: warps of 32 / lanes rows x (8 lanes) columns; blockIdx.x = column segment, blockIdx.y = row block.
+// How a matrix is dealt out: a warp takes 32 / lanes rows x (8 lanes) columns; a block's 8 warps stand 1 << wide_shift side by
+// side (up to four: a block then reads two kilobytes of a row, which HBM serves up to 1.6 times faster than the same bytes
+// from many rows) and the rest below one another; blockIdx.x = column segment, blockIdx.y = row block.
 struct Deal {
   int64_t rows, rows_per_block;
-  int32_t cols, lane_shift;                  // lanes = 1 << lane_shift
+  int32_t cols, lane_shift, wide_shift;      // lanes = 1 << lane_shift
 };
 template <bool RUNS>
 struct Spot {
@@ -49,13 +51,13 @@ struct Spot {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int lanes = 1 << d.lane_shift, per_warp = 32 >> d.lane_shift;
     sub = lane >> d.lane_shift;
-    const int seg = (int)blockIdx.x * lanes * kRun, in = lane & (lanes - 1);
+    const int seg = ((((int)blockIdx.x << d.wide_shift) + (warp & ((1 << d.wide_shift) - 1))) << d.lane_shift) * kRun, in = lane & (lanes - 1);
     col = seg + (RUNS ? in * kRun : in);
     have = RUNS ? min(kRun, d.cols - col) : (col < d.cols ? min(kRun, (d.cols - col + 31) / 32) : 0);
     const int64_t first = (int64_t)blockIdx.y * d.rows_per_block;
-    row = first + warp * per_warp + sub;
+    row = first + (warp >> d.wide_shift) * per_warp + sub;
     row_end = min(d.rows, first + d.rows_per_block);
-    row_step = kWarps * per_warp;
+    row_step = (kWarps >> d.wide_shift) * per_warp;
   }
   static __device__ __forceinline__ constexpr int step() { return RUNS ? 1 : 32; }      // between the thread's columns
 };
@@ -65,8 +67,10 @@ Deal make_deal(int64_t rows, int32_t cols, bool runs, int ctas_wanted, int64_t l
   d.cols = cols;
   d.lane_shift = runs ? 2 : 5;
   while (d.lane_shift < 5 && (8 << d.lane_shift) < cols) ++d.lane_shift;
-  const int64_t segs = ceil_div64(cols, 8ll << d.lane_shift);
-  const int64_t step = kWarps * (32 >> d.lane_shift);              // rows one pass of a block covers
+  d.wide_shift = 0;
+  while (d.wide_shift < 2 && (8ll << (d.lane_shift + d.wide_shift)) < cols) ++d.wide_shift;
+  const int64_t segs = ceil_div64(cols, 8ll << (d.lane_shift + d.wide_shift));
+  const int64_t step = (kWarps >> d.wide_shift) * (32 >> d.lane_shift);   // rows one pass of a block covers
   const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>({ceil_div64(rows, step * least_rows), ceil_div64(ctas_wanted, segs), 65535}));
   d.rows_per_block = ceil_div64(ceil_div64(rows, blocks), step) * step;
   *grid = dim3((unsigned)segs, (unsigned)std::max<int64_t>(1, ceil_div64(rows, d.rows_per_block)));
@@ -156,6 +160,9 @@ pack8_kernel(Deal d, const void* __restrict__ x, int64_t ld_x, bool vec_x, lqsgd
   using T = typename Elem<DT>::T;
   const Spot<RUNS> s(d);
   const bool vx = vec_x && s.have == kRun, vc = vec_c && s.have == kRun;
+  // strides: a row's 256 codes pass through shared memory, where the lanes put them by columns and take them by runs
+  __shared__ __align__(8) uint8_t turn[RUNS ? 1 : kWarps][256];
+  uint8_t* mine_at = turn[RUNS ? 0 : threadIdx.x >> 5];
   // a warp whose last rows lie past the end stays together for the shuffles: those lanes hold zeros and store nothing
   for (int64_t r0 = s.row; r0 - s.sub < s.row_end; r0 += kRows * s.row_step) {
     Piece<DT> raw[kRows];
@@ -189,15 +196,18 @@ pack8_kernel(Deal d, const void* __restrict__ x, int64_t ld_x, bool vec_x, lqsgd
           if ((s.col & (kGroup - 1)) == 0) *exps = (uint8_t)eb;
         }
       } else {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x & 31, seg = s.col - lane, run = seg + kRun * lane, have = min(kRun, d.cols - run);
         uint32_t mine = 0;                                // lane j keeps the j-th group's byte
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
           const int eb = exp_byte(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu)));
           if (lane == j) mine = (uint32_t)eb;
-          const uint32_t c = (mag_bits(v[j], inv_step(eb)) & 127u) | ((__float_as_uint(v[j]) >> 24) & 128u);
-          if (on && j < s.have) codes[32 * j] = (uint8_t)c;
+          mine_at[32 * j + lane] = (uint8_t)((mag_bits(v[j], inv_step(eb)) & 127u) | ((__float_as_uint(v[j]) >> 24) & 128u));
         }
+        __syncwarp();
+        const uint2 w = *reinterpret_cast<const uint2*>(mine_at + kRun * lane);
+        __syncwarp();
+        if (r < s.row_end && have > 0) store_codes<true>(out.dev_codes + r * out.ld_codes + run, vec_c && have == kRun, have, w);
         // the segment's groups that exist: those whose first column, lane 0's, does
         if (r < s.row_end && lane < kRun && s.col - lane + 32 * lane < d.cols) exps[lane] = (uint8_t)mine;
       }
@@ -212,30 +222,49 @@ unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64
   train_pdl_wait();
   using T = typename Elem<DT>::T;
   const Spot<RUNS> s(d);
-  if (s.have <= 0) return;
-  const bool vy = vec_y && s.have == kRun, vc = vec_c && s.have == kRun;
+  // Codes are read by runs in either layout; with strides the values pass through shared memory to be stored by columns.
+  __shared__ __align__(16) T turn[RUNS ? 1 : kWarps][256];
+  const int lane = threadIdx.x & 31, run = RUNS ? s.col : s.col - lane + kRun * lane, have = min(kRun, d.cols - run);
+  if (RUNS && have <= 0) return;
+  const bool vy = vec_y && have == kRun, vc = vec_c && have == kRun;
   for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
-    uint2 w[kRows], e[kRows];
+    uint2 w[kRows];
+    int e[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
-      w[u] = load_codes<RUNS>(in.dev_codes + r * in.ld_codes + s.col, vc, s.have);
-      e[u] = load_exps<RUNS>(in.dev_exps + r * in.ld_exps, s.col, s.have);
+      w[u] = make_uint2(0u, 0u);
+      e[u] = kExpBias;
+      if (have > 0) {
+        w[u] = load_codes<true>(in.dev_codes + r * in.ld_codes + run, vc, have);
+        e[u] = in.dev_exps[r * in.ld_exps + run / kGroup];
+      }
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int64_t r = r0 + u * s.row_step;
       if (r >= s.row_end) break;
       float v[kRun];
-      decode_piece<RUNS>(w[u], e[u], v);
+      decode_run(w[u], e[u], v);
       // only sources wider than the target can exceed its range: the largest finite value then (a NaN stays)
       constexpr float kTop = DT == LQSGD_F16 ? 65504.f : (DT == LQSGD_BF16 ? 3.3895314e38f : 3.402823466e38f);
-      if (DT != LQSGD_F32 && (!RUNS || (int)e[u].x >= (DT == LQSGD_F16 ? kExpBias + 9 : kQuickByte))) {
+      if (DT != LQSGD_F32 && e[u] >= (DT == LQSGD_F16 ? kExpBias + 9 : kQuickByte)) {
 #pragma unroll
         for (int j = 0; j < kRun; ++j)
           if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
       }
-      store_piece<DT, RUNS>(static_cast<T*>(y) + r * ld_y + s.col, vy, s.have, v);
+      if (RUNS) {
+        store_run<DT, kRun>(static_cast<T*>(y) + r * ld_y + run, vy, have, v);
+      } else {
+        T* row = turn[threadIdx.x >> 5];
+        store_run<DT, kRun>(row + kRun * lane, true, kRun, v);
+        __syncwarp();
+        T* to = static_cast<T*>(y) + r * ld_y + s.col;
+#pragma unroll
+        for (int j = 0; j < kRun; ++j)
+          if (j < s.have) to[32 * j] = row[32 * j + lane];
+        __syncwarp();
+      }
     }
   }
 }
@@ -245,13 +274,20 @@ unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64
 // times a step, and both slopes satisfy s(-z) = 1 - s(z).  So a block that has work enough first tabulates the slopes for the
 // steps 2^-16 .. 2^4; below them the slope is 1/2 + s'(0) z to 2^-31, above them 0 or 1 (or 1/2 at 0) to 2^-23: those, and
 // blocks with little work, compute them.
+// Rows in flight per thread and blocks per SM, measured on 8192 x 16384 in bf16: without z, one row and six blocks (48 us; two
+// rows 72); with z, four rows and three blocks (gelu 122 us, two rows and four blocks 148, one and six 142).
+template <int DT, int KIND>
+struct SumShape {
+  static constexpr int kRows = KIND == 0 ? 1 : (DT == LQSGD_F32 ? 2 : 4);
+  static constexpr int kBlocks = KIND == 0 ? 6 : 3;
+};
 enum SlopeKind { kSlopeNone = 0, kSlopeRelu = 1, kSlopeCurve = 2 };
 constexpr int kTabLow = kExpBias - 16, kTabSteps = 21;
 template <int DT, bool RUNS, int KIND>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, SumShape<DT, KIND>::kBlocks)
 act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed8 z8, bool vec_c, int act, bool table,
                 void* dz, int64_t ld_dz, bool vec_dz, float* __restrict__ partial) {
-  constexpr int kRows = DT == LQSGD_F32 ? 2 : 4;
+  constexpr int kRows = SumShape<DT, KIND>::kRows;
   using T = typename Elem<DT>::T;
   __shared__ float tab[KIND == kSlopeCurve ? kTabSteps * 128 : 1];
   __shared__ float sums[kWarps][32][kRun + 1];
@@ -333,13 +369,14 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
 #pragma unroll
   for (int j = 0; j < kRun; ++j) sums[warp][lane][j] = acc[j];
   __syncthreads();
-  const int lanes = 1 << d.lane_shift;
-  for (int c = threadIdx.x; c < lanes * kRun; c += kThreads) {
-    const int col = (int)blockIdx.x * lanes * kRun + c;
+  const int warp_cols = kRun << d.lane_shift;
+  for (int c = threadIdx.x; c < warp_cols << d.wide_shift; c += kThreads) {
+    const int col = (int)blockIdx.x * (warp_cols << d.wide_shift) + c;
     if (col >= d.cols) continue;
-    const int from = RUNS ? c / kRun : c & 31, j = RUNS ? c % kRun : c >> 5;
+    const int beside = c / warp_cols, in = c - beside * warp_cols;
+    const int from = RUNS ? in / kRun : in & 31, j = RUNS ? in % kRun : in >> 5;
     float t = 0.f;
-    for (int w = 0; w < kWarps; ++w)
+    for (int w = beside; w < kWarps; w += 1 << d.wide_shift)
       for (int sub = 0; sub < (32 >> d.lane_shift); ++sub) t += sums[w][(sub << d.lane_shift) + from][j];
     partial[(size_t)blockIdx.y * d.cols + col] = t;
   }
@@ -367,10 +404,10 @@ join_columns_kernel(const float* __restrict__ partial, int blocks, int cols, flo
   }
 }
 
-// CTAs that fill the card: 148 SMs x 8 blocks of 256 threads (x 4 where they leave column sums behind to be joined).  Constants,
+// CTAs that fill the card: 148 SMs x 8 blocks of 256 threads (x 6 where they leave column sums behind to be joined).  Constants,
 // so that the order of the sums, and the workspace, depend on the sizes alone.
-constexpr int kCtas = 148 * 8, kCtasSums = 148 * 4;
-Deal deal_sums(int64_t rows, int32_t cols, bool runs, dim3* grid) { return make_deal(rows, cols, runs, kCtasSums, 4, grid); }
+constexpr int kCtas = 148 * 8, kCtasSums = 148 * 6;
+Deal deal_sums(int64_t rows, int32_t cols, bool runs, dim3* grid) { return make_deal(rows, cols, runs, kCtasSums, 8, grid); }
 
 int check_matrix(int64_t rows, int32_t cols) {
   return rows < 0 || cols < 1 || rows > (int64_t)1 << 40 ? LQSGD_ERR_BAD_SHAPE : LQSGD_OK;
@@ -450,7 +487,7 @@ static cudaError_t launch_act_grad(int act, dim3 grid, cudaStream_t st, const De
   if (act == LQSGD_ACT_RELU)
     return train_launch(act_grad_kernel<DT, RUNS, kSlopeRelu>, grid, dim3(kThreads), 0, st, 1, d, dy, ld_dy, vg, z8, vc, act, false, dz, ld_dz, vz, partial);
   // a block's table takes about ten slopes per thread: worth it from four times as many values on
-  const bool table = d.rows_per_block * (kRun << d.lane_shift) >= 40 * kThreads;
+  const bool table = d.rows_per_block * (kRun << (d.lane_shift + d.wide_shift)) >= 40 * kThreads;
   return train_launch(act_grad_kernel<DT, RUNS, kSlopeCurve>, grid, dim3(kThreads), 0, st, 1, d, dy, ld_dy, vg, z8, vc, act, table, dz, ld_dz, vz, partial);
 }
 

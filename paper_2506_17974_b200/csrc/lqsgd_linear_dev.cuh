@@ -504,6 +504,11 @@ struct LinWalk {
   }
 };
 
+// Rows that each of the CTAs that sum a tile together finishes: an equal part of those that exist.
+__device__ __forceinline__ int meet_slice(const LinProblem& p, const LinWalk& w, int meet) {
+  return (int)quick_div(min(kLinBM, p.M - w.m_tile * kLinBM) + meet - 1, meet);
+}
+
 // WF32: the result is fp32 (a weight gradient).
 template <int CG, int BN, int OA, int OB, bool WF32>
 struct LinCfg {
@@ -696,7 +701,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
         }
         if (CG == 1 && meet > 1) {                // to the CTA whose slice the row is in, for this CTA's place there
-          const int r = 32 * q + lane, slice = (kLinBM + meet - 1) / meet, to = r / slice;
+          const int r = 32 * q + lane, slice = meet_slice(p, w, meet), to = min((int)quick_div(r, slice), meet - 1);
+          if (m >= p.M) continue;
           const uint32_t o = map_to(reinterpret_cast<float*>(base) + (part_of * slice + r - to * slice) * S::kMeetPitch + c, to);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -731,10 +737,9 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     // ---- the CTAs' sums of one tile have met: a warp takes a row of this CTA's slice, a lane four of its columns
     train_pdl_wait();                               // (the warps that had no need to yet)
     const LinWalk w(p, cluster, clusters, part_of);
-    const int slice = (kLinBM + meet - 1) / meet, rows = min(slice, kLinBM - part_of * slice);
+    const int slice = meet_slice(p, w, meet), rows = min(slice, min(kLinBM, p.M - w.m_tile * kLinBM) - part_of * slice);
     for (int r = warp; r < rows; r += S::kThreads / 32) {
       const int row = w.m_tile * kLinBM + part_of * slice + r;
-      if (row >= p.ep.rows) break;
       float v[4] = {0.f, 0.f, 0.f, 0.f};
       const float* mine = reinterpret_cast<const float*>(base) + r * S::kMeetPitch + 4 * lane;
 #pragma unroll 4
