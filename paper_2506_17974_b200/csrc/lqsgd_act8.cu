@@ -1,12 +1,11 @@
 // Activations kept in 8 bits: packing, unpacking, and the activation's backward step that reads them.
 //
-// All three are streams: each value is read once and written once, and what bounds them is HBM.  Two layouts of the work:
-//   runs      rows of 16-byte pieces: a thread owns 8 consecutive columns of a row, so four neighbouring lanes hold one group of
-//             32 and agree on its exponent with two shuffles.  A warp covers `lanes` x 8 columns of 32 / lanes rows, lanes = 4 .. 32
-//             by the row length, so that short rows do not leave lanes idle.
-//   strides   rows at any alignment, more than 128 columns: a thread owns 8 columns 32 apart, so that a warp's access to one of
-//             them is 32 neighbouring elements (a run of 8 read element by element touches 32 places instead), and a group is
-//             one column of every lane.
+// All three are streams: each value is read once and written once, and what bounds them is HBM.  A thread works on runs of 8
+// consecutive columns of a row, so four neighbouring lanes hold one group of 32 and agree on its exponent with two
+// shuffles.  A warp covers `lanes` x 8 columns of 32 / lanes rows, lanes = 4 .. 32 by the row length, so that short rows do
+// not leave lanes idle.  Rows of 16-byte pieces are read and written as such (RUNS).  Rows at any other alignment are
+// read and written 32 neighbouring elements at a time, a lane each (a run of 8 taken element by element touches 32
+// places instead), and turned between the two forms in shared memory.
 // A thread takes several rows at a time, all their loads first: one row in flight per thread does not fill HBM's latency.
 #include "lqsgd_train_dev.cuh"
 
@@ -42,24 +41,24 @@ struct Deal {
   int64_t rows, rows_per_block;
   int32_t cols, lane_shift, wide_shift;      // lanes = 1 << lane_shift
 };
-template <bool RUNS>
 struct Spot {
   int64_t row, row_end, row_step;            // rows row, row + row_step, ... < row_end
-  int col, have;                             // first column; how many of its 8 exist (<= 0: none)
+  int col, have;                             // first column of the run; how many of its 8 exist (<= 0: none)
+  int side;                                  // the warp's first column + lane: columns side, side + 32, ... of the other form
   int sub;                                   // which of the warp's rows
   __device__ __forceinline__ explicit Spot(const Deal& d) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int lanes = 1 << d.lane_shift, per_warp = 32 >> d.lane_shift;
     sub = lane >> d.lane_shift;
-    const int seg = ((((int)blockIdx.x << d.wide_shift) + (warp & ((1 << d.wide_shift) - 1))) << d.lane_shift) * kRun, in = lane & (lanes - 1);
-    col = seg + (RUNS ? in * kRun : in);
-    have = RUNS ? min(kRun, d.cols - col) : (col < d.cols ? min(kRun, (d.cols - col + 31) / 32) : 0);
+    const int seg = ((((int)blockIdx.x << d.wide_shift) + (warp & ((1 << d.wide_shift) - 1))) << d.lane_shift) * kRun;
+    col = seg + (lane & (lanes - 1)) * kRun;
+    have = min(kRun, d.cols - col);
+    side = seg + lane;
     const int64_t first = (int64_t)blockIdx.y * d.rows_per_block;
     row = first + (warp >> d.wide_shift) * per_warp + sub;
     row_end = min(d.rows, first + d.rows_per_block);
     row_step = (kWarps >> d.wide_shift) * per_warp;
   }
-  static __device__ __forceinline__ constexpr int step() { return RUNS ? 1 : 32; }      // between the thread's columns
 };
 Deal make_deal(int64_t rows, int32_t cols, bool runs, int ctas_wanted, int64_t least_rows, dim3* grid) {
   Deal d;
@@ -76,93 +75,86 @@ Deal make_deal(int64_t rows, int32_t cols, bool runs, int ctas_wanted, int64_t l
   *grid = dim3((unsigned)segs, (unsigned)std::max<int64_t>(1, ceil_div64(rows, d.rows_per_block)));
   return d;
 }
-// Layout for these operands: runs where every one has 16-byte pieces (8-byte for codes), or rows too short for strides.
-bool use_runs(bool vec_a, bool vec_b, bool vec_c, int32_t cols) { return (vec_a && vec_b && vec_c) || cols <= 128; }
+// Runs where the values have 16-byte pieces, or where the rows are too short for a warp's 256 columns.
+bool use_runs(bool vec, int32_t cols) { return vec || cols <= 128; }
 
 // Raw pieces, so that several rows' loads can be outstanding before any is converted.
 template <int DT> struct Piece { uint32_t w[kRun * sizeof(typename Elem<DT>::T) / 4]; };
+// row: the row's first element.  What does not exist reads as 0.
 template <int DT, bool RUNS>
-__device__ __forceinline__ void load_piece(const typename Elem<DT>::T* p, bool vec, int have, Piece<DT>& out) {
+__device__ __forceinline__ void load_piece(const typename Elem<DT>::T* row, const Spot& s, int cols, bool vec, Piece<DT>& out) {
   using T = typename Elem<DT>::T;
-  if (RUNS && vec) {
+  T* t = reinterpret_cast<T*>(out.w);
+  if (!RUNS) {
 #pragma unroll
-    for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) *reinterpret_cast<uint4*>(out.w + 4 * i) = reinterpret_cast<const uint4*>(p)[i];
+    for (int j = 0; j < kRun; ++j) t[j] = s.side + 32 * j < cols ? row[s.side + 32 * j] : Elem<DT>::down(0.f);
+  } else if (vec) {
+#pragma unroll
+    for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) *reinterpret_cast<uint4*>(out.w + 4 * i) = reinterpret_cast<const uint4*>(row + s.col)[i];
   } else {
-    T* t = reinterpret_cast<T*>(out.w);
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) t[j] = j < have ? p[j * Spot<RUNS>::step()] : Elem<DT>::down(0.f);
+    for (int j = 0; j < kRun; ++j) t[j] = j < s.have ? row[s.col + j] : Elem<DT>::down(0.f);
   }
 }
-template <int DT>
-__device__ __forceinline__ void open_piece(const Piece<DT>& in, float (&v)[kRun]) {
-  const typename Elem<DT>::T* t = reinterpret_cast<const typename Elem<DT>::T*>(in.w);
+// The run as floats; `turn` is the warp's 256 elements of shared memory (unused with RUNS).
+template <int DT, bool RUNS>
+__device__ __forceinline__ void open_piece(const Piece<DT>& in, typename Elem<DT>::T* turn, float (&v)[kRun]) {
+  using T = typename Elem<DT>::T;
+  const T* t = reinterpret_cast<const T*>(in.w);
+  if (RUNS) {
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) v[j] = Elem<DT>::up(t[j]);
+    for (int j = 0; j < kRun; ++j) v[j] = Elem<DT>::up(t[j]);
+  } else {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) turn[32 * j + lane] = t[j];
+    __syncwarp();
+    load_run<DT, kRun>(turn + kRun * lane, true, kRun, v);
+    __syncwarp();
+  }
 }
 template <int DT, bool RUNS>
-__device__ __forceinline__ void store_piece(typename Elem<DT>::T* p, bool vec, int have, const float (&v)[kRun]) {
+__device__ __forceinline__ void store_piece(typename Elem<DT>::T* row, const Spot& s, int cols, bool vec, typename Elem<DT>::T* turn, const float (&v)[kRun]) {
   if (RUNS) {
-    store_run<DT, kRun>(p, vec, have, v);
+    store_run<DT, kRun>(row + s.col, vec, s.have, v);
   } else {
+    const int lane = threadIdx.x & 31;
+    store_run<DT, kRun>(turn + kRun * lane, true, kRun, v);
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
-      if (j < have) p[32 * j] = Elem<DT>::down(v[j]);
+      if (s.side + 32 * j < cols) row[s.side + 32 * j] = turn[32 * j + lane];
+    __syncwarp();
   }
 }
-template <bool RUNS>
 __device__ __forceinline__ void store_codes(uint8_t* p, bool vec, int have, uint2 w) {
-  if (RUNS && vec) {
+  if (vec) {
     *reinterpret_cast<uint2*>(p) = w;
   } else {
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
-      if (j < have) p[j * Spot<RUNS>::step()] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+      if (j < have) p[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
   }
 }
-template <bool RUNS>
 __device__ __forceinline__ uint2 load_codes(const uint8_t* p, bool vec, int have) {
-  if (RUNS && vec) return *reinterpret_cast<const uint2*>(p);
+  if (vec) return *reinterpret_cast<const uint2*>(p);
   uint2 w = make_uint2(0u, 0u);
 #pragma unroll
   for (int j = 0; j < kRun; ++j)
-    if (j < have) (j < 4 ? w.x : w.y) |= (uint32_t)p[j * Spot<RUNS>::step()] << (8 * (j & 3));
+    if (j < have) (j < 4 ? w.x : w.y) |= (uint32_t)p[j] << (8 * (j & 3));
   return w;
-}
-// The exponent bytes of a thread's columns: one for a run, eight (of consecutive groups) for strides.
-template <bool RUNS>
-__device__ __forceinline__ uint2 load_exps(const uint8_t* row, int col, int have) {
-  uint2 e = make_uint2(0u, 0u);
-  if (RUNS) {
-    e.x = row[col / kGroup];
-  } else {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j)
-      if (j < have) (j < 4 ? e.x : e.y) |= (uint32_t)row[col / kGroup + j] << (8 * (j & 3));
-  }
-  return e;
-}
-template <bool RUNS>
-__device__ __forceinline__ void decode_piece(uint2 w, uint2 e, float (&v)[kRun]) {
-  if (RUNS) {
-    decode_run(w, (int)e.x, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j)
-      v[j] = decode8((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255u, step_of((int)((j < 4 ? e.x : e.y) >> (8 * (j & 3)) & 255u)));
-  }
 }
 
 template <int DT, bool RUNS>
 __global__ void __launch_bounds__(kThreads)
 pack8_kernel(Deal d, const void* __restrict__ x, int64_t ld_x, bool vec_x, lqsgd_packed8 out, bool vec_c) {
   constexpr int kRows = DT == LQSGD_F32 ? 2 : 4;
-  train_pdl_wait();
   using T = typename Elem<DT>::T;
-  const Spot<RUNS> s(d);
+  __shared__ __align__(16) T turn[RUNS ? 1 : kWarps][RUNS ? 8 : 256];
+  train_pdl_wait();
+  const Spot s(d);
   const bool vx = vec_x && s.have == kRun, vc = vec_c && s.have == kRun;
-  // strides: a row's 256 codes pass through shared memory, where the lanes put them by columns and take them by runs
-  __shared__ __align__(8) uint8_t turn[RUNS ? 1 : kWarps][256];
-  uint8_t* mine_at = turn[RUNS ? 0 : threadIdx.x >> 5];
+  T* mine = turn[RUNS ? 0 : threadIdx.x >> 5];
   // a warp whose last rows lie past the end stays together for the shuffles: those lanes hold zeros and store nothing
   for (int64_t r0 = s.row; r0 - s.sub < s.row_end; r0 += kRows * s.row_step) {
     Piece<DT> raw[kRows];
@@ -171,45 +163,26 @@ pack8_kernel(Deal d, const void* __restrict__ x, int64_t ld_x, bool vec_x, lqsgd
       const int64_t r = r0 + u * s.row_step;
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(raw[u].w) / 4); ++i) raw[u].w[i] = 0u;
-      if (r < s.row_end && s.have > 0) load_piece<DT, RUNS>(static_cast<const T*>(x) + r * ld_x + s.col, vx, s.have, raw[u]);
+      if (r < s.row_end && (!RUNS || s.have > 0)) load_piece<DT, RUNS>(static_cast<const T*>(x) + r * ld_x, s, d.cols, vx, raw[u]);
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int64_t r = r0 + u * s.row_step;
       if (r - s.sub >= s.row_end) break;
-      const bool on = r < s.row_end && s.have > 0;
       float v[kRun];
-      open_piece<DT>(raw[u], v);
-      uint8_t* codes = out.dev_codes + r * out.ld_codes + s.col;
-      uint8_t* exps = out.dev_exps + r * out.ld_exps + s.col / kGroup;
-      if (RUNS) {
-        // magnitudes as bit patterns: their order is the values', and NaN comes out on top
-        uint32_t top = 0;
+      open_piece<DT, RUNS>(raw[u], mine, v);
+      // magnitudes as bit patterns: their order is the values', and NaN comes out on top
+      uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int eb = exp_byte(__uint_as_float(top));
-        const float inv = inv_step(eb);
-        if (on) {
-          store_codes<RUNS>(codes, vc, s.have, make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
-          if ((s.col & (kGroup - 1)) == 0) *exps = (uint8_t)eb;
-        }
-      } else {
-        const int lane = threadIdx.x & 31, seg = s.col - lane, run = seg + kRun * lane, have = min(kRun, d.cols - run);
-        uint32_t mine = 0;                                // lane j keeps the j-th group's byte
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-          const int eb = exp_byte(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v[j]) & 0x7fffffffu)));
-          if (lane == j) mine = (uint32_t)eb;
-          mine_at[32 * j + lane] = (uint8_t)((mag_bits(v[j], inv_step(eb)) & 127u) | ((__float_as_uint(v[j]) >> 24) & 128u));
-        }
-        __syncwarp();
-        const uint2 w = *reinterpret_cast<const uint2*>(mine_at + kRun * lane);
-        __syncwarp();
-        if (r < s.row_end && have > 0) store_codes<true>(out.dev_codes + r * out.ld_codes + run, vec_c && have == kRun, have, w);
-        // the segment's groups that exist: those whose first column, lane 0's, does
-        if (r < s.row_end && lane < kRun && s.col - lane + 32 * lane < d.cols) exps[lane] = (uint8_t)mine;
+      for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int eb = exp_byte(__uint_as_float(top));
+      const float inv = inv_step(eb);
+      if (r < s.row_end && s.have > 0) {
+        store_codes(out.dev_codes + r * out.ld_codes + s.col, vc, s.have,
+                    make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
+        if ((s.col & (kGroup - 1)) == 0) out.dev_exps[r * out.ld_exps + s.col / kGroup] = (uint8_t)eb;
       }
     }
   }
@@ -219,14 +192,12 @@ template <int DT, bool RUNS>
 __global__ void __launch_bounds__(kThreads)
 unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64_t ld_y, bool vec_y) {
   constexpr int kRows = 4;
-  train_pdl_wait();
   using T = typename Elem<DT>::T;
-  const Spot<RUNS> s(d);
-  // Codes are read by runs in either layout; with strides the values pass through shared memory to be stored by columns.
-  __shared__ __align__(16) T turn[RUNS ? 1 : kWarps][256];
-  const int lane = threadIdx.x & 31, run = RUNS ? s.col : s.col - lane + kRun * lane, have = min(kRun, d.cols - run);
-  if (RUNS && have <= 0) return;
-  const bool vy = vec_y && have == kRun, vc = vec_c && have == kRun;
+  __shared__ __align__(16) T turn[RUNS ? 1 : kWarps][RUNS ? 8 : 256];
+  train_pdl_wait();
+  const Spot s(d);
+  if (RUNS && s.have <= 0) return;
+  const bool vy = vec_y && s.have == kRun, vc = vec_c && s.have == kRun;
   for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
     uint2 w[kRows];
     int e[kRows];
@@ -235,9 +206,9 @@ unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64
       const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
       w[u] = make_uint2(0u, 0u);
       e[u] = kExpBias;
-      if (have > 0) {
-        w[u] = load_codes<true>(in.dev_codes + r * in.ld_codes + run, vc, have);
-        e[u] = in.dev_exps[r * in.ld_exps + run / kGroup];
+      if (s.have > 0) {
+        w[u] = load_codes(in.dev_codes + r * in.ld_codes + s.col, vc, s.have);
+        e[u] = in.dev_exps[r * in.ld_exps + s.col / kGroup];
       }
     }
 #pragma unroll
@@ -253,18 +224,7 @@ unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64
         for (int j = 0; j < kRun; ++j)
           if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
       }
-      if (RUNS) {
-        store_run<DT, kRun>(static_cast<T*>(y) + r * ld_y + run, vy, have, v);
-      } else {
-        T* row = turn[threadIdx.x >> 5];
-        store_run<DT, kRun>(row + kRun * lane, true, kRun, v);
-        __syncwarp();
-        T* to = static_cast<T*>(y) + r * ld_y + s.col;
-#pragma unroll
-        for (int j = 0; j < kRun; ++j)
-          if (j < s.have) to[32 * j] = row[32 * j + lane];
-        __syncwarp();
-      }
+      store_piece<DT, RUNS>(static_cast<T*>(y) + r * ld_y, s, d.cols, vy, turn[RUNS ? 0 : threadIdx.x >> 5], v);
     }
   }
 }
@@ -272,26 +232,25 @@ unpack8_kernel(Deal d, lqsgd_packed8 in, bool vec_c, void* __restrict__ y, int64
 // dz = dy act'(z); the block's column sums of dz go to partial[blockIdx.y][cols].
 // GELU's and SiLU's slopes cost 20 to 30 instructions, more than HBM leaves time for.  But z takes few values: 128 magnitudes
 // times a step, and both slopes satisfy s(-z) = 1 - s(z).  So a block that has work enough first tabulates the slopes for the
-// steps 2^-16 .. 2^4; below them the slope is 1/2 + s'(0) z to 2^-31, above them 0 or 1 (or 1/2 at 0) to 2^-23: those, and
-// blocks with little work, compute them.
+// steps 2^-16 .. 2^4; groups with other steps, and blocks with little work, compute them.
 // Rows in flight per thread and blocks per SM, measured on 8192 x 16384 in bf16: without z, one row and six blocks (48 us; two
 // rows 72); with z, four rows and three blocks (gelu 122 us, two rows and four blocks 148, one and six 142).
-template <int DT, int KIND>
+template <int DT, bool RUNS, int KIND>
 struct SumShape {
-  static constexpr int kRows = KIND == 0 ? 1 : (DT == LQSGD_F32 ? 2 : 4);
+  static constexpr int kRows = KIND == 0 ? 1 : (DT == LQSGD_F32 || !RUNS ? 2 : 4);
   static constexpr int kBlocks = KIND == 0 ? 6 : 3;
 };
 enum SlopeKind { kSlopeNone = 0, kSlopeRelu = 1, kSlopeCurve = 2 };
 constexpr int kTabLow = kExpBias - 16, kTabSteps = 21;
 template <int DT, bool RUNS, int KIND>
-__global__ void __launch_bounds__(kThreads, SumShape<DT, KIND>::kBlocks)
+__global__ void __launch_bounds__(kThreads, SumShape<DT, RUNS, KIND>::kBlocks)
 act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed8 z8, bool vec_c, int act, bool table,
                 void* dz, int64_t ld_dz, bool vec_dz, float* __restrict__ partial) {
-  constexpr int kRows = SumShape<DT, KIND>::kRows;
+  constexpr int kRows = SumShape<DT, RUNS, KIND>::kRows;
   using T = typename Elem<DT>::T;
   __shared__ float tab[KIND == kSlopeCurve ? kTabSteps * 128 : 1];
-  __shared__ float sums[kWarps][32][kRun + 1];
-  const Spot<RUNS> s(d);
+  __shared__ __align__(16) float sums[kWarps][32][kRun + 1];
+  const Spot s(d);
   if (KIND == kSlopeCurve && table) {
     for (int i = threadIdx.x; i < kTabSteps * 128; i += kThreads) {
       const float z = (float)(i & 127) * step_of(kTabLow + (i >> 7));
@@ -300,56 +259,54 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
     __syncthreads();
   }
   train_pdl_wait();
+  // the warp's place for turning rows is the one that its sums take at the end
+  T* turn = reinterpret_cast<T*>(&sums[threadIdx.x >> 5][0][0]);
   const bool vg = vec_dy && s.have == kRun, vz = vec_dz && s.have == kRun, vc = vec_c && s.have == kRun;
   float acc[kRun];
 #pragma unroll
   for (int j = 0; j < kRun; ++j) acc[j] = 0.f;
-  if (s.have > 0)
+  if (!RUNS || s.have > 0)
     for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
       Piece<DT> raw[kRows];
-      uint2 w[kRows], e[kRows];
+      uint2 w[kRows];
+      uint32_t e[kRows];
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
-        load_piece<DT, RUNS>(static_cast<const T*>(dy) + r * ld_dy + s.col, vg, s.have, raw[u]);
-        if (KIND != kSlopeNone) {
-          w[u] = load_codes<RUNS>(z8.dev_codes + r * z8.ld_codes + s.col, vc, s.have);
-          e[u] = load_exps<RUNS>(z8.dev_exps + r * z8.ld_exps, s.col, s.have);
+        load_piece<DT, RUNS>(static_cast<const T*>(dy) + r * ld_dy, s, d.cols, vg, raw[u]);
+        w[u] = make_uint2(0u, 0u);
+        e[u] = kExpBias;
+        if (KIND != kSlopeNone && s.have > 0) {
+          w[u] = load_codes(z8.dev_codes + r * z8.ld_codes + s.col, vc, s.have);
+          e[u] = z8.dev_exps[r * z8.ld_exps + s.col / kGroup];
         }
       }
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int64_t r = r0 + u * s.row_step;
         if (r >= s.row_end) break;
-        float g[kRun], z[kRun];
-        open_piece<DT>(raw[u], g);
+        float g[kRun];
+        open_piece<DT, RUNS>(raw[u], turn, g);
         if (KIND == kSlopeRelu) {
           // 1 for a positive value, 0 for the others, NaN for a group that is not finite
+          const float one = e[u] == kExpNonFinite ? step_of(kExpNonFinite) : 1.f, none = one - one;
 #pragma unroll
           for (int j = 0; j < kRun; ++j) {
             const uint32_t c = (j < 4 ? w[u].x : w[u].y) >> (8 * (j & 3)) & 255u;
-            const uint32_t eb = RUNS ? e[u].x : (j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u;
-            const float one = c - 1u < 127u ? 1.f : 0.f;                // 1 .. 127
-            g[j] *= eb == kExpNonFinite ? step_of(kExpNonFinite) : one;
+            g[j] *= c - 1u < 127u ? one : none;
           }
         } else if (KIND == kSlopeCurve) {
-          bool quick = table;
-          if (RUNS) {
-            quick = quick && e[u].x - kTabLow < (uint32_t)kTabSteps;
-          } else {
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) quick = quick && (j >= s.have || ((j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u) - kTabLow < (uint32_t)kTabSteps);
-          }
-          if (quick) {
+          if (table && e[u] - kTabLow < (uint32_t)kTabSteps) {
+            const float* row = tab + (e[u] - kTabLow) * 128;
 #pragma unroll
             for (int j = 0; j < kRun; ++j) {
               const uint32_t c = (j < 4 ? w[u].x : w[u].y) >> (8 * (j & 3));
-              const uint32_t eb = RUNS ? e[u].x : (j < s.have ? (j < 4 ? e[u].x : e[u].y) >> (8 * (j & 3)) & 255u : (uint32_t)kTabLow);
-              const float t = tab[(eb - kTabLow) * 128 + (c & 127u)];
+              const float t = row[c & 127u];
               g[j] *= c & 128u ? 1.f - t : t;
             }
           } else {
-            decode_piece<RUNS>(w[u], e[u], z);
+            float z[kRun];
+            decode_run(w[u], (int)e[u], z);
             if (act == LQSGD_ACT_GELU) {
 #pragma unroll
               for (int j = 0; j < kRun; ++j) g[j] *= act_slope<LQSGD_ACT_GELU>(z[j]);
@@ -359,13 +316,14 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
             }
           }
         }
-        if (dz) store_piece<DT, RUNS>(static_cast<T*>(dz) + r * ld_dz + s.col, vz, s.have, g);
+        if (dz) store_piece<DT, RUNS>(static_cast<T*>(dz) + r * ld_dz, s, d.cols, vz, turn, g);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) acc[j] += g[j];
       }
     }
   if (!partial) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncwarp();
 #pragma unroll
   for (int j = 0; j < kRun; ++j) sums[warp][lane][j] = acc[j];
   __syncthreads();
@@ -374,10 +332,9 @@ act_grad_kernel(Deal d, const void* dy, int64_t ld_dy, bool vec_dy, lqsgd_packed
     const int col = (int)blockIdx.x * (warp_cols << d.wide_shift) + c;
     if (col >= d.cols) continue;
     const int beside = c / warp_cols, in = c - beside * warp_cols;
-    const int from = RUNS ? in / kRun : in & 31, j = RUNS ? in % kRun : in >> 5;
     float t = 0.f;
     for (int w = beside; w < kWarps; w += 1 << d.wide_shift)
-      for (int sub = 0; sub < (32 >> d.lane_shift); ++sub) t += sums[w][(sub << d.lane_shift) + from][j];
+      for (int sub = 0; sub < (32 >> d.lane_shift); ++sub) t += sums[w][(sub << d.lane_shift) + in / kRun][in % kRun];
     partial[(size_t)blockIdx.y * d.cols + col] = t;
   }
 }
@@ -438,7 +395,7 @@ extern "C" int lqsgd_pack8(const void* dev_x, int64_t ld_x, int32_t dtype, int64
   const int es = train_elem(dtype);
   if (!train_aligned(dev_x, es)) return LQSGD_ERR_MISALIGNED;
   const bool vx = vec_rows(dev_x, ld_x, es, 16), vc = vec_rows(host_out->dev_codes, host_out->ld_codes, 1, 8);
-  const bool runs = use_runs(vx, vc, true, cols);
+  const bool runs = use_runs(vx, cols);
   dim3 grid;
   const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
   TRAIN_CK(BY_DTYPE(dtype, runs, pack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, dev_x, ld_x, vx, *host_out, vc), "pack8_kernel launch");
@@ -456,7 +413,7 @@ extern "C" int lqsgd_unpack8(const lqsgd_packed8* host_in, int64_t rows, int32_t
   const int es = train_elem(dtype);
   if (!train_aligned(dev_y, es)) return LQSGD_ERR_MISALIGNED;
   const bool vy = vec_rows(dev_y, ld_y, es, 16), vc = vec_rows(host_in->dev_codes, host_in->ld_codes, 1, 8);
-  const bool runs = use_runs(vy, vc, true, cols);
+  const bool runs = use_runs(vy, cols);
   dim3 grid;
   const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
   TRAIN_CK(BY_DTYPE(dtype, runs, unpack8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, *host_in, vc, dev_y, ld_y, vy), "unpack8_kernel launch");
@@ -515,7 +472,7 @@ extern "C" int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_pac
   if (!train_aligned(dev_dy, es) || !train_aligned(dev_dz, es)) return LQSGD_ERR_MISALIGNED;
   const bool vg = vec_rows(dev_dy, ld_dy, es, 16), vz = !dev_dz || vec_rows(dev_dz, ld_dz, es, 16),
              vc = act == LQSGD_ACT_NONE || vec_rows(z8.dev_codes, z8.ld_codes, 1, 8);
-  const bool runs = use_runs(vg, vz, vc, cols);
+  const bool runs = use_runs(vg && vz, cols);
   dim3 grid;
   const Deal d = deal_sums(rows, cols, runs, &grid);
   float* partial = dev_db;

@@ -819,11 +819,14 @@ bool plan_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
       const int64_t ctas = (int64_t)d.n * r.blocks * parts;
       if (ctas > 0x7fffffff) return false;
       const int per_sm = (int)std::min<size_t>(4, 226 * 1024 / (smem + 1024));
-      // What was measured: 6 ns per CTA whatever it holds (9 where CTAs meet), 0.9 ns per 1000 values while at least three
-      // CTAs overlap on an SM, up to 1.5 times that with one; and the last round of CTAs is paid in full.
+      // Fitted to the times of five shapes, forward and backward, over all these choices: 6 ns per CTA whatever it holds (9
+      // where CTAs meet), 0.9 ns per 1000 values while four CTAs overlap on an SM, up to 1.9 times that with one, and a part of
+      // what the last round of CTAs leaves idle.  (512 threads per CTA, or CTAs that walk over units with the next
+      // one's copies under way, were built and were never the fastest.)
       const double values = (double)d.n * d.hw * d.c, wave = 148.0 * per_sm, full = std::ceil(ctas / wave) * wave / ctas;
       const double idle = (double)((1 << r.lane_shift) * kRun * r.blocks) / d.c;
-      const double score = ctas * (parts > 1 ? 9e-3 : 6e-3) + values * 0.9e-6 * (per_sm == 1 ? 1.5 : per_sm == 2 ? 1.1 : 1.0) * std::min(full, 2.0) * idle;
+      const double slow = per_sm == 1 ? 1.9 : per_sm == 2 ? 1.45 : per_sm == 3 ? 1.05 : 1.0;
+      const double score = ctas * (parts > 1 ? 9e-3 : 6e-3) + values * 0.9e-6 * slow * (1 + 0.3 * std::min(full - 1, 2.0)) * idle;
       if (score < best_score) { best_score = score; best = r; }
     }
     if (last) break;
