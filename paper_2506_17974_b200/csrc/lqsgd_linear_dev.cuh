@@ -15,7 +15,7 @@
 //
 // A cluster of CG CTAs (1 or 2) works on a tile of 128 CG x BN: with CG = 2 each SM holds 128 rows of A and half of B's, and
 // one tcgen05.mma.cta_group::2 drives both tensor cores, so that an SM fetches (128 + BN / 2) rows per k instead of
-// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 (4-7 for a weight gradient) drain the
+// 128 + BN.  Per CTA: warp 0 issues the TMA loads, warp 1 (of the cluster's first CTA) the MMAs, warps 4-11 drain the
 // accumulator (two of them, so that the next tile's sum runs under the epilogue).  Clusters walk
 // the work items (tile, piece of the sum) with a fixed stride.
 //
@@ -170,6 +170,17 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&f)[16]) {
+  uint32_t v[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
+}
+
 // ---- 16-bit words of either operand type
 __device__ __forceinline__ uint32_t pack2(int dtype, float lo, float hi) {
   if (dtype == LQSGD_BF16) {
@@ -222,46 +233,26 @@ __device__ __forceinline__ void put_packed(const lqsgd_packed8& p, bool vec, int
   p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
 }
 
-// Epilogues of a 32 x 32 piece held by a warp, a row per thread (on: the row exists; row0: lane 0's row): a weight gradient, ...
-// Rows that are not 32-byte aligned go through the warp's scratch in shared memory, so that a warp's access is one row's
-// 32 columns instead of one column of 32 rows (which costs a sector per element).
-constexpr int kScratchPitch = 33;                      // words; odd, so neither rows nor columns meet on one bank
-constexpr uint32_t kScratchBytes = 32 * kScratchPitch * 4, kScratchBytes16 = 32 * 34 * 2;
-__device__ __forceinline__ void finish_rows_f32(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], float* scratch) {
-  const int lane = threadIdx.x & 31;
-  const int have = min(32, e.cols - col);
-  if (e.vec_out && have == 32) {
-    if (!on) return;
-    float* o = static_cast<float*>(e.out) + (row0 + lane) * e.ld_out + col;
+// Epilogue of 8 columns of a weight gradient held by a warp, a row per thread (row0: lane 0's row), where rows are not 32-byte
+// aligned or the tile passes the matrix: through the warp's scratch in shared memory (rows of 9 words), so that an access is
+// four rows' 8 columns instead of one column of 32 rows (which costs a sector per element).
+__device__ __forceinline__ void finish_ragged_f32(const LinEpilogue& e, int64_t row0, int col, const float* v, float* scratch) {
+  const int lane = threadIdx.x & 31, c = lane & 7;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t w[8];
-      if (e.accumulate) {
-        ld_global_32(o + 8 * i, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[8 * i + j] += __uint_as_float(w[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
-      st_global_32(o + 8 * i, w);
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 32; ++i) scratch[lane * kScratchPitch + i] = v[i];
+  for (int i = 0; i < 8; ++i) scratch[lane * 9 + i] = v[i];
   __syncwarp();
   const int rows = (int)min((int64_t)32, e.rows - row0);
-  float* o = static_cast<float*>(e.out) + row0 * e.ld_out + col + lane;
-  if (lane < have) {
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-      const float t = scratch[r * kScratchPitch + lane];
+  float* o = static_cast<float*>(e.out) + row0 * e.ld_out + col + c;
+  if (col + c < e.cols) {
+#pragma unroll 2
+    for (int r = lane >> 3; r < rows; r += 4) {
+      const float t = scratch[r * 9 + c];
       o[r * e.ld_out] = e.accumulate ? o[r * e.ld_out] + t : t;
     }
   }
   __syncwarp();
 }
-// ... or a layer's output.
+// Epilogue of a 32 x 32 piece of a layer's output.
 __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], float* scratch) {
   const int lane = threadIdx.x & 31;
   const int have = min(32, e.cols - col);
@@ -515,11 +506,15 @@ struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
   static constexpr uint32_t kStage = kABytes + ((kBBytes + 1023) / 1024 * 1024);
-  // Two warps per quarter of tensor memory where the epilogue computes per value (GELU and the 8-bit form take as
-  // long as the product of a 4096-wide layer with one).
-  static constexpr int kEpiWarps = WF32 ? 4 : 8;
+  // Two warps per quarter of tensor memory: GELU and the 8-bit form take as long as the product of a 4096-wide layer with one.
+  static constexpr int kEpiWarps = 8;
+  // A weight gradient is a sum over thousands of rows, and the tensor core's accumulator loses a little at every step (K = 16)
+  // that it adds.  So it takes kChunk k blocks at a time, and the epilogue warps add these sums up in registers, rounding to
+  // nearest.
+  static constexpr int kChunk = WF32 ? 32 : 1 << 30;
+  static constexpr int kMine = BN / (kEpiWarps / 4);                      // columns per epilogue warp
   static constexpr int kThreads = (4 + kEpiWarps) * 32;
-  static constexpr uint32_t kScratch = WF32 ? 4 * kScratchBytes : 8 * kScratchBytes16;   // one per epilogue warp
+  static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2, kScratch = kEpiWarps * kScratchWarp;
   static constexpr uint32_t kRoom = 225u * 1024 - kScratch;
   static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
   static constexpr int kTmemCols = 2 * BN;
@@ -638,28 +633,34 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       bool ok = true;
       LinWalk w(p, cluster, clusters, part_of);
       for (; !w.done() && ok; w.next_tile(p)) {
-        if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
-        lin_fence_after();
-        const uint32_t d = tmem + db * BN;
-        uint32_t more = 0;                          // the tile's first product starts the sum
+        uint32_t left = 0, d = 0, more = 0;         // k blocks until the accumulator changes; its first product starts the sum
         for (int kb = w.kb; kb < w.kb_end; ++kb) {
+          if (left == 0) {
+            if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
+            lin_fence_after();
+            d = tmem + db * BN;
+            left = min(S::kChunk, w.kb_end - kb);
+            more = 0;
+          }
           if (!lin_wait_all(full_s + 8 * s, full + s, turn, abort_flag)) { ok = false; break; }
           lin_fence_after();
           const uint64_t ad = ad0 + (uint64_t)(s * (S::kStage >> 4)), bd = bd0 + (uint64_t)(s * (S::kStage >> 4));
+          --left;
           if (elect_one()) {
 #pragma unroll
             for (int ks = 0; ks < kLinBK / 16; ++ks)
               lin_mma<CG>(d, ad + ((ks * lin_kstep<OA != kOpK>()) >> 4), bd + ((ks * lin_kstep<OB != kOpK>()) >> 4), idesc, ks > 0 ? 1u : more);
             lin_commit<CG>(empty_s + 8 * s);
+            if (left == 0) lin_commit<CG>(d_full_s + 8 * db);
           }
           __syncwarp();
           more = 1;
           if (++s == S::kStages) { s = 0; turn ^= 1; }
+          if (left == 0) {
+            db ^= 1;
+            if (db == 0) dturn ^= 1;
+          }
         }
-        if (ok && elect_one()) lin_commit<CG>(d_full_s + 8 * db);
-        __syncwarp();
-        db ^= 1;
-        if (db == 0) dturn ^= 1;
       }
       if (elect_one()) lin_commit<CG>(smem_u32(fin));   // every MMA has completed before tensor memory is released
       __syncwarp();
@@ -671,63 +672,133 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     __syncwarp();
   } else if (warp >= 4) {
     // ---- epilogue: a warp reads its quarter of the accumulator's rows (warp % 4), and with eight warps half of its columns
-    uint32_t seq = 0;
-    const int q = warp & 3;
+    uint32_t seq = 0;                                                     // accumulators taken so far
+    bool ok = true;
+    const int q = warp & 3, c0 = ((warp - 4) >> 2) * S::kMine;
+    float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * S::kScratchWarp);
     LinWalk w(p, cluster, clusters, part_of);
     train_pdl_wait();
-    for (; !w.done(); w.next_tile(p), ++seq) {
-      const uint32_t db = seq & 1;
-      if (!lin_wait_warp(d_full + db, (seq >> 1) & 1, abort_flag, lane)) break;
-      lin_fence_after();
-      const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + db * BN;
-      const int m = (w.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane;
-      const int n0 = w.n_tile * BN;
-      if (CG == 1 && meet > 1) {                  // every CTA's MMAs are done with the stages that the sums go to
-        cluster_sync_all();
-        met = true;
-      }
+    for (; !w.done(); w.next_tile(p)) {
+      const int m = (w.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane, n0 = w.n_tile * BN;
       const int piece = w.piece(p);
       float* part = piece >= 0 ? p.partial + (int64_t)piece * (CG * kLinBM * BN) : nullptr;
-      constexpr int kStep = 32, kMine = BN / (S::kEpiWarps / 4);
-      const int c0 = ((warp - 4) >> 2) * kMine;
-      float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * (WF32 ? kScratchBytes : kScratchBytes16));
+      // waits for the next accumulator; its columns c0.. for this warp's rows
+      auto open = [&]() -> uint32_t {
+        const uint32_t db = seq & 1;
+        if (!lin_wait_warp(d_full + db, (seq >> 1) & 1, abort_flag, lane)) ok = false;
+        lin_fence_after();
+        return tmem + ((uint32_t)(32 * q) << 16) + db * BN + c0;
+      };
+      auto hand_back = [&]() {                        // the accumulator is in registers
+        const uint32_t db = seq & 1;
+        lin_fence_before();
+        __syncwarp();
+        if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
+        ++seq;
+      };
+      float* to_slice = nullptr;                      // the sums meet: this row's place in shared memory, and whose it is
+      int to = 0;
+      if (CG == 1 && meet > 1) {
+        const int r = 32 * q + lane, slice = meet_slice(p, w, meet);
+        to = min((int)quick_div(r, slice), meet - 1);
+        to_slice = reinterpret_cast<float*>(base) + (part_of * slice + r - to * slice) * S::kMeetPitch;
+      }
+      auto meet_first = [&]() {                       // every CTA's MMAs are done with the stages that the sums go to
+        if (CG == 1 && meet > 1) {
+          cluster_sync_all();
+          met = true;
+        }
+      };
+      if constexpr (WF32) {
+        float acc[S::kMine];
+#pragma unroll
+        for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
+        const int chunks = (w.kb_end - w.kb + S::kChunk - 1) / S::kChunk;
 #pragma unroll 1
-      for (int c = c0; c < c0 + kMine; c += kStep) {
-        float v[32];
-        tmem_ld32(taddr + c, v);
-        if (c + kStep >= c0 + kMine) {            // the accumulator is in registers: hand it back
-          lin_fence_before();
-          __syncwarp();
-          if (lane == 0) { if constexpr (CG == 2) arrive_at(map_to(d_empty + db, 0)); else mbar_arrive(d_empty + db); }
-        }
-        if (CG == 1 && meet > 1) {                // to the CTA whose slice the row is in, for this CTA's place there
-          const int r = 32 * q + lane, slice = meet_slice(p, w, meet), to = min((int)quick_div(r, slice), meet - 1);
-          if (m >= p.M) continue;
-          const uint32_t o = map_to(reinterpret_cast<float*>(base) + (part_of * slice + r - to * slice) * S::kMeetPitch + c, to);
+        for (int k = 0; k < chunks; ++k) {
+          const uint32_t taddr = open();
+          if (!ok) break;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(o + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
-          continue;
-        }
-        if (n0 + c >= p.N || m - lane >= p.M) continue;
-        if (part) {                               // [row of the tile][BN]
-          float* o = part + (int64_t)((int)rank * kLinBM + 32 * q + lane) * BN + c;
+          for (int c = 0; c < S::kMine; c += 16) {
+            float v[16];
+            tmem_ld16(taddr + c, v);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t u[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
-            st_global_32(o + 8 * i, u);
+            for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
           }
-        } else if constexpr (WF32) {
-          finish_rows_f32(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
-        } else {
-          finish_rows(p.ep, m - lane, n0 + c, m < p.M, v, scratch);
+          hand_back();
+        }
+        if (!ok) break;
+        meet_first();
+        if (CG == 1 && meet > 1) {
+          if (m < p.M) {
+            const uint32_t o = map_to(to_slice + c0, to);
+#pragma unroll
+            for (int c = 0; c < S::kMine; c += 4)
+              asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                           ::"r"(o + 4 * c), "f"(acc[c]), "f"(acc[c + 1]), "f"(acc[c + 2]), "f"(acc[c + 3]) : "memory");
+          }
+        } else if (part || (p.ep.vec_out && n0 + c0 + S::kMine <= p.N)) {
+          const bool add = !part && p.ep.accumulate;
+          float* o = part ? part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0            // [row of the tile][BN]
+                          : static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
+          if (m < p.M) {
+#pragma unroll
+            for (int c = 0; c < S::kMine; c += 8) {
+              uint32_t u[8];
+              if (add) {
+                ld_global_32(o + c, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
+              st_global_32(o + c, u);
+            }
+          }
+        } else if (m - lane < p.M) {
+#pragma unroll
+          for (int c = 0; c < S::kMine; c += 8)
+            if (n0 + c0 + c < p.N) finish_ragged_f32(p.ep, m - lane, n0 + c0 + c, acc + c, scratch);
+        }
+        __syncwarp();
+      } else {
+        const uint32_t taddr = open();
+        if (!ok) break;
+        meet_first();
+#pragma unroll 1
+        for (int c = 0; c < S::kMine; c += 32) {
+          float v[32];
+          tmem_ld32(taddr + c, v);
+          if (c + 32 >= S::kMine) hand_back();
+          if (CG == 1 && meet > 1) {
+            if (m < p.M) {
+              const uint32_t o = map_to(to_slice + c0 + c, to);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                             ::"r"(o + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
+            }
+            __syncwarp();
+            continue;
+          }
+          if (n0 + c0 + c >= p.N || m - lane >= p.M) continue;
+          if (part) {
+            float* o = part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0 + c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t u[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
+              st_global_32(o + 8 * i, u);
+            }
+          } else {
+            finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, scratch);
+          }
         }
       }
     }
   }
+  __syncwarp();
   if (CG == 1 && meet > 1 && !met) cluster_sync_all();
   lin_fence_before();
   __syncthreads();

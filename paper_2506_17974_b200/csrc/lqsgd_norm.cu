@@ -3,9 +3,10 @@
 // A thread owns 8 consecutive channels (16 bytes of a 16-bit type) and walks over pixels; what it sums stays in its registers
 // per channel, so groups of any width need no special case.  What bounds it is HBM: every tensor should be read once.
 //
-// Resident kernels (rows of 16-byte pieces, slices that fit): a cluster of 1 .. 8 CTAs takes one sample's block of whole groups
+// Resident kernels (channels a multiple of 8, slices that fit): a cluster of 1 .. 8 CTAs takes one sample's block of whole groups
 // (at least 64 bytes of a pixel), each CTA a range of its pixels, and brings it into shared memory with asynchronous
-// copies of 16 bytes (no registers are held meanwhile, so the whole slice is in flight at once).  Sums meet through
+// copies of 16 bytes (no registers are held meanwhile, so the whole slice is in flight at once; rows without 16-byte pieces
+// are read element by element).  Sums meet through
 // distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
 //
 // Streaming kernels (everything else): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
@@ -505,6 +506,69 @@ struct Groups {
   static __device__ __forceinline__ constexpr int of(int j) { return ONE ? 0 : j; }
 };
 
+// Brings a thread's `count` pieces (8 elements, `hop` elements apart) to shared memory, `step` bytes apart; the copies are on
+// their way when it returns, except those of rows without 16-byte pieces, which go through registers.
+template <typename T>
+__device__ __forceinline__ void fetch_pieces(uint8_t* to, int step, const T* src, int64_t hop, int count, bool vec) {
+  if (vec) {
+#pragma unroll 4
+    for (int k = 0; k < count; ++k, src += hop, to += step) {
+#pragma unroll
+      for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) copy_async<16>(to + 16 * i, reinterpret_cast<const uint8_t*>(src) + 16 * i);
+    }
+  } else {
+#pragma unroll 2
+    for (int k = 0; k < count; ++k, src += hop, to += step) {
+      __align__(16) T t[kRun];
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) t[j] = src[j];
+#pragma unroll
+      for (int i = 0; i < kRun * (int)sizeof(T) / 16; ++i) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(t)[i];
+    }
+  }
+}
+// Stores a run and leaves in v what a reader of it sees.
+template <int DT>
+__device__ __forceinline__ void store_rounded(typename Elem<DT>::T* p, bool vec, float (&v)[kRun]) {
+  if constexpr (DT == LQSGD_F32) {
+    store_run<DT, kRun>(p, vec, kRun, v);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_pair<DT>(v[2 * i], v[2 * i + 1]);
+    if (vec) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      uint16_t* h = reinterpret_cast<uint16_t*>(p);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) h[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 t = open_pair<DT>(w[i]); v[2 * i] = t.x; v[2 * i + 1] = t.y; }
+  }
+}
+// pack_run for whole runs.
+__device__ __forceinline__ void pack_whole(const lqsgd_packed8& out, bool vec, int64_t row, int col, bool on, const float (&v)[kRun]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  if (!on) top = 0;
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  if (!on) return;
+  const int eb = exp_byte(__uint_as_float(top));
+  const float inv = inv_step(eb);
+  const uint2 w = make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv));
+  uint8_t* p = out.dev_codes + row * out.ld_codes + col;
+  if (vec) {
+    *reinterpret_cast<uint2*>(p) = w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) p[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+  }
+  if ((col & (kGroup - 1)) == 0) out.dev_exps[row * out.ld_exps + col / kGroup] = (uint8_t)eb;
+}
+
 template <int DT, bool ONE>
 __global__ void __launch_bounds__(kResThreads, ONE ? 4 : 3)
 norm_resident_kernel(Resident r) {
@@ -524,14 +588,8 @@ norm_resident_kernel(Resident r) {
   uint8_t* own = data + threadIdx.x * kBytes;
   train_pdl_wait();
   {
-    const uint8_t* src = reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col);
-    const int64_t hop = q.row_step * d.ld_x * (int64_t)sizeof(T);
-    uint32_t to = smem_at(own);
-#pragma unroll 4
-    for (int k = 0; k < count; ++k, src += hop, to += kStep) {
-#pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16 * i), "l"(src + 16 * i) : "memory");
-    }
+    const T* src = static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col;
+    fetch_pieces<T>(own, kStep, src, q.row_step * d.ld_x, count, d.vec_x);
   }
   const G at(q.col - q.c0, d.cpg);
   float gamma[kRun], beta[kRun];
@@ -605,7 +663,7 @@ norm_resident_kernel(Resident r) {
         unpack_run<DT>(own + k * kStep, v);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) v[j] = act_value<decltype(tag)::value>(fmaf(v[j] - m[G::of(j)], gamma[j], beta[j]));
-        store_run<DT, kRun>(dst, true, kRun, v);
+        store_run<DT, kRun>(dst, d.vec_out, kRun, v);
       }
     });
   } else {
@@ -616,17 +674,13 @@ norm_resident_kernel(Resident r) {
         const bool on = k < count;
         const int64_t row = (int64_t)q.sample * d.hw + q.first + p;
         if (on) unpack_run<DT>(own + k * kStep, v);
-        if (d.x8.dev_codes) pack_run(d.x8, d.vec_x8, row, q.col, kRun, on, v);
+        if (d.x8.dev_codes) pack_whole(d.x8, d.vec_x8, row, q.col, on, v);
         if (on) {
 #pragma unroll
           for (int j = 0; j < kRun; ++j) v[j] = act_value<decltype(tag)::value>(fmaf(v[j] - m[G::of(j)], gamma[j], beta[j]));
-          store_run<DT, kRun>(dst, true, kRun, v);
+          store_rounded<DT>(dst, d.vec_out, v);
         }
-        if (d.y8.dev_codes) {
-#pragma unroll
-          for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
-          pack_run(d.y8, d.vec_y8, row, q.col, kRun, on, v);
-        }
+        if (d.y8.dev_codes) pack_whole(d.y8, d.vec_y8, row, q.col, on, v);
       }
     });
   }
@@ -657,20 +711,25 @@ norm_grad_resident_kernel(Resident r) {
   train_pdl_wait();
   const int64_t row0 = (int64_t)q.sample * d.hw + q.first + q.row;
   {
-    const uint8_t* gsrc = reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.dy) + q.sample * d.sample_dy + (int64_t)(q.first + q.row) * d.ld_dy + q.col);
-    const uint8_t* xsrc = KEPT ? d.x8.dev_codes + row0 * d.x8.ld_codes + q.col
-                               : reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col);
-    const int64_t ghop = q.row_step * d.ld_dy * (int64_t)sizeof(T), xhop = KEPT ? q.row_step * d.x8.ld_codes : q.row_step * d.ld_x * (int64_t)sizeof(T);
+    fetch_pieces<T>(gown, kResThreads * kDy, static_cast<const T*>(d.dy) + q.sample * d.sample_dy + (int64_t)(q.first + q.row) * d.ld_dy + q.col,
+                    q.row_step * d.ld_dy, count, d.vec_dy);
+    if constexpr (KEPT) {
+      const uint8_t* src = d.x8.dev_codes + row0 * d.x8.ld_codes + q.col;
+      const int64_t hop = q.row_step * d.x8.ld_codes;
+      if (d.vec_x8) {
 #pragma unroll 4
-    for (int k = 0; k < count; ++k, gsrc += ghop, xsrc += xhop) {
-#pragma unroll
-      for (int i = 0; i < kDy / 16; ++i) copy_async<16>(gown + k * (kResThreads * kDy) + 16 * i, gsrc + 16 * i);
-      if constexpr (KEPT) {
-        copy_async<8>(xown + k * (kResThreads * kX), xsrc);
+        for (int k = 0; k < count; ++k) copy_async<8>(xown + k * (kResThreads * kX), src + k * hop);
       } else {
+        for (int k = 0; k < count; ++k) {
+          uint2 w = make_uint2(0u, 0u);
 #pragma unroll
-        for (int i = 0; i < kX / 16; ++i) copy_async<16>(xown + k * (kResThreads * kX) + 16 * i, xsrc + 16 * i);
+          for (int j = 0; j < kRun; ++j) (j < 4 ? w.x : w.y) |= (uint32_t)src[k * hop + j] << (8 * (j & 3));
+          *reinterpret_cast<uint2*>(xown + k * (kResThreads * kX)) = w;
+        }
       }
+    } else {
+      fetch_pieces<T>(xown, kResThreads * kX, static_cast<const T*>(d.x) + q.sample * d.sample_x + (int64_t)(q.first + q.row) * d.ld_x + q.col,
+                      q.row_step * d.ld_x, count, d.vec_x);
     }
     if constexpr (KEPT) {
       const uint8_t* esrc = d.x8.dev_exps + row0 * d.x8.ld_exps + q.col / kGroup;
@@ -750,7 +809,7 @@ norm_grad_resident_kernel(Resident r) {
       piece(tag, k, e, dh);
 #pragma unroll
       for (int j = 0; j < kRun; ++j) e[j] = fmaf(dh[j], f[j], fmaf(e[j], c1[G::of(j)], c0[G::of(j)]));
-      store_run<DT, kRun>(to, true, kRun, e);
+      store_run<DT, kRun>(to, d.vec_out, kRun, e);
     }
   });
   if (r.parts > 1) norm_cluster_sync();
@@ -875,13 +934,12 @@ int launch_backward(const Resident& r, cudaStream_t st) {
   return r.d.cpg % kRun == 0 ? launch_resident<norm_grad_resident_kernel<DT, KEPT, true>>(r, piece, st, "norm_grad_resident_kernel launch")
                              : launch_resident<norm_grad_resident_kernel<DT, KEPT, false>>(r, piece, st, "norm_grad_resident_kernel launch");
 }
-// The resident kernels' terms: 16-byte pieces everywhere.
 bool forward_resident(const NormDev& d, int dtype, Resident* r) {
-  return d.vec_x && d.vec_out && make_resident(d, d.x8.dev_codes || d.y8.dev_codes, kRun * train_elem(dtype), r);
+  return make_resident(d, d.x8.dev_codes || d.y8.dev_codes, kRun * train_elem(dtype), r);
 }
 bool backward_resident(const NormDev& d, int dtype, Resident* r) {
   const bool kept = d.x8.dev_codes != nullptr;
-  return d.vec_dy && d.vec_out && (kept ? d.vec_x8 : d.vec_x) && make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun + 1 : kRun * train_elem(dtype)), r);
+  return make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun + 1 : kRun * train_elem(dtype)), r);
 }
 
 void make_geometry(NormDev* d) {
