@@ -36,7 +36,7 @@ linear_join_kernel(LinPieces q, LinEpilogue e) {
     const int64_t row = row0 + r;
     const bool mine = u < units && row < e.rows && (int)(n_tile * q.bn + strip * 128) < e.cols;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (mine) {
+    if (mine && (int)(n_tile * q.bn + strip * 128 + 4 * lane) < e.cols) {
       const float* src = q.partial + (size_t)(part * q.rows + r) * q.bn + strip * 128 + 4 * lane;
 #pragma unroll 6
       for (uint32_t g = g0 + sub; g <= g1; g += WAYS) {
