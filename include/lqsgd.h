@@ -415,8 +415,8 @@ int lqsgd_orthonormalize_noalloc(const float* dev_p_in, float* dev_p_out, int32_
  * narrower accesses).  Base pointers are aligned to their element.  Outputs must not overlap inputs, except where a
  * call says so.  A call on zero rows writes what an empty sum gives (zeros in weight and bias gradients) and nothing else.
  * Workspaces: device memory, 16-byte aligned, of the size the matching *_workspace_bytes reports (0: may be NULL); it
- * may be reused by the next call on the same stream.  All sums are taken in fp32 in an order fixed by the sizes and alignments:
- * the same call gives the same bits.  The calls may be captured in CUDA graphs. */
+ * may be reused by the next call on the same stream.  All sums are held in fp32 and taken in an order fixed by the sizes,
+ * strides and alignments: the same call gives the same bits.  The calls may be captured in CUDA graphs. */
 typedef enum lqsgd_dtype { LQSGD_BF16 = 0, LQSGD_F16 = 1, LQSGD_F32 = 2 } lqsgd_dtype;
 typedef enum lqsgd_act {
   LQSGD_ACT_NONE = 0,
@@ -460,7 +460,10 @@ int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_packed8* host_
  *                             z8 = pack8(x w^T + bias), y8 = pack8(y as stored)    each optional (NULL codes)
  *   lqsgd_linear_grad_input   dx = dz w + residual                  rows x in      residual: the skip connection's gradient
  *   lqsgd_linear_grad_weight  dw = dz^T x  (or dw += dz^T x)        out x in       x from x8 when its codes are set
- * Where few tiles would leave SMs idle the sum is cut in pieces whose partial results meet in the workspace.
+ * Where few tiles would leave SMs idle the sum is cut in pieces whose partial results meet in the workspace.  There, too,
+ * x8 is decoded for the tensor cores (rows x in 16-bit values), and operands whose rows are not 16-byte aligned are copied.
+ * A weight gradient adds at most 1024 rows in a tensor core's accumulator (which cuts toward zero) and those sums in
+ * registers; forward and grad_input, rounded to 16 bits, take the whole sum in the accumulator.
  * dev_status: NULL, or one device uint32 into which LQSGD_STATUS_TIMEOUT is ORed should a bounded device-side wait run
  * out (the outputs are then undefined). */
 typedef struct lqsgd_linear {
