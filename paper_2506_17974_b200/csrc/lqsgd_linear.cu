@@ -240,8 +240,9 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   if ((rc = place(&p.a, ws, p.off_a, st)) != LQSGD_OK || (rc = place(&p.b, ws, p.off_b, st)) != LQSGD_OK) return rc;
   const int es = ep.dtype == LQSGD_F32 ? 4 : 2;
   auto rows_aligned = [](const void* ptr, int64_t bytes, size_t to) { return train_aligned(ptr, to) && bytes % (int64_t)to == 0; };
-  ep.vec_out = rows_aligned(ep.out, ep.ld_out * es, 32);
-  ep.vec_res = rows_aligned(ep.residual, ep.ld_res * 2, 32);
+  auto rows_vec = [&](const void* q, int64_t ld) { return rows_aligned(q, ld, 32) ? 2 : rows_aligned(q, ld, 16) ? 1 : 0; };
+  ep.vec_out = rows_vec(ep.out, ep.ld_out * es);
+  ep.vec_res = rows_vec(ep.residual, ep.ld_res * 2);
   ep.vec_z8 = rows_aligned(ep.z8.dev_codes, ep.z8.ld_codes, 16);
   ep.vec_y8 = rows_aligned(ep.y8.dev_codes, ep.y8.ld_codes, 16);
   LinProblem q;

@@ -46,7 +46,8 @@ struct LinEpilogue {
   int32_t dtype;                       // of out and residual; LQSGD_F32: out is fp32 and residual is not used
   int32_t act;
   int32_t accumulate;                  // fp32 out only: add to what is there
-  int32_t vec_out, vec_res, vec_z8, vec_y8;   // rows are aligned to 32 bytes (out, residual) / 16 bytes (codes)
+  int32_t vec_out, vec_res;            // rows are aligned to 32 bytes (2), to 16 bytes (1), to neither (0)
+  int32_t vec_z8, vec_y8;              // rows are aligned to 16 bytes
 };
 
 struct alignas(64) LinProblem {
@@ -233,6 +234,23 @@ __device__ __forceinline__ void put_packed(const lqsgd_packed8& p, bool vec, int
   p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
 }
 
+// 32 bytes of a row that is aligned to 32 (vec = 2) or 16 bytes (vec = 1)
+__device__ __forceinline__ void ld_row32(const void* p, int vec, uint32_t (&w)[8]) {
+  if (vec == 2) {
+    ld_global_32(p, w);
+  } else {
+    const uint4 a = *static_cast<const uint4*>(p), b = *(static_cast<const uint4*>(p) + 1);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  }
+}
+__device__ __forceinline__ void st_row32(void* p, int vec, const uint32_t (&w)[8]) {
+  if (vec == 2) {
+    st_global_32(p, w);
+  } else {
+    *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    *(static_cast<uint4*>(p) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
 // Epilogue of 8 columns of a weight gradient held by a warp, a row per thread (row0: lane 0's row), where rows are not 32-byte
 // aligned or the tile passes the matrix: through the warp's scratch in shared memory (rows of 9 words), so that an access is
 // four rows' 8 columns instead of one column of 32 rows (which costs a sector per element).
@@ -253,21 +271,30 @@ __device__ __forceinline__ void finish_ragged_f32(const LinEpilogue& e, int64_t 
   __syncwarp();
 }
 // Epilogue of a 32 x 32 piece of a layer's output.
-__device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], float* scratch) {
+// bias: these columns' values in shared memory (zeros past the matrix).
+__device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], const float* bias, float* scratch) {
   const int lane = threadIdx.x & 31;
   const int have = min(32, e.cols - col);
   const int64_t row = row0 + lane;
   const int rows = (int)min((int64_t)32, e.rows - row0);
   uint16_t* half = reinterpret_cast<uint16_t*>(scratch);                // 16-bit values: rows of 2 x 17 halves
   constexpr int kHalfPitch = 34;
+  // The residual: this row's 32 columns where rows are aligned, else a column of all 32 rows, turned in shared memory.
+  const bool res_rows = e.residual && e.vec_res && have == 32, res_cols = e.residual && !res_rows;
+  const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row0 * e.ld_res + col;
+  if (res_cols) {
+    uint16_t t[32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) t[k] = lane < have && k < rows ? r[k * e.ld_res + lane] : (uint16_t)0;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) half[k * kHalfPitch + lane] = t[k];
+    __syncwarp();
+  }
   if (e.bias) {
-    if (have == 32) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] += __ldg(e.bias + col + i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i < have) v[i] += __ldg(e.bias + col + i);
+    for (int i = 0; i < 8; ++i) {
+      const float4 b = *(reinterpret_cast<const float4*>(bias) + i);
+      v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
     }
   }
   if (have < 32) {
@@ -277,36 +304,27 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
   }
   if (e.z8.dev_codes && on) put_packed(e.z8, e.vec_z8, row, col, have, v);
   act_run(e.act, v);
-  if (e.residual) {
-    const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row0 * e.ld_res + col;
-    if (e.vec_res && have == 32) {
-      if (on) {
+  if (res_rows && on) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t w[8];
-          ld_global_32(r + lane * e.ld_res + 16 * i, w);
+    for (int i = 0; i < 2; ++i) {
+      uint32_t w[8];
+      ld_row32(r + lane * e.ld_res + 16 * i, e.vec_res, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 f = unpack2(e.dtype, w[j]);
-            v[16 * i + 2 * j] += f.x;
-            v[16 * i + 2 * j + 1] += f.y;
-          }
-        }
+      for (int j = 0; j < 8; ++j) {
+        const float2 f = unpack2(e.dtype, w[j]);
+        v[16 * i + 2 * j] += f.x;
+        v[16 * i + 2 * j + 1] += f.y;
       }
-    } else {
-      if (lane < have) {
-#pragma unroll 8
-        for (int k = 0; k < rows; ++k) half[k * kHalfPitch + lane] = r[k * e.ld_res + lane];
-      }
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float2 f = unpack2(e.dtype, *reinterpret_cast<const uint32_t*>(half + lane * kHalfPitch + 2 * j));
-        if (2 * j < have) v[2 * j] += f.x;
-        if (2 * j + 1 < have) v[2 * j + 1] += f.y;
-      }
-      __syncwarp();
     }
+  }
+  if (res_cols) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float2 f = unpack2(e.dtype, *reinterpret_cast<const uint32_t*>(half + lane * kHalfPitch + 2 * j));
+      if (2 * j < have) v[2 * j] += f.x;
+      if (2 * j + 1 < have) v[2 * j + 1] += f.y;
+    }
+    __syncwarp();
   }
   uint32_t w[16];
 #pragma unroll
@@ -319,7 +337,7 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
         uint32_t h[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = w[8 * i + j];
-        st_global_32(o + lane * e.ld_out + 16 * i, h);
+        st_row32(o + lane * e.ld_out + 16 * i, e.vec_out, h);
       }
     }
   } else {
@@ -516,7 +534,7 @@ struct LinCfg {
   static constexpr int kChunk = WF32 ? 16 : 1 << 30;
   static constexpr int kMine = BN / (kEpiWarps / 4);                      // columns per epilogue warp
   static constexpr int kThreads = (4 + kEpiWarps) * 32;
-  static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2, kScratch = kEpiWarps * kScratchWarp;
+  static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2 + kMine * 4, kScratch = kEpiWarps * kScratchWarp;
   static constexpr uint32_t kRoom = 225u * 1024 - kScratch;
   static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
   static constexpr int kTmemCols = 2 * BN;
@@ -679,8 +697,36 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     const int q = warp & 3, c0 = ((warp - 4) >> 2) * S::kMine;
     float* scratch = reinterpret_cast<float*>(base + S::kScratchOff + (warp - 4) * S::kScratchWarp);
     LinWalk w(p, cluster, clusters, part_of);
+    // What the epilogue of a layer reads besides the sum is asked for a tile ahead: the bias of this warp's columns in
+    // registers, the residual into L2.
+    float* bias = scratch + 32 * 34 / 2;
+    float bias_next[S::kMine / 32] = {};
+    auto fetch_ahead = [&](const LinWalk& t) {
+      if (WF32 || meet > 1 || t.done() || t.piece(p) >= 0) return;
+      const int m = (t.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane, n = t.n_tile * BN + c0, have = min(S::kMine, p.N - n);
+      if (p.ep.bias) {
+#pragma unroll
+        for (int i = 0; i < S::kMine / 32; ++i) bias_next[i] = 32 * i + lane < have ? __ldg(p.ep.bias + n + 32 * i + lane) : 0.f;
+      }
+      if (p.ep.residual && m < p.M && have > 0) {
+        const char* r = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.ep.residual) + (int64_t)m * p.ep.ld_res + n);
+#pragma unroll
+        for (int b = 0; b < S::kMine * 2; b += 128)
+          if (b < 2 * have) asm volatile("prefetch.global.L2 [%0];" ::"l"(r + b));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(r + 2 * have - 2));
+      }
+    };
     train_pdl_wait();
+    fetch_ahead(w);
     for (; !w.done(); w.next_tile(p)) {
+      if (!WF32 && (p.ep.residual || p.ep.bias)) {
+#pragma unroll
+        for (int i = 0; i < S::kMine / 32; ++i) bias[32 * i + lane] = bias_next[i];
+        __syncwarp();
+        LinWalk t = w;
+        t.next_tile(p);
+        fetch_ahead(t);
+      }
       const int m = (w.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane, n0 = w.n_tile * BN;
       const int piece = w.piece(p);
       float* part = piece >= 0 ? p.partial + (int64_t)piece * (CG * kLinBM * BN) : nullptr;
@@ -741,6 +787,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           }
         } else if (part || (p.ep.vec_out && n0 + c0 + S::kMine <= p.N)) {
           const bool add = !part && p.ep.accumulate;
+          const int vec = part ? 2 : p.ep.vec_out;
           float* o = part ? part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0            // [row of the tile][BN]
                           : static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
           if (m < p.M && n0 + c0 < p.N) {
@@ -748,13 +795,13 @@ linear_kernel(const __grid_constant__ LinProblem p) {
             for (int c = 0; c < S::kMine; c += 8) {
               uint32_t u[8];
               if (add) {
-                ld_global_32(o + c, u);
+                ld_row32(o + c, vec, u);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
               }
 #pragma unroll
               for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
-              st_global_32(o + c, u);
+              st_row32(o + c, vec, u);
             }
           }
         } else if (m - lane < p.M) {
@@ -794,7 +841,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
               st_global_32(o + 8 * i, u);
             }
           } else {
-            finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, scratch);
+            finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
+            __syncwarp();
           }
         }
       }
