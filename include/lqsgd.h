@@ -506,7 +506,7 @@ typedef struct lqsgd_group_norm {
   int32_t dtype;        /* of x, y, dy, dx: any lqsgd_dtype */
   int32_t act;
   int32_t groups;       /* divides c */
-  int32_t n, hw, c;     /* n >= 0, hw >= 1, c 1 .. 2^16 */
+  int32_t n, hw, c;     /* n >= 0, hw 1 .. 2^31 - 4096, c 1 .. 2^16 */
   float eps;            /* forward only, > 0 */
   const void* dev_x;    int64_t ld_x, sample_x;   /* elements between pixels and between samples */
   const void* dev_dy;   int64_t ld_dy, sample_dy; /* backward */

@@ -9,7 +9,9 @@
 // are read element by element).  Sums meet through
 // distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
 //
-// Streaming kernels (everything else): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
+// Streaming kernels (everything else; a pixel is dealt to as many lanes as it has 8-channel pieces, so that few channels leave none
+// idle: 431 x 9957 x 5 takes 61 us forward and 191 backward; with four pixels at once per thread 80 and 202, since
+// fewer threads fit then): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
 // figures, and a last kernel reads the tensor a second time (from L2 up to about 100 MB) and applies them.  Their forward sums
 // are (mean, squared distances from it) about a value of the channel itself, merged pairwise; the resident kernel takes the
 // mean first and the distances from it in a second pass.  Either way a mean far from zero cancels nothing.
@@ -106,46 +108,62 @@ template <int DT>
 __global__ void __launch_bounds__(kThreads)
 norm_stats_kernel(NormDev d) {
   train_pdl_wait();
-  __shared__ float smean[kWarps * 32][kRun + 1], sq[kWarps * 32][kRun + 1], scount[kWarps * 32];
+  __shared__ float smean[kThreads][kRun + 1], sq[kThreads][kRun + 1], scount[kThreads];
   const Spot s = spot_of(d);
   d.x8.dev_codes = nullptr;
-  float ref[kRun], sum[kRun], sum2[kRun];
+  float mean[kRun], sum[kRun], sum2[kRun];                  // mean: first of all a value of the channel
   int count = 0;
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) ref[j] = sum[j] = sum2[j] = 0.f;
-  if (s.have > 0)
-    for (int p = s.pix; p < s.pix_end; p += s.pix_step, ++count) {
+  for (int j = 0; j < kRun; ++j) mean[j] = sum[j] = sum2[j] = 0.f;
+  if (s.have > 0) {
+    if (s.pix < s.pix_end) load_x<DT>(d, s, s.pix, mean), count = 1;
+    for (int p = s.pix + s.pix_step; p < s.pix_end; p += s.pix_step, ++count) {
       float v[kRun];
       load_x<DT>(d, s, p, v);
-      if (count == 0) {
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) ref[j] = v[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-          const float t = v[j] - ref[j];
-          sum[j] += t;
-          sum2[j] = fmaf(t, t, sum2[j]);
-        }
+      for (int j = 0; j < kRun; ++j) {
+        const float t = v[j] - mean[j];
+        sum[j] += t;
+        sum2[j] = fmaf(t, t, sum2[j]);
       }
     }
+  }
   const float inv = count ? 1.f / count : 0.f;
+  float n = (float)count, q[kRun];
 #pragma unroll
   for (int j = 0; j < kRun; ++j) {
-    smean[threadIdx.x][j] = fmaf(sum[j], inv, ref[j]);
-    sq[threadIdx.x][j] = fmaxf(fmaf(-sum[j] * inv, sum[j], sum2[j]), 0.f) + 0.f * sum2[j];   // the last term keeps NaN
+    mean[j] = fmaf(sum[j], inv, mean[j]);
+    q[j] = fmaxf(fmaf(-sum[j] * inv, sum[j], sum2[j]), 0.f) + 0.f * sum2[j];   // the last term keeps NaN
   }
-  scount[threadIdx.x] = (float)count;
+  // the warp's lanes with the same channels, then its warps
+  const int lanes = 1 << d.lane_shift, lane = threadIdx.x & 31;
+  for (int o = 16; o >= lanes; o >>= 1) {
+    const float n2 = __shfl_down_sync(0xffffffffu, n, o), t = n + n2, f = n2 > 0.f ? n2 / t : 0.f;
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      const float m2 = __shfl_down_sync(0xffffffffu, mean[j], o), q2 = __shfl_down_sync(0xffffffffu, q[j], o);
+      const float dist = m2 - mean[j];
+      if (n2 > 0.f) {
+        q[j] += q2 + dist * dist * n * f;
+        mean[j] = n > 0.f ? fmaf(dist, f, mean[j]) : m2;
+      }
+    }
+    n = t;
+  }
+  if (lane < lanes) {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) { smean[threadIdx.x][j] = mean[j]; sq[threadIdx.x][j] = q[j]; }
+    scount[threadIdx.x] = n;
+  }
   __syncthreads();
-  const int lanes = 1 << d.lane_shift;
   for (int ch = threadIdx.x; ch < lanes * kRun; ch += kThreads) {
     const int col = (int)(blockIdx.x % (unsigned)d.segs) * lanes * kRun + ch;
     if (col >= d.c) continue;
-    float n = 0.f, m = 0.f, q = 0.f;
-    for (int t = ch / kRun; t < kThreads; t += lanes) merge(n, m, q, scount[t], smean[t][ch % kRun], sq[t][ch % kRun]);
+    float n1 = 0.f, m1 = 0.f, q1 = 0.f;
+    for (int w = 0; w < kWarps; ++w) merge(n1, m1, q1, scount[32 * w + ch / kRun], smean[32 * w + ch / kRun][ch % kRun], sq[32 * w + ch / kRun][ch % kRun]);
     const size_t at = ((size_t)s.sample * d.chunks + s.chunk) * d.c + col;
-    d.part0[at] = m;
-    d.part1[at] = q;
+    d.part0[at] = m1;
+    d.part1[at] = q1;
   }
 }
 
@@ -186,13 +204,14 @@ __device__ __forceinline__ void channel_figures(const NormDev& d, const Spot& s,
   }
 }
 
-// Packs 8 of a row's columns per thread, four neighbouring lanes to a group of 32; the whole warp calls it.
-__device__ __forceinline__ void pack_run(const lqsgd_packed8& out, bool vec, int64_t row, int col, int have, bool on, const float (&v)[kRun]) {
+// Packs 8 of a row's columns per thread, four neighbouring lanes to a group of 32 (a row of one or two lanes is one group);
+// the whole warp calls it.
+__device__ __forceinline__ void pack_run(const lqsgd_packed8& out, bool vec, int lane_shift, int64_t row, int col, int have, bool on, const float (&v)[kRun]) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < kRun; ++j) top = max(top, on && j < have ? __float_as_uint(v[j]) & 0x7fffffffu : 0u);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  if (lane_shift > 0) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  if (lane_shift > 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const int eb = exp_byte(__uint_as_float(top));
   if (!on) return;
   const float inv = inv_step(eb);
@@ -226,7 +245,7 @@ norm_apply_kernel(NormDev d) {
     const int64_t row = (int64_t)s.sample * d.hw + p;
     float v[kRun];
     if (on) load_x<DT>(d, s, p, v);
-    if (x8.dev_codes) pack_run(x8, d.vec_x8, row, s.col, s.have, on, v);
+    if (x8.dev_codes) pack_run(x8, d.vec_x8, d.lane_shift, row, s.col, s.have, on, v);
     if (on) {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) v[j] = fmaf(v[j] - mean[j], scale[j], beta[j]);
@@ -236,7 +255,7 @@ norm_apply_kernel(NormDev d) {
     if (d.y8.dev_codes) {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
-      pack_run(d.y8, d.vec_y8, row, s.col, s.have, on, v);
+      pack_run(d.y8, d.vec_y8, d.lane_shift, row, s.col, s.have, on, v);
     }
   }
 }
@@ -246,7 +265,7 @@ __global__ void __launch_bounds__(kThreads)
 norm_grad_sums_kernel(NormDev d) {
   train_pdl_wait();
   using T = typename Elem<DT>::T;
-  __shared__ float s0[kThreads][kRun + 1], s1[kThreads][kRun + 1];
+  __shared__ float s0[kWarps][32 * kRun], s1[kWarps][32 * kRun];
   const Spot s = spot_of(d);
   float a[kRun], b[kRun];
 #pragma unroll
@@ -255,10 +274,9 @@ norm_grad_sums_kernel(NormDev d) {
     float mean[kRun], rstd[kRun], gamma[kRun], beta[kRun];
     channel_figures(d, s, mean, rstd, gamma, beta);
     for (int p = s.pix; p < s.pix_end; p += s.pix_step) {
-      float v[kRun], g[kRun];
+      float v[kRun], g[kRun], h[kRun];
       load_x<DT>(d, s, p, v);
       load_run<DT, kRun>(static_cast<const T*>(d.dy) + s.sample * d.sample_dy + p * d.ld_dy + s.col, d.vec_dy && s.have == kRun, s.have, g);
-      float h[kRun];
 #pragma unroll
       for (int j = 0; j < kRun; ++j) { v[j] = (v[j] - mean[j]) * rstd[j]; h[j] = fmaf(v[j], gamma[j], beta[j]); }
       slope_run(d.act, h);
@@ -270,29 +288,39 @@ norm_grad_sums_kernel(NormDev d) {
       }
     }
   }
+  const int lanes = 1 << d.lane_shift, lane = threadIdx.x & 31;
+  for (int o = 16; o >= lanes; o >>= 1)
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) { s0[threadIdx.x][j] = a[j]; s1[threadIdx.x][j] = b[j]; }
+    for (int j = 0; j < kRun; ++j) {
+      a[j] += __shfl_down_sync(0xffffffffu, a[j], o);
+      b[j] += __shfl_down_sync(0xffffffffu, b[j], o);
+    }
+  if (lane < lanes) {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) { s0[threadIdx.x >> 5][lane * kRun + j] = a[j]; s1[threadIdx.x >> 5][lane * kRun + j] = b[j]; }
+  }
   __syncthreads();
-  const int lanes = 1 << d.lane_shift;
   for (int ch = threadIdx.x; ch < lanes * kRun; ch += kThreads) {
     const int col = (int)(blockIdx.x % (unsigned)d.segs) * lanes * kRun + ch;
     if (col >= d.c) continue;
     float u = 0.f, w = 0.f;
-    for (int t = ch / kRun; t < kThreads; t += lanes) { u += s0[t][ch % kRun]; w += s1[t][ch % kRun]; }
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) { u += s0[k][ch]; w += s1[k][ch]; }
     const size_t at = ((size_t)s.sample * d.chunks + s.chunk) * d.c + col;
     d.part0[at] = u;
     d.part1[at] = w;
   }
 }
 
+constexpr int kJoinWarps = 32;
 // Blocks [0, group_blocks): a warp per (sample, group) forms <u> and <u xh>.  The others: 32 channels each, dgamma and dbeta.
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(32 * kJoinWarps)
 norm_grad_join_kernel(NormDev d, int group_blocks) {
   train_pdl_wait();
-  __shared__ float s0[kWarps][33], s1[kWarps][33];
+  __shared__ float s0[kJoinWarps][33], s1[kJoinWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if ((int)blockIdx.x < group_blocks) {
-    const int64_t u = (int64_t)blockIdx.x * kWarps + warp;
+    const int64_t u = (int64_t)blockIdx.x * kJoinWarps + warp;
     if (u >= (int64_t)d.n * d.groups) return;
     const int sample = (int)(u / d.groups), g = (int)(u - (int64_t)sample * d.groups);
     float a = 0.f, b = 0.f;
@@ -316,18 +344,21 @@ norm_grad_join_kernel(NormDev d, int group_blocks) {
   }
   const int col = ((int)blockIdx.x - group_blocks) * 32 + lane;
   float a = 0.f, b = 0.f;
-  if (col < d.c)
-    for (int64_t r = warp; r < (int64_t)d.n * d.chunks; r += kWarps) {
+  const int rows = d.n * d.chunks;
+  if (col < d.c) {
+#pragma unroll 8
+    for (int r = warp; r < rows; r += kJoinWarps) {
       a += d.part0[(size_t)r * d.c + col];
       b += d.part1[(size_t)r * d.c + col];
     }
+  }
   s0[warp][lane] = a;
   s1[warp][lane] = b;
   __syncthreads();
   if (warp == 0 && col < d.c) {
     float u = 0.f, w = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) { u += s0[k][lane]; w += s1[k][lane]; }
+    for (int k = 0; k < kJoinWarps; ++k) { u += s0[k][lane]; w += s1[k][lane]; }
     d.dbeta[col] = u;
     d.dgamma[col] = w;
   }
@@ -349,10 +380,9 @@ norm_grad_apply_kernel(NormDev d) {
     c1[j] = d.group1[at];
   }
   for (int p = s.pix; p < s.pix_end; p += s.pix_step) {
-    float v[kRun], g[kRun];
+    float v[kRun], g[kRun], h[kRun];
     load_x<DT>(d, s, p, v);
     load_run<DT, kRun>(static_cast<const T*>(d.dy) + s.sample * d.sample_dy + p * d.ld_dy + s.col, d.vec_dy && s.have == kRun, s.have, g);
-    float h[kRun];
 #pragma unroll
     for (int j = 0; j < kRun; ++j) { v[j] = (v[j] - mean[j]) * rstd[j]; h[j] = fmaf(v[j], gamma[j], beta[j]); }
     slope_run(d.act, h);
@@ -548,13 +578,13 @@ __device__ __forceinline__ void store_rounded(typename Elem<DT>::T* p, bool vec,
   }
 }
 // pack_run for whole runs.
-__device__ __forceinline__ void pack_whole(const lqsgd_packed8& out, bool vec, int64_t row, int col, bool on, const float (&v)[kRun]) {
+__device__ __forceinline__ void pack_whole(const lqsgd_packed8& out, bool vec, int lane_shift, int64_t row, int col, bool on, const float (&v)[kRun]) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
   if (!on) top = 0;
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  if (lane_shift > 0) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  if (lane_shift > 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   if (!on) return;
   const int eb = exp_byte(__uint_as_float(top));
   const float inv = inv_step(eb);
@@ -674,13 +704,13 @@ norm_resident_kernel(Resident r) {
         const bool on = k < count;
         const int64_t row = (int64_t)q.sample * d.hw + q.first + p;
         if (on) unpack_run<DT>(own + k * kStep, v);
-        if (d.x8.dev_codes) pack_whole(d.x8, d.vec_x8, row, q.col, on, v);
+        if (d.x8.dev_codes) pack_whole(d.x8, d.vec_x8, r.lane_shift, row, q.col, on, v);
         if (on) {
 #pragma unroll
           for (int j = 0; j < kRun; ++j) v[j] = act_value<decltype(tag)::value>(fmaf(v[j] - m[G::of(j)], gamma[j], beta[j]));
           store_rounded<DT>(dst, d.vec_out, v);
         }
-        if (d.y8.dev_codes) pack_whole(d.y8, d.vec_y8, row, q.col, on, v);
+        if (d.y8.dev_codes) pack_whole(d.y8, d.vec_y8, r.lane_shift, row, q.col, on, v);
       }
     });
   }
@@ -848,13 +878,14 @@ size_t resident_smem(const Resident& r, int piece_bytes) {
   return (size_t)r.steps * kResThreads * piece_bytes + 4 * ((size_t)(2 * kRun * kResWarps << std::min(r.lane_shift, 5)) + 2 * r.cb + 4 * (r.cb / r.d.cpg));
 }
 // Whether the resident kernels take a problem, and how.  piece_bytes: shared memory per 8 channels of a pixel.
-bool plan_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
+bool plan_resident(const NormDev& d, bool packs, bool backward, int piece_bytes, Resident* out) {
   auto gcd = [](int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; };
   if (d.c % kRun) return false;
   const int unit = packs ? kGroup : kRun;
   const int64_t base = (int64_t)d.cpg / gcd(d.cpg, unit) * unit;
   Resident best = {};
   double best_score = 1e30;
+  bool best_alone = false;                                  // more CTAs than SMs, one at a time on each
   for (int64_t cb = base;; cb += base) {
     const int64_t block = std::min<int64_t>(cb, d.c);
     if (block > kResThreads * kRun) break;
@@ -865,7 +896,6 @@ bool plan_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
     r.d = d;
     r.cb = (int)block;
     r.blocks = (int)ceil_div64(d.c, block);
-    if (packs) r.lane_shift = 2;                            // a group of 32 is four neighbouring lanes
     while ((kRun << r.lane_shift) < block) ++r.lane_shift;
     const int row_step = kResThreads >> r.lane_shift;
     for (int parts = 1; parts <= 8; parts *= 2) {
@@ -886,27 +916,31 @@ bool plan_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out)
       const double idle = (double)((1 << r.lane_shift) * kRun * r.blocks) / d.c;
       const double slow = per_sm == 1 ? 1.9 : per_sm == 2 ? 1.45 : per_sm == 3 ? 1.05 : 1.0;
       const double score = ctas * (parts > 1 ? 9e-3 : 6e-3) + values * 0.9e-6 * slow * (1 + 0.3 * std::min(full - 1, 2.0)) * idle;
-      if (score < best_score) { best_score = score; best = r; }
+      if (score < best_score) { best_score = score; best = r; best_alone = per_sm == 1 && ctas > 148; }
     }
     if (last) break;
   }
   if (best_score > 1e29) return false;
+  // A forward pass that packs works long between its reads and its writes; with nothing else on the SM meanwhile the streaming
+  // kernels are faster (33 x 3560 x 192, 8 groups: 98 us against 144; 38 x 6153 x 80: 85 against 136), without packing they
+  // are not (67 against 44, 52 against 47), and a backward pass has more to read twice (166 against 82).
+  if (packs && !backward && best_alone) return false;
   *out = best;
   return true;
 }
 // The last plans of this host thread, by the sizes they are made from: a training step asks for the same ones over and over.
-bool make_resident(const NormDev& d, bool packs, int piece_bytes, Resident* out) {
-  struct Memo { int32_t n = -1, hw, c, groups, packs, piece_bytes; bool ok; Resident r; };
+bool make_resident(const NormDev& d, bool packs, bool backward, int piece_bytes, Resident* out) {
+  struct Memo { int32_t n = -1, hw, c, groups, packs, backward, piece_bytes; bool ok; Resident r; };
   static thread_local Memo memo[16];
   static thread_local unsigned next = 0;
   for (const Memo& m : memo)
-    if (m.n == d.n && m.hw == d.hw && m.c == d.c && m.groups == d.groups && m.packs == (int)packs && m.piece_bytes == piece_bytes) {
+    if (m.n == d.n && m.hw == d.hw && m.c == d.c && m.groups == d.groups && m.packs == (int)packs && m.backward == (int)backward && m.piece_bytes == piece_bytes) {
       if (m.ok) { *out = m.r; out->d = d; }
       return m.ok;
     }
   Memo& m = memo[next++ % 16];
-  m.ok = plan_resident(d, packs, piece_bytes, &m.r);
-  m.n = d.n; m.hw = d.hw; m.c = d.c; m.groups = d.groups; m.packs = packs; m.piece_bytes = piece_bytes;
+  m.ok = plan_resident(d, packs, backward, piece_bytes, &m.r);
+  m.n = d.n; m.hw = d.hw; m.c = d.c; m.groups = d.groups; m.packs = packs; m.backward = backward; m.piece_bytes = piece_bytes;
   if (m.ok) *out = m.r;
   return m.ok;
 }
@@ -935,16 +969,16 @@ int launch_backward(const Resident& r, cudaStream_t st) {
                              : launch_resident<norm_grad_resident_kernel<DT, KEPT, false>>(r, piece, st, "norm_grad_resident_kernel launch");
 }
 bool forward_resident(const NormDev& d, int dtype, Resident* r) {
-  return make_resident(d, d.x8.dev_codes || d.y8.dev_codes, kRun * train_elem(dtype), r);
+  return make_resident(d, d.x8.dev_codes || d.y8.dev_codes, false, kRun * train_elem(dtype), r);
 }
 bool backward_resident(const NormDev& d, int dtype, Resident* r) {
   const bool kept = d.x8.dev_codes != nullptr;
-  return make_resident(d, kept, kRun * train_elem(dtype) + (kept ? kRun + 1 : kRun * train_elem(dtype)), r);
+  return make_resident(d, kept, true, kRun * train_elem(dtype) + (kept ? kRun + 1 : kRun * train_elem(dtype)), r);
 }
 
 void make_geometry(NormDev* d) {
   d->cpg = d->c / d->groups;
-  d->lane_shift = 2;
+  d->lane_shift = 0;
   while (d->lane_shift < 5 && (8 << d->lane_shift) < d->c) ++d->lane_shift;
   d->segs = (int)ceil_div64(d->c, 8ll << d->lane_shift);
   const int step = kWarps * (32 >> d->lane_shift);          // pixels one pass of a block covers
@@ -966,7 +1000,7 @@ size_t workspace_of(const NormDev& d, int dtype, bool backward) {
 int check_common(const lqsgd_group_norm* a) {
   if (!a || a->struct_size != sizeof(lqsgd_group_norm)) return LQSGD_ERR_INVALID_ARG;
   if (!train_dtype_ok(a->dtype) || !train_act_ok(a->act)) return LQSGD_ERR_INVALID_ARG;
-  if (a->n < 0 || a->hw < 1 || a->c < 1 || a->c > 65536 || a->groups < 1 || a->c % a->groups) return LQSGD_ERR_BAD_SHAPE;
+  if (a->n < 0 || a->hw < 1 || a->hw > 0x7fffffff - 4095 || a->c < 1 || a->c > 65536 || a->groups < 1 || a->c % a->groups) return LQSGD_ERR_BAD_SHAPE;
   const int64_t segs = ceil_div64(a->c, 32);
   // one block per sample, chunk and segment: the grid's limit; chunks beyond 1 only come with few samples
   if ((int64_t)a->n * segs > (1ll << 30)) return LQSGD_ERR_BAD_SHAPE;
@@ -1081,9 +1115,9 @@ extern "C" int lqsgd_group_norm_backward(const lqsgd_group_norm* a, void* cuda_s
   }
   place_workspace(&d, *a, (size_t)d.n * d.chunks * d.c);
   const dim3 grid((unsigned)((int64_t)d.n * d.chunks * d.segs));
-  const int group_blocks = (int)ceil_div64((int64_t)d.n * d.groups, kWarps);
+  const int group_blocks = (int)ceil_div64((int64_t)d.n * d.groups, kJoinWarps);
   TRAIN_CK(NORM_BY_DTYPE(a->dtype, norm_grad_sums_kernel, grid, dim3(kThreads), 0, st, 1, d), "norm_grad_sums_kernel launch");
-  TRAIN_CK(train_launch(norm_grad_join_kernel, dim3((unsigned)(group_blocks + (d.c + 31) / 32)), dim3(kThreads), 0, st, 1, d, group_blocks), "norm_grad_join_kernel launch");
+  TRAIN_CK(train_launch(norm_grad_join_kernel, dim3((unsigned)(group_blocks + (d.c + 31) / 32)), dim3(32 * kJoinWarps), 0, st, 1, d, group_blocks), "norm_grad_join_kernel launch");
   TRAIN_CK(NORM_BY_DTYPE(a->dtype, norm_grad_apply_kernel, grid, dim3(kThreads), 0, st, 1, d), "norm_grad_apply_kernel launch");
   return LQSGD_OK;
 }
