@@ -59,18 +59,34 @@ linear_join_kernel(LinPieces q, LinEpilogue e) {
 }
 
 // Copies a matrix whose rows TMA cannot address (base or row distance not a multiple of 16 bytes) to rows of ld_dst elements, a
-// multiple of 16 bytes; what lies past cols is never read.
+// multiple of 16 bytes, zeros past cols; what lies past cols is never read.  A warp takes 256 columns of a row at a time, a thread
+// 8 of them: words where the row starts on one, else 16-bit values.
+constexpr int kRealignCols = 256;
 __global__ void __launch_bounds__(256)
 realign_kernel(const uint16_t* __restrict__ src, int64_t ld_src, int64_t rows, int cols, uint16_t* __restrict__ dst, int64_t ld_dst) {
   train_pdl_wait();
-  const int pairs = (cols + 1) / 2;
-  const int64_t units = rows * pairs;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t row = u / pairs;
-    const int col = (int)(u - row * pairs) * 2;
-    const uint16_t* s = src + row * ld_src + col;
-    const uint32_t lo = s[0], hi = col + 1 < cols ? s[1] : 0;
-    *reinterpret_cast<uint32_t*>(dst + row * ld_dst + col) = lo | (hi << 16);
+  const int lane = threadIdx.x & 31, strips = (cols + kRealignCols - 1) / kRealignCols, warps = (int)gridDim.x * 8;
+  const int first = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+  int strip = first % strips;
+  for (int64_t row = first / strips; row < rows; row += warps / strips) {
+    const int col = strip * kRealignCols + 8 * lane, have = cols - col;
+    if (have > 0) {
+      const uint16_t* s = src + row * ld_src + col;
+      uint32_t w[4];
+      if (have >= 8 && (reinterpret_cast<uintptr_t>(s) & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(s) + i);
+      } else {
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = i < have ? __ldg(s + i) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (h[2 * i + 1] << 16);
+      }
+      *reinterpret_cast<uint4*>(dst + row * ld_dst + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    strip += warps % strips;
+    if (strip >= strips) { strip -= strips; ++row; }
   }
 }
 
@@ -194,7 +210,7 @@ int check_matrix(const void* p, int64_t ld, int32_t cols, int elem) {
 int place(Stored* s, char* ws, size_t off, cudaStream_t st) {
   if (s->tma_ready()) return LQSGD_OK;
   const int64_t ld = s->aligned_ld();
-  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ((s->cols + 1) / 2), 256), kSms * 16);
+  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ceil_div64(s->cols, kRealignCols), 8), kSms * 8);
   TRAIN_CK(train_launch(realign_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows,
                         (int)s->cols, reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
   s->base = ws + off;

@@ -282,12 +282,22 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
   // The residual: this row's 32 columns where rows are aligned, else a column of all 32 rows, turned in shared memory.
   const bool res_rows = e.residual && e.vec_res && have == 32, res_cols = e.residual && !res_rows;
   const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row0 * e.ld_res + col;
+  const int word_row = lane >> 4, word_col = 2 * (lane & 15);             // rows that start on words: two at a time
   if (res_cols) {
-    uint16_t t[32];
+    if (have == 32 && ((reinterpret_cast<uintptr_t>(r) | (2 * e.ld_res)) & 3) == 0) {
+      uint32_t t[16];
 #pragma unroll
-    for (int k = 0; k < 32; ++k) t[k] = lane < have && k < rows ? r[k * e.ld_res + lane] : (uint16_t)0;
+      for (int k = 0; k < 16; ++k)
+        t[k] = 2 * k + word_row < rows ? *reinterpret_cast<const uint32_t*>(r + (2 * k + word_row) * e.ld_res + word_col) : 0u;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) half[k * kHalfPitch + lane] = t[k];
+      for (int k = 0; k < 16; ++k) *reinterpret_cast<uint32_t*>(half + (2 * k + word_row) * kHalfPitch + word_col) = t[k];
+    } else {
+      uint16_t t[32];
+#pragma unroll
+      for (int k = 0; k < 32; ++k) t[k] = lane < have && k < rows ? r[k * e.ld_res + lane] : (uint16_t)0;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) half[k * kHalfPitch + lane] = t[k];
+    }
     __syncwarp();
   }
   if (e.bias) {
@@ -344,7 +354,11 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
 #pragma unroll
     for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(half + lane * kHalfPitch + 2 * j) = w[j];
     __syncwarp();
-    if (lane < have) {
+    if (have == 32 && ((reinterpret_cast<uintptr_t>(o) | (2 * e.ld_out)) & 3) == 0) {
+#pragma unroll 8
+      for (int k = word_row; k < rows; k += 2)
+        *reinterpret_cast<uint32_t*>(o + k * e.ld_out + word_col) = *reinterpret_cast<const uint32_t*>(half + k * kHalfPitch + word_col);
+    } else if (lane < have) {
 #pragma unroll 8
       for (int k = 0; k < rows; ++k) o[k * e.ld_out + lane] = half[k * kHalfPitch + lane];
     }
