@@ -151,7 +151,11 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
     if (p.unpacked) p.b = {nullptr, rows, a.in, ceil_div64(a.in, 8) * 8};
   }
   p.kb_total = (int)ceil_div64(p.K, kLinBK);
-  // The cheapest of the ways to deal the tiles out, by what they were measured to cost (microseconds).
+  // The cheapest of the ways to deal the tiles out, by what they were measured to cost (microseconds).  Pairs of SMs on tiles of
+  // 256 x 256 or single ones on 128 x 128: 94 against 134 us at 4096 x 4096 x 4096, but 10.7 against 9.2 at 1024 x 1024 x 1024, where
+  // 16 pairs would work.  A forward product of 256 x 3136 x 512 takes 17.6 us in whole tiles, 12.6 in shares, 9.9 with the sums
+  // of a cluster's CTAs meeting; a weight gradient of 65536 rows, 64 x 128, 281 us in whole tiles and 14.4 in shares; one of
+  // 8192 rows, 512 x 512, 39.9, 18.1, and 14.4 where they meet.  8 x 4096 x 16384, 128 tiles: 27.7 us whole, 30.0 in shares.
   constexpr double kTileUs = 2.2, kMeetUs = 4.0, kJoinUs = 4.0;
   double best = 1e30;
   auto consider = [&](int cg, int bn) {

@@ -6,15 +6,17 @@
 // Resident kernels (channels a multiple of 8, slices that fit): a cluster of 1 .. 8 CTAs takes one sample's block of whole groups
 // (at least 64 bytes of a pixel), each CTA a range of its pixels, and brings it into shared memory with asynchronous
 // copies of 16 bytes (no registers are held meanwhile, so the whole slice is in flight at once; rows without 16-byte pieces
-// are read element by element).  Sums meet through
-// distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
+// are read element by element).  Sums meet through distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
 //
-// Streaming kernels (everything else; a pixel is dealt to as many lanes as it has 8-channel pieces, so that few channels leave none
-// idle: 431 x 9957 x 5 takes 61 us forward and 191 backward; with four pixels at once per thread 80 and 202, since
-// fewer threads fit then): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
-// figures, and a last kernel reads the tensor a second time (from L2 up to about 100 MB) and applies them.  Their forward sums
-// are (mean, squared distances from it) about a value of the channel itself, merged pairwise; the resident kernel takes the
+// Streaming kernels (everything else): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
+// figures, and a last kernel reads the tensor a second time (from L2 up to about 100 MB) and applies them.  A pixel is dealt to as many
+// lanes as it has 8-channel pieces, so that few channels leave none idle: 431 x 9957 x 5 takes 62 us forward and 195 backward
+// (80 and 202 with four pixels at once per thread: fewer threads fit then).  Their forward sums are
+// (mean, squared distances from it) about a value of the channel itself, merged pairwise; the resident kernel takes the
 // mean first and the distances from it in a second pass.  Either way a mean far from zero cancels nothing.
+//
+// 256 x 1024 x 64 in bf16, 8 groups, silu: 20 us forward resident and 36 streaming, 41 and 61 with both 8-bit copies, backward from
+// the 8-bit x 45 and 83; 79 x 15713 x 8: 19 and 28, 30 and 39, 45 and 54.
 #include "lqsgd_train_dev.cuh"
 
 #include <algorithm>
