@@ -6,7 +6,8 @@
 // Resident kernels (channels a multiple of 8, slices that fit): a cluster of 1 .. 8 CTAs takes one sample's block of whole groups
 // (at least 64 bytes of a pixel), each CTA a range of its pixels, and brings it into shared memory with asynchronous
 // copies of 16 bytes (no registers are held meanwhile, so the whole slice is in flight at once; rows without 16-byte pieces
-// are read element by element).  Sums meet through distributed shared memory; the passes after the first read shared memory.  A thread reads only what it copied itself.
+// are read element by element).  Sums meet through distributed shared memory; the passes after the first read shared memory.
+// A thread reads only what it copied itself.
 //
 // Streaming kernels (everything else): per-channel sums of a chunk of pixels meet in a small kernel, which forms the groups'
 // figures, and a last kernel reads the tensor a second time (from L2 up to about 100 MB) and applies them.  A pixel is dealt to as many

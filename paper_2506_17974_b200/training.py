@@ -475,10 +475,17 @@ def group_norm_grad(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], groups: i
 
 # ------------------------------------------------------------------------------------- differentiable layers, 8 bits in between
 
+def _apart(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy of it where its rows overlap (an expanded tensor, the gradient of a sum) or do not lie along memory."""
+    row = t.shape[-1]
+    return t if t.stride(-1) == 1 and all(s >= row or n == 1 for n, s in zip(t.shape[:-1], t.stride()[:-1])) else t.contiguous()
+
+
 class _LinearLayer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, act, x8):
-        w = weight.to(x.dtype)
+        x, w = _apart(x), _apart(weight.to(x.dtype))
+        residual = residual if residual is None else _apart(residual)
         r = linear(x, w, bias, act, residual, save_z8=act != "none")
         x8 = pack8(x) if x8 is None else x8
         saved = [w, x8.codes, x8.exps] + ([r.z8.codes, r.z8.exps] if r.z8 is not None else [])
@@ -489,7 +496,7 @@ class _LinearLayer(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         w, xc, xe, *z = ctx.saved_tensors
-        dy = dy if dy.stride(-1) == 1 else dy.contiguous()
+        dy = _apart(dy)
         dz, db = act_grad(dy, Packed8(*z) if z else None, ctx.act, bias_grad=ctx.has_bias and ctx.needs_input_grad[2])
         dx = linear_grad_input(dz, w) if ctx.needs_input_grad[0] else None
         dw = linear_grad_weight(dz, Packed8(xc, xe)) if ctx.needs_input_grad[1] else None
@@ -507,7 +514,7 @@ def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
 class _NormLayer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta, groups, eps, act, keep):
-        r = group_norm(x, groups, gamma, beta, eps, act, save_x8=True, save_y8=keep is not None)
+        r = group_norm(_apart(x), groups, gamma, beta, eps, act, save_x8=True, save_y8=keep is not None)
         ctx.save_for_backward(r.x8.codes, r.x8.exps, gamma, beta, r.mean, r.rstd)
         ctx.groups, ctx.act = groups, act
         if keep is not None:
