@@ -135,6 +135,7 @@ struct Plan {
   size_t off_a, off_b, off_x, off_partial, bytes;
 };
 
+constexpr size_t kPieceAlign = 32;     // of the pieces of sums in the workspace: the kernels move them in 32-byte accesses
 constexpr int kSms = 148;              // sums are cut for this many SMs whatever the card has: results do not depend on it
 
 int make_plan(int product, const lqsgd_linear& a, Plan* out) {
@@ -191,7 +192,8 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   if (p.unpacked) p.off_x = room((size_t)rows * p.b.ld * 2);
   p.off_a = room(p.a.copy_bytes());
   p.off_b = room(p.b.copy_bytes());
-  if (p.deal == kShares) p.off_partial = room((size_t)2 * p.clusters * kLinBM * p.cg * p.bn * 4);
+  // The pieces are written and read 32 bytes at a time, and the caller's workspace starts on 16: room to move their start.
+  if (p.deal == kShares) p.off_partial = room((size_t)2 * p.clusters * kLinBM * p.cg * p.bn * 4 + kPieceAlign);
   p.bytes = off;
   *out = p;
   return LQSGD_OK;
@@ -268,7 +270,7 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   LinProblem q;
   std::memset(&q, 0, sizeof(q));
   q.ep = ep;
-  q.partial = p.deal == kShares ? reinterpret_cast<float*>(ws + p.off_partial) : nullptr;
+  q.partial = p.deal == kShares ? reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ws + p.off_partial) + kPieceAlign - 1) & ~(uintptr_t)(kPieceAlign - 1)) : nullptr;
   q.M = (int32_t)p.M; q.N = (int32_t)p.N; q.K = (int32_t)p.K;
   q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total;
   q.deal = p.deal; q.share = p.share; q.meet = p.meet;
