@@ -17,6 +17,7 @@ import threading
 from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -474,6 +475,7 @@ def group_norm_grad(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], groups: i
 
 
 # ------------------------------------------------------------------------------------- differentiable layers, 8 bits in between
+# Differentiable once: the kernels of a backward pass leave nothing for autograd to follow, so a second derivative raises.
 
 def _apart(t: torch.Tensor) -> torch.Tensor:
     """t, or a copy of it where its rows overlap (an expanded tensor, the gradient of a sum) or do not lie along memory."""
@@ -494,6 +496,7 @@ class _LinearLayer(torch.autograd.Function):
         return r.y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         w, xc, xe, *z = ctx.saved_tensors
         dy = _apart(dy)
@@ -507,7 +510,7 @@ def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
                  residual: Optional[torch.Tensor] = None, x8: Optional[Packed8] = None) -> torch.Tensor:
     """linear() as a differentiable function: weight and bias float32 (the weights a round updates; the products run in x's
     type), x and the pre-activation kept in 8 bits, the weight gradient float32.  x8: x's 8-bit form where it exists
-    already (norm_layer and other producers can hand it on)."""
+    already (norm_layer and other producers can hand it on).  Differentiable once: a second derivative raises."""
     return _LinearLayer.apply(x, weight, bias, residual, act, x8)
 
 
@@ -522,6 +525,7 @@ class _NormLayer(torch.autograd.Function):
         return r.y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         codes, exps, gamma, beta, mean, rstd = ctx.saved_tensors
         dx, dgamma, dbeta = group_norm_grad(dy.contiguous(), Packed8(codes, exps), ctx.groups, gamma, beta, mean, rstd, ctx.act)
@@ -531,5 +535,5 @@ class _NormLayer(torch.autograd.Function):
 def norm_layer(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, groups: int, eps: float = 1e-5, act: str = "none",
                keep: Optional[list] = None) -> torch.Tensor:
     """group_norm() as a differentiable function with x kept in 8 bits.  `keep`, a list, receives the output's 8-bit form
-    (for the linear layer that follows)."""
+    (for the linear layer that follows).  Differentiable once: a second derivative raises."""
     return _NormLayer.apply(x, gamma, beta, groups, eps, act, keep)
