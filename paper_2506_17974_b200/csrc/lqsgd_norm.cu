@@ -71,7 +71,7 @@ __device__ __forceinline__ Spot spot_of(const NormDev& d) {
   s.have = min(kRun, d.c - s.col);
   const int first = s.chunk * d.chunk_rows;
   s.pix = first + warp * per_warp + s.sub;
-  s.pix_end = min(d.hw, first + d.chunk_rows);
+  s.pix_end = first + min(d.chunk_rows, d.hw - first);      // first + chunk_rows can pass 2^31
   s.pix_step = kWarps * per_warp;
   return s;
 }
@@ -182,7 +182,7 @@ norm_group_kernel(NormDev d) {
   for (int i = lane; i < d.chunks * d.cpg; i += 32) {
     const int chunk = i / d.cpg, ch = g * d.cpg + i % d.cpg;
     const size_t at = ((size_t)sample * d.chunks + chunk) * d.c + ch;
-    merge(n, m, q, (float)(min(d.hw, (chunk + 1) * d.chunk_rows) - chunk * d.chunk_rows), d.part0[at], d.part1[at]);
+    merge(n, m, q, (float)min(d.chunk_rows, d.hw - chunk * d.chunk_rows), d.part0[at], d.part1[at]);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
