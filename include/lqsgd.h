@@ -494,6 +494,16 @@ int lqsgd_linear_forward(const lqsgd_linear* host_args, void* cuda_stream);
 int lqsgd_linear_grad_input(const lqsgd_linear* host_args, void* cuda_stream);
 int lqsgd_linear_grad_weight(const lqsgd_linear* host_args, void* cuda_stream);
 
+/* TEST SUPPORT - the path a bounded wait of a linear product takes when it runs out (compare lqsgd_test_expire_wait).
+ * Arms the NEXT product of this host thread only: in its first cluster of CTAs `role` stops after `after` k blocks (of 64
+ * terms), and every bounded wait of that launch gives up after `wait_limit` polls (16 .. 2^18, about a microsecond each).
+ * The kernel returns, *dev_status has LQSGD_STATUS_TIMEOUT, the outputs are undefined.  A product without that many k blocks,
+ * or without a second CTA to a cluster, runs normally.  Host-only; never needed in production. */
+#define LQSGD_LINEAR_ROLE_LOADER 1        /* the loader of the first CTA */
+#define LQSGD_LINEAR_ROLE_LOADER_SECOND 2 /* the loader of a pair's second CTA */
+#define LQSGD_LINEAR_ROLE_MMA 3           /* the warp that issues the matrix products */
+int lqsgd_test_linear_wait(int32_t role, int32_t after, uint32_t wait_limit);
+
 /* Group norm with an activation on channels-last tensors: n samples of hw pixels of c channels, the channels in
  * `groups` equal groups.  With m and v the mean and the (biased) variance of a sample's group over its pixels and channels,
  *   forward   rstd = 1 / sqrt(v + eps),  h = gamma (x - m) rstd + beta,  y = act(h)

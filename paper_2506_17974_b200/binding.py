@@ -45,7 +45,7 @@ EXPORTED = [
     "lqsgd_round_begin", "lqsgd_round_pack", "lqsgd_round_reduce", "lqsgd_round_end", "lqsgd_exchange_view",
     "lqsgd_launches_per_step", "lqsgd_set_phase_events", "lqsgd_release_graph_tables", "lqsgd_test_expire_wait", "lqsgd_round_timeline", "lqsgd_check_guards", "lqsgd_plan_check", "lqsgd_test_plan_defect",
     "lqsgd_pack8", "lqsgd_unpack8", "lqsgd_act_grad_workspace_bytes", "lqsgd_act_grad",
-    "lqsgd_linear_workspace_bytes", "lqsgd_linear_forward", "lqsgd_linear_grad_input", "lqsgd_linear_grad_weight",
+    "lqsgd_linear_workspace_bytes", "lqsgd_linear_forward", "lqsgd_linear_grad_input", "lqsgd_linear_grad_weight", "lqsgd_test_linear_wait",
     "lqsgd_group_norm_workspace_bytes", "lqsgd_group_norm_forward", "lqsgd_group_norm_backward",
     "lqsgd_destroy", "lqsgd_strerror", "lqsgd_last_cuda_error", "lqsgd_version",
 ]

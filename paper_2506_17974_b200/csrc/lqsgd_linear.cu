@@ -246,7 +246,13 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
   return LQSGD_OK;
 }
 
+// What lqsgd_test_linear_wait asked of this host thread's next product.
+struct TestWait { uint32_t limit = 0, after = 0; int32_t role = kNoRole; };
+thread_local TestWait test_wait;
+
 int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
+  const TestWait test = test_wait;
+  test_wait = TestWait();
   Plan p;
   int rc = make_plan(product, a, &p);
   if (rc != LQSGD_OK) return rc;
@@ -276,6 +282,7 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   q.deal = p.deal; q.share = p.share; q.meet = p.meet;
   q.dtype = a.dtype;
   q.status = a.dev_status;
+  q.test_limit = test.limit; q.test_after = test.after; q.test_role = test.role;
   if (product == LQSGD_LINEAR_FORWARD)
     rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false>(p, q, st);
   else if (product == LQSGD_LINEAR_GRAD_INPUT)
@@ -310,6 +317,14 @@ extern "C" int lqsgd_linear_workspace_bytes(int32_t product, const lqsgd_linear*
   Plan p;
   if ((rc = make_plan(product, *host_args, &p)) != LQSGD_OK) return rc;
   *host_bytes_out = p.bytes;
+  return LQSGD_OK;
+}
+
+extern "C" int lqsgd_test_linear_wait(int32_t role, int32_t after, uint32_t wait_limit) {
+  if (role < LQSGD_LINEAR_ROLE_LOADER || role > LQSGD_LINEAR_ROLE_MMA || after < 0 || wait_limit < 16 || wait_limit > kWaitLimit) return LQSGD_ERR_INVALID_ARG;
+  test_wait.limit = wait_limit;
+  test_wait.after = (uint32_t)after;
+  test_wait.role = role;
   return LQSGD_OK;
 }
 

@@ -19,8 +19,9 @@
 // accumulator (two of them, so that the next tile's sum runs under the epilogue).  Clusters walk
 // the work items (tile, piece of the sum) with a fixed stride.
 //
-// Every wait is bounded (lqsgd_stream_common.cuh): on expiry the CTA's abort flag goes up, all roles leave their loops,
-// copies in flight are waited for, tensor memory is released and the caller's status word gets LQSGD_STATUS_TIMEOUT.
+// Every wait is bounded (lqsgd_stream_common.cuh) and begins after the kernel in front has ended.  On expiry the CTA's abort
+// flag goes up and all roles leave their loops; then the copies that either CTA of a pair still has in flight are waited for,
+// tensor memory is released and the caller's status word gets LQSGD_STATUS_TIMEOUT.
 #pragma once
 #include <cuda.h>
 
@@ -63,7 +64,12 @@ struct alignas(64) LinProblem {
   uint32_t box_a;                      // rows of A that TMA brings per stage and CTA: 128, fewer (a multiple of 8) where A has fewer and
                                        // they lie along k; what the stage holds beyond them only meets rows that do not exist
   uint32_t* status;
+  // Test support (lqsgd_test_linear_wait; zeros in normal operation): the limit of the bounded waits, and which role of the
+  // first cluster stops after how many k blocks (LinRole).
+  uint32_t test_limit, test_after;
+  int32_t test_role;
 };
+enum LinRole { kNoRole = 0, kLoader0 = 1, kLoader1 = 2, kMma = 3 };
 
 namespace {
 
@@ -111,6 +117,24 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
   return ok != 0;
+}
+
+// Completes `bytes` of a barrier's phase in place of a copy that was announced and never issued.
+__device__ __forceinline__ void complete_tx(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+// Waits (each time with a limit) for the last copies into a CTA's stages, `issued` k blocks of them so far.
+__device__ __forceinline__ void lin_drain(uint64_t* full, uint32_t stages, uint32_t issued, uint32_t limit) {
+  for (uint32_t j = issued > stages ? issued - stages : 0; j < issued; ++j)
+    for (uint32_t i = 0; i < limit && !mbar_try(full + j % stages, (j / stages) & 1); ++i) {}
+}
+// The same for a pair, whose copies all count on the first CTA's barriers: `mine` and `other` k blocks were issued by the first and
+// the second CTA, `bytes` each per k block.  Where one of them went on longer (by no more than the stages: neither refills
+// a stage before both have filled it and it was read), its phases are made whole first.
+__device__ __forceinline__ void lin_drain_pair(uint64_t* full, uint32_t stages, uint32_t mine, uint32_t other, uint32_t bytes, uint32_t limit) {
+  for (uint32_t j = other; j < mine; ++j) complete_tx(full + j % stages, bytes);             // announced for both, issued by one
+  for (uint32_t j = mine; j < other; ++j) mbar_arrive_expect_tx(full + j % stages, bytes);   // issued by the second, never announced
+  lin_drain(full, stages, max(mine, other), limit);
 }
 
 template <int CG>
@@ -578,6 +602,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   uint64_t* fin = d_empty + 2;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(fin + 1);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(fin + 1) + 2;
+  volatile uint32_t* ends = tmem_slot + 2;                           // [2] of each CTA of a pair: k blocks its loader issued * 2 + gave up
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
@@ -591,7 +616,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     }
     for (int s = 0; s < 2; ++s) { mbar_init(d_full + s, 1); mbar_init(d_empty + s, S::kEpiWarps * CG); }
     mbar_init(fin, 1);
-    wait_ctl_init(abort_flag, 0);
+    wait_ctl_init(abort_flag, p.test_limit);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
@@ -617,6 +642,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   // Every role first finds its place in the work, then waits for the kernel in front.
   bool met = false;                    // kMeet: this warp has passed the cluster's first barrier
   const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), empty_s = smem_u32(empty);
+  const int test_role = cluster == 0 ? p.test_role : (int)kNoRole;
+  uint32_t issued = 0;                 // k blocks whose copies this CTA's loader asked for
 
   if (warp == 0) {
     // ---- loader
@@ -624,10 +651,10 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     train_pdl_wait();
     const uint32_t full0 = CG == 2 ? map_to(full, 0) : full_s;          // the first CTA's barriers count both CTAs' bytes
     const uint32_t tx = CG * (p.box_a * 128 + S::kBBytes);
-    uint32_t s = 0, turn = 0, it = 0;
-    bool ok = true;
-    for (; !w.done(); w.next(p), ++it) {
-      if (!lin_wait_all(empty_s + 8 * s, empty + s, turn ^ 1, abort_flag)) { ok = false; break; }
+    uint32_t s = 0, turn = 0;
+    const uint32_t stop = test_role == (rank == 0 ? (int)kLoader0 : (int)kLoader1) ? p.test_after : 0xffffffffu;
+    for (; !w.done(); w.next(p), ++issued) {
+      if (issued == stop || !lin_wait_all(empty_s + 8 * s, empty + s, turn ^ 1, abort_flag)) break;
       const uint32_t a = base_s + s * S::kStage, b = a + S::kABytes, bar = full0 + 8 * s;
       const int k0 = w.kb * kLinBK, m0 = (w.m_tile * CG + (int)rank) * kLinBM, n0 = w.n_tile * BN + (int)rank * S::kBNc;
       if (elect_one()) {
@@ -648,11 +675,6 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       __syncwarp();
       if (++s == S::kStages) { s = 0; turn ^= 1; }
     }
-    if (!ok && rank == 0 && lane == 0) {            // copies in flight land before the CTA's memory goes away
-      const uint32_t limit = wait_limit_of(abort_flag);
-      for (uint32_t j = it > (uint32_t)S::kStages ? it - S::kStages : 0; j < it; ++j)
-        for (uint32_t i = 0; i < limit && !mbar_try(full + j % S::kStages, (j / S::kStages) & 1); ++i) {}
-    }
     __syncwarp();
   } else if (warp == 1) {
     // ---- MMA issue: the cluster's first CTA
@@ -663,12 +685,14 @@ linear_kernel(const __grid_constant__ LinProblem p) {
                              ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((kLinBM * CG) >> 4) << 24);
       const uint64_t ad0 = lin_desc<OA != kOpK>(base_s), bd0 = lin_desc<OB != kOpK>(base_s + S::kABytes);
       const uint32_t d_full_s = smem_u32(d_full), d_empty_s = smem_u32(d_empty);
-      uint32_t s = 0, turn = 0, db = 0, dturn = 0;
+      uint32_t s = 0, turn = 0, db = 0, dturn = 0, until = test_role == kMma ? p.test_after : 0xffffffffu;
       bool ok = true;
       LinWalk w(p, cluster, clusters, part_of);
+      train_pdl_wait();
       for (; !w.done() && ok; w.next_tile(p)) {
         uint32_t left = 0, d = 0, more = 0;         // k blocks until the accumulator changes; its first product starts the sum
         for (int kb = w.kb; kb < w.kb_end; ++kb) {
+          if (until-- == 0) { ok = false; break; }
           if (left == 0) {
             if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
             lin_fence_after();
@@ -866,8 +890,30 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   if (CG == 1 && meet > 1 && !met) cluster_sync_all();
   lin_fence_before();
   __syncthreads();
-  if (tid == 0 && *abort_flag && p.status) atomicOr(p.status, kStatusTimeout);
-  if (CG == 2 || meet > 1) cluster_sync_all();      // the sums have arrived; no CTA leaves while another may still signal its barriers
+  // No CTA leaves while copies into its memory are in flight, or while another may still signal its barriers: of a pair, `fin` is the
+  // last thing that the MMAs signal in both CTAs (it has come when the roles have met above, unless they gave up).
+  if (tid == 0) {
+    const uint32_t limit = wait_limit_of(abort_flag), gave_up = *abort_flag ? 1u : 0u;
+    if (gave_up && p.status) atomicOr(p.status, kStatusTimeout);
+    if constexpr (CG == 2) {
+      for (uint32_t i = 0; i < limit && !mbar_try(fin, 0); ++i) {}
+      for (uint32_t r = 0; r < 2; ++r)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to((const void*)(ends + rank), r)), "r"(2 * issued + gave_up) : "memory");
+    } else if (gave_up) {
+      lin_drain(full, S::kStages, issued, limit);
+    }
+  }
+  __syncwarp();
+  if (CG == 2 || meet > 1) cluster_sync_all();      // the sums have arrived
+  if constexpr (CG == 2) {
+    const uint32_t first = ends[0], second = ends[1];
+    if ((first | second) & 1) {
+      if (tid == 0 && rank == 0)
+        lin_drain_pair(full, S::kStages, first >> 1, second >> 1, p.box_a * 128 + S::kBBytes, wait_limit_of(abort_flag));
+      __syncwarp();
+      cluster_sync_all();
+    }
+  }
   if (CG == 1 && meet > 1) {
     // ---- the CTAs' sums of one tile have met: a warp takes a row of this CTA's slice, a lane four of its columns
     train_pdl_wait();                               // (the warps that had no need to yet)
