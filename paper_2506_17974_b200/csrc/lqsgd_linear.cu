@@ -233,6 +233,11 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
   TRAIN_CK(cudaGetDevice(&dev), "cudaGetDevice");
   if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
     TRAIN_CK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem), "cudaFuncSetAttribute(linear_kernel)");
+    if (S::kMoveRegs) {                                      // the epilogue's warps would wait for registers that nobody brought
+      cudaFuncAttributes fa;
+      TRAIN_CK(cudaFuncGetAttributes(&fa, kernel), "cudaFuncGetAttributes(linear_kernel)");
+      if (fa.numRegs * S::kThreads < S::kRegsAll) return record_cuda_failure(cudaErrorInvalidConfiguration, "registers of linear_kernel");
+    }
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   q.box_a = OA == kOpK ? (uint32_t)std::min<int64_t>(kLinBM, ceil_div64(p.M, 8) * 8) : kLinBM;
@@ -280,6 +285,7 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   q.M = (int32_t)p.M; q.N = (int32_t)p.N; q.K = (int32_t)p.K;
   q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total;
   q.deal = p.deal; q.share = p.share; q.meet = p.meet;
+  q.chunk = pair_chunk(p.kb_total);
   q.dtype = a.dtype;
   q.status = a.dev_status;
   q.test_limit = test.limit; q.test_after = test.after; q.test_role = test.role;

@@ -60,6 +60,7 @@ struct alignas(64) LinProblem {
   int32_t deal;                        // how the work is dealt out (LinDeal), see LinWalk
   int32_t share;                       // k blocks per cluster (kShares) or per CTA of a cluster (kMeet)
   int32_t meet;                        // CTAs that sum one tile (kMeet)
+  int32_t chunk;                       // k blocks that an accumulator takes, for pairs with results in 16 bits (pair_chunk)
   int32_t dtype;                       // of the operands
   uint32_t box_a;                      // rows of A that TMA brings per stage and CTA: 128, fewer (a multiple of 8) where A has fewer and
                                        // they lie along k; what the stage holds beyond them only meets rows that do not exist
@@ -474,6 +475,25 @@ __device__ __forceinline__ void finish_quad(const LinEpilogue& e, int64_t row, i
   }
 }
 
+// Sums of a row's neighbouring columns: into a piece in the workspace (32-byte aligned), into the shared memory of a CTA of the cluster.
+template <int N>
+__device__ __forceinline__ void store_sums(float* o, const float (&v)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; c += 8) {
+    uint32_t u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[c + j]);
+    st_global_32(o + c, u);
+  }
+}
+template <int N>
+__device__ __forceinline__ void to_meeting(uint32_t o, const float (&v)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; c += 4)
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                 ::"r"(o + 4 * c), "f"(v[c]), "f"(v[c + 1]), "f"(v[c + 2]), "f"(v[c + 3]) : "memory");
+}
+
 // a / b for a < 2^31, b >= 1: in floating point and put right, where 32-bit integer division is a long chain.
 __device__ __forceinline__ uint32_t quick_div(uint32_t a, uint32_t b) {
   if (a >= (1u << 22)) return a / b;
@@ -556,6 +576,20 @@ __device__ __forceinline__ int meet_slice(const LinProblem& p, const LinWalk& w,
   return (int)quick_div(min(kLinBM, p.M - w.m_tile * kLinBM) + meet - 1, meet);
 }
 
+// The tensor core's accumulator is cut toward zero at every step (K = 16) that it adds, so that its error grows with their number:
+// in relative 2-norm 3.4e-7 at 256 terms, 1.25e-6 at 1024, 2.4e-6 at 2048, 1.4e-5 at 16384 and 5.7e-5 at 65536 (fp32 products on
+// the CUDA cores, of normally distributed values: 2.8e-7, 5.6e-7, 8e-7, 2.3e-6, 4.6e-6).  So an accumulator takes `chunk` k blocks of
+// 64 terms, and the epilogue warps add these sums up in registers, rounding to nearest, while the next one grows: the error stays
+// that of one accumulator, however long the sum.
+// Weight gradients and tiles of single SMs: 1024 terms.  8192 rows, 16384 x 4096: 695 us so, as without (512 rows: 737 us; 2048: 715);
+// 7 x 16384 x 4096 takes 27.5 us (27.4 without).
+// Pairs, results in 16 bits: the MMAs can run two accumulators ahead of an epilogue, which takes about 10 us with GELU and an 8-bit
+// copy, so shorter ones make them wait: 8192 x 4096 x 16384 took 815 us without, 827 with 1536 terms, 864 with 1280 and 961 with
+// 1024 (its gradient of the input, with a residual: 802, 803, 805 and 878).  Sums of up to 2048 terms stay whole: the epilogue reads
+// them from tensor memory piece by piece (4096 x 2048 x 4096 with GELU and both 8-bit copies: 72 us, 82 in two accumulators).
+constexpr int kChunk = 16;
+inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 24; }
+
 // WF32: the result is fp32 (a weight gradient).
 template <int CG, int BN, int OA, int OB, bool WF32>
 struct LinCfg {
@@ -564,14 +598,12 @@ struct LinCfg {
   static constexpr uint32_t kStage = kABytes + ((kBBytes + 1023) / 1024 * 1024);
   // Two warps per quarter of tensor memory: GELU and the 8-bit form take as long as the product of a 4096-wide layer with one.
   static constexpr int kEpiWarps = 8;
-  // A weight gradient is a sum over thousands of rows, and the tensor core's accumulator is cut toward zero at every step
-  // (K = 16) that it adds, so that its error grows with their number: 2.3e-7 in relative 2-norm at 256 rows, 1.0e-6 at 1024,
-  // 2.8e-6 for 8192 activations of the large layer (an fp32 product on the CUDA cores: 3.1e-7).  So it takes kChunk k blocks =
-  // 1024 rows at a time, and the epilogue warps add these sums up in registers, rounding to nearest, while the next one grows:
-  // 2.0e-7 there, and never above 1.0e-6.  8192 x 16384 x 4096 takes 695 us so, as without (512 rows: 737 us; 2048: 715).
-  static constexpr int kChunk = WF32 ? 16 : 1 << 30;
   static constexpr int kMine = BN / (kEpiWarps / 4);                      // columns per epilogue warp
   static constexpr int kThreads = (4 + kEpiWarps) * 32;
+  // With 128 sums of a long chain in registers the epilogue of a layer needs more of them than the 168 that every thread starts with
+  // (75 of them spilled, 8192 x 4096 x 16384 took 990 us instead of 840): the first four warps hand some over.
+  static constexpr bool kMoveRegs = CG == 2 && !WF32;
+  static constexpr int kRegsFront = 56, kRegsEpi = 224, kRegsAll = 128 * kRegsFront + 32 * kEpiWarps * kRegsEpi;   // the launch has to bring these
   static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2 + kMine * 4, kScratch = kEpiWarps * kScratchWarp;
   static constexpr uint32_t kRoom = 225u * 1024 - kScratch;
   static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
@@ -585,6 +617,7 @@ struct LinCfg {
   static constexpr int kMeetPitch = BN + 4;
   static_assert(kSmem <= 227 * 1024 && kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "one CTA per SM");
   static_assert(OB == kOpK || kBNc % 64 == 0, "MN-major operands come in blocks of 64");
+  static_assert(!kMoveRegs || kRegsAll <= kThreads * 168, "the launch brings 168 per thread");
   static_assert(CG == 2 || BN == 128, "a warp finishes a row of a tile");
   static_assert(CG == 2 || (kLinBM + 7) * kMeetPitch * 4 <= kStages * kStage, "a tile, in up to 8 slices, fits in the operand stages");
 };
@@ -639,13 +672,16 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   lin_fence_after();
   const uint32_t tmem = *tmem_slot;
   train_pdl_trigger();
+  const int chunk = CG == 2 && !WF32 ? p.chunk : kChunk;
   // Every role first finds its place in the work, then waits for the kernel in front.
   bool met = false;                    // kMeet: this warp has passed the cluster's first barrier
   const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), empty_s = smem_u32(empty);
   const int test_role = cluster == 0 ? p.test_role : (int)kNoRole;
   uint32_t issued = 0;                 // k blocks whose copies this CTA's loader asked for
 
-  if (warp == 0) {
+  if (warp < 4) {
+    if constexpr (S::kMoveRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kRegsFront));
+    if (warp == 0) {
     // ---- loader
     LinWalk w(p, cluster, clusters, part_of);
     train_pdl_wait();
@@ -697,7 +733,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
             if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
             lin_fence_after();
             d = tmem + db * BN;
-            left = min(S::kChunk, w.kb_end - kb);
+            left = min(chunk, w.kb_end - kb);
             more = 0;
           }
           if (!lin_wait_all(full_s + 8 * s, full + s, turn, abort_flag)) { ok = false; break; }
@@ -728,7 +764,9 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       }
     }
     __syncwarp();
-  } else if (warp >= 4) {
+    }
+  } else {
+    if constexpr (S::kMoveRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kRegsEpi));
     // ---- epilogue: a warp reads its quarter of the accumulator's rows (warp % 4), and with eight warps half of its columns
     uint32_t seq = 0;                                                     // accumulators taken so far
     bool ok = true;
@@ -795,60 +833,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           met = true;
         }
       };
-      if constexpr (WF32) {
-        float acc[S::kMine];
-#pragma unroll
-        for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
-        const int chunks = (w.kb_end - w.kb + S::kChunk - 1) / S::kChunk;
-#pragma unroll 1
-        for (int k = 0; k < chunks; ++k) {
-          const uint32_t taddr = open();
-          if (!ok) break;
-#pragma unroll
-          for (int c = 0; c < S::kMine; c += 16) {
-            float v[16];
-            tmem_ld16(taddr + c, v);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
-          }
-          hand_back();
-        }
-        if (!ok) break;
-        meet_first();
-        if (CG == 1 && meet > 1) {
-          if (m < p.M) {
-            const uint32_t o = map_to(to_slice + c0, to);
-#pragma unroll
-            for (int c = 0; c < S::kMine; c += 4)
-              asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
-                           ::"r"(o + 4 * c), "f"(acc[c]), "f"(acc[c + 1]), "f"(acc[c + 2]), "f"(acc[c + 3]) : "memory");
-          }
-        } else if (part || (p.ep.vec_out && n0 + c0 + S::kMine <= p.N)) {
-          const bool add = !part && p.ep.accumulate;
-          const int vec = part ? 2 : p.ep.vec_out;
-          float* o = part ? part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0            // [row of the tile][BN]
-                          : static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
-          if (m < p.M && n0 + c0 < p.N) {
-#pragma unroll
-            for (int c = 0; c < S::kMine; c += 8) {
-              uint32_t u[8];
-              if (add) {
-                ld_row32(o + c, vec, u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
-              st_row32(o + c, vec, u);
-            }
-          }
-        } else if (m - lane < p.M) {
-#pragma unroll
-          for (int c = 0; c < S::kMine; c += 8)
-            if (n0 + c0 + c < p.N) finish_ragged_f32(p.ep, m - lane, n0 + c0 + c, acc + c, scratch);
-        }
-        __syncwarp();
-      } else {
+      if (!WF32 && w.kb_end - w.kb <= chunk && !part) {          // one accumulator has the whole sum: piece by piece from tensor memory
         const uint32_t taddr = open();
         if (!ok) break;
         meet_first();
@@ -858,32 +843,71 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           tmem_ld32(taddr + c, v);
           if (c + 32 >= S::kMine) hand_back();
           if (CG == 1 && meet > 1) {
-            if (m < p.M) {
-              const uint32_t o = map_to(to_slice + c0 + c, to);
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
-                             ::"r"(o + 16 * i), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
-            }
-            __syncwarp();
-            continue;
-          }
-          if (n0 + c0 + c >= p.N || m - lane >= p.M) continue;
-          if (part) {
-            float* o = part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0 + c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t u[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * i + j]);
-              st_global_32(o + 8 * i, u);
-            }
-          } else {
+            if (m < p.M) to_meeting(map_to(to_slice + c0 + c, to), v);
+          } else if (n0 + c0 + c < p.N && m - lane < p.M) {
             finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
-            __syncwarp();
           }
+          __syncwarp();
+        }
+        continue;
+      }
+      float acc[S::kMine];
+#pragma unroll
+      for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
+#pragma unroll 1
+      for (int left = w.kb_end - w.kb; left > 0; left -= chunk) {
+        const uint32_t taddr = open();
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < S::kMine; c += 16) {
+          float v[16];
+          tmem_ld16(taddr + c, v);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
+        }
+        hand_back();
+      }
+      if (!ok) break;
+      meet_first();
+      if (CG == 1 && meet > 1) {
+        if (m < p.M) to_meeting(map_to(to_slice + c0, to), acc);
+      } else if (part) {
+        if (m < p.M && n0 + c0 < p.N) store_sums(part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0, acc);
+      } else if constexpr (WF32) {
+        if (p.ep.vec_out && n0 + c0 + S::kMine <= p.N) {
+          float* o = static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
+          if (m < p.M) {
+#pragma unroll
+            for (int c = 0; c < S::kMine; c += 8) {
+              uint32_t u[8];
+              if (p.ep.accumulate) {
+                ld_row32(o + c, p.ep.vec_out, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
+              st_row32(o + c, p.ep.vec_out, u);
+            }
+          }
+        } else if (m - lane < p.M) {
+#pragma unroll
+          for (int c = 0; c < S::kMine; c += 8)
+            if (n0 + c0 + c < p.N) finish_ragged_f32(p.ep, m - lane, n0 + c0 + c, acc + c, scratch);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < S::kMine; c += 32) {
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = acc[j];
+#pragma unroll
+          for (int j = 32; j < S::kMine; ++j) acc[j - 32] = acc[j];      // the next piece's: one copy of the epilogue's code, registers by number
+          if (n0 + c0 + c < p.N && m - lane < p.M) finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
+          __syncwarp();
         }
       }
+      __syncwarp();
     }
   }
   __syncwarp();
