@@ -5,6 +5,8 @@
     pack8 / unpack8 / act_grad                         activations kept in 8 bits until the backward pass
     group_norm / group_norm_grad                       group norm with an activation, channels last
 
+A tensor given as `out` is written in place, which autograd is told.
+
 Argument marshalling only, as in binding.py: tensors are checked here for type, device and layout, everything else by the
 library; the arithmetic runs in its CUDA kernels, on the current stream of the tensors' device.  `linear_layer` and
 `norm_layer` are the same operators as differentiable functions that keep only 8-bit activations between the passes.
@@ -18,6 +20,7 @@ from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import binding as B
 
@@ -148,6 +151,14 @@ def _call(fn, args: tuple, layout: struct.Struct, bytes_fn, which: int, device: 
         B._check(rc)
 
 
+def _written(*tensors: torch.Tensor) -> None:
+    """Tells autograd that a caller's tensors were written in place: a backward pass that saved one then raises, as after
+    PyTorch's own in-place operators (tensors of inference mode have no such history)."""
+    for t in tensors:
+        if not t.is_inference():
+            increment_version(t)
+
+
 def _empty(rows: int, cols: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
     return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
 
@@ -231,14 +242,17 @@ def pack8(x: torch.Tensor, out: Optional[Packed8] = None) -> Packed8:
             return pack8(x, out)
     xp, xl = _matrix(x, "x", dev)
     rows, cols = x.shape
-    if out is None:
+    given = out is not None
+    if given:
+        of = _kept(out, "out", dev, rows, cols)
+    else:
         out = Packed8.empty(rows, cols, x.device)
         of = out._fresh()
-    else:
-        of = _kept(out, "out", dev, rows, cols)
     rc = _library().lqsgd_pack8(xp, xl, _dtype(x, "x"), rows, cols, _PACKED8.pack(*of), _stream(dev))
     if rc:
         B._check(rc)
+    if given:
+        _written(out.codes, out.exps)
     return out
 
 
@@ -252,13 +266,14 @@ def unpack8(p: Packed8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch
     rows, cols = codes.shape
     if dtype not in DTYPES:
         raise ValueError(f"dtype must be one of {list(DTYPES)}")
-    if out is None:
-        out = _empty(rows, cols, dtype, codes.device)
-    yp, yl = _matrix(out, "out", dev, dtype, rows, cols)
+    y = _empty(rows, cols, dtype, codes.device) if out is None else out
+    yp, yl = _matrix(y, "out", dev, dtype, rows, cols)
     rc = _library().lqsgd_unpack8(_PACKED8.pack(*p.fields()), rows, cols, yp, yl, DTYPES[dtype], _stream(dev))
     if rc:
         B._check(rc)
-    return out
+    if out is not None:
+        _written(out)
+    return y
 
 
 def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_grad: bool = True,
@@ -293,6 +308,8 @@ def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_gr
         rc = lib.lqsgd_act_grad(yp, yl, zf, a, dt, rows, cols, dp, dl, bp, ws.data_ptr(), ws.numel(), stream)
     if rc:
         B._check(rc)
+    if dp and out is not None:
+        _written(out)
     return dz, db
 
 
@@ -331,6 +348,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
            0 if bias is None else _vector(bias, "bias", dev, cout), rp, rl, yp, yl, *_NONE8,
            *(z8._fresh() if save_z8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8), _status_word(device)),
           _LINEAR, lib.lqsgd_linear_workspace_bytes, FORWARD, device)
+    if out is not None:
+        _written(out)
     return LinearOut(y, z8, y8)
 
 
@@ -356,6 +375,8 @@ def linear_grad_input(dz: torch.Tensor, w: torch.Tensor, residual: Optional[torc
           (_LINEAR.size, _dtype(dz, "dz", True), 0, 0, rows, cin, cout, 0, 0, wp, wl, zp, zl, 0, rp, rl, op, ol, *_NONE8, *_NONE8, *_NONE8,
            _status_word(device)),
           _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_INPUT, device)
+    if out is not None:
+        _written(out)
     return dx
 
 
@@ -386,6 +407,8 @@ def linear_grad_weight(dz: torch.Tensor, x: Union[torch.Tensor, Packed8], out: O
           (_LINEAR.size, _dtype(dz, "dz", True), 0, int(accumulate), rows, cin, cout, xp, xl, 0, 0, zp, zl, 0, 0, 0, op, ol,
            *xf, *_NONE8, *_NONE8, _status_word(device)),
           _LINEAR, lib.lqsgd_linear_workspace_bytes, GRAD_WEIGHT, device)
+    if out is not None:
+        _written(out)
     return dw
 
 
