@@ -279,7 +279,7 @@ def unpack8(p: Packed8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch
 def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_grad: bool = True,
              out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(dz, db): dz = dy act'(z) with z from its 8-bit form, db its column sums in float32 (None without bias_grad).
-    With act "none" dz is dy itself.  `out` may be dy."""
+    `out` may be dy.  With act "none" dz is dy itself, or `out`, to which dy is copied."""
     dev = dy.get_device()
     if _elsewhere(dev):
         with torch.cuda.device(dev):
@@ -290,6 +290,7 @@ def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_gr
     dz, dp, dl, zf = dy, 0, 0, None
     if a:
         zf = _PACKED8.pack(*_kept(z8, "z8", dev, rows, cols))
+    if a or (out is not None and out is not dy):
         dz = _empty(rows, cols, dy.dtype, dy.device) if out is None else out
         dp, dl = _matrix(dz, "out", dev, dy.dtype, rows, cols)
     elif not bias_grad:

@@ -1,4 +1,4 @@
-"""Tensors given as `out` are written in place, and autograd has to learn of it."""
+"""Tensors given as `out` are written in place: autograd has to learn of it, and the result has to be there."""
 import pytest
 import torch
 
@@ -47,3 +47,18 @@ def test_out_under_inference_mode():
         x, w = randn(32, 64, seed=1, dtype=BF), randn(64, 64, seed=2, dtype=BF)
         out = torch.empty(32, 64, dtype=BF, device=DEV)
         assert torch.equal(tr.linear(x, w, out=out).y, tr.linear(x, w).y)
+
+
+@pytest.mark.parametrize("bias_grad", [False, True])
+@pytest.mark.parametrize("cols", [64, 67])
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_act_grad_without_an_activation_fills_out(bias_grad, cols, dtype):
+    dy = randn(33, cols, seed=1, dtype=dtype)
+    out = torch.zeros_like(dy)
+    dz, db = tr.act_grad(dy, None, "none", bias_grad=bias_grad, out=out)
+    assert dz.data_ptr() == out.data_ptr() and torch.equal(out, dy)
+    assert (db is None) == (not bias_grad)
+    if bias_grad:
+        assert torch.equal(db, tr.act_grad(dy, None, "none")[1])
+    with pytest.raises(ValueError):
+        tr.act_grad(dy, None, "none", out=torch.zeros(33, cols + 1, dtype=dtype, device=DEV))
