@@ -509,40 +509,48 @@ def _apart(t: torch.Tensor) -> torch.Tensor:
 
 class _LinearLayer(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, act, x8):
+    def forward(ctx, x, weight, bias, residual, act, x8, recording):
         x, w = _apart(x), _apart(weight.to(x.dtype))
         residual = residual if residual is None else _apart(residual)
-        r = linear(x, w, bias, act, residual, save_z8=act != "none")
-        x8 = pack8(x) if x8 is None else x8
-        saved = [w, x8.codes, x8.exps] + ([r.z8.codes, r.z8.exps] if r.z8 is not None else [])
-        ctx.save_for_backward(*saved)
-        ctx.act, ctx.has_bias, ctx.has_residual = act, bias is not None, residual is not None
+        for_x, for_w, for_bias = (n and recording for n in ctx.needs_input_grad[:3])
+        r = linear(x, w, bias, act, residual, save_z8=act != "none" and (for_x or for_w or for_bias))
+        if for_w and x8 is None:
+            x8 = pack8(x)
+        kept = (x8 if for_w else None), r.z8
+        ctx.save_for_backward(w if for_x else None, *(t for p in kept for t in ((p.codes, p.exps) if p is not None else (None, None))))
+        ctx.act = act
         return r.y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        w, xc, xe, *z = ctx.saved_tensors
+        w, xc, xe, zc, ze = ctx.saved_tensors
+        for_x, for_w, for_bias, for_residual = ctx.needs_input_grad[:4]
         dy = _apart(dy)
-        dz, db = act_grad(dy, Packed8(*z) if z else None, ctx.act, bias_grad=ctx.has_bias and ctx.needs_input_grad[2])
-        dx = linear_grad_input(dz, w) if ctx.needs_input_grad[0] else None
-        dw = linear_grad_weight(dz, Packed8(xc, xe)) if ctx.needs_input_grad[1] else None
-        return dx, dw, db, (dy if ctx.has_residual else None), None, None
+        dx = dw = db = None
+        if for_x or for_w or for_bias:
+            dz, db = act_grad(dy, None if zc is None else Packed8(zc, ze), ctx.act, bias_grad=for_bias)
+            dx = linear_grad_input(dz, w) if for_x else None
+            dw = linear_grad_weight(dz, Packed8(xc, xe)) if for_w else None
+        return dx, dw, db, (dy if for_residual else None), None, None, None
 
 
 def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
                  residual: Optional[torch.Tensor] = None, x8: Optional[Packed8] = None) -> torch.Tensor:
     """linear() as a differentiable function: weight and bias float32 (the weights a round updates; the products run in x's
     type), x and the pre-activation kept in 8 bits, the weight gradient float32.  x8: x's 8-bit form where it exists
-    already (norm_layer and other producers can hand it on).  Differentiable once: a second derivative raises."""
-    return _LinearLayer.apply(x, weight, bias, residual, act, x8)
+    already (norm_layer and other producers can hand it on).  Kept is what the wanted gradients need: nothing under no_grad, no x
+    where the weight is frozen.  Differentiable once: a second derivative raises."""
+    return _LinearLayer.apply(x, weight, bias, residual, act, x8, torch.is_grad_enabled())
 
 
 class _NormLayer(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, gamma, beta, groups, eps, act, keep):
-        r = group_norm(_apart(x), groups, gamma, beta, eps, act, save_x8=True, save_y8=keep is not None)
-        ctx.save_for_backward(r.x8.codes, r.x8.exps, gamma, beta, r.mean, r.rstd)
+    def forward(ctx, x, gamma, beta, groups, eps, act, keep, recording):
+        wanted = recording and any(ctx.needs_input_grad[:3])
+        r = group_norm(_apart(x), groups, gamma, beta, eps, act, save_x8=wanted, save_y8=keep is not None)
+        if wanted:
+            ctx.save_for_backward(r.x8.codes, r.x8.exps, gamma, beta, r.mean, r.rstd)
         ctx.groups, ctx.act = groups, act
         if keep is not None:
             keep.append(r.y8)
@@ -553,11 +561,11 @@ class _NormLayer(torch.autograd.Function):
     def backward(ctx, dy):
         codes, exps, gamma, beta, mean, rstd = ctx.saved_tensors
         dx, dgamma, dbeta = group_norm_grad(dy.contiguous(), Packed8(codes, exps), ctx.groups, gamma, beta, mean, rstd, ctx.act)
-        return dx, dgamma, dbeta, None, None, None, None
+        return dx, dgamma, dbeta, None, None, None, None, None
 
 
 def norm_layer(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, groups: int, eps: float = 1e-5, act: str = "none",
                keep: Optional[list] = None) -> torch.Tensor:
     """group_norm() as a differentiable function with x kept in 8 bits.  `keep`, a list, receives the output's 8-bit form
     (for the linear layer that follows).  Differentiable once: a second derivative raises."""
-    return _NormLayer.apply(x, gamma, beta, groups, eps, act, keep)
+    return _NormLayer.apply(x, gamma, beta, groups, eps, act, keep, torch.is_grad_enabled())
