@@ -494,6 +494,6 @@ extern "C" int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_pac
              : launch_act_grad<LQSGD_F32, false>(act, grid, st, d, dev_dy, ld_dy, vg, z8, vc, dev_dz, ld_dz, vz, partial);
   TRAIN_CK(e, "act_grad_kernel launch");
   if (partial != dev_db)
-    TRAIN_CK(train_launch(join_columns_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, 1, partial, (int)grid.y, cols, dev_db), "join_columns_kernel launch");
+    TRAIN_CK(train_launch(join_columns_kernel, dim3((unsigned)ceil_div64(cols, 32)), dim3(1024), 0, st, 1, partial, (int)grid.y, cols, dev_db), "join_columns_kernel launch");
   return LQSGD_OK;
 }

@@ -18,7 +18,7 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Checks of an 8-bit matrix argument whose codes are set.
 inline int check_packed8(const lqsgd_packed8& p, int32_t cols) {
   if (!p.dev_codes || !p.dev_exps) return LQSGD_ERR_INVALID_ARG;
-  if (p.ld_codes < cols || p.ld_exps < (cols + LQSGD_PACK8_GROUP - 1) / LQSGD_PACK8_GROUP) return LQSGD_ERR_INVALID_ARG;
+  if (p.ld_codes < cols || p.ld_exps < ceil_div64(cols, LQSGD_PACK8_GROUP)) return LQSGD_ERR_INVALID_ARG;
   return LQSGD_OK;
 }
 
