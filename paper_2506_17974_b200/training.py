@@ -178,8 +178,10 @@ def _status_word(device: torch.device) -> int:
 
 
 def status(device: Union[str, int, torch.device] = "cuda:0") -> int:
-    """Status bits (binding.STATUS_TIMEOUT) that the linear layers' kernels have raised on a device so far; synchronises."""
-    word = _status.get(torch.device(device).index or 0)
+    """Status bits (binding.STATUS_TIMEOUT) that the linear layers' kernels have raised on a device ("cuda": the current one) so
+    far; synchronises.  Products captured in a graph before the device's first ordinary one have no status word and raise none."""
+    index = torch.device(device).index
+    word = _status.get(torch.cuda.current_device() if index is None else index)
     return 0 if word is None else int(word.item())
 
 
@@ -540,7 +542,8 @@ def linear_layer(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     """linear() as a differentiable function: weight and bias float32 (the weights a round updates; the products run in x's
     type), x and the pre-activation kept in 8 bits, the weight gradient float32.  x8: x's 8-bit form where it exists
     already (norm_layer and other producers can hand it on).  Kept is what the wanted gradients need: nothing under no_grad, no x
-    where the weight is frozen.  Differentiable once: a second derivative raises."""
+    where the weight is frozen.  Differentiable once: a second derivative raises.  Should a bounded wait on the device run out,
+    output and gradients are undefined and status() says so: a training loop asks it where it reads its loss."""
     return _LinearLayer.apply(x, weight, bias, residual, act, x8, torch.is_grad_enabled())
 
 
