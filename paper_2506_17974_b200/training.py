@@ -111,19 +111,26 @@ def _elsewhere(device: int) -> bool:
 _stream = torch._C._cuda_getCurrentRawStream
 
 
-# Workspaces up to _KEEP bytes are kept per host thread, device and stream, so that a call in a training step needs no
+# Workspaces up to _KEEP bytes are kept per host thread, device and stream for the life of the thread, so that a call in a training step needs no
 # allocation of its own; larger ones, and those of calls that are being captured in a graph (whose memory has to last as
 # long as the graph), come from PyTorch's allocator for the one call.  Calls of one thread on one stream follow one
 # another, so they may share one; the allocator does not hand out a call's own workspace again before its kernels are done.
 _KEEP = 16 << 20
-_scratch = {}
+
+
+class _Scratch(threading.local):
+    def __init__(self):
+        self.kept = {}
+
+
+_scratch = _Scratch()
 
 
 def _workspace(need: int, device: torch.device, stream: int) -> torch.Tensor:
     if need > _KEEP or torch._C._cuda_isCurrentStreamCapturing():
         return torch.empty_strided((need,), (1,), dtype=torch.uint8, device=device)
     ws = torch.empty_strided((max(need, 1 << 20),), (1,), dtype=torch.uint8, device=device)
-    _scratch[(threading.get_ident(), device.index, stream)] = (ws, ws.data_ptr(), ws.numel())
+    _scratch.kept[(device.index, stream)] = (ws, ws.data_ptr(), ws.numel())
     return ws
 
 
@@ -133,7 +140,7 @@ _NO_SCRATCH = (None, 0, 0)
 def _kept_scratch(index: int, stream: int) -> tuple:
     if torch._C._cuda_isCurrentStreamCapturing():
         return _NO_SCRATCH
-    return _scratch.get((threading.get_ident(), index, stream), _NO_SCRATCH)
+    return _scratch.kept.get((index, stream), _NO_SCRATCH)
 
 
 def _call(fn, args: tuple, layout: struct.Struct, bytes_fn, which: int, device: torch.device) -> None:
