@@ -464,7 +464,7 @@ int lqsgd_act_grad(const void* dev_dy, int64_t ld_dy, const lqsgd_packed8* host_
  * x8 is decoded for the tensor cores (rows x in 16-bit values), and operands whose rows are not 16-byte aligned are copied.
  * A tensor core's accumulator cuts toward zero at every step.  So at most 1024 rows of a weight gradient, at most 2048 terms of
  * the other products are summed in one, and those sums are added in registers: the relative error (2-norm, normally
- * distributed values) stays below 1.3e-6 and 2.5e-6, however long the sum.
+ * distributed values) stays below 1.3e-6 and 2.5e-6 (1.5e-6 beyond 2048 terms), however long the sum.
  * dev_status: NULL, or one device uint32 into which LQSGD_STATUS_TIMEOUT is ORed should a bounded device-side wait run
  * out (the outputs are then undefined). */
 typedef struct lqsgd_linear {

@@ -285,7 +285,7 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   q.M = (int32_t)p.M; q.N = (int32_t)p.N; q.K = (int32_t)p.K;
   q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total;
   q.deal = p.deal; q.share = p.share; q.meet = p.meet;
-  q.chunk = pair_chunk(p.kb_total);
+  q.first_chunk = pair_chunk(p.kb_total);
   q.dtype = a.dtype;
   q.status = a.dev_status;
   q.test_limit = test.limit; q.test_after = test.after; q.test_role = test.role;

@@ -60,7 +60,7 @@ struct alignas(64) LinProblem {
   int32_t deal;                        // how the work is dealt out (LinDeal), see LinWalk
   int32_t share;                       // k blocks per cluster (kShares) or per CTA of a cluster (kMeet)
   int32_t meet;                        // CTAs that sum one tile (kMeet)
-  int32_t chunk;                       // k blocks that an accumulator takes, for pairs with results in 16 bits (pair_chunk)
+  int32_t first_chunk;                 // k blocks that a tile's first two accumulators take, for pairs with results in 16 bits (pair_chunk)
   int32_t dtype;                       // of the operands
   uint32_t box_a;                      // rows of A that TMA brings per stage and CTA: 128, fewer (a multiple of 8) where A has fewer and
                                        // they lie along k; what the stage holds beyond them only meets rows that do not exist
@@ -578,17 +578,20 @@ __device__ __forceinline__ int meet_slice(const LinProblem& p, const LinWalk& w,
 
 // The tensor core's accumulator is cut toward zero at every step (K = 16) that it adds, so that its error grows with their number:
 // in relative 2-norm 3.4e-7 at 256 terms, 1.25e-6 at 1024, 2.4e-6 at 2048, 1.4e-5 at 16384 and 5.7e-5 at 65536 (fp32 products on
-// the CUDA cores, of normally distributed values: 2.8e-7, 5.6e-7, 8e-7, 2.3e-6, 4.6e-6).  So an accumulator takes `chunk` k blocks of
+// the CUDA cores, of normally distributed values: 2.8e-7, 5.6e-7, 8e-7, 2.3e-6, 4.6e-6).  So an accumulator takes a few k blocks of
 // 64 terms, and the epilogue warps add these sums up in registers, rounding to nearest, while the next one grows: the error stays
-// that of one accumulator, however long the sum.
+// about that of one accumulator, however long the sum.
 // Weight gradients and tiles of single SMs: 1024 terms.  8192 rows, 16384 x 4096: 695 us so, as without (512 rows: 737 us; 2048: 715);
 // 7 x 16384 x 4096 takes 27.5 us (27.4 without).
-// Pairs, results in 16 bits: the MMAs can run two accumulators ahead of an epilogue, which takes about 10 us with GELU and an 8-bit
-// copy, so shorter ones make them wait: 8192 x 4096 x 16384 took 815 us without, 827 with 1536 terms, 864 with 1280 and 961 with
-// 1024 (its gradient of the input, with a residual: 802, 803, 805 and 878).  Sums of up to 2048 terms stay whole: the epilogue reads
-// them from tensor memory piece by piece (4096 x 2048 x 4096 with GELU and both 8-bit copies: 72 us, 82 in two accumulators).
-constexpr int kChunk = 16;
-inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 24; }
+// Pairs, results in 16 bits: while an epilogue runs (about 15 us with GELU and an 8-bit copy beside the MMAs) they can fill two
+// accumulators and then wait, so a tile's first two take more, 1344 terms, and the later ones, which are drained at once, 512:
+// error 1.45e-6 at 4096 terms, 1.0e-6 at 16384, 0.8e-6 at 65536.  8192 x 4096 x 16384 took 861 us (842 in one accumulator, 859 with
+// 1536 terms throughout and an error of 1.7e-6, 886 with 1280 first; 1024 throughout: 14 to 18 % more than one, 512: 36 %), its gradient of
+// the input, with a residual, 837 us (828), 4096 x 4096 x 4096 107.6 (105.5).
+// Sums of up to 2048 terms stay whole: the epilogue reads them from tensor memory piece by piece, which is what bounds them
+// (4096 x 2048 x 4096 with GELU and both 8-bit copies: 76 us, 85 in two accumulators; error 2.4e-6 and 1.3e-6).
+constexpr int kChunk = 16, kLaterChunk = 8;
+inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 21; }
 
 // WF32: the result is fp32 (a weight gradient).
 template <int CG, int BN, int OA, int OB, bool WF32>
@@ -672,7 +675,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   lin_fence_after();
   const uint32_t tmem = *tmem_slot;
   train_pdl_trigger();
-  const int chunk = CG == 2 && !WF32 ? p.chunk : kChunk;
+  // k blocks of a tile's n-th accumulator
+  auto chunk = [&](int n) { return CG == 1 || WF32 ? kChunk : n < 2 ? p.first_chunk : kLaterChunk; };
   // Every role first finds its place in the work, then waits for the kernel in front.
   bool met = false;                    // kMeet: this warp has passed the cluster's first barrier
   const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), empty_s = smem_u32(empty);
@@ -726,6 +730,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       LinWalk w(p, cluster, clusters, part_of);
       train_pdl_wait();
       for (; !w.done() && ok; w.next_tile(p)) {
+        int nth = 0;
         uint32_t left = 0, d = 0, more = 0;         // k blocks until the accumulator changes; its first product starts the sum
         for (int kb = w.kb; kb < w.kb_end; ++kb) {
           if (until-- == 0) { ok = false; break; }
@@ -733,7 +738,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
             if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
             lin_fence_after();
             d = tmem + db * BN;
-            left = min(chunk, w.kb_end - kb);
+            left = min(chunk(nth++), w.kb_end - kb);
             more = 0;
           }
           if (!lin_wait_all(full_s + 8 * s, full + s, turn, abort_flag)) { ok = false; break; }
@@ -833,7 +838,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           met = true;
         }
       };
-      if (!WF32 && w.kb_end - w.kb <= chunk && !part) {          // one accumulator has the whole sum: piece by piece from tensor memory
+      if (!WF32 && w.kb_end - w.kb <= chunk(0) && !part) {          // one accumulator has the whole sum: piece by piece from tensor memory
         const uint32_t taddr = open();
         if (!ok) break;
         meet_first();
@@ -855,7 +860,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
 #pragma unroll
       for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
 #pragma unroll 1
-      for (int left = w.kb_end - w.kb; left > 0; left -= chunk) {
+      for (int left = w.kb_end - w.kb, n = 0; left > 0; left -= chunk(n++)) {
         const uint32_t taddr = open();
         if (!ok) break;
 #pragma unroll

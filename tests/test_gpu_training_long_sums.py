@@ -5,6 +5,7 @@ The outputs have 16 bits, too few to show it.  So the residual takes the exact r
 import pytest
 import torch
 
+import test_gpu_training as base
 from paper_2506_17974_b200 import training as tr
 
 pytestmark = pytest.mark.gpu
@@ -32,3 +33,11 @@ def test_long_sums(rows, out, long):
     exact = a.double() @ b.double().t()
     assert error(lambda r: tr.linear(a, b, residual=r).y, exact) <= BOUND
     assert error(lambda r: tr.linear_grad_input(a, b.t().contiguous(), residual=r), exact) <= BOUND
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cin,cout", [(4100, 2500, 4100), (4101, 2504, 4104), (4099, 3401, 4097), (128, 1500, 9000), (127, 1502, 9003)])
+def test_everything_behind_several_accumulators(dtype, rows, cin, cout):
+    """Bias, activation, residual and 8-bit copies of tiles that several accumulators summed, ragged and aligned, pairs and single SMs."""
+    base.test_linear(dtype, rows, cin, cout)
+    base.test_linear_grad_input(dtype, rows, cout, cin)
