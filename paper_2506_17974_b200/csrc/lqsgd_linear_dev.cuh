@@ -8,8 +8,8 @@
 //
 // An operand whose rows hold k ("K-major") is staged as 64 k x R rows; one whose rows hold m or n ("MN-major") as blocks of
 // 64 columns x 64 k: both arrive from TMA with the 128-byte swizzle that the tensor core reads, so nothing is transposed.
-// x kept in 8 bits is decoded to 16 bits (exactly, see lqsgd_pack8) into the workspace ahead of the product: 5 bytes of
-// traffic per value, once.  Decoding inside the product (warps that turn codes into the operand's layout in shared memory)
+// x kept in 8 bits is decoded to 16 bits into the workspace ahead of the product (exactly in bf16; in fp16 values past 65504
+// saturate and those below its normal range round): 5 bytes of traffic per value, once.  Decoding inside the product (warps that turn codes into the operand's layout in shared memory)
 // was built and measured: every row tile decodes x again, and the decoders' shared memory traffic and hand-over take the
 // MMAs' time: 1.37 against 0.86 ms for 8192 rows, 16384 x 4096, and 22.7 against 18.4 us for 65536 rows, 64 x 128.
 //
@@ -599,7 +599,8 @@ struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
   static constexpr uint32_t kStage = kABytes + ((kBBytes + 1023) / 1024 * 1024);
-  // Two warps per quarter of tensor memory: GELU and the 8-bit form take as long as the product of a 4096-wide layer with one.
+  // Two warps per quarter of tensor memory: GELU and the 8-bit form take as long as the product of a 4096-wide layer with one;
+  // with three the sums of a pair's tile no longer fit their registers.
   static constexpr int kEpiWarps = 8;
   static constexpr int kMine = BN / (kEpiWarps / 4);                      // columns per epilogue warp
   static constexpr int kThreads = (4 + kEpiWarps) * 32;
@@ -732,8 +733,10 @@ linear_kernel(const __grid_constant__ LinProblem p) {
       for (; !w.done() && ok; w.next_tile(p)) {
         int nth = 0;
         uint32_t left = 0, d = 0, more = 0;         // k blocks until the accumulator changes; its first product starts the sum
-        for (int kb = w.kb; kb < w.kb_end; ++kb) {
-          if (until-- == 0) { ok = false; break; }
+        const uint32_t run = min((uint32_t)(w.kb_end - w.kb), until);
+        const int stop = w.kb + (int)run;
+        until -= run;
+        for (int kb = w.kb; kb < stop; ++kb) {
           if (left == 0) {
             if (!lin_wait_all(d_empty_s + 8 * db, d_empty + db, dturn ^ 1, abort_flag)) { ok = false; break; }
             lin_fence_after();
@@ -760,6 +763,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
             if (db == 0) dturn ^= 1;
           }
         }
+        ok = ok && stop == w.kb_end;
       }
       if (elect_one()) lin_commit<CG>(smem_u32(fin));   // every MMA has completed before tensor memory is released
       __syncwarp();
