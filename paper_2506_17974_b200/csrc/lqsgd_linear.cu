@@ -276,8 +276,8 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   auto rows_vec = [&](const void* q, int64_t ld) { return rows_aligned(q, ld, 32) ? 2 : rows_aligned(q, ld, 16) ? 1 : 0; };
   ep.vec_out = rows_vec(ep.out, ep.ld_out * es);
   ep.vec_res = rows_vec(ep.residual, ep.ld_res * 2);
-  ep.vec_z8 = rows_aligned(ep.z8.dev_codes, ep.z8.ld_codes, 16);
-  ep.vec_y8 = rows_aligned(ep.y8.dev_codes, ep.y8.ld_codes, 16);
+  ep.vec_z8 = rows_vec(ep.z8.dev_codes, ep.z8.ld_codes);
+  ep.vec_y8 = rows_vec(ep.y8.dev_codes, ep.y8.ld_codes);
   LinProblem q;
   std::memset(&q, 0, sizeof(q));
   q.ep = ep;

@@ -47,8 +47,7 @@ struct LinEpilogue {
   int32_t dtype;                       // of out and residual; LQSGD_F32: out is fp32 and residual is not used
   int32_t act;
   int32_t accumulate;                  // fp32 out only: add to what is there
-  int32_t vec_out, vec_res;            // rows are aligned to 32 bytes (2), to 16 bytes (1), to neither (0)
-  int32_t vec_z8, vec_y8;              // rows are aligned to 16 bytes
+  int32_t vec_out, vec_res, vec_z8, vec_y8;   // rows are aligned to 32 bytes (2), to 16 bytes (1), to neither (0)
 };
 
 struct alignas(64) LinProblem {
@@ -233,32 +232,6 @@ __device__ __forceinline__ void ld_global_32(const void* p, uint32_t (&w)[8]) {
                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
 }
 
-// Eight-bit form of 32 values of one row in one thread (those from `have` on must be 0): the exponent byte and 8 code words.
-__device__ __forceinline__ int encode32(const float (&v)[32], uint32_t (&w)[8]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-  const int eb = exp_byte(__uint_as_float(top));
-  const float inv = inv_step(eb);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = code_word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
-  return eb;
-}
-__device__ __forceinline__ void put_packed(const lqsgd_packed8& p, bool vec, int64_t row, int col, int have, const float (&v)[32]) {
-  uint32_t w[8];
-  const int eb = encode32(v, w);
-  uint8_t* c = p.dev_codes + row * p.ld_codes + col;
-  if (vec && have == 32) {
-    *reinterpret_cast<uint4*>(c) = make_uint4(w[0], w[1], w[2], w[3]);
-    *(reinterpret_cast<uint4*>(c) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < have) c[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-  }
-  p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
-}
-
 // 32 bytes of a row that is aligned to 32 (vec = 2) or 16 bytes (vec = 1)
 __device__ __forceinline__ void ld_row32(const void* p, int vec, uint32_t (&w)[8]) {
   if (vec == 2) {
@@ -276,6 +249,32 @@ __device__ __forceinline__ void st_row32(void* p, int vec, const uint32_t (&w)[8
     *(static_cast<uint4*>(p) + 1) = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
+
+// Eight-bit form of 32 values of one row in one thread (those from `have` on must be 0): the exponent byte and 8 code words.
+__device__ __forceinline__ int encode32(const float (&v)[32], uint32_t (&w)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  const int eb = exp_byte(__uint_as_float(top));
+  const float inv = inv_step(eb);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = code_word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+  return eb;
+}
+__device__ __forceinline__ void put_packed(const lqsgd_packed8& p, int vec, int64_t row, int col, int have, const float (&v)[32]) {
+  uint32_t w[8];
+  const int eb = encode32(v, w);
+  uint8_t* c = p.dev_codes + row * p.ld_codes + col;
+  if (vec && have == 32) {
+    st_row32(c, vec, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < have) c[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+  p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
+}
+
 // Epilogue of 8 columns of a weight gradient held by a warp, a row per thread (row0: lane 0's row), where rows are not 32-byte
 // aligned or the tile passes the matrix: through the warp's scratch in shared memory (rows of 9 words), so that an access is
 // four rows' 8 columns instead of one column of 32 rows (which costs a sector per element).
@@ -584,14 +583,14 @@ __device__ __forceinline__ int meet_slice(const LinProblem& p, const LinWalk& w,
 // Weight gradients and tiles of single SMs: 1024 terms.  8192 rows, 16384 x 4096: 695 us so, as without (512 rows: 737 us; 2048: 715);
 // 7 x 16384 x 4096 takes 27.5 us (27.4 without).
 // Pairs, results in 16 bits: while an epilogue runs (about 15 us with GELU and an 8-bit copy beside the MMAs) they can fill two
-// accumulators and then wait, so a tile's first two take more, 1344 terms, and the later ones, which are drained at once, 512:
-// error 1.45e-6 at 4096 terms, 1.0e-6 at 16384, 0.8e-6 at 65536.  8192 x 4096 x 16384 took 861 us (842 in one accumulator, 859 with
-// 1536 terms throughout and an error of 1.7e-6, 886 with 1280 first; 1024 throughout: 14 to 18 % more than one, 512: 36 %), its gradient of
-// the input, with a residual, 837 us (828), 4096 x 4096 x 4096 107.6 (105.5).
+// accumulators and then wait, so a tile's first two take more, 1280 terms, and the later ones, which are drained at once, 512:
+// error 1.4e-6 at 4096 terms, 1.0e-6 at 16384, 0.8e-6 at 65536.  8192 x 4096 x 16384 took 917 us (893 in one accumulator, 900 with
+// 1344 first and an error of 1.45e-6, 1010 with 1024), its gradient of the input, with a residual, 831 us (828), 4096 x 4096 x 4096
+// 107.7 (105.5).  512 terms throughout: 36 % more than one accumulator, error 0.65e-6.
 // Sums of up to 2048 terms stay whole: the epilogue reads them from tensor memory piece by piece, which is what bounds them
-// (4096 x 2048 x 4096 with GELU and both 8-bit copies: 76 us, 85 in two accumulators; error 2.4e-6 and 1.3e-6).
+// (4096 x 2048 x 4096 with GELU and both 8-bit copies in two accumulators: 12 % more; error 2.4e-6 and 1.3e-6).
 constexpr int kChunk = 16, kLaterChunk = 8;
-inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 21; }
+inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 20; }
 
 // WF32: the result is fp32 (a weight gradient).
 template <int CG, int BN, int OA, int OB, bool WF32>
