@@ -536,6 +536,98 @@ int lqsgd_group_norm_workspace_bytes(int32_t backward, const lqsgd_group_norm* h
 int lqsgd_group_norm_forward(const lqsgd_group_norm* host_args, void* cuda_stream);
 int lqsgd_group_norm_backward(const lqsgd_group_norm* host_args, void* cuda_stream);
 
+/* Rows of signed 8-bit codes with one scale each: the operands of lqsgd_linear_rows8_forward.  With top = max |x| of a row,
+ *   scale = max(top / 127, 2^-120),  code = rint(x min(127 / top, 2^120))   (halves to even; both divisions rounded once to fp32)
+ * so that |x - scale code| <= scale / 2 up to fp32 rounding for rows with top >= 127 2^-120.  A row with a value that is not
+ * finite has the scale NaN and codes 0: everything computed from it is NaN.  1 byte per value and 4 per row. */
+typedef struct lqsgd_rows8 {
+  int8_t* dev_codes; /* rows x cols */
+  int64_t ld_codes;  /* bytes between rows, >= cols; a multiple of 16 (and a 16-byte aligned base) is read fastest */
+  float* dev_scales; /* rows */
+} lqsgd_rows8;
+
+int lqsgd_pack_rows8(const void* dev_x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols,
+                     const lqsgd_rows8* host_out, void* cuda_stream);
+/* y = scale code, rounded to dtype; past its range its largest finite value.  cols 1 .. 2^24 in both. */
+int lqsgd_unpack_rows8(const lqsgd_rows8* host_in, int64_t rows, int32_t cols, void* dev_y, int64_t ld_y, int32_t dtype,
+                       void* cuda_stream);
+
+/* Dropout from a counter-based generator: the mask is a function of its arguments and never stored, so the backward pass is
+ * the same call on the gradient.  With T = min(rint(65536 p), 65535), a value is kept where its 16 random bits are >= T, and is
+ * then multiplied by 65536 / (65536 - T); the others are exactly 0, whatever they were.  Random bits of row r, column c of a
+ * matrix of `cols` columns: Philox4x32 with 10 rounds (Salmon, Moraes, Dror, Shaw: Parallel Random Numbers, SC11), key
+ * (seed's low word, its high word), counter (b's low word, its high word, offset's low word, its high word) with
+ * b = r ceil(cols / 8) + floor(c / 8); word (c mod 8) / 2, low half for even c, high half for odd c.  The mask does not depend on type,
+ * strides or alignment. */
+typedef struct lqsgd_drop {
+  float p;               /* 0 <= p < 1 */
+  uint32_t reserved;     /* 0 */
+  uint64_t seed, offset; /* an offset not used before with a seed gives a fresh mask */
+  const uint64_t* dev_seed; /* NULL, or two device words read when the kernels run: {seed, what is added to offset}; `seed` is then
+                               not used.  For captured graphs, whose replays would repeat the mask of the capture. */
+} lqsgd_drop;
+
+/* out = residual + dropout(x); residual optional.  out may be x or the residual (then with the same ld). */
+int lqsgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int64_t ld_residual, int32_t dtype, int64_t rows,
+                  int32_t cols, const lqsgd_drop* host_drop, void* dev_out, int64_t ld_out, void* cuda_stream);
+
+/* Root-mean-square norm of rows, with the dropout and the residual's addition in front of it:
+ *   forward   h = residual + dropout(x), rounded to dtype;  rstd = 1 / sqrt(<h^2> + eps);  y = h rstd gamma
+ *             outputs, each optional: h (needed where there is a residual or p > 0; without them h is x), y, h8 = pack8(h),
+ *             y8 = pack8(y as stored), rows8 = pack_rows8(y before its rounding to dtype)
+ *   backward  u = gamma dy,  xh = h rstd,  d = rstd (u - xh <u xh>) + skip  (skip: the gradient that arrives at h from elsewhere)
+ *             dresidual = d,  dx = dropout(d) (the forward call's mask),  dgamma = sum over rows of dy xh
+ *             dx, dresidual (the same as dx where p = 0), dgamma each optional, at least one; h from h8 when its codes are set
+ * < > is the mean over a row.  Squares and sums are held in fp32. */
+typedef struct lqsgd_rms_norm {
+  uint32_t struct_size;   /* sizeof(lqsgd_rms_norm) */
+  int32_t dtype;          /* of all matrices: any lqsgd_dtype */
+  int64_t rows;           /* 0 .. 2^31 - 1 */
+  int32_t cols;           /* 1 .. 2^24 */
+  float eps;              /* forward only, >= 0 */
+  lqsgd_drop drop;
+  const void* dev_x;        int64_t ld_x;         /* forward */
+  const void* dev_residual; int64_t ld_residual;  /* forward, or NULL */
+  const void* dev_dy;       int64_t ld_dy;        /* backward */
+  const void* dev_skip;     int64_t ld_skip;      /* backward, or NULL */
+  void* dev_h;              int64_t ld_h;         /* forward: output; backward: input (only read) unless h8 is given */
+  void* dev_y;              int64_t ld_y;         /* forward */
+  void* dev_dx;             int64_t ld_dx;        /* backward */
+  void* dev_dresidual;      int64_t ld_dresidual; /* backward */
+  const float* dev_gamma;   /* cols */
+  float* dev_rstd;          /* rows: written by the forward call, read by the backward call */
+  float* dev_dgamma;        /* cols (backward) */
+  lqsgd_packed8 h8;         /* forward: output; backward: input */
+  lqsgd_packed8 y8;         /* forward */
+  lqsgd_rows8 rows8;        /* forward */
+  void* dev_workspace;      size_t workspace_bytes;
+} lqsgd_rms_norm;
+int lqsgd_rms_norm_workspace_bytes(int32_t backward, const lqsgd_rms_norm* host_args, size_t* host_bytes_out);
+int lqsgd_rms_norm_forward(const lqsgd_rms_norm* host_args, void* cuda_stream);
+int lqsgd_rms_norm_backward(const lqsgd_rms_norm* host_args, void* cuda_stream);
+
+/* A linear layer's forward product in 8-bit integers, x of shape rows x in and w of shape out x in as rows of signed codes (a scale
+ * per token, a scale per output channel):
+ *   y = act((sum over k of xc wc) sx sw + bias) + residual,  z8 = pack8(the value in front of act),  y8 = pack8(y as stored)
+ * on the tensor cores.  The sum is exact in 32 bits (|code| <= 128 and in <= 131071); the scales are applied in fp32, sx first. */
+typedef struct lqsgd_linear_rows8 {
+  uint32_t struct_size; /* sizeof(lqsgd_linear_rows8) */
+  int32_t dtype;        /* of residual and out: LQSGD_BF16 or LQSGD_F16 */
+  int32_t act;
+  uint32_t reserved;    /* 0 */
+  int64_t rows;         /* 0 .. 2^31 - 512 */
+  int32_t in, out;      /* in 1 .. 131071, out 1 .. 2^24 */
+  lqsgd_rows8 x, w;
+  const float* dev_bias;                         /* out, fp32, or NULL */
+  const void* dev_residual; int64_t ld_residual; /* rows x out, or NULL; may be the output */
+  void* dev_out;        int64_t ld_out;
+  lqsgd_packed8 z8, y8; /* outputs, each optional (NULL codes) */
+  uint32_t* dev_status; /* as of lqsgd_linear */
+  void* dev_workspace;  size_t workspace_bytes;
+} lqsgd_linear_rows8;
+int lqsgd_linear_rows8_workspace_bytes(const lqsgd_linear_rows8* host_args, size_t* host_bytes_out);
+int lqsgd_linear_rows8_forward(const lqsgd_linear_rows8* host_args, void* cuda_stream);
+
 /* Frees the host-side context.  The workspace stays the caller's. */
 void lqsgd_destroy(lqsgd_ctx* ctx);
 

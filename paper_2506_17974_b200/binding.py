@@ -47,6 +47,8 @@ EXPORTED = [
     "lqsgd_pack8", "lqsgd_unpack8", "lqsgd_act_grad_workspace_bytes", "lqsgd_act_grad",
     "lqsgd_linear_workspace_bytes", "lqsgd_linear_forward", "lqsgd_linear_grad_input", "lqsgd_linear_grad_weight", "lqsgd_test_linear_wait",
     "lqsgd_group_norm_workspace_bytes", "lqsgd_group_norm_forward", "lqsgd_group_norm_backward",
+    "lqsgd_pack_rows8", "lqsgd_unpack_rows8", "lqsgd_dropout", "lqsgd_rms_norm_workspace_bytes", "lqsgd_rms_norm_forward", "lqsgd_rms_norm_backward",
+    "lqsgd_linear_rows8_workspace_bytes", "lqsgd_linear_rows8_forward",
     "lqsgd_destroy", "lqsgd_strerror", "lqsgd_last_cuda_error", "lqsgd_version",
 ]
 

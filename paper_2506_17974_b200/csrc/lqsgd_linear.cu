@@ -16,7 +16,7 @@ struct LinPieces {
   const float* partial;
   uint32_t tiles_m, tiles_n, kb_total, share, cg, bn, rows;
 };
-template <uint32_t WAYS>
+template <uint32_t WAYS, int KIND>
 __global__ void __launch_bounds__(256)
 linear_join_kernel(LinPieces q, LinEpilogue e) {
   __shared__ float4 sums[8][32];
@@ -41,7 +41,7 @@ linear_join_kernel(LinPieces q, LinEpilogue e) {
 #pragma unroll 6
       for (uint32_t g = g0 + sub; g <= g1; g += WAYS) {
         const float4 s = *reinterpret_cast<const float4*>(src + (2 * g + (g * q.share < first ? 1 : 0)) * tile);
-        v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
+        v[0] = add_sums<KIND>(v[0], s.x); v[1] = add_sums<KIND>(v[1], s.y); v[2] = add_sums<KIND>(v[2], s.z); v[3] = add_sums<KIND>(v[3], s.w);
       }
     }
     if (WAYS > 1) {
@@ -50,38 +50,43 @@ linear_join_kernel(LinPieces q, LinEpilogue e) {
       if (sub == 0)
         for (uint32_t k = 1; k < WAYS; ++k) {
           const float4 s = sums[warp + k][lane];
-          v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
+          v[0] = add_sums<KIND>(v[0], s.x); v[1] = add_sums<KIND>(v[1], s.y); v[2] = add_sums<KIND>(v[2], s.z); v[3] = add_sums<KIND>(v[3], s.w);
         }
       __syncthreads();
     }
-    if (mine && sub == 0) finish_quad(e, row, n_tile * q.bn + strip * 128 + 4 * lane, v);
+    if (mine && sub == 0) finish_quad<KIND>(e, row, n_tile * q.bn + strip * 128 + 4 * lane, v);
   }
 }
 
 // Copies a matrix whose rows TMA cannot address (base or row distance not a multiple of 16 bytes) to rows of ld_dst elements, a
-// multiple of 16 bytes, zeros past cols; what lies past cols is never read.  A warp takes 256 columns of a row at a time, a thread
-// 8 of them: words where the row starts on one, else 16-bit values.
-constexpr int kRealignCols = 256;
+// multiple of 16 bytes, zeros past cols; what lies past cols is never read.  A warp takes 512 bytes of a row at a time, a thread
+// 16 of them: words where the row starts on one, else the elements (T: of 16 or of 8 bits).
+constexpr int kRealignBytes = 512;
+template <typename T>
 __global__ void __launch_bounds__(256)
-realign_kernel(const uint16_t* __restrict__ src, int64_t ld_src, int64_t rows, int cols, uint16_t* __restrict__ dst, int64_t ld_dst) {
+realign_kernel(const T* __restrict__ src, int64_t ld_src, int64_t rows, int cols, T* __restrict__ dst, int64_t ld_dst) {
   train_pdl_wait();
-  const int lane = threadIdx.x & 31, strips = (cols + kRealignCols - 1) / kRealignCols, warps = (int)gridDim.x * 8;
+  const int lane = threadIdx.x & 31, kEach = 16 / (int)sizeof(T), strips = (cols + 32 * kEach - 1) / (32 * kEach), warps = (int)gridDim.x * 8;
   const int first = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
   int strip = first % strips;
   for (int64_t row = first / strips; row < rows; row += warps / strips) {
-    const int col = strip * kRealignCols + 8 * lane, have = cols - col;
+    const int col = (strip * 32 + lane) * kEach, have = cols - col;
     if (have > 0) {
-      const uint16_t* s = src + row * ld_src + col;
+      const T* s = src + row * ld_src + col;
       uint32_t w[4];
-      if (have >= 8 && (reinterpret_cast<uintptr_t>(s) & 3) == 0) {
+      if (have >= kEach && (reinterpret_cast<uintptr_t>(s) & 3) == 0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(s) + i);
       } else {
-        uint32_t h[8];
+        uint32_t h[kEach];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = i < have ? __ldg(s + i) : 0;
+        for (int i = 0; i < kEach; ++i) h[i] = i < have ? __ldg(s + i) : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (h[2 * i + 1] << 16);
+        for (int i = 0; i < 4; ++i) {
+          w[i] = 0;
+#pragma unroll
+          for (int j = 0; j < kEach / 4; ++j) w[i] |= h[kEach / 4 * i + j] << (8 * (int)sizeof(T) * j);
+        }
       }
       *reinterpret_cast<uint4*>(dst + row * ld_dst + col) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -104,23 +109,24 @@ EncodeFn tensor_map_encoder() {
   cached.store(fn, std::memory_order_release);
   return fn;
 }
-// One operand as it lies in memory, 16-bit values.
+// One operand as it lies in memory, values of `elem` bytes.
 struct Stored {
   const void* base = nullptr;
   int64_t rows = 0, cols = 0, ld = 0;
-  int64_t aligned_ld() const { return ceil_div64(cols, 8) * 8; }
+  int elem = 2;
+  int64_t aligned_ld() const { return ceil_div64(cols * elem, 16) * 16 / elem; }
   // One row needs no row distance.
-  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld % 8 == 0); }
-  size_t copy_bytes() const { return tma_ready() ? 0 : (size_t)rows * aligned_ld() * 2; }
+  bool tma_ready() const { return train_aligned(base, 16) && (rows == 1 || ld * elem % 16 == 0); }
+  size_t copy_bytes() const { return tma_ready() ? 0 : (size_t)rows * aligned_ld() * elem; }
 };
-// Map over an operand: boxes of 64 columns x box_rows, 128-byte swizzle, zeros outside.
+// Map over an operand: boxes of 128 bytes (64 columns, 128 of 8 bits) x box_rows, 128-byte swizzle, zeros outside.
 int encode_map(CUtensorMap* map, const Stored& s, int box_rows) {
   EncodeFn fn = tensor_map_encoder();
   if (!fn) return record_cuda_failure(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
   const cuuint64_t dim[2] = {(cuuint64_t)s.cols, (cuuint64_t)s.rows};
-  const cuuint64_t stride[1] = {(cuuint64_t)(s.rows == 1 ? s.aligned_ld() : s.ld) * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, es[2] = {1, 1};
-  if (fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(s.base), dim, stride, box, es,
+  const cuuint64_t stride[1] = {(cuuint64_t)(s.rows == 1 ? s.aligned_ld() : s.ld) * (cuuint64_t)s.elem};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / s.elem), (cuuint32_t)box_rows}, es[2] = {1, 1};
+  if (fn(map, s.elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(s.base), dim, stride, box, es,
          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return record_cuda_failure(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
@@ -138,6 +144,7 @@ struct Plan {
 constexpr size_t kPieceAlign = 32;     // of the pieces of sums in the workspace: the kernels move them in 32-byte accesses
 constexpr int kSms = 148;              // sums are cut for this many SMs whatever the card has: results do not depend on it
 
+int deal_out(Plan p, int bk, Plan* out);
 int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   Plan p = {};
   const int64_t rows = a.rows;
@@ -151,7 +158,18 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
     p.unpacked = a.x8.dev_codes != nullptr;
     if (p.unpacked) p.b = {nullptr, rows, a.in, ceil_div64(a.in, 8) * 8};
   }
-  p.kb_total = (int)ceil_div64(p.K, kLinBK);
+  return deal_out(p, kLinBK, out);
+}
+int make_plan(const lqsgd_linear_rows8& a, Plan* out) {
+  Plan p = {};
+  p.a = {a.x.dev_codes, a.rows, a.in, a.x.ld_codes, 1};
+  p.b = {a.w.dev_codes, a.out, a.in, a.w.ld_codes, 1};
+  p.M = a.rows; p.N = a.out; p.K = a.in;
+  return deal_out(p, lin_bk<kInt8>(), out);
+}
+// Tiles and shares for the operands and sizes that p has; bk: k per block.
+int deal_out(Plan p, int bk, Plan* out) {
+  p.kb_total = (int)ceil_div64(p.K, bk);
   // The cheapest of the ways to deal the tiles out, by what they were measured to cost (microseconds).  Pairs of SMs on tiles of
   // 256 x 256 or single ones on 128 x 128: 94 against 134 us at 4096 x 4096 x 4096, but 10.7 against 9.2 at 1024 x 1024 x 1024, where
   // 16 pairs would work.  A forward product of 256 x 3136 x 512 takes 17.6 us in whole tiles, 12.6 in shares, 9.9 with the sums
@@ -189,7 +207,7 @@ int make_plan(int product, const lqsgd_linear& a, Plan* out) {
   if (best > 1e29) return LQSGD_ERR_BAD_SHAPE;
   size_t off = 0;
   auto room = [&](size_t n) { const size_t at = off; off += (n + 255) / 256 * 256; return at; };
-  if (p.unpacked) p.off_x = room((size_t)rows * p.b.ld * 2);
+  if (p.unpacked) p.off_x = room((size_t)p.b.rows * p.b.ld * 2);
   p.off_a = room(p.a.copy_bytes());
   p.off_b = room(p.b.copy_bytes());
   // The pieces are written and read 32 bytes at a time, and the caller's workspace starts on 16: room to move their start.
@@ -216,18 +234,22 @@ int check_matrix(const void* p, int64_t ld, int32_t cols, int elem) {
 int place(Stored* s, char* ws, size_t off, cudaStream_t st) {
   if (s->tma_ready()) return LQSGD_OK;
   const int64_t ld = s->aligned_ld();
-  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ceil_div64(s->cols, kRealignCols), 8), kSms * 8);
-  TRAIN_CK(train_launch(realign_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows,
-                        (int)s->cols, reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
+  const int64_t blocks = std::min<int64_t>(ceil_div64(s->rows * ceil_div64(s->cols * s->elem, kRealignBytes), 8), kSms * 8);
+  if (s->elem == 1)
+    TRAIN_CK(train_launch(realign_kernel<uint8_t>, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint8_t*>(s->base), s->ld, s->rows,
+                          (int)s->cols, reinterpret_cast<uint8_t*>(ws + off), ld), "realign_kernel launch");
+  else
+    TRAIN_CK(train_launch(realign_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, 1, static_cast<const uint16_t*>(s->base), s->ld, s->rows,
+                          (int)s->cols, reinterpret_cast<uint16_t*>(ws + off), ld), "realign_kernel launch");
   s->base = ws + off;
   s->ld = ld;
   return LQSGD_OK;
 }
 
-template <int CG, int BN, int OA, int OB, bool WF32>
+template <int CG, int BN, int OA, int OB, bool WF32, int KIND = kHalf>
 int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
-  using S = LinCfg<CG, BN, OA, OB, WF32>;
-  auto kernel = linear_kernel<CG, BN, OA, OB, WF32>;
+  using S = LinCfg<CG, BN, OA, OB, WF32, KIND>;
+  auto kernel = linear_kernel<CG, BN, OA, OB, WF32, KIND>;
   static std::atomic<uint64_t> ready{0};                     // devices on which the kernel may use its shared memory
   int dev = 0;
   TRAIN_CK(cudaGetDevice(&dev), "cudaGetDevice");
@@ -255,21 +277,12 @@ int launch(const Plan& p, LinProblem& q, cudaStream_t st) {
 struct TestWait { uint32_t limit = 0, after = 0; int32_t role = kNoRole; };
 thread_local TestWait test_wait;
 
-int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
+// What both forms of a product share: checks of the workspace `ws`, aligned copies, the kernel (started by `go`) and the join of pieces.
+template <int KIND, typename Go>
+int run_plan(Plan p, LinEpilogue ep, int dtype, uint32_t* status, char* ws, cudaStream_t st, Go&& go) {
   const TestWait test = test_wait;
   test_wait = TestWait();
-  Plan p;
-  int rc = make_plan(product, a, &p);
-  if (rc != LQSGD_OK) return rc;
-  if (p.bytes) {
-    if (!a.dev_workspace || a.workspace_bytes < p.bytes) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
-    if (!train_aligned(a.dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;
-  }
-  char* ws = static_cast<char*>(a.dev_workspace);
-  if (p.unpacked) {
-    p.b.base = ws + p.off_x;
-    if ((rc = lqsgd_unpack8(&a.x8, a.rows, a.in, ws + p.off_x, p.b.ld, a.dtype, st)) != LQSGD_OK) return rc;
-  }
+  int rc;
   if ((rc = place(&p.a, ws, p.off_a, st)) != LQSGD_OK || (rc = place(&p.b, ws, p.off_b, st)) != LQSGD_OK) return rc;
   const int es = ep.dtype == LQSGD_F32 ? 4 : 2;
   auto rows_aligned = [](const void* ptr, int64_t bytes, size_t to) { return train_aligned(ptr, to) && bytes % (int64_t)to == 0; };
@@ -286,16 +299,10 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
   q.tiles_m = p.tiles_m; q.tiles_n = p.tiles_n; q.kb_total = p.kb_total;
   q.deal = p.deal; q.share = p.share; q.meet = p.meet;
   q.first_chunk = pair_chunk(p.kb_total);
-  q.dtype = a.dtype;
-  q.status = a.dev_status;
+  q.dtype = dtype;
+  q.status = status;
   q.test_limit = test.limit; q.test_after = test.after; q.test_role = test.role;
-  if (product == LQSGD_LINEAR_FORWARD)
-    rc = p.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(p, q, st) : launch<1, 128, kOpK, kOpK, false>(p, q, st);
-  else if (product == LQSGD_LINEAR_GRAD_INPUT)
-    rc = p.cg == 2 ? launch<2, 256, kOpK, kOpMN, false>(p, q, st) : launch<1, 128, kOpK, kOpMN, false>(p, q, st);
-  else
-    rc = p.cg == 2 ? launch<2, 256, kOpMN, kOpMN, true>(p, q, st) : launch<1, 128, kOpMN, kOpMN, true>(p, q, st);
-  if (rc != LQSGD_OK) return rc;
+  if ((rc = go(p, q)) != LQSGD_OK) return rc;
   if (p.deal == kShares) {
     const int most = (int)((p.kb_total - 1) / p.share + 2);           // pieces of one tile
     const uint32_t tiles = (uint32_t)p.tiles_m * p.tiles_n, high = kLinBM * p.cg;
@@ -303,9 +310,56 @@ int run(int product, const lqsgd_linear& a, LinEpilogue ep, cudaStream_t st) {
     while (rows > (most >= 8 ? 1u : 8u) && tiles * (high / rows) < kSms * 4) rows /= 2;
     const LinPieces j = {q.partial, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.kb_total, (uint32_t)p.share, (uint32_t)p.cg, (uint32_t)p.bn, rows};
     const dim3 grid(tiles * (high / rows));
-    if (most >= 8) TRAIN_CK(train_launch(linear_join_kernel<8>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
-    else TRAIN_CK(train_launch(linear_join_kernel<1>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
+    if (most >= 8) TRAIN_CK(train_launch(linear_join_kernel<8, KIND>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
+    else TRAIN_CK(train_launch(linear_join_kernel<1, KIND>, grid, dim3(256), 0, st, 1, j, ep), "linear_join_kernel launch");
   }
+  return LQSGD_OK;
+}
+int check_workspace(const Plan& p, const void* ws, size_t bytes) {
+  if (!p.bytes) return LQSGD_OK;
+  if (!ws || bytes < p.bytes) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
+  return train_aligned(ws, 16) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+}
+
+int run(int product, const lqsgd_linear& a, const LinEpilogue& ep, cudaStream_t st) {
+  Plan p;
+  int rc = make_plan(product, a, &p);
+  if (rc == LQSGD_OK) rc = check_workspace(p, a.dev_workspace, a.workspace_bytes);
+  char* ws = static_cast<char*>(a.dev_workspace);
+  if (rc == LQSGD_OK && p.unpacked) {
+    p.b.base = ws + p.off_x;
+    rc = lqsgd_unpack8(&a.x8, a.rows, a.in, ws + p.off_x, p.b.ld, a.dtype, st);
+  }
+  if (rc != LQSGD_OK) {
+    test_wait = TestWait();
+    return rc;
+  }
+  return run_plan<kHalf>(p, ep, a.dtype, a.dev_status, ws, st, [&](const Plan& plan, LinProblem& q) {
+    if (product == LQSGD_LINEAR_FORWARD)
+      return plan.cg == 2 ? launch<2, 256, kOpK, kOpK, false>(plan, q, st) : launch<1, 128, kOpK, kOpK, false>(plan, q, st);
+    if (product == LQSGD_LINEAR_GRAD_INPUT)
+      return plan.cg == 2 ? launch<2, 256, kOpK, kOpMN, false>(plan, q, st) : launch<1, 128, kOpK, kOpMN, false>(plan, q, st);
+    return plan.cg == 2 ? launch<2, 256, kOpMN, kOpMN, true>(plan, q, st) : launch<1, 128, kOpMN, kOpMN, true>(plan, q, st);
+  });
+}
+int run(const lqsgd_linear_rows8& a, const LinEpilogue& ep, cudaStream_t st) {
+  Plan p;
+  int rc = make_plan(a, &p);
+  if (rc == LQSGD_OK) rc = check_workspace(p, a.dev_workspace, a.workspace_bytes);
+  if (rc != LQSGD_OK) {
+    test_wait = TestWait();
+    return rc;
+  }
+  return run_plan<kInt8>(p, ep, a.dtype, a.dev_status, static_cast<char*>(a.dev_workspace), st, [&](const Plan& plan, LinProblem& q) {
+    return plan.cg == 2 ? launch<2, 256, kOpK, kOpK, false, kInt8>(plan, q, st) : launch<1, 128, kOpK, kOpK, false, kInt8>(plan, q, st);
+  });
+}
+
+int check_rows8_args(const lqsgd_linear_rows8* a) {
+  if (!a || a->struct_size != sizeof(lqsgd_linear_rows8)) return LQSGD_ERR_INVALID_ARG;
+  if ((a->dtype != LQSGD_BF16 && a->dtype != LQSGD_F16) || !train_act_ok(a->act) || a->reserved) return LQSGD_ERR_INVALID_ARG;
+  // 128^2 terms of at most 131071 stay below 2^31
+  if (a->rows < 0 || a->rows > 0x7fffffffll - 511 || a->in < 1 || a->out < 1 || a->in > 131071 || a->out > (1 << 24)) return LQSGD_ERR_BAD_SHAPE;
   return LQSGD_OK;
 }
 
@@ -388,4 +442,35 @@ extern "C" int lqsgd_linear_grad_weight(const lqsgd_linear* a, void* cuda_stream
   ep.out = a->dev_out; ep.ld_out = a->ld_out;
   ep.rows = a->out; ep.cols = a->in; ep.dtype = LQSGD_F32; ep.act = LQSGD_ACT_NONE; ep.accumulate = a->accumulate;
   return run(LQSGD_LINEAR_GRAD_WEIGHT, *a, ep, st);
+}
+
+extern "C" int lqsgd_linear_rows8_workspace_bytes(const lqsgd_linear_rows8* host_args, size_t* host_bytes_out) {
+  if (!host_bytes_out) return LQSGD_ERR_INVALID_ARG;
+  int rc = check_rows8_args(host_args);
+  if (rc != LQSGD_OK) return rc;
+  *host_bytes_out = 0;
+  if (host_args->rows == 0) return LQSGD_OK;
+  Plan p;
+  if ((rc = make_plan(*host_args, &p)) != LQSGD_OK) return rc;
+  *host_bytes_out = p.bytes;
+  return LQSGD_OK;
+}
+
+extern "C" int lqsgd_linear_rows8_forward(const lqsgd_linear_rows8* a, void* cuda_stream) {
+  int rc = check_rows8_args(a);
+  if (rc != LQSGD_OK) return rc;
+  if (a->rows == 0) return LQSGD_OK;
+  if ((rc = check_rows8(a->x, a->in)) != LQSGD_OK || (rc = check_rows8(a->w, a->in)) != LQSGD_OK || (rc = check_matrix(a->dev_out, a->ld_out, a->out, 2)) != LQSGD_OK)
+    return rc;
+  if (a->dev_residual && (rc = check_matrix(a->dev_residual, a->ld_residual, a->out, 2)) != LQSGD_OK) return rc;
+  if (!train_aligned(a->dev_bias, 4) || !train_aligned(a->dev_status, 4)) return LQSGD_ERR_MISALIGNED;
+  if (a->z8.dev_codes && (rc = check_packed8(a->z8, a->out)) != LQSGD_OK) return rc;
+  if (a->y8.dev_codes && (rc = check_packed8(a->y8, a->out)) != LQSGD_OK) return rc;
+  LinEpilogue ep = {};
+  ep.out = a->dev_out; ep.ld_out = a->ld_out; ep.bias = a->dev_bias;
+  ep.row_scale = a->x.dev_scales; ep.col_scale = a->w.dev_scales;
+  ep.residual = a->dev_residual; ep.ld_res = a->ld_residual;
+  ep.z8 = a->z8; ep.y8 = a->y8;
+  ep.rows = (int32_t)a->rows; ep.cols = a->out; ep.dtype = a->dtype; ep.act = a->act;
+  return run(*a, ep, static_cast<cudaStream_t>(cuda_stream));
 }

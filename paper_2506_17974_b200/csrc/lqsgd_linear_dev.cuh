@@ -32,6 +32,11 @@ namespace lqsgd {
 
 constexpr int kLinBM = 128;            // rows of A per CTA
 constexpr int kLinBK = 64;             // k per stage: 128 bytes of a 16-bit type, one swizzle span
+// Operands in 16 bits, or in signed 8 (a forward product of rows of codes).  The tensor core takes 32 bytes of k per step and row of either, so
+// a stage holds 64 or 128 k in the same bytes and costs the same time.  Sums of 8-bit codes are 32-bit integers and exact: one
+// accumulator takes the whole sum, pieces of sums are added as integers, and the scales come in the epilogue.
+enum LinKind { kHalf = 0, kInt8 = 1 };
+template <int KIND> __device__ __host__ constexpr int lin_bk() { return KIND == kInt8 ? 128 : kLinBK; }
 enum LinOperand { kOpK = 0, kOpMN = 1 };
 enum LinDeal { kWhole = 0, kShares = 1, kMeet = 2 };
 
@@ -40,6 +45,7 @@ struct LinEpilogue {
   void* out;
   int64_t ld_out;
   const float* bias;
+  const float *row_scale, *col_scale;  // of integer sums; else not used
   const void* residual;
   int64_t ld_res;
   lqsgd_packed8 z8, y8;
@@ -146,9 +152,15 @@ __device__ __forceinline__ void lin_tma(uint32_t dst, const CUtensorMap* map, in
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-template <int CG>
+template <int CG, int KIND>
 __device__ __forceinline__ void lin_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (CG == 2)
+  if constexpr (KIND == kInt8 && CG == 2)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  else if constexpr (KIND == kInt8)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  else if constexpr (CG == 2)
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
   else
@@ -179,7 +191,7 @@ __device__ __forceinline__ uint64_t lin_desc(uint32_t addr) {
   d |= (uint64_t)2 << 61;              // 128-byte swizzle
   return d;
 }
-// Byte step of a descriptor from one K = 16 slice to the next.
+// Byte step of a descriptor from one slice of 16 (8-bit: 32) k to the next.
 template <bool MN> __device__ __forceinline__ constexpr uint32_t lin_kstep() { return MN ? 16 * 128 : 32; }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32]) {
@@ -293,6 +305,15 @@ __device__ __forceinline__ void finish_ragged_f32(const LinEpilogue& e, int64_t 
     }
   }
   __syncwarp();
+}
+// An integer sum as the value it stands for.
+__device__ __forceinline__ float scaled_sum(float bits, float row_scale, float col_scale) {
+  return (float)__float_as_int(bits) * row_scale * col_scale;
+}
+// a + b of two sums: of integers where KIND has them.
+template <int KIND>
+__device__ __forceinline__ float add_sums(float a, float b) {
+  return KIND == kInt8 ? __int_as_float(__float_as_int(a) + __float_as_int(b)) : a + b;
 }
 // Epilogue of a 32 x 32 piece of a layer's output.
 // bias: these columns' values in shared memory (zeros past the matrix).
@@ -421,9 +442,10 @@ __device__ __forceinline__ void put_packed_quad(const lqsgd_packed8& p, int64_t 
   if ((col & (kGroup - 1)) == 0) p.dev_exps[row * p.ld_exps + col / kGroup] = (uint8_t)eb;
 }
 // The whole warp calls it; col is the lane's first column.
+template <int KIND = kHalf>
 __device__ __forceinline__ void finish_quad(const LinEpilogue& e, int64_t row, int col, float (&v)[4]) {
   const int have = min(4, e.cols - col);
-  if (e.dtype == LQSGD_F32) {
+  if (KIND == kHalf && e.dtype == LQSGD_F32) {
     float* o = static_cast<float*>(e.out) + row * e.ld_out + col;
     if (have == 4 && e.vec_out) {
       float4 t = make_float4(v[0], v[1], v[2], v[3]);
@@ -439,8 +461,10 @@ __device__ __forceinline__ void finish_quad(const LinEpilogue& e, int64_t row, i
     }
     return;
   }
+  const float row_scale = KIND == kInt8 ? __ldg(e.row_scale + row) : 1.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    if (KIND == kInt8 && i < have) v[i] = scaled_sum(v[i], row_scale, __ldg(e.col_scale + col + i));
     if (i >= have) v[i] = 0.f;
     else if (e.bias) v[i] += __ldg(e.bias + col + i);
   }
@@ -593,7 +617,7 @@ constexpr int kChunk = 16, kLaterChunk = 8;
 inline int pair_chunk(int kb_total) { return kb_total <= 32 ? 32 : 20; }
 
 // WF32: the result is fp32 (a weight gradient).
-template <int CG, int BN, int OA, int OB, bool WF32>
+template <int CG, int BN, int OA, int OB, bool WF32, int KIND>
 struct LinCfg {
   static constexpr int kBNc = BN / CG;                                    // rows of B per CTA
   static constexpr uint32_t kABytes = kLinBM * 128, kBBytes = kBNc * 128;
@@ -605,9 +629,9 @@ struct LinCfg {
   static constexpr int kThreads = (4 + kEpiWarps) * 32;
   // With 128 sums of a long chain in registers the epilogue of a layer needs more of them than the 168 that every thread starts with
   // (75 of them spilled, 8192 x 4096 x 16384 took 990 us instead of 840): the first four warps hand some over.
-  static constexpr bool kMoveRegs = CG == 2 && !WF32;
+  static constexpr bool kMoveRegs = CG == 2 && !WF32 && KIND == kHalf;
   static constexpr int kRegsFront = 56, kRegsEpi = 224, kRegsAll = 128 * kRegsFront + 32 * kEpiWarps * kRegsEpi;   // the launch has to bring these
-  static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2 + kMine * 4, kScratch = kEpiWarps * kScratchWarp;
+  static constexpr uint32_t kScratchWarp = WF32 ? 32 * 9 * 4 : 32 * 34 * 2 + kMine * 4 * (KIND == kInt8 ? 2 : 1), kScratch = kEpiWarps * kScratchWarp;
   static constexpr uint32_t kRoom = 225u * 1024 - kScratch;
   static constexpr int kStages = (int)(kRoom / kStage) > 12 ? 12 : (int)(kRoom / kStage);
   static constexpr int kTmemCols = 2 * BN;
@@ -621,14 +645,15 @@ struct LinCfg {
   static_assert(kSmem <= 227 * 1024 && kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "one CTA per SM");
   static_assert(OB == kOpK || kBNc % 64 == 0, "MN-major operands come in blocks of 64");
   static_assert(!kMoveRegs || kRegsAll <= kThreads * 168, "the launch brings 168 per thread");
+  static_assert(KIND == kHalf || (OA == kOpK && OB == kOpK && !WF32), "products of codes are forward products");
   static_assert(CG == 2 || BN == 128, "a warp finishes a row of a tile");
   static_assert(CG == 2 || (kLinBM + 7) * kMeetPitch * 4 <= kStages * kStage, "a tile, in up to 8 slices, fits in the operand stages");
 };
 
-template <int CG, int BN, int OA, int OB, bool WF32>
-__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB, WF32>::kThreads, 1)
+template <int CG, int BN, int OA, int OB, bool WF32, int KIND>
+__global__ void __launch_bounds__(LinCfg<CG, BN, OA, OB, WF32, KIND>::kThreads, 1)
 linear_kernel(const __grid_constant__ LinProblem p) {
-  using S = LinCfg<CG, BN, OA, OB, WF32>;
+  using S = LinCfg<CG, BN, OA, OB, WF32, KIND>;
   extern __shared__ uint8_t lin_smem[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(lin_smem) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(base + S::kBarOff);   // [stages] TMA bytes landed, in both CTAs (first CTA's barrier)
@@ -676,7 +701,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
   const uint32_t tmem = *tmem_slot;
   train_pdl_trigger();
   // k blocks of a tile's n-th accumulator
-  auto chunk = [&](int n) { return CG == 1 || WF32 ? kChunk : n < 2 ? p.first_chunk : kLaterChunk; };
+  auto chunk = [&](int n) { return KIND == kInt8 ? 1 << 30 : CG == 1 || WF32 ? kChunk : n < 2 ? p.first_chunk : kLaterChunk; };
   // Every role first finds its place in the work, then waits for the kernel in front.
   bool met = false;                    // kMeet: this warp has passed the cluster's first barrier
   const uint32_t base_s = smem_u32(base), full_s = smem_u32(full), empty_s = smem_u32(empty);
@@ -696,7 +721,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     for (; !w.done(); w.next(p), ++issued) {
       if (issued == stop || !lin_wait_all(empty_s + 8 * s, empty + s, turn ^ 1, abort_flag)) break;
       const uint32_t a = base_s + s * S::kStage, b = a + S::kABytes, bar = full0 + 8 * s;
-      const int k0 = w.kb * kLinBK, m0 = (w.m_tile * CG + (int)rank) * kLinBM, n0 = w.n_tile * BN + (int)rank * S::kBNc;
+      const int k0 = w.kb * lin_bk<KIND>(), m0 = (w.m_tile * CG + (int)rank) * kLinBM, n0 = w.n_tile * BN + (int)rank * S::kBNc;
       if (elect_one()) {
         if (rank == 0) mbar_arrive_expect_tx(full + s, tx);
         if constexpr (OA == kOpK) {
@@ -720,8 +745,8 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     // ---- MMA issue: the cluster's first CTA
     if (rank == 0) {
       const uint32_t fmt = p.dtype == LQSGD_BF16 ? 1u : 0u;
-      // fp32 accumulator, operand type, which operands are MN-major, N / 8, M / 16
-      const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((OA == kOpK ? 0u : 1u) << 15) | ((OB == kOpK ? 0u : 1u) << 16) |
+      // fp32 accumulator (8-bit: 32-bit integers, signed operands), operand type, which operands are MN-major, N / 8, M / 16
+      const uint32_t idesc = (KIND == kInt8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4) | (fmt << 7) | (fmt << 10)) | ((OA == kOpK ? 0u : 1u) << 15) | ((OB == kOpK ? 0u : 1u) << 16) |
                              ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((kLinBM * CG) >> 4) << 24);
       const uint64_t ad0 = lin_desc<OA != kOpK>(base_s), bd0 = lin_desc<OB != kOpK>(base_s + S::kABytes);
       const uint32_t d_full_s = smem_u32(d_full), d_empty_s = smem_u32(d_empty);
@@ -750,7 +775,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           if (elect_one()) {
 #pragma unroll
             for (int ks = 0; ks < kLinBK / 16; ++ks)
-              lin_mma<CG>(d, ad + ((ks * lin_kstep<OA != kOpK>()) >> 4), bd + ((ks * lin_kstep<OB != kOpK>()) >> 4), idesc, ks > 0 ? 1u : more);
+              lin_mma<CG, KIND>(d, ad + ((ks * lin_kstep<OA != kOpK>()) >> 4), bd + ((ks * lin_kstep<OB != kOpK>()) >> 4), idesc, ks > 0 ? 1u : more);
             lin_commit<CG>(empty_s + 8 * s);
             if (left == 0) lin_commit<CG>(d_full_s + 8 * db);
           }
@@ -784,10 +809,16 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     // What the epilogue of a layer reads besides the sum is asked for a tile ahead: the bias of this warp's columns in
     // registers, the residual into L2.
     float* bias = scratch + 32 * 34 / 2;
-    float bias_next[S::kMine / 32] = {};
+    float* col_scale = bias + S::kMine;
+    float bias_next[S::kMine / 32] = {}, scale_next[KIND == kInt8 ? S::kMine / 32 : 1] = {}, row_scale_next = 0.f;
     auto fetch_ahead = [&](const LinWalk& t) {
       if (WF32 || meet > 1 || t.done() || t.piece(p) >= 0) return;
       const int m = (t.m_tile * CG + (int)rank) * kLinBM + 32 * q + lane, n = t.n_tile * BN + c0, have = min(S::kMine, p.N - n);
+      if constexpr (KIND == kInt8) {
+#pragma unroll
+        for (int i = 0; i < S::kMine / 32; ++i) scale_next[i] = 32 * i + lane < have ? __ldg(p.ep.col_scale + n + 32 * i + lane) : 0.f;
+        row_scale_next = m < p.M ? __ldg(p.ep.row_scale + m) : 0.f;
+      }
       if (p.ep.bias) {
 #pragma unroll
         for (int i = 0; i < S::kMine / 32; ++i) bias_next[i] = 32 * i + lane < have ? __ldg(p.ep.bias + n + 32 * i + lane) : 0.f;
@@ -803,9 +834,13 @@ linear_kernel(const __grid_constant__ LinProblem p) {
     train_pdl_wait();
     fetch_ahead(w);
     for (; !w.done(); w.next_tile(p)) {
-      if (!WF32 && (p.ep.residual || p.ep.bias)) {
+      const float row_scale = row_scale_next;
+      if (!WF32 && (KIND == kInt8 || p.ep.residual || p.ep.bias)) {
 #pragma unroll
-        for (int i = 0; i < S::kMine / 32; ++i) bias[32 * i + lane] = bias_next[i];
+        for (int i = 0; i < S::kMine / 32; ++i) {
+          bias[32 * i + lane] = bias_next[i];
+          if constexpr (KIND == kInt8) col_scale[32 * i + lane] = scale_next[i];
+        }
         __syncwarp();
         LinWalk t = w;
         t.next_tile(p);
@@ -841,7 +876,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           met = true;
         }
       };
-      if (!WF32 && w.kb_end - w.kb <= chunk(0) && !part) {          // one accumulator has the whole sum: piece by piece from tensor memory
+      if (KIND == kInt8 || (!WF32 && w.kb_end - w.kb <= chunk(0) && !part)) {          // one accumulator has the whole sum: piece by piece from tensor memory
         const uint32_t taddr = open();
         if (!ok) break;
         meet_first();
@@ -852,67 +887,81 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           if (c + 32 >= S::kMine) hand_back();
           if (CG == 1 && meet > 1) {
             if (m < p.M) to_meeting(map_to(to_slice + c0 + c, to), v);
+          } else if (KIND == kInt8 && part) {
+            if (m < p.M && n0 + c0 + c < p.N) store_sums(part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0 + c, v);
           } else if (n0 + c0 + c < p.N && m - lane < p.M) {
+            if constexpr (KIND == kInt8) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float4 t = *(reinterpret_cast<const float4*>(col_scale + c) + i);
+                v[4 * i] = scaled_sum(v[4 * i], row_scale, t.x);
+                v[4 * i + 1] = scaled_sum(v[4 * i + 1], row_scale, t.y);
+                v[4 * i + 2] = scaled_sum(v[4 * i + 2], row_scale, t.z);
+                v[4 * i + 3] = scaled_sum(v[4 * i + 3], row_scale, t.w);
+              }
+            }
             finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
           }
           __syncwarp();
         }
         continue;
       }
-      float acc[S::kMine];
+      if constexpr (KIND == kHalf) {
+        float acc[S::kMine];
 #pragma unroll
-      for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
+        for (int c = 0; c < S::kMine; ++c) acc[c] = 0.f;
 #pragma unroll 1
-      for (int left = w.kb_end - w.kb, n = 0; left > 0; left -= chunk(n++)) {
-        const uint32_t taddr = open();
-        if (!ok) break;
+        for (int left = w.kb_end - w.kb, n = 0; left > 0; left -= chunk(n++)) {
+          const uint32_t taddr = open();
+          if (!ok) break;
 #pragma unroll
-        for (int c = 0; c < S::kMine; c += 16) {
-          float v[16];
-          tmem_ld16(taddr + c, v);
+          for (int c = 0; c < S::kMine; c += 16) {
+            float v[16];
+            tmem_ld16(taddr + c, v);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
-        }
-        hand_back();
-      }
-      if (!ok) break;
-      meet_first();
-      if (CG == 1 && meet > 1) {
-        if (m < p.M) to_meeting(map_to(to_slice + c0, to), acc);
-      } else if (part) {
-        if (m < p.M && n0 + c0 < p.N) store_sums(part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0, acc);
-      } else if constexpr (WF32) {
-        if (p.ep.vec_out && n0 + c0 + S::kMine <= p.N) {
-          float* o = static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
-          if (m < p.M) {
-#pragma unroll
-            for (int c = 0; c < S::kMine; c += 8) {
-              uint32_t u[8];
-              if (p.ep.accumulate) {
-                ld_row32(o + c, p.ep.vec_out, u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
-              st_row32(o + c, p.ep.vec_out, u);
-            }
+            for (int j = 0; j < 16; ++j) acc[c + j] += v[j];
           }
-        } else if (m - lane < p.M) {
-#pragma unroll
-          for (int c = 0; c < S::kMine; c += 8)
-            if (n0 + c0 + c < p.N) finish_ragged_f32(p.ep, m - lane, n0 + c0 + c, acc + c, scratch);
+          hand_back();
         }
-      } else {
+        if (!ok) break;
+        meet_first();
+        if (CG == 1 && meet > 1) {
+          if (m < p.M) to_meeting(map_to(to_slice + c0, to), acc);
+        } else if (part) {
+          if (m < p.M && n0 + c0 < p.N) store_sums(part + ((int)rank * kLinBM + 32 * q + lane) * BN + c0, acc);
+        } else if constexpr (WF32) {
+          if (p.ep.vec_out && n0 + c0 + S::kMine <= p.N) {
+            float* o = static_cast<float*>(p.ep.out) + (int64_t)m * p.ep.ld_out + n0 + c0;
+            if (m < p.M) {
+#pragma unroll
+              for (int c = 0; c < S::kMine; c += 8) {
+                uint32_t u[8];
+                if (p.ep.accumulate) {
+                  ld_row32(o + c, p.ep.vec_out, u);
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) acc[c + j] += __uint_as_float(u[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(acc[c + j]);
+                st_row32(o + c, p.ep.vec_out, u);
+              }
+            }
+          } else if (m - lane < p.M) {
+#pragma unroll
+            for (int c = 0; c < S::kMine; c += 8)
+              if (n0 + c0 + c < p.N) finish_ragged_f32(p.ep, m - lane, n0 + c0 + c, acc + c, scratch);
+          }
+        } else {
 #pragma unroll 1
-        for (int c = 0; c < S::kMine; c += 32) {
-          float v[32];
+          for (int c = 0; c < S::kMine; c += 32) {
+            float v[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = acc[j];
+            for (int j = 0; j < 32; ++j) v[j] = acc[j];
 #pragma unroll
-          for (int j = 32; j < S::kMine; ++j) acc[j - 32] = acc[j];      // the next piece's: one copy of the epilogue's code, registers by number
-          if (n0 + c0 + c < p.N && m - lane < p.M) finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
-          __syncwarp();
+            for (int j = 32; j < S::kMine; ++j) acc[j - 32] = acc[j];      // the next piece's: one copy of the epilogue's code, registers by number
+            if (n0 + c0 + c < p.N && m - lane < p.M) finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
+            __syncwarp();
+          }
         }
       }
       __syncwarp();
@@ -958,9 +1007,10 @@ linear_kernel(const __grid_constant__ LinProblem p) {
 #pragma unroll 4
       for (int k = 0; k < meet; ++k) {
         const float4 t = *reinterpret_cast<const float4*>(mine + k * slice * S::kMeetPitch);
-        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
+        v[0] = add_sums<KIND>(v[0], t.x); v[1] = add_sums<KIND>(v[1], t.y);
+        v[2] = add_sums<KIND>(v[2], t.z); v[3] = add_sums<KIND>(v[3], t.w);
       }
-      finish_quad(p.ep, row, w.n_tile * BN + 4 * lane, v);
+      finish_quad<KIND>(p.ep, row, w.n_tile * BN + 4 * lane, v);
     }
   }
   if (warp == 2) {

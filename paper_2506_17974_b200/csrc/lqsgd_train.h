@@ -22,8 +22,21 @@ inline int check_packed8(const lqsgd_packed8& p, int32_t cols) {
   return LQSGD_OK;
 }
 
+// Checks of an argument of signed 8-bit rows (codes set), and of a dropout.
+inline int check_rows8(const lqsgd_rows8& p, int32_t cols) {
+  if (!p.dev_codes || !p.dev_scales || p.ld_codes < cols) return LQSGD_ERR_INVALID_ARG;
+  return train_aligned(p.dev_scales, 4) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+}
+inline int check_drop(const lqsgd_drop& d) {
+  if (!(d.p >= 0.f && d.p < 1.f) || d.reserved) return LQSGD_ERR_INVALID_ARG;
+  return train_aligned(d.dev_seed, 8) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+}
+
 // SM count of the current device; asked once per device, 0 when it cannot be had.
 int train_sm_count();
+
+// out[c] = sum over b of partial[b][c], b < blocks, in an order fixed by blocks (lqsgd_act8.cu).
+int join_columns(const float* partial, int blocks, int32_t cols, float* out, cudaStream_t st);
 
 // Launch whose start may overlap the tail of the kernel in front of it in the stream; every kernel launched this way
 // begins with griddepcontrol.wait before it touches memory.

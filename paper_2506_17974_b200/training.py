@@ -4,12 +4,15 @@
                                                        epilogue
     pack8 / unpack8 / act_grad                         activations kept in 8 bits until the backward pass
     group_norm / group_norm_grad                       group norm with an activation, channels last
+    rms_norm / rms_norm_grad                           root-mean-square norm of rows, dropout and the residual's addition in front
+    dropout                                            from a counter-based generator, the mask is never stored
+    pack_rows8 / unpack_rows8 / linear_rows8           rows of signed 8-bit codes, a linear layer's forward product of them
 
 A tensor given as `out` is written in place, which autograd is told.
 
 Argument marshalling only, as in binding.py: tensors are checked here for type, device and layout, everything else by the
-library; the arithmetic runs in its CUDA kernels, on the current stream of the tensors' device.  `linear_layer` and
-`norm_layer` are the same operators as differentiable functions that keep only 8-bit activations between the passes.
+library; the arithmetic runs in its CUDA kernels, on the current stream of the tensors' device.  The `*_layer` functions
+are the same operators as differentiable functions that keep only 8-bit activations between the passes.
 """
 from __future__ import annotations
 
@@ -36,6 +39,12 @@ _PACKED8 = struct.Struct("@PqPq")
 _LINEAR = struct.Struct("@Iiii q ii PqPqPq P Pq Pq PqPq PqPq PqPq P PN")
 _NORM = struct.Struct("@Iiiiiiif PqqPqqPqq PP PP PP PqPq PqPq PN")
 _NONE8 = (0, 0, 0, 0)
+# lqsgd_rows8, lqsgd_drop, lqsgd_rms_norm and lqsgd_linear_rows8 (whose operands and kept copies are the first two's fields)
+_ROWS8 = struct.Struct("@PqP")
+_DROP = struct.Struct("@fIQQP")
+_RMS = struct.Struct("@Ii q if fIQQP PqPqPqPq PqPqPqPq PPP PqPq PqPq PqP PN")
+_LINEAR8 = struct.Struct("@IiiI q ii PqP PqP P Pq Pq PqPq PqPq P PN")
+_NO_ROWS8 = (0, 0, 0)
 
 _lib = None
 
@@ -51,7 +60,12 @@ def _library() -> C.CDLL:
         lib.lqsgd_act_grad.argtypes = [vp, i64, vp, i32, i32, i64, i32, vp, i64, vp, vp, sz, vp]
         lib.lqsgd_linear_workspace_bytes.argtypes = [i32, vp, C.POINTER(sz)]
         lib.lqsgd_group_norm_workspace_bytes.argtypes = [i32, vp, C.POINTER(sz)]
-        for f in (lib.lqsgd_linear_forward, lib.lqsgd_linear_grad_input, lib.lqsgd_linear_grad_weight,
+        lib.lqsgd_pack_rows8.argtypes = [vp, i64, i32, i64, i32, vp, vp]
+        lib.lqsgd_unpack_rows8.argtypes = [vp, i64, i32, vp, i64, i32, vp]
+        lib.lqsgd_dropout.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, vp, i64, vp]
+        lib.lqsgd_rms_norm_workspace_bytes.argtypes = [i32, vp, C.POINTER(sz)]
+        lib.lqsgd_linear_rows8_workspace_bytes.argtypes = [vp, C.POINTER(sz)]
+        for f in (lib.lqsgd_rms_norm_forward, lib.lqsgd_rms_norm_backward, lib.lqsgd_linear_rows8_forward, lib.lqsgd_linear_forward, lib.lqsgd_linear_grad_input, lib.lqsgd_linear_grad_weight,
                   lib.lqsgd_group_norm_forward, lib.lqsgd_group_norm_backward):
             f.argtypes = [vp, vp]
         _lib = lib
@@ -323,6 +337,220 @@ def act_grad(dy: torch.Tensor, z8: Optional[Packed8], act: str = "none", bias_gr
     return dz, db
 
 
+# ------------------------------------------------------------------------------------------- rows of signed 8-bit codes
+
+class Rows8:
+    """A matrix as rows of signed 8-bit codes: codes, int8 rows x cols, and scales, float32 rows (see lqsgd_rows8)."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        self.codes, self.scales = codes, scales
+        self.fields()
+
+    @staticmethod
+    def empty(rows: int, cols: int, device) -> "Rows8":
+        """Uninitialised; rows of codes start on 16-byte boundaries."""
+        p = object.__new__(Rows8)
+        p.codes = torch.empty_strided((rows, cols), ((cols + 15) & -16, 1), dtype=torch.int8, device=device)
+        p.scales = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+        return p
+
+    def _fresh(self) -> Tuple[int, int, int]:
+        """fields() of what empty() just made."""
+        return self.codes.data_ptr(), (self.codes.shape[1] + 15) & -16, self.scales.data_ptr()
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def fields(self) -> Tuple[int, int, int]:
+        """The members of lqsgd_rows8, checked."""
+        codes = self.codes
+        dev = codes.get_device()
+        cp, cl = _matrix(codes, "codes", dev, torch.int8)
+        return cp, cl, _vector(self.scales, "scales", dev, codes.shape[0])
+
+
+def _rows(p: "Rows8", what: str, device: int, rows: int = -1, cols: int = -1) -> Tuple[int, int, int]:
+    """The fields of an argument in rows of signed codes (any number of rows or columns where -1)."""
+    if not isinstance(p, Rows8):
+        raise ValueError(f"{what} must be the Rows8 form of a matrix")
+    r, c = p.codes.shape
+    if (rows >= 0 and r != rows) or (cols >= 0 and c != cols) or p.codes.get_device() != device:
+        raise ValueError(f"{what} must be the Rows8 form of {rows if rows >= 0 else 'any'} x {cols if cols >= 0 else 'any'} values on the call's device, "
+                         f"not of {r} x {c}")
+    return p.fields()
+
+
+def pack_rows8(x: torch.Tensor, out: Optional[Rows8] = None) -> Rows8:
+    """A matrix (bfloat16, float16 or float32) as rows of signed 8-bit codes with one scale each."""
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return pack_rows8(x, out)
+    xp, xl = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    given = out is not None
+    if given:
+        of = _rows(out, "out", dev, rows, cols)
+    else:
+        out = Rows8.empty(rows, cols, x.device)
+        of = out._fresh()
+    rc = _library().lqsgd_pack_rows8(xp, xl, _dtype(x, "x"), rows, cols, _ROWS8.pack(*of), _stream(dev))
+    if rc:
+        B._check(rc)
+    if given:
+        _written(out.codes, out.scales)
+    return out
+
+
+def unpack_rows8(p: Rows8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that rows of signed codes stand for, rounded to dtype."""
+    codes = p.codes
+    dev = codes.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return unpack_rows8(p, dtype, out)
+    rows, cols = codes.shape
+    if dtype not in DTYPES:
+        raise ValueError(f"dtype must be one of {list(DTYPES)}")
+    y = _empty(rows, cols, dtype, codes.device) if out is None else out
+    yp, yl = _matrix(y, "out", dev, dtype, rows, cols)
+    rc = _library().lqsgd_unpack_rows8(_ROWS8.pack(*p.fields()), rows, cols, yp, yl, DTYPES[dtype], _stream(dev))
+    if rc:
+        B._check(rc)
+    if out is not None:
+        _written(out)
+    return y
+
+
+# -------------------------------------------------------------------------------------------------------------- dropout
+
+Seed = Union[int, torch.Tensor]
+
+
+def _drop(p: float, seed: Seed, offset: int, device: int) -> Tuple[float, int, int, int, int]:
+    """The members of lqsgd_drop."""
+    if isinstance(seed, torch.Tensor):
+        if seed.dtype != torch.int64 or seed.numel() != 2 or not seed.is_contiguous() or seed.get_device() != device:
+            raise ValueError("seed must be a whole number or a contiguous int64 tensor of two on the call's device: the seed and what is added to offset")
+        return p, 0, 0, offset & 0xFFFFFFFFFFFFFFFF, seed.data_ptr()
+    return p, 0, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF, 0
+
+
+def dropout(x: torch.Tensor, p: float, seed: Seed, offset: int = 0, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + dropout(x): a value is dropped with probability rint(65536 p) / 65536, 0 <= p < 1, what is kept grows by the inverse of the
+    rest.  The mask is a function of seed, offset and the value's row and column alone and never stored: dropout(dy, p, seed, offset) is the
+    gradient.  Take an offset once per mask.  seed: a whole number, or a CUDA int64 tensor (seed, what is added to offset), read when the
+    kernels run, so that the replays of a captured graph need not repeat a mask.  `out` may be x or the residual."""
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return dropout(x, p, seed, offset, residual, out)
+    xp, xl = _matrix(x, "x", dev)
+    dtype = x.dtype
+    rows, cols = x.shape
+    rp = rl = 0
+    if residual is not None:
+        rp, rl = _matrix(residual, "residual", dev, dtype, rows, cols)
+    y = _empty(rows, cols, dtype, x.device) if out is None else out
+    yp, yl = _matrix(y, "out", dev, dtype, rows, cols)
+    rc = _library().lqsgd_dropout(xp, xl, rp, rl, _dtype(x, "x"), rows, cols, _DROP.pack(*_drop(p, seed, offset, dev)), yp, yl, _stream(dev))
+    if rc:
+        B._check(rc)
+    if out is not None:
+        _written(out)
+    return y
+
+
+# ----------------------------------------------------------------------------------------------- root-mean-square norm
+
+class RmsNormOut(NamedTuple):
+    y: Optional[torch.Tensor]
+    h: torch.Tensor
+    rstd: torch.Tensor
+    h8: Optional[Packed8]
+    y8: Optional[Packed8]
+    rows8: Optional[Rows8]
+
+
+def rms_norm(x: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: Optional[torch.Tensor] = None, p: float = 0.0, seed: Seed = 0,
+             offset: int = 0, want_y: bool = True, save_h8: bool = False, save_y8: bool = False, save_rows8: bool = False) -> RmsNormOut:
+    """h = residual + dropout(x, p, seed, offset) and y = gamma h rstd, rstd = 1 / sqrt(mean(h^2) + eps) over each row; x and residual rows x cols,
+    bfloat16, float16 or float32, gamma float32.  Without a residual and with p = 0, h is x itself.  save_h8 / save_y8 also return the 8-bit
+    forms of h / of y as stored, save_rows8 y (before its rounding) in rows of signed codes; y itself is None without want_y."""
+    dev = x.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rms_norm(x, gamma, eps, residual, p, seed, offset, want_y, save_h8, save_y8, save_rows8)
+    dtype, device = x.dtype, x.device
+    xp, xl = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    rp = rl = hp = yp = 0
+    if residual is not None:
+        rp, rl = _matrix(residual, "residual", dev, dtype, rows, cols)
+    h, y = x, None
+    if residual is not None or p > 0:
+        h = _empty(rows, cols, dtype, device)
+        hp = h.data_ptr()
+    if want_y:
+        y = _empty(rows, cols, dtype, device)
+        yp = y.data_ptr()
+    rstd = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+    h8 = Packed8.empty(rows, cols, device) if save_h8 else None
+    y8 = Packed8.empty(rows, cols, device) if save_y8 else None
+    r8 = Rows8.empty(rows, cols, device) if save_rows8 else None
+    rc = _library().lqsgd_rms_norm_forward(
+        _RMS.pack(_RMS.size, _dtype(x, "x"), rows, cols, eps, *_drop(p, seed, offset, dev), xp, xl, rp, rl, 0, 0, 0, 0, hp, cols, yp, cols, 0, 0, 0, 0,
+                  _vector(gamma, "gamma", dev, cols), rstd.data_ptr(), 0, *(h8._fresh() if save_h8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8),
+                  *(r8._fresh() if save_rows8 else _NO_ROWS8), 0, 0), _stream(dev))
+    if rc:
+        B._check(rc)
+    return RmsNormOut(y, h, rstd, h8, y8, r8)
+
+
+def rms_norm_grad(dy: torch.Tensor, h: Union[torch.Tensor, Packed8], gamma: torch.Tensor, rstd: torch.Tensor, skip: Optional[torch.Tensor] = None,
+                  p: float = 0.0, seed: Seed = 0, offset: int = 0, gamma_grad: bool = True) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """(dx, dresidual, dgamma) of rms_norm: h as the forward call returned it, or its 8-bit form, rstd as it returned it, skip the gradient that
+    arrives at h from elsewhere, p, seed and offset the forward call's.  With p = 0 dx and dresidual are one tensor.  dgamma is None without
+    gamma_grad."""
+    dev = dy.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rms_norm_grad(dy, h, gamma, rstd, skip, p, seed, offset, gamma_grad)
+    dtype, device = dy.dtype, dy.device
+    yp, yl = _matrix(dy, "dy", dev)
+    rows, cols = dy.shape
+    hp, hl, hf, sp, sl = 0, 0, _NONE8, 0, 0
+    if isinstance(h, Packed8):
+        hf = _kept(h, "h", dev, rows, cols)
+    else:
+        hp, hl = _matrix(h, "h", dev, dtype, rows, cols)
+    if skip is not None:
+        sp, sl = _matrix(skip, "skip", dev, dtype, rows, cols)
+    dx = _empty(rows, cols, dtype, device)
+    dres, dp = dx, 0
+    if p > 0:
+        dres = _empty(rows, cols, dtype, device)
+        dp = dres.data_ptr()
+    dgamma, gp = None, 0
+    if gamma_grad:
+        dgamma = torch.empty_strided((cols,), (1,), dtype=torch.float32, device=device)
+        gp = dgamma.data_ptr()
+    lib = _library()
+    _call(lib.lqsgd_rms_norm_backward,
+          (_RMS.size, _dtype(dy, "dy"), rows, cols, 0.0, *_drop(p, seed, offset, dev), 0, 0, 0, 0, yp, yl, sp, sl, hp, hl, 0, 0, dx.data_ptr(), cols, dp, cols,
+           _vector(gamma, "gamma", dev, cols), _vector(rstd, "rstd", dev, rows), gp, *hf, *_NONE8, *_NO_ROWS8),
+          _RMS, lib.lqsgd_rms_norm_workspace_bytes, 1, device)
+    return dx, dres, dgamma
+
+
 # -------------------------------------------------------------------------------------------------------- linear layers
 
 class LinearOut(NamedTuple):
@@ -420,6 +648,47 @@ def linear_grad_weight(dz: torch.Tensor, x: Union[torch.Tensor, Packed8], out: O
     if out is not None:
         _written(out)
     return dw
+
+
+def _rows8_bytes(_, args: bytes, need) -> int:
+    return _library().lqsgd_linear_rows8_workspace_bytes(args, need)
+
+
+def linear_rows8(x: Rows8, w: Rows8, bias: Optional[torch.Tensor] = None, act: str = "none", residual: Optional[torch.Tensor] = None,
+                 dtype: torch.dtype = torch.bfloat16, save_z8: bool = False, save_y8: bool = False, out: Optional[torch.Tensor] = None) -> LinearOut:
+    """y = act(x w^T + bias) + residual in 8-bit integers: x rows x in with a scale per row, w out x in with a scale per output channel, the
+    sums exact in 32 bits (in <= 131071).  residual and y have `dtype`, bfloat16 or float16 (that of residual or out where one is given); bias
+    float32.  save_z8 / save_y8 as of linear.  `out` may be the residual."""
+    if not isinstance(x, Rows8):
+        raise ValueError("x must be the Rows8 form of a matrix")
+    dev = x.codes.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return linear_rows8(x, w, bias, act, residual, dtype, save_z8, save_y8, out)
+    device = x.codes.device
+    if residual is not None or out is not None:
+        dtype = (residual if residual is not None else out).dtype
+    code = DTYPES.get(dtype)
+    if code is None or code == 2:
+        raise ValueError(f"dtype must be bfloat16 or float16, not {dtype}")
+    xf = _rows(x, "x", dev)
+    rows, cin = x.codes.shape
+    wf = _rows(w, "w", dev, -1, cin)
+    cout = w.codes.shape[0]
+    rp = rl = 0
+    if residual is not None:
+        rp, rl = _matrix(residual, "residual", dev, dtype, rows, cout)
+    y = _empty(rows, cout, dtype, device) if out is None else out
+    yp, yl = _matrix(y, "out", dev, dtype, rows, cout)
+    z8 = Packed8.empty(rows, cout, device) if save_z8 else None
+    y8 = Packed8.empty(rows, cout, device) if save_y8 else None
+    _call(_library().lqsgd_linear_rows8_forward,
+          (_LINEAR8.size, code, _act(act), 0, rows, cin, cout, *xf, *wf, 0 if bias is None else _vector(bias, "bias", dev, cout), rp, rl, yp, yl,
+           *(z8._fresh() if save_z8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8), _status_word(device)),
+          _LINEAR8, _rows8_bytes, 0, device)
+    if out is not None:
+        _written(out)
+    return LinearOut(y, z8, y8)
 
 
 # ------------------------------------------------------------------------------------------------------------ group norm
@@ -579,3 +848,114 @@ def norm_layer(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, groups:
     """group_norm() as a differentiable function with x kept in 8 bits.  `keep`, a list, receives the output's 8-bit form
     (for the linear layer that follows).  Differentiable once: a second derivative raises."""
     return _NormLayer.apply(x, gamma, beta, groups, eps, act, keep, torch.is_grad_enabled())
+
+
+def _kept_seed(ctx, p: float, seed: Seed, offset: int, *tensors) -> None:
+    """Keeps a dropout's arguments for the backward pass, a seed on the device among the saved tensors (writing it in between raises)."""
+    on_device = isinstance(seed, torch.Tensor)
+    ctx.save_for_backward(*tensors, seed if on_device else None)
+    ctx.drop = p, None if on_device else seed, offset
+
+
+def _drop_again(ctx, saved: Optional[torch.Tensor]) -> Tuple[float, Seed, int]:
+    p, seed, offset = ctx.drop
+    return p, saved if seed is None else seed, offset
+
+
+class _DropoutLayer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, offset):
+        _kept_seed(ctx, p, seed, offset)
+        return dropout(_apart(x), p, seed, offset, residual if residual is None else _apart(residual))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        p, seed, offset = _drop_again(ctx, *ctx.saved_tensors)
+        dx = dropout(_apart(dy), p, seed, offset) if ctx.needs_input_grad[0] else None
+        return dx, (dy if ctx.needs_input_grad[1] else None), None, None, None
+
+
+def dropout_layer(x: torch.Tensor, p: float, seed: Seed, offset: int = 0, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dropout() as a differentiable function that keeps nothing but its arguments.  Differentiable once: a second derivative raises."""
+    return _DropoutLayer.apply(x, residual, p, seed, offset)
+
+
+class _RmsLayer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, gamma, eps, p, seed, offset, keep, keep_rows8, recording):
+        wanted = recording and any(ctx.needs_input_grad[:3])
+        r = rms_norm(_apart(x), gamma, eps, residual if residual is None else _apart(residual), p, seed, offset, save_h8=wanted, save_y8=keep is not None,
+                     save_rows8=keep_rows8 is not None)
+        ctx.set_materialize_grads(False)
+        if wanted:
+            _kept_seed(ctx, p, seed, offset, r.h8.codes, r.h8.exps, gamma, r.rstd)
+        if keep is not None:
+            keep.append(r.y8)
+        if keep_rows8 is not None:
+            keep_rows8.append(r.rows8)
+        return r.y if residual is None else (r.y, r.h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        codes, exps, gamma, rstd, seed = ctx.saved_tensors
+        for_x, for_residual, for_gamma = ctx.needs_input_grad[:3]
+        drop = _drop_again(ctx, seed)
+        dh = None if dh is None else _apart(dh)
+        if dy is not None:
+            dx, dresidual, dgamma = rms_norm_grad(_apart(dy), Packed8(codes, exps), gamma, rstd, dh, *drop, gamma_grad=for_gamma)
+        elif dh is not None:                            # y was not used: only the sum's gradient arrives
+            dx, dresidual, dgamma = dropout(dh, *drop) if drop[0] > 0 else dh, dh, None
+        else:
+            dx = dresidual = dgamma = None
+        return (dx if for_x else None), (dresidual if for_residual else None), dgamma, None, None, None, None, None, None, None
+
+
+def rms_norm_layer(x: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, keep: Optional[list] = None, keep_rows8: Optional[list] = None) -> torch.Tensor:
+    """rms_norm() of a matrix as a differentiable function with x kept in 8 bits.  `keep` and `keep_rows8`, lists, receive the output's 8-bit
+    forms: of kept activations (linear_layer's x8) and of rows of signed codes (linear_rows8_layer's rows8).  Differentiable once."""
+    return _RmsLayer.apply(x, None, gamma, eps, 0.0, 0, 0, keep, keep_rows8, torch.is_grad_enabled())
+
+
+def add_rms_norm_layer(x: torch.Tensor, residual: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, p: float = 0.0, seed: Seed = 0, offset: int = 0,
+                       keep: Optional[list] = None, keep_rows8: Optional[list] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(y, h) of rms_norm() with a residual, h = residual + dropout(x), as a differentiable function that keeps h in 8 bits and no mask;
+    `keep` and `keep_rows8` as of rms_norm_layer.  Differentiable once."""
+    return _RmsLayer.apply(x, residual, gamma, eps, p, seed, offset, keep, keep_rows8, torch.is_grad_enabled())
+
+
+class _LinearRows8Layer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, act, rows8, weight8, recording):
+        _dtype(x, "x", True)
+        for_x, for_w, for_bias = (n and recording for n in ctx.needs_input_grad[:3])
+        x8 = pack_rows8(_apart(x)) if rows8 is None else rows8
+        w8 = pack_rows8(_apart(weight.detach())) if weight8 is None else weight8
+        r = linear_rows8(x8, w8, bias, act, residual if residual is None else _apart(residual), x.dtype, save_z8=act != "none" and (for_x or for_w or for_bias))
+        z8 = (None, None) if r.z8 is None else (r.z8.codes, r.z8.exps)
+        ctx.save_for_backward(weight if for_x else None, *((x8.codes, x8.scales) if for_w else (None, None)), *z8)
+        ctx.act, ctx.dtype = act, x.dtype
+        return r.y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        weight, xc, xs, zc, ze = ctx.saved_tensors
+        for_x, for_w, for_bias, for_residual = ctx.needs_input_grad[:4]
+        dy = _apart(dy)
+        dx = dw = db = None
+        if for_x or for_w or for_bias:
+            dz, db = act_grad(dy, None if zc is None else Packed8(zc, ze), ctx.act, bias_grad=for_bias)
+            dx = linear_grad_input(dz, _apart(weight.to(ctx.dtype))) if for_x else None
+            dw = linear_grad_weight(dz, unpack_rows8(Rows8(xc, xs), ctx.dtype)) if for_w else None
+        return dx, dw, db, (dy if for_residual else None), None, None, None, None
+
+
+def linear_rows8_layer(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none", residual: Optional[torch.Tensor] = None,
+                       rows8: Optional[Rows8] = None, weight8: Optional[Rows8] = None) -> torch.Tensor:
+    """linear_rows8() as a differentiable function: x bfloat16 or float16, weight and bias float32; both operands of the forward product become
+    rows of signed codes, unless the caller has them (rows8 from the norm in front, weight8 = pack_rows8(weight) kept over micro-batches;
+    x's values are then not read).  The gradients pass the rounding to 8 bits straight through: dx = dz w with the weight in x's type, dw = dz^T x in
+    float32 with x as it was multiplied, and x is kept in those 8 bits.  Differentiable once."""
+    return _LinearRows8Layer.apply(x, weight, bias, residual, act, rows8, weight8, torch.is_grad_enabled())
