@@ -548,7 +548,8 @@ typedef struct lqsgd_rows8 {
 
 int lqsgd_pack_rows8(const void* dev_x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t cols,
                      const lqsgd_rows8* host_out, void* cuda_stream);
-/* y = scale code, rounded to dtype; past its range its largest finite value.  cols 1 .. 2^24 in both. */
+/* y = scale code, rounded to dtype; past its range its largest finite value.  rows 0 .. 2^28, cols 1 .. 2^24, no
+ * more than 2^40 values, here, in packing, in dropout and in the norm. */
 int lqsgd_unpack_rows8(const lqsgd_rows8* host_in, int64_t rows, int32_t cols, void* dev_y, int64_t ld_y, int32_t dtype,
                        void* cuda_stream);
 
@@ -582,7 +583,7 @@ int lqsgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int
 typedef struct lqsgd_rms_norm {
   uint32_t struct_size;   /* sizeof(lqsgd_rms_norm) */
   int32_t dtype;          /* of all matrices: any lqsgd_dtype */
-  int64_t rows;           /* 0 .. 2^31 - 1 */
+  int64_t rows;           /* 0 .. 2^28 */
   int32_t cols;           /* 1 .. 2^24 */
   float eps;              /* forward only, >= 0 */
   lqsgd_drop drop;

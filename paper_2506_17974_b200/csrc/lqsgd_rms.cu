@@ -5,6 +5,8 @@
 // lanes of a warp, longer ones by a block; rows beyond what a block holds are read twice.
 #include "lqsgd_rows_dev.cuh"
 
+#include <atomic>
+
 namespace lqsgd {
 namespace {
 
@@ -19,336 +21,464 @@ struct RmsArgs {
   Drop drop;
   int64_t rows;
   int32_t cols, lane_shift;
-  float eps;
-  bool vec_x, vec_residual, vec_dy, vec_skip, vec_h, vec_y, vec_dx, vec_dresidual, vec_gamma, vec_h8, vec_y8, vec_r8;
+  float eps, per_col;                        // 1 / cols
+  uint32_t ranks;                            // blocks that hold a row together
+  bool vec_gamma, vec_h8, vec_y8, vec_r8;    // on 16 bytes; rows of 8-bit copies on 8
+};
+// Threads of a block: as many as hold 4096 columns, N runs of 8 each.
+template <int N, bool NARROW> struct RowBlock { static constexpr int kThreads = NARROW ? 256 : kBlockRuns / N; };
+
+// What a thread touches of one row of the forward call.
+template <int DT, int HOW>
+struct ForwardRow {
+  const RmsArgs& a;
+  const uint32_t (&room)[kDropRoom];
+  Lanes l;
+  int64_t row;
+  Cursor<DT, HOW> x, residual, h, y;
+  const float* gamma;
+  uint64_t block;                            // dropout's of the thread's first run
+  __device__ __forceinline__ ForwardRow(const RmsArgs& a_, const uint32_t (&room_)[kDropRoom], int64_t row_, const Lanes& l_)
+      : a(a_), room(room_), l(l_), row(row_), x(a.x, row * a.ld_x, l), residual(a.residual, row * a.ld_residual, l), h(a.h, row * a.ld_h, l),
+        y(a.y, row * a.ld_y, l), gamma(a.gamma + l.col), block((uint64_t)row * (uint32_t)((a.cols + kRun - 1) / kRun) + l.col / kRun) {}
+  __device__ __forceinline__ void ask(int i, Raw<DT, HOW>& rx, Raw<DT, HOW>& rr) const {
+    fetch(x, l, i, rx);
+    if (a.residual) fetch(residual, l, i, rr);
+  }
+  // h = residual + dropout(x), as it is stored, and its values
+  __device__ __forceinline__ void make_h(int i, const Raw<DT, HOW>& rx, const Raw<DT, HOW>& rr, Piece<DT>& ph, float (&v)[kRun]) const {
+    settle(rx, x, l, i, ph);
+    open_words<DT>(ph, v);
+    if (!a.h) return;
+    float r[kRun] = {};
+    if (a.residual) {
+      Piece<DT> t;
+      settle(rr, residual, l, i, t);
+      open_words<DT>(t, r);
+    }
+    if (a.drop.threshold) {
+      drop_run(a.drop, room, block + 32 * i, v, r);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) v[j] += r[j];
+    }
+    close_words<DT>(v, ph);
+    open_words<DT>(ph, v);
+  }
+  // squares into `sum`, the largest |h gamma| into `top`
+  __device__ __forceinline__ void add_squares(int i, const float (&v)[kRun], float& sum, float& top) const {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) sum = fmaf(v[j], v[j], sum);
+    if (a.r8.dev_codes) {
+      float g[kRun];
+      fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) g[j] *= v[j];
+      top = largest(top, g);
+    }
+  }
+  // the row's figures, written by one of its threads
+  __device__ __forceinline__ void figures(bool mine, float sum, float top, float& rstd, float& inv) const {
+    rstd = rsqrtf(fmaf(sum, a.per_col, a.eps));
+    float scale = 0.f;
+    if (a.r8.dev_codes) row_scale(top * rstd, scale, inv);
+    if (mine && l.on) {
+      a.rstd[row] = rstd;
+      if (a.r8.dev_codes) a.r8.dev_scales[row] = scale;
+    }
+  }
+  // y of run i of N and the copies in 8 bits; py holds y as stored, of the run before when it comes
+  template <int N>
+  __device__ __forceinline__ void put_y(int i, float rstd, float inv, const Piece<DT>& ph, Piece<DT>& py) const {
+    float v[kRun], g[kRun];
+    open_words<DT>(ph, v);
+    fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
+    if (a.h8.dev_codes) put_packed_run<HOW>(a.h8.dev_codes + row * a.h8.ld_codes + l.col, a.h8.dev_exps + row * a.h8.ld_exps + l.col / kGroup, a.vec_h8, l, i, v);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) v[j] = v[j] * rstd * g[j];
+    if (a.r8.dev_codes)
+      put_codes<HOW>(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + l.col, a.vec_r8, l, i, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
+    if (!a.y && !a.y8.dev_codes) return;
+    Piece<DT> p;
+    close_words<DT>(v, p);
+    if (a.y) put<DT, HOW, N>(y, l, i, p, py);
+    py = p;
+    if (a.y8.dev_codes) {
+      open_words<DT>(p, v);
+      put_packed_run<HOW>(a.y8.dev_codes + row * a.y8.ld_codes + l.col, a.y8.dev_exps + row * a.y8.ld_exps + l.col / kGroup, a.vec_y8, l, i, v);
+    }
+  }
 };
 
-// h = residual + dropout(x) of one run, as stored.
-template <int DT, bool RUNS>
-__device__ __forceinline__ void open_h(const RmsArgs& a, const Piece<DT>& x, const Piece<DT>& res, uint64_t block, typename Elem<DT>::T* turn, float (&v)[kRun]) {
-  open_piece<DT, RUNS>(x, turn, v);
-  float r[kRun] = {};
-  if (a.residual) open_piece<DT, RUNS>(res, turn, r);
-  if (a.drop.threshold) drop_run(a.drop, block, v, r);
-  else if (a.residual) {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] += r[j];
-  }
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
-}
-// Squares into `sum`, the largest |h gamma| into `top`.
-__device__ __forceinline__ void add_squares(const RmsArgs& a, const Place& s, const float (&v)[kRun], float& sum, uint32_t& top) {
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) sum = fmaf(v[j], v[j], sum);
-  if (a.r8.dev_codes) {
-    float g[kRun];
-    load_vector(a.gamma, s, a.vec_gamma, g);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j] * g[j]) & 0x7fffffffu);
-  }
-}
-// y of one run and its copies in 8 bits.
-template <int DT, bool RUNS>
-__device__ __forceinline__ void put_y(const RmsArgs& a, int64_t row, const Place& s, bool on, float rstd, float inv, typename Elem<DT>::T* turn, float (&v)[kRun]) {
-  using T = typename Elem<DT>::T;
-  if (a.h8.dev_codes) put_packed_run(a.h8, a.vec_h8, row, s, on && s.have > 0, v);
-  float g[kRun];
-  load_vector(a.gamma, s, a.vec_gamma, g);
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) v[j] = v[j] * rstd * g[j];
-  if (a.r8.dev_codes && on && s.have > 0)
-    store_codes(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + s.col, a.vec_r8 && s.have == kRun, s.have,
-                make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
-  if (a.y && on && (!RUNS || s.have > 0)) store_piece<DT, RUNS>(static_cast<T*>(a.y) + row * a.ld_y, s, a.cols, a.vec_y && s.have == kRun, turn, v);
-  if (a.y8.dev_codes) {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] = as_stored<DT>(v[j]);
-    put_packed_run(a.y8, a.vec_y8, row, s, on && s.have > 0, v);
-  }
-}
-__device__ __forceinline__ float inverse_rms(float sum, int cols, float eps) { return 1.f / sqrtf(sum / (float)cols + eps); }
-
-template <int DT, int N, bool NARROW, bool RUNS>
-__global__ void __launch_bounds__(NARROW ? 256 : 512)
-rms_forward_kernel(RmsArgs a) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : NARROW ? 8 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[32];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<NARROW> team(a.lane_shift);
-  const int64_t row = team.row;
-  const bool on = !NARROW || row < a.rows;
+template <int DT, int N, bool NARROW, int HOW>
+__global__ void __launch_bounds__(RowBlock<N, NARROW>::kThreads)
+rms_forward_kernel(const __grid_constant__ RmsArgs a) {
+  using Rows = Team<NARROW, N>;
+  __shared__ typename Rows::Slots slots;
+  __shared__ uint32_t room[kDropRoom];
+  const Rows team(a.lane_shift, a.ranks);
+  const ForwardRow<DT, HOW> io(a, room, team.row, team.lanes(a.cols, !NARROW || team.row < a.rows));
   train_pdl_wait();
-  open_drop(a.drop);
-  Piece<DT> x[N], res[N];
+  open_drop(a.drop, room);
+  Raw<DT, HOW> x[N], res[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
+  Piece<DT> h[N], y;
+  float sum = 0.f, top = 0.f, rstd, inv = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const Place s = team.place(i, a.cols);
-#pragma unroll
-    for (int k = 0; k < (int)(sizeof(x[i].w) / 4); ++k) x[i].w[k] = res[i].w[k] = 0u;
-    if (on && (!RUNS || s.have > 0)) {
-      load_piece<DT, RUNS>(static_cast<const T*>(a.x) + row * a.ld_x, s, a.cols, a.vec_x && s.have == kRun, x[i]);
-      if (a.residual) load_piece<DT, RUNS>(static_cast<const T*>(a.residual) + row * a.ld_residual, s, a.cols, a.vec_residual && s.have == kRun, res[i]);
-    }
+    float v[kRun];
+    io.make_h(i, x[i], res[i], h[i], v);
+    if (a.h) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
+    io.add_squares(i, v, sum, top);
   }
-  float v[N][kRun], sum = 0.f;
-  uint32_t top = 0;
-  const uint64_t block0 = (uint64_t)row * ((a.cols + kRun - 1) / kRun);
+  team.join(sum, top, a.r8.dev_codes != nullptr, slots);
+  io.figures(team.first(), sum, top, rstd, inv);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const Place s = team.place(i, a.cols);
-    open_h<DT, RUNS>(a, x[i], res[i], block0 + s.col / kRun, turn, v[i]);
-    if (a.h && on && (!RUNS || s.have > 0)) store_piece<DT, RUNS>(static_cast<T*>(a.h) + row * a.ld_h, s, a.cols, a.vec_h && s.have == kRun, turn, v[i]);
-    add_squares(a, s, v[i], sum, top);
-  }
-  team.join(sum, top, slots);
-  const float rstd = inverse_rms(sum, a.cols, a.eps);
-  float scale = 0.f, inv = 0.f;
-  if (a.r8.dev_codes) row_scale(__uint_as_float(top) * rstd, scale, inv);
-  if (on && team.t == 0) {
-    a.rstd[row] = rstd;
-    if (a.r8.dev_codes) a.r8.dev_scales[row] = scale;
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) put_y<DT, RUNS>(a, row, team.place(i, a.cols), on, rstd, inv, turn, v[i]);
+  for (int i = 0; i < N; ++i) io.template put_y<N>(i, rstd, inv, h[i], y);
 }
 
-// Rows longer than a block holds: h is computed (and stored) in a first pass and computed again in a second.
-template <int DT, bool RUNS>
+// Rows longer than a cluster holds: h is computed (and stored) in a first pass and computed again in a second.
+template <int DT, int HOW>
 __global__ void __launch_bounds__(512)
-rms_forward_long_kernel(RmsArgs a) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[32];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<false> team(0);
-  const int64_t row = team.row;
+rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
+  using Rows = Team<false, 1>;
+  __shared__ typename Rows::Slots slots;
+  __shared__ uint32_t room[kDropRoom];
+  const Rows team(0, 1);
   train_pdl_wait();
-  open_drop(a.drop);
-  const uint64_t block0 = (uint64_t)row * ((a.cols + kRun - 1) / kRun);
-  const int steps = team.steps(a.cols);
-  auto fetch = [&](const Place& s, float (&v)[kRun]) {
-    Piece<DT> x = {}, res = {};
-    if (!RUNS || s.have > 0) {
-      load_piece<DT, RUNS>(static_cast<const T*>(a.x) + row * a.ld_x, s, a.cols, a.vec_x && s.have == kRun, x);
-      if (a.residual) load_piece<DT, RUNS>(static_cast<const T*>(a.residual) + row * a.ld_residual, s, a.cols, a.vec_residual && s.have == kRun, res);
+  open_drop(a.drop, room);
+  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
+  float sum = 0.f, top = 0.f, rstd = 0.f, inv = 0.f;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+    for (int k = 0; k < steps; ++k) {
+      const ForwardRow<DT, HOW> io(a, room, team.row, team.lanes(a.cols, true, k));
+      Raw<DT, HOW> x, res;
+      Piece<DT> h, y;
+      float v[kRun];
+      io.ask(0, x, res);
+      io.make_h(0, x, res, h, v);
+      if (pass == 0) {
+        if (a.h) put<DT, HOW, 1>(io.h, io.l, 0, h, h);
+        io.add_squares(0, v, sum, top);
+      } else {
+        io.template put_y<1>(0, rstd, inv, h, y);
+      }
     }
-    open_h<DT, RUNS>(a, x, res, block0 + s.col / kRun, turn, v);
-  };
-  float sum = 0.f;
-  uint32_t top = 0;
-  for (int i = 0; i < steps; ++i) {
-    const Place s = team.place(i, a.cols);
-    float v[kRun];
-    fetch(s, v);
-    if (a.h && (!RUNS || s.have > 0)) store_piece<DT, RUNS>(static_cast<T*>(a.h) + row * a.ld_h, s, a.cols, a.vec_h && s.have == kRun, turn, v);
-    add_squares(a, s, v, sum, top);
-  }
-  team.join(sum, top, slots);
-  const float rstd = inverse_rms(sum, a.cols, a.eps);
-  float scale = 0.f, inv = 0.f;
-  if (a.r8.dev_codes) row_scale(__uint_as_float(top) * rstd, scale, inv);
-  if (team.t == 0) {
-    a.rstd[row] = rstd;
-    if (a.r8.dev_codes) a.r8.dev_scales[row] = scale;
-  }
-  for (int i = 0; i < steps; ++i) {
-    const Place s = team.place(i, a.cols);
-    float v[kRun];
-    fetch(s, v);
-    put_y<DT, RUNS>(a, row, s, true, rstd, inv, turn, v);
+    if (pass == 0) {
+      team.join(sum, top, a.r8.dev_codes != nullptr, slots);
+      ForwardRow<DT, HOW>(a, room, team.row, team.lanes(a.cols, true)).figures(team.first(), sum, top, rstd, inv);
+    }
   }
 }
 
 // ---- backward
-// dy and h of one run, whichever form h has.
-template <int DT, bool RUNS>
-struct GradPieces {
-  Piece<DT> dy, h, skip;
-  uint2 codes;
-  uint32_t exp;
-  __device__ __forceinline__ void load(const RmsArgs& a, int64_t row, const Place& s, bool on, bool with_skip) {
-    using T = typename Elem<DT>::T;
+// With h as it comes (xh = h rstd), a row needs <u xh> = rstd <dy h gamma>, and then d = gamma rstd dy - (rstd^2 <u xh>) h + skip.
+// A block (or cluster) keeps its columns' sums for dgamma in registers and walks rows.  What it reads goes through shared memory, a row
+// ahead (cp.async), every thread its own runs: registers have no room for rows in flight, and a row's values are read a second time behind the
+// sum.  h from its 8-bit form is decoded once, to bf16, in which it is exact.
+constexpr int kStages = 2;
+// Eight codes as bf16: |128 + m| with the magnitude m below is a bf16 number (0x4300 | m), and (128 + m) 2^e - 128 2^e is m 2^e exactly; the
+// signs are put on top.  For exponents from kQuickByte on 128 2^e leaves the range.
+__device__ __forceinline__ void decode_bf16(uint2 c, uint32_t eb, uint32_t (&w)[4]) {
+  if (eb <= kQuickByte) {
+    const uint32_t step = ((eb + 1) << 7) * 0x00010001u, off = (((eb + 8) << 7) | 0x8000u) * 0x00010001u;
 #pragma unroll
-    for (int k = 0; k < (int)(sizeof(dy.w) / 4); ++k) dy.w[k] = h.w[k] = skip.w[k] = 0u;
-    codes = make_uint2(0u, 0u);
-    exp = kExpBias;
-    if (!on || (RUNS && s.have <= 0)) return;
-    load_piece<DT, RUNS>(static_cast<const T*>(a.dy) + row * a.ld_dy, s, a.cols, a.vec_dy && s.have == kRun, dy);
-    if (!a.h8.dev_codes) {
-      load_piece<DT, RUNS>(static_cast<const T*>(a.h) + row * a.ld_h, s, a.cols, a.vec_h && s.have == kRun, h);
-    } else if (s.have > 0) {
-      codes = load_codes(a.h8.dev_codes + row * a.h8.ld_codes + s.col, a.vec_h8 && s.have == kRun, s.have);
-      exp = a.h8.dev_exps[row * a.h8.ld_exps + s.col / kGroup];
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t of = j < 2 ? c.x : c.y, m = of & 0x7f7f7f7fu;
+      const uint32_t big = __byte_perm(m, 0x43u, j & 1 ? 0x4342 : 0x4140), sign = __byte_perm(of, 0u, j & 1 ? 0x3424 : 0x1404);
+      uint32_t r;
+      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(big), "r"(step), "r"(off));
+      w[j] = r | (sign & 0x80008000u);
     }
-    if (with_skip && a.skip) load_piece<DT, RUNS>(static_cast<const T*>(a.skip) + row * a.ld_skip, s, a.cols, a.vec_skip && s.have == kRun, skip);
-  }
-  __device__ __forceinline__ void open_h(const RmsArgs& a, typename Elem<DT>::T* turn, float (&v)[kRun]) const {
-    if (a.h8.dev_codes) decode_run(codes, (int)exp, v);
-    else open_piece<DT, RUNS>(h, turn, v);
-  }
-};
-// d of one run into dx and dresidual.
-template <int DT, bool RUNS>
-__device__ __forceinline__ void put_d(const RmsArgs& a, int64_t row, const Place& s, bool on, uint64_t block, const Piece<DT>& skip, typename Elem<DT>::T* turn, float (&d)[kRun]) {
-  using T = typename Elem<DT>::T;
-  if (a.skip) {
-    float k[kRun];
-    open_piece<DT, RUNS>(skip, turn, k);
+  } else {
+    float v[kRun];
+    decode_run(c, (int)eb, v);
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) d[j] += k[j];
-  }
-  if (!on || (RUNS && s.have <= 0)) return;
-  if (a.dresidual) store_piece<DT, RUNS>(static_cast<T*>(a.dresidual) + row * a.ld_dresidual, s, a.cols, a.vec_dresidual && s.have == kRun, turn, d);
-  if (a.dx) {
-    const float none[kRun] = {};
-    if (a.drop.threshold) drop_run(a.drop, block, d, none);
-    store_piece<DT, RUNS>(static_cast<T*>(a.dx) + row * a.ld_dx, s, a.cols, a.vec_dx && s.have == kRun, turn, d);
+    for (int j = 0; j < 4; ++j) w[j] = pack_pair<LQSGD_BF16>(v[2 * j], v[2 * j + 1]);
   }
 }
+__device__ __forceinline__ void open_bf16(const uint32_t (&w)[4], float (&v)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = open_pair<LQSGD_BF16>(w[j]);
+    v[2 * j] = f.x;
+    v[2 * j + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void copy_async(uint8_t* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+// What a thread reads and writes of one row of the backward call.
+template <int DT, int HOW>
+struct BackwardRow {
+  static constexpr int kPieces = Raw<DT, HOW>::kPieces;
+  const RmsArgs& a;
+  const uint32_t (&room)[kDropRoom];
+  Lanes l;
+  int64_t row;
+  Cursor<DT, HOW> dy, h, skip;
+  __device__ __forceinline__ BackwardRow(const RmsArgs& a_, const uint32_t (&room_)[kDropRoom], int64_t row_, const Lanes& l_)
+      : a(a_), room(room_), l(l_), row(row_), dy(a.dy, row * a.ld_dy, l), h(a.h, row * a.ld_h, l), skip(a.skip, row * a.ld_skip, l) {}
+  __device__ __forceinline__ const uint8_t* codes() const { return a.h8.dev_codes + row * a.h8.ld_codes + l.col; }
+  __device__ __forceinline__ bool codes_whole(int i) const { return HOW == kWhole || (a.vec_h8 && l.have(i) >= kRun); }
+  // Run i on its way into a thread's places in shared memory, `unit` bytes apart.
+  __device__ __forceinline__ void ask(const Cursor<DT, HOW>& c, int i, uint8_t* to, uint32_t unit) const {
+    using T = typename Elem<DT>::T;
+    if (HOW == kWhole || c.pieces(l, i)) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        if (k < kRunBytes<DT> / 16 || c.shift) copy_async(to + k * unit, c.at(i) + 16 * k);
+    } else {
+      Raw<DT, HOW> v;
+      fetch(c, l, i, v);
+#pragma unroll
+      for (int k = 0; k < kRunBytes<DT> / 16; ++k) *reinterpret_cast<uint4*>(to + k * unit) = reinterpret_cast<const uint4*>(v.w)[k];
+    }
+  }
+  __device__ __forceinline__ void take(const Cursor<DT, HOW>& c, int i, const uint8_t* from, uint32_t unit, float (&v)[kRun]) const {
+    Raw<DT, HOW> raw;
+    Piece<DT> p;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) reinterpret_cast<uint4*>(raw.w)[k] = *reinterpret_cast<const uint4*>(from + k * unit);
+    settle(raw, c, l, i, p);
+    open_words<DT>(p, v);
+  }
+  // d of run i of N into dx and dresidual; as stored in px and pr, of the run before when they come
+  template <int N>
+  __device__ __forceinline__ void put_d(int i, float (&d)[kRun], Piece<DT>& px, Piece<DT>& pr) const {
+    Piece<DT> out;
+    if (a.dresidual) {
+      close_words<DT>(d, out);
+      put<DT, HOW, N>(Cursor<DT, HOW>(a.dresidual, row * a.ld_dresidual, l), l, i, out, pr);
+      pr = out;
+    }
+    if (a.dx) {
+      const float none[kRun] = {};
+      if (a.drop.threshold) drop_run(a.drop, room, (uint64_t)row * (uint32_t)((a.cols + kRun - 1) / kRun) + l.col / kRun + 32 * i, d, none);
+      close_words<DT>(d, out);
+      put<DT, HOW, N>(Cursor<DT, HOW>(a.dx, row * a.ld_dx, l), l, i, out, px);
+      px = out;
+    }
+  }
+};
 
-template <int DT, int N, bool NARROW, bool RUNS>
-__global__ void __launch_bounds__(NARROW ? 256 : 512)
-rms_backward_kernel(RmsArgs a) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : NARROW ? 8 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[2][32];
-  __shared__ float sums[NARROW ? 256 * (kRun + 1) : 1];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<NARROW> team(a.lane_shift);
+template <int DT, int N, bool NARROW, int HOW>
+__global__ void __launch_bounds__(RowBlock<N, NARROW>::kThreads, 512 / RowBlock<N, NARROW>::kThreads)
+rms_backward_kernel(const __grid_constant__ RmsArgs a) {
+  using Rows = Team<NARROW, N>;
+  using Row = BackwardRow<DT, HOW>;
+  extern __shared__ __align__(16) uint8_t grad_smem[];
+  __shared__ typename Rows::Slots slots[2];
+  __shared__ uint32_t room[kDropRoom];
+  const Rows team(a.lane_shift, a.ranks);
   train_pdl_wait();
-  open_drop(a.drop);
-  const float mean = 1.f / (float)a.cols;
+  open_drop(a.drop, room);
+  // [stage][run][dy pieces, skip pieces, h pieces or 8 bytes of codes][thread]
+  const uint32_t unit = blockDim.x * 16, off_skip = Row::kPieces * unit, off_h = off_skip + (a.skip ? Row::kPieces * unit : 0);
+  const uint32_t run_bytes = off_h + (a.h8.dev_codes ? unit / 2 : Row::kPieces * unit), stage_bytes = run_bytes * N;
+  uint8_t* const mine = grad_smem + threadIdx.x * 16;
+  uint8_t* const mine8 = grad_smem + off_h + threadIdx.x * 8;
   float acc[N][kRun];
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int j = 0; j < kRun; ++j) acc[i][j] = 0.f;
-  const int step = team.rows_per_grid();
-  int turn_of = 0;
-  // NARROW: a warp stays together while one of its rows exists
-  const int64_t first = NARROW ? team.row - ((threadIdx.x & 31) >> a.lane_shift) : team.row;
-  for (int64_t r0 = first; r0 < a.rows; r0 += step) {
-    const int64_t row = team.row + (r0 - first);
-    const bool on = row < a.rows;
-    GradPieces<DT, RUNS> p[N];
+  uint32_t exps[N], exps_next[N];
+  float rstd, rstd_next;
+  auto ask = [&](int64_t row, uint32_t at) {
+    rstd_next = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) p[i].load(a, row, team.place(i, a.cols), on, true);
-    const float rstd = on ? a.rstd[row] : 0.f;
-    float xh[N][kRun], u[N][kRun], sum = 0.f;
-    uint32_t top = 0;
+    for (int i = 0; i < N; ++i) exps_next[i] = kExpBias;
+    if (row < a.rows) {
+      const Row r(a, room, row, team.lanes(a.cols, true));
+      rstd_next = a.rstd[row];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const Place s = team.place(i, a.cols);
-      float g[kRun];
-      p[i].open_h(a, turn, xh[i]);
-      open_piece<DT, RUNS>(p[i].dy, turn, u[i]);
-      load_vector(a.gamma, s, a.vec_gamma, g);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) {
-        xh[i][j] *= rstd;
-        acc[i][j] = fmaf(u[i][j], xh[i][j], acc[i][j]);
-        u[i][j] *= g[j];
-        sum = fmaf(u[i][j], xh[i][j], sum);
+      for (int i = 0; i < N; ++i) {
+        if (r.l.have(i) <= 0) continue;
+        uint8_t* to = mine + at + i * run_bytes;
+        r.ask(r.dy, i, to, unit);
+        if (a.skip) r.ask(r.skip, i, to + off_skip, unit);
+        if (a.h8.dev_codes) {
+          uint8_t* to8 = mine8 + at + i * run_bytes;
+          if (r.codes_whole(i))
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to8)), "l"(r.codes() + i * kWarpCols) : "memory");
+          else
+            *reinterpret_cast<uint2*>(to8) = load_codes(r.codes() + i * kWarpCols, false, min(r.l.have(i), kRun));
+          exps_next[i] = a.h8.dev_exps[row * a.h8.ld_exps + r.l.col / kGroup + i * (kWarpCols / kGroup)];
+        } else {
+          r.ask(r.h, i, to + off_h, unit);
+        }
       }
     }
-    team.join(sum, top, slots[turn_of]);
-    turn_of ^= 1;
-    sum *= mean;
-    const uint64_t block0 = (uint64_t)row * ((a.cols + kRun - 1) / kRun);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // NARROW: a warp stays together while one of its rows exists
+  const int64_t first = NARROW ? team.row - ((threadIdx.x & 31) >> team.shift) : team.row;
+  ask(team.row, 0);
+  uint32_t at = 0;
+  int turn = 0;
+#pragma unroll 1
+  for (int64_t r0 = first; r0 < a.rows; r0 += team.rows_per_grid) {
+    const int64_t row = team.row + (r0 - first);
+    rstd = rstd_next;
+#pragma unroll
+    for (int i = 0; i < N; ++i) exps[i] = exps_next[i];
+    ask(row + team.rows_per_grid, at ^ stage_bytes);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    const Row r(a, room, row, team.lanes(a.cols, row < a.rows));
+    const float* gamma = a.gamma + r.l.col;
+    float sum = 0.f, top = 0.f;
+    uint32_t h8[N][4];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const Place s = team.place(i, a.cols);
+      if (!r.l.on || r.l.have(i) <= 0) continue;
+      const uint8_t* from = mine + at + i * run_bytes;
+      float u[kRun], v[kRun], g[kRun];
+      if (a.h8.dev_codes) {
+        decode_bf16(*reinterpret_cast<const uint2*>(mine8 + at + i * run_bytes), exps[i], h8[i]);
+        open_bf16(h8[i], v);
+      } else {
+        r.take(r.h, i, from + off_h, unit, v);
+      }
+      r.take(r.dy, i, from, unit, u);
+      fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) u[i][j] = rstd * (u[i][j] - xh[i][j] * sum);
-      put_d<DT, RUNS>(a, row, s, on, block0 + s.col / kRun, p[i].skip, turn, u[i]);
+      for (int j = 0; j < kRun; ++j) {
+        const float t = u[j] * v[j];
+        acc[i][j] = fmaf(t, rstd, acc[i][j]);
+        sum = fmaf(t, g[j], sum);
+      }
     }
+    team.join(sum, top, false, slots[turn]);
+    turn ^= 1;
+    const float k = rstd * rstd * (rstd * (sum * a.per_col));
+    Piece<DT> px, pr;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float d[kRun] = {}, v[kRun], g[kRun];
+      if (r.l.on && r.l.have(i) > 0) {
+        const uint8_t* from = mine + at + i * run_bytes;
+        if (a.skip) r.take(r.skip, i, from + off_skip, unit, d);
+        if (a.h8.dev_codes) open_bf16(h8[i], v);
+        else r.take(r.h, i, from + off_h, unit, v);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) d[j] = fmaf(-k, v[j], d[j]);
+        r.take(r.dy, i, from, unit, v);
+        fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) d[j] = fmaf(g[j] * rstd, v[j], d[j]);
+      }
+      r.template put_d<N>(i, d, px, pr);
+    }
+    at ^= stage_bytes;
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   if (!a.partial) return;
-  float* out = a.partial + (size_t)blockIdx.x * a.cols;
+  float* out = a.partial + (size_t)(blockIdx.x / team.ranks) * a.cols;
+  float* sums = reinterpret_cast<float*>(grad_smem);
+  const Lanes l = team.lanes(a.cols, true);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const Place s = team.place(i, a.cols);
     if (NARROW) {                                          // the block's rows meet in shared memory
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < kRun; ++j) sums[threadIdx.x * (kRun + 1) + j] = acc[i][j];
       __syncthreads();
-      for (int c = threadIdx.x; c < team.size * kRun; c += 256) {
-        const int col = i * team.size * kRun + c;
+      for (int c = threadIdx.x; c < l.lanes * kRun; c += 256) {
+        const int col = i * kWarpCols + c;
         if (col >= a.cols) continue;
         float t = 0.f;
-        for (int k = 0; k < 256 >> a.lane_shift; ++k) t += sums[((k << a.lane_shift) + c / kRun) * (kRun + 1) + c % kRun];
+        for (int k = 0; k < 256 >> team.shift; ++k) t += sums[((k << team.shift) + c / kRun) * (kRun + 1) + c % kRun];
         out[col] = t;
       }
     } else {
 #pragma unroll
       for (int j = 0; j < kRun; ++j)
-        if (j < s.have) out[s.col + j] = acc[i][j];
+        if (j < l.have(i)) out[l.col + i * kWarpCols + j] = acc[i][j];
     }
   }
 }
 
-// Rows longer than a block holds: <u xh> of each in a first kernel, the rest as a stream over columns.
-template <int DT, bool RUNS>
-__global__ void __launch_bounds__(512)
-rms_dot_kernel(RmsArgs a, float* dots) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[32];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<false> team(0);
-  const int64_t row = team.row;
-  train_pdl_wait();
-  const float rstd = a.rstd[row];
-  float sum = 0.f;
-  uint32_t top = 0;
-  const int steps = team.steps(a.cols);
-  for (int i = 0; i < steps; ++i) {
-    const Place s = team.place(i, a.cols);
-    GradPieces<DT, RUNS> p;
-    p.load(a, row, s, true, false);
-    float h[kRun], u[kRun], g[kRun];
-    p.open_h(a, turn, h);
-    open_piece<DT, RUNS>(p.dy, turn, u);
-    load_vector(a.gamma, s, a.vec_gamma, g);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) sum = fmaf(u[j] * g[j], h[j] * rstd, sum);
+// Rows longer than a cluster holds: <dy h gamma> of each in a first kernel, the rest as a stream over columns.
+template <int DT, int HOW>
+__device__ __forceinline__ void load_dy_h(const BackwardRow<DT, HOW>& r, float (&dy)[kRun], float (&h)[kRun]) {
+  Raw<DT, HOW> raw;
+  Piece<DT> p;
+  fetch(r.dy, r.l, 0, raw);
+  settle(raw, r.dy, r.l, 0, p);
+  open_words<DT>(p, dy);
+  if (!r.a.h8.dev_codes) {
+    fetch(r.h, r.l, 0, raw);
+    settle(raw, r.h, r.l, 0, p);
+    open_words<DT>(p, h);
+  } else {
+    uint2 codes = make_uint2(0u, 0u);
+    int exp = kExpBias;
+    if (r.l.have(0) > 0) {
+      codes = load_codes(r.codes(), r.codes_whole(0), min(r.l.have(0), kRun));
+      exp = r.a.h8.dev_exps[r.row * r.a.h8.ld_exps + r.l.col / kGroup];
+    }
+    decode_run(codes, exp, h);
   }
-  team.join(sum, top, slots);
-  if (team.t == 0) dots[row] = sum / (float)a.cols;
 }
-template <int DT, bool RUNS>
-__global__ void __launch_bounds__(kThreads)
-rms_columns_kernel(RmsArgs a, Deal d, const float* dots) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) float sums[kWarps][32][kRun + 1];
-  T* turn = reinterpret_cast<T*>(&sums[threadIdx.x >> 5][0][0]);
+template <int DT, int HOW>
+__global__ void __launch_bounds__(512)
+rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
+  using Rows = Team<false, 1>;
+  __shared__ typename Rows::Slots slots;
+  __shared__ uint32_t room[kDropRoom];
+  const Rows team(0, 1);
   train_pdl_wait();
-  open_drop(a.drop);
+  float sum = 0.f, top = 0.f;
+  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
+  for (int k = 0; k < steps; ++k) {
+    const BackwardRow<DT, HOW> r(a, room, team.row, team.lanes(a.cols, true, k));
+    float dy[kRun], h[kRun], g[kRun];
+    load_dy_h(r, dy, h);
+    fetch_vector<HOW>(a.gamma + r.l.col, a.vec_gamma, r.l, 0, g);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) sum = fmaf(dy[j] * h[j], g[j], sum);
+  }
+  team.join(sum, top, false, slots);
+  if (team.first()) dots[team.row] = sum * a.per_col;
+}
+template <int DT, int HOW>
+__global__ void __launch_bounds__(kThreads)
+rms_columns_kernel(const __grid_constant__ RmsArgs a, const __grid_constant__ Deal d, const float* dots) {
+  __shared__ __align__(16) float sums[kWarps][32][kRun + 1];
+  __shared__ uint32_t room[kDropRoom];
+  train_pdl_wait();
+  open_drop(a.drop, room);
   const Spot s(d);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warp_cols = kRun * 32;
+  const Lanes l = {s.col, a.cols - s.col, lane, 32, true};
   float acc[kRun] = {}, g[kRun];
-  load_vector(a.gamma, s, a.vec_gamma, g);
+  fetch_vector<HOW>(a.gamma + l.col, a.vec_gamma, l, 0, g);
   for (int64_t row = s.row; row < s.row_end; row += s.row_step) {
-    GradPieces<DT, RUNS> p;
-    p.load(a, row, s, true, true);
-    const float rstd = a.rstd[row], dot = dots[row];
-    float h[kRun], u[kRun];
-    p.open_h(a, turn, h);
-    open_piece<DT, RUNS>(p.dy, turn, u);
+    const BackwardRow<DT, HOW> r(a, room, row, l);
+    float dy[kRun], h[kRun], e[kRun] = {};
+    load_dy_h(r, dy, h);
+    const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
+    if (a.skip) {
+      Raw<DT, HOW> raw;
+      Piece<DT> t;
+      fetch(r.skip, l, 0, raw);
+      settle(raw, r.skip, l, 0, t);
+      open_words<DT>(t, e);
+    }
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      h[j] *= rstd;
-      acc[j] = fmaf(u[j], h[j], acc[j]);
-      u[j] = rstd * (u[j] * g[j] - h[j] * dot);
+      acc[j] = fmaf(dy[j] * h[j], rstd, acc[j]);
+      e[j] = fmaf(g[j] * rstd, dy[j], fmaf(-k, h[j], e[j]));
     }
-    put_d<DT, RUNS>(a, row, s, true, (uint64_t)row * ((a.cols + kRun - 1) / kRun) + s.col / kRun, p.skip, turn, u);
+    Piece<DT> px, pr;
+    r.template put_d<1>(0, e, px, pr);
   }
   if (!a.partial) return;
   // the rows that the block's warps have of one column: warps side by side hold other columns
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warp_cols = kRun * 32;
-  __syncwarp();
 #pragma unroll
   for (int j = 0; j < kRun; ++j) sums[warp][lane][j] = acc[j];
   __syncthreads();
@@ -362,103 +492,102 @@ rms_columns_kernel(RmsArgs a, Deal d, const float* dots) {
   }
 }
 
-// ---- choice of kernel: how a row is dealt out
-constexpr int kNarrow = 1024, kMostForward = 512 * kRun * 8, kMostBackward = 512 * kRun * 4;
-struct Shape {
-  bool narrow;
-  int lane_shift, threads, n;                // n: runs per thread
-  int64_t teams;                             // rows per block
-};
-// Rows of up to 1024 columns in a warp or less, then in blocks of up to 512 threads; the fewest runs per thread that hold the row.
-Shape shape_of(int32_t cols) {
-  Shape s = {};
-  const int runs = (int)ceil_div64(cols, kRun);
-  s.narrow = cols <= kNarrow;
-  if (s.narrow) {
-    s.lane_shift = 2;
-    while (s.lane_shift < 5 && (1 << s.lane_shift) < runs) ++s.lane_shift;
-    s.n = 1;
-    while ((s.n << s.lane_shift) < runs) s.n *= 2;
-    s.threads = 256;
-    s.teams = 256 >> s.lane_shift;
-  } else {
-    s.n = 1;
-    while (s.n * 512 < runs) s.n *= 2;
-    s.threads = (int)ceil_div64(ceil_div64(runs, s.n), 32) * 32;
-    s.teams = 1;
-  }
-  return s;
-}
-bool whole_warps(int32_t cols) { return cols > 128; }                    // rows of fewer columns leave lanes of a warp to other rows
-
+// ---- choice of kernel
 constexpr int kSms = 148;
-int64_t backward_blocks(const Shape& s, int64_t rows) {
-  const int64_t per_sm = s.narrow ? 4 : std::max(1, 1024 / s.threads);
-  return std::min<int64_t>(ceil_div64(rows, s.teams), kSms * per_sm);
+// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type) where rows fill the card; with few rows one run per thread, whose
+// latency is the row's.
+constexpr int kNarrow = 1024;
+template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
+RowShape forward_shape(const lqsgd_rms_norm& a) {
+  return shape_of(a.cols, a.rows < kSms ? 1 : a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow);
 }
 constexpr int kCtasColumns = kSms * 6;
-
+template <int DT> constexpr int kGradRuns = DT == LQSGD_F32 ? 2 : 4;
 struct GradPlan {
-  bool wide;                                 // the two kernels for long rows
-  Shape shape;
+  RowShape shape;
   Deal deal;
   dim3 grid;
   int blocks;                                // of the sums over rows
-  size_t off_partial, bytes;
+  size_t smem, off_partial, bytes;
 };
-GradPlan plan_backward(const lqsgd_rms_norm& a, bool runs) {
+GradPlan plan_backward(const lqsgd_rms_norm& a, int how) {
   GradPlan p = {};
-  p.wide = a.cols > kMostBackward;
-  if (p.wide) {
-    p.deal = make_deal(a.rows, a.cols, runs, kCtasColumns, 8, &p.grid);
+  const bool wide = a.dtype == LQSGD_F32;
+  p.shape = shape_of(a.cols, wide ? kGradRuns<LQSGD_F32> : kGradRuns<LQSGD_BF16>, wide ? 256 : 512);
+  if (!p.shape.held) {
+    p.deal = make_deal(a.rows, a.cols, true, kCtasColumns, 8, &p.grid);
     p.blocks = (int)p.grid.y;
     p.off_partial = (size_t)ceil_div64(a.rows * 4, 256) * 256;
   } else {
-    p.shape = shape_of(a.cols);
-    p.blocks = (int)backward_blocks(p.shape, a.rows);
+    const int pieces = kRun * train_elem(a.dtype) / 16 + (how == kShift ? 1 : 0);
+    const bool kept = a.h8.dev_codes != nullptr;
+    const size_t run = (size_t)16 * pieces * (1 + (a.dev_skip ? 1 : 0) + (kept ? 0 : 1)) + (kept ? 8 : 0);
+    p.smem = std::max(run * kStages * p.shape.n * p.shape.threads, p.shape.narrow ? sizeof(float) * 256 * (kRun + 1) : 0);
+    // 512 threads an SM have registers, as many blocks shared memory (1.5 KB of it are not for rows)
+    const int64_t per_sm = std::max<int64_t>(1, std::min<int64_t>(512 / p.shape.threads, 226 * 1024 / (p.smem + 1536)));
+    p.blocks = (int)std::min<int64_t>(ceil_div64(a.rows, p.shape.teams), std::max<int64_t>(1, kSms * per_sm / p.shape.ranks));
+    p.grid = dim3((unsigned)(p.blocks * p.shape.ranks));
   }
   p.bytes = p.off_partial + (a.dev_dgamma && p.blocks > 1 ? (size_t)p.blocks * a.cols * 4 : 0);
   return p;
 }
 
-template <int DT, bool RUNS>
-cudaError_t launch_forward(const Shape& s, bool wide, const RmsArgs& a, cudaStream_t st) {
-  if (wide) return train_launch(rms_forward_long_kernel<DT, RUNS>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
-  const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
-#define GO(N, NARROW) train_launch(rms_forward_kernel<DT, N, NARROW, RUNS>, grid, block, 0, st, 1, a)
+template <int DT, int HOW>
+cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st) {
+  if (!s.held) return train_launch(rms_forward_long_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
+  const dim3 grid((unsigned)(ceil_div64(a.rows, s.teams) * s.ranks)), block(s.threads);
+#define GO(N, NARROW) train_launch(rms_forward_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, s.ranks, a)
   if (s.narrow) return s.n == 1 ? GO(1, true) : s.n == 2 ? GO(2, true) : GO(4, true);
-  return s.n == 1 ? GO(1, false) : s.n == 2 ? GO(2, false) : s.n == 4 ? GO(4, false) : GO(8, false);
+  return s.n == 1 ? GO(1, false) : GO(kForwardRuns<DT>, false);
 #undef GO
 }
-template <int DT, bool RUNS>
-cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
-  if (p.wide) {
-    const cudaError_t e = train_launch(rms_dot_kernel<DT, RUNS>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a, dots);
-    return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, RUNS>, p.grid, dim3(kThreads), 0, st, 1, a, p.deal, dots);
+template <int DT, int N, bool NARROW, int HOW>
+cudaError_t launch_held(const GradPlan& p, const RmsArgs& a, cudaStream_t st) {
+  auto kernel = rms_backward_kernel<DT, N, NARROW, HOW>;
+  static std::atomic<uint64_t> ready{0};                     // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024)) != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
-  const dim3 grid((unsigned)p.blocks), block(p.shape.threads);
-#define GO(N, NARROW) train_launch(rms_backward_kernel<DT, N, NARROW, RUNS>, grid, block, 0, st, 1, a)
-  if (p.shape.narrow) return p.shape.n == 1 ? GO(1, true) : p.shape.n == 2 ? GO(2, true) : GO(4, true);
-  return p.shape.n == 1 ? GO(1, false) : p.shape.n == 2 ? GO(2, false) : GO(4, false);
+  return train_launch(kernel, p.grid, dim3(p.shape.threads), p.smem, st, p.shape.ranks, a);
+}
+template <int DT, int HOW>
+cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
+  if (!p.shape.held) {
+    const cudaError_t e = train_launch(rms_dot_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a, dots);
+    return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.deal, dots);
+  }
+  const RowShape& s = p.shape;
+#define GO(N, NARROW) launch_held<DT, N, NARROW, HOW>(p, a, st)
+  if (!s.narrow) return GO(kGradRuns<DT>, false);
+  if constexpr (DT == LQSGD_F32) return GO(1, true);
+  else return s.n == 1 ? GO(1, true) : GO(2, true);
 #undef GO
 }
-#define BY_TYPE(dtype, runs, f, ...)                                                                       \
-  ((dtype) == LQSGD_BF16 ? ((runs) ? f<LQSGD_BF16, true>(__VA_ARGS__) : f<LQSGD_BF16, false>(__VA_ARGS__)) \
-   : (dtype) == LQSGD_F16 ? ((runs) ? f<LQSGD_F16, true>(__VA_ARGS__) : f<LQSGD_F16, false>(__VA_ARGS__))  \
-                          : ((runs) ? f<LQSGD_F32, true>(__VA_ARGS__) : f<LQSGD_F32, false>(__VA_ARGS__)))
 
 int check_args(const lqsgd_rms_norm* a) {
   if (!a || a->struct_size != sizeof(lqsgd_rms_norm) || !train_dtype_ok(a->dtype)) return LQSGD_ERR_INVALID_ARG;
-  if (a->rows < 0 || a->rows > 0x7fffffffll || a->cols < 1 || a->cols > (1 << 24)) return LQSGD_ERR_BAD_SHAPE;
+  if (a->rows < 0 || a->rows > (1 << 28) || a->cols < 1 || a->cols > (1 << 24) || a->rows * a->cols > (1ll << 40)) return LQSGD_ERR_BAD_SHAPE;
   return check_drop(a->drop);
 }
-// A matrix argument: *vec tells whether its rows start on 16 bytes (an absent one does not stand in the way).
-int check_matrix(const void* p, int64_t ld, const lqsgd_rms_norm& a, bool* vec) {
-  const int es = train_elem(a.dtype);
-  *vec = !p || vec_rows(p, ld, es, 16) || (a.rows == 1 && train_aligned(p, 16));
+// A matrix argument, or none.
+int check_matrix(const void* p, int64_t ld, const lqsgd_rms_norm& a) {
   if (!p) return LQSGD_OK;
   if (ld < a.cols) return LQSGD_ERR_INVALID_ARG;
-  return train_aligned(p, es) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+  return train_aligned(p, train_elem(a.dtype)) ? LQSGD_OK : LQSGD_ERR_MISALIGNED;
+}
+// Whether its rows start on 16 bytes (an absent one does not stand in the way).
+bool on16(const void* p, int64_t ld, const lqsgd_rms_norm& a) {
+  return !p || (train_aligned(p, 16) && (a.rows == 1 || ld * train_elem(a.dtype) % 16 == 0));
+}
+bool on8(const void* p, int64_t ld, int64_t rows) { return !p || (train_aligned(p, 8) && (rows == 1 || ld % 8 == 0)); }
+int backward_access(const lqsgd_rms_norm& a) {
+  const bool rows = on16(a.dev_dy, a.ld_dy, a) && on16(a.dev_skip, a.ld_skip, a) && on16(a.dev_dx, a.ld_dx, a) && on16(a.dev_dresidual, a.ld_dresidual, a) &&
+                    (a.h8.dev_codes || on16(a.dev_h, a.ld_h, a));
+  return access_of(rows, train_aligned(a.dev_gamma, 16) && on8(a.h8.dev_codes, a.h8.ld_codes, a.rows), a.cols);
 }
 
 }  // namespace
@@ -470,7 +599,7 @@ extern "C" int lqsgd_rms_norm_workspace_bytes(int32_t backward, const lqsgd_rms_
   if (!host_bytes_out || (backward != 0 && backward != 1)) return LQSGD_ERR_INVALID_ARG;
   const int rc = check_args(a);
   if (rc != LQSGD_OK) return rc;
-  *host_bytes_out = backward && a->rows > 0 ? plan_backward(*a, true).bytes : 0;
+  *host_bytes_out = backward && a->rows > 0 ? plan_backward(*a, backward_access(*a)).bytes : 0;
   return LQSGD_OK;
 }
 
@@ -482,9 +611,10 @@ extern "C" int lqsgd_rms_norm_forward(const lqsgd_rms_norm* a, void* cuda_stream
   if (!a->dev_x || !a->dev_gamma || !a->dev_rstd) return LQSGD_ERR_INVALID_ARG;
   if (!a->dev_h && (a->dev_residual || a->drop.p > 0.f)) return LQSGD_ERR_INVALID_ARG;
   RmsArgs k = {};
-  if ((rc = check_matrix(a->dev_x, a->ld_x, *a, &k.vec_x)) != LQSGD_OK || (rc = check_matrix(a->dev_residual, a->ld_residual, *a, &k.vec_residual)) != LQSGD_OK ||
-      (rc = check_matrix(a->dev_h, a->ld_h, *a, &k.vec_h)) != LQSGD_OK || (rc = check_matrix(a->dev_y, a->ld_y, *a, &k.vec_y)) != LQSGD_OK)
+  if ((rc = check_matrix(a->dev_x, a->ld_x, *a)) != LQSGD_OK || (rc = check_matrix(a->dev_residual, a->ld_residual, *a)) != LQSGD_OK ||
+      (rc = check_matrix(a->dev_h, a->ld_h, *a)) != LQSGD_OK || (rc = check_matrix(a->dev_y, a->ld_y, *a)) != LQSGD_OK)
     return rc;
+  const bool rows16 = on16(a->dev_x, a->ld_x, *a) && on16(a->dev_residual, a->ld_residual, *a) && on16(a->dev_h, a->ld_h, *a) && on16(a->dev_y, a->ld_y, *a);
   if (a->h8.dev_codes && (rc = check_packed8(a->h8, a->cols)) != LQSGD_OK) return rc;
   if (a->y8.dev_codes && (rc = check_packed8(a->y8, a->cols)) != LQSGD_OK) return rc;
   if (a->rows8.dev_codes && (rc = check_rows8(a->rows8, a->cols)) != LQSGD_OK) return rc;
@@ -494,15 +624,16 @@ extern "C" int lqsgd_rms_norm_forward(const lqsgd_rms_norm* a, void* cuda_stream
   k.gamma = a->dev_gamma; k.rstd = a->dev_rstd;
   k.h8 = a->h8; k.y8 = a->y8; k.r8 = a->rows8;
   k.drop = make_drop(a->drop);
-  k.rows = a->rows; k.cols = a->cols; k.eps = a->eps;
+  k.rows = a->rows; k.cols = a->cols; k.per_col = (float)(1.0 / a->cols); k.eps = a->eps;
   k.vec_gamma = train_aligned(a->dev_gamma, 16);
-  k.vec_h8 = vec_rows(a->h8.dev_codes, a->h8.ld_codes, 1, 8);
-  k.vec_y8 = vec_rows(a->y8.dev_codes, a->y8.ld_codes, 1, 8);
-  k.vec_r8 = vec_rows(a->rows8.dev_codes, a->rows8.ld_codes, 1, 8);
-  const bool wide = a->cols > kMostForward, runs = (k.vec_x && k.vec_residual && k.vec_h && k.vec_y) || !whole_warps(a->cols);
-  const Shape s = wide ? Shape{} : shape_of(a->cols);
+  k.vec_h8 = on8(a->h8.dev_codes, a->h8.ld_codes, a->rows);
+  k.vec_y8 = on8(a->y8.dev_codes, a->y8.ld_codes, a->rows);
+  k.vec_r8 = on8(a->rows8.dev_codes, a->rows8.ld_codes, a->rows);
+  const int how = access_of(rows16, k.vec_gamma && k.vec_h8 && k.vec_y8 && k.vec_r8, a->cols);
+  const RowShape s = forward_shape(*a);
   k.lane_shift = s.lane_shift;
-  TRAIN_CK(BY_TYPE(a->dtype, runs, launch_forward, s, wide, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
+  k.ranks = (uint32_t)s.ranks;
+  TRAIN_CK(BY_TYPE(a->dtype, how, launch_forward, s, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
   return LQSGD_OK;
 }
 
@@ -519,15 +650,16 @@ extern "C" int lqsgd_rms_norm_backward(const lqsgd_rms_norm* a, void* cuda_strea
   const bool kept = a->h8.dev_codes != nullptr;
   if (!a->dev_dy || !a->dev_gamma || !a->dev_rstd || (!kept && !a->dev_h)) return LQSGD_ERR_INVALID_ARG;
   RmsArgs k = {};
-  if ((rc = check_matrix(a->dev_dy, a->ld_dy, *a, &k.vec_dy)) != LQSGD_OK || (rc = check_matrix(a->dev_skip, a->ld_skip, *a, &k.vec_skip)) != LQSGD_OK ||
-      (rc = check_matrix(a->dev_dx, a->ld_dx, *a, &k.vec_dx)) != LQSGD_OK ||
-      (rc = check_matrix(a->dev_dresidual, a->ld_dresidual, *a, &k.vec_dresidual)) != LQSGD_OK ||
-      (rc = check_matrix(kept ? nullptr : a->dev_h, a->ld_h, *a, &k.vec_h)) != LQSGD_OK)
+  if ((rc = check_matrix(a->dev_dy, a->ld_dy, *a)) != LQSGD_OK || (rc = check_matrix(a->dev_skip, a->ld_skip, *a)) != LQSGD_OK ||
+      (rc = check_matrix(a->dev_dx, a->ld_dx, *a)) != LQSGD_OK || (rc = check_matrix(a->dev_dresidual, a->ld_dresidual, *a)) != LQSGD_OK ||
+      (rc = check_matrix(kept ? nullptr : a->dev_h, a->ld_h, *a)) != LQSGD_OK)
     return rc;
   if (kept && (rc = check_packed8(a->h8, a->cols)) != LQSGD_OK) return rc;
   if (!train_aligned(a->dev_gamma, 4) || !train_aligned(a->dev_rstd, 4)) return LQSGD_ERR_MISALIGNED;
-  const bool runs = (k.vec_dy && k.vec_skip && k.vec_dx && k.vec_dresidual && k.vec_h) || !whole_warps(a->cols);
-  const GradPlan p = plan_backward(*a, runs);
+  k.vec_gamma = train_aligned(a->dev_gamma, 16);
+  k.vec_h8 = on8(a->h8.dev_codes, a->h8.ld_codes, a->rows);
+  const int how = backward_access(*a);
+  const GradPlan p = plan_backward(*a, how);
   if (p.bytes) {
     if (!a->dev_workspace || a->workspace_bytes < p.bytes) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
     if (!train_aligned(a->dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;
@@ -539,9 +671,7 @@ extern "C" int lqsgd_rms_norm_backward(const lqsgd_rms_norm* a, void* cuda_strea
   k.gamma = a->dev_gamma; k.rstd = a->dev_rstd;
   k.partial = !a->dev_dgamma ? nullptr : p.blocks > 1 ? reinterpret_cast<float*>(ws + p.off_partial) : a->dev_dgamma;
   k.drop = make_drop(a->drop);
-  k.rows = a->rows; k.cols = a->cols; k.lane_shift = p.shape.lane_shift;
-  k.vec_gamma = train_aligned(a->dev_gamma, 16);
-  k.vec_h8 = vec_rows(a->h8.dev_codes, a->h8.ld_codes, 1, 8);
-  TRAIN_CK(BY_TYPE(a->dtype, runs, launch_backward, p, k, reinterpret_cast<float*>(ws), st), "rms_backward_kernel launch");
+  k.rows = a->rows; k.cols = a->cols; k.per_col = (float)(1.0 / a->cols); k.lane_shift = p.shape.lane_shift; k.ranks = (uint32_t)p.shape.ranks;
+  TRAIN_CK(BY_TYPE(a->dtype, how, launch_backward, p, k, reinterpret_cast<float*>(ws), st), "rms_backward_kernel launch");
   return a->dev_dgamma && p.blocks > 1 ? join_columns(k.partial, p.blocks, a->cols, a->dev_dgamma, st) : LQSGD_OK;
 }

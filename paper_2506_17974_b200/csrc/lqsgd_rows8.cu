@@ -10,189 +10,218 @@ struct PackArgs {
   int64_t ld_x, rows;
   lqsgd_rows8 out;
   int32_t cols, lane_shift;
-  bool vec_x, vec_c;
+  uint32_t ranks;
+  bool vec_c;
 };
-__device__ __forceinline__ uint32_t largest(const float (&v)[kRun], uint32_t top) {
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  return top;
-}
-__device__ __forceinline__ void put_row_codes(const PackArgs& a, int64_t row, const Place& s, float inv, const float (&v)[kRun]) {
-  store_codes(reinterpret_cast<uint8_t*>(a.out.dev_codes) + row * a.out.ld_codes + s.col, a.vec_c && s.have == kRun, s.have,
-              make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
-}
+__device__ __forceinline__ uint8_t* codes_of(const lqsgd_rows8& r, int64_t row, int col) { return reinterpret_cast<uint8_t*>(r.dev_codes) + row * r.ld_codes + col; }
 
-template <int DT, int N, bool NARROW, bool RUNS>
-__global__ void __launch_bounds__(NARROW ? 256 : 512)
-pack_rows8_kernel(PackArgs a) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : NARROW ? 8 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[32];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<NARROW> team(a.lane_shift);
+template <int DT, int N, bool NARROW, int HOW>
+__global__ void __launch_bounds__(NARROW ? 256 : kBlockRuns / N)
+pack_rows8_kernel(const __grid_constant__ PackArgs a) {
+  using Rows = Team<NARROW, N>;
+  __shared__ typename Rows::Slots slots;
+  const Rows team(a.lane_shift, a.ranks);
   const int64_t row = team.row;
-  const bool on = !NARROW || row < a.rows;
+  const Lanes l = team.lanes(a.cols, !NARROW || row < a.rows);
+  const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
   train_pdl_wait();
-  Piece<DT> x[N];
+  Raw<DT, HOW> raw[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
+  Piece<DT> p[N];
+  float none = 0.f, top = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const Place s = team.place(i, a.cols);
-#pragma unroll
-    for (int k = 0; k < (int)(sizeof(x[i].w) / 4); ++k) x[i].w[k] = 0u;
-    if (on && (!RUNS || s.have > 0)) load_piece<DT, RUNS>(static_cast<const T*>(a.x) + row * a.ld_x, s, a.cols, a.vec_x && s.have == kRun, x[i]);
+    float v[kRun];
+    settle(raw[i], x, l, i, p[i]);
+    open_words<DT>(p[i], v);
+    top = largest(top, v);
   }
-  float v[N][kRun], none = 0.f;
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    open_piece<DT, RUNS>(x[i], turn, v[i]);
-    top = largest(v[i], top);
-  }
-  team.join(none, top, slots);
+  team.join(none, top, true, slots);
   float scale, inv;
-  row_scale(__uint_as_float(top), scale, inv);
-  if (!on) return;
-  if (team.t == 0) a.out.dev_scales[row] = scale;
+  row_scale(top, scale, inv);
+  if (team.first() && l.on) a.out.dev_scales[row] = scale;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const Place s = team.place(i, a.cols);
-    if (s.have > 0) put_row_codes(a, row, s, inv, v[i]);
+    float v[kRun];
+    open_words<DT>(p[i], v);
+    put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, i, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
   }
 }
 
-// Rows longer than a block holds: read twice.
-template <int DT, bool RUNS>
+// Rows longer than a cluster holds: read twice.
+template <int DT, int HOW>
 __global__ void __launch_bounds__(512)
-pack_rows8_long_kernel(PackArgs a) {
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : 16][RUNS ? 8 : 256];
-  __shared__ float2 slots[32];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
-  const Team<false> team(0);
+pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
+  using Rows = Team<false, 1>;
+  __shared__ typename Rows::Slots slots;
+  const Rows team(0, 1);
   const int64_t row = team.row;
   train_pdl_wait();
-  const int steps = team.steps(a.cols);
-  auto fetch = [&](const Place& s, float (&v)[kRun]) {
-    Piece<DT> x = {};
-    if (!RUNS || s.have > 0) load_piece<DT, RUNS>(static_cast<const T*>(a.x) + row * a.ld_x, s, a.cols, a.vec_x && s.have == kRun, x);
-    open_piece<DT, RUNS>(x, turn, v);
-  };
-  float none = 0.f;
-  uint32_t top = 0;
-  for (int i = 0; i < steps; ++i) {
-    float v[kRun];
-    fetch(team.place(i, a.cols), v);
-    top = largest(v, top);
-  }
-  team.join(none, top, slots);
-  float scale, inv;
-  row_scale(__uint_as_float(top), scale, inv);
-  if (team.t == 0) a.out.dev_scales[row] = scale;
-  for (int i = 0; i < steps; ++i) {
-    const Place s = team.place(i, a.cols);
-    float v[kRun];
-    fetch(s, v);
-    if (s.have > 0) put_row_codes(a, row, s, inv, v);
-  }
-}
-
-template <int DT, bool RUNS>
-__global__ void __launch_bounds__(kThreads)
-unpack_rows8_kernel(Deal d, lqsgd_rows8 in, bool vec_c, void* __restrict__ y, int64_t ld_y, bool vec_y) {
-  constexpr int kRows = 4;
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turn[RUNS ? 1 : kWarps][RUNS ? 8 : 256];
-  train_pdl_wait();
-  const Spot s(d);
-  if (RUNS && s.have <= 0) return;
-  const bool vy = vec_y && s.have == kRun, vc = vec_c && s.have == kRun;
-  for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
-    uint2 w[kRows];
-    float scale[kRows];
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
-      w[u] = make_uint2(0u, 0u);
-      if (s.have > 0) w[u] = load_codes(reinterpret_cast<const uint8_t*>(in.dev_codes) + r * in.ld_codes + s.col, vc, s.have);
-      scale[u] = in.dev_scales[r];
-    }
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = r0 + u * s.row_step;
-      if (r >= s.row_end) break;
+  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
+  float none = 0.f, top = 0.f, scale, inv = 0.f;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 2
+    for (int k = 0; k < steps; ++k) {
+      const Lanes l = team.lanes(a.cols, true, k);
+      const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
+      Raw<DT, HOW> raw;
+      Piece<DT> p;
       float v[kRun];
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] = (float)(int8_t)((j < 4 ? w[u].x : w[u].y) >> (8 * (j & 3))) * scale[u];
-      // past the type's range (for the source's own type: only by the scale's rounding): the largest finite value; a NaN stays
-      constexpr float kTop = DT == LQSGD_F16 ? 65504.f : (DT == LQSGD_BF16 ? 3.3895314e38f : 3.402823466e38f);
-      if (scale[u] > kTop / 128.5f) {
-#pragma unroll
-        for (int j = 0; j < kRun; ++j)
-          if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
-      }
-      store_piece<DT, RUNS>(static_cast<T*>(y) + r * ld_y, s, d.cols, vy, turn[RUNS ? 0 : threadIdx.x >> 5], v);
+      fetch(x, l, 0, raw);
+      settle(raw, x, l, 0, p);
+      open_words<DT>(p, v);
+      if (pass == 0) top = largest(top, v);
+      else put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, 0, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
+    }
+    if (pass == 0) {
+      team.join(none, top, true, slots);
+      row_scale(top, scale, inv);
+      if (team.first()) a.out.dev_scales[row] = scale;
     }
   }
 }
 
-template <int DT, bool RUNS>
+// ---- streams: a warp takes a strip of N runs per lane of one row, or, of rows of up to 128 columns, one run per lane of several rows
+struct Strips {
+  int64_t rows;
+  int32_t cols, lane_shift;
+  uint32_t per_row;                          // strips
+};
+template <int N>
+struct Strip {
+  Lanes l;
+  int64_t row;
+  __device__ __forceinline__ explicit Strip(const Strips& s) {
+    const uint32_t warp = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), me = threadIdx.x & 31;
+    l.lanes = 1 << s.lane_shift;
+    l.lane = me & (l.lanes - 1);
+    uint32_t in = 0;
+    if (s.lane_shift < 5) {
+      row = (int64_t)warp * (32 >> s.lane_shift) + (me >> s.lane_shift);
+    } else {
+      row = warp / s.per_row;
+      in = warp - (uint32_t)row * s.per_row;
+    }
+    l.col = (int)in * N * kWarpCols + l.lane * kRun;
+    l.left = s.cols - l.col;
+    l.on = row < s.rows;
+  }
+};
+
+template <int DT, int N, int HOW>
 __global__ void __launch_bounds__(kThreads)
-dropout_kernel(Deal d, const void* x, int64_t ld_x, bool vec_x, const void* residual, int64_t ld_r, bool vec_r, Drop drop,
-               void* out, int64_t ld_o, bool vec_o) {
-  constexpr int kRows = DT == LQSGD_F32 ? 1 : 2;
-  using T = typename Elem<DT>::T;
-  __shared__ __align__(16) T turns[RUNS ? 1 : kWarps][RUNS ? 8 : 256];
-  T* turn = turns[RUNS ? 0 : threadIdx.x >> 5];
+unpack_rows8_kernel(const __grid_constant__ Strips s, lqsgd_rows8 in, bool vec_c, void* y, int64_t ld_y) {
+  const Strip<N> w(s);
+  const Lanes& l = w.l;
   train_pdl_wait();
-  open_drop(drop);
-  const Spot s(d);
-  if (RUNS && s.have <= 0) return;
-  const bool vx = vec_x && s.have == kRun, vr = vec_r && s.have == kRun, vo = vec_o && s.have == kRun;
-  const uint64_t blocks = (uint64_t)((d.cols + kRun - 1) / kRun);
-  for (int64_t r0 = s.row; r0 < s.row_end; r0 += kRows * s.row_step) {
-    Piece<DT> px[kRows], pr[kRows];
+  uint2 c[N];
+  float scale = 0.f;
+  if (l.on) scale = in.dev_scales[w.row];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = min(r0 + u * s.row_step, s.row_end - 1);
-      load_piece<DT, RUNS>(static_cast<const T*>(x) + r * ld_x, s, d.cols, vx, px[u]);
-      if (residual) load_piece<DT, RUNS>(static_cast<const T*>(residual) + r * ld_r, s, d.cols, vr, pr[u]);
-    }
+  for (int i = 0; i < N; ++i) {
+    c[i] = make_uint2(0u, 0u);
+    if (l.on && l.have(i) > 0) c[i] = load_codes(codes_of(in, w.row, l.col) + i * kWarpCols, HOW == kWhole || (vec_c && l.have(i) >= kRun), min(l.have(i), kRun));
+  }
+  const Cursor<DT, HOW> out(y, w.row * ld_y, l);
+  Piece<DT> p[N];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int64_t r = r0 + u * s.row_step;
-      if (r >= s.row_end) break;
-      float v[kRun], add[kRun] = {};
-      open_piece<DT, RUNS>(px[u], turn, v);
-      if (residual) open_piece<DT, RUNS>(pr[u], turn, add);
-      drop_run(drop, (uint64_t)r * blocks + s.col / kRun, v, add);
-      store_piece<DT, RUNS>(static_cast<T*>(out) + r * ld_o, s, d.cols, vo, turn, v);
+  for (int i = 0; i < N; ++i) {
+    float v[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) v[j] = (float)(int8_t)((j < 4 ? c[i].x : c[i].y) >> (8 * (j & 3))) * scale;
+    // past the type's range (for the source's own type: only by the scale's rounding): the largest finite value; a NaN stays
+    constexpr float kTop = DT == LQSGD_F16 ? 65504.f : (DT == LQSGD_BF16 ? 3.3895314e38f : 3.402823466e38f);
+    if (scale > kTop / 128.5f) {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j)
+        if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
     }
+    close_words<DT>(v, p[i]);
+    put<DT, HOW, N>(out, l, i, p[i], p[i > 0 ? i - 1 : 0]);
   }
 }
 
-constexpr int kNarrow = 1024, kMostHeld = 512 * kRun * 8;
-template <int DT, bool RUNS>
-cudaError_t launch_pack(const PackArgs& a0, cudaStream_t st) {
-  PackArgs a = a0;
-  const int runs = (int)ceil_div64(a.cols, kRun);
-  if (a.cols > kMostHeld) return train_launch(pack_rows8_long_kernel<DT, RUNS>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
-#define GO(N, NARROW) train_launch(pack_rows8_kernel<DT, N, NARROW, RUNS>, grid, block, 0, st, 1, a)
-  int n = 1;
-  if (a.cols <= kNarrow) {
-    a.lane_shift = 2;
-    while (a.lane_shift < 5 && (1 << a.lane_shift) < runs) ++a.lane_shift;
-    while ((n << a.lane_shift) < runs) n *= 2;
-    const dim3 grid((unsigned)ceil_div64(a.rows, 256 >> a.lane_shift)), block(256);
-    return n == 1 ? GO(1, true) : n == 2 ? GO(2, true) : GO(4, true);
+template <int DT, int N, int HOW>
+__global__ void __launch_bounds__(kThreads)
+dropout_kernel(const __grid_constant__ Strips s, const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const __grid_constant__ Drop drop, void* out, int64_t ld_o) {
+  __shared__ uint32_t room[kDropRoom];
+  const Strip<N> w(s);
+  const Lanes& l = w.l;
+  const Cursor<DT, HOW> cx(x, w.row * ld_x, l), cr(residual, w.row * ld_r, l), co(out, w.row * ld_o, l);
+  train_pdl_wait();
+  open_drop(drop, room);
+  Raw<DT, HOW> rx[N], rr[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    fetch(cx, l, i, rx[i]);
+    if (residual) fetch(cr, l, i, rr[i]);
   }
-  while (n * 512 < runs) n *= 2;
-  const dim3 grid((unsigned)a.rows), block((unsigned)(ceil_div64(ceil_div64(runs, n), 32) * 32));
-  return n == 1 ? GO(1, false) : n == 2 ? GO(2, false) : n == 4 ? GO(4, false) : GO(8, false);
+  const uint64_t block = (uint64_t)w.row * (uint32_t)((s.cols + kRun - 1) / kRun) + l.col / kRun;
+  Piece<DT> p[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float v[kRun], add[kRun] = {};
+    if (residual) {
+      settle(rr[i], cr, l, i, p[i]);
+      open_words<DT>(p[i], add);
+    }
+    settle(rx[i], cx, l, i, p[i]);
+    open_words<DT>(p[i], v);
+    drop_run(drop, room, block + 32 * i, v, add);
+    close_words<DT>(v, p[i]);
+    put<DT, HOW, N>(co, l, i, p[i], p[i > 0 ? i - 1 : 0]);
+  }
+}
+
+template <int DT, int HOW>
+cudaError_t launch_pack(PackArgs a, cudaStream_t st) {
+  // 64 bytes per thread where rows fill the card, else one run
+  constexpr int kMany = DT == LQSGD_F32 ? 2 : 4;
+  const RowShape s = shape_of(a.cols, a.rows < 148 ? 1 : kMany, 1024);
+  if (!s.held) return train_launch(pack_rows8_long_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
+  a.lane_shift = s.lane_shift;
+  a.ranks = (uint32_t)s.ranks;
+  const dim3 grid((unsigned)(ceil_div64(a.rows, s.teams) * s.ranks)), block(s.threads);
+#define GO(N, NARROW) train_launch(pack_rows8_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, s.ranks, a)
+  if (s.narrow) return s.n == 1 ? GO(1, true) : s.n == 2 ? GO(2, true) : GO(4, true);
+  return s.n == 1 ? GO(1, false) : GO(kMany, false);
+#undef GO
+}
+// Strips of up to N runs per lane; false: more warps than a grid counts.
+Strips strips_of(int64_t rows, int32_t cols, int most, int* n, dim3* grid) {
+  Strips s = {rows, cols, 2, 1};
+  while (s.lane_shift < 5 && (kRun << s.lane_shift) < cols) ++s.lane_shift;
+  *n = 1;
+  while (*n < most && *n * kWarpCols < cols) *n *= 2;
+  s.per_row = (uint32_t)ceil_div64(cols, (int64_t)*n * kWarpCols);
+  const int64_t warps = s.lane_shift < 5 ? ceil_div64(rows, 32 >> s.lane_shift) : rows * s.per_row;
+  *grid = dim3((unsigned)ceil_div64(warps, kWarps));
+  return s;
+}
+template <int DT, int HOW>
+cudaError_t launch_unpack(int64_t rows, int32_t cols, cudaStream_t st, const lqsgd_rows8& in, bool vec_c, void* y, int64_t ld_y) {
+  int n;
+  dim3 grid;
+  const Strips s = strips_of(rows, cols, 4, &n, &grid);
+#define GO(N) train_launch(unpack_rows8_kernel<DT, N, HOW>, grid, dim3(kThreads), 0, st, 1, s, in, vec_c, y, ld_y)
+  return n == 1 ? GO(1) : n == 2 ? GO(2) : GO(4);
+#undef GO
+}
+template <int DT, int HOW>
+cudaError_t launch_dropout(int64_t rows, int32_t cols, cudaStream_t st, const void* x, int64_t ld_x, const void* r, int64_t ld_r, const Drop& drop, void* out, int64_t ld_o) {
+  int n;
+  dim3 grid;
+  const Strips s = strips_of(rows, cols, DT == LQSGD_F32 ? 2 : 4, &n, &grid);
+#define GO(N) train_launch(dropout_kernel<DT, N, HOW>, grid, dim3(kThreads), 0, st, 1, s, x, ld_x, r, ld_r, drop, out, ld_o)
+  if constexpr (DT == LQSGD_F32) return n == 1 ? GO(1) : GO(2);
+  else return n == 1 ? GO(1) : n == 2 ? GO(2) : GO(4);
 #undef GO
 }
 
 int check_shape(int64_t rows, int32_t cols) {
-  return rows < 0 || rows > 0x7fffffffll || cols < 1 || cols > (1 << 24) ? LQSGD_ERR_BAD_SHAPE : LQSGD_OK;
+  return rows < 0 || rows > (1 << 28) || cols < 1 || cols > (1 << 24) || rows * cols > (1ll << 40) ? LQSGD_ERR_BAD_SHAPE : LQSGD_OK;
 }
 
 }  // namespace
@@ -211,12 +240,8 @@ extern "C" int lqsgd_pack_rows8(const void* dev_x, int64_t ld_x, int32_t dtype, 
   const int es = train_elem(dtype);
   if (!train_aligned(dev_x, es)) return LQSGD_ERR_MISALIGNED;
   const bool vx = vec_rows(dev_x, ld_x, es, 16), vc = vec_rows(host_out->dev_codes, host_out->ld_codes, 1, 8);
-  const PackArgs a = {dev_x, ld_x, rows, *host_out, cols, 0, vx, vc};
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool runs = use_runs(vx, cols);
-  TRAIN_CK(dtype == LQSGD_BF16 ? (runs ? launch_pack<LQSGD_BF16, true>(a, st) : launch_pack<LQSGD_BF16, false>(a, st))
-           : dtype == LQSGD_F16 ? (runs ? launch_pack<LQSGD_F16, true>(a, st) : launch_pack<LQSGD_F16, false>(a, st))
-                                : (runs ? launch_pack<LQSGD_F32, true>(a, st) : launch_pack<LQSGD_F32, false>(a, st)), "pack_rows8_kernel launch");
+  const PackArgs a = {dev_x, ld_x, rows, *host_out, cols, 0, 1, vc};
+  TRAIN_CK(BY_TYPE(dtype, access_of(vx, vc, cols), launch_pack, a, static_cast<cudaStream_t>(cuda_stream)), "pack_rows8_kernel launch");
   return LQSGD_OK;
 }
 
@@ -231,10 +256,7 @@ extern "C" int lqsgd_unpack_rows8(const lqsgd_rows8* host_in, int64_t rows, int3
   const int es = train_elem(dtype);
   if (!train_aligned(dev_y, es)) return LQSGD_ERR_MISALIGNED;
   const bool vy = vec_rows(dev_y, ld_y, es, 16), vc = vec_rows(host_in->dev_codes, host_in->ld_codes, 1, 8);
-  const bool runs = use_runs(vy, cols);
-  dim3 grid;
-  const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
-  TRAIN_CK(BY_DTYPE(dtype, runs, unpack_rows8_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, *host_in, vc, dev_y, ld_y, vy), "unpack_rows8_kernel launch");
+  TRAIN_CK(BY_TYPE(dtype, access_of(vy, vc, cols), launch_unpack, rows, cols, static_cast<cudaStream_t>(cuda_stream), *host_in, vc, dev_y, ld_y), "unpack_rows8_kernel launch");
   return LQSGD_OK;
 }
 
@@ -248,10 +270,7 @@ extern "C" int lqsgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_re
   const int es = train_elem(dtype);
   if (!train_aligned(dev_x, es) || !train_aligned(dev_residual, es) || !train_aligned(dev_out, es)) return LQSGD_ERR_MISALIGNED;
   const bool vx = vec_rows(dev_x, ld_x, es, 16), vr = !dev_residual || vec_rows(dev_residual, ld_residual, es, 16), vo = vec_rows(dev_out, ld_out, es, 16);
-  const bool runs = use_runs(vx && vr && vo, cols);
-  dim3 grid;
-  const Deal d = make_deal(rows, cols, runs, kCtas, 1, &grid);
-  TRAIN_CK(BY_DTYPE(dtype, runs, dropout_kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), 1, d, dev_x, ld_x, vx, dev_residual,
-                    ld_residual, vr, make_drop(*host_drop), dev_out, ld_out, vo), "dropout_kernel launch");
+  TRAIN_CK(BY_TYPE(dtype, access_of(vx && vr && vo, true, cols), launch_dropout, rows, cols, static_cast<cudaStream_t>(cuda_stream), dev_x, ld_x, dev_residual,
+                   ld_residual, make_drop(*host_drop), dev_out, ld_out), "dropout_kernel launch");
   return LQSGD_OK;
 }

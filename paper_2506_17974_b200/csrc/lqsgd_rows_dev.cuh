@@ -5,54 +5,79 @@
 
 namespace lqsgd {
 
-// Dropout as the kernels take it: threshold T in the upper half of a word, 65536 / (65536 - T).
+// Dropout as the kernels take it: threshold T in the upper half of a word, 65536 / (65536 - T), the generator's keys of every round (a
+// third of its instructions would be adding them up; from the kernel's arguments they are operands).
 struct Drop {
-  uint64_t seed, offset;
-  const uint64_t* dev_seed;
+  uint64_t offset;
+  const uint64_t* dev_seed;                  // NULL: keys and offset are complete
   uint32_t threshold;                        // 0: nothing is dropped
   float scale;
+  uint32_t keys[20];
 };
 inline Drop make_drop(const lqsgd_drop& d) {
   const int t = std::min((int)rint(65536.0 * (double)d.p), 65535);
-  return {d.seed, d.offset, d.dev_seed, (uint32_t)t << 16, (float)(65536.0 / (65536 - t))};
+  Drop o = {d.offset, d.dev_seed, (uint32_t)t << 16, (float)(65536.0 / (65536 - t)), {}};
+  for (uint32_t r = 0; r < 10; ++r) {
+    o.keys[2 * r] = (uint32_t)d.seed + r * 0x9E3779B9u;
+    o.keys[2 * r + 1] = (uint32_t)(d.seed >> 32) + r * 0xBB67AE85u;
+  }
+  return o;
 }
 
 namespace {
 
-// Philox4x32, 10 rounds: a product of each even word by a constant, its high half mixed with a neighbour and the key, which grows by
-// a constant every round.
-__device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, uint64_t seed) {
+// How the rows of a call's matrices are read and written.
+//   kWhole  every row of every matrix starts on 16 bytes and is a whole number of runs (8-bit copies: on 8 bytes)
+//   kShift  any alignment.  A run is taken from the 16-byte pieces around it, which lie inside the row for all but its first and last
+//           runs, and moved into place in registers; it is written as the piece that begins in the run of the lane in front.  Element by
+//           element a run would touch as many places as it has elements; turned in shared memory, as the 8-bit streams do it, a
+//           row of 16-bit values still goes through 2-byte accesses.
+enum RowAccess { kWhole = 0, kShift = 1 };
+
+// Philox4x32, 10 rounds: a product of each even word by a constant, its high half mixed with a neighbour and the round's key.
+__device__ __forceinline__ uint4 philox(uint64_t block, uint64_t offset, const uint32_t* keys) {
   uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
-  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ keys[2 * r];
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ keys[2 * r + 1];
     c3 = (uint32_t)a;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
   return make_uint4(c0, c1, c2, c3);
 }
-// Seed and offset of this launch: read on the device where the caller keeps them there.
-__device__ __forceinline__ void open_drop(Drop& d) {
-  if (d.threshold && d.dev_seed) {
-    d.seed = d.dev_seed[0];
-    d.offset += d.dev_seed[1];
+// Where the caller keeps the seed on the device, a block makes the keys and the offset in shared memory.
+constexpr int kDropRoom = 22;
+__device__ __forceinline__ void open_drop(const Drop& d, uint32_t (&room)[kDropRoom]) {
+  if (!d.threshold || !d.dev_seed) return;                 // the same for all threads
+  if (threadIdx.x < 20) {
+    const uint64_t seed = d.dev_seed[0];
+    const uint32_t r = threadIdx.x >> 1;
+    room[threadIdx.x] = (threadIdx.x & 1) ? (uint32_t)(seed >> 32) + r * 0xBB67AE85u : (uint32_t)seed + r * 0x9E3779B9u;
+  } else if (threadIdx.x < kDropRoom) {
+    room[threadIdx.x] = (uint32_t)((d.offset + d.dev_seed[1]) >> (threadIdx.x == 20 ? 0 : 32));
   }
+  __syncthreads();
 }
 // v = r + dropout(v) for a run of 8 columns; block = row * ceil(cols / 8) + column / 8.  A half word's bits are compared in the upper half of
 // a word, where what lies below them does not count.  One rounding, the same in every kernel that drops.
-__device__ __forceinline__ void drop_run(const Drop& d, uint64_t block, float (&v)[kRun], const float (&r)[kRun]) {
-  const uint4 bits = philox(block, d.offset, d.seed);
+__device__ __forceinline__ void drop_run(const Drop& d, const uint32_t (&room)[kDropRoom], uint64_t block, float (&v)[kRun], const float (&r)[kRun]) {
+  const uint4 bits = d.dev_seed ? philox(block, (uint64_t)room[21] << 32 | room[20], room) : philox(block, d.offset, d.keys);
   const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     v[2 * j] = (w[j] << 16) >= d.threshold ? __fmaf_rn(v[2 * j], d.scale, r[2 * j]) : r[2 * j];
     v[2 * j + 1] = w[j] >= d.threshold ? __fmaf_rn(v[2 * j + 1], d.scale, r[2 * j + 1]) : r[2 * j + 1];
   }
+}
+
+// ---- largest magnitudes; an infinity or a NaN comes out as one
+__device__ __forceinline__ float larger(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float largest(float top, const float (&v)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(top) : "f"(top), "f"(v[j]), "f"(v[j + 1]));
+  return top;
 }
 
 // ---- rows of signed 8-bit codes
@@ -72,82 +97,316 @@ __device__ __forceinline__ uint32_t signed_word(const float* v, float inv) {
   const uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
   return inv == 0.f ? 0u : w;
 }
-// The 8-bit form of a run: four neighbouring lanes hold a group of 32.  The whole warp calls it; `store`: this lane's run is written.
-__device__ __forceinline__ void put_packed_run(const lqsgd_packed8& p, bool vec, int64_t row, const Place& s, bool store, const float (&v)[kRun]) {
-  uint32_t top = 0;
+// ---- a run as it is stored: of 16-bit types half the registers that its values take
+template <int DT>
+__device__ __forceinline__ void open_words(const Piece<DT>& in, float (&v)[kRun]) {
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  const int eb = exp_byte(__uint_as_float(top));
+  for (int j = 0; j < kRun / 2; ++j) {
+    if constexpr (DT == LQSGD_F32) {
+      v[2 * j] = __uint_as_float(in.w[2 * j]);
+      v[2 * j + 1] = __uint_as_float(in.w[2 * j + 1]);
+    } else {
+      const float2 f = open_pair<DT>(in.w[j]);
+      v[2 * j] = f.x;
+      v[2 * j + 1] = f.y;
+    }
+  }
+}
+template <int DT>
+__device__ __forceinline__ void close_words(const float (&v)[kRun], Piece<DT>& out) {
+#pragma unroll
+  for (int j = 0; j < kRun / 2; ++j) {
+    if constexpr (DT == LQSGD_F32) {
+      out.w[2 * j] = __float_as_uint(v[2 * j]);
+      out.w[2 * j + 1] = __float_as_uint(v[2 * j + 1]);
+    } else {
+      out.w[j] = pack_pair<DT>(v[2 * j], v[2 * j + 1]);
+    }
+  }
+}
+
+// ---- a thread's runs of a row
+// Up to N of them, kWarpCols apart, so that whatever a thread touches of a matrix's row is one address and constants; neighbouring lanes hold
+// neighbouring runs.  `left`: columns from the thread's first run to the row's end.
+constexpr int kWarpCols = 32 * kRun;
+template <int DT> constexpr int kRunBytes = kRun * (int)sizeof(typename Elem<DT>::T);
+struct Lanes {
+  int col, left;                             // the thread's first run
+  int lane, lanes;                           // this lane among those that hold neighbouring runs of the row
+  bool on;                                   // the row exists
+  __device__ __forceinline__ int have(int i) const { return left - i * kWarpCols; }
+};
+// Where a thread's first run of a matrix's row lies.  With kShift: the 16-byte piece that it begins in, how far into it, how many columns a
+// run must have in front of the row's end to be taken from whole pieces of the row (its first run in no case, if it is shifted).
+template <int DT, int HOW>
+struct Cursor {
+  char* p;
+  uint32_t shift;
+  int need;
+  bool head;
+  __device__ __forceinline__ Cursor(const void* matrix, int64_t at, const Lanes& l) {
+    constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
+    p = static_cast<char*>(const_cast<void*>(matrix)) + (at + l.col) * kSize;
+    shift = 0;
+    need = kRun;
+    head = false;
+    if (HOW == kShift) {
+      shift = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u;
+      p -= shift;
+      if (shift) {
+        need = kRun + (int)(16 - shift) / kSize;
+        head = l.col == 0;
+      }
+    }
+  }
+  __device__ __forceinline__ char* at(int i) const { return p + i * (32 * kRunBytes<DT>); }
+  __device__ __forceinline__ bool pieces(const Lanes& l, int i) const { return l.have(i) >= need && !(i == 0 && head); }
+};
+// A run as it is fetched: with kShift 16 bytes more.
+template <int DT, int HOW>
+struct Raw {
+  static constexpr int kPieces = kRunBytes<DT> / 16 + (HOW == kShift ? 1 : 0);
+  uint32_t w[4 * kPieces];
+};
+// Run i (zeros where nothing is).
+template <int DT, int HOW>
+__device__ __forceinline__ void fetch(const Cursor<DT, HOW>& c, const Lanes& l, int i, Raw<DT, HOW>& out) {
+  using T = typename Elem<DT>::T;
+  constexpr int kPieces = Raw<DT, HOW>::kPieces;
+#pragma unroll
+  for (int k = 0; k < 4 * kPieces; ++k) out.w[k] = 0u;
+  if (!l.on || l.have(i) <= 0) return;
+  if (HOW == kWhole || c.pieces(l, i)) {
+    const uint4* p = reinterpret_cast<const uint4*>(c.at(i));
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (k < kRunBytes<DT> / 16 || c.shift) reinterpret_cast<uint4*>(out.w)[k] = p[k];
+  } else {
+    const T* e = reinterpret_cast<const T*>(c.at(i) + c.shift);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j)
+      if (j < l.have(i)) reinterpret_cast<T*>(out.w)[j] = e[j];
+  }
+}
+// N words that begin `shift` bytes into in.
+template <int N, int M>
+__device__ __forceinline__ void shift_words(const uint32_t (&in)[M], uint32_t shift, bool halves, uint32_t (&out)[N]) {
+  static_assert(M >= N + 4, "room to shift");
+  uint32_t t[N + 3], u[N + 1];
+#pragma unroll
+  for (int k = 0; k < N + 3; ++k) t[k] = shift & 4 ? in[k + 1] : in[k];
+#pragma unroll
+  for (int k = 0; k < N + 1; ++k) u[k] = shift & 8 ? t[k + 2] : t[k];
+#pragma unroll
+  for (int k = 0; k < N; ++k) out[k] = halves ? __funnelshift_r(u[k], u[k + 1], (shift & 3) * 8) : u[k];
+}
+// What fetch brought as run i.
+template <int DT, int HOW>
+__device__ __forceinline__ void settle(const Raw<DT, HOW>& in, const Cursor<DT, HOW>& c, const Lanes& l, int i, Piece<DT>& out) {
+  if constexpr (HOW == kWhole) {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(out.w) / 4); ++k) out.w[k] = in.w[k];
+  } else {
+    shift_words(in.w, c.pieces(l, i) ? c.shift : 0u, DT != LQSGD_F32, out.w);
+  }
+}
+// Writes run i of N.  With kShift the whole warp calls it, with the run before, `prev`, in hand (i > 0).
+template <int DT, int HOW, int N>
+__device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, int i, const Piece<DT>& p, const Piece<DT>& prev) {
+  using T = typename Elem<DT>::T;
+  constexpr int kWords = kRunBytes<DT> / 4;
+  const int have = l.have(i);
+  if constexpr (HOW == kWhole) {
+    if (!l.on || have <= 0) return;
+    uint4* o = reinterpret_cast<uint4*>(c.at(i));
+#pragma unroll
+    for (int k = 0; k < kWords / 4; ++k) o[k] = reinterpret_cast<const uint4*>(p.w)[k];
+  } else {
+    uint32_t both[kWords + 4];                                // the end of the run in front, this one
+    const int me = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      both[k] = __shfl_sync(0xffffffffu, i > 0 && me == 31 ? prev.w[kWords - 4 + k] : p.w[kWords - 4 + k], (me + 31) & 31);
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) both[4 + k] = p.w[k];
+    if (!l.on || have <= 0) return;
+    const bool whole = have >= kRun && (l.lane > 0 || i > 0 || c.shift == 0), next = have >= 2 * kRun && (l.lane + 1 < l.lanes || i + 1 < N);
+    if (whole) {
+      uint32_t w[kWords];
+      // with shift 0 the run itself, 16 bytes in
+      if (c.shift) {
+        shift_words(both, 16 - c.shift, DT != LQSGD_F32, w);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = p.w[k];
+      }
+      uint4* o = reinterpret_cast<uint4*>(c.at(i));
+#pragma unroll
+      for (int k = 0; k < kWords / 4; ++k) o[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    }
+    if (!whole || (c.shift && !next)) {                       // what no piece holds: the ends of the row, of the warp's part of it
+      T* o = reinterpret_cast<T*>(c.at(i) + c.shift);
+      const int head = (kRunBytes<DT> - (int)c.shift) / (int)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j)
+        if (j < have && (j < head ? !whole : !next)) o[j] = reinterpret_cast<const T*>(p.w)[j];
+    }
+  }
+}
+// Run i of a vector of floats, from its element l.col on.
+template <int HOW>
+__device__ __forceinline__ void fetch_vector(const float* p, bool vec, const Lanes& l, int i, float (&v)[kRun]) {
+  const int have = l.have(i);
+  if (HOW == kWhole ? have > 0 : vec && have >= kRun) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p + i * kWarpCols)), b = __ldg(reinterpret_cast<const float4*>(p + i * kWarpCols) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) v[j] = HOW != kWhole && j < have ? __ldg(p + i * kWarpCols + j) : 0.f;
+  }
+}
+// Codes of run i at p, the row's from column l.col on.
+template <int HOW>
+__device__ __forceinline__ void put_codes(uint8_t* p, bool vec, const Lanes& l, int i, uint2 w) {
+  const int have = l.have(i);
+  if (!l.on || have <= 0) return;
+  if (HOW == kWhole || (vec && have >= kRun)) *reinterpret_cast<uint2*>(p + i * kWarpCols) = w;
+  else store_codes(p + i * kWarpCols, false, min(have, kRun), w);
+}
+// The 8-bit form of run i: four neighbouring lanes hold a group of 32.  codes and exps: the row's from column l.col on.  The whole warp calls it.
+template <int HOW>
+__device__ __forceinline__ void put_packed_run(uint8_t* codes, uint8_t* exps, bool vec, const Lanes& l, int i, const float (&v)[kRun]) {
+  float top = largest(0.f, v);
+  top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = larger(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const int eb = exp_byte(top);
   const float inv = inv_step(eb);
-  if (!store) return;
-  store_codes(p.dev_codes + row * p.ld_codes + s.col, vec && s.have == kRun, s.have,
-              make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
-  if ((s.col & (kGroup - 1)) == 0) p.dev_exps[row * p.ld_exps + s.col / kGroup] = (uint8_t)eb;
+  put_codes<HOW>(codes, vec, l, i, make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
+  if (l.on && l.have(i) > 0 && (l.lane & 3) == 0) exps[i * (kWarpCols / kGroup)] = (uint8_t)eb;
 }
 
 // ---- a row and its threads
-// NARROW: 4, 8, 16 or 32 lanes of a warp hold a row, a block of 256 threads several rows.  Otherwise a block holds one row.
-// A thread's i-th run of 8 columns is the (i * size + t)-th of the row.
-template <bool NARROW>
+// NARROW: 4, 8, 16 or 32 lanes of a warp hold a row, a block of 256 threads several rows.  Otherwise a block holds a row, or a cluster
+// of up to 8 blocks does.  A warp's columns lie side by side.  N runs per thread (one where fewer than 32 lanes hold a row).
+constexpr int kBlockRuns = 512, kMostRanks = 8;
+template <bool NARROW, int N>
 struct Team {
-  int t, size, warps;
-  int64_t row;
-  __device__ __forceinline__ explicit Team(int lane_shift) {
+  int warps, shift;
+  uint32_t rank, ranks;
+  int64_t row, rows_per_grid;
+  __device__ __forceinline__ Team(int lane_shift, uint32_t ranks_) : warps(blockDim.x >> 5), shift(NARROW ? lane_shift : 5), rank(0), ranks(1) {
     if (NARROW) {
-      size = 1 << lane_shift;
-      t = threadIdx.x & (size - 1);
-      warps = 1;
-      row = (int64_t)blockIdx.x * (blockDim.x >> lane_shift) + (threadIdx.x >> lane_shift);
+      const int each = (int)blockDim.x >> shift;
+      row = (int64_t)blockIdx.x * each + (threadIdx.x >> shift);
+      rows_per_grid = (int64_t)gridDim.x * each;
+    } else if (ranks_ > 1) {
+      ranks = ranks_;
+      asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+      row = blockIdx.x / ranks;
+      rows_per_grid = gridDim.x / ranks;
     } else {
-      size = blockDim.x;
-      t = threadIdx.x;
-      warps = blockDim.x >> 5;
       row = blockIdx.x;
+      rows_per_grid = gridDim.x;
     }
   }
-  __device__ __forceinline__ int rows_per_grid() const { return NARROW ? (int)gridDim.x * ((int)blockDim.x / size) : (int)gridDim.x; }
-  // runs per thread of a row
-  __device__ __forceinline__ int steps(int cols) const { return (cols + size * kRun - 1) / (size * kRun); }
-  __device__ __forceinline__ Place place(int i, int cols) const {
-    Place s;
-    s.col = (i * size + t) * kRun;
-    s.have = min(kRun, cols - s.col);
-    s.side = (i * size + (t & ~31)) * kRun + (threadIdx.x & 31);
-    return s;
+  // step: how many times over the team's columns the row was walked before (rows longer than the team)
+  __device__ __forceinline__ Lanes lanes(int cols, bool on, int step = 0) const {
+    Lanes l;
+    l.lanes = 1 << shift;
+    l.lane = threadIdx.x & (l.lanes - 1);
+    l.col = NARROW ? l.lane * kRun : (int)(((step * ranks + rank) * warps + (threadIdx.x >> 5)) * N * kWarpCols) + l.lane * kRun;
+    l.left = cols - l.col;
+    l.on = on;
+    return l;
   }
-  // Sum and largest of the team's values, in every thread of it.  `slots`: two warps' worth of shared memory (unused by NARROW);
-  // of two calls in a row the second takes other slots, or a barrier lies between them.
-  __device__ __forceinline__ void join(float& sum, uint32_t& top, float2* slots) const {
-    const int lanes = NARROW ? size : 32;
-    for (int o = 1; o < lanes; o <<= 1) {
-      sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  __device__ __forceinline__ bool first() const { return NARROW ? (threadIdx.x & ((1 << shift) - 1)) == 0 : threadIdx.x == 0 && rank == 0; }
+  // Sum and (where with_top) largest of the team's values, in every thread of it; all blocks of a cluster call it.  `slots`: shared memory
+  // (unused by NARROW); of two calls in a row the second takes other slots.
+  struct Slots { float2 warps[16], ranks[kMostRanks]; };
+  __device__ __forceinline__ void join(float& sum, float& top, bool with_top, Slots& slots) const {
+    if constexpr (NARROW) {
+      for (int o = 1; o < 1 << shift; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (with_top)
+        for (int o = 1; o < 1 << shift; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
+    } else {
+      join_blocks(sum, top, with_top, slots);
     }
-    if (!NARROW) {
-      const int lane = threadIdx.x & 31;
-      if (lane == 0) slots[threadIdx.x >> 5] = make_float2(sum, __uint_as_float(top));
+  }
+  __device__ __forceinline__ void join_blocks(float& sum, float& top, bool with_top, Slots& slots) const {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (with_top) {
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    if (warps > 1) {
+      if ((threadIdx.x & 31) == 0) slots.warps[threadIdx.x >> 5] = make_float2(sum, top);
       __syncthreads();
-      const float2 s = lane < warps ? slots[lane] : make_float2(0.f, 0.f);
-      sum = s.x;
-      top = __float_as_uint(s.y);
-      for (int o = 1; o < 32; o <<= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      sum = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < warps; ++w) {
+        const float2 s = slots.warps[w];
+        sum += s.x;
+        top = larger(top, s.y);
+      }
+    }
+    if (ranks > 1) {
+      if (threadIdx.x < ranks) {                             // this block's into every block's slot of it
+        uint32_t to;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&slots.ranks[rank])), "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(sum), "f"(top) : "memory");
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+      sum = 0.f;
+      for (uint32_t r = 0; r < ranks; ++r) {
+        const float2 s = slots.ranks[r];
+        sum += s.x;
+        top = larger(top, s.y);
       }
     }
   }
 };
-__device__ __forceinline__ void load_vector(const float* p, const Place& s, bool vec, float (&v)[kRun]) {
-  if (vec && s.have == kRun) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p + s.col)), b = __ldg(reinterpret_cast<const float4*>(p + s.col) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] = j < s.have ? __ldg(p + s.col + j) : 0.f;
+
+// ---- host side
+// How the matrices of a call are read and written: all rows start on 16 bytes, all 8-bit copies' rows on 8, vectors on 16.
+static inline int access_of(bool rows, bool others, int32_t cols) { return rows && others && cols % kRun == 0 ? kWhole : kShift; }
+
+// How rows are dealt out.  Up to `narrow` columns: 4 to 32 lanes each.  Longer: blocks of up to 4096 columns, n runs per thread, up to 8 of
+// them in a cluster.
+struct RowShape {
+  bool narrow, held;                         // held: a row fits into the registers of a team
+  int lane_shift, threads, n, ranks;
+  int64_t teams;                             // rows per block
+};
+static inline RowShape shape_of(int32_t cols, int n, int narrow) {
+  RowShape s = {};
+  const int64_t runs = ceil_div64(cols, kRun);
+  s.ranks = 1;
+  s.held = true;
+  s.teams = 1;
+  if (cols <= narrow) {
+    s.narrow = true;
+    s.lane_shift = 2;
+    s.n = 1;
+    while (s.lane_shift < 5 && (1 << s.lane_shift) < runs) ++s.lane_shift;
+    while ((s.n << s.lane_shift) < runs) s.n *= 2;
+    s.threads = 256;
+    s.teams = 256 >> s.lane_shift;
+    return s;
   }
+  s.n = n;
+  s.ranks = (int)std::min<int64_t>(ceil_div64(runs, kBlockRuns), kMostRanks + 1);
+  s.held = s.ranks <= kMostRanks;
+  s.threads = (int)ceil_div64(ceil_div64(ceil_div64(runs, s.ranks), n), 32) * 32;
+  return s;
 }
 
 }  // namespace
 }  // namespace lqsgd
+
+// f<type, access>(...) for a type and an access known at run time
+#define BY_ACCESS(DT, how, f, ...) ((how) == kWhole ? f<DT, kWhole>(__VA_ARGS__) : f<DT, kShift>(__VA_ARGS__))
+#define BY_TYPE(dtype, how, f, ...)                                  \
+  ((dtype) == LQSGD_BF16  ? BY_ACCESS(LQSGD_BF16, how, f, __VA_ARGS__) \
+   : (dtype) == LQSGD_F16 ? BY_ACCESS(LQSGD_F16, how, f, __VA_ARGS__)  \
+                          : BY_ACCESS(LQSGD_F32, how, f, __VA_ARGS__))
