@@ -22,11 +22,9 @@ struct RmsArgs {
   int64_t rows;
   int32_t cols, lane_shift;
   float eps, per_col;                        // 1 / cols
-  uint32_t ranks;                            // blocks that hold a row together
   bool vec_gamma, vec_h8, vec_y8, vec_r8;    // on 16 bytes; rows of 8-bit copies on 8
 };
-// Threads of a block: as many as hold 4096 columns, N runs of 8 each.
-template <int N, bool NARROW> struct RowBlock { static constexpr int kThreads = NARROW ? 256 : kBlockRuns / N; };
+constexpr int kForwardThreads = 256, kLongThreads = 256;
 
 // What a thread touches of one row of the forward call.
 template <int DT, int HOW>
@@ -45,35 +43,50 @@ struct ForwardRow {
     fetch(x, l, i, rx);
     if (a.residual) fetch(residual, l, i, rr);
   }
-  // h = residual + dropout(x), as it is stored, and its values
-  __device__ __forceinline__ void make_h(int i, const Raw<DT, HOW>& rx, const Raw<DT, HOW>& rr, Piece<DT>& ph, float (&v)[kRun]) const {
-    settle(rx, x, l, i, ph);
-    open_words<DT>(ph, v);
+  // h = residual + dropout(x) of all runs, as it is stored
+  template <int N>
+  __device__ __forceinline__ void make_h(const Raw<DT, HOW> (&rx)[N], const Raw<DT, HOW> (&rr)[N], Piece<DT> (&ph)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) settle(rx[i], x, l, i, ph[i]);
     if (!a.h) return;
-    float r[kRun] = {};
+    float v[kRun], r[kRun];
+    if (a.drop.threshold) {
+      uint4 bits[N];
+      drop_bits<N>(a.drop, room, block, bits);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        sum_of(i, rr[i], r);
+        open_words<DT>(ph[i], v);
+        drop_run(a.drop, bits[i], v, r);
+        close_words<DT>(r, ph[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        sum_of(i, rr[i], r);
+        open_words<DT>(ph[i], v);
+        add_run(r, r, v);
+        close_words<DT>(r, ph[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ void sum_of(int i, const Raw<DT, HOW>& rr, float (&r)[kRun]) const {
+    clear_run(r);
     if (a.residual) {
       Piece<DT> t;
       settle(rr, residual, l, i, t);
       open_words<DT>(t, r);
     }
-    if (a.drop.threshold) {
-      drop_run(a.drop, room, block + 32 * i, v, r);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] += r[j];
-    }
-    close_words<DT>(v, ph);
-    open_words<DT>(ph, v);
   }
   // squares into `sum`, the largest |h gamma| into `top`
-  __device__ __forceinline__ void add_squares(int i, const float (&v)[kRun], float& sum, float& top) const {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) sum = fmaf(v[j], v[j], sum);
+  __device__ __forceinline__ void add_squares(int i, const Piece<DT>& ph, float (&sum)[2], float& top) const {
+    float v[kRun];
+    open_words<DT>(ph, v);
+    dot_run(sum, v, v);
     if (a.r8.dev_codes) {
       float g[kRun];
       fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) g[j] *= v[j];
+      mul_run(g, g, v);
       top = largest(top, g);
     }
   }
@@ -94,10 +107,9 @@ struct ForwardRow {
     open_words<DT>(ph, v);
     fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
     if (a.h8.dev_codes) put_packed_run<HOW>(a.h8.dev_codes + row * a.h8.ld_codes + l.col, a.h8.dev_exps + row * a.h8.ld_exps + l.col / kGroup, a.vec_h8, l, i, v);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) v[j] = v[j] * rstd * g[j];
-    if (a.r8.dev_codes)
-      put_codes<HOW>(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + l.col, a.vec_r8, l, i, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
+    mul_run(v, v, rstd);
+    mul_run(v, v, g);
+    if (a.r8.dev_codes) put_codes<HOW>(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + l.col, a.vec_r8, l, i, signed_codes(v, inv));
     if (!a.y && !a.y8.dev_codes) return;
     Piece<DT> p;
     close_words<DT>(v, p);
@@ -111,12 +123,11 @@ struct ForwardRow {
 };
 
 template <int DT, int N, bool NARROW, int HOW>
-__global__ void __launch_bounds__(RowBlock<N, NARROW>::kThreads)
+__global__ void __launch_bounds__(NARROW ? 256 : kForwardThreads)
 rms_forward_kernel(const __grid_constant__ RmsArgs a) {
-  using Rows = Team<NARROW, N>;
-  __shared__ typename Rows::Slots slots;
+  __shared__ float2 slots[16];
   __shared__ uint32_t room[kDropRoom];
-  const Rows team(a.lane_shift, a.ranks);
+  const Team<NARROW, N> team(a.lane_shift);
   const ForwardRow<DT, HOW> io(a, room, team.row, team.lanes(a.cols, !NARROW || team.row < a.rows));
   train_pdl_wait();
   open_drop(a.drop, room);
@@ -124,62 +135,68 @@ rms_forward_kernel(const __grid_constant__ RmsArgs a) {
 #pragma unroll
   for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
   Piece<DT> h[N], y;
-  float sum = 0.f, top = 0.f, rstd, inv = 0.f;
+  float sum[2] = {0.f, 0.f}, top = 0.f, rstd, inv = 0.f;
+  io.make_h(x, res, h);
+  if (a.h) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float v[kRun];
-    io.make_h(i, x[i], res[i], h[i], v);
-    if (a.h) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
-    io.add_squares(i, v, sum, top);
+    for (int i = 0; i < N; ++i) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
   }
-  team.join(sum, top, a.r8.dev_codes != nullptr, slots);
-  io.figures(team.first(), sum, top, rstd, inv);
+#pragma unroll
+  for (int i = 0; i < N; ++i) io.add_squares(i, h[i], sum, top);
+  sum[0] += sum[1];
+  team.join(sum[0], top, a.r8.dev_codes != nullptr, slots);
+  io.figures(team.first(), sum[0], top, rstd, inv);
 #pragma unroll
   for (int i = 0; i < N; ++i) io.template put_y<N>(i, rstd, inv, h[i], y);
 }
 
-// Rows longer than a cluster holds: h is computed (and stored) in a first pass and computed again in a second.
-template <int DT, int HOW>
-__global__ void __launch_bounds__(512)
+// Rows longer than a block holds: h is computed (and stored) in a first pass and computed again, from L2, in a second.
+template <int DT, int N, int HOW>
+__global__ void __launch_bounds__(kLongThreads)
 rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
-  using Rows = Team<false, 1>;
-  __shared__ typename Rows::Slots slots;
+  __shared__ float2 slots[16];
   __shared__ uint32_t room[kDropRoom];
-  const Rows team(0, 1);
+  const Team<false, N> team(0);
   train_pdl_wait();
   open_drop(a.drop, room);
-  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
-  float sum = 0.f, top = 0.f, rstd = 0.f, inv = 0.f;
+  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
+  float sum[2] = {0.f, 0.f}, top = 0.f, rstd = 0.f, inv = 0.f;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
     for (int k = 0; k < steps; ++k) {
       const ForwardRow<DT, HOW> io(a, room, team.row, team.lanes(a.cols, true, k));
-      Raw<DT, HOW> x, res;
-      Piece<DT> h, y;
-      float v[kRun];
-      io.ask(0, x, res);
-      io.make_h(0, x, res, h, v);
-      if (pass == 0) {
-        if (a.h) put<DT, HOW, 1>(io.h, io.l, 0, h, h);
-        io.add_squares(0, v, sum, top);
-      } else {
-        io.template put_y<1>(0, rstd, inv, h, y);
+      Raw<DT, HOW> x[N], res[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
+      Piece<DT> h[N], y;
+      io.make_h(x, res, h);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (pass == 0) {
+          if (a.h) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
+          io.add_squares(i, h[i], sum, top);
+        } else {
+          io.template put_y<N>(i, rstd, inv, h[i], y);
+        }
       }
     }
     if (pass == 0) {
-      team.join(sum, top, a.r8.dev_codes != nullptr, slots);
-      ForwardRow<DT, HOW>(a, room, team.row, team.lanes(a.cols, true)).figures(team.first(), sum, top, rstd, inv);
+      sum[0] += sum[1];
+      team.join(sum[0], top, a.r8.dev_codes != nullptr, slots);
+      ForwardRow<DT, HOW>(a, room, team.row, team.lanes(a.cols, true)).figures(team.first(), sum[0], top, rstd, inv);
     }
   }
 }
 
 // ---- backward
 // With h as it comes (xh = h rstd), a row needs <u xh> = rstd <dy h gamma>, and then d = gamma rstd dy - (rstd^2 <u xh>) h + skip.
-// A block (or cluster) keeps its columns' sums for dgamma in registers and walks rows.  What it reads goes through shared memory, a row
+// A block keeps its columns' sums for dgamma in registers and walks rows.  What it reads goes through shared memory, a row
 // ahead (cp.async), every thread its own runs: registers have no room for rows in flight, and a row's values are read a second time behind the
 // sum.  h from its 8-bit form is decoded once, to bf16, in which it is exact.
 constexpr int kStages = 2;
+template <int DT> constexpr int kGradRuns = DT == LQSGD_F32 ? 1 : 2;
+template <int DT, bool NARROW> constexpr int kGradThreads = NARROW || DT != LQSGD_F32 ? 256 : 384;
 // Eight codes as bf16: |128 + m| with the magnitude m below is a bf16 number (0x4300 | m), and (128 + m) 2^e - 128 2^e is m 2^e exactly; the
 // signs are put on top.  For exponents from kQuickByte on 128 2^e leaves the range.
 __device__ __forceinline__ void decode_bf16(uint2 c, uint32_t eb, uint32_t (&w)[4]) {
@@ -246,34 +263,45 @@ struct BackwardRow {
     settle(raw, c, l, i, p);
     open_words<DT>(p, v);
   }
-  // d of run i of N into dx and dresidual; as stored in px and pr, of the run before when they come
+  // d of all runs into dx and dresidual
   template <int N>
-  __device__ __forceinline__ void put_d(int i, float (&d)[kRun], Piece<DT>& px, Piece<DT>& pr) const {
-    Piece<DT> out;
+  __device__ __forceinline__ void put_d(float (&d)[N][kRun]) const {
+    Piece<DT> out[N];
+    if (a.dresidual || !a.drop.threshold) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) close_words<DT>(d[i], out[i]);
+    }
     if (a.dresidual) {
-      close_words<DT>(d, out);
-      put<DT, HOW, N>(Cursor<DT, HOW>(a.dresidual, row * a.ld_dresidual, l), l, i, out, pr);
-      pr = out;
+      const Cursor<DT, HOW> c(a.dresidual, row * a.ld_dresidual, l);
+#pragma unroll
+      for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, l, i, out[i], out[i > 0 ? i - 1 : 0]);
     }
-    if (a.dx) {
-      const float none[kRun] = {};
-      if (a.drop.threshold) drop_run(a.drop, room, (uint64_t)row * (uint32_t)((a.cols + kRun - 1) / kRun) + l.col / kRun + 32 * i, d, none);
-      close_words<DT>(d, out);
-      put<DT, HOW, N>(Cursor<DT, HOW>(a.dx, row * a.ld_dx, l), l, i, out, px);
-      px = out;
+    if (!a.dx) return;
+    if (a.drop.threshold) {
+      uint4 bits[N];
+      drop_bits<N>(a.drop, room, (uint64_t)row * (uint32_t)((a.cols + kRun - 1) / kRun) + l.col / kRun, bits);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float t[kRun];
+        clear_run(t);
+        drop_run(a.drop, bits[i], d[i], t);
+        close_words<DT>(t, out[i]);
+      }
     }
+    const Cursor<DT, HOW> c(a.dx, row * a.ld_dx, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, l, i, out[i], out[i > 0 ? i - 1 : 0]);
   }
 };
 
 template <int DT, int N, bool NARROW, int HOW>
-__global__ void __launch_bounds__(RowBlock<N, NARROW>::kThreads, 512 / RowBlock<N, NARROW>::kThreads)
+__global__ void __launch_bounds__(kGradThreads<DT, NARROW>, 768 / kGradThreads<DT, NARROW>)
 rms_backward_kernel(const __grid_constant__ RmsArgs a) {
-  using Rows = Team<NARROW, N>;
   using Row = BackwardRow<DT, HOW>;
   extern __shared__ __align__(16) uint8_t grad_smem[];
-  __shared__ typename Rows::Slots slots[2];
+  __shared__ float2 slots[2][16];
   __shared__ uint32_t room[kDropRoom];
-  const Rows team(a.lane_shift, a.ranks);
+  const Team<NARROW, N> team(a.lane_shift);
   train_pdl_wait();
   open_drop(a.drop, room);
   // [stage][run][dy pieces, skip pieces, h pieces or 8 bytes of codes][thread]
@@ -283,9 +311,7 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
   uint8_t* const mine8 = grad_smem + off_h + threadIdx.x * 8;
   float acc[N][kRun];
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) acc[i][j] = 0.f;
+  for (int i = 0; i < N; ++i) clear_run(acc[i]);
   uint32_t exps[N], exps_next[N];
   float rstd, rstd_next;
   auto ask = [&](int64_t row, uint32_t at) {
@@ -297,7 +323,7 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
       rstd_next = a.rstd[row];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (r.l.have(i) <= 0) continue;
+        if (!r.l.has(i)) continue;
         uint8_t* to = mine + at + i * run_bytes;
         r.ask(r.dy, i, to, unit);
         if (a.skip) r.ask(r.skip, i, to + off_skip, unit);
@@ -315,6 +341,10 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  // Places of runs that no row has hold zeros, so that the work on them needs no branch.  (Those of a row that does not exist keep what an
+  // earlier row left: it counts with rstd = 0 and is not written.)
+  for (uint32_t i = threadIdx.x; i < kStages * stage_bytes / 16; i += blockDim.x) reinterpret_cast<uint4*>(grad_smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+  __syncthreads();
   // NARROW: a warp stays together while one of its rows exists
   const int64_t first = NARROW ? team.row - ((threadIdx.x & 31) >> team.shift) : team.row;
   ask(team.row, 0);
@@ -330,11 +360,10 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     const Row r(a, room, row, team.lanes(a.cols, row < a.rows));
     const float* gamma = a.gamma + r.l.col;
-    float sum = 0.f, top = 0.f;
+    float sum[2] = {0.f, 0.f}, top = 0.f;
     uint32_t h8[N][4];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (!r.l.on || r.l.have(i) <= 0) continue;
       const uint8_t* from = mine + at + i * run_bytes;
       float u[kRun], v[kRun], g[kRun];
       if (a.h8.dev_codes) {
@@ -345,39 +374,36 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
       }
       r.take(r.dy, i, from, unit, u);
       fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) {
-        const float t = u[j] * v[j];
-        acc[i][j] = fmaf(t, rstd, acc[i][j]);
-        sum = fmaf(t, g[j], sum);
-      }
+      mul_run(u, u, v);
+      fma_run(acc[i], u, rstd, acc[i]);
+      dot_run(sum, u, g);
     }
-    team.join(sum, top, false, slots[turn]);
+    sum[0] += sum[1];
+    team.join(sum[0], top, false, slots[turn]);
     turn ^= 1;
-    const float k = rstd * rstd * (rstd * (sum * a.per_col));
-    Piece<DT> px, pr;
+    const float k = rstd * rstd * (rstd * (sum[0] * a.per_col));
+    float d[N][kRun];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float d[kRun] = {}, v[kRun], g[kRun];
-      if (r.l.on && r.l.have(i) > 0) {
-        const uint8_t* from = mine + at + i * run_bytes;
-        if (a.skip) r.take(r.skip, i, from + off_skip, unit, d);
-        if (a.h8.dev_codes) open_bf16(h8[i], v);
-        else r.take(r.h, i, from + off_h, unit, v);
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) d[j] = fmaf(-k, v[j], d[j]);
-        r.take(r.dy, i, from, unit, v);
-        fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) d[j] = fmaf(g[j] * rstd, v[j], d[j]);
-      }
-      r.template put_d<N>(i, d, px, pr);
+      float v[kRun], g[kRun];
+      const uint8_t* from = mine + at + i * run_bytes;
+      if (a.skip) r.take(r.skip, i, from + off_skip, unit, d[i]);
+      else clear_run(d[i]);
+      if (a.h8.dev_codes) open_bf16(h8[i], v);
+      else r.take(r.h, i, from + off_h, unit, v);
+      fma_run(d[i], v, -k, d[i]);
+      r.take(r.dy, i, from, unit, v);
+      fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
+      mul_run(g, g, rstd);
+      fma_run(d[i], g, v, d[i]);
     }
+    r.template put_d<N>(d);
     at ^= stage_bytes;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   if (!a.partial) return;
-  float* out = a.partial + (size_t)(blockIdx.x / team.ranks) * a.cols;
+  train_pdl_trigger();
+  float* out = a.partial + (size_t)blockIdx.x * a.cols;
   float* sums = reinterpret_cast<float*>(grad_smem);
   const Lanes l = team.lanes(a.cols, true);
 #pragma unroll
@@ -402,7 +428,7 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
   }
 }
 
-// Rows longer than a cluster holds: <dy h gamma> of each in a first kernel, the rest as a stream over columns.
+// Rows longer than a block holds: <dy h gamma> of each in a first kernel, the rest as a stream over columns.
 template <int DT, int HOW>
 __device__ __forceinline__ void load_dy_h(const BackwardRow<DT, HOW>& r, float (&dy)[kRun], float (&h)[kRun]) {
   Raw<DT, HOW> raw;
@@ -415,35 +441,33 @@ __device__ __forceinline__ void load_dy_h(const BackwardRow<DT, HOW>& r, float (
     settle(raw, r.h, r.l, 0, p);
     open_words<DT>(p, h);
   } else {
-    uint2 codes = make_uint2(0u, 0u);
-    int exp = kExpBias;
-    if (r.l.have(0) > 0) {
-      codes = load_codes(r.codes(), r.codes_whole(0), min(r.l.have(0), kRun));
-      exp = r.a.h8.dev_exps[r.row * r.a.h8.ld_exps + r.l.col / kGroup];
-    }
-    decode_run(codes, exp, h);
+    uint32_t w[4];
+    decode_bf16(load_codes(r.codes(), r.codes_whole(0), min(r.l.have(0), kRun)), r.a.h8.dev_exps[r.row * r.a.h8.ld_exps + r.l.col / kGroup], w);
+    open_bf16(w, h);
   }
 }
 template <int DT, int HOW>
 __global__ void __launch_bounds__(512)
 rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
-  using Rows = Team<false, 1>;
-  __shared__ typename Rows::Slots slots;
+  __shared__ float2 slots[16];
   __shared__ uint32_t room[kDropRoom];
-  const Rows team(0, 1);
+  const Team<false, 1> team(0);
   train_pdl_wait();
-  float sum = 0.f, top = 0.f;
+  float sum[2] = {0.f, 0.f}, top = 0.f;
   const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
+#pragma unroll 2
   for (int k = 0; k < steps; ++k) {
     const BackwardRow<DT, HOW> r(a, room, team.row, team.lanes(a.cols, true, k));
     float dy[kRun], h[kRun], g[kRun];
+    if (!r.l.has(0)) continue;
     load_dy_h(r, dy, h);
     fetch_vector<HOW>(a.gamma + r.l.col, a.vec_gamma, r.l, 0, g);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) sum = fmaf(dy[j] * h[j], g[j], sum);
+    mul_run(dy, dy, h);
+    dot_run(sum, dy, g);
   }
-  team.join(sum, top, false, slots);
-  if (team.first()) dots[team.row] = sum * a.per_col;
+  sum[0] += sum[1];
+  team.join(sum[0], top, false, slots);
+  if (team.first()) dots[team.row] = sum[0] * a.per_col;
 }
 template <int DT, int HOW>
 __global__ void __launch_bounds__(kThreads)
@@ -459,23 +483,26 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, const __grid_constant__ De
   fetch_vector<HOW>(a.gamma + l.col, a.vec_gamma, l, 0, g);
   for (int64_t row = s.row; row < s.row_end; row += s.row_step) {
     const BackwardRow<DT, HOW> r(a, room, row, l);
-    float dy[kRun], h[kRun], e[kRun] = {};
-    load_dy_h(r, dy, h);
-    const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
-    if (a.skip) {
-      Raw<DT, HOW> raw;
-      Piece<DT> t;
-      fetch(r.skip, l, 0, raw);
-      settle(raw, r.skip, l, 0, t);
-      open_words<DT>(t, e);
+    float dy[kRun], h[kRun], d1[1][kRun];
+    float (&e)[kRun] = d1[0];
+    if (l.has(0)) {
+      load_dy_h(r, dy, h);
+      const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
+      clear_run(e);
+      if (a.skip) {
+        Raw<DT, HOW> raw;
+        Piece<DT> t;
+        fetch(r.skip, l, 0, raw);
+        settle(raw, r.skip, l, 0, t);
+        open_words<DT>(t, e);
+      }
+      fma_run(e, h, -k, e);
+      mul_run(h, h, dy);
+      fma_run(acc, h, rstd, acc);
+      mul_run(dy, dy, rstd);
+      fma_run(e, dy, g, e);
     }
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-      acc[j] = fmaf(dy[j] * h[j], rstd, acc[j]);
-      e[j] = fmaf(g[j] * rstd, dy[j], fmaf(-k, h[j], e[j]));
-    }
-    Piece<DT> px, pr;
-    r.template put_d<1>(0, e, px, pr);
+    r.template put_d<1>(d1);
   }
   if (!a.partial) return;
   // the rows that the block's warps have of one column: warps side by side hold other columns
@@ -494,15 +521,13 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, const __grid_constant__ De
 
 // ---- choice of kernel
 constexpr int kSms = 148;
-// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type) where rows fill the card; with few rows one run per thread, whose
-// latency is the row's.
+// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type).
 constexpr int kNarrow = 1024;
 template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
 RowShape forward_shape(const lqsgd_rms_norm& a) {
-  return shape_of(a.cols, a.rows < kSms ? 1 : a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow);
+  return shape_of(a.cols, a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow, kForwardThreads);
 }
 constexpr int kCtasColumns = kSms * 6;
-template <int DT> constexpr int kGradRuns = DT == LQSGD_F32 ? 2 : 4;
 struct GradPlan {
   RowShape shape;
   Deal deal;
@@ -513,20 +538,21 @@ struct GradPlan {
 GradPlan plan_backward(const lqsgd_rms_norm& a, int how) {
   GradPlan p = {};
   const bool wide = a.dtype == LQSGD_F32;
-  p.shape = shape_of(a.cols, wide ? kGradRuns<LQSGD_F32> : kGradRuns<LQSGD_BF16>, wide ? 256 : 512);
+  p.shape = shape_of(a.cols, wide ? kGradRuns<LQSGD_F32> : kGradRuns<LQSGD_BF16>, wide ? 256 : 512, wide ? kGradThreads<LQSGD_F32, false> : kGradThreads<LQSGD_BF16, false>);
+  const int pieces = kRun * train_elem(a.dtype) / 16 + (how == kShift ? 1 : 0);
+  const bool kept = a.h8.dev_codes != nullptr;
+  const size_t run = (size_t)16 * pieces * (1 + (a.dev_skip ? 1 : 0) + (kept ? 0 : 1)) + (kept ? 8 : 0);
+  p.smem = std::max(run * kStages * p.shape.n * p.shape.threads, p.shape.narrow ? sizeof(float) * 256 * (kRun + 1) : 0);
+  p.shape.held = p.shape.held && p.smem <= 224 * 1024;
   if (!p.shape.held) {
     p.deal = make_deal(a.rows, a.cols, true, kCtasColumns, 8, &p.grid);
     p.blocks = (int)p.grid.y;
     p.off_partial = (size_t)ceil_div64(a.rows * 4, 256) * 256;
   } else {
-    const int pieces = kRun * train_elem(a.dtype) / 16 + (how == kShift ? 1 : 0);
-    const bool kept = a.h8.dev_codes != nullptr;
-    const size_t run = (size_t)16 * pieces * (1 + (a.dev_skip ? 1 : 0) + (kept ? 0 : 1)) + (kept ? 8 : 0);
-    p.smem = std::max(run * kStages * p.shape.n * p.shape.threads, p.shape.narrow ? sizeof(float) * 256 * (kRun + 1) : 0);
-    // 512 threads an SM have registers, as many blocks shared memory (1.5 KB of it are not for rows)
-    const int64_t per_sm = std::max<int64_t>(1, std::min<int64_t>(512 / p.shape.threads, 226 * 1024 / (p.smem + 1536)));
-    p.blocks = (int)std::min<int64_t>(ceil_div64(a.rows, p.shape.teams), std::max<int64_t>(1, kSms * per_sm / p.shape.ranks));
-    p.grid = dim3((unsigned)(p.blocks * p.shape.ranks));
+    // 768 threads an SM have registers, as many blocks shared memory (1.5 KB of it are not for rows)
+    const int64_t per_sm = std::max<int64_t>(1, std::min<int64_t>(768 / p.shape.threads, 226 * 1024 / (p.smem + 1536)));
+    p.blocks = (int)std::min<int64_t>(ceil_div64(a.rows, p.shape.teams), kSms * per_sm);
+    p.grid = dim3((unsigned)p.blocks);
   }
   p.bytes = p.off_partial + (a.dev_dgamma && p.blocks > 1 ? (size_t)p.blocks * a.cols * 4 : 0);
   return p;
@@ -534,11 +560,11 @@ GradPlan plan_backward(const lqsgd_rms_norm& a, int how) {
 
 template <int DT, int HOW>
 cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st) {
-  if (!s.held) return train_launch(rms_forward_long_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
-  const dim3 grid((unsigned)(ceil_div64(a.rows, s.teams) * s.ranks)), block(s.threads);
-#define GO(N, NARROW) train_launch(rms_forward_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, s.ranks, a)
+  if (!s.held) return train_launch(rms_forward_long_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a);
+  const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
+#define GO(N, NARROW) train_launch(rms_forward_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, 1, a)
   if (s.narrow) return s.n == 1 ? GO(1, true) : s.n == 2 ? GO(2, true) : GO(4, true);
-  return s.n == 1 ? GO(1, false) : GO(kForwardRuns<DT>, false);
+  return GO(kForwardRuns<DT>, false);
 #undef GO
 }
 template <int DT, int N, bool NARROW, int HOW>
@@ -552,7 +578,7 @@ cudaError_t launch_held(const GradPlan& p, const RmsArgs& a, cudaStream_t st) {
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024)) != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
-  return train_launch(kernel, p.grid, dim3(p.shape.threads), p.smem, st, p.shape.ranks, a);
+  return train_launch(kernel, p.grid, dim3(p.shape.threads), p.smem, st, 1, a);
 }
 template <int DT, int HOW>
 cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
@@ -632,7 +658,6 @@ extern "C" int lqsgd_rms_norm_forward(const lqsgd_rms_norm* a, void* cuda_stream
   const int how = access_of(rows16, k.vec_gamma && k.vec_h8 && k.vec_y8 && k.vec_r8, a->cols);
   const RowShape s = forward_shape(*a);
   k.lane_shift = s.lane_shift;
-  k.ranks = (uint32_t)s.ranks;
   TRAIN_CK(BY_TYPE(a->dtype, how, launch_forward, s, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
   return LQSGD_OK;
 }
@@ -671,7 +696,7 @@ extern "C" int lqsgd_rms_norm_backward(const lqsgd_rms_norm* a, void* cuda_strea
   k.gamma = a->dev_gamma; k.rstd = a->dev_rstd;
   k.partial = !a->dev_dgamma ? nullptr : p.blocks > 1 ? reinterpret_cast<float*>(ws + p.off_partial) : a->dev_dgamma;
   k.drop = make_drop(a->drop);
-  k.rows = a->rows; k.cols = a->cols; k.per_col = (float)(1.0 / a->cols); k.lane_shift = p.shape.lane_shift; k.ranks = (uint32_t)p.shape.ranks;
+  k.rows = a->rows; k.cols = a->cols; k.per_col = (float)(1.0 / a->cols); k.lane_shift = p.shape.lane_shift;
   TRAIN_CK(BY_TYPE(a->dtype, how, launch_backward, p, k, reinterpret_cast<float*>(ws), st), "rms_backward_kernel launch");
   return a->dev_dgamma && p.blocks > 1 ? join_columns(k.partial, p.blocks, a->cols, a->dev_dgamma, st) : LQSGD_OK;
 }

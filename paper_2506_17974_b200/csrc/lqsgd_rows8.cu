@@ -10,17 +10,16 @@ struct PackArgs {
   int64_t ld_x, rows;
   lqsgd_rows8 out;
   int32_t cols, lane_shift;
-  uint32_t ranks;
   bool vec_c;
 };
 __device__ __forceinline__ uint8_t* codes_of(const lqsgd_rows8& r, int64_t row, int col) { return reinterpret_cast<uint8_t*>(r.dev_codes) + row * r.ld_codes + col; }
 
+constexpr int kPackThreads = 512, kLongThreads = 256;
 template <int DT, int N, bool NARROW, int HOW>
-__global__ void __launch_bounds__(NARROW ? 256 : kBlockRuns / N)
+__global__ void __launch_bounds__(NARROW ? 256 : kPackThreads, NARROW || HOW == kShift ? 1 : 3)
 pack_rows8_kernel(const __grid_constant__ PackArgs a) {
-  using Rows = Team<NARROW, N>;
-  __shared__ typename Rows::Slots slots;
-  const Rows team(a.lane_shift, a.ranks);
+  __shared__ float2 slots[16];
+  const Team<NARROW, N> team(a.lane_shift);
   const int64_t row = team.row;
   const Lanes l = team.lanes(a.cols, !NARROW || row < a.rows);
   const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
@@ -45,35 +44,38 @@ pack_rows8_kernel(const __grid_constant__ PackArgs a) {
   for (int i = 0; i < N; ++i) {
     float v[kRun];
     open_words<DT>(p[i], v);
-    put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, i, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
+    put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, i, signed_codes(v, inv));
   }
 }
 
-// Rows longer than a cluster holds: read twice.
-template <int DT, int HOW>
-__global__ void __launch_bounds__(512)
+// Rows longer than a block holds: read twice, the second time from L2.
+template <int DT, int N, int HOW>
+__global__ void __launch_bounds__(kLongThreads)
 pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
-  using Rows = Team<false, 1>;
-  __shared__ typename Rows::Slots slots;
-  const Rows team(0, 1);
+  __shared__ float2 slots[16];
+  const Team<false, N> team(0);
   const int64_t row = team.row;
   train_pdl_wait();
-  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
+  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
   float none = 0.f, top = 0.f, scale, inv = 0.f;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 2
+#pragma unroll 1
     for (int k = 0; k < steps; ++k) {
       const Lanes l = team.lanes(a.cols, true, k);
       const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
-      Raw<DT, HOW> raw;
-      Piece<DT> p;
-      float v[kRun];
-      fetch(x, l, 0, raw);
-      settle(raw, x, l, 0, p);
-      open_words<DT>(p, v);
-      if (pass == 0) top = largest(top, v);
-      else put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, 0, make_uint2(signed_word(v, inv), signed_word(v + 4, inv)));
+      Raw<DT, HOW> raw[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        Piece<DT> p;
+        float v[kRun];
+        settle(raw[i], x, l, i, p);
+        open_words<DT>(p, v);
+        if (pass == 0) top = largest(top, v);
+        else put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, i, signed_codes(v, inv));
+      }
     }
     if (pass == 0) {
       team.join(none, top, true, slots);
@@ -160,36 +162,38 @@ dropout_kernel(const __grid_constant__ Strips s, const void* x, int64_t ld_x, co
   }
   const uint64_t block = (uint64_t)w.row * (uint32_t)((s.cols + kRun - 1) / kRun) + l.col / kRun;
   Piece<DT> p[N];
+  uint4 bits[N];
+  drop_bits<N>(drop, room, block, bits);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    float v[kRun], add[kRun] = {};
+    float v[kRun], sum[kRun];
     if (residual) {
       settle(rr[i], cr, l, i, p[i]);
-      open_words<DT>(p[i], add);
+      open_words<DT>(p[i], sum);
+    } else {
+      clear_run(sum);
     }
     settle(rx[i], cx, l, i, p[i]);
     open_words<DT>(p[i], v);
-    drop_run(drop, room, block + 32 * i, v, add);
-    close_words<DT>(v, p[i]);
+    drop_run(drop, bits[i], v, sum);
+    close_words<DT>(sum, p[i]);
     put<DT, HOW, N>(co, l, i, p[i], p[i > 0 ? i - 1 : 0]);
   }
 }
 
 template <int DT, int HOW>
 cudaError_t launch_pack(PackArgs a, cudaStream_t st) {
-  // 64 bytes per thread where rows fill the card, else one run
-  constexpr int kMany = DT == LQSGD_F32 ? 2 : 4;
-  const RowShape s = shape_of(a.cols, a.rows < 148 ? 1 : kMany, 1024);
-  if (!s.held) return train_launch(pack_rows8_long_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a);
+  constexpr int kRuns = DT == LQSGD_F32 ? 2 : 4;              // 64 bytes per thread
+  const RowShape s = shape_of(a.cols, kRuns, 1024, kPackThreads);
+  if (!s.held) return train_launch(pack_rows8_long_kernel<DT, kRuns, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a);
   a.lane_shift = s.lane_shift;
-  a.ranks = (uint32_t)s.ranks;
-  const dim3 grid((unsigned)(ceil_div64(a.rows, s.teams) * s.ranks)), block(s.threads);
-#define GO(N, NARROW) train_launch(pack_rows8_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, s.ranks, a)
+  const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
+#define GO(N, NARROW) train_launch(pack_rows8_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, 1, a)
   if (s.narrow) return s.n == 1 ? GO(1, true) : s.n == 2 ? GO(2, true) : GO(4, true);
-  return s.n == 1 ? GO(1, false) : GO(kMany, false);
+  return GO(kRuns, false);
 #undef GO
 }
-// Strips of up to N runs per lane; false: more warps than a grid counts.
+// Strips of up to `most` runs per lane.
 Strips strips_of(int64_t rows, int32_t cols, int most, int* n, dim3* grid) {
   Strips s = {rows, cols, 2, 1};
   while (s.lane_shift < 5 && (kRun << s.lane_shift) < cols) ++s.lane_shift;
@@ -240,7 +244,7 @@ extern "C" int lqsgd_pack_rows8(const void* dev_x, int64_t ld_x, int32_t dtype, 
   const int es = train_elem(dtype);
   if (!train_aligned(dev_x, es)) return LQSGD_ERR_MISALIGNED;
   const bool vx = vec_rows(dev_x, ld_x, es, 16), vc = vec_rows(host_out->dev_codes, host_out->ld_codes, 1, 8);
-  const PackArgs a = {dev_x, ld_x, rows, *host_out, cols, 0, 1, vc};
+  const PackArgs a = {dev_x, ld_x, rows, *host_out, cols, 0, vc};
   TRAIN_CK(BY_TYPE(dtype, access_of(vx, vc, cols), launch_pack, a, static_cast<cudaStream_t>(cuda_stream)), "pack_rows8_kernel launch");
   return LQSGD_OK;
 }

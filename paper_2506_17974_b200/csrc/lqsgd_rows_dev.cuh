@@ -60,16 +60,71 @@ __device__ __forceinline__ void open_drop(const Drop& d, uint32_t (&room)[kDropR
   }
   __syncthreads();
 }
-// v = r + dropout(v) for a run of 8 columns; block = row * ceil(cols / 8) + column / 8.  A half word's bits are compared in the upper half of
-// a word, where what lies below them does not count.  One rounding, the same in every kernel that drops.
-__device__ __forceinline__ void drop_run(const Drop& d, const uint32_t (&room)[kDropRoom], uint64_t block, float (&v)[kRun], const float (&r)[kRun]) {
-  const uint4 bits = d.dev_seed ? philox(block, (uint64_t)room[21] << 32 | room[20], room) : philox(block, d.offset, d.keys);
+// Random bits of a thread's N runs (32 blocks apart); block = row * ceil(cols / 8) + column / 8 of the first.  All at once: the rounds of one
+// run depend on one another, those of several fill the gaps.
+template <int N>
+__device__ __forceinline__ void drop_bits(const Drop& d, const uint32_t (&room)[kDropRoom], uint64_t block, uint4 (&bits)[N]) {
+  if (d.dev_seed) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) bits[i] = philox(block + 32 * i, (uint64_t)room[21] << 32 | room[20], room);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) bits[i] = philox(block + 32 * i, d.offset, d.keys);
+  }
+}
+// r += dropout(v) for a run.  A half word's bits are compared in the upper half of a word, where what lies below them does not count.  One
+// rounding, the same in every kernel that drops.
+__device__ __forceinline__ void drop_run(const Drop& d, const uint4& bits, const float (&v)[kRun], float (&r)[kRun]) {
   const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[2 * j] = (w[j] << 16) >= d.threshold ? __fmaf_rn(v[2 * j], d.scale, r[2 * j]) : r[2 * j];
-    v[2 * j + 1] = w[j] >= d.threshold ? __fmaf_rn(v[2 * j + 1], d.scale, r[2 * j + 1]) : r[2 * j + 1];
+    if ((w[j] << 16) >= d.threshold) r[2 * j] = __fmaf_rn(v[2 * j], d.scale, r[2 * j]);
+    if (w[j] >= d.threshold) r[2 * j + 1] = __fmaf_rn(v[2 * j + 1], d.scale, r[2 * j + 1]);
   }
+}
+
+// ---- arithmetic on two values at a time (one instruction for both; each rounded by itself)
+__device__ __forceinline__ void fma2(float& a0, float& a1, float b0, float b1, float c0, float c1, float d0, float d1) {
+  asm("{\n .reg .b64 b, c, d;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mov.b64 d, {%6, %7};\n fma.rn.f32x2 d, b, c, d;\n mov.b64 {%0, %1}, d;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1), "f"(d0), "f"(d1));
+}
+__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
+  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mul.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
+  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n add.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+// a = b c + d and the like, of a run
+__device__ __forceinline__ void fma_run(float (&a)[kRun], const float (&b)[kRun], const float (&c)[kRun], const float (&d)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) fma2(a[j], a[j + 1], b[j], b[j + 1], c[j], c[j + 1], d[j], d[j + 1]);
+}
+__device__ __forceinline__ void fma_run(float (&a)[kRun], const float (&b)[kRun], float c, const float (&d)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) fma2(a[j], a[j + 1], b[j], b[j + 1], c, c, d[j], d[j + 1]);
+}
+__device__ __forceinline__ void mul_run(float (&a)[kRun], const float (&b)[kRun], const float (&c)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) mul2(a[j], a[j + 1], b[j], b[j + 1], c[j], c[j + 1]);
+}
+__device__ __forceinline__ void mul_run(float (&a)[kRun], const float (&b)[kRun], float c) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) mul2(a[j], a[j + 1], b[j], b[j + 1], c, c);
+}
+__device__ __forceinline__ void add_run(float (&a)[kRun], const float (&b)[kRun], const float (&c)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) add2(a[j], a[j + 1], b[j], b[j + 1], c[j], c[j + 1]);
+}
+__device__ __forceinline__ void clear_run(float (&a)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) a[j] = 0.f;
+}
+// sum += the run's products, even and odd columns apart
+__device__ __forceinline__ void dot_run(float (&sum)[2], const float (&b)[kRun], const float (&c)[kRun]) {
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) fma2(sum[0], sum[1], b[j], b[j + 1], c[j], c[j + 1], sum[0], sum[1]);
 }
 
 // ---- largest magnitudes; an infinity or a NaN comes out as one
@@ -88,15 +143,22 @@ __device__ __forceinline__ void row_scale(float top, float& scale, float& inv) {
   scale = finite ? fmaxf(__fdiv_rn(top, 127.f), kRowStepLow) : __uint_as_float(0x7fc00000u);
   inv = finite ? fminf(__fdiv_rn(127.f, top), kRowInvHigh) : 0.f;
 }
-// Four codes rint(v inv) in a word: adding 1.5 * 2^23 to the rounded product leaves an integer in two's complement below.  v inv is rounded by
-// itself, as the definition has it (no fused multiply-add).
-__device__ __forceinline__ uint32_t signed_word(const float* v, float inv) {
-  uint32_t b[4];
+// Eight codes rint(v inv): adding 1.5 * 2^23 to the rounded product leaves an integer in two's complement below.  v inv is rounded by
+// itself, as the definition has it (one at a time: of two at a time, product and sum come out fused).
+__device__ __forceinline__ uint2 signed_codes(const float (&v)[kRun], float inv) {
+  float t[kRun];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[j], inv), 12582912.f));
-  const uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-  return inv == 0.f ? 0u : w;
+  for (int j = 0; j < kRun; ++j) t[j] = __fmul_rn(v[j], inv);
+#pragma unroll
+  for (int j = 0; j < kRun; j += 2) add2(t[j], t[j + 1], t[j], t[j + 1], 12582912.f, 12582912.f);
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    w[k] = __byte_perm(__byte_perm(__float_as_uint(t[4 * k]), __float_as_uint(t[4 * k + 1]), 0x0040),
+                       __byte_perm(__float_as_uint(t[4 * k + 2]), __float_as_uint(t[4 * k + 3]), 0x0040), 0x5410);
+  return inv == 0.f ? make_uint2(0u, 0u) : make_uint2(w[0], w[1]);
 }
+
 // ---- a run as it is stored: of 16-bit types half the registers that its values take
 template <int DT>
 __device__ __forceinline__ void open_words(const Piece<DT>& in, float (&v)[kRun]) {
@@ -135,6 +197,7 @@ struct Lanes {
   int lane, lanes;                           // this lane among those that hold neighbouring runs of the row
   bool on;                                   // the row exists
   __device__ __forceinline__ int have(int i) const { return left - i * kWarpCols; }
+  __device__ __forceinline__ bool has(int i) const { return on && have(i) > 0; }
 };
 // Where a thread's first run of a matrix's row lies.  With kShift: the 16-byte piece that it begins in, how far into it, how many columns a
 // run must have in front of the row's end to be taken from whole pieces of the row (its first run in no case, if it is shifted).
@@ -168,14 +231,14 @@ struct Raw {
   static constexpr int kPieces = kRunBytes<DT> / 16 + (HOW == kShift ? 1 : 0);
   uint32_t w[4 * kPieces];
 };
-// Run i (zeros where nothing is).
+// Run i, zeros where there is none: what follows then needs no branch, and the work on a thread's runs interleaves.
 template <int DT, int HOW>
 __device__ __forceinline__ void fetch(const Cursor<DT, HOW>& c, const Lanes& l, int i, Raw<DT, HOW>& out) {
   using T = typename Elem<DT>::T;
   constexpr int kPieces = Raw<DT, HOW>::kPieces;
 #pragma unroll
   for (int k = 0; k < 4 * kPieces; ++k) out.w[k] = 0u;
-  if (!l.on || l.have(i) <= 0) return;
+  if (!l.has(i)) return;
   if (HOW == kWhole || c.pieces(l, i)) {
     const uint4* p = reinterpret_cast<const uint4*>(c.at(i));
 #pragma unroll
@@ -217,7 +280,7 @@ __device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, in
   constexpr int kWords = kRunBytes<DT> / 4;
   const int have = l.have(i);
   if constexpr (HOW == kWhole) {
-    if (!l.on || have <= 0) return;
+    if (!l.has(i)) return;
     uint4* o = reinterpret_cast<uint4*>(c.at(i));
 #pragma unroll
     for (int k = 0; k < kWords / 4; ++k) o[k] = reinterpret_cast<const uint4*>(p.w)[k];
@@ -229,7 +292,7 @@ __device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, in
       both[k] = __shfl_sync(0xffffffffu, i > 0 && me == 31 ? prev.w[kWords - 4 + k] : p.w[kWords - 4 + k], (me + 31) & 31);
 #pragma unroll
     for (int k = 0; k < kWords; ++k) both[4 + k] = p.w[k];
-    if (!l.on || have <= 0) return;
+    if (!l.has(i)) return;
     const bool whole = have >= kRun && (l.lane > 0 || i > 0 || c.shift == 0), next = have >= 2 * kRun && (l.lane + 1 < l.lanes || i + 1 < N);
     if (whole) {
       uint32_t w[kWords];
@@ -269,11 +332,12 @@ __device__ __forceinline__ void fetch_vector(const float* p, bool vec, const Lan
 template <int HOW>
 __device__ __forceinline__ void put_codes(uint8_t* p, bool vec, const Lanes& l, int i, uint2 w) {
   const int have = l.have(i);
-  if (!l.on || have <= 0) return;
+  if (!l.has(i)) return;
   if (HOW == kWhole || (vec && have >= kRun)) *reinterpret_cast<uint2*>(p + i * kWarpCols) = w;
   else store_codes(p + i * kWarpCols, false, min(have, kRun), w);
 }
-// The 8-bit form of run i: four neighbouring lanes hold a group of 32.  codes and exps: the row's from column l.col on.  The whole warp calls it.
+// The 8-bit form of run i: four neighbouring lanes hold a group of 32.  codes and exps: the row's from column l.col on.  The whole warp calls
+// it, with zeros in lanes that have no run.
 template <int HOW>
 __device__ __forceinline__ void put_packed_run(uint8_t* codes, uint8_t* exps, bool vec, const Lanes& l, int i, const float (&v)[kRun]) {
   float top = largest(0.f, v);
@@ -282,86 +346,56 @@ __device__ __forceinline__ void put_packed_run(uint8_t* codes, uint8_t* exps, bo
   const int eb = exp_byte(top);
   const float inv = inv_step(eb);
   put_codes<HOW>(codes, vec, l, i, make_uint2(code_word(v[0], v[1], v[2], v[3], inv), code_word(v[4], v[5], v[6], v[7], inv)));
-  if (l.on && l.have(i) > 0 && (l.lane & 3) == 0) exps[i * (kWarpCols / kGroup)] = (uint8_t)eb;
+  if (l.has(i) && (l.lane & 3) == 0) exps[i * (kWarpCols / kGroup)] = (uint8_t)eb;
 }
 
 // ---- a row and its threads
-// NARROW: 4, 8, 16 or 32 lanes of a warp hold a row, a block of 256 threads several rows.  Otherwise a block holds a row, or a cluster
-// of up to 8 blocks does.  A warp's columns lie side by side.  N runs per thread (one where fewer than 32 lanes hold a row).
-constexpr int kBlockRuns = 512, kMostRanks = 8;
+// NARROW: 4, 8, 16 or 32 lanes of a warp hold a row, a block of 256 threads several rows.  Otherwise a block holds one.  A warp's columns lie
+// side by side.  N runs per thread (one where fewer than 32 lanes hold a row).
 template <bool NARROW, int N>
 struct Team {
   int warps, shift;
-  uint32_t rank, ranks;
   int64_t row, rows_per_grid;
-  __device__ __forceinline__ Team(int lane_shift, uint32_t ranks_) : warps(blockDim.x >> 5), shift(NARROW ? lane_shift : 5), rank(0), ranks(1) {
-    if (NARROW) {
-      const int each = (int)blockDim.x >> shift;
-      row = (int64_t)blockIdx.x * each + (threadIdx.x >> shift);
-      rows_per_grid = (int64_t)gridDim.x * each;
-    } else if (ranks_ > 1) {
-      ranks = ranks_;
-      asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-      row = blockIdx.x / ranks;
-      rows_per_grid = gridDim.x / ranks;
-    } else {
-      row = blockIdx.x;
-      rows_per_grid = gridDim.x;
-    }
+  __device__ __forceinline__ explicit Team(int lane_shift) : warps(blockDim.x >> 5), shift(NARROW ? lane_shift : 5) {
+    const int each = NARROW ? (int)blockDim.x >> shift : 1;
+    row = NARROW ? (int64_t)blockIdx.x * each + (threadIdx.x >> shift) : blockIdx.x;
+    rows_per_grid = (int64_t)gridDim.x * each;
   }
   // step: how many times over the team's columns the row was walked before (rows longer than the team)
   __device__ __forceinline__ Lanes lanes(int cols, bool on, int step = 0) const {
     Lanes l;
     l.lanes = 1 << shift;
     l.lane = threadIdx.x & (l.lanes - 1);
-    l.col = NARROW ? l.lane * kRun : (int)(((step * ranks + rank) * warps + (threadIdx.x >> 5)) * N * kWarpCols) + l.lane * kRun;
+    l.col = NARROW ? l.lane * kRun : (step * warps + (int)(threadIdx.x >> 5)) * N * kWarpCols + l.lane * kRun;
     l.left = cols - l.col;
     l.on = on;
     return l;
   }
-  __device__ __forceinline__ bool first() const { return NARROW ? (threadIdx.x & ((1 << shift) - 1)) == 0 : threadIdx.x == 0 && rank == 0; }
-  // Sum and (where with_top) largest of the team's values, in every thread of it; all blocks of a cluster call it.  `slots`: shared memory
-  // (unused by NARROW); of two calls in a row the second takes other slots.
-  struct Slots { float2 warps[16], ranks[kMostRanks]; };
-  __device__ __forceinline__ void join(float& sum, float& top, bool with_top, Slots& slots) const {
+  __device__ __forceinline__ bool first() const { return (threadIdx.x & (NARROW ? (1 << shift) - 1 : 0xffff)) == 0; }
+  // Sum and (where with_top) largest of the team's values, in every thread of it.  `slots`: shared memory (unused by NARROW); of two
+  // calls in a row the second takes other slots.
+  __device__ __forceinline__ void join(float& sum, float& top, bool with_top, float2 (&slots)[16]) const {
     if constexpr (NARROW) {
       for (int o = 1; o < 1 << shift; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       if (with_top)
         for (int o = 1; o < 1 << shift; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
     } else {
-      join_blocks(sum, top, with_top, slots);
-    }
-  }
-  __device__ __forceinline__ void join_blocks(float& sum, float& top, bool with_top, Slots& slots) const {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (with_top) {
+      for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (with_top) {
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
-    }
-    if (warps > 1) {
-      if ((threadIdx.x & 31) == 0) slots.warps[threadIdx.x >> 5] = make_float2(sum, top);
-      __syncthreads();
-      sum = 0.f;
+        for (int o = 1; o < 32; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
+      }
+      if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = make_float2(sum, top);
+        __syncthreads();
+        sum = 0.f;
 #pragma unroll 4
-      for (int w = 0; w < warps; ++w) {
-        const float2 s = slots.warps[w];
-        sum += s.x;
-        top = larger(top, s.y);
-      }
-    }
-    if (ranks > 1) {
-      if (threadIdx.x < ranks) {                             // this block's into every block's slot of it
-        uint32_t to;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&slots.ranks[rank])), "r"(threadIdx.x));
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(sum), "f"(top) : "memory");
-      }
-      asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-      sum = 0.f;
-      for (uint32_t r = 0; r < ranks; ++r) {
-        const float2 s = slots.ranks[r];
-        sum += s.x;
-        top = larger(top, s.y);
+        for (int w = 0; w < warps; ++w) {
+          const float2 s = slots[w];
+          sum += s.x;
+          top = larger(top, s.y);
+        }
       }
     }
   }
@@ -371,21 +405,19 @@ struct Team {
 // How the matrices of a call are read and written: all rows start on 16 bytes, all 8-bit copies' rows on 8, vectors on 16.
 static inline int access_of(bool rows, bool others, int32_t cols) { return rows && others && cols % kRun == 0 ? kWhole : kShift; }
 
-// How rows are dealt out.  Up to `narrow` columns: 4 to 32 lanes each.  Longer: blocks of up to 4096 columns, n runs per thread, up to 8 of
-// them in a cluster.
+// How rows are dealt out.  Up to `narrow` columns: 4 to 32 lanes each.  Longer: a block each, n runs per thread, if `threads` threads hold them;
+// else not held, and walked in several steps.
 struct RowShape {
-  bool narrow, held;                         // held: a row fits into the registers of a team
-  int lane_shift, threads, n, ranks;
+  bool narrow, held;
+  int lane_shift, threads, n;
   int64_t teams;                             // rows per block
 };
-static inline RowShape shape_of(int32_t cols, int n, int narrow) {
+static inline RowShape shape_of(int32_t cols, int n, int narrow, int threads) {
   RowShape s = {};
   const int64_t runs = ceil_div64(cols, kRun);
-  s.ranks = 1;
-  s.held = true;
   s.teams = 1;
   if (cols <= narrow) {
-    s.narrow = true;
+    s.narrow = s.held = true;
     s.lane_shift = 2;
     s.n = 1;
     while (s.lane_shift < 5 && (1 << s.lane_shift) < runs) ++s.lane_shift;
@@ -395,9 +427,8 @@ static inline RowShape shape_of(int32_t cols, int n, int narrow) {
     return s;
   }
   s.n = n;
-  s.ranks = (int)std::min<int64_t>(ceil_div64(runs, kBlockRuns), kMostRanks + 1);
-  s.held = s.ranks <= kMostRanks;
-  s.threads = (int)ceil_div64(ceil_div64(ceil_div64(runs, s.ranks), n), 32) * 32;
+  s.threads = (int)std::min<int64_t>(ceil_div64(ceil_div64(runs, n), 32) * 32, 1 << 20);
+  s.held = s.threads <= threads;
   return s;
 }
 
