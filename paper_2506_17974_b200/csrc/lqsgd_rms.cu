@@ -24,7 +24,7 @@ struct RmsArgs {
   float eps, per_col;                        // 1 / cols
   bool vec_gamma, vec_h8, vec_y8, vec_r8;    // on 16 bytes; rows of 8-bit copies on 8
 };
-constexpr int kForwardThreads = 256, kLongThreads = 256;
+constexpr int kForwardThreads = 256, kLongThreads = 256, kGradThreads = 512, kGradRuns = 2;
 
 // What a thread touches of one row of the forward call.
 template <int DT, int HOW>
@@ -52,7 +52,7 @@ struct ForwardRow {
     float v[kRun], r[kRun];
     if (a.drop.threshold) {
       uint4 bits[N];
-      drop_bits<N>(a.drop, room, block, bits);
+      drop_bits(a.drop, room, block, bits);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         sum_of(i, rr[i], r);
@@ -144,7 +144,8 @@ rms_forward_kernel(const __grid_constant__ RmsArgs a) {
 #pragma unroll
   for (int i = 0; i < N; ++i) io.add_squares(i, h[i], sum, top);
   sum[0] += sum[1];
-  team.join(sum[0], top, a.r8.dev_codes != nullptr, slots);
+  if (a.r8.dev_codes) team.template join<true>(sum[0], top, slots);
+  else team.template join<false>(sum[0], top, slots);
   io.figures(team.first(), sum[0], top, rstd, inv);
 #pragma unroll
   for (int i = 0; i < N; ++i) io.template put_y<N>(i, rstd, inv, h[i], y);
@@ -183,7 +184,7 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
     }
     if (pass == 0) {
       sum[0] += sum[1];
-      team.join(sum[0], top, a.r8.dev_codes != nullptr, slots);
+      team.template join<true>(sum[0], top, slots);
       ForwardRow<DT, HOW>(a, room, team.row, team.lanes(a.cols, true)).figures(team.first(), sum[0], top, rstd, inv);
     }
   }
@@ -191,12 +192,9 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
 
 // ---- backward
 // With h as it comes (xh = h rstd), a row needs <u xh> = rstd <dy h gamma>, and then d = gamma rstd dy - (rstd^2 <u xh>) h + skip.
-// A block keeps its columns' sums for dgamma in registers and walks rows.  What it reads goes through shared memory, a row
-// ahead (cp.async), every thread its own runs: registers have no room for rows in flight, and a row's values are read a second time behind the
-// sum.  h from its 8-bit form is decoded once, to bf16, in which it is exact.
-constexpr int kStages = 2;
-template <int DT> constexpr int kGradRuns = DT == LQSGD_F32 ? 1 : 2;
-template <int DT, bool NARROW> constexpr int kGradThreads = NARROW || DT != LQSGD_F32 ? 256 : 384;
+// A team walks rows: loads of all runs, the sum, stores; its columns' sums for dgamma stay in registers.  That leaves 16 warps an SM, too few to
+// hide HBM's latency, so one thread asks L2 for the next row meanwhile (8192 x 4096 without dropout 75 -> 61 us, fp32 136 -> 122).  h from its
+// 8-bit form is decoded once, to bf16, in which it is exact.
 // Eight codes as bf16: |128 + m| with the magnitude m below is a bf16 number (0x4300 | m), and (128 + m) 2^e - 128 2^e is m 2^e exactly; the
 // signs are put on top.  For exponents from kQuickByte on 128 2^e leaves the range.
 __device__ __forceinline__ void decode_bf16(uint2 c, uint32_t eb, uint32_t (&w)[4]) {
@@ -225,186 +223,173 @@ __device__ __forceinline__ void open_bf16(const uint32_t (&w)[4], float (&v)[kRu
     v[2 * j + 1] = f.y;
   }
 }
-__device__ __forceinline__ void copy_async(uint8_t* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
-// What a thread reads and writes of one row of the backward call.
+// What a thread reads of one row of the backward call.
 template <int DT, int HOW>
 struct BackwardRow {
-  static constexpr int kPieces = Raw<DT, HOW>::kPieces;
-  const RmsArgs& a;
-  const uint32_t (&room)[kDropRoom];
   Lanes l;
   int64_t row;
   Cursor<DT, HOW> dy, h, skip;
-  __device__ __forceinline__ BackwardRow(const RmsArgs& a_, const uint32_t (&room_)[kDropRoom], int64_t row_, const Lanes& l_)
-      : a(a_), room(room_), l(l_), row(row_), dy(a.dy, row * a.ld_dy, l), h(a.h, row * a.ld_h, l), skip(a.skip, row * a.ld_skip, l) {}
-  __device__ __forceinline__ const uint8_t* codes() const { return a.h8.dev_codes + row * a.h8.ld_codes + l.col; }
-  __device__ __forceinline__ bool codes_whole(int i) const { return HOW == kWhole || (a.vec_h8 && l.have(i) >= kRun); }
-  // Run i on its way into a thread's places in shared memory, `unit` bytes apart.
-  __device__ __forceinline__ void ask(const Cursor<DT, HOW>& c, int i, uint8_t* to, uint32_t unit) const {
-    using T = typename Elem<DT>::T;
-    if (HOW == kWhole || c.pieces(l, i)) {
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k)
-        if (k < kRunBytes<DT> / 16 || c.shift) copy_async(to + k * unit, c.at(i) + 16 * k);
-    } else {
-      Raw<DT, HOW> v;
-      fetch(c, l, i, v);
-#pragma unroll
-      for (int k = 0; k < kRunBytes<DT> / 16; ++k) *reinterpret_cast<uint4*>(to + k * unit) = reinterpret_cast<const uint4*>(v.w)[k];
-    }
+  __device__ __forceinline__ BackwardRow(const RmsArgs& a, int64_t row_, const Lanes& l_)
+      : l(l_), row(row_), dy(a.dy, row * a.ld_dy, l), h(a.h, row * a.ld_h, l), skip(a.skip, row * a.ld_skip, l) {}
+  // codes and exponent of run i of h's 8-bit form
+  __device__ __forceinline__ uint2 codes(const RmsArgs& a, int i) const {
+    const uint8_t* c = a.h8.dev_codes + row * a.h8.ld_codes + l.col + i * kWarpCols;
+    if (!l.has(i)) return make_uint2(0u, 0u);
+    return load_codes(c, HOW == kWhole || (a.vec_h8 && l.have(i) >= kRun), min(l.have(i), kRun));
   }
-  __device__ __forceinline__ void take(const Cursor<DT, HOW>& c, int i, const uint8_t* from, uint32_t unit, float (&v)[kRun]) const {
-    Raw<DT, HOW> raw;
-    Piece<DT> p;
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k) reinterpret_cast<uint4*>(raw.w)[k] = *reinterpret_cast<const uint4*>(from + k * unit);
-    settle(raw, c, l, i, p);
-    open_words<DT>(p, v);
-  }
-  // d of all runs into dx and dresidual
-  template <int N>
-  __device__ __forceinline__ void put_d(float (&d)[N][kRun]) const {
-    Piece<DT> out[N];
-    if (a.dresidual || !a.drop.threshold) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) close_words<DT>(d[i], out[i]);
-    }
-    if (a.dresidual) {
-      const Cursor<DT, HOW> c(a.dresidual, row * a.ld_dresidual, l);
-#pragma unroll
-      for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, l, i, out[i], out[i > 0 ? i - 1 : 0]);
-    }
-    if (!a.dx) return;
-    if (a.drop.threshold) {
-      uint4 bits[N];
-      drop_bits<N>(a.drop, room, (uint64_t)row * (uint32_t)((a.cols + kRun - 1) / kRun) + l.col / kRun, bits);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float t[kRun];
-        clear_run(t);
-        drop_run(a.drop, bits[i], d[i], t);
-        close_words<DT>(t, out[i]);
-      }
-    }
-    const Cursor<DT, HOW> c(a.dx, row * a.ld_dx, l);
-#pragma unroll
-    for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, l, i, out[i], out[i > 0 ? i - 1 : 0]);
+  __device__ __forceinline__ uint32_t exponent(const RmsArgs& a, int i) const {
+    return l.has(i) ? a.h8.dev_exps[row * a.h8.ld_exps + l.col / kGroup + i * (kWarpCols / kGroup)] : kExpBias;
   }
 };
+template <int DT>
+__device__ __forceinline__ void open_h(const RmsArgs& a, const Piece<DT>& h, float (&v)[kRun]) {
+  if (DT != LQSGD_BF16 && a.h8.dev_codes) {
+    const uint32_t w[4] = {h.w[0], h.w[1], h.w[2], h.w[3]};
+    open_bf16(w, v);
+  } else {
+    open_words<DT>(h, v);
+  }
+}
+// d of a thread's N runs into dx and dresidual.
+template <int DT, int HOW, int N>
+__device__ __forceinline__ void put_d(const RmsArgs& a, const uint32_t (&room)[kDropRoom], const BackwardRow<DT, HOW>& r, float (&d)[N][kRun]) {
+  Piece<DT> out[N];
+  auto write = [&](void* matrix, int64_t ld) {
+    const Cursor<DT, HOW> c(matrix, r.row * ld, r.l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, r.l, i, out[i], out[i > 0 ? i - 1 : 0]);
+  };
+  if (a.dresidual || !a.drop.threshold) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) close_words<DT>(d[i], out[i]);
+  }
+  if (a.dresidual) write(a.dresidual, a.ld_dresidual);
+  if (!a.dx) return;
+  if (a.drop.threshold) {
+    uint4 bits[N];
+    drop_bits(a.drop, room, (uint64_t)r.row * (uint32_t)((a.cols + kRun - 1) / kRun) + r.l.col / kRun, bits);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float t[kRun];
+      clear_run(t);
+      drop_run(a.drop, bits[i], d[i], t);
+      close_words<DT>(t, out[i]);
+    }
+  }
+  write(a.dx, a.ld_dx);
+}
+
+// Asks L2 for the whole 16-byte pieces of `bytes` from p on: one instruction.
+__device__ __forceinline__ void ahead(const void* p, int64_t bytes) {
+  const uintptr_t from = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, to = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
+  if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(to - from)) : "memory");
+}
+// The rows that a team comes to next.
+template <int DT>
+__device__ __forceinline__ void rows_ahead(const RmsArgs& a, int64_t row) {
+  constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
+  if (row >= a.rows) return;
+  ahead(static_cast<const char*>(a.dy) + row * a.ld_dy * kSize, (int64_t)a.cols * kSize);
+  if (a.skip) ahead(static_cast<const char*>(a.skip) + row * a.ld_skip * kSize, (int64_t)a.cols * kSize);
+  if (a.h8.dev_codes) ahead(a.h8.dev_codes + row * a.h8.ld_codes, a.cols);
+  else ahead(static_cast<const char*>(a.h) + row * a.ld_h * kSize, (int64_t)a.cols * kSize);
+}
 
 template <int DT, int N, bool NARROW, int HOW>
-__global__ void __launch_bounds__(kGradThreads<DT, NARROW>, 768 / kGradThreads<DT, NARROW>)
+__global__ void __launch_bounds__(NARROW ? 256 : kGradThreads, NARROW ? 2 : 1)
 rms_backward_kernel(const __grid_constant__ RmsArgs a) {
-  using Row = BackwardRow<DT, HOW>;
-  extern __shared__ __align__(16) uint8_t grad_smem[];
   __shared__ float2 slots[2][16];
+  __shared__ float sums[NARROW ? 256 * (kRun + 1) : 1];
   __shared__ uint32_t room[kDropRoom];
   const Team<NARROW, N> team(a.lane_shift);
   train_pdl_wait();
   open_drop(a.drop, room);
-  // [stage][run][dy pieces, skip pieces, h pieces or 8 bytes of codes][thread]
-  const uint32_t unit = blockDim.x * 16, off_skip = Row::kPieces * unit, off_h = off_skip + (a.skip ? Row::kPieces * unit : 0);
-  const uint32_t run_bytes = off_h + (a.h8.dev_codes ? unit / 2 : Row::kPieces * unit), stage_bytes = run_bytes * N;
-  uint8_t* const mine = grad_smem + threadIdx.x * 16;
-  uint8_t* const mine8 = grad_smem + off_h + threadIdx.x * 8;
   float acc[N][kRun];
 #pragma unroll
   for (int i = 0; i < N; ++i) clear_run(acc[i]);
-  uint32_t exps[N], exps_next[N];
-  float rstd, rstd_next;
-  auto ask = [&](int64_t row, uint32_t at) {
-    rstd_next = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) exps_next[i] = kExpBias;
-    if (row < a.rows) {
-      const Row r(a, room, row, team.lanes(a.cols, true));
-      rstd_next = a.rstd[row];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (!r.l.has(i)) continue;
-        uint8_t* to = mine + at + i * run_bytes;
-        r.ask(r.dy, i, to, unit);
-        if (a.skip) r.ask(r.skip, i, to + off_skip, unit);
-        if (a.h8.dev_codes) {
-          uint8_t* to8 = mine8 + at + i * run_bytes;
-          if (r.codes_whole(i))
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to8)), "l"(r.codes() + i * kWarpCols) : "memory");
-          else
-            *reinterpret_cast<uint2*>(to8) = load_codes(r.codes() + i * kWarpCols, false, min(r.l.have(i), kRun));
-          exps_next[i] = a.h8.dev_exps[row * a.h8.ld_exps + r.l.col / kGroup + i * (kWarpCols / kGroup)];
-        } else {
-          r.ask(r.h, i, to + off_h, unit);
-        }
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  // Places of runs that no row has hold zeros, so that the work on them needs no branch.  (Those of a row that does not exist keep what an
-  // earlier row left: it counts with rstd = 0 and is not written.)
-  for (uint32_t i = threadIdx.x; i < kStages * stage_bytes / 16; i += blockDim.x) reinterpret_cast<uint4*>(grad_smem)[i] = make_uint4(0u, 0u, 0u, 0u);
-  __syncthreads();
+  int turn = 0;
   // NARROW: a warp stays together while one of its rows exists
   const int64_t first = NARROW ? team.row - ((threadIdx.x & 31) >> team.shift) : team.row;
-  ask(team.row, 0);
-  uint32_t at = 0;
-  int turn = 0;
 #pragma unroll 1
   for (int64_t r0 = first; r0 < a.rows; r0 += team.rows_per_grid) {
     const int64_t row = team.row + (r0 - first);
-    rstd = rstd_next;
-#pragma unroll
-    for (int i = 0; i < N; ++i) exps[i] = exps_next[i];
-    ask(row + team.rows_per_grid, at ^ stage_bytes);
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    const Row r(a, room, row, team.lanes(a.cols, row < a.rows));
+    if (!NARROW && threadIdx.x == 0) rows_ahead<DT>(a, row + team.rows_per_grid);
+    const BackwardRow<DT, HOW> r(a, row, team.lanes(a.cols, row < a.rows));
     const float* gamma = a.gamma + r.l.col;
-    float sum[2] = {0.f, 0.f}, top = 0.f;
-    uint32_t h8[N][4];
+    Piece<DT> dy[N], h[N], skip[N];
+    {
+      Raw<DT, HOW> raw_dy[N], raw_h[N], raw_skip[N];
+      uint2 codes[N];
+      uint32_t exps[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(r.dy, r.l, i, raw_dy[i]);
+      if (a.h8.dev_codes) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          codes[i] = r.codes(a, i);
+          exps[i] = r.exponent(a, i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(r.h, r.l, i, raw_h[i]);
+      }
+      if (a.skip) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(r.skip, r.l, i, raw_skip[i]);
+      }
+      if (a.h8.dev_codes) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          uint32_t w[4];
+          decode_bf16(codes[i], exps[i], w);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[i].w[k] = w[k];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) settle(raw_h[i], r.h, r.l, i, h[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) settle(raw_dy[i], r.dy, r.l, i, dy[i]);
+      if (a.skip) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) settle(raw_skip[i], r.skip, r.l, i, skip[i]);
+      }
+    }
+    const float rstd = r.l.on ? a.rstd[row] : 0.f;
+    float sum[2] = {0.f, 0.f}, none = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint8_t* from = mine + at + i * run_bytes;
       float u[kRun], v[kRun], g[kRun];
-      if (a.h8.dev_codes) {
-        decode_bf16(*reinterpret_cast<const uint2*>(mine8 + at + i * run_bytes), exps[i], h8[i]);
-        open_bf16(h8[i], v);
-      } else {
-        r.take(r.h, i, from + off_h, unit, v);
-      }
-      r.take(r.dy, i, from, unit, u);
+      open_words<DT>(dy[i], u);
+      open_h<DT>(a, h[i], v);
       fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
       mul_run(u, u, v);
-      fma_run(acc[i], u, rstd, acc[i]);
       dot_run(sum, u, g);
+      fma_run(acc[i], u, rstd, acc[i]);
     }
     sum[0] += sum[1];
-    team.join(sum[0], top, false, slots[turn]);
+    team.template join<false>(sum[0], none, slots[turn]);
     turn ^= 1;
     const float k = rstd * rstd * (rstd * (sum[0] * a.per_col));
     float d[N][kRun];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float v[kRun], g[kRun];
-      const uint8_t* from = mine + at + i * run_bytes;
-      if (a.skip) r.take(r.skip, i, from + off_skip, unit, d[i]);
-      else clear_run(d[i]);
-      if (a.h8.dev_codes) open_bf16(h8[i], v);
-      else r.take(r.h, i, from + off_h, unit, v);
+      clear_run(d[i]);
+      if (a.skip) open_words<DT>(skip[i], d[i]);
+      open_h<DT>(a, h[i], v);
       fma_run(d[i], v, -k, d[i]);
-      r.take(r.dy, i, from, unit, v);
+      open_words<DT>(dy[i], v);
       fetch_vector<HOW>(gamma, a.vec_gamma, r.l, i, g);
       mul_run(g, g, rstd);
       fma_run(d[i], g, v, d[i]);
     }
-    r.template put_d<N>(d);
-    at ^= stage_bytes;
+    put_d<DT, HOW, N>(a, room, r, d);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
   if (!a.partial) return;
   train_pdl_trigger();
   float* out = a.partial + (size_t)blockIdx.x * a.cols;
-  float* sums = reinterpret_cast<float*>(grad_smem);
   const Lanes l = team.lanes(a.cols, true);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -429,44 +414,60 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
 }
 
 // Rows longer than a block holds: <dy h gamma> of each in a first kernel, the rest as a stream over columns.
+// The first run of a row as it is fetched, so that several rows' loads are out before any is used.
 template <int DT, int HOW>
-__device__ __forceinline__ void load_dy_h(const BackwardRow<DT, HOW>& r, float (&dy)[kRun], float (&h)[kRun]) {
-  Raw<DT, HOW> raw;
-  Piece<DT> p;
-  fetch(r.dy, r.l, 0, raw);
-  settle(raw, r.dy, r.l, 0, p);
-  open_words<DT>(p, dy);
-  if (!r.a.h8.dev_codes) {
-    fetch(r.h, r.l, 0, raw);
-    settle(raw, r.h, r.l, 0, p);
-    open_words<DT>(p, h);
-  } else {
-    uint32_t w[4];
-    decode_bf16(load_codes(r.codes(), r.codes_whole(0), min(r.l.have(0), kRun)), r.a.h8.dev_exps[r.row * r.a.h8.ld_exps + r.l.col / kGroup], w);
-    open_bf16(w, h);
+struct GradRun {
+  BackwardRow<DT, HOW> r;
+  Raw<DT, HOW> dy, h, skip;
+  uint2 codes;
+  uint32_t exp;
+  float rstd;
+  __device__ __forceinline__ GradRun(const RmsArgs& a, int64_t row, const Lanes& l, bool with_skip) : r(a, row, l) {
+    fetch(r.dy, l, 0, dy);
+    if (a.h8.dev_codes) {
+      codes = r.codes(a, 0);
+      exp = r.exponent(a, 0);
+    } else {
+      fetch(r.h, l, 0, h);
+    }
+    if (with_skip && a.skip) fetch(r.skip, l, 0, skip);
+    rstd = l.on ? a.rstd[row] : 0.f;
   }
-}
+  __device__ __forceinline__ void open_dy_h(const RmsArgs& a, float (&u)[kRun], float (&v)[kRun]) const {
+    Piece<DT> p;
+    settle(dy, r.dy, r.l, 0, p);
+    open_words<DT>(p, u);
+    if (a.h8.dev_codes) {
+      uint32_t w[4];
+      decode_bf16(codes, exp, w);
+      open_bf16(w, v);
+    } else {
+      settle(h, r.h, r.l, 0, p);
+      open_words<DT>(p, v);
+    }
+  }
+};
 template <int DT, int HOW>
 __global__ void __launch_bounds__(512)
 rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   __shared__ float2 slots[16];
-  __shared__ uint32_t room[kDropRoom];
   const Team<false, 1> team(0);
   train_pdl_wait();
   float sum[2] = {0.f, 0.f}, top = 0.f;
   const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
-#pragma unroll 2
-  for (int k = 0; k < steps; ++k) {
-    const BackwardRow<DT, HOW> r(a, room, team.row, team.lanes(a.cols, true, k));
-    float dy[kRun], h[kRun], g[kRun];
-    if (!r.l.has(0)) continue;
-    load_dy_h(r, dy, h);
-    fetch_vector<HOW>(a.gamma + r.l.col, a.vec_gamma, r.l, 0, g);
-    mul_run(dy, dy, h);
-    dot_run(sum, dy, g);
+  for (int k = 0; k < steps; k += 2) {
+    const GradRun<DT, HOW> p[2] = {{a, team.row, team.lanes(a.cols, true, k), false}, {a, team.row, team.lanes(a.cols, true, k + 1), false}};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float u[kRun], v[kRun], g[kRun];
+      p[i].open_dy_h(a, u, v);
+      fetch_vector<HOW>(a.gamma + p[i].r.l.col, a.vec_gamma, p[i].r.l, 0, g);
+      mul_run(u, u, v);
+      dot_run(sum, u, g);
+    }
   }
   sum[0] += sum[1];
-  team.join(sum[0], top, false, slots);
+  team.template join<false>(sum[0], top, slots);
   if (team.first()) dots[team.row] = sum[0] * a.per_col;
 }
 template <int DT, int HOW>
@@ -479,30 +480,31 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, const __grid_constant__ De
   const Spot s(d);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warp_cols = kRun * 32;
   const Lanes l = {s.col, a.cols - s.col, lane, 32, true};
-  float acc[kRun] = {}, g[kRun];
+  float acc[kRun], g[kRun];
+  clear_run(acc);
   fetch_vector<HOW>(a.gamma + l.col, a.vec_gamma, l, 0, g);
-  for (int64_t row = s.row; row < s.row_end; row += s.row_step) {
-    const BackwardRow<DT, HOW> r(a, room, row, l);
-    float dy[kRun], h[kRun], d1[1][kRun];
-    float (&e)[kRun] = d1[0];
-    if (l.has(0)) {
-      load_dy_h(r, dy, h);
-      const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
-      clear_run(e);
+  for (int64_t row = s.row; row < s.row_end; row += 2 * s.row_step) {
+    Lanes l2 = l;
+    l2.on = row + s.row_step < s.row_end;
+    const GradRun<DT, HOW> p[2] = {{a, row, l, true}, {a, row + s.row_step, l2, true}};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float rstd = p[i].rstd, k = p[i].r.l.on ? rstd * rstd * (rstd * dots[p[i].r.row]) : 0.f;
+      float u[kRun], v[kRun], d[1][kRun];
+      p[i].open_dy_h(a, u, v);
+      clear_run(d[0]);
       if (a.skip) {
-        Raw<DT, HOW> raw;
         Piece<DT> t;
-        fetch(r.skip, l, 0, raw);
-        settle(raw, r.skip, l, 0, t);
-        open_words<DT>(t, e);
+        settle(p[i].skip, p[i].r.skip, p[i].r.l, 0, t);
+        open_words<DT>(t, d[0]);
       }
-      fma_run(e, h, -k, e);
-      mul_run(h, h, dy);
-      fma_run(acc, h, rstd, acc);
-      mul_run(dy, dy, rstd);
-      fma_run(e, dy, g, e);
+      fma_run(d[0], v, -k, d[0]);
+      mul_run(v, v, u);
+      fma_run(acc, v, rstd, acc);
+      mul_run(u, u, rstd);
+      fma_run(d[0], u, g, d[0]);
+      put_d<DT, HOW, 1>(a, room, p[i].r, d);
     }
-    r.template put_d<1>(d1);
   }
   if (!a.partial) return;
   // the rows that the block's warps have of one column: warps side by side hold other columns
@@ -533,25 +535,17 @@ struct GradPlan {
   Deal deal;
   dim3 grid;
   int blocks;                                // of the sums over rows
-  size_t smem, off_partial, bytes;
+  size_t off_partial, bytes;
 };
-GradPlan plan_backward(const lqsgd_rms_norm& a, int how) {
+GradPlan plan_backward(const lqsgd_rms_norm& a) {
   GradPlan p = {};
-  const bool wide = a.dtype == LQSGD_F32;
-  p.shape = shape_of(a.cols, wide ? kGradRuns<LQSGD_F32> : kGradRuns<LQSGD_BF16>, wide ? 256 : 512, wide ? kGradThreads<LQSGD_F32, false> : kGradThreads<LQSGD_BF16, false>);
-  const int pieces = kRun * train_elem(a.dtype) / 16 + (how == kShift ? 1 : 0);
-  const bool kept = a.h8.dev_codes != nullptr;
-  const size_t run = (size_t)16 * pieces * (1 + (a.dev_skip ? 1 : 0) + (kept ? 0 : 1)) + (kept ? 8 : 0);
-  p.smem = std::max(run * kStages * p.shape.n * p.shape.threads, p.shape.narrow ? sizeof(float) * 256 * (kRun + 1) : 0);
-  p.shape.held = p.shape.held && p.smem <= 224 * 1024;
+  p.shape = shape_of(a.cols, kGradRuns, 512, kGradThreads);
   if (!p.shape.held) {
     p.deal = make_deal(a.rows, a.cols, true, kCtasColumns, 8, &p.grid);
     p.blocks = (int)p.grid.y;
     p.off_partial = (size_t)ceil_div64(a.rows * 4, 256) * 256;
   } else {
-    // 768 threads an SM have registers, as many blocks shared memory (1.5 KB of it are not for rows)
-    const int64_t per_sm = std::max<int64_t>(1, std::min<int64_t>(768 / p.shape.threads, 226 * 1024 / (p.smem + 1536)));
-    p.blocks = (int)std::min<int64_t>(ceil_div64(a.rows, p.shape.teams), kSms * per_sm);
+    p.blocks = (int)std::min<int64_t>(ceil_div64(a.rows, p.shape.teams), kSms * (512 / p.shape.threads));    // what registers hold
     p.grid = dim3((unsigned)p.blocks);
   }
   p.bytes = p.off_partial + (a.dev_dgamma && p.blocks > 1 ? (size_t)p.blocks * a.cols * 4 : 0);
@@ -567,19 +561,6 @@ cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st)
   return GO(kForwardRuns<DT>, false);
 #undef GO
 }
-template <int DT, int N, bool NARROW, int HOW>
-cudaError_t launch_held(const GradPlan& p, const RmsArgs& a, cudaStream_t st) {
-  auto kernel = rms_backward_kernel<DT, N, NARROW, HOW>;
-  static std::atomic<uint64_t> ready{0};                     // devices on which the kernel may use its shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024)) != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
-  }
-  return train_launch(kernel, p.grid, dim3(p.shape.threads), p.smem, st, 1, a);
-}
 template <int DT, int HOW>
 cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
   if (!p.shape.held) {
@@ -587,10 +568,9 @@ cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cu
     return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.deal, dots);
   }
   const RowShape& s = p.shape;
-#define GO(N, NARROW) launch_held<DT, N, NARROW, HOW>(p, a, st)
-  if (!s.narrow) return GO(kGradRuns<DT>, false);
-  if constexpr (DT == LQSGD_F32) return GO(1, true);
-  else return s.n == 1 ? GO(1, true) : GO(2, true);
+#define GO(N, NARROW) train_launch(rms_backward_kernel<DT, N, NARROW, HOW>, p.grid, dim3(s.threads), 0, st, 1, a)
+  if (s.narrow) return s.n == 1 ? GO(1, true) : GO(2, true);
+  return GO(kGradRuns, false);
 #undef GO
 }
 
@@ -625,7 +605,7 @@ extern "C" int lqsgd_rms_norm_workspace_bytes(int32_t backward, const lqsgd_rms_
   if (!host_bytes_out || (backward != 0 && backward != 1)) return LQSGD_ERR_INVALID_ARG;
   const int rc = check_args(a);
   if (rc != LQSGD_OK) return rc;
-  *host_bytes_out = backward && a->rows > 0 ? plan_backward(*a, backward_access(*a)).bytes : 0;
+  *host_bytes_out = backward && a->rows > 0 ? plan_backward(*a).bytes : 0;
   return LQSGD_OK;
 }
 
@@ -684,7 +664,7 @@ extern "C" int lqsgd_rms_norm_backward(const lqsgd_rms_norm* a, void* cuda_strea
   k.vec_gamma = train_aligned(a->dev_gamma, 16);
   k.vec_h8 = on8(a->h8.dev_codes, a->h8.ld_codes, a->rows);
   const int how = backward_access(*a);
-  const GradPlan p = plan_backward(*a, how);
+  const GradPlan p = plan_backward(*a);
   if (p.bytes) {
     if (!a->dev_workspace || a->workspace_bytes < p.bytes) return LQSGD_ERR_WORKSPACE_TOO_SMALL;
     if (!train_aligned(a->dev_workspace, 16)) return LQSGD_ERR_MISALIGNED;

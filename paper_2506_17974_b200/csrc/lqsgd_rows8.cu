@@ -36,7 +36,7 @@ pack_rows8_kernel(const __grid_constant__ PackArgs a) {
     open_words<DT>(p[i], v);
     top = largest(top, v);
   }
-  team.join(none, top, true, slots);
+  team.template join<true>(none, top, slots);
   float scale, inv;
   row_scale(top, scale, inv);
   if (team.first() && l.on) a.out.dev_scales[row] = scale;
@@ -78,7 +78,7 @@ pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
       }
     }
     if (pass == 0) {
-      team.join(none, top, true, slots);
+      team.template join<true>(none, top, slots);
       row_scale(top, scale, inv);
       if (team.first()) a.out.dev_scales[row] = scale;
     }
@@ -163,7 +163,7 @@ dropout_kernel(const __grid_constant__ Strips s, const void* x, int64_t ld_x, co
   const uint64_t block = (uint64_t)w.row * (uint32_t)((s.cols + kRun - 1) / kRun) + l.col / kRun;
   Piece<DT> p[N];
   uint4 bits[N];
-  drop_bits<N>(drop, room, block, bits);
+  drop_bits(drop, room, block, bits);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float v[kRun], sum[kRun];

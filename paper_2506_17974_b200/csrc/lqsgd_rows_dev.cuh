@@ -207,9 +207,13 @@ struct Cursor {
   uint32_t shift;
   int need;
   bool head;
-  __device__ __forceinline__ Cursor(const void* matrix, int64_t at, const Lanes& l) {
+  Cursor() = default;
+  __device__ __forceinline__ Cursor(const void* matrix, int64_t at, const Lanes& l)
+      : Cursor(static_cast<const char*>(matrix) + (at + l.col) * (int64_t)sizeof(typename Elem<DT>::T), l) {}
+  // from the address of the thread's first run
+  __device__ __forceinline__ Cursor(const char* run, const Lanes& l) {
     constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
-    p = static_cast<char*>(const_cast<void*>(matrix)) + (at + l.col) * kSize;
+    p = const_cast<char*>(run);
     shift = 0;
     need = kRun;
     head = false;
@@ -372,17 +376,18 @@ struct Team {
     return l;
   }
   __device__ __forceinline__ bool first() const { return (threadIdx.x & (NARROW ? (1 << shift) - 1 : 0xffff)) == 0; }
-  // Sum and (where with_top) largest of the team's values, in every thread of it.  `slots`: shared memory (unused by NARROW); of two
-  // calls in a row the second takes other slots.
-  __device__ __forceinline__ void join(float& sum, float& top, bool with_top, float2 (&slots)[16]) const {
+  // Sum and, where TOP, largest of the team's values, in every thread of it.  `slots`: shared memory (unused by NARROW); of two calls in
+  // a row the second takes other slots.
+  template <bool TOP>
+  __device__ __forceinline__ void join(float& sum, float& top, float2 (&slots)[16]) const {
     if constexpr (NARROW) {
       for (int o = 1; o < 1 << shift; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (with_top)
+      if (TOP)
         for (int o = 1; o < 1 << shift; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
     } else {
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (with_top) {
+      if (TOP) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
       }
@@ -394,7 +399,7 @@ struct Team {
         for (int w = 0; w < warps; ++w) {
           const float2 s = slots[w];
           sum += s.x;
-          top = larger(top, s.y);
+          if (TOP) top = larger(top, s.y);
         }
       }
     }
