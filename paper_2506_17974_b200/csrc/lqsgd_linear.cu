@@ -342,7 +342,13 @@ int run(int product, const lqsgd_linear& a, const LinEpilogue& ep, cudaStream_t 
     return plan.cg == 2 ? launch<2, 256, kOpMN, kOpMN, true>(plan, q, st) : launch<1, 128, kOpMN, kOpMN, true>(plan, q, st);
   });
 }
+int run_few(const lqsgd_linear_rows8& a, const LinEpilogue& ep, cudaStream_t st);
+bool few_rows(const lqsgd_linear_rows8& a);
 int run(const lqsgd_linear_rows8& a, const LinEpilogue& ep, cudaStream_t st) {
+  if (few_rows(a)) {
+    test_wait = TestWait();
+    return run_few(a, ep, st);
+  }
   Plan p;
   int rc = make_plan(a, &p);
   if (rc == LQSGD_OK) rc = check_workspace(p, a.dev_workspace, a.workspace_bytes);
@@ -353,6 +359,88 @@ int run(const lqsgd_linear_rows8& a, const LinEpilogue& ep, cudaStream_t st) {
   return run_plan<kInt8>(p, ep, a.dtype, a.dev_status, static_cast<char*>(a.dev_workspace), st, [&](const Plan& plan, LinProblem& q) {
     return plan.cg == 2 ? launch<2, 256, kOpK, kOpK, false, kInt8>(plan, q, st) : launch<1, 128, kOpK, kOpK, false, kInt8>(plan, q, st);
   });
+}
+
+// ---- products of codes for a few rows (a token between two layers): w is read once, and its bytes are all that the call costs.  The tensor
+// cores' tile fills 128 of the SMs for 16384 channels and starts with a tensor map, tensor memory and a first copy's latency; plain wide
+// loads of w, straight into integer dot products of four codes, start at once and fill the card.  A warp takes four channels, so that a piece
+// of x is loaded once for them; where there are few channels, several warps of a block share the terms of a sum.
+constexpr int kFewRows = 2, kFewChannels = 4;
+template <int R>
+__global__ void __launch_bounds__(256)
+rows8_few_kernel(const int8_t* __restrict__ x, int64_t ld_x, const int8_t* __restrict__ w, int64_t ld_w, int cin, int ksplit, const __grid_constant__ LinEpilogue e) {
+  __shared__ int parts[8][R * kFewChannels];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int part = warp % ksplit, group = warp / ksplit, channel0 = ((int)blockIdx.x * ((int)(blockDim.x >> 5) / ksplit) + group) * kFewChannels;
+  train_pdl_wait();
+  int acc[R][kFewChannels] = {};
+  const int pieces = cin / 16;
+  const int8_t* wr[kFewChannels];
+#pragma unroll
+  for (int c = 0; c < kFewChannels; ++c) wr[c] = w + (int64_t)min(channel0 + c, e.cols - 1) * ld_w;      // channels past the last are not written
+#pragma unroll 4
+  for (int k = part * 32 + lane; k < pieces; k += 32 * ksplit) {
+    int4 a[R], b[kFewChannels];
+#pragma unroll
+    for (int c = 0; c < kFewChannels; ++c) b[c] = __ldg(reinterpret_cast<const int4*>(wr[c]) + k);
+#pragma unroll
+    for (int r = 0; r < R; ++r) a[r] = r < e.rows ? __ldg(reinterpret_cast<const int4*>(x + r * ld_x) + k) : make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < kFewChannels; ++c)
+        acc[r][c] = __dp4a(a[r].w, b[c].w, __dp4a(a[r].z, b[c].z, __dp4a(a[r].y, b[c].y, __dp4a(a[r].x, b[c].x, acc[r][c]))));
+  }
+  const int k = pieces * 16 + lane;                                       // the last piece, if it is not whole
+  if (part == 0 && lane < 16 && k < cin) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < kFewChannels; ++c)
+        if (r < e.rows) acc[r][c] += (int)x[r * ld_x + k] * (int)wr[c][k];
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int c = 0; c < kFewChannels; ++c) {
+      acc[r][c] = __reduce_add_sync(0xffffffffu, acc[r][c]);
+      if (ksplit > 1 && lane == 0) parts[warp][r * kFewChannels + c] = acc[r][c];
+    }
+  if (ksplit > 1) {
+    __syncthreads();
+    if (part != 0) return;
+  }
+  if (lane >= R * kFewChannels) return;
+  const int r = lane / kFewChannels, c = lane % kFewChannels, channel = channel0 + c;
+  if (r >= e.rows || channel >= e.cols) return;
+  int sum = 0;
+  if (ksplit > 1) {
+    for (int p = 0; p < ksplit; ++p) sum += parts[warp + p][lane];
+  } else {
+#pragma unroll
+    for (int i = 0; i < R * kFewChannels; ++i)
+      if (i == lane) sum = acc[i / kFewChannels][i % kFewChannels];
+  }
+  float v[1] = {(float)sum * __ldg(e.row_scale + r) * __ldg(e.col_scale + channel)};
+  if (e.bias) v[0] += __ldg(e.bias + channel);
+  act_run(e.act, v);
+  if (e.residual) v[0] += unpack1(e.dtype, static_cast<const uint16_t*>(e.residual)[r * e.ld_res + channel]);
+  static_cast<uint16_t*>(e.out)[r * e.ld_out + channel] = pack1(e.dtype, v[0]);
+}
+// Whether the call takes that way: rows on 16 bytes, and no copies in 8 bits (their groups of 32 channels span warps).
+bool few_rows(const lqsgd_linear_rows8& a) {
+  return a.rows <= kFewRows && !a.z8.dev_codes && !a.y8.dev_codes && train_aligned(a.x.dev_codes, 16) && train_aligned(a.w.dev_codes, 16) &&
+         (a.rows == 1 || a.x.ld_codes % 16 == 0) && (a.out == 1 || a.w.ld_codes % 16 == 0);
+}
+int run_few(const lqsgd_linear_rows8& a, const LinEpilogue& ep, cudaStream_t st) {
+  const int64_t warps = ceil_div64(a.out, kFewChannels);
+  int ksplit = 1;                                                         // until the card has four warps a scheduler, or a warp 8 pieces a lane
+  while (ksplit < 8 && warps * ksplit < kSms * 16 && a.in > 32 * 16 * 8 * ksplit) ksplit *= 2;
+  const int together = std::max(4, ksplit);                               // warps of a block: small ones deal out evenly
+  const dim3 grid((unsigned)ceil_div64(warps, together / ksplit));
+  auto go = [&](auto kernel) { return train_launch(kernel, grid, dim3(32 * together), 0, st, 1, a.x.dev_codes, a.x.ld_codes, a.w.dev_codes, a.w.ld_codes, a.in, ksplit, ep); };
+  TRAIN_CK(a.rows == 1 ? go(rows8_few_kernel<1>) : go(rows8_few_kernel<2>), "rows8_few_kernel launch");
+  return LQSGD_OK;
 }
 
 int check_rows8_args(const lqsgd_linear_rows8* a) {
@@ -449,7 +537,7 @@ extern "C" int lqsgd_linear_rows8_workspace_bytes(const lqsgd_linear_rows8* host
   int rc = check_rows8_args(host_args);
   if (rc != LQSGD_OK) return rc;
   *host_bytes_out = 0;
-  if (host_args->rows == 0) return LQSGD_OK;
+  if (host_args->rows == 0 || few_rows(*host_args)) return LQSGD_OK;
   Plan p;
   if ((rc = make_plan(*host_args, &p)) != LQSGD_OK) return rc;
   *host_bytes_out = p.bytes;

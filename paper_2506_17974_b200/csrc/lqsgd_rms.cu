@@ -388,7 +388,6 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
     put_d<DT, HOW, N>(a, room, r, d);
   }
   if (!a.partial) return;
-  train_pdl_trigger();
   float* out = a.partial + (size_t)blockIdx.x * a.cols;
   const Lanes l = team.lanes(a.cols, true);
 #pragma unroll
@@ -414,54 +413,61 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
 }
 
 // Rows longer than a block holds: <dy h gamma> of each in a first kernel, the rest as a stream over columns.
-// The first run of a row as it is fetched, so that several rows' loads are out before any is used.
-template <int DT, int HOW>
-struct GradRun {
+// A thread's N runs of a row as they are fetched.
+template <int DT, int N, int HOW>
+struct GradRuns {
   BackwardRow<DT, HOW> r;
-  Raw<DT, HOW> dy, h, skip;
-  uint2 codes;
-  uint32_t exp;
-  float rstd;
-  __device__ __forceinline__ GradRun(const RmsArgs& a, int64_t row, const Lanes& l, bool with_skip) : r(a, row, l) {
-    fetch(r.dy, l, 0, dy);
+  Raw<DT, HOW> dy[N], h[N], skip[N];
+  uint2 codes[N];
+  uint32_t exps[N];
+  __device__ __forceinline__ GradRuns(const RmsArgs& a, int64_t row, const Lanes& l, bool with_skip) : r(a, row, l) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) fetch(r.dy, l, i, dy[i]);
     if (a.h8.dev_codes) {
-      codes = r.codes(a, 0);
-      exp = r.exponent(a, 0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        codes[i] = r.codes(a, i);
+        exps[i] = r.exponent(a, i);
+      }
     } else {
-      fetch(r.h, l, 0, h);
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(r.h, l, i, h[i]);
     }
-    if (with_skip && a.skip) fetch(r.skip, l, 0, skip);
-    rstd = l.on ? a.rstd[row] : 0.f;
+    if (with_skip && a.skip) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) fetch(r.skip, l, i, skip[i]);
+    }
   }
-  __device__ __forceinline__ void open_dy_h(const RmsArgs& a, float (&u)[kRun], float (&v)[kRun]) const {
+  __device__ __forceinline__ void open_dy_h(const RmsArgs& a, int i, float (&u)[kRun], float (&v)[kRun]) const {
     Piece<DT> p;
-    settle(dy, r.dy, r.l, 0, p);
+    settle(dy[i], r.dy, r.l, i, p);
     open_words<DT>(p, u);
     if (a.h8.dev_codes) {
       uint32_t w[4];
-      decode_bf16(codes, exp, w);
+      decode_bf16(codes[i], exps[i], w);
       open_bf16(w, v);
     } else {
-      settle(h, r.h, r.l, 0, p);
+      settle(h[i], r.h, r.l, i, p);
       open_words<DT>(p, v);
     }
   }
 };
-template <int DT, int HOW>
-__global__ void __launch_bounds__(512)
+template <int DT, int N, int HOW>
+__global__ void __launch_bounds__(kLongThreads)
 rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   __shared__ float2 slots[16];
-  const Team<false, 1> team(0);
+  const Team<false, N> team(0);
   train_pdl_wait();
   float sum[2] = {0.f, 0.f}, top = 0.f;
-  const int steps = (a.cols + 512 * kRun - 1) / (512 * kRun);
-  for (int k = 0; k < steps; k += 2) {
-    const GradRun<DT, HOW> p[2] = {{a, team.row, team.lanes(a.cols, true, k), false}, {a, team.row, team.lanes(a.cols, true, k + 1), false}};
+  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
+#pragma unroll 1
+  for (int k = 0; k < steps; ++k) {
+    const GradRuns<DT, N, HOW> p(a, team.row, team.lanes(a.cols, true, k), false);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N; ++i) {
       float u[kRun], v[kRun], g[kRun];
-      p[i].open_dy_h(a, u, v);
-      fetch_vector<HOW>(a.gamma + p[i].r.l.col, a.vec_gamma, p[i].r.l, 0, g);
+      p.open_dy_h(a, i, u, v);
+      fetch_vector<HOW>(a.gamma + p.r.l.col, a.vec_gamma, p.r.l, i, g);
       mul_run(u, u, v);
       dot_run(sum, u, g);
     }
@@ -470,54 +476,66 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   team.template join<false>(sum[0], top, slots);
   if (team.first()) dots[team.row] = sum[0] * a.per_col;
 }
-template <int DT, int HOW>
-__global__ void __launch_bounds__(kThreads)
-rms_columns_kernel(const __grid_constant__ RmsArgs a, const __grid_constant__ Deal d, const float* dots) {
-  __shared__ __align__(16) float sums[kWarps][32][kRun + 1];
+// A block's warps take the same strip of N runs per lane of different rows; blockIdx.x = strip, blockIdx.y = block of rows.
+template <int DT, int N, int HOW>
+__global__ void __launch_bounds__(kThreads, 2)
+rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, const float* dots) {
+  __shared__ float sums[kWarps][kWarpCols];
   __shared__ uint32_t room[kDropRoom];
+  constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
   train_pdl_wait();
   open_drop(a.drop, room);
-  const Spot s(d);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warp_cols = kRun * 32;
-  const Lanes l = {s.col, a.cols - s.col, lane, 32, true};
-  float acc[kRun], g[kRun];
-  clear_run(acc);
-  fetch_vector<HOW>(a.gamma + l.col, a.vec_gamma, l, 0, g);
-  for (int64_t row = s.row; row < s.row_end; row += 2 * s.row_step) {
-    Lanes l2 = l;
-    l2.on = row + s.row_step < s.row_end;
-    const GradRun<DT, HOW> p[2] = {{a, row, l, true}, {a, row + s.row_step, l2, true}};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, strip = (int)blockIdx.x * N * kWarpCols, wide = min(N * kWarpCols, a.cols - strip);
+  const Lanes l = {strip + lane * kRun, a.cols - strip - lane * kRun, lane, 32, true};
+  float acc[N][kRun];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float rstd = p[i].rstd, k = p[i].r.l.on ? rstd * rstd * (rstd * dots[p[i].r.row]) : 0.f;
-      float u[kRun], v[kRun], d[1][kRun];
-      p[i].open_dy_h(a, u, v);
-      clear_run(d[0]);
+  for (int i = 0; i < N; ++i) clear_run(acc[i]);
+  const int64_t end = min(a.rows, (int64_t)(blockIdx.y + 1) * rows_per_block);
+#pragma unroll 1
+  for (int64_t row = blockIdx.y * rows_per_block + warp; row < end; row += kWarps) {
+    if (lane == 0 && row + kWarps < end) {
+      const int64_t next = row + kWarps;
+      ahead(static_cast<const char*>(a.dy) + (next * a.ld_dy + strip) * kSize, wide * kSize);
+      if (a.skip) ahead(static_cast<const char*>(a.skip) + (next * a.ld_skip + strip) * kSize, wide * kSize);
+      if (a.h8.dev_codes) ahead(a.h8.dev_codes + next * a.h8.ld_codes + strip, wide);
+      else ahead(static_cast<const char*>(a.h) + (next * a.ld_h + strip) * kSize, wide * kSize);
+    }
+    const GradRuns<DT, N, HOW> p(a, row, l, true);
+    const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
+    float d[N][kRun];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float u[kRun], v[kRun], g[kRun];
+      p.open_dy_h(a, i, u, v);
+      clear_run(d[i]);
       if (a.skip) {
         Piece<DT> t;
-        settle(p[i].skip, p[i].r.skip, p[i].r.l, 0, t);
-        open_words<DT>(t, d[0]);
+        settle(p.skip[i], p.r.skip, l, i, t);
+        open_words<DT>(t, d[i]);
       }
-      fma_run(d[0], v, -k, d[0]);
+      fma_run(d[i], v, -k, d[i]);
       mul_run(v, v, u);
-      fma_run(acc, v, rstd, acc);
+      fma_run(acc[i], v, rstd, acc[i]);
       mul_run(u, u, rstd);
-      fma_run(d[0], u, g, d[0]);
-      put_d<DT, HOW, 1>(a, room, p[i].r, d);
+      fetch_vector<HOW>(a.gamma + l.col, a.vec_gamma, l, i, g);
+      fma_run(d[i], u, g, d[i]);
     }
+    put_d<DT, HOW, N>(a, room, p.r, d);
   }
   if (!a.partial) return;
-  // the rows that the block's warps have of one column: warps side by side hold other columns
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) sums[warp][lane][j] = acc[j];
-  __syncthreads();
-  for (int c = threadIdx.x; c < warp_cols << d.wide_shift; c += kThreads) {
-    const int col = (int)blockIdx.x * (warp_cols << d.wide_shift) + c;
-    if (col >= a.cols) continue;
-    const int beside = c / warp_cols, in = c - beside * warp_cols;
-    float t = 0.f;
-    for (int w = beside; w < kWarps; w += 1 << d.wide_shift) t += sums[w][in / kRun][in % kRun];
-    a.partial[(size_t)blockIdx.y * a.cols + col] = t;
+  for (int i = 0; i < N; ++i) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) sums[warp][lane * kRun + j] = acc[i][j];
+    __syncthreads();
+    const int c = threadIdx.x, col = strip + i * kWarpCols + c;
+    if (col < a.cols) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) t += sums[w][c];
+      a.partial[(size_t)blockIdx.y * a.cols + col] = t;
+    }
   }
 }
 
@@ -529,11 +547,11 @@ template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
 RowShape forward_shape(const lqsgd_rms_norm& a) {
   return shape_of(a.cols, a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow, kForwardThreads);
 }
-constexpr int kCtasColumns = kSms * 6;
+constexpr int kCtasColumns = kSms * 2;
 struct GradPlan {
   RowShape shape;
-  Deal deal;
   dim3 grid;
+  int64_t rows_per_block;                    // of the kernels for long rows
   int blocks;                                // of the sums over rows
   size_t off_partial, bytes;
 };
@@ -541,7 +559,11 @@ GradPlan plan_backward(const lqsgd_rms_norm& a) {
   GradPlan p = {};
   p.shape = shape_of(a.cols, kGradRuns, 512, kGradThreads);
   if (!p.shape.held) {
-    p.deal = make_deal(a.rows, a.cols, true, kCtasColumns, 8, &p.grid);
+    // blocks that fill the card, as many of them below one another as the strips of a row leave; a warp takes two rows at least
+    const int64_t strips = ceil_div64(a.cols, kGradRuns * kWarpCols);
+    const int64_t below = std::max<int64_t>(1, std::min<int64_t>({kCtasColumns / strips, ceil_div64(a.rows, 2 * kWarps), 65535}));
+    p.rows_per_block = ceil_div64(a.rows, below);
+    p.grid = dim3((unsigned)strips, (unsigned)ceil_div64(a.rows, p.rows_per_block));
     p.blocks = (int)p.grid.y;
     p.off_partial = (size_t)ceil_div64(a.rows * 4, 256) * 256;
   } else {
@@ -564,8 +586,8 @@ cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st)
 template <int DT, int HOW>
 cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
   if (!p.shape.held) {
-    const cudaError_t e = train_launch(rms_dot_kernel<DT, HOW>, dim3((unsigned)a.rows), dim3(512), 0, st, 1, a, dots);
-    return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.deal, dots);
+    const cudaError_t e = train_launch(rms_dot_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a, dots);
+    return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, kGradRuns, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.rows_per_block, dots);
   }
   const RowShape& s = p.shape;
 #define GO(N, NARROW) train_launch(rms_backward_kernel<DT, N, NARROW, HOW>, p.grid, dim3(s.threads), 0, st, 1, a)

@@ -269,7 +269,7 @@ def test_empty_batches():
 
 # ------------------------------------------------------------------------------------------ products of rows of codes
 
-def check_product(rows, cin, cout, dtype, act, bias, residual, seed=0, x_pad=0, w_pad=0, out_pad=0, extreme=False):
+def check_product(rows, cin, cout, dtype, act, bias, residual, seed=0, x_pad=0, w_pad=0, out_pad=0, extreme=False, copies=True):
     g = torch.Generator(device="cuda").manual_seed(seed)
     def codes(r, pad):                                                                         # noqa: E306
         if extreme:
@@ -284,7 +284,7 @@ def check_product(rows, cin, cout, dtype, act, bias, residual, seed=0, x_pad=0, 
     res = matrix(rows, cout, dtype, seed + 1, out_pad) if residual else None
     out = torch.full((rows, cout + out_pad), 5.0, device="cuda", dtype=dtype)
     acc = (xc.double() @ wc.double().t()).cpu().numpy()                                        # exact: below 2^53
-    r = tr.linear_rows8(tr.Rows8(xc, sx), tr.Rows8(wc, sw), b, act, res, dtype, save_z8=True, save_y8=True, out=out[:, :cout] if out_pad else None)
+    r = tr.linear_rows8(tr.Rows8(xc, sx), tr.Rows8(wc, sw), b, act, res, dtype, save_z8=copies, save_y8=copies, out=out[:, :cout] if out_pad else None)
     product = acc * f64(sx)[:, None] * f64(sw)
     z = product + (0 if b is None else f64(b))
     z_off = 3 * U * np.abs(product) + U * np.abs(z)                                            # the integer's rounding and two scales; the bias
@@ -296,7 +296,9 @@ def check_product(rows, cin, cout, dtype, act, bias, residual, seed=0, x_pad=0, 
         y = y + f64(res)
         slack = slack + U * np.abs(y)
     near(r.y, y, dtype, slack)
-    assert (f64(out)[:, cout:] == 5).all()
+    assert (f64(out)[:, cout:] == 5).all() and tr.status() == 0
+    if not copies:
+        return
     z8 = f64(tr.unpack8(r.z8, torch.float32))
     groups = np.abs(np.pad(z, ((0, 0), (0, -cout % 32)))).reshape(rows, -1, 32).max(2)
     step = np.exp2(np.maximum(np.ceil(np.log2(np.maximum(groups * (1 + 8 * U), 1e-300) / 127.5)), -126))
@@ -304,7 +306,6 @@ def check_product(rows, cin, cout, dtype, act, bias, residual, seed=0, x_pad=0, 
     assert (np.abs(z8 - z) <= step / 2 + z_off * 2).all()
     want = tr.pack8(r.y)
     assert r.y8.codes.equal(want.codes) and r.y8.exps.equal(want.exps)
-    assert tr.status() == 0
 
 
 @pytest.mark.parametrize("rows,cin,cout", [
@@ -324,9 +325,18 @@ def test_linear_rows8_layouts(act, rows, cin, cout):
         check_product(rows, cin, cout, torch.float16, act, True, out_pad != 2, x_pad + 10 * w_pad, x_pad, w_pad, out_pad)
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("cin,cout", [(1, 1), (15, 3), (16, 4), (17, 33), (496, 5), (512, 1001), (4100, 7), (4096, 130), (40000, 9), (131071, 2), (520, 40000)])
+def test_linear_rows8_of_few_rows(rows, cin, cout):
+    """Without copies in 8 bits a few rows take a kernel of their own."""
+    check_product(rows, cin, cout, torch.bfloat16, "silu", True, rows != 2, seed=cin, copies=False)
+    check_product(rows, cin, cout, torch.float16, "none", rows == 3, False, seed=cout, out_pad=rows - 1, copies=False)
+
+
 def test_longest_and_largest_sums():
     """131071 products of 128 by 128: one short of leaving 32 bits."""
     check_product(3, 131071, 5, torch.bfloat16, "none", False, False, extreme=True)
+    check_product(3, 131071, 5, torch.bfloat16, "none", False, False, extreme=True, copies=False)
     check_product(300, 131071, 140, torch.float16, "none", True, False)
 
 
