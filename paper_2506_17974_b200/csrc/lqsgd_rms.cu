@@ -46,36 +46,30 @@ struct ForwardRow {
   // h = residual + dropout(x) of all runs, as it is stored
   template <int N>
   __device__ __forceinline__ void make_h(const Raw<DT, HOW> (&rx)[N], const Raw<DT, HOW> (&rr)[N], Piece<DT> (&ph)[N]) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) settle(rx[i], x, l, i, ph[i]);
+    settle(rx, x, l, ph);
     if (!a.h) return;
+    Piece<DT> pr[N];
+    if (a.residual) settle(rr, residual, l, pr);
     float v[kRun], r[kRun];
     if (a.drop.threshold) {
       uint4 bits[N];
       drop_bits(a.drop, room, block, bits);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        sum_of(i, rr[i], r);
+        clear_run(r);
+        if (a.residual) open_words<DT>(pr[i], r);
         open_words<DT>(ph[i], v);
         drop_run(a.drop, bits[i], v, r);
         close_words<DT>(r, ph[i]);
       }
-    } else {
+    } else if (a.residual) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        sum_of(i, rr[i], r);
+        open_words<DT>(pr[i], r);
         open_words<DT>(ph[i], v);
         add_run(r, r, v);
         close_words<DT>(r, ph[i]);
       }
-    }
-  }
-  __device__ __forceinline__ void sum_of(int i, const Raw<DT, HOW>& rr, float (&r)[kRun]) const {
-    clear_run(r);
-    if (a.residual) {
-      Piece<DT> t;
-      settle(rr, residual, l, i, t);
-      open_words<DT>(t, r);
     }
   }
   // squares into `sum`, the largest |h gamma| into `top`
@@ -100,25 +94,27 @@ struct ForwardRow {
       if (a.r8.dev_codes) a.r8.dev_scales[row] = scale;
     }
   }
-  // y of run i of N and the copies in 8 bits; py holds y as stored, of the run before when it comes
+  // y of all runs and the copies in 8 bits
   template <int N>
-  __device__ __forceinline__ void put_y(int i, float rstd, float inv, const Piece<DT>& ph, Piece<DT>& py) const {
-    float v[kRun], g[kRun];
-    open_words<DT>(ph, v);
-    fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
-    if (a.h8.dev_codes) put_packed_run<HOW>(a.h8.dev_codes + row * a.h8.ld_codes + l.col, a.h8.dev_exps + row * a.h8.ld_exps + l.col / kGroup, a.vec_h8, l, i, v);
-    mul_run(v, v, rstd);
-    mul_run(v, v, g);
-    if (a.r8.dev_codes) put_codes<HOW>(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + l.col, a.vec_r8, l, i, signed_codes(v, inv));
-    if (!a.y && !a.y8.dev_codes) return;
-    Piece<DT> p;
-    close_words<DT>(v, p);
-    if (a.y) put<DT, HOW, N>(y, l, i, p, py);
-    py = p;
-    if (a.y8.dev_codes) {
-      open_words<DT>(p, v);
-      put_packed_run<HOW>(a.y8.dev_codes + row * a.y8.ld_codes + l.col, a.y8.dev_exps + row * a.y8.ld_exps + l.col / kGroup, a.vec_y8, l, i, v);
+  __device__ __forceinline__ void put_y(float rstd, float inv, const Piece<DT> (&ph)[N]) const {
+    Piece<DT> py[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float v[kRun], g[kRun];
+      open_words<DT>(ph[i], v);
+      fetch_vector<HOW>(gamma, a.vec_gamma, l, i, g);
+      if (a.h8.dev_codes) put_packed_run<HOW>(a.h8.dev_codes + row * a.h8.ld_codes + l.col, a.h8.dev_exps + row * a.h8.ld_exps + l.col / kGroup, a.vec_h8, l, i, v);
+      mul_run(v, v, rstd);
+      mul_run(v, v, g);
+      if (a.r8.dev_codes) put_codes<HOW>(reinterpret_cast<uint8_t*>(a.r8.dev_codes) + row * a.r8.ld_codes + l.col, a.vec_r8, l, i, signed_codes(v, inv));
+      if (!a.y && !a.y8.dev_codes) continue;
+      close_words<DT>(v, py[i]);
+      if (a.y8.dev_codes) {
+        open_words<DT>(py[i], v);
+        put_packed_run<HOW>(a.y8.dev_codes + row * a.y8.ld_codes + l.col, a.y8.dev_exps + row * a.y8.ld_exps + l.col / kGroup, a.vec_y8, l, i, v);
+      }
     }
+    if (a.y) put(y, l, py);
   }
 };
 
@@ -134,26 +130,22 @@ rms_forward_kernel(const __grid_constant__ RmsArgs a) {
   Raw<DT, HOW> x[N], res[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
-  Piece<DT> h[N], y;
+  Piece<DT> h[N];
   float sum[2] = {0.f, 0.f}, top = 0.f, rstd, inv = 0.f;
   io.make_h(x, res, h);
-  if (a.h) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
-  }
+  if (a.h) put(io.h, io.l, h);
 #pragma unroll
   for (int i = 0; i < N; ++i) io.add_squares(i, h[i], sum, top);
   sum[0] += sum[1];
   if (a.r8.dev_codes) team.template join<true>(sum[0], top, slots);
   else team.template join<false>(sum[0], top, slots);
   io.figures(team.first(), sum[0], top, rstd, inv);
-#pragma unroll
-  for (int i = 0; i < N; ++i) io.template put_y<N>(i, rstd, inv, h[i], y);
+  io.put_y(rstd, inv, h);
 }
 
 // Rows longer than a block holds: h is computed (and stored) in a first pass and computed again, from L2, in a second.
 template <int DT, int N, int HOW>
-__global__ void __launch_bounds__(kLongThreads)
+__global__ void __launch_bounds__(kLongThreads, 2)
 rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
   __shared__ float2 slots[16];
   __shared__ uint32_t room[kDropRoom];
@@ -170,16 +162,14 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
       Raw<DT, HOW> x[N], res[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
-      Piece<DT> h[N], y;
+      Piece<DT> h[N];
       io.make_h(x, res, h);
+      if (pass == 0) {
+        if (a.h) put(io.h, io.l, h);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (pass == 0) {
-          if (a.h) put<DT, HOW, N>(io.h, io.l, i, h[i], h[i > 0 ? i - 1 : 0]);
-          io.add_squares(i, h[i], sum, top);
-        } else {
-          io.template put_y<N>(i, rstd, inv, h[i], y);
-        }
+        for (int i = 0; i < N; ++i) io.add_squares(i, h[i], sum, top);
+      } else {
+        io.put_y(rstd, inv, h);
       }
     }
     if (pass == 0) {
@@ -255,9 +245,7 @@ template <int DT, int HOW, int N>
 __device__ __forceinline__ void put_d(const RmsArgs& a, const uint32_t (&room)[kDropRoom], const BackwardRow<DT, HOW>& r, float (&d)[N][kRun]) {
   Piece<DT> out[N];
   auto write = [&](void* matrix, int64_t ld) {
-    const Cursor<DT, HOW> c(matrix, r.row * ld, r.l);
-#pragma unroll
-    for (int i = 0; i < N; ++i) put<DT, HOW, N>(c, r.l, i, out[i], out[i > 0 ? i - 1 : 0]);
+    put(Cursor<DT, HOW>(matrix, r.row * ld, r.l), r.l, out);
   };
   if (a.dresidual || !a.drop.threshold) {
 #pragma unroll
@@ -346,15 +334,10 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
           for (int k = 0; k < 4; ++k) h[i].w[k] = w[k];
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) settle(raw_h[i], r.h, r.l, i, h[i]);
+        settle(raw_h, r.h, r.l, h);
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) settle(raw_dy[i], r.dy, r.l, i, dy[i]);
-      if (a.skip) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) settle(raw_skip[i], r.skip, r.l, i, skip[i]);
-      }
+      settle(raw_dy, r.dy, r.l, dy);
+      if (a.skip) settle(raw_skip, r.skip, r.l, skip);
     }
     const float rstd = r.l.on ? a.rstd[row] : 0.f;
     float sum[2] = {0.f, 0.f}, none = 0.f;
@@ -438,17 +421,19 @@ struct GradRuns {
       for (int i = 0; i < N; ++i) fetch(r.skip, l, i, skip[i]);
     }
   }
-  __device__ __forceinline__ void open_dy_h(const RmsArgs& a, int i, float (&u)[kRun], float (&v)[kRun]) const {
-    Piece<DT> p;
-    settle(dy[i], r.dy, r.l, i, p);
-    open_words<DT>(p, u);
+  // dy and h as words (h from its 8-bit form as bf16: open_h)
+  __device__ __forceinline__ void settle_dy_h(const RmsArgs& a, Piece<DT> (&pd)[N], Piece<DT> (&ph)[N]) const {
+    settle(dy, r.dy, r.l, pd);
     if (a.h8.dev_codes) {
-      uint32_t w[4];
-      decode_bf16(codes[i], exps[i], w);
-      open_bf16(w, v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        uint32_t w[4];
+        decode_bf16(codes[i], exps[i], w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ph[i].w[k] = w[k];
+      }
     } else {
-      settle(h[i], r.h, r.l, i, p);
-      open_words<DT>(p, v);
+      settle(h, r.h, r.l, ph);
     }
   }
 };
@@ -463,10 +448,13 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
 #pragma unroll 1
   for (int k = 0; k < steps; ++k) {
     const GradRuns<DT, N, HOW> p(a, team.row, team.lanes(a.cols, true, k), false);
+    Piece<DT> dy[N], h[N];
+    p.settle_dy_h(a, dy, h);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float u[kRun], v[kRun], g[kRun];
-      p.open_dy_h(a, i, u, v);
+      open_words<DT>(dy[i], u);
+      open_h<DT>(a, h[i], v);
       fetch_vector<HOW>(a.gamma + p.r.l.col, a.vec_gamma, p.r.l, i, g);
       mul_run(u, u, v);
       dot_run(sum, u, g);
@@ -502,17 +490,17 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, co
     }
     const GradRuns<DT, N, HOW> p(a, row, l, true);
     const float rstd = a.rstd[row], k = rstd * rstd * (rstd * dots[row]);
+    Piece<DT> dy[N], h[N], skip[N];
+    p.settle_dy_h(a, dy, h);
+    if (a.skip) settle(p.skip, p.r.skip, l, skip);
     float d[N][kRun];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float u[kRun], v[kRun], g[kRun];
-      p.open_dy_h(a, i, u, v);
+      open_words<DT>(dy[i], u);
+      open_h<DT>(a, h[i], v);
       clear_run(d[i]);
-      if (a.skip) {
-        Piece<DT> t;
-        settle(p.skip[i], p.r.skip, l, i, t);
-        open_words<DT>(t, d[i]);
-      }
+      if (a.skip) open_words<DT>(skip[i], d[i]);
       fma_run(d[i], v, -k, d[i]);
       mul_run(v, v, u);
       fma_run(acc[i], v, rstd, acc[i]);

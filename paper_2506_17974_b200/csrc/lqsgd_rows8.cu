@@ -29,10 +29,10 @@ pack_rows8_kernel(const __grid_constant__ PackArgs a) {
   for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
   Piece<DT> p[N];
   float none = 0.f, top = 0.f;
+  settle(raw, x, l, p);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float v[kRun];
-    settle(raw[i], x, l, i, p[i]);
     open_words<DT>(p[i], v);
     top = largest(top, v);
   }
@@ -67,12 +67,12 @@ pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
       Raw<DT, HOW> raw[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
+      Piece<DT> p[N];
+      settle(raw, x, l, p);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        Piece<DT> p;
         float v[kRun];
-        settle(raw[i], x, l, i, p);
-        open_words<DT>(p, v);
+        open_words<DT>(p[i], v);
         if (pass == 0) top = largest(top, v);
         else put_codes<HOW>(codes_of(a.out, row, l.col), a.vec_c, l, i, signed_codes(v, inv));
       }
@@ -141,12 +141,12 @@ unpack_rows8_kernel(const __grid_constant__ Strips s, lqsgd_rows8 in, bool vec_c
         if (fabsf(v[j]) > kTop) v[j] = copysignf(kTop, v[j]);
     }
     close_words<DT>(v, p[i]);
-    put<DT, HOW, N>(out, l, i, p[i], p[i > 0 ? i - 1 : 0]);
   }
+  put(out, l, p);
 }
 
 template <int DT, int N, int HOW>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 dropout_kernel(const __grid_constant__ Strips s, const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const __grid_constant__ Drop drop, void* out, int64_t ld_o) {
   __shared__ uint32_t room[kDropRoom];
   const Strip<N> w(s);
@@ -161,24 +161,21 @@ dropout_kernel(const __grid_constant__ Strips s, const void* x, int64_t ld_x, co
     if (residual) fetch(cr, l, i, rr[i]);
   }
   const uint64_t block = (uint64_t)w.row * (uint32_t)((s.cols + kRun - 1) / kRun) + l.col / kRun;
-  Piece<DT> p[N];
+  Piece<DT> p[N], pr[N];
+  settle(rx, cx, l, p);
+  if (residual) settle(rr, cr, l, pr);
   uint4 bits[N];
   drop_bits(drop, room, block, bits);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float v[kRun], sum[kRun];
-    if (residual) {
-      settle(rr[i], cr, l, i, p[i]);
-      open_words<DT>(p[i], sum);
-    } else {
-      clear_run(sum);
-    }
-    settle(rx[i], cx, l, i, p[i]);
+    clear_run(sum);
+    if (residual) open_words<DT>(pr[i], sum);
     open_words<DT>(p[i], v);
     drop_run(drop, bits[i], v, sum);
     close_words<DT>(sum, p[i]);
-    put<DT, HOW, N>(co, l, i, p[i], p[i > 0 ? i - 1 : 0]);
   }
+  put(co, l, p);
 }
 
 template <int DT, int HOW>

@@ -229,7 +229,36 @@ struct Cursor {
   __device__ __forceinline__ char* at(int i) const { return p + i * (32 * kRunBytes<DT>); }
   __device__ __forceinline__ bool pieces(const Lanes& l, int i) const { return l.have(i) >= need && !(i == 0 && head); }
 };
-// A run as it is fetched: with kShift 16 bytes more.
+// N words that begin `shift` bytes into in, at any shift of a thread's own, and at one of Q words and `bits` bits.
+template <int N, int M>
+__device__ __forceinline__ void shift_words(const uint32_t (&in)[M], uint32_t shift, uint32_t (&out)[N]) {
+  static_assert(M >= N + 4, "room to shift");
+  uint32_t t[N + 3], u[N + 1];
+#pragma unroll
+  for (int k = 0; k < N + 3; ++k) t[k] = shift & 4 ? in[k + 1] : in[k];
+#pragma unroll
+  for (int k = 0; k < N + 1; ++k) u[k] = shift & 8 ? t[k + 2] : t[k];
+#pragma unroll
+  for (int k = 0; k < N; ++k) out[k] = __funnelshift_r(u[k], u[k + 1], (shift & 3) * 8);
+}
+template <int Q, int N, int M>
+__device__ __forceinline__ void shift_words_by(const uint32_t (&in)[M], uint32_t bits, uint32_t (&out)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) out[k] = __funnelshift_r(in[k + Q], in[k + Q + 1 < M ? k + Q + 1 : k + Q], bits);
+}
+// f with the number of whole words in a shift below 16 bytes as a constant.
+template <int Q> struct WordsTag { static constexpr int value = Q; };
+template <typename F>
+__device__ __forceinline__ void by_words(uint32_t shift, F&& f) {
+  switch (shift >> 2) {
+    case 0: f(WordsTag<0>()); break;
+    case 1: f(WordsTag<1>()); break;
+    case 2: f(WordsTag<2>()); break;
+    default: f(WordsTag<3>()); break;
+  }
+}
+
+// A run as it is fetched: with kShift 16 bytes more, the run beginning c.shift into them (at the row's ends one element to a word).
 template <int DT, int HOW>
 struct Raw {
   static constexpr int kPieces = kRunBytes<DT> / 16 + (HOW == kShift ? 1 : 0);
@@ -248,75 +277,116 @@ __device__ __forceinline__ void fetch(const Cursor<DT, HOW>& c, const Lanes& l, 
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
       if (k < kRunBytes<DT> / 16 || c.shift) reinterpret_cast<uint4*>(out.w)[k] = p[k];
-  } else {
+  } else if constexpr (HOW == kShift) {                       // the row's ends: an element to a word (nothing here waits for a load)
     const T* e = reinterpret_cast<const T*>(c.at(i) + c.shift);
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
-      if (j < l.have(i)) reinterpret_cast<T*>(out.w)[j] = e[j];
+      if (j < l.have(i)) {
+        if constexpr (DT == LQSGD_F32) out.w[j] = __float_as_uint(e[j]);
+        else out.w[j] = reinterpret_cast<const uint16_t*>(e)[j];
+      }
   }
 }
-// N words that begin `shift` bytes into in.
-template <int N, int M>
-__device__ __forceinline__ void shift_words(const uint32_t (&in)[M], uint32_t shift, bool halves, uint32_t (&out)[N]) {
-  static_assert(M >= N + 4, "room to shift");
-  uint32_t t[N + 3], u[N + 1];
+// A run at the row's ends as it is stored.
+template <int DT, int M>
+__device__ __forceinline__ void gather_words(const uint32_t (&in)[M], Piece<DT>& out) {
 #pragma unroll
-  for (int k = 0; k < N + 3; ++k) t[k] = shift & 4 ? in[k + 1] : in[k];
-#pragma unroll
-  for (int k = 0; k < N + 1; ++k) u[k] = shift & 8 ? t[k + 2] : t[k];
-#pragma unroll
-  for (int k = 0; k < N; ++k) out[k] = halves ? __funnelshift_r(u[k], u[k + 1], (shift & 3) * 8) : u[k];
+  for (int k = 0; k < kRunBytes<DT> / 4; ++k) {
+    if constexpr (DT == LQSGD_F32) out.w[k] = in[k];
+    else out.w[k] = in[2 * k] | (in[2 * k + 1] << 16);
+  }
 }
-// What fetch brought as run i.
-template <int DT, int HOW>
-__device__ __forceinline__ void settle(const Raw<DT, HOW>& in, const Cursor<DT, HOW>& c, const Lanes& l, int i, Piece<DT>& out) {
+// What fetch brought as a thread's N runs.  Where a warp holds one row the shift is the warp's.
+template <int DT, int HOW, int N>
+__device__ __forceinline__ void settle(const Raw<DT, HOW> (&in)[N], const Cursor<DT, HOW>& c, const Lanes& l, Piece<DT> (&out)[N]) {
   if constexpr (HOW == kWhole) {
 #pragma unroll
-    for (int k = 0; k < (int)(sizeof(out.w) / 4); ++k) out.w[k] = in.w[k];
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int k = 0; k < kRunBytes<DT> / 4; ++k) out[i].w[k] = in[i].w[k];
+  } else if (N > 1 || l.lanes == 32) {
+    by_words(__shfl_sync(0xffffffffu, c.shift, 0), [&](auto q) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        shift_words_by<decltype(q)::value>(in[i].w, (c.shift & 3) * 8, out[i].w);
+        if (!c.pieces(l, i)) gather_words<DT>(in[i].w, out[i]);
+      }
+    });
   } else {
-    shift_words(in.w, c.pieces(l, i) ? c.shift : 0u, DT != LQSGD_F32, out.w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      shift_words(in[i].w, c.shift, out[i].w);
+      if (!c.pieces(l, i)) gather_words<DT>(in[i].w, out[i]);
+    }
   }
 }
-// Writes run i of N.  With kShift the whole warp calls it, with the run before, `prev`, in hand (i > 0).
+// Writes a thread's N runs.  With kShift the whole warp calls it: a run is written as the 16-byte pieces that begin in the run in front, with
+// that run's end from the neighbouring lane.
 template <int DT, int HOW, int N>
-__device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, int i, const Piece<DT>& p, const Piece<DT>& prev) {
+__device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, const Piece<DT> (&p)[N]) {
   using T = typename Elem<DT>::T;
   constexpr int kWords = kRunBytes<DT> / 4;
-  const int have = l.have(i);
   if constexpr (HOW == kWhole) {
-    if (!l.has(i)) return;
-    uint4* o = reinterpret_cast<uint4*>(c.at(i));
 #pragma unroll
-    for (int k = 0; k < kWords / 4; ++k) o[k] = reinterpret_cast<const uint4*>(p.w)[k];
-  } else {
-    uint32_t both[kWords + 4];                                // the end of the run in front, this one
-    const int me = threadIdx.x & 31;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      both[k] = __shfl_sync(0xffffffffu, i > 0 && me == 31 ? prev.w[kWords - 4 + k] : p.w[kWords - 4 + k], (me + 31) & 31);
-#pragma unroll
-    for (int k = 0; k < kWords; ++k) both[4 + k] = p.w[k];
-    if (!l.has(i)) return;
-    const bool whole = have >= kRun && (l.lane > 0 || i > 0 || c.shift == 0), next = have >= 2 * kRun && (l.lane + 1 < l.lanes || i + 1 < N);
-    if (whole) {
-      uint32_t w[kWords];
-      // with shift 0 the run itself, 16 bytes in
-      if (c.shift) {
-        shift_words(both, 16 - c.shift, DT != LQSGD_F32, w);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) w[k] = p.w[k];
-      }
+    for (int i = 0; i < N; ++i) {
+      if (!l.has(i)) continue;
       uint4* o = reinterpret_cast<uint4*>(c.at(i));
 #pragma unroll
-      for (int k = 0; k < kWords / 4; ++k) o[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+      for (int k = 0; k < kWords / 4; ++k) o[k] = reinterpret_cast<const uint4*>(p[i].w)[k];
     }
-    if (!whole || (c.shift && !next)) {                       // what no piece holds: the ends of the row, of the warp's part of it
-      T* o = reinterpret_cast<T*>(c.at(i) + c.shift);
-      const int head = (kRunBytes<DT> - (int)c.shift) / (int)sizeof(T);
+  } else {
+    const int me = threadIdx.x & 31;
+    // run i as pieces in w; the ends of the row and of the warp's part of it element by element
+    auto write = [&](int i, const uint32_t (&w)[kWords]) {
+      const int have = l.have(i);
+      if (!l.has(i)) return;
+      const bool whole = have >= kRun && (l.lane > 0 || i > 0 || c.shift == 0), next = have >= 2 * kRun && (l.lane + 1 < l.lanes || i + 1 < N);
+      if (whole) {
+        uint4* o = reinterpret_cast<uint4*>(c.at(i));
 #pragma unroll
-      for (int j = 0; j < kRun; ++j)
-        if (j < have && (j < head ? !whole : !next)) o[j] = reinterpret_cast<const T*>(p.w)[j];
+        for (int k = 0; k < kWords / 4; ++k) o[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+      }
+      if (!whole || (c.shift && !next)) {
+        T* o = reinterpret_cast<T*>(c.at(i) + c.shift);
+        const int head = (kRunBytes<DT> - (int)c.shift) / (int)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < kRun; ++j)
+          if (j < have && (j < head ? !whole : !next)) o[j] = reinterpret_cast<const T*>(p[i].w)[j];
+      }
+    };
+    // the last FROM .. 3 of the four words in front of run i, and the run
+    auto both = [&](int i, int from, uint32_t (&b)[kWords + 4]) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        b[k] = k < from ? 0u : __shfl_sync(0xffffffffu, i > 0 && me == 31 ? p[i > 0 ? i - 1 : 0].w[kWords - 4 + k] : p[i].w[kWords - 4 + k], (me + 31) & 31);
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) b[4 + k] = p[i].w[k];
+    };
+    if (N > 1 || l.lanes == 32) {
+      const uint32_t shift = __shfl_sync(0xffffffffu, c.shift, 0);
+      if (shift == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) write(i, p[i].w);
+      } else {
+        by_words(16 - shift, [&](auto q) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            uint32_t b[kWords + 4], w[kWords];
+            both(i, decltype(q)::value, b);
+            shift_words_by<decltype(q)::value>(b, ((16 - shift) & 3) * 8, w);
+            write(i, w);
+          }
+        });
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        uint32_t b[kWords + 4], w[kWords];
+        both(i, 0, b);
+        shift_words(b, 16 - c.shift & 15, w);
+        if (c.shift) write(i, w);
+        else write(i, p[i].w);
+      }
     }
   }
 }
