@@ -149,8 +149,13 @@ __global__ void __launch_bounds__(kLongThreads, 2)
 rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
   __shared__ float2 slots[16];
   __shared__ uint32_t room[kDropRoom];
+  constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
   const Team<false, N> team(0);
   train_pdl_wait();
+  if (threadIdx.x == 0) {                                  // the whole row on its way: the first pass waits for its first step only
+    ahead(static_cast<const char*>(a.x) + team.row * a.ld_x * kSize, (int64_t)a.cols * kSize);
+    if (a.residual) ahead(static_cast<const char*>(a.residual) + team.row * a.ld_residual * kSize, (int64_t)a.cols * kSize);
+  }
   open_drop(a.drop, room);
   const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
   float sum[2] = {0.f, 0.f}, top = 0.f, rstd = 0.f, inv = 0.f;
@@ -267,18 +272,13 @@ __device__ __forceinline__ void put_d(const RmsArgs& a, const uint32_t (&room)[k
   write(a.dx, a.ld_dx);
 }
 
-// Asks L2 for the whole 16-byte pieces of `bytes` from p on: one instruction.
-__device__ __forceinline__ void ahead(const void* p, int64_t bytes) {
-  const uintptr_t from = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, to = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
-  if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(to - from)) : "memory");
-}
 // The rows that a team comes to next.
 template <int DT>
-__device__ __forceinline__ void rows_ahead(const RmsArgs& a, int64_t row) {
+__device__ __forceinline__ void rows_ahead(const RmsArgs& a, int64_t row, bool with_skip) {
   constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
   if (row >= a.rows) return;
   ahead(static_cast<const char*>(a.dy) + row * a.ld_dy * kSize, (int64_t)a.cols * kSize);
-  if (a.skip) ahead(static_cast<const char*>(a.skip) + row * a.ld_skip * kSize, (int64_t)a.cols * kSize);
+  if (with_skip && a.skip) ahead(static_cast<const char*>(a.skip) + row * a.ld_skip * kSize, (int64_t)a.cols * kSize);
   if (a.h8.dev_codes) ahead(a.h8.dev_codes + row * a.h8.ld_codes, a.cols);
   else ahead(static_cast<const char*>(a.h) + row * a.ld_h * kSize, (int64_t)a.cols * kSize);
 }
@@ -301,7 +301,7 @@ rms_backward_kernel(const __grid_constant__ RmsArgs a) {
 #pragma unroll 1
   for (int64_t r0 = first; r0 < a.rows; r0 += team.rows_per_grid) {
     const int64_t row = team.row + (r0 - first);
-    if (!NARROW && threadIdx.x == 0) rows_ahead<DT>(a, row + team.rows_per_grid);
+    if (!NARROW && threadIdx.x == 0) rows_ahead<DT>(a, row + team.rows_per_grid, true);
     const BackwardRow<DT, HOW> r(a, row, team.lanes(a.cols, row < a.rows));
     const float* gamma = a.gamma + r.l.col;
     Piece<DT> dy[N], h[N], skip[N];
@@ -443,6 +443,7 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   __shared__ float2 slots[16];
   const Team<false, N> team(0);
   train_pdl_wait();
+  if (threadIdx.x == 0) rows_ahead<DT>(a, team.row, false);
   float sum[2] = {0.f, 0.f}, top = 0.f;
   const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
 #pragma unroll 1

@@ -56,6 +56,7 @@ pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
   const Team<false, N> team(0);
   const int64_t row = team.row;
   train_pdl_wait();
+  if (threadIdx.x == 0) ahead(static_cast<const typename Elem<DT>::T*>(a.x) + row * a.ld_x, (int64_t)a.cols * (int)sizeof(typename Elem<DT>::T));
   const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
   float none = 0.f, top = 0.f, scale, inv = 0.f;
 #pragma unroll 1

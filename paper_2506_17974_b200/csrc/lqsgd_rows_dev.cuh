@@ -423,6 +423,12 @@ __device__ __forceinline__ void put_packed_run(uint8_t* codes, uint8_t* exps, bo
   if (l.has(i) && (l.lane & 3) == 0) exps[i * (kWarpCols / kGroup)] = (uint8_t)eb;
 }
 
+// Asks L2 for the whole 16-byte pieces of `bytes` from p on: one instruction.
+__device__ __forceinline__ void ahead(const void* p, int64_t bytes) {
+  const uintptr_t from = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, to = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
+  if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(to - from)) : "memory");
+}
+
 // ---- a row and its threads
 // NARROW: 4, 8, 16 or 32 lanes of a warp hold a row, a block of 256 threads several rows.  Otherwise a block holds one.  A warp's columns lie
 // side by side.  N runs per thread (one where fewer than 32 lanes hold a row).
