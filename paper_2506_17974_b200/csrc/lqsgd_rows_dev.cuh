@@ -31,7 +31,8 @@ namespace {
 //   kShift  any alignment.  A run is taken from the 16-byte pieces around it, which lie inside the row for all but its first and last
 //           runs, and moved into place in registers; it is written as the piece that begins in the run of the lane in front.  Element by
 //           element a run would touch as many places as it has elements; turned in shared memory, as the 8-bit streams do it, a
-//           row of 16-bit values still goes through 2-byte accesses.
+//           row of 16-bit values still goes through 2-byte accesses (the norm of 1021 x 25087 fp16 into codes: 87 us element by element or
+//           turned, 73 so; rows of 25088 46).
 enum RowAccess { kWhole = 0, kShift = 1 };
 
 // Philox4x32, 10 rounds: a product of each even word by a constant, its high half mixed with a neighbour and the round's key.
@@ -143,7 +144,7 @@ __device__ __forceinline__ void row_scale(float top, float& scale, float& inv) {
   scale = finite ? fmaxf(__fdiv_rn(top, 127.f), kRowStepLow) : __uint_as_float(0x7fc00000u);
   inv = finite ? fminf(__fdiv_rn(127.f, top), kRowInvHigh) : 0.f;
 }
-// Eight codes rint(v inv): adding 1.5 * 2^23 to the rounded product leaves an integer in two's complement below.  v inv is rounded by
+// Eight codes rint(v inv), |v inv| <= 127 (1 + 2^-23): adding 1.5 * 2^23 to the rounded product leaves an integer in two's complement below.  v inv is rounded by
 // itself, as the definition has it (one at a time: of two at a time, product and sum come out fused).
 __device__ __forceinline__ uint2 signed_codes(const float (&v)[kRun], float inv) {
   float t[kRun];
@@ -207,13 +208,9 @@ struct Cursor {
   uint32_t shift;
   int need;
   bool head;
-  Cursor() = default;
-  __device__ __forceinline__ Cursor(const void* matrix, int64_t at, const Lanes& l)
-      : Cursor(static_cast<const char*>(matrix) + (at + l.col) * (int64_t)sizeof(typename Elem<DT>::T), l) {}
-  // from the address of the thread's first run
-  __device__ __forceinline__ Cursor(const char* run, const Lanes& l) {
+  __device__ __forceinline__ Cursor(const void* matrix, int64_t at, const Lanes& l) {
     constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
-    p = const_cast<char*>(run);
+    p = static_cast<char*>(const_cast<void*>(matrix)) + (at + l.col) * kSize;
     shift = 0;
     need = kRun;
     head = false;

@@ -933,6 +933,9 @@ class _LinearRows8Layer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, act, rows8, weight8, recording):
         _dtype(x, "x", True)
+        for p, t, what in ((rows8, x, "rows8"), (weight8, weight, "weight8")):
+            if p is not None and p.shape != t.shape:
+                raise ValueError(f"{what} must be the Rows8 form of {tuple(t.shape)} values, not of {tuple(p.shape)}")
         for_x, for_w, for_bias = (n and recording for n in ctx.needs_input_grad[:3])
         x8 = pack_rows8(_apart(x)) if rows8 is None else rows8
         w8 = pack_rows8(_apart(weight.detach())) if weight8 is None else weight8

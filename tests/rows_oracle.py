@@ -20,10 +20,10 @@ def threshold(p):
     return min(int(np.rint(65536 * np.float64(np.float32(p)))), 65535)
 
 
-def kept(rows, cols, p, seed, offset):
-    """Which values dropout keeps, bool rows x cols."""
+def kept(rows, cols, p, seed, offset, row0=0):
+    """Which values dropout keeps, bool rows x cols, from row row0 on."""
     blocks = (cols + 7) // 8
-    b = np.arange(rows * blocks, dtype=np.uint64)
+    b = np.arange(row0 * blocks, (row0 + rows) * blocks, dtype=np.uint64)
     low, seed, offset = np.uint64(LOW), seed % 2 ** 64, offset % 2 ** 64
     c = [b & low, b >> np.uint64(32), np.full_like(b, offset & LOW), np.full_like(b, offset >> 32)]
     k0, k1 = seed & LOW, seed >> 32

@@ -361,6 +361,49 @@ def test_product_of_kept_rows_is_near_the_real_one():
 
 # ----------------------------------------------------------------------------------------------------- calls and refusals
 
+def test_matrices_of_more_than_2_to_the_31_values():
+    """Rows whose offsets pass 32 bits: the last rows of a large matrix against the same rows by themselves."""
+    rows, cols = 53700, 40001                                   # 2.148e9 values; every row starts elsewhere in 16 bytes
+    x = torch.empty(rows, cols, device="cuda", dtype=torch.bfloat16)
+    x.copy_(torch.randn(1, cols, device="cuda") * torch.linspace(1, 2, rows, device="cuda")[:, None])
+    last, gamma = x[-3:].clone(), torch.ones(cols, device="cuda")
+    y = tr.dropout(x, 0.5, 3)
+    assert ((f64(y[-3:]) != 0) == (ro.kept(3, cols, 0.5, 3, 0, rows - 3) & (f64(last) != 0))).all()
+    del y
+    r, want = tr.rms_norm(x, gamma), tr.rms_norm(last, gamma)
+    assert r.y[-3:].equal(want.y) and r.rstd[-3:].equal(want.rstd)
+    dx, _, dgamma = tr.rms_norm_grad(r.y, x, gamma, r.rstd)
+    assert dx[-3:].equal(tr.rms_norm_grad(want.y, last, gamma, want.rstd)[0])
+    xh = x[::4000].double() * r.rstd[::4000].double()[:, None]   # gamma = 1: dgamma = the sum over rows of y xh, rows nearly alike
+    assert ((dgamma.double() / rows - (xh * xh).mean(0)).abs() <= 0.02 * (xh * xh).mean(0) + 1e-6).all()
+    del r, dx
+    p, want = tr.pack_rows8(x), tr.pack_rows8(last)
+    assert p.codes[-3:].equal(want.codes) and p.scales[-3:].equal(want.scales)
+    assert tr.unpack_rows8(p)[-3:].equal(tr.unpack_rows8(want))
+
+
+def test_largest_kept_values():
+    """h near the end of fp32's range, kept in 8 bits: the gradient reads what unpack8 gives in bfloat16."""
+    h = torch.zeros(2, 96, device="cuda")
+    h[0, :40], h[1, 50] = torch.finfo(torch.float32).max, -3e38
+    h8, gamma, rstd = tr.pack8(h), torch.ones(96, device="cuda"), torch.full((2,), 1e-38, device="cuda")
+    dy = matrix(2, 96, torch.float32, 1)
+    got, want = (tr.rms_norm_grad(dy, t, gamma, rstd) for t in (h8, tr.unpack8(h8, torch.bfloat16).float()))
+    # a sum of such rows' products may pass fp32's range (then NaN in both); xh = h rstd, of size 1, and dgamma do not
+    assert all(torch.allclose(a, b, rtol=0, atol=0, equal_nan=True) for a, b in zip(got, want)) and torch.isfinite(got[2]).all()
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-18, 1e15, 1e30])
+@pytest.mark.parametrize("cols", [40, 1100, 9000])
+def test_rms_norm_grad_of_rows_of_any_size(size, cols):
+    """Without eps the norm does not see a row's size, and its gradient is divided by it."""
+    h, dy, gamma = matrix(4, cols, torch.float32, 1), matrix(4, cols, torch.float32, 2), torch.ones(cols, device="cuda")
+    rstd = (1 / h.double().square().mean(1).sqrt()).float()
+    dx, _, dgamma = tr.rms_norm_grad(dy, h * size, gamma, rstd / size)
+    want, wantg = ro.rms_grad(f64(dy), f64(h * size), np.ones(cols), f64(rstd / size))
+    assert np.linalg.norm(f64(dx) - want) < 1e-5 * np.linalg.norm(want) and np.linalg.norm(f64(dgamma) - wantg) < 1e-5 * np.linalg.norm(wantg)
+
+
 def test_refusals():
     x, gamma = matrix(4, 64, torch.bfloat16, 1), torch.ones(64, device="cuda")
     x8, w8 = tr.pack_rows8(x), tr.pack_rows8(matrix(8, 64, torch.float32, 2))
