@@ -263,19 +263,27 @@ __device__ __forceinline__ void st_row32(void* p, int vec, const uint32_t (&w)[8
 }
 
 // Eight-bit form of 32 values of one row in one thread (those from `have` on must be 0): the exponent byte and 8 code words.
+template <int KIND>
 __device__ __forceinline__ int encode32(const float (&v)[32], uint32_t (&w)[8]) {
-  uint32_t top = 0;
+  float most = 0.f;
+  if (KIND == kInt8) {
+    most = largest(0.f, v);
+  } else {
+    uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-  const int eb = exp_byte(__uint_as_float(top));
+    for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    most = __uint_as_float(top);
+  }
+  const int eb = exp_byte(most);
   const float inv = inv_step(eb);
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = code_word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
   return eb;
 }
+template <int KIND>
 __device__ __forceinline__ void put_packed(const lqsgd_packed8& p, int vec, int64_t row, int col, int have, const float (&v)[32]) {
   uint32_t w[8];
-  const int eb = encode32(v, w);
+  const int eb = encode32<KIND>(v, w);
   uint8_t* c = p.dev_codes + row * p.ld_codes + col;
   if (vec && have == 32) {
     st_row32(c, vec, w);
@@ -317,6 +325,8 @@ __device__ __forceinline__ float add_sums(float a, float b) {
 }
 // Epilogue of a 32 x 32 piece of a layer's output.
 // bias: these columns' values in shared memory (zeros past the matrix).
+// Products of codes take half the time of those in 16 bits, so that their epilogue is what a tile waits for: it goes two values at a time.
+template <int KIND>
 __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], const float* bias, float* scratch) {
   const int lane = threadIdx.x & 31;
   const int have = min(32, e.cols - col);
@@ -349,7 +359,12 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float4 b = *(reinterpret_cast<const float4*>(bias) + i);
-      v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
+      if (KIND == kInt8) {
+        add2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], b.x, b.y);
+        add2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], b.z, b.w);
+      } else {
+        v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
+      }
     }
   }
   if (have < 32) {
@@ -357,8 +372,9 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
     for (int i = 0; i < 32; ++i)
       if (i >= have) v[i] = 0.f;
   }
-  if (e.z8.dev_codes && on) put_packed(e.z8, e.vec_z8, row, col, have, v);
-  act_run(e.act, v);
+  if (e.z8.dev_codes && on) put_packed<KIND>(e.z8, e.vec_z8, row, col, have, v);
+  if (KIND == kInt8) act_pairs(e.act, v);
+  else act_run(e.act, v);
   if (res_rows && on) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -416,7 +432,7 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
       v[2 * i] = f.x;
       v[2 * i + 1] = f.y;
     }
-    put_packed(e.y8, e.vec_y8, row, col, have, v);
+    put_packed<KIND>(e.y8, e.vec_y8, row, col, have, v);
   }
 }
 
@@ -894,13 +910,15 @@ linear_kernel(const __grid_constant__ LinProblem p) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const float4 t = *(reinterpret_cast<const float4*>(col_scale + c) + i);
-                v[4 * i] = scaled_sum(v[4 * i], row_scale, t.x);
-                v[4 * i + 1] = scaled_sum(v[4 * i + 1], row_scale, t.y);
-                v[4 * i + 2] = scaled_sum(v[4 * i + 2], row_scale, t.z);
-                v[4 * i + 3] = scaled_sum(v[4 * i + 3], row_scale, t.w);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * i + j] = (float)__float_as_int(v[4 * i + j]);
+                mul2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], row_scale, row_scale);
+                mul2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], row_scale, row_scale);
+                mul2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], t.x, t.y);
+                mul2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], t.z, t.w);
               }
             }
-            finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
+            finish_rows<KIND>(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
           }
           __syncwarp();
         }
@@ -959,7 +977,7 @@ linear_kernel(const __grid_constant__ LinProblem p) {
             for (int j = 0; j < 32; ++j) v[j] = acc[j];
 #pragma unroll
             for (int j = 32; j < S::kMine; ++j) acc[j - 32] = acc[j];      // the next piece's: one copy of the epilogue's code, registers by number
-            if (n0 + c0 + c < p.N && m - lane < p.M) finish_rows(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
+            if (n0 + c0 + c < p.N && m - lane < p.M) finish_rows<KIND>(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);
             __syncwarp();
           }
         }

@@ -84,19 +84,7 @@ __device__ __forceinline__ void drop_run(const Drop& d, const uint4& bits, const
   }
 }
 
-// ---- arithmetic on two values at a time (one instruction for both; each rounded by itself)
-__device__ __forceinline__ void fma2(float& a0, float& a1, float b0, float b1, float c0, float c1, float d0, float d1) {
-  asm("{\n .reg .b64 b, c, d;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mov.b64 d, {%6, %7};\n fma.rn.f32x2 d, b, c, d;\n mov.b64 {%0, %1}, d;\n}"
-      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1), "f"(d0), "f"(d1));
-}
-__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
-  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mul.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
-      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
-}
-__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
-  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n add.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
-      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
-}
+// ---- arithmetic on runs, two values at a time
 // a = b c + d and the like, of a run
 __device__ __forceinline__ void fma_run(float (&a)[kRun], const float (&b)[kRun], const float (&c)[kRun], const float (&d)[kRun]) {
 #pragma unroll
@@ -126,14 +114,6 @@ __device__ __forceinline__ void clear_run(float (&a)[kRun]) {
 __device__ __forceinline__ void dot_run(float (&sum)[2], const float (&b)[kRun], const float (&c)[kRun]) {
 #pragma unroll
   for (int j = 0; j < kRun; j += 2) fma2(sum[0], sum[1], b[j], b[j + 1], c[j], c[j + 1], sum[0], sum[1]);
-}
-
-// ---- largest magnitudes; an infinity or a NaN comes out as one
-__device__ __forceinline__ float larger(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float largest(float top, const float (&v)[kRun]) {
-#pragma unroll
-  for (int j = 0; j < kRun; j += 2) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(top) : "f"(top), "f"(v[j]), "f"(v[j + 1]));
-  return top;
 }
 
 // ---- rows of signed 8-bit codes

@@ -117,6 +117,29 @@ __device__ __forceinline__ void store_run(typename Elem<DT>::T* p, bool vec, int
       if (j < have) p[j] = E::down(v[j]);
   }
 }
+// ---- arithmetic on two values at a time (one instruction for both; each rounded by itself)
+__device__ __forceinline__ void fma2(float& a0, float& a1, float b0, float b1, float c0, float c1, float d0, float d1) {
+  asm("{\n .reg .b64 b, c, d;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mov.b64 d, {%6, %7};\n fma.rn.f32x2 d, b, c, d;\n mov.b64 {%0, %1}, d;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1), "f"(d0), "f"(d1));
+}
+__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
+  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n mul.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1, float c0, float c1) {
+  asm("{\n .reg .b64 b, c;\n mov.b64 b, {%2, %3};\n mov.b64 c, {%4, %5};\n add.rn.f32x2 b, b, c;\n mov.b64 {%0, %1}, b;\n}"
+      : "=f"(a0), "=f"(a1) : "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
+// ---- largest magnitudes; an infinity or a NaN comes out as one
+__device__ __forceinline__ float larger(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+template <int N>
+__device__ __forceinline__ float largest(float top, const float (&v)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; j += 2) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(top) : "f"(top), "f"(v[j]), "f"(v[j + 1]));
+  return top;
+}
+
 // Rounds to the element type and back: the value a later reader of the stored output sees.
 template <int DT> __device__ __forceinline__ float as_stored(float v) { return Elem<DT>::up(Elem<DT>::down(v)); }
 
@@ -233,6 +256,49 @@ __device__ __forceinline__ void act_run(int act, float (&v)[N]) {
   } else if (act == LQSGD_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = act_value<LQSGD_ACT_SILU>(v[i]);
+  }
+}
+// The same two values at a time: where a product is over sooner than its epilogue.
+__device__ __forceinline__ void gelu2(float& z0, float& z1) {
+  float t0, t1, r0, r1, g0, g1;
+  fma2(t0, t1, fabsf(z0), fabsf(z1), 0.30476302f, 0.30476302f, 1.f, 1.f);
+  t0 = rcp_approx(t0);
+  t1 = rcp_approx(t1);
+  fma2(r0, r1, t0, t1, 0.036738604f, 0.036738604f, -0.15354006f, -0.15354006f);
+  fma2(r0, r1, r0, r1, t0, t1, 0.18724863f, 0.18724863f);
+  fma2(r0, r1, r0, r1, t0, t1, -0.039188605f, -0.039188605f);
+  fma2(r0, r1, r0, r1, t0, t1, 0.12161422f, 0.12161422f);
+  fma2(r0, r1, r0, r1, t0, t1, 0.10318742f, 0.10318742f);
+  fma2(r0, r1, r0, r1, t0, t1, 0.12239605f, 0.12239605f);
+  fma2(r0, r1, r0, r1, t0, t1, 0.12154379f, 0.12154379f);
+  mul2(r0, r1, r0, r1, t0, t1);
+  mul2(g0, g1, z0, z1, z0, z1);
+  mul2(g0, g1, g0, g1, -0.72134752f, -0.72134752f);
+  g0 = exp2_approx(g0);
+  g1 = exp2_approx(g1);
+  // z (z < 0 ? q : 1 - q), q = gauss r: max(z, 0) - |z| q (q is 0 from 14 on, and infinity counts as the largest value there)
+  mul2(r0, r1, r0, r1, g0, g1);
+  fma2(z0, z1, -fminf(fabsf(z0), 3.402823466e38f), -fminf(fabsf(z1), 3.402823466e38f), r0, r1, act_value<LQSGD_ACT_RELU>(z0), act_value<LQSGD_ACT_RELU>(z1));
+}
+__device__ __forceinline__ void silu2(float& z0, float& z1) {
+  float e0, e1;
+  mul2(e0, e1, z0, z1, -1.44269504f, -1.44269504f);
+  e0 = exp2_approx(e0);
+  e1 = exp2_approx(e1);
+  add2(e0, e1, e0, e1, 1.f, 1.f);
+  mul2(z0, z1, z0, z1, rcp_approx(e0), rcp_approx(e1));
+}
+template <int N>
+__device__ __forceinline__ void act_pairs(int act, float (&v)[N]) {
+  if (act == LQSGD_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_value<LQSGD_ACT_RELU>(v[i]);
+  } else if (act == LQSGD_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) gelu2(v[i], v[i + 1]);
+  } else if (act == LQSGD_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) silu2(v[i], v[i + 1]);
   }
 }
 template <int N>

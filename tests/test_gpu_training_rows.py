@@ -351,6 +351,20 @@ def test_rows_that_are_not_finite():
     assert (r.z8.exps[bad] == 255).all()
 
 
+@pytest.mark.parametrize("rows", [1, 40, 600])
+def test_sums_that_leave_the_range(rows):
+    """Scales that carry a sum past fp32's range: infinity through every activation, nothing through those that cut negative values."""
+    codes = torch.ones(rows, 64, dtype=torch.int8, device="cuda")
+    w = torch.ones(300, 64, dtype=torch.int8, device="cuda")
+    w[::2] = -1
+    x8, w8 = tr.Rows8(codes, torch.full((rows,), 1e30, device="cuda")), tr.Rows8(w, torch.full((300,), 1e30, device="cuda"))
+    for act in ("none", "relu", "gelu", "silu"):
+        y = tr.linear_rows8(x8, w8, act=act).y
+        assert (y[:, 1::2] == float("inf")).all()
+        if act in ("relu", "none"):
+            assert (y[:, ::2] == (0 if act == "relu" else -float("inf"))).all()
+
+
 def test_product_of_kept_rows_is_near_the_real_one():
     """x and w to codes and their product, against the product of the values that the codes stand for."""
     x, w = matrix(65, 700, torch.bfloat16, 1), matrix(90, 700, torch.float32, 2, scale=700 ** -0.5)
