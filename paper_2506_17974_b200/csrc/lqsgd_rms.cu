@@ -27,7 +27,7 @@ struct RmsArgs {
   float eps, per_col;                        // 1 / cols
   bool vec_gamma, vec_h8, vec_y8, vec_r8;    // on 16 bytes; rows of 8-bit copies on 8
 };
-constexpr int kForwardThreads = 256, kLongThreads = 256, kGradThreads = 512, kGradRuns = 2;
+constexpr int kForwardThreads = 416, kLongThreads = 256, kGradThreads = 512, kGradRuns = 2;
 
 // What a thread touches of one row of the forward call.
 template <int DT, int HOW>
@@ -146,7 +146,7 @@ rms_forward_kernel(const __grid_constant__ RmsArgs a) {
   io.put_y(rstd, inv, h);
 }
 
-// Rows longer than a block holds: h is computed (and stored) in a first pass and computed again, from L2, in a second.
+// Rows longer than a block holds: h is computed (and stored) in a first pass and read again, from L2, in a second.
 template <int DT, int N, int HOW>
 __global__ void __launch_bounds__(kLongThreads, 2)
 rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
@@ -167,16 +167,21 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
 #pragma unroll 1
     for (int k = 0; k < steps; ++k) {
       const ForwardRow<DT, HOW> io(a, room, team.row, team.lanes(a.cols, true, k));
-      Raw<DT, HOW> x[N], res[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
       Piece<DT> h[N];
-      io.make_h(x, res, h);
       if (pass == 0) {
+        Raw<DT, HOW> x[N], res[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) io.ask(i, x[i], res[i]);
+        io.make_h(x, res, h);
         if (a.h) put(io.h, io.l, h);
 #pragma unroll
         for (int i = 0; i < N; ++i) io.add_squares(i, h[i], sum, top);
-      } else {
+      } else {                                               // what other threads of the block wrote of it lies behind the sum's barrier
+        const Cursor<DT, HOW>& from = a.h ? io.h : io.x;
+        Raw<DT, HOW> raw[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(from, io.l, i, raw[i]);
+        settle(raw, from, io.l, h);
         io.put_y(rstd, inv, h);
       }
     }
@@ -549,11 +554,14 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, co
 
 // ---- choice of kernel
 constexpr int kSms = 148;
-// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type).
-constexpr int kNarrow = 1024;
+// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type), and blocks of as many threads as leave registers for a second block on
+// an SM, which loads while the first one waits for its sum (16384 columns of bf16 in one block of 512: 82 us at 4000 rows, read twice 60; 12000 with
+// everything in two blocks of 384: 50 at 2000 rows, read twice 71).
+constexpr int kNarrow = 1024, kForwardThreadsShift = 320;
 template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
-RowShape forward_shape(const lqsgd_rms_norm& a) {
-  return shape_of(a.cols, a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow, kForwardThreads);
+RowShape forward_shape(const lqsgd_rms_norm& a, int how) {
+  return shape_of(a.cols, a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow,
+                  how == kWhole || a.dtype == LQSGD_F32 ? kForwardThreads : kForwardThreadsShift);
 }
 constexpr int kCtasColumns = kSms * 2;
 struct GradPlan {
@@ -666,7 +674,7 @@ extern "C" int lqsgd_rms_norm_forward(const lqsgd_rms_norm* a, void* cuda_stream
   k.vec_y8 = on8(a->y8.dev_codes, a->y8.ld_codes, a->rows);
   k.vec_r8 = on8(a->rows8.dev_codes, a->rows8.ld_codes, a->rows);
   const int how = access_of(rows16, k.vec_gamma && k.vec_h8 && k.vec_y8 && k.vec_r8, a->cols);
-  const RowShape s = forward_shape(*a);
+  const RowShape s = forward_shape(*a, how);
   k.lane_shift = s.lane_shift;
   TRAIN_CK(BY_TYPE(a->dtype, how, launch_forward, s, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
   return LQSGD_OK;
