@@ -4,10 +4,10 @@
 // instructions: random bits, two 8-bit forms and the sum cost 350 a run of 8 columns, where HBM leaves time for 330.  So a row's values are
 // read once and stay in registers, as they are stored, while its threads agree on the sum; the steps of a thread's runs interleave
 // without branches between them; and arithmetic goes two values to an instruction.
-// Rows of up to 1024 columns (512 backward) are held by 4 to 32 lanes of a warp, those of up to 8192 (fp32: 4096 forward) by a block; longer ones are
-// read twice, the second time from L2.
-// Measured, 8192 x 4096 bf16: norm alone 28 us (4.7 TB/s), with a residual 43 (6.2 TB/s), with dropout, residual and both kept copies 59 (5.7 TB/s);
-// its gradient with skip 61 (4.4 TB/s), with dropout from 8-bit h 82 (3.7 TB/s).
+// Rows of up to 1024 columns (512 backward) are held by 4 to 32 lanes of a warp, longer ones by a block: forward up to 13312 columns (10240 at any
+// alignment; fp32 6656), backward up to 8192.  Rows beyond are read twice, the second time from L2.
+// Measured, 8192 x 4096 bf16: norm alone 27 us (5.0 TB/s), with a residual 43 (6.2 TB/s), with dropout, residual and both kept copies 57 (6.0 TB/s);
+// its gradient with skip 58 (4.7 TB/s), with dropout from 8-bit h 80 (3.7 TB/s).
 #include "lqsgd_rows_dev.cuh"
 
 namespace lqsgd {
@@ -27,7 +27,14 @@ struct RmsArgs {
   float eps, per_col;                        // 1 / cols
   bool vec_gamma, vec_h8, vec_y8, vec_r8;    // on 16 bytes; rows of 8-bit copies on 8
 };
-constexpr int kForwardThreads = 416, kLongThreads = 256, kGradThreads = 512, kGradRuns = 2;
+// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type), and blocks of as many threads as leave registers for a second block on
+// an SM, which loads while the first one waits for its sum (16384 columns of bf16 in one block of 512: 82 us at 4000 rows, read twice 60; 12000 with
+// everything in two blocks of 384: 50 at 2000 rows, read twice 71).
+constexpr int kNarrow = 1024, kForwardThreads = 416;
+template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
+template <int DT> constexpr int kLongRuns = DT == LQSGD_F32 ? 1 : 2;     // rows in steps: twice the threads in their place (four runs, balanced: 75 us to 58)
+constexpr int forward_threads(int dtype, int how) { return how == kWhole || dtype == LQSGD_F32 ? kForwardThreads : 320; }
+constexpr int kLongThreads = 448, kDotThreads = 256, kGradThreads = 512, kGradRuns = 2;
 
 // What a thread touches of one row of the forward call.
 template <int DT, int HOW>
@@ -160,7 +167,7 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
     if (a.residual) ahead(static_cast<const char*>(a.residual) + team.row * a.ld_residual * kSize, (int64_t)a.cols * kSize);
   }
   open_drop(a.drop, room);
-  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
+  const int each = blockDim.x * N * kRun, steps = (a.cols + each - 1) / each;
   float sum[2] = {0.f, 0.f}, top = 0.f, rstd = 0.f, inv = 0.f;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
@@ -197,7 +204,7 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
 // A row needs <u xh>, xh = h rstd, and then d = (gamma rstd) dy - (rstd <u xh>) xh + skip.  (With h itself in the place of xh a run takes 8
 // multiplications less, but products of very large or small rows leave fp32's range on the way.)
 // A team walks rows: loads of all runs, the sum, stores; its columns' sums for dgamma stay in registers.  That leaves 16 warps an SM, too few to
-// hide HBM's latency, so one thread asks L2 for the next row meanwhile (8192 x 4096 without dropout 75 -> 61 us, fp32 136 -> 122).  h from its
+// hide HBM's latency, so one thread asks L2 for the next row meanwhile (8192 x 4096 without dropout, at that step, 75 -> 61 us, fp32 136 -> 122).  h from its
 // 8-bit form is decoded once, to bf16, in which it is exact.
 // Eight codes as bf16: |128 + m| with the magnitude m below is a bf16 number (0x4300 | m), and (128 + m) 2^e - 128 2^e is m 2^e exactly; the
 // signs are put on top.  For exponents from kQuickByte on 128 2^e leaves the range.
@@ -460,7 +467,7 @@ struct GradRuns {
   }
 };
 template <int DT, int N, int HOW>
-__global__ void __launch_bounds__(kLongThreads)
+__global__ void __launch_bounds__(kDotThreads)
 rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   __shared__ float2 slots[16];
   const Team<false, N> team(0);
@@ -468,7 +475,7 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   if (threadIdx.x == 0) rows_ahead<DT>(a, team.row, false);
   const float rstd = a.rstd[team.row];
   float sum[2] = {0.f, 0.f}, top = 0.f;
-  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
+  const int steps = (a.cols + kDotThreads * N * kRun - 1) / (kDotThreads * N * kRun);
 #pragma unroll 1
   for (int k = 0; k < steps; ++k) {
     const GradRuns<DT, N, HOW> p(a, team.row, team.lanes(a.cols, true, k), false);
@@ -554,15 +561,6 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, co
 
 // ---- choice of kernel
 constexpr int kSms = 148;
-// Forward: 64 bytes of each matrix per thread (4 runs of a 16-bit type), and blocks of as many threads as leave registers for a second block on
-// an SM, which loads while the first one waits for its sum (16384 columns of bf16 in one block of 512: 82 us at 4000 rows, read twice 60; 12000 with
-// everything in two blocks of 384: 50 at 2000 rows, read twice 71).
-constexpr int kNarrow = 1024, kForwardThreadsShift = 320;
-template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
-RowShape forward_shape(const lqsgd_rms_norm& a, int how) {
-  return shape_of(a.cols, a.dtype == LQSGD_F32 ? kForwardRuns<LQSGD_F32> : kForwardRuns<LQSGD_BF16>, kNarrow,
-                  how == kWhole || a.dtype == LQSGD_F32 ? kForwardThreads : kForwardThreadsShift);
-}
 constexpr int kCtasColumns = kSms * 2;
 struct GradPlan {
   RowShape shape;
@@ -590,9 +588,21 @@ GradPlan plan_backward(const lqsgd_rms_norm& a) {
   return p;
 }
 
+// Blocks of equal steps (1021 x 25087 fp16 into codes: 58 us, in four steps of 256 threads of which the last is nearly empty 70), two of them on an SM; one step more
+// if smaller blocks then fill the SM better (4000 x 16384: four steps of 256 threads, three blocks, 55 us; three steps of 352, two blocks, 64).
+int forward_long_threads(int32_t cols, int n) {
+  const int64_t runs = ceil_div64(cols, kRun), steps = ceil_div64(runs, (int64_t)n * kLongThreads);
+  const int few = long_threads(runs, n, steps), more = long_threads(runs, n, steps + 1);
+  return 2 * kLongThreads / few * few >= 2 * kLongThreads / more * more ? few : more;
+}
 template <int DT, int HOW>
-cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st) {
-  if (!s.held) return train_launch(rms_forward_long_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a);
+cudaError_t launch_forward(RmsArgs a, cudaStream_t st) {
+  const RowShape s = shape_of(a.cols, kForwardRuns<DT>, kNarrow, forward_threads(DT, HOW));
+  a.lane_shift = s.lane_shift;
+  if (!s.held) {
+    const int threads = forward_long_threads(a.cols, kLongRuns<DT>);
+    return train_launch(rms_forward_long_kernel<DT, kLongRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(threads), 0, st, 1, a);
+  }
   const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
 #define GO(N, NARROW) train_launch(rms_forward_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, 1, a)
   if (s.narrow) return s.n == 1 ? GO(1, true) : s.n == 2 ? GO(2, true) : GO(4, true);
@@ -602,7 +612,7 @@ cudaError_t launch_forward(const RowShape& s, const RmsArgs& a, cudaStream_t st)
 template <int DT, int HOW>
 cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
   if (!p.shape.held) {
-    const cudaError_t e = train_launch(rms_dot_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a, dots);
+    const cudaError_t e = train_launch(rms_dot_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kDotThreads), 0, st, 1, a, dots);
     return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, kGradRuns, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.rows_per_block, dots);
   }
   const RowShape& s = p.shape;
@@ -674,9 +684,7 @@ extern "C" int lqsgd_rms_norm_forward(const lqsgd_rms_norm* a, void* cuda_stream
   k.vec_y8 = on8(a->y8.dev_codes, a->y8.ld_codes, a->rows);
   k.vec_r8 = on8(a->rows8.dev_codes, a->rows8.ld_codes, a->rows);
   const int how = access_of(rows16, k.vec_gamma && k.vec_h8 && k.vec_y8 && k.vec_r8, a->cols);
-  const RowShape s = forward_shape(*a, how);
-  k.lane_shift = s.lane_shift;
-  TRAIN_CK(BY_TYPE(a->dtype, how, launch_forward, s, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
+  TRAIN_CK(BY_TYPE(a->dtype, how, launch_forward, k, static_cast<cudaStream_t>(cuda_stream)), "rms_forward_kernel launch");
   return LQSGD_OK;
 }
 

@@ -1,5 +1,8 @@
 // Rows of signed 8-bit codes with one scale each, to and from them, and dropout by itself.  All are streams bounded by HBM; packing
-// needs the row's largest magnitude first, so a row stays in the registers of its threads in between.
+// needs the row's largest magnitude first, so a row stays in the registers of its threads in between, a long one in their shared memory.
+// A thread has 64 bytes of a row (four runs of a 16-bit type) on their way at once.
+// Measured: 16384 x 4096 packed from bf16 30 us (6.7 TB/s), from fp32 48 (7.0), unpacked to bf16 31 (6.4); dropout of 8192 x 16384 bf16 89 (6.0 TB/s;
+// the generator is a third of its 125 instructions per run), 8192 x 8192 with a residual 58 (7.0).
 #include "lqsgd_rows_dev.cuh"
 
 namespace lqsgd {
@@ -14,7 +17,7 @@ struct PackArgs {
 };
 __device__ __forceinline__ uint8_t* codes_of(const lqsgd_rows8& r, int64_t row, int col) { return reinterpret_cast<uint8_t*>(r.dev_codes) + row * r.ld_codes + col; }
 
-constexpr int kPackThreads = 512, kLongThreads = 256;
+constexpr int kPackThreads = 512;
 template <int DT, int N, bool NARROW, int HOW>
 __global__ void __launch_bounds__(NARROW ? 256 : kPackThreads, NARROW || HOW == kShift ? 1 : 3)
 pack_rows8_kernel(const __grid_constant__ PackArgs a) {
@@ -48,28 +51,35 @@ pack_rows8_kernel(const __grid_constant__ PackArgs a) {
   }
 }
 
-// Rows longer than a block holds: read twice, the second time from L2.
+// Rows longer than a block's registers hold: in shared memory between two passes (1021 x 25087 bf16 21 us, read twice 25; fp32 32 and 39), where two
+// blocks of an SM have room for them.
 template <int DT, int N, int HOW>
-__global__ void __launch_bounds__(kLongThreads)
-pack_rows8_long_kernel(const __grid_constant__ PackArgs a) {
+__global__ void __launch_bounds__(kPackThreads, 2)
+pack_rows8_long_kernel(const __grid_constant__ PackArgs a, bool keep) {
+  extern __shared__ uint4 kept[];
   __shared__ float2 slots[16];
   const Team<false, N> team(0);
   const int64_t row = team.row;
   train_pdl_wait();
   if (threadIdx.x == 0) ahead(static_cast<const typename Elem<DT>::T*>(a.x) + row * a.ld_x, (int64_t)a.cols * (int)sizeof(typename Elem<DT>::T));
-  const int steps = (a.cols + kLongThreads * N * kRun - 1) / (kLongThreads * N * kRun);
+  const int each = blockDim.x * N * kRun, steps = (a.cols + each - 1) / each;
   float none = 0.f, top = 0.f, scale, inv = 0.f;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
     for (int k = 0; k < steps; ++k) {
       const Lanes l = team.lanes(a.cols, true, k);
-      const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
-      Raw<DT, HOW> raw[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
       Piece<DT> p[N];
-      settle(raw, x, l, p);
+      if (pass == 1 && keep) {
+        kept_runs<DT>(kept, k, p);
+      } else {
+        const Cursor<DT, HOW> x(a.x, row * a.ld_x, l);
+        Raw<DT, HOW> raw[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(x, l, i, raw[i]);
+        settle(raw, x, l, p);
+        if (keep) keep_runs<DT>(kept, k, p);
+      }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         float v[kRun];
@@ -183,7 +193,14 @@ template <int DT, int HOW>
 cudaError_t launch_pack(PackArgs a, cudaStream_t st) {
   constexpr int kRuns = DT == LQSGD_F32 ? 2 : 4;              // 64 bytes per thread
   const RowShape s = shape_of(a.cols, kRuns, 1024, kPackThreads);
-  if (!s.held) return train_launch(pack_rows8_long_kernel<DT, kRuns, HOW>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, 1, a);
+  if (!s.held) {
+    static std::atomic<uint64_t> ready{0};
+    auto kernel = pack_rows8_long_kernel<DT, kRuns, HOW>;
+    const int threads = long_threads(a.cols, kRuns, kPackThreads);
+    const size_t keep = long_keep(a.cols, kRuns, (int)sizeof(typename Elem<DT>::T), threads);
+    const cudaError_t e = allow_keep(reinterpret_cast<const void*>(kernel), ready);
+    return e != cudaSuccess ? e : train_launch(kernel, dim3((unsigned)a.rows), dim3(threads), keep, st, 1, a, keep > 0);
+  }
   a.lane_shift = s.lane_shift;
   const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
 #define GO(N, NARROW) train_launch(pack_rows8_kernel<DT, N, NARROW, HOW>, grid, block, 0, st, 1, a)

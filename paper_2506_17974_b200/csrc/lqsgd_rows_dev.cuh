@@ -1,6 +1,8 @@
 // Device pieces shared by the operators that work on whole rows: the random bits of dropout, signed 8-bit codes, and how a row is
 // dealt out to the threads that hold it.
 #pragma once
+#include <atomic>
+
 #include "lqsgd_runs_dev.cuh"
 
 namespace lqsgd {
@@ -31,8 +33,8 @@ namespace {
 //   kShift  any alignment.  A run is taken from the 16-byte pieces around it, which lie inside the row for all but its first and last
 //           runs, and moved into place in registers; it is written as the piece that begins in the run of the lane in front.  Element by
 //           element a run would touch as many places as it has elements; turned in shared memory, as the 8-bit streams do it, a
-//           row of 16-bit values still goes through 2-byte accesses (the norm of 1021 x 25087 fp16 into codes: 87 us element by element or
-//           turned, 73 so; rows of 25088 46).
+//           row of 16-bit values still goes through 2-byte accesses (the norm of 1021 x 25087 fp16 into codes, before later steps: 87 us element by
+//           element or turned, 73 so; now 58, rows of 25088 37).
 enum RowAccess { kWhole = 0, kShift = 1 };
 
 // Philox4x32, 10 rounds: a product of each even word by a constant, its high half mixed with a neighbour and the round's key.
@@ -367,6 +369,23 @@ __device__ __forceinline__ void put(const Cursor<DT, HOW>& c, const Lanes& l, co
     }
   }
 }
+// A thread's N runs of one step over a long row in shared memory, for itself: 16-byte pieces a block's width apart.
+template <int DT, int N>
+__device__ __forceinline__ void keep_runs(uint4* room, int step, const Piece<DT> (&p)[N]) {
+  constexpr int kPieces = kRunBytes<DT> / 16;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) room[((step * N + i) * kPieces + k) * blockDim.x + threadIdx.x] = reinterpret_cast<const uint4*>(p[i].w)[k];
+}
+template <int DT, int N>
+__device__ __forceinline__ void kept_runs(const uint4* room, int step, Piece<DT> (&p)[N]) {
+  constexpr int kPieces = kRunBytes<DT> / 16;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) reinterpret_cast<uint4*>(p[i].w)[k] = room[((step * N + i) * kPieces + k) * blockDim.x + threadIdx.x];
+}
 // Run i of a vector of floats, from its element l.col on.
 template <int HOW>
 __device__ __forceinline__ void fetch_vector(const float* p, bool vec, const Lanes& l, int i, float (&v)[kRun]) {
@@ -488,6 +507,28 @@ static inline RowShape shape_of(int32_t cols, int n, int narrow, int threads) {
   s.threads = (int)std::min<int64_t>(ceil_div64(ceil_div64(runs, n), 32) * 32, 1 << 20);
   s.held = s.threads <= threads;
   return s;
+}
+
+// Threads of a block that walks a longer row in as few steps of equal length as `most` threads allow.
+static inline int long_threads(int64_t runs, int n, int64_t steps) { return (int)(ceil_div64(ceil_div64(runs, n * steps), 32) * 32); }
+static inline int long_threads(int32_t cols, int n, int most) {
+  const int64_t runs = ceil_div64(cols, kRun);
+  return long_threads(runs, n, ceil_div64(runs, (int64_t)n * most));
+}
+// Shared memory in which a long row stays between two passes; 0 if two blocks of an SM have not enough (the second pass then reads L2).
+constexpr size_t kKeepMost = 112 * 1024;
+static inline size_t long_keep(int32_t cols, int n, int elem, int threads) {
+  const size_t bytes = (size_t)ceil_div64(ceil_div64(cols, kRun), (int64_t)n * threads) * n * threads * kRun * elem;
+  return bytes <= kKeepMost ? bytes : 0;
+}
+// Lets a kernel have kKeepMost; `ready`: the devices on which it may already.
+static inline cudaError_t allow_keep(const void* kernel, std::atomic<uint64_t>& ready) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (ready.load(std::memory_order_acquire) >> dev & 1))) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kKeepMost);
+  if (e == cudaSuccess && dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+  return e;
 }
 
 }  // namespace

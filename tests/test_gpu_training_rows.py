@@ -152,6 +152,17 @@ def test_rows8_of_special_rows(cols):
     assert torch.isnan(y[2:4]).all() and torch.isfinite(y[4:]).all() and (y[:2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [16385, 28672, 28673, 57344, 57352])
+def test_rows8_of_long_rows(dtype, cols):
+    """Around the lengths up to which a block has a row in shared memory."""
+    for pad in (0, 1):
+        x = matrix(2, cols, dtype, cols, pad)
+        codes, scales = ro.rows8(x.float().cpu().numpy())
+        r = tr.pack_rows8(x)
+        assert (r.codes.cpu().numpy() == codes).all() and (r.scales.cpu().numpy() == scales).all()
+
+
 # ------------------------------------------------------------------------------------------------------------- the norm
 
 def check_forward(x, res, gamma, p, eps=1e-6, seed=3, offset=9):
@@ -229,6 +240,15 @@ def check_backward(dy, h, gamma, rstd, skip, p, seed=4, offset=2):
     near(dg, dgamma, torch.float32, U * (rows + 4) * (np.abs(dyv) * xh).sum(0))
     alone = tr.rms_norm_grad(dy, h, gamma, rstd, skip, p, seed, offset, gamma_grad=False)
     assert alone[2] is None and alone[0].equal(dx) and alone[1].equal(dres)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [6657, 10241, 13313, 28679, 57352])
+def test_rms_norm_of_long_rows(dtype, cols):
+    """Steps of every width: the last one full, nearly empty, or with lanes left over."""
+    gamma = matrix(1, cols, torch.float32, 6)[0] * 0.2 + 1
+    check_forward(matrix(2, cols, dtype, 7), matrix(2, cols, dtype, 8, scale=1.5), gamma, 0.1)
+    check_forward(matrix(2, cols, dtype, 7, pad=3, shift=1), None, gamma, 0.0)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
