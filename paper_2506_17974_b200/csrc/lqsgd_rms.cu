@@ -34,7 +34,7 @@ constexpr int kNarrow = 1024, kForwardThreads = 416;
 template <int DT> constexpr int kForwardRuns = DT == LQSGD_F32 ? 2 : 4;
 template <int DT> constexpr int kLongRuns = DT == LQSGD_F32 ? 1 : 2;     // rows in steps: twice the threads in their place (four runs, balanced: 75 us to 58)
 constexpr int forward_threads(int dtype, int how) { return how == kWhole || dtype == LQSGD_F32 ? kForwardThreads : 320; }
-constexpr int kLongThreads = 448, kDotThreads = 256, kGradThreads = 512, kGradRuns = 2;
+constexpr int kLongThreads = 448, kGradThreads = 512, kGradRuns = 2;
 
 // What a thread touches of one row of the forward call.
 template <int DT, int HOW>
@@ -467,7 +467,7 @@ struct GradRuns {
   }
 };
 template <int DT, int N, int HOW>
-__global__ void __launch_bounds__(kDotThreads)
+__global__ void __launch_bounds__(kLongThreads, 2)
 rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   __shared__ float2 slots[16];
   const Team<false, N> team(0);
@@ -475,7 +475,7 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   if (threadIdx.x == 0) rows_ahead<DT>(a, team.row, false);
   const float rstd = a.rstd[team.row];
   float sum[2] = {0.f, 0.f}, top = 0.f;
-  const int steps = (a.cols + kDotThreads * N * kRun - 1) / (kDotThreads * N * kRun);
+  const int each = blockDim.x * N * kRun, steps = (a.cols + each - 1) / each;
 #pragma unroll 1
   for (int k = 0; k < steps; ++k) {
     const GradRuns<DT, N, HOW> p(a, team.row, team.lanes(a.cols, true, k), false);
@@ -590,7 +590,7 @@ GradPlan plan_backward(const lqsgd_rms_norm& a) {
 
 // Blocks of equal steps (1021 x 25087 fp16 into codes: 58 us, in four steps of 256 threads of which the last is nearly empty 70), two of them on an SM; one step more
 // if smaller blocks then fill the SM better (4000 x 16384: four steps of 256 threads, three blocks, 55 us; three steps of 352, two blocks, 64).
-int forward_long_threads(int32_t cols, int n) {
+int walk_threads(int32_t cols, int n) {
   const int64_t runs = ceil_div64(cols, kRun), steps = ceil_div64(runs, (int64_t)n * kLongThreads);
   const int few = long_threads(runs, n, steps), more = long_threads(runs, n, steps + 1);
   return 2 * kLongThreads / few * few >= 2 * kLongThreads / more * more ? few : more;
@@ -600,7 +600,7 @@ cudaError_t launch_forward(RmsArgs a, cudaStream_t st) {
   const RowShape s = shape_of(a.cols, kForwardRuns<DT>, kNarrow, forward_threads(DT, HOW));
   a.lane_shift = s.lane_shift;
   if (!s.held) {
-    const int threads = forward_long_threads(a.cols, kLongRuns<DT>);
+    const int threads = walk_threads(a.cols, kLongRuns<DT>);
     return train_launch(rms_forward_long_kernel<DT, kLongRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(threads), 0, st, 1, a);
   }
   const dim3 grid((unsigned)ceil_div64(a.rows, s.teams)), block(s.threads);
@@ -612,7 +612,8 @@ cudaError_t launch_forward(RmsArgs a, cudaStream_t st) {
 template <int DT, int HOW>
 cudaError_t launch_backward(const GradPlan& p, const RmsArgs& a, float* dots, cudaStream_t st) {
   if (!p.shape.held) {
-    const cudaError_t e = train_launch(rms_dot_kernel<DT, kForwardRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(kDotThreads), 0, st, 1, a, dots);
+    const int threads = walk_threads(a.cols, kLongRuns<DT>);
+    const cudaError_t e = train_launch(rms_dot_kernel<DT, kLongRuns<DT>, HOW>, dim3((unsigned)a.rows), dim3(threads), 0, st, 1, a, dots);
     return e != cudaSuccess ? e : train_launch(rms_columns_kernel<DT, kGradRuns, HOW>, p.grid, dim3(kThreads), 0, st, 1, a, p.rows_per_block, dots);
   }
   const RowShape& s = p.shape;
