@@ -496,25 +496,26 @@ rms_dot_kernel(const __grid_constant__ RmsArgs a, float* dots) {
   team.template join<false>(sum[0], top, slots);
   if (team.first()) dots[team.row] = sum[0] * a.per_col;
 }
-// A block's warps take the same strip of N runs per lane of different rows; blockIdx.x = strip, blockIdx.y = block of rows.
+// A warp walks down N runs per lane; a block's warps stand side by side, so that a row's piece is several kilobytes (each of eight rows of their
+// own: 1021 x 40000 118 us, so 103; 25088, whose last strip is ragged, 69 and 72).  blockIdx.x = strip, blockIdx.y = block of rows.
 template <int DT, int N, int HOW>
 __global__ void __launch_bounds__(kThreads, 2)
 rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, const float* dots) {
-  __shared__ float sums[kWarps][kWarpCols];
   __shared__ uint32_t room[kDropRoom];
   constexpr int kSize = (int)sizeof(typename Elem<DT>::T);
   train_pdl_wait();
   open_drop(a.drop, room);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, strip = (int)blockIdx.x * N * kWarpCols, wide = min(N * kWarpCols, a.cols - strip);
+  const int lane = threadIdx.x & 31, strip = (int)(blockIdx.x * kWarps + (threadIdx.x >> 5)) * N * kWarpCols, wide = min(N * kWarpCols, a.cols - strip);
+  if (wide <= 0) return;
   const Lanes l = {strip + lane * kRun, a.cols - strip - lane * kRun, lane, 32, true};
   float acc[N][kRun];
 #pragma unroll
   for (int i = 0; i < N; ++i) clear_run(acc[i]);
   const int64_t end = min(a.rows, (int64_t)(blockIdx.y + 1) * rows_per_block);
 #pragma unroll 1
-  for (int64_t row = blockIdx.y * rows_per_block + warp; row < end; row += kWarps) {
-    if (lane == 0 && row + kWarps < end) {
-      const int64_t next = row + kWarps;
+  for (int64_t row = blockIdx.y * rows_per_block; row < end; ++row) {
+    if (lane == 0 && row + 1 < end) {
+      const int64_t next = row + 1;
       ahead(static_cast<const char*>(a.dy) + (next * a.ld_dy + strip) * kSize, wide * kSize);
       if (a.skip) ahead(static_cast<const char*>(a.skip) + (next * a.ld_skip + strip) * kSize, wide * kSize);
       if (a.h8.dev_codes) ahead(a.h8.dev_codes + next * a.h8.ld_codes + strip, wide);
@@ -544,28 +545,18 @@ rms_columns_kernel(const __grid_constant__ RmsArgs a, int64_t rows_per_block, co
   }
   if (!a.partial) return;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __syncthreads();
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) sums[warp][lane * kRun + j] = acc[i][j];
-    __syncthreads();
-    const int c = threadIdx.x, col = strip + i * kWarpCols + c;
-    if (col < a.cols) {
-      float t = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) t += sums[w][c];
-      a.partial[(size_t)blockIdx.y * a.cols + col] = t;
-    }
-  }
+    for (int j = 0; j < kRun; ++j)
+      if (j < l.have(i)) a.partial[(size_t)blockIdx.y * a.cols + l.col + i * kWarpCols + j] = acc[i][j];
 }
 
 // ---- choice of kernel
 constexpr int kSms = 148;
-constexpr int kCtasColumns = kSms * 2;
 struct GradPlan {
   RowShape shape;
   dim3 grid;
-  int64_t rows_per_block;                    // of the kernels for long rows
+  int64_t rows_per_block;                    // of the kernel for long rows' columns
   int blocks;                                // of the sums over rows
   size_t off_partial, bytes;
 };
@@ -573,9 +564,9 @@ GradPlan plan_backward(const lqsgd_rms_norm& a) {
   GradPlan p = {};
   p.shape = shape_of(a.cols, kGradRuns, 512, kGradThreads);
   if (!p.shape.held) {
-    // blocks that fill the card, as many of them below one another as the strips of a row leave; a warp takes two rows at least
-    const int64_t strips = ceil_div64(a.cols, kGradRuns * kWarpCols);
-    const int64_t below = std::max<int64_t>(1, std::min<int64_t>({kCtasColumns / strips, ceil_div64(a.rows, 2 * kWarps), 65535}));
+    // blocks that fill the card, as many of them below one another as the strips of a row leave, of two rows at least
+    const int64_t strips = ceil_div64(a.cols, kWarps * kGradRuns * kWarpCols);
+    const int64_t below = std::max<int64_t>(1, std::min<int64_t>(kSms * 2 / strips, ceil_div64(a.rows, 2)));
     p.rows_per_block = ceil_div64(a.rows, below);
     p.grid = dim3((unsigned)strips, (unsigned)ceil_div64(a.rows, p.rows_per_block));
     p.blocks = (int)p.grid.y;
