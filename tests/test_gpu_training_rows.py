@@ -458,6 +458,7 @@ def test_refusals():
         with pytest.raises(B.LqsgdError) as e:
             call()
         assert e.value.code == B.ERR_INVALID_ARG
+        del e                                                 # with its traceback it would keep this frame, and the tensors, until a collection
 
 
 def test_other_stream_and_capture():
