@@ -261,7 +261,8 @@ __device__ __forceinline__ void act_run(int act, float (&v)[N]) {
 // The same two values at a time: where a product is over sooner than its epilogue.
 __device__ __forceinline__ void gelu2(float& z0, float& z1) {
   float t0, t1, r0, r1, g0, g1;
-  fma2(t0, t1, fabsf(z0), fabsf(z1), 0.30476302f, 0.30476302f, 1.f, 1.f);
+  const float n0 = -fabsf(fminf(z0, 3.402823466e38f)), n1 = -fabsf(fminf(z1, 3.402823466e38f));
+  fma2(t0, t1, n0, n1, -0.30476302f, -0.30476302f, 1.f, 1.f);
   t0 = rcp_approx(t0);
   t1 = rcp_approx(t1);
   fma2(r0, r1, t0, t1, 0.036738604f, 0.036738604f, -0.15354006f, -0.15354006f);
@@ -276,9 +277,10 @@ __device__ __forceinline__ void gelu2(float& z0, float& z1) {
   mul2(g0, g1, g0, g1, -0.72134752f, -0.72134752f);
   g0 = exp2_approx(g0);
   g1 = exp2_approx(g1);
-  // z (z < 0 ? q : 1 - q), q = gauss r: max(z, 0) - |z| q (q is 0 from 14 on, and infinity counts as the largest value there)
+  // z (z < 0 ? q : 1 - q), q = gauss r: max(z, 0) - |z| q.  q is 0 from 14 on; plus infinity counts as the largest value there, minus infinity
+  // does not: infinity times 0, NaN, as act_value() has it.
   mul2(r0, r1, r0, r1, g0, g1);
-  fma2(z0, z1, -fminf(fabsf(z0), 3.402823466e38f), -fminf(fabsf(z1), 3.402823466e38f), r0, r1, act_value<LQSGD_ACT_RELU>(z0), act_value<LQSGD_ACT_RELU>(z1));
+  fma2(z0, z1, n0, n1, r0, r1, act_value<LQSGD_ACT_RELU>(z0), act_value<LQSGD_ACT_RELU>(z1));
 }
 __device__ __forceinline__ void silu2(float& z0, float& z1) {
   float e0, e1;
