@@ -610,7 +610,8 @@ int lqsgd_rms_norm_backward(const lqsgd_rms_norm* host_args, void* cuda_stream);
 /* A linear layer's forward product in 8-bit integers, x of shape rows x in and w of shape out x in as rows of signed codes (a scale
  * per token, a scale per output channel):
  *   y = act((sum over k of xc wc) sx sw + bias) + residual,  z8 = pack8(the value in front of act),  y8 = pack8(y as stored)
- * on the tensor cores.  The sum is exact in 32 bits (|code| <= 128 and in <= 131071); the scales are applied in fp32, sx first. */
+ * on the tensor cores.  The sum is exact in 32 bits (|code| <= 128 and in <= 131071); it is rounded to fp32, so is its product with sx,
+ * and sw and the bias come with one rounding more.  A row's results do not depend on the call's other rows, in any bit. */
 typedef struct lqsgd_linear_rows8 {
   uint32_t struct_size; /* sizeof(lqsgd_linear_rows8) */
   int32_t dtype;        /* of residual and out: LQSGD_BF16 or LQSGD_F16 */

@@ -423,10 +423,9 @@ rows8_few_kernel(const int8_t* __restrict__ x, int64_t ld_x, const int8_t* __res
     for (int i = 0; i < R * kFewChannels; ++i)
       if (i == lane) sum = acc[i / kFewChannels][i % kFewChannels];
   }
-  float v[1] = {(float)sum * __ldg(e.row_scale + r) * __ldg(e.col_scale + channel)};
-  if (e.bias) v[0] += __ldg(e.bias + channel);
-  act_run(e.act, v);
-  if (e.residual) v[0] += unpack1(e.dtype, static_cast<const uint16_t*>(e.residual)[r * e.ld_res + channel]);
+  float v[2] = {finish_sum(sum, __ldg(e.row_scale + r), __ldg(e.col_scale + channel), e.bias ? __ldg(e.bias + channel) : 0.f), 0.f};
+  act_pairs(e.act, v);
+  if (e.residual) v[0] = add_residual<kInt8>(v[0], unpack1(e.dtype, static_cast<const uint16_t*>(e.residual)[r * e.ld_res + channel]));
   static_cast<uint16_t*>(e.out)[r * e.ld_out + channel] = pack1(e.dtype, v[0]);
 }
 // Whether the call takes that way: rows on 16 bytes, and no copies in 8 bits (their groups of 32 channels span warps).

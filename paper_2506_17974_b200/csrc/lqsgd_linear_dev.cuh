@@ -314,17 +314,20 @@ __device__ __forceinline__ void finish_ragged_f32(const LinEpilogue& e, int64_t 
   }
   __syncwarp();
 }
-// An integer sum as the value it stands for.
-__device__ __forceinline__ float scaled_sum(float bits, float row_scale, float col_scale) {
-  return (float)__float_as_int(bits) * row_scale * col_scale;
+// Integer sums are exact, and every way to deal a product out rounds what follows alike, so that a row's bits do not depend on the other rows of a
+// call: the integer to fp32, its product with the row's scale, one rounding for the channel's scale and the bias, the activation as
+// act_pairs() has it, the residual's addition.  Roundings that the compiler may merge are spelled out.
+__device__ __forceinline__ float finish_sum(int sum, float row_scale, float col_scale, float bias) {
+  return __fmaf_rn(__fmul_rn((float)sum, row_scale), col_scale, bias);
 }
+template <int KIND> __device__ __forceinline__ float add_residual(float v, float r) { return KIND == kInt8 ? __fadd_rn(v, r) : v + r; }
 // a + b of two sums: of integers where KIND has them.
 template <int KIND>
 __device__ __forceinline__ float add_sums(float a, float b) {
   return KIND == kInt8 ? __int_as_float(__float_as_int(a) + __float_as_int(b)) : a + b;
 }
 // Epilogue of a 32 x 32 piece of a layer's output.
-// bias: these columns' values in shared memory (zeros past the matrix).
+// bias: these columns' values in shared memory (zeros past the matrix).  Sums of codes come with their scales and the bias in them.
 // Products of codes take half the time of those in 16 bits, so that their epilogue is what a tile waits for: it goes two values at a time.
 template <int KIND>
 __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, int col, bool on, float (&v)[32], const float* bias, float* scratch) {
@@ -355,16 +358,11 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
     }
     __syncwarp();
   }
-  if (e.bias) {
+  if (KIND == kHalf && e.bias) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float4 b = *(reinterpret_cast<const float4*>(bias) + i);
-      if (KIND == kInt8) {
-        add2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], b.x, b.y);
-        add2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], b.z, b.w);
-      } else {
-        v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
-      }
+      v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
     }
   }
   if (have < 32) {
@@ -383,8 +381,8 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float2 f = unpack2(e.dtype, w[j]);
-        v[16 * i + 2 * j] += f.x;
-        v[16 * i + 2 * j + 1] += f.y;
+        v[16 * i + 2 * j] = add_residual<KIND>(v[16 * i + 2 * j], f.x);
+        v[16 * i + 2 * j + 1] = add_residual<KIND>(v[16 * i + 2 * j + 1], f.y);
       }
     }
   }
@@ -392,8 +390,8 @@ __device__ __forceinline__ void finish_rows(const LinEpilogue& e, int64_t row0, 
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float2 f = unpack2(e.dtype, *reinterpret_cast<const uint32_t*>(half + lane * kHalfPitch + 2 * j));
-      if (2 * j < have) v[2 * j] += f.x;
-      if (2 * j + 1 < have) v[2 * j + 1] += f.y;
+      if (2 * j < have) v[2 * j] = add_residual<KIND>(v[2 * j], f.x);
+      if (2 * j + 1 < have) v[2 * j + 1] = add_residual<KIND>(v[2 * j + 1], f.y);
     }
     __syncwarp();
   }
@@ -480,22 +478,24 @@ __device__ __forceinline__ void finish_quad(const LinEpilogue& e, int64_t row, i
   const float row_scale = KIND == kInt8 ? __ldg(e.row_scale + row) : 1.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (KIND == kInt8 && i < have) v[i] = scaled_sum(v[i], row_scale, __ldg(e.col_scale + col + i));
     if (i >= have) v[i] = 0.f;
+    else if (KIND == kInt8) v[i] = finish_sum(__float_as_int(v[i]), row_scale, __ldg(e.col_scale + col + i), e.bias ? __ldg(e.bias + col + i) : 0.f);
     else if (e.bias) v[i] += __ldg(e.bias + col + i);
   }
   if (e.z8.dev_codes) put_packed_quad(e.z8, row, col, have, v);
-  act_run(e.act, v);
+  if (KIND == kInt8) act_pairs(e.act, v);
+  else act_run(e.act, v);
   if (e.residual && have > 0) {
     const uint16_t* r = static_cast<const uint16_t*>(e.residual) + row * e.ld_res + col;
     if (have == 4 && e.vec_res) {
       const uint2 w = *reinterpret_cast<const uint2*>(r);
       const float2 f = unpack2(e.dtype, w.x), g = unpack2(e.dtype, w.y);
-      v[0] += f.x; v[1] += f.y; v[2] += g.x; v[3] += g.y;
+      v[0] = add_residual<KIND>(v[0], f.x); v[1] = add_residual<KIND>(v[1], f.y);
+      v[2] = add_residual<KIND>(v[2], g.x); v[3] = add_residual<KIND>(v[3], g.y);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (i < have) v[i] += unpack1(e.dtype, r[i]);
+        if (i < have) v[i] = add_residual<KIND>(v[i], unpack1(e.dtype, r[i]));
     }
   }
   const uint2 w = make_uint2(pack2(e.dtype, v[0], v[1]), pack2(e.dtype, v[2], v[3]));
@@ -908,14 +908,14 @@ linear_kernel(const __grid_constant__ LinProblem p) {
           } else if (n0 + c0 + c < p.N && m - lane < p.M) {
             if constexpr (KIND == kInt8) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float4 t = *(reinterpret_cast<const float4*>(col_scale + c) + i);
+              for (int i = 0; i < 8; ++i) {                                  // finish_sum(), two at a time
+                const float4 t = *(reinterpret_cast<const float4*>(col_scale + c) + i), b = *(reinterpret_cast<const float4*>(bias + c) + i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[4 * i + j] = (float)__float_as_int(v[4 * i + j]);
                 mul2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], row_scale, row_scale);
                 mul2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], row_scale, row_scale);
-                mul2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], t.x, t.y);
-                mul2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], t.z, t.w);
+                fma2(v[4 * i], v[4 * i + 1], v[4 * i], v[4 * i + 1], t.x, t.y, b.x, b.y);
+                fma2(v[4 * i + 2], v[4 * i + 3], v[4 * i + 2], v[4 * i + 3], t.z, t.w, b.z, b.w);
               }
             }
             finish_rows<KIND>(p.ep, m - lane, n0 + c0 + c, m < p.M, v, bias + c, scratch);

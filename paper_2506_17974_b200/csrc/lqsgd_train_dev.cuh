@@ -258,7 +258,8 @@ __device__ __forceinline__ void act_run(int act, float (&v)[N]) {
     for (int i = 0; i < N; ++i) v[i] = act_value<LQSGD_ACT_SILU>(v[i]);
   }
 }
-// The same two values at a time: where a product is over sooner than its epilogue.
+// The same two values at a time: where a product is over sooner than its epilogue.  Every operation's rounding is its own, so that a value comes out
+// the same wherever these are used.
 __device__ __forceinline__ void gelu2(float& z0, float& z1) {
   float t0, t1, r0, r1, g0, g1;
   const float n0 = -fabsf(fminf(z0, 3.402823466e38f)), n1 = -fabsf(fminf(z1, 3.402823466e38f));
