@@ -933,6 +933,8 @@ class _LinearRows8Layer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, act, rows8, weight8, recording):
         _dtype(x, "x", True)
+        if residual is not None and residual.dtype != x.dtype:
+            raise ValueError(f"residual must have x's type {x.dtype}, not {residual.dtype}")
         for p, t, what in ((rows8, x, "rows8"), (weight8, weight, "weight8")):
             if p is not None and p.shape != t.shape:
                 raise ValueError(f"{what} must be the Rows8 form of {tuple(t.shape)} values, not of {tuple(p.shape)}")
