@@ -94,11 +94,12 @@ struct ForwardRow {
       top = largest(top, g);
     }
   }
-  // the row's figures, written by one of its threads
+  // The row's figures, written by one of its threads.  A product h gamma is off by up to 2^-150 at the range's lower end, which a large rstd (no
+  // eps, small rows) carries up: with twice the smallest number on top of the largest one no code passes 127.
   __device__ __forceinline__ void figures(bool mine, float sum, float top, float& rstd, float& inv) const {
     rstd = rsqrtf(fmaf(sum, a.per_col, a.eps));
     float scale = 0.f;
-    if (a.r8.dev_codes) row_scale(top * rstd, scale, inv);
+    if (a.r8.dev_codes) row_scale((top + 2.80259693e-45f) * rstd, scale, inv);
     if (mine && l.on) {
       a.rstd[row] = rstd;
       if (a.r8.dev_codes) a.r8.dev_scales[row] = scale;
