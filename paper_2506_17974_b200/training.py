@@ -102,6 +102,8 @@ def _matrix(t: torch.Tensor, what: str, device: int, dtype: Optional[torch.dtype
         raise ValueError(f"{what} must be a CUDA tensor on the device of the call's other tensors")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
+    if c >> 31:                       # the library's counts of columns are 32 bits wide: more would arrive as another number
+        raise ValueError(f"{what} must have fewer than 2^31 columns, not {c}")
     if (rows >= 0 and r != rows) or (cols >= 0 and c != cols):
         raise ValueError(f"{what} must have {rows if rows >= 0 else 'any number of'} rows and {cols if cols >= 0 else 'any number of'} columns, "
                          f"not {tuple(shape)}")

@@ -1,0 +1,31 @@
+"""Arguments on their way into the library, without a GPU: sizes that would not fit."""
+import pytest
+import torch
+
+from paper_2506_17974_b200 import training as tr
+
+
+class Matrix:
+    """What the checks ask of a tensor, of any size."""
+    dtype = torch.bfloat16
+
+    def __init__(self, rows, cols):
+        self.shape = rows, cols
+
+    def stride(self):
+        return self.shape[1], 1
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return 0x7f0000000000
+
+
+@pytest.mark.parametrize("cols", [1 << 31, (1 << 32) + 8, 1 << 40])
+def test_more_columns_than_the_library_counts(cols):
+    """32 bits hold the number of columns on the way: 2^32 + 8 of them would arrive as 8, and the call would leave the rest of the row undone."""
+    with pytest.raises(ValueError, match="columns"):
+        tr._matrix(Matrix(1, cols), "x", 0)
+    assert tr._matrix(Matrix(1, (1 << 31) - 1), "x", 0) == (0x7f0000000000, (1 << 31) - 1)
+    assert tr._matrix(Matrix(1 << 33, 4), "x", 0) == (0x7f0000000000, 4)
