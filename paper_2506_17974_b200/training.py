@@ -19,6 +19,7 @@ from __future__ import annotations
 import ctypes as C
 import struct
 import threading
+from operator import index
 from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
@@ -442,11 +443,12 @@ Seed = Union[int, torch.Tensor]
 
 def _drop(p: float, seed: Seed, offset: int, device: int) -> Tuple[float, int, int, int, int]:
     """The members of lqsgd_drop."""
+    offset = index(offset) & 0xFFFFFFFFFFFFFFFF             # index(): numpy's whole numbers are masked as Python's
     if isinstance(seed, torch.Tensor):
         if seed.dtype != torch.int64 or seed.numel() != 2 or not seed.is_contiguous() or seed.get_device() != device:
             raise ValueError("seed must be a whole number or a contiguous int64 tensor of two on the call's device: the seed and what is added to offset")
-        return p, 0, 0, offset & 0xFFFFFFFFFFFFFFFF, seed.data_ptr()
-    return p, 0, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF, 0
+        return p, 0, 0, offset, seed.data_ptr()
+    return p, 0, index(seed) & 0xFFFFFFFFFFFFFFFF, offset, 0
 
 
 def dropout(x: torch.Tensor, p: float, seed: Seed, offset: int = 0, residual: Optional[torch.Tensor] = None,

@@ -1,4 +1,5 @@
-"""Arguments on their way into the library, without a GPU: sizes that would not fit."""
+"""Arguments on their way into the library, without a GPU: numbers of other kinds, and sizes that would not fit."""
+import numpy as np
 import pytest
 import torch
 
@@ -29,3 +30,13 @@ def test_more_columns_than_the_library_counts(cols):
         tr._matrix(Matrix(1, cols), "x", 0)
     assert tr._matrix(Matrix(1, (1 << 31) - 1), "x", 0) == (0x7f0000000000, (1 << 31) - 1)
     assert tr._matrix(Matrix(1 << 33, 4), "x", 0) == (0x7f0000000000, 4)
+
+
+def test_whole_numbers_of_numpy():
+    want = tr._drop(0.25, 5, 3, 0)
+    for kind in (np.int64, np.int32, np.uint32, np.uint64):
+        assert tr._drop(0.25, kind(5), kind(3), 0) == want
+    assert tr._drop(0.25, np.int64(-4), np.int32(-1), 0) == tr._drop(0.25, -4, -1, 0) == (0.25, 0, 2 ** 64 - 4, 2 ** 64 - 1, 0)
+    for seed in (2.5, "5"):
+        with pytest.raises(TypeError):
+            tr._drop(0.25, seed, 0, 0)
