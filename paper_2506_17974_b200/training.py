@@ -118,6 +118,13 @@ def _vector(t: torch.Tensor, what: str, device: int, n: int) -> int:
     return t.data_ptr()
 
 
+def _real(v: float, what: str) -> float:
+    """v, which the library takes as a float32; what that cannot hold would not be packed."""
+    if abs(v) > 3.4028234663852886e38:
+        raise ValueError(f"{what} must be a number of float32's range, not {v}")
+    return v
+
+
 def _elsewhere(device: int) -> bool:
     """Whether `device` is not the current one: the calls then run again under torch.cuda.device."""
     if device < 0:
@@ -443,7 +450,7 @@ Seed = Union[int, torch.Tensor]
 
 def _drop(p: float, seed: Seed, offset: int, device: int) -> Tuple[float, int, int, int, int]:
     """The members of lqsgd_drop."""
-    offset = index(offset) & 0xFFFFFFFFFFFFFFFF             # index(): numpy's whole numbers are masked as Python's
+    p, offset = _real(p, "p"), index(offset) & 0xFFFFFFFFFFFFFFFF             # index(): numpy's whole numbers are masked as Python's
     if isinstance(seed, torch.Tensor):
         if seed.dtype != torch.int64 or seed.numel() != 2 or not seed.is_contiguous() or seed.get_device() != device:
             raise ValueError("seed must be a whole number or a contiguous int64 tensor of two on the call's device: the seed and what is added to offset")
@@ -515,7 +522,7 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: 
     y8 = Packed8.empty(rows, cols, device) if save_y8 else None
     r8 = Rows8.empty(rows, cols, device) if save_rows8 else None
     rc = _library().lqsgd_rms_norm_forward(
-        _RMS.pack(_RMS.size, _dtype(x, "x"), rows, cols, eps, *_drop(p, seed, offset, dev), xp, xl, rp, rl, 0, 0, 0, 0, hp, cols, yp, cols, 0, 0, 0, 0,
+        _RMS.pack(_RMS.size, _dtype(x, "x"), rows, cols, _real(eps, "eps"), *_drop(p, seed, offset, dev), xp, xl, rp, rl, 0, 0, 0, 0, hp, cols, yp, cols, 0, 0, 0, 0,
                   _vector(gamma, "gamma", dev, cols), rstd.data_ptr(), 0, *(h8._fresh() if save_h8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8),
                   *(r8._fresh() if save_rows8 else _NO_ROWS8), 0, 0), _stream(dev))
     if rc:
@@ -748,7 +755,7 @@ def group_norm(x: torch.Tensor, groups: int, gamma: torch.Tensor, beta: torch.Te
     y8 = Packed8.empty(n * hw, c, device) if save_y8 else None
     lib = _library()
     _call(lib.lqsgd_group_norm_forward,
-          (_NORM.size, _dtype(x, "x"), _act(act), groups, n, hw, c, eps, x.data_ptr(), ld, sample, 0, 0, 0, y.data_ptr(), c, hw * c,
+          (_NORM.size, _dtype(x, "x"), _act(act), groups, n, hw, c, _real(eps, "eps"), x.data_ptr(), ld, sample, 0, 0, 0, y.data_ptr(), c, hw * c,
            _vector(gamma, "gamma", dev, c), _vector(beta, "beta", dev, c), mean.data_ptr(), rstd.data_ptr(), 0, 0,
            *(x8._fresh() if save_x8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8)),
           _NORM, lib.lqsgd_group_norm_workspace_bytes, 0, device)

@@ -40,3 +40,13 @@ def test_whole_numbers_of_numpy():
     for seed in (2.5, "5"):
         with pytest.raises(TypeError):
             tr._drop(0.25, seed, 0, 0)
+
+
+@pytest.mark.parametrize("value", [1e39, -1e39, 1e300, float("inf")])
+def test_numbers_past_the_range_of_float32(value):
+    with pytest.raises(ValueError, match="eps"):
+        tr._real(value, "eps")
+    with pytest.raises(ValueError, match="p must"):
+        tr._drop(value, 0, 0, 0)
+    assert tr._real(1e-5, "eps") == 1e-5 and tr._real(3.4028234663852886e38, "eps") > 3e38      # what a float32 holds is the library's to judge
+    assert tr._drop(-0.5, 0, 0, 0)[0] == -0.5 and tr._drop(float("nan"), 0, 0, 0)[0] != tr._drop(float("nan"), 0, 0, 0)[0]
