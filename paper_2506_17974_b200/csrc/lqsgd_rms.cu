@@ -5,9 +5,12 @@
 // read once and stay in registers, as they are stored, while its threads agree on the sum; the steps of a thread's runs interleave
 // without branches between them; and arithmetic goes two values to an instruction.
 // Rows of up to 1024 columns (512 backward) are held by 4 to 32 lanes of a warp, longer ones by a block: forward up to 13312 columns (10240 at any
-// alignment; fp32 6656), backward up to 8192.  Rows beyond are read twice, the second time from L2.
+// alignment; fp32 6656), backward up to 8192.  Rows beyond are read twice: forward by one block, the second time from L2; backward by two kernels, each
+// over the whole matrix, so that what does not fit L2 comes from HBM twice (1021 x 25088 bf16 72 us, of which 28 are its bytes read once).
 // Measured, 8192 x 4096 bf16: norm alone 27 us (5.0 TB/s), with a residual 43 (6.2 TB/s), with dropout, residual and both kept copies 57 (6.0 TB/s);
-// its gradient with skip 58 (4.7 TB/s), with dropout from 8-bit h 80 (3.7 TB/s).
+// its gradient with skip 59 (4.5 TB/s), with dropout from 8-bit h 81 (3.7 TB/s).  Gradients of fp32, two runs
+// a thread as of 16 bits, spill registers: 64 bytes a thread in the aligned block (8192 x 4096 127 us), 540 at any alignment; 244 and 656 where rows
+// are narrow, 228 and 412 in strips.
 #include "lqsgd_rows_dev.cuh"
 
 namespace lqsgd {
@@ -204,8 +207,8 @@ rms_forward_long_kernel(const __grid_constant__ RmsArgs a) {
 // ---- backward
 // A row needs <u xh>, xh = h rstd, and then d = (gamma rstd) dy - (rstd <u xh>) xh + skip.  (With h itself in the place of xh a run takes 8
 // multiplications less, but products of very large or small rows leave fp32's range on the way.)
-// A team walks rows: loads of all runs, the sum, stores; its columns' sums for dgamma stay in registers.  That leaves 16 warps an SM, too few to
-// hide HBM's latency, so one thread asks L2 for the next row meanwhile (8192 x 4096 without dropout, at that step, 75 -> 61 us, fp32 136 -> 122).  h from its
+// A team walks rows: loads of all runs, the sum, stores; its columns' sums for dgamma stay in registers.  That leaves at most 16 warps an SM (a block
+// of 9 to 16 alone from 4097 columns on: 4000 x 4097 bf16 81 us, 4000 x 7168 58, at floors of 18 and 26), too few to hide HBM's latency, so one thread asks L2 for the next row meanwhile (8192 x 4096 without dropout, at that step, 75 -> 61 us, fp32 136 -> 122).  h from its
 // 8-bit form is decoded once, to bf16, in which it is exact.
 // Eight codes as bf16: |128 + m| with the magnitude m below is a bf16 number (0x4300 | m), and (128 + m) 2^e - 128 2^e is m 2^e exactly; the
 // signs are put on top.  For exponents from kQuickByte on 128 2^e leaves the range.
