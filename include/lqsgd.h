@@ -581,7 +581,7 @@ int lqsgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int
  *             dresidual = d,  dx = dropout(d) (the forward call's mask),  dgamma = sum over rows of dy xh
  *             dx, dresidual (the same as dx where p = 0), dgamma each optional, at least one; h from h8 when its codes are set
  * < > is the mean over a row.  Squares and sums are held in fp32: rstd is 0 where a row's squares add up past its range, infinity where they
- * vanish and eps is 0. */
+ * vanish and eps is 0.  Outputs overlap neither inputs nor one another. */
 typedef struct lqsgd_rms_norm {
   uint32_t struct_size;   /* sizeof(lqsgd_rms_norm) */
   int32_t dtype;          /* of all matrices: any lqsgd_dtype */
