@@ -118,9 +118,12 @@ def _vector(t: torch.Tensor, what: str, device: int, n: int) -> int:
     return t.data_ptr()
 
 
+_MOST, _WORD = 3.4028234663852886e38, 0xFFFFFFFFFFFFFFFF
+
+
 def _real(v: float, what: str) -> float:
     """v, which the library takes as a float32; what that cannot hold would not be packed."""
-    if abs(v) > 3.4028234663852886e38:
+    if abs(v) > _MOST:
         raise ValueError(f"{what} must be a number of float32's range, not {v}")
     return v
 
@@ -450,12 +453,16 @@ Seed = Union[int, torch.Tensor]
 
 def _drop(p: float, seed: Seed, offset: int, device: int) -> Tuple[float, int, int, int, int]:
     """The members of lqsgd_drop."""
-    p, offset = _real(p, "p"), index(offset) & 0xFFFFFFFFFFFFFFFF             # index(): numpy's whole numbers are masked as Python's
+    if not -_MOST <= p <= _MOST:
+        _real(p, "p")
     if isinstance(seed, torch.Tensor):
         if seed.dtype != torch.int64 or seed.numel() != 2 or not seed.is_contiguous() or seed.get_device() != device:
             raise ValueError("seed must be a whole number or a contiguous int64 tensor of two on the call's device: the seed and what is added to offset")
-        return p, 0, 0, offset, seed.data_ptr()
-    return p, 0, index(seed) & 0xFFFFFFFFFFFFFFFF, offset, 0
+        return p, 0, 0, index(offset) & _WORD, seed.data_ptr()
+    try:
+        return p, 0, seed & _WORD, offset & _WORD, 0
+    except OverflowError:                                    # numpy's whole numbers
+        return p, 0, index(seed) & _WORD, index(offset) & _WORD, 0
 
 
 def dropout(x: torch.Tensor, p: float, seed: Seed, offset: int = 0, residual: Optional[torch.Tensor] = None,
@@ -522,7 +529,7 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, residual: 
     y8 = Packed8.empty(rows, cols, device) if save_y8 else None
     r8 = Rows8.empty(rows, cols, device) if save_rows8 else None
     rc = _library().lqsgd_rms_norm_forward(
-        _RMS.pack(_RMS.size, _dtype(x, "x"), rows, cols, _real(eps, "eps"), *_drop(p, seed, offset, dev), xp, xl, rp, rl, 0, 0, 0, 0, hp, cols, yp, cols, 0, 0, 0, 0,
+        _RMS.pack(_RMS.size, _dtype(x, "x"), rows, cols, eps if -_MOST <= eps <= _MOST else _real(eps, "eps"), *_drop(p, seed, offset, dev), xp, xl, rp, rl, 0, 0, 0, 0, hp, cols, yp, cols, 0, 0, 0, 0,
                   _vector(gamma, "gamma", dev, cols), rstd.data_ptr(), 0, *(h8._fresh() if save_h8 else _NONE8), *(y8._fresh() if save_y8 else _NONE8),
                   *(r8._fresh() if save_rows8 else _NO_ROWS8), 0, 0), _stream(dev))
     if rc:
