@@ -575,8 +575,8 @@ int lqsgd_dropout(const void* dev_x, int64_t ld_x, const void* dev_residual, int
 /* Root-mean-square norm of rows, with the dropout and the residual's addition in front of it:
  *   forward   h = residual + dropout(x), rounded to dtype;  rstd = 1 / sqrt(<h^2> + eps);  y = h rstd gamma
  *             outputs, each optional: h (needed where there is a residual or p > 0; without them h is x), y, h8 = pack8(h),
- *             y8 = pack8(y as stored), rows8 = pack_rows8(y before its rounding to dtype; max |y| as rstd max |h gamma|, so that a row
- *             where h gamma passes fp32's range counts as not finite)
+ *             y8 = pack8(y as stored), rows8 = pack_rows8(y before its rounding to dtype; max |y| as rstd (max |h gamma| + 2^-148), so
+ *             that a row where h gamma passes fp32's range counts as not finite, and codes stay within 127 where it is subnormal)
  *   backward  u = gamma dy,  xh = h rstd,  d = rstd (u - xh <u xh>) + skip  (skip: the gradient that arrives at h from elsewhere)
  *             dresidual = d,  dx = dropout(d) (the forward call's mask),  dgamma = sum over rows of dy xh
  *             dx, dresidual (the same as dx where p = 0), dgamma each optional, at least one; h from h8 when its codes are set
